@@ -391,6 +391,102 @@ int gala_sweep_agents(float* x, const float* g, float* v, float* snap, const flo
                       long long d_padded, const gala_sweep_item* items, int n_items, const gala_hparams* hp,
                       void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Operators of sequence policies: what a policy with a memory, residual blocks and a large action or token
+ * vocabulary needs beside the networks above.  They stand alone: no context, caller-owned DEVICE arrays, work
+ * enqueued on `stream` (a cudaStream_t, NULL = the legacy default stream) of the current device; no call allocates,
+ * waits or copies to the host, and all of them may be captured into a CUDA graph.  Workspaces come from the caller;
+ * their size follows from the matching gala_*_workspace call, they need no clearing, and two calls whose work may
+ * overlap need two.  Sums, statistics and states are float32 (or wider) whatever the element type; a result is rounded
+ * once, when it is stored.  errbuf (may be NULL) receives a NUL-terminated message of at most errbuf_len bytes on
+ * failure.  GALA_EINVAL: nothing was enqueued.  Outputs must not overlap inputs or one another except where said.
+ * Arrays are addressed with 64-bit offsets; every stride is in elements and at least the extent it spans.  */
+typedef enum { GALA_F32 = 0, GALA_BF16 = 1, GALA_F16 = 2 } gala_dtype;
+
+/* Layer norm over the columns of s = x (+ residual):  y = (s - mean s) / sqrt(var s + eps) * weight + bias,
+ * var = mean (s - mean s)^2.  residual, sum, weight (= 1), bias (= 0), mean and rstd may be NULL; sum receives s.
+ * 1 <= cols <= 16384, rows >= 0.  y or sum may be x itself or residual itself (same pointer and stride). */
+typedef struct {
+    int dtype;                 /* x, residual, sum, y */
+    int wdtype;                /* weight, bias: GALA_F32 or dtype */
+    long long rows;
+    int cols;
+    float eps;                 /* >= 0 */
+    const void* x;             long long x_ld;
+    const void* residual;      long long residual_ld;
+    const void* weight;
+    const void* bias;
+    void* y;                   long long y_ld;
+    void* sum;                 long long sum_ld;
+    float* mean;               /* [rows] */
+    float* rstd;               /* [rows] 1 / sqrt(var + eps) */
+} gala_layer_norm_args;
+int gala_layer_norm_forward(const gala_layer_norm_args* a, void* stream, char* errbuf, int errbuf_len);
+
+/* Its gradient.  x: what was normalised (s); xh = (x - mean) rstd, e = dy weight:
+ *   dx = rstd (e - mean e - xh mean(e xh)) + dsum      dweight = sum over rows of dy xh      dbias = sum over rows of dy
+ * dsum (the gradient that reaches s by another path), weight, dx, dweight and dbias may be NULL.  The sums over rows
+ * have a fixed order: the same call gives the same bits.  dx may be dy itself or dsum itself.  The workspace
+ * (16-byte aligned) is needed for dweight / dbias only. */
+typedef struct {
+    int dtype;                 /* dy, x, dsum, dx */
+    int wdtype;                /* weight, dweight, dbias: GALA_F32 or dtype */
+    long long rows;
+    int cols;
+    const void* dy;            long long dy_ld;
+    const void* x;             long long x_ld;
+    const void* dsum;          long long dsum_ld;
+    const float* mean;
+    const float* rstd;
+    const void* weight;
+    void* dx;                  long long dx_ld;
+    void* dweight;
+    void* dbias;
+    void* workspace;
+    long long workspace_bytes;
+} gala_layer_norm_grad_args;
+long long gala_layer_norm_workspace(long long rows, int cols);
+int gala_layer_norm_backward(const gala_layer_norm_grad_args* a, void* stream, char* errbuf, int errbuf_len);
+
+/* Gated linear recurrence over time, per sequence b and channel d (time-major like the rollouts, any strides for
+ * time and sequence, channels contiguous):
+ *   a_t = sigmoid(f_t)     h_t = a_t c_{t-1} + (1 - a_t) x_t     c_t = 0 where done_t, else h_t     c_{-1} = h0
+ * done[t] has the meaning it has in gala_rollout (the episode ended at step t), so packed sequences are sequences with
+ * flags between them; what a flag cuts off does not pass it, infinities and NaN included.  h_last = c_{steps-1}, which
+ * is h0 of the next call; steps = 1 is the acting step, and h_last may be h0 itself.  h0 (= 0), done (= none),
+ * h_last and states may be NULL.  states: what gala_gated_recurrence_backward needs, float32
+ * [ceil(steps / 16)][batch][dim], c before every 16th step.  steps, batch, dim >= 0. */
+typedef struct {
+    int dtype;                 /* f, x, h */
+    long long steps, batch, dim;
+    const void* f;             long long f_t, f_b;      /* strides of time and sequence */
+    const void* x;             long long x_t, x_b;
+    const unsigned char* done; long long done_t, done_b;
+    const float* h0;           /* [batch][dim] */
+    void* h;                   long long h_t, h_b;
+    float* h_last;             /* [batch][dim] */
+    float* states;
+} gala_recurrence_args;
+int gala_gated_recurrence_forward(const gala_recurrence_args* a, void* stream, char* errbuf, int errbuf_len);
+
+/* Its gradient.  With g_t = dh_t + (1 - done_t) q_{t+1}, q_t = a_t g_t, q_steps = dh_last:
+ *   dx_t = (1 - a_t) g_t     df_t = g_t (c_{t-1} - x_t) a_t (1 - a_t)     dh0 = q_0
+ * dh (= 0), dh_last (= 0), dh0 and done may be NULL; states is the forward call's. */
+typedef struct {
+    int dtype;                 /* f, x, dh, df, dx */
+    long long steps, batch, dim;
+    const void* f;             long long f_t, f_b;
+    const void* x;             long long x_t, x_b;
+    const unsigned char* done; long long done_t, done_b;
+    const float* states;
+    const void* dh;            long long dh_t, dh_b;
+    const float* dh_last;      /* [batch][dim] */
+    void* df;                  long long df_t, df_b;
+    void* dx;                  long long dx_t, dx_b;
+    float* dh0;                /* [batch][dim] */
+} gala_recurrence_grad_args;
+int gala_gated_recurrence_backward(const gala_recurrence_grad_args* a, void* stream, char* errbuf, int errbuf_len);
+
 #ifdef __cplusplus
 }
 #endif

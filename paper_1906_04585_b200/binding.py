@@ -54,6 +54,43 @@ class gala_sweep_item(C.Structure):
                 ("peer_slot", C.c_int * 2), ("has_grad", C.c_int)]
 
 
+GALA_F32, GALA_BF16, GALA_F16 = 0, 1, 2
+
+
+class gala_layer_norm_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("wdtype", C.c_int), ("rows", C.c_longlong), ("cols", C.c_int), ("eps", C.c_float),
+                ("x", C.c_void_p), ("x_ld", C.c_longlong), ("residual", C.c_void_p), ("residual_ld", C.c_longlong),
+                ("weight", C.c_void_p), ("bias", C.c_void_p), ("y", C.c_void_p), ("y_ld", C.c_longlong),
+                ("sum", C.c_void_p), ("sum_ld", C.c_longlong), ("mean", C.c_void_p), ("rstd", C.c_void_p)]
+
+
+class gala_layer_norm_grad_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("wdtype", C.c_int), ("rows", C.c_longlong), ("cols", C.c_int),
+                ("dy", C.c_void_p), ("dy_ld", C.c_longlong), ("x", C.c_void_p), ("x_ld", C.c_longlong),
+                ("dsum", C.c_void_p), ("dsum_ld", C.c_longlong), ("mean", C.c_void_p), ("rstd", C.c_void_p),
+                ("weight", C.c_void_p), ("dx", C.c_void_p), ("dx_ld", C.c_longlong), ("dweight", C.c_void_p),
+                ("dbias", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_longlong)]
+
+
+class gala_recurrence_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("steps", C.c_longlong), ("batch", C.c_longlong), ("dim", C.c_longlong),
+                ("f", C.c_void_p), ("f_t", C.c_longlong), ("f_b", C.c_longlong),
+                ("x", C.c_void_p), ("x_t", C.c_longlong), ("x_b", C.c_longlong),
+                ("done", C.c_void_p), ("done_t", C.c_longlong), ("done_b", C.c_longlong), ("h0", C.c_void_p),
+                ("h", C.c_void_p), ("h_t", C.c_longlong), ("h_b", C.c_longlong),
+                ("h_last", C.c_void_p), ("states", C.c_void_p)]
+
+
+class gala_recurrence_grad_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("steps", C.c_longlong), ("batch", C.c_longlong), ("dim", C.c_longlong),
+                ("f", C.c_void_p), ("f_t", C.c_longlong), ("f_b", C.c_longlong),
+                ("x", C.c_void_p), ("x_t", C.c_longlong), ("x_b", C.c_longlong),
+                ("done", C.c_void_p), ("done_t", C.c_longlong), ("done_b", C.c_longlong), ("states", C.c_void_p),
+                ("dh", C.c_void_p), ("dh_t", C.c_longlong), ("dh_b", C.c_longlong), ("dh_last", C.c_void_p),
+                ("df", C.c_void_p), ("df_t", C.c_longlong), ("df_b", C.c_longlong),
+                ("dx", C.c_void_p), ("dx_t", C.c_longlong), ("dx_b", C.c_longlong), ("dh0", C.c_void_p)]
+
+
 EXPORTS = (
     "gala_create", "gala_destroy", "gala_act", "gala_learn", "gala_gossip", "gala_step_sync",
     "gala_sync_agent", "gala_sync_all", "gala_in_peers", "gala_get_state", "gala_set_state",
@@ -66,6 +103,8 @@ EXPORTS = (
     "gala_actor_loop", "gala_actor_loop_all", "gala_actor_read",
     "gala_learn_many", "gala_gossip_many", "gala_poll_agent", "gala_sweep_agents", "gala_set_group_lanes",
     "gala_debug_wait_runs_out",
+    "gala_layer_norm_forward", "gala_layer_norm_backward", "gala_layer_norm_workspace",
+    "gala_gated_recurrence_forward", "gala_gated_recurrence_backward",
 )
 
 _lib = None
@@ -129,6 +168,11 @@ def lib() -> C.CDLL:
             "gala_get_stream": (vp, [vp, i]),
             "gala_gemm_bf16": (i, [vp, vp, vp, i, i, i, i, i, i, i, vp]),
             "gala_gemm_bf16_static": (i, [vp, vp, vp, i, i, i, i, i, i, i, vp, C.c_char_p, i]),
+            "gala_layer_norm_forward": (i, [C.POINTER(gala_layer_norm_args), vp, C.c_char_p, i]),
+            "gala_layer_norm_backward": (i, [C.POINTER(gala_layer_norm_grad_args), vp, C.c_char_p, i]),
+            "gala_layer_norm_workspace": (ll, [ll, i]),
+            "gala_gated_recurrence_forward": (i, [C.POINTER(gala_recurrence_args), vp, C.c_char_p, i]),
+            "gala_gated_recurrence_backward": (i, [C.POINTER(gala_recurrence_grad_args), vp, C.c_char_p, i]),
             "gala_sweep_sync": (i, [vp, vp, vp, vp, i, ll, C.POINTER(gala_topology), ll, C.POINTER(gala_hparams), vp]),
         }
         for name, (res, args) in sig.items():
@@ -422,6 +466,37 @@ def gala_sweep_agents(x, g, v, snap, clip, n_agents: int, n_slots: int, d_padded
                                  len(items), C.byref(hp), stream)
     if rc < 0:
         raise GalaError(rc, "gala_sweep_agents")
+
+
+def _operator(name: str, args, stream):
+    """One of the stand-alone operators: its argument struct, the caller's stream, the library's message on failure."""
+    buf = C.create_string_buffer(512)
+    rc = getattr(lib(), name)(C.byref(args), stream, buf, 512)
+    if rc < 0:
+        raise GalaError(rc, buf.value.decode() or name)
+
+
+def gala_layer_norm_forward(args: gala_layer_norm_args, stream=None):
+    _operator("gala_layer_norm_forward", args, stream)
+
+
+def gala_layer_norm_backward(args: gala_layer_norm_grad_args, stream=None):
+    _operator("gala_layer_norm_backward", args, stream)
+
+
+def gala_layer_norm_workspace(rows: int, cols: int) -> int:
+    n = lib().gala_layer_norm_workspace(rows, cols)
+    if n < 0:
+        raise GalaError(n, "gala_layer_norm_workspace: %d rows of %d columns" % (rows, cols))
+    return n
+
+
+def gala_gated_recurrence_forward(args: gala_recurrence_args, stream=None):
+    _operator("gala_gated_recurrence_forward", args, stream)
+
+
+def gala_gated_recurrence_backward(args: gala_recurrence_grad_args, stream=None):
+    _operator("gala_gated_recurrence_backward", args, stream)
 
 
 def default_hparams(n_envs: int, n_steps: int, **kw) -> gala_hparams:

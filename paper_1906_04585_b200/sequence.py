@@ -1,0 +1,206 @@
+"""Operators of sequence policies on torch tensors: layer norm, a gated linear recurrence over time, a gated
+feed-forward block, and the draw of an action or token.
+
+Argument checks and marshalling only, as in `learner`: every operator runs inside libgala.so (include/gala.h has the
+formulas) on torch's current stream of the tensors' device, which has to be the current one.  Element types are float32,
+bfloat16 and float16 (the feed-forward block: the 16-bit ones); states, statistics and log-probabilities are float32.
+`out`-like arguments receive results in place; without them results are new tensors.  What a call may not do raises
+GalaError (from the library) or TypeError / ValueError (from here) before anything is enqueued.
+
+Tensors that other streams still use have to be ordered by the caller, as with any torch operation.
+"""
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import torch
+
+from . import binding as B
+
+_DTYPE = {torch.float32: B.GALA_F32, torch.bfloat16: B.GALA_BF16, torch.float16: B.GALA_F16}
+
+
+def _stream(t: torch.Tensor) -> int:
+    if not t.is_cuda:
+        raise ValueError("CUDA tensors are needed: there is no CPU fallback")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("tensors are on %s, the current device is cuda:%d" % (t.device, torch.cuda.current_device()))
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _want(name: str, t: torch.Tensor, shape, dtype, like: torch.Tensor):
+    if t.shape != shape:
+        raise ValueError("%s is %s, not %s" % (name, tuple(t.shape), tuple(shape)))
+    if t.dtype != dtype:
+        raise TypeError("%s is %s, not %s" % (name, t.dtype, dtype))
+    if t.device != like.device:
+        raise ValueError("%s is on %s, not on %s" % (name, t.device, like.device))
+
+
+def _rows(name: str, t: Optional[torch.Tensor], shape, like: torch.Tensor):
+    """Pointer and row stride of a matrix with contiguous columns (None: nothing)."""
+    if t is None:
+        return None, 0
+    _want(name, t, shape, like.dtype, like)
+    if shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError("the columns of %s have to be contiguous" % name)
+    # a single row may carry any stride
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1])
+
+
+def _flat(name: str, t: Optional[torch.Tensor], shape, dtype, like: torch.Tensor):
+    """Pointer of a contiguous tensor (None: nothing)."""
+    if t is None:
+        return None
+    _want(name, t, shape, dtype, like)
+    if not t.is_contiguous():
+        raise ValueError("%s has to be contiguous" % name)
+    return t.data_ptr()
+
+
+def _type_of(t: torch.Tensor) -> int:
+    try:
+        return _DTYPE[t.dtype]
+    except KeyError:
+        raise TypeError("%s: float32, bfloat16 or float16 is needed" % t.dtype) from None
+
+
+# ---------------------------------------------------------------------------------------------- layer norm
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5, *,
+               residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None):
+    """Layer norm of s = x (+ residual) over its columns; x [rows, cols].  Returns (y, s, mean, rstd); s is x itself
+    without a residual.  weight and bias [cols] are float32 or of x's type."""
+    st = _stream(x)
+    if x.dim() != 2:
+        raise ValueError("x has to be a matrix [rows, cols]")
+    a = B.gala_layer_norm_args()
+    a.dtype, shape = _type_of(x), x.shape
+    a.rows, a.cols, a.eps = shape[0], shape[1], eps
+    wdt = weight.dtype if weight is not None else bias.dtype if bias is not None else x.dtype
+    a.wdtype = _DTYPE.get(wdt, -1)
+    a.weight = _flat("weight", weight, shape[1:], wdt, x)
+    a.bias = _flat("bias", bias, shape[1:], wdt, x)
+    y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
+    a.x, a.x_ld = _rows("x", x, shape, x)
+    a.y, a.y_ld = _rows("out", y, shape, x)
+    s = x
+    if residual is not None:
+        s = torch.empty(shape, dtype=x.dtype, device=x.device) if sum_out is None else sum_out
+        a.residual, a.residual_ld = _rows("residual", residual, shape, x)
+        a.sum, a.sum_ld = _rows("sum_out", s, shape, x)
+    elif sum_out is not None:
+        raise ValueError("sum_out without residual")
+    stats = torch.empty((2, shape[0]), dtype=torch.float32, device=x.device)
+    a.mean = stats.data_ptr()
+    a.rstd = a.mean + 4 * shape[0] if shape[0] else a.mean
+    B.gala_layer_norm_forward(a, st)
+    return y, s, stats[0], stats[1]
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, weight: Optional[torch.Tensor] = None, *,
+                        dsum: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None,
+                        dbias: Optional[torch.Tensor] = None):
+    """Gradients (dx, dweight, dbias) of layer_norm.  x: what was normalised (the s that layer_norm returned); dsum: the
+    gradient that reaches s past the norm, added to dx, which is then the gradient of x and of the residual alike.
+    dweight and dbias have weight's type (float32 without a weight)."""
+    st = _stream(x)
+    if x.dim() != 2:
+        raise ValueError("x has to be a matrix [rows, cols]")
+    a = B.gala_layer_norm_grad_args()
+    a.dtype, shape = _type_of(x), x.shape
+    a.rows, a.cols = shape[0], shape[1]
+    wdt = weight.dtype if weight is not None else torch.float32
+    a.wdtype = _DTYPE.get(wdt, -1)
+    dx = torch.empty(shape, dtype=x.dtype, device=x.device) if dx is None else dx
+    dweight = torch.empty(shape[1], dtype=wdt, device=x.device) if dweight is None else dweight
+    dbias = torch.empty(shape[1], dtype=wdt, device=x.device) if dbias is None else dbias
+    a.dy, a.dy_ld = _rows("dy", dy, shape, x)
+    a.x, a.x_ld = _rows("x", x, shape, x)
+    a.dsum, a.dsum_ld = _rows("dsum", dsum, shape, x)
+    a.dx, a.dx_ld = _rows("dx", dx, shape, x)
+    a.mean = _flat("mean", mean, shape[:1], torch.float32, x)
+    a.rstd = _flat("rstd", rstd, shape[:1], torch.float32, x)
+    a.weight = _flat("weight", weight, shape[1:], wdt, x)
+    a.dweight = _flat("dweight", dweight, shape[1:], wdt, x)
+    a.dbias = _flat("dbias", dbias, shape[1:], wdt, x)
+    a.workspace_bytes = B.gala_layer_norm_workspace(shape[0], shape[1])
+    ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=x.device)
+    a.workspace = ws.data_ptr()
+    B.gala_layer_norm_backward(a, st)
+    return dx, dweight, dbias
+
+
+# ---------------------------------------------------------------------------------------------- gated recurrence
+def _steps(name: str, t: Optional[torch.Tensor], shape, dtype, like: torch.Tensor):
+    """Pointer and the strides of time and sequence of a [steps, batch, dim] tensor with contiguous channels."""
+    if t is None:
+        return None, 0, 0
+    _want(name, t, shape, dtype, like)
+    if shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError("the channels of %s have to be contiguous" % name)
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _done(done: Optional[torch.Tensor], shape, like: torch.Tensor):
+    if done is None:
+        return None, 0, 0
+    if done.dtype not in (torch.uint8, torch.bool):
+        raise TypeError("done is %s, not uint8 or bool" % done.dtype)
+    _want("done", done, shape[:2], done.dtype, like)
+    return done.data_ptr(), done.stride(0), done.stride(1)
+
+
+def gated_recurrence(f: torch.Tensor, x: torch.Tensor, h0: Optional[torch.Tensor] = None, *, done: Optional[torch.Tensor] = None,
+                     out: Optional[torch.Tensor] = None, h_last: Optional[torch.Tensor] = None, save: bool = False):
+    """h_t = sigmoid(f_t) c_{t-1} + (1 - sigmoid(f_t)) x_t over time; c_t is h_t, or 0 where done_t; c_{-1} = h0.
+
+    f, x [steps, batch, dim] with any strides for time and sequence (x.transpose(0, 1) for sequence-major data); done
+    [steps, batch] with the meaning it has in a rollout.  Returns (h, h_last, states): h_last [batch, dim] is the h0 of
+    the next call (pass the same tensor as h0 and h_last to keep a state in place), states is what the backward call
+    needs (None unless `save`)."""
+    st = _stream(x)
+    if x.dim() != 3:
+        raise ValueError("x has to be [steps, batch, dim]")
+    a = B.gala_recurrence_args()
+    a.dtype, shape = _type_of(x), x.shape
+    T, N, D = shape
+    a.steps, a.batch, a.dim = T, N, D
+    h = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
+    h_last = torch.empty((N, D), dtype=torch.float32, device=x.device) if h_last is None else h_last
+    states = torch.empty(((T + 15) // 16, N, D), dtype=torch.float32, device=x.device) if save else None
+    a.f, a.f_t, a.f_b = _steps("f", f, shape, x.dtype, x)
+    a.x, a.x_t, a.x_b = _steps("x", x, shape, x.dtype, x)
+    a.h, a.h_t, a.h_b = _steps("out", h, shape, x.dtype, x)
+    a.done, a.done_t, a.done_b = _done(done, shape, x)
+    a.h0 = _flat("h0", h0, shape[1:], torch.float32, x)
+    a.h_last = _flat("h_last", h_last, shape[1:], torch.float32, x)
+    a.states = states.data_ptr() if save else None
+    B.gala_gated_recurrence_forward(a, st)
+    return h, h_last, states
+
+
+def gated_recurrence_backward(dh: Optional[torch.Tensor], f: torch.Tensor, x: torch.Tensor, states: torch.Tensor, *,
+                              done: Optional[torch.Tensor] = None, dh_last: Optional[torch.Tensor] = None, df: Optional[torch.Tensor] = None,
+                              dx: Optional[torch.Tensor] = None, dh0: Optional[torch.Tensor] = None):
+    """Gradients (df, dx, dh0) of gated_recurrence from those of h (dh) and h_last (dh_last); states is the forward call's."""
+    st = _stream(x)
+    if x.dim() != 3:
+        raise ValueError("x has to be [steps, batch, dim]")
+    a = B.gala_recurrence_grad_args()
+    a.dtype, shape = _type_of(x), x.shape
+    T, N, D = shape
+    a.steps, a.batch, a.dim = T, N, D
+    df = torch.empty(shape, dtype=x.dtype, device=x.device) if df is None else df
+    dx = torch.empty(shape, dtype=x.dtype, device=x.device) if dx is None else dx
+    dh0 = torch.empty((N, D), dtype=torch.float32, device=x.device) if dh0 is None else dh0
+    a.f, a.f_t, a.f_b = _steps("f", f, shape, x.dtype, x)
+    a.x, a.x_t, a.x_b = _steps("x", x, shape, x.dtype, x)
+    a.dh, a.dh_t, a.dh_b = _steps("dh", dh, shape, x.dtype, x)
+    a.df, a.df_t, a.df_b = _steps("df", df, shape, x.dtype, x)
+    a.dx, a.dx_t, a.dx_b = _steps("dx", dx, shape, x.dtype, x)
+    a.done, a.done_t, a.done_b = _done(done, shape, x)
+    a.states = _flat("states", states, ((T + 15) // 16, N, D), torch.float32, x)
+    a.dh_last = _flat("dh_last", dh_last, shape[1:], torch.float32, x)
+    a.dh0 = _flat("dh0", dh0, shape[1:], torch.float32, x)
+    B.gala_gated_recurrence_backward(a, st)
+    return df, dx, dh0

@@ -2,19 +2,20 @@
 //
 //   a_t = sigmoid(f_t)  b_t = 1 - a_t   h_t = a_t c_{t-1} + b_t x_t   c_t = done_t ? 0 : h_t
 //   backward, from the last step:  g_t = dh_t + (done_t ? 0 : q_{t+1})   q_t = a_t g_t
-//                                  dx_t = b_t g_t      df_t = g_t (c_{t-1} - x_t) a_t b_t
+//                                  dx_t = b_t g_t      df_t = q_t b_t (c_{t-1} - x_t)
 //
 // A step is the map c -> A c + B; maps compose ((A2, B2) after (A1, B1) is (A2 A1, A2 B1 + B2)), so the time axis is
 // cut at three levels and read from memory once:
-//   a thread    takes 16 successive steps of V channels, holds their inputs in registers and composes their map;
+//   a thread    takes 16 (backward: 8) successive steps of one 32-bit word of channels, holds them in registers and
+//               composes their map;
 //   a block     has a warp for each of up to 8 such pieces and joins the warps' maps through shared memory;
 //   a cluster   of up to 8 blocks joins the blocks' maps through distributed shared memory (one cluster barrier a
 //               turn; the slots alternate, so that a block that is ahead never overwrites what another still reads).
-// Then every thread knows the state that enters its 16 steps and walks over them again, from registers, writing
-// results.  A cluster goes over the time axis in turns of up to 1024 steps, the state carried in registers, so memory
-// for the channels of one warp is streamed once in order and no block waits for another cluster.
-// The backward kernel does the same from the other end; it recomputes c inside a 16-step piece from the state at its
-// beginning, which the forward kernel stored in 32 bits (0.25 bytes an element, against 2 or 4 for reading h back).
+// Then every thread knows the state that enters its piece and walks over it again, from registers, writing results.
+// A cluster goes over the time axis in turns of up to 1024 steps, the state carried in registers; the loads of the next
+// turn are under way while the maps of this one are joined.  No block waits for another cluster.
+// The backward kernel does the same from the other end; it recomputes c inside a piece from the state at its beginning,
+// which the forward kernel stored in 32 bits (0.5 bytes an element, against 2 or 4 for reading h back, and exact).
 //
 // What a `done` flag cuts off must not leak through it (0 * inf), so A = -0.0f marks a map that does not depend on
 // its input: products keep the sign (A is never negative otherwise), and applying such a map selects B.
@@ -25,7 +26,8 @@
 namespace gala {
 namespace cg = cooperative_groups;
 
-constexpr int kPiece = 16;     // steps of a thread; the distance of the stored states
+constexpr int kStateStep = 8;    // distance of the stored states, and the steps of a thread in the backward kernel
+constexpr int kFwdPiece = 16;
 constexpr int kMaxWarps = 8;
 constexpr int kMaxCluster = 8;
 
@@ -42,67 +44,112 @@ template <bool DONE> __device__ __forceinline__ Map then(Map m, Map n) {
 // What the first piece of a turn starts from: its state is known, so it walks from there instead of from zero (one
 // rounding less where the state and the first input cancel) and its map has nothing left to depend on.
 template <bool DONE> __device__ __forceinline__ Map known(float c) { return Map{DONE ? -0.0f : 0.0f, c}; }
-// The gate as one number: the smaller of a = sigmoid(f) and 1 - a, negative (sign bit) when that is a.  Either extreme
-// keeps its full relative precision, and the step is an interpolation from the side with the larger weight, so that
-// neither a long memory (1 - a small) nor a memory wiped by the gate (a small) loses digits to cancellation.
-__device__ __forceinline__ float gate(float f) {
-    const float e = __expf(-fabsf(f));           // 2 ulp and |f| 2^-24: below 1e-6 wherever the result is above 1e-7
-    const float small = __fdividef(e, 1.0f + e);
-    return __uint_as_float(__float_as_uint(small) | (__float_as_uint(f) & 0x80000000u));
+
+// a = sigmoid(f) and b = 1 - a.  The smaller of the two is e / (1 + e) with e = exp(-|f|) (fast exponential and division:
+// a few units in its last place), the larger is 1 minus it, rounded once: neither a long memory (b small, where an error
+// of a in its last places would add up over 1 / b steps) nor a memory wiped by the gate (a small) loses digits.
+__device__ __forceinline__ void gate(float f, float& a, float& b) {
+    const float e = __expf(-fabsf(f));
+    const float small = __fdividef(e, 1.0f + e), big = 1.0f - small;
+    a = f < 0.0f ? small : big;
+    b = f < 0.0f ? big : small;
 }
-__device__ __forceinline__ bool closed(float s) { return (__float_as_uint(s) >> 31) != 0; }     // a is the smaller
-__device__ __forceinline__ float keep_of(float s) { return closed(s) ? fabsf(s) : 1.0f - fabsf(s); }    // a
-__device__ __forceinline__ float take_of(float s) { return closed(s) ? 1.0f - fabsf(s) : fabsf(s); }    // 1 - a
-// a c + (1 - a) x
-__device__ __forceinline__ float step(float s, float c, float x) {
-    const float base = closed(s) ? x : c, other = closed(s) ? c : x;
-    return fmaf(fabsf(s), other - base, base);
+
+// What one lane reads of one step: a 32-bit word (one float, or two 16-bit channels), or a single 16-bit channel where
+// rows are not aligned to words.
+template <typename T, int V> struct Word;
+template <> struct Word<float, 1> {
+    using type = float;
+    static __device__ __forceinline__ float get(type w, int) { return w; }
+    static __device__ __forceinline__ type put(const float (&v)[1]) { return v[0]; }
+};
+template <typename T> struct Word<T, 1> {
+    using type = T;
+    static __device__ __forceinline__ float get(type w, int) { return to_f32<T>(w); }
+    static __device__ __forceinline__ type put(const float (&v)[1]) { return from_f32<T>(v[0]); }
+};
+template <> struct Word<__nv_bfloat16, 2> {
+    using type = uint32_t;
+    static __device__ __forceinline__ float get(type w, int v) { return __uint_as_float(v ? w & 0xffff0000u : w << 16); }
+    static __device__ __forceinline__ type put(const float (&v)[2]) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[0], v[1]);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+};
+template <> struct Word<__half, 2> {
+    using type = uint32_t;
+    static __device__ __forceinline__ float get(type w, int v) {
+        const __half2 h = *reinterpret_cast<const __half2*>(&w);
+        return v ? __high2float(h) : __low2float(h);
+    }
+    static __device__ __forceinline__ type put(const float (&v)[2]) {
+        const __half2 h = __floats2half2_rn(v[0], v[1]);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+};
+
+// L successive steps of one lane, `n` of them inside the sequence (1 <= n; the others repeat the last one, so that all
+// loads are issued without a condition).
+template <int L, typename W, typename T>
+__device__ __forceinline__ void load_steps(W (&r)[L], const T* p, long long stride, int n) {
+    if (n >= L) {
+#pragma unroll
+        for (int i = 0; i < L; i++) {
+            r[i] = *reinterpret_cast<const W*>(p);
+            p += stride;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < L; i++) {
+            r[i] = *reinterpret_cast<const W*>(p);
+            if (i + 1 < n) p += stride;
+        }
+    }
 }
 
 struct RecurrenceGrid {
-    long long pieces;       // ceil(steps / 16)
+    long long pieces;       // ceil(steps / L)
     int chan_blocks;        // ceil(dim / (32 V))
     long long units;        // batch * chan_blocks
     int warps, cluster;     // warps of a block along time, blocks of a cluster along time
 };
 
-// The maps of all pieces of a turn, and the state before this thread's piece.  `order`: this warp's place in the turn
-// (0 = first to act).  On return *carry is the state after the whole turn.
-// slots: [2][kMaxCluster][32 V] of this block, maps: [kMaxWarps][32 V].
+// Joins the maps of all pieces of a turn: `enter` is the state before this thread's piece, and carry, on entry the state
+// before the turn, the one behind it.  w, rank: this warp's and block's place in the turn (0 = first to act).
+// maps: [kMaxWarps][32 V], slots: [2][kMaxCluster][32 V] of this block.
 template <int V, bool DONE>
 __device__ __forceinline__ void join(const Map (&m)[V], float (&enter)[V], float (&carry)[V], Map* maps, Map* slots, int warps, int w, int cluster,
                                      int rank, int turn) {
     const int lane = threadIdx.x & 31;
-    Map before[V];     // the pieces of this block ahead of this warp
-#pragma unroll
-    for (int v = 0; v < V; v++) {
-        before[v].a = 1.0f;
-        before[v].b = 0.0f;
-    }
     if (warps > 1) {
 #pragma unroll
         for (int v = 0; v < V; v++) maps[w * 32 * V + lane * V + v] = m[v];
         __syncthreads();
     }
-    Map all[V];        // the whole block
+    Map before[V], all[V];     // the pieces of this block ahead of this warp, and the whole block
 #pragma unroll
-    for (int v = 0; v < V; v++) all[v] = m[v];
+    for (int v = 0; v < V; v++) {
+        before[v] = Map{1.0f, 0.0f};
+        all[v] = m[v];
+    }
     if (warps > 1) {
 #pragma unroll
-        for (int v = 0; v < V; v++) {
-            Map r = maps[lane * V + v];
-            for (int k = 1; k < warps; k++) {
-                if (k == w) before[v] = r;
-                r = then<DONE>(r, maps[k * 32 * V + lane * V + v]);
+        for (int v = 0; v < V; v++) all[v] = maps[lane * V + v];
+#pragma unroll
+        for (int k = 1; k < kMaxWarps; k++)
+            if (k < warps) {
+#pragma unroll
+                for (int v = 0; v < V; v++) {
+                    if (k == w) before[v] = all[v];
+                    all[v] = then<DONE>(all[v], maps[k * 32 * V + lane * V + v]);
+                }
             }
-            all[v] = r;
-        }
     }
     if (cluster > 1) {
         cg::cluster_group cl = cg::this_cluster();
         Map* mine = slots + ((turn & 1) * kMaxCluster + rank) * 32 * V + lane * V;
-        for (int r = w; r < cluster; r += warps) {
-            Map* there = cl.map_shared_rank(mine, r);
+        if (w < cluster) {         // warp w tells block w (a cluster has all kMaxWarps warps in every block)
+            Map* there = cl.map_shared_rank(mine, w);
 #pragma unroll
             for (int v = 0; v < V; v++) there[v] = all[v];
         }
@@ -111,10 +158,12 @@ __device__ __forceinline__ void join(const Map (&m)[V], float (&enter)[V], float
 #pragma unroll
         for (int v = 0; v < V; v++) {
             float c = carry[v];
-            for (int r = 0; r < cluster; r++) {
-                if (r == rank) enter[v] = apply<DONE>(before[v], c);
-                c = apply<DONE>(from[r * 32 * V + v], c);
-            }
+#pragma unroll
+            for (int r = 0; r < kMaxCluster; r++)
+                if (r < cluster) {
+                    if (r == rank) enter[v] = apply<DONE>(before[v], c);
+                    c = apply<DONE>(from[r * 32 * V + v], c);
+                }
             carry[v] = c;
         }
     } else {
@@ -127,12 +176,13 @@ __device__ __forceinline__ void join(const Map (&m)[V], float (&enter)[V], float
     }
 }
 
-// SINGLE: no more than 16 steps, so that a thread has the whole time axis; the warps of a block take different units.
-template <typename T, int V, bool SINGLE, bool DONE>
-__global__ void __launch_bounds__(32 * kMaxWarps) recurrence_fwd_kernel(const gala_recurrence_args p, const RecurrenceGrid g) {
+// SINGLE: no more than L steps, so that a thread has the whole time axis; the warps of a block take different units.
+template <typename T, int V, int L, bool SINGLE, bool DONE>
+__global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const gala_recurrence_args p, const RecurrenceGrid g) {
     __shared__ Map maps[SINGLE ? 1 : kMaxWarps * 32 * V];
     __shared__ Map slots[SINGLE ? 1 : 2 * kMaxCluster * 32 * V];
-    using P = Pack<T, V>;
+    using Wd = Word<T, V>;
+    using W = typename Wd::type;
     const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = SINGLE ? 0 : (int)(blockIdx.x % g.cluster);
     const long long unit = SINGLE ? (long long)blockIdx.x * (blockDim.x >> 5) + w : (long long)blockIdx.x / g.cluster;
@@ -141,78 +191,91 @@ __global__ void __launch_bounds__(32 * kMaxWarps) recurrence_fwd_kernel(const ga
     if (SINGLE && unit >= g.units) return;
     const long long b = unit / g.chan_blocks;
     const long long d = (unit % g.chan_blocks) * 32 * V + lane * V;
-    const bool on = d < p.dim;      // dim is a multiple of V
-    const T* f = static_cast<const T*>(p.f) + b * p.f_b + d;
-    const T* x = static_cast<const T*>(p.x) + b * p.x_b + d;
-    T* h = static_cast<T*>(p.h) + b * p.h_b + d;
+    const bool on = d < p.dim;              // dim is a multiple of V; lanes past it work on channel 0 and write nothing
+    const long long dl = on ? d : 0;
+    const T* f = static_cast<const T*>(p.f) + b * p.f_b + dl;
+    const T* x = static_cast<const T*>(p.x) + b * p.x_b + dl;
+    T* h = static_cast<T*>(p.h) + b * p.h_b + dl;
     const unsigned char* done = DONE ? p.done + b * p.done_b : nullptr;
     float carry[V];
 #pragma unroll
-    for (int v = 0; v < V; v++) carry[v] = on && p.h0 ? p.h0[b * p.dim + d + v] : 0.0f;
+    for (int v = 0; v < V; v++) carry[v] = p.h0 ? p.h0[b * p.dim + dl + v] : 0.0f;
     const int per_turn = SINGLE ? 1 : g.warps * g.cluster;
     const int place = SINGLE ? 0 : rank * g.warps + w;
+    W rf[L], rx[L];
+    uint32_t flag = 0;                       // this lane's step of the piece ends an episode
+    auto fetch = [&](long long piece) -> int {
+        const long long t0 = piece * L;
+        const int n = t0 >= p.steps ? 0 : (int)(p.steps - t0 < L ? p.steps - t0 : L);
+        if (n) {
+            load_steps<L>(rf, f + t0 * p.f_t, p.f_t, n);
+            load_steps<L>(rx, x + t0 * p.x_t, p.x_t, n);
+            if (DONE) flag = lane < n ? done[(t0 + lane) * p.done_t] : 0;
+        }
+        return n;
+    };
+    // every block of the cluster has to run before another writes to its shared memory
+    if (!SINGLE && g.cluster > 1) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+    int n = fetch(place);
+    if (!SINGLE && g.cluster > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     int turn = 0;
     for (long long first = 0; first < g.pieces; first += per_turn, turn++) {
-        const long long t0 = (first + place) * kPiece;
-        const int n = t0 >= p.steps ? 0 : (int)(p.steps - t0 < kPiece ? p.steps - t0 : kPiece);
-        P rf[kPiece], rx[kPiece];
-        uint32_t ends = 0;
-        if (on) {
+        const long long piece = first + place, t0 = piece * L;
+        const int now = n;
+        const uint32_t ends = DONE ? __ballot_sync(0xffffffffu, now && flag) : 0;
+        float a[L][V], bx[L][V];
+        if (now) {
 #pragma unroll
-            for (int i = 0; i < kPiece; i++)
-                if (i < n) {
-                    rf[i] = *reinterpret_cast<const P*>(f + (t0 + i) * p.f_t);
-                    rx[i] = *reinterpret_cast<const P*>(x + (t0 + i) * p.x_t);
+            for (int i = 0; i < L; i++)
+#pragma unroll
+                for (int v = 0; v < V; v++) {
+                    float bb;
+                    gate(Wd::get(rf[i], v), a[i][v], bb);
+                    bx[i][v] = bb * Wd::get(rx[i], v);
+                    if (!SINGLE && i >= now) a[i][v] = 1.0f, bx[i][v] = 0.0f;
                 }
         }
-        if (DONE) {
-            const bool e = lane < n && done[(t0 + lane) * p.done_t] != 0;
-            ends = __ballot_sync(0xffffffffu, e);
-        }
-        float st[kPiece][V];
-        Map m[V];
-#pragma unroll
-        for (int v = 0; v < V; v++) m[v] = place == 0 ? known<DONE>(carry[v]) : Map{1.0f, 0.0f};
-        if (on) {
-#pragma unroll
-            for (int i = 0; i < kPiece; i++)
-                if (i < n) {
-#pragma unroll
-                    for (int v = 0; v < V; v++) {
-                        st[i][v] = gate(to_f32<T>(rf[i].v[v]));
-                        if (!SINGLE) {
-                            m[v].b = step(st[i][v], m[v].b, to_f32<T>(rx[i].v[v]));
-                            m[v].a = cut<DONE>(m[v].a) ? -0.0f : m[v].a * keep_of(st[i][v]);
-                            if (DONE && ((ends >> i) & 1u)) m[v].a = -0.0f, m[v].b = 0.0f;
-                        }
-                    }
-                }
-        }
+        if (!SINGLE && first + per_turn < g.pieces) n = fetch(piece + per_turn);
         float c[V];
         if (SINGLE) {
 #pragma unroll
             for (int v = 0; v < V; v++) c[v] = carry[v];
         } else {
+            Map m[V];
+#pragma unroll
+            for (int v = 0; v < V; v++) m[v] = place == 0 ? known<DONE>(carry[v]) : Map{1.0f, 0.0f};
+            if (now) {
+#pragma unroll
+                for (int i = 0; i < L; i++)
+#pragma unroll
+                    for (int v = 0; v < V; v++) {
+                        m[v].b = fmaf(a[i][v], m[v].b, bx[i][v]);
+                        m[v].a = cut<DONE>(m[v].a) ? -0.0f : m[v].a * a[i][v];
+                        if (DONE && ((ends >> i) & 1u)) m[v] = Map{-0.0f, 0.0f};
+                    }
+            }
             join<V, DONE>(m, c, carry, maps, slots, g.warps, w, g.cluster, rank, turn);
         }
-        if (!on || n == 0) continue;
-        if (p.states) {
-            float* s = p.states + ((first + place) * p.batch + b) * p.dim + d;
+        if (!now) continue;
+        float* s = p.states ? p.states + ((t0 / kStateStep) * p.batch + b) * p.dim + dl : nullptr;
+        T* ht = h + t0 * p.h_t;
 #pragma unroll
-            for (int v = 0; v < V; v++) s[v] = c[v];
-        }
+        for (int i = 0; i < L; i++) {
+            if (i < now) {
+                if (i % kStateStep == 0 && s && on) {
 #pragma unroll
-        for (int i = 0; i < kPiece; i++)
-            if (i < n) {
-                P o;
-#pragma unroll
-                for (int v = 0; v < V; v++) {
-                    const float hv = step(st[i][v], c[v], to_f32<T>(rx[i].v[v]));
-                    o.v[v] = from_f32<T>(hv);
-                    c[v] = DONE && ((ends >> i) & 1u) ? 0.0f : hv;
+                    for (int v = 0; v < V; v++) s[(i / kStateStep) * p.batch * p.dim + v] = c[v];
                 }
-                *reinterpret_cast<P*>(h + (t0 + i) * p.h_t) = o;
+#pragma unroll
+                for (int v = 0; v < V; v++) c[v] = fmaf(a[i][v], c[v], bx[i][v]);
+                if (on) *reinterpret_cast<W*>(ht) = Wd::put(c);
+                if (DONE && ((ends >> i) & 1u)) {
+#pragma unroll
+                    for (int v = 0; v < V; v++) c[v] = 0.0f;
+                }
             }
+            ht += p.h_t;
+        }
         if (SINGLE) {
 #pragma unroll
             for (int v = 0; v < V; v++) carry[v] = c[v];
@@ -225,11 +288,13 @@ __global__ void __launch_bounds__(32 * kMaxWarps) recurrence_fwd_kernel(const ga
     if (!SINGLE && g.cluster > 1) cg::this_cluster().sync();   // no block leaves while another may still write to it
 }
 
-template <typename T, int V, bool SINGLE, bool DONE>
-__global__ void __launch_bounds__(32 * kMaxWarps) recurrence_bwd_kernel(const gala_recurrence_grad_args p, const RecurrenceGrid g) {
+template <typename T, int V, int L, bool SINGLE, bool DONE>
+__global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const gala_recurrence_grad_args p, const RecurrenceGrid g) {
+    static_assert(L <= kStateStep, "a piece begins where a state is stored");
     __shared__ Map maps[SINGLE ? 1 : kMaxWarps * 32 * V];
     __shared__ Map slots[SINGLE ? 1 : 2 * kMaxCluster * 32 * V];
-    using P = Pack<T, V>;
+    using Wd = Word<T, V>;
+    using W = typename Wd::type;
     const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = SINGLE ? 0 : (int)(blockIdx.x % g.cluster);
     const long long unit = SINGLE ? (long long)blockIdx.x * (blockDim.x >> 5) + w : (long long)blockIdx.x / g.cluster;
@@ -239,99 +304,101 @@ __global__ void __launch_bounds__(32 * kMaxWarps) recurrence_bwd_kernel(const ga
     const long long b = unit / g.chan_blocks;
     const long long d = (unit % g.chan_blocks) * 32 * V + lane * V;
     const bool on = d < p.dim;
-    const T* f = static_cast<const T*>(p.f) + b * p.f_b + d;
-    const T* x = static_cast<const T*>(p.x) + b * p.x_b + d;
-    const T* dh = p.dh ? static_cast<const T*>(p.dh) + b * p.dh_b + d : nullptr;
-    T* df = static_cast<T*>(p.df) + b * p.df_b + d;
-    T* dx = static_cast<T*>(p.dx) + b * p.dx_b + d;
+    const long long dl = on ? d : 0;
+    const T* f = static_cast<const T*>(p.f) + b * p.f_b + dl;
+    const T* x = static_cast<const T*>(p.x) + b * p.x_b + dl;
+    const T* dh = p.dh ? static_cast<const T*>(p.dh) + b * p.dh_b + dl : nullptr;
+    T* df = static_cast<T*>(p.df) + b * p.df_b + dl;
+    T* dx = static_cast<T*>(p.dx) + b * p.dx_b + dl;
     const unsigned char* done = DONE ? p.done + b * p.done_b : nullptr;
     float carry[V];      // q of the step after those still to come
 #pragma unroll
-    for (int v = 0; v < V; v++) carry[v] = on && p.dh_last ? p.dh_last[b * p.dim + d + v] : 0.0f;
+    for (int v = 0; v < V; v++) carry[v] = p.dh_last ? p.dh_last[b * p.dim + dl + v] : 0.0f;
     const int per_turn = SINGLE ? 1 : g.warps * g.cluster;
     const int place = SINGLE ? 0 : rank * g.warps + w;       // 0 acts first and has the latest piece
+    W rf[L], rx[L], rg[L];
+    float rc[V];
+    uint32_t flag = 0;
+    auto fetch = [&](long long piece) -> int {
+        const long long t0 = piece * L;
+        const int n = piece < 0 ? 0 : (int)(p.steps - t0 < L ? p.steps - t0 : L);
+        if (n) {
+            load_steps<L>(rf, f + t0 * p.f_t, p.f_t, n);
+            load_steps<L>(rx, x + t0 * p.x_t, p.x_t, n);
+            if (dh) load_steps<L>(rg, dh + t0 * p.dh_t, p.dh_t, n);
+            const float* s = p.states + ((t0 / kStateStep) * p.batch + b) * p.dim + dl;
+#pragma unroll
+            for (int v = 0; v < V; v++) rc[v] = s[v];
+            if (DONE) flag = lane < n ? done[(t0 + lane) * p.done_t] : 0;
+        }
+        return n;
+    };
+    if (!SINGLE && g.cluster > 1) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+    int n = fetch(g.pieces - 1 - place);
+    if (!SINGLE && g.cluster > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     int turn = 0;
     for (long long first = 0; first < g.pieces; first += per_turn, turn++) {
-        const long long piece = g.pieces - 1 - (first + place);
-        const long long t0 = piece * kPiece;
-        const int n = piece < 0 ? 0 : (int)(p.steps - t0 < kPiece ? p.steps - t0 : kPiece);
-        P rf[kPiece], rx[kPiece], rg[kPiece];
-        uint32_t ends = 0;
-        float c0[V];
-        if (on && n) {
+        const long long piece = g.pieces - 1 - (first + place), t0 = piece * L;
+        const int now = n;
+        const uint32_t ends = DONE ? __ballot_sync(0xffffffffu, now && flag) : 0;
+        float a[L][V], bb[L][V], cx[L][V], gg[L][V];     // gates, c_{t-1} - x_t, dh_t
+        if (now) {
 #pragma unroll
-            for (int i = 0; i < kPiece; i++)
-                if (i < n) {
-                    rf[i] = *reinterpret_cast<const P*>(f + (t0 + i) * p.f_t);
-                    rx[i] = *reinterpret_cast<const P*>(x + (t0 + i) * p.x_t);
-                    if (dh) {
-                        rg[i] = *reinterpret_cast<const P*>(dh + (t0 + i) * p.dh_t);
-                    } else {
+            for (int i = 0; i < L; i++)
 #pragma unroll
-                        for (int v = 0; v < V; v++) rg[i].v[v] = from_f32<T>(0.0f);
-                    }
+                for (int v = 0; v < V; v++) {
+                    const float xv = Wd::get(rx[i], v);
+                    gate(Wd::get(rf[i], v), a[i][v], bb[i][v]);
+                    cx[i][v] = rc[v] - xv;
+                    rc[v] = DONE && ((ends >> i) & 1u) ? 0.0f : fmaf(a[i][v], rc[v], bb[i][v] * xv);
+                    gg[i][v] = dh ? Wd::get(rg[i], v) : 0.0f;
                 }
-            const float* s = p.states + (piece * p.batch + b) * p.dim + d;
-#pragma unroll
-            for (int v = 0; v < V; v++) c0[v] = s[v];
         }
-        if (DONE) {
-            const bool e = lane < n && done[(t0 + lane) * p.done_t] != 0;
-            ends = __ballot_sync(0xffffffffu, e);
-        }
-        float st[kPiece][V], cb[kPiece][V];     // gates, and c_{t-1}
-        Map m[V];
-#pragma unroll
-        for (int v = 0; v < V; v++) m[v] = place == 0 ? known<DONE>(carry[v]) : Map{1.0f, 0.0f};
-        if (on && n) {
-#pragma unroll
-            for (int i = 0; i < kPiece; i++)
-                if (i < n) {
-#pragma unroll
-                    for (int v = 0; v < V; v++) {
-                        st[i][v] = gate(to_f32<T>(rf[i].v[v]));
-                        cb[i][v] = c0[v];
-                        const float hv = step(st[i][v], c0[v], to_f32<T>(rx[i].v[v]));
-                        c0[v] = DONE && ((ends >> i) & 1u) ? 0.0f : hv;
-                    }
-                }
-            if (!SINGLE) {
-#pragma unroll
-                for (int i = kPiece - 1; i >= 0; i--)
-                    if (i < n) {
-#pragma unroll
-                        for (int v = 0; v < V; v++) {
-                            if (DONE && ((ends >> i) & 1u)) m[v].a = -0.0f, m[v].b = 0.0f;
-                            const float a = keep_of(st[i][v]);
-                            m[v].b = a * (to_f32<T>(rg[i].v[v]) + m[v].b);
-                            m[v].a = cut<DONE>(m[v].a) ? -0.0f : m[v].a * a;
-                        }
-                    }
-            }
-        }
+        if (!SINGLE && first + per_turn < g.pieces) n = fetch(piece - per_turn);
         float q[V];
         if (SINGLE) {
 #pragma unroll
             for (int v = 0; v < V; v++) q[v] = carry[v];
         } else {
+            Map m[V];
+#pragma unroll
+            for (int v = 0; v < V; v++) m[v] = place == 0 ? known<DONE>(carry[v]) : Map{1.0f, 0.0f};
+            if (now) {
+#pragma unroll
+                for (int i = L - 1; i >= 0; i--)
+                    if (i < now) {
+#pragma unroll
+                        for (int v = 0; v < V; v++) {
+                            if (DONE && ((ends >> i) & 1u)) m[v] = Map{-0.0f, 0.0f};
+                            m[v].b = a[i][v] * (gg[i][v] + m[v].b);
+                            m[v].a = cut<DONE>(m[v].a) ? -0.0f : m[v].a * a[i][v];
+                        }
+                    }
+            }
             join<V, DONE>(m, q, carry, maps, slots, g.warps, w, g.cluster, rank, turn);
         }
-        if (!on || n == 0) continue;
+        if (!now) continue;
+        T* dft = df + (t0 + L - 1) * p.df_t;
+        T* dxt = dx + (t0 + L - 1) * p.dx_t;
 #pragma unroll
-        for (int i = kPiece - 1; i >= 0; i--)
-            if (i < n) {
-                P of, ox;
+        for (int i = L - 1; i >= 0; i--) {
+            if (i < now) {
+                float of[V], ox[V];
 #pragma unroll
                 for (int v = 0; v < V; v++) {
-                    const float b1 = take_of(st[i][v]);
-                    const float gt = to_f32<T>(rg[i].v[v]) + (DONE && ((ends >> i) & 1u) ? 0.0f : q[v]);
-                    q[v] = keep_of(st[i][v]) * gt;
-                    ox.v[v] = from_f32<T>(b1 * gt);
-                    of.v[v] = from_f32<T>(q[v] * b1 * (cb[i][v] - to_f32<T>(rx[i].v[v])));
+                    const float gt = DONE && ((ends >> i) & 1u) ? gg[i][v] : gg[i][v] + q[v];
+                    q[v] = a[i][v] * gt;
+                    ox[v] = bb[i][v] * gt;
+                    of[v] = q[v] * bb[i][v] * cx[i][v];
                 }
-                *reinterpret_cast<P*>(df + (t0 + i) * p.df_t) = of;
-                *reinterpret_cast<P*>(dx + (t0 + i) * p.dx_t) = ox;
+                if (on) {
+                    *reinterpret_cast<W*>(dft) = Wd::put(of);
+                    *reinterpret_cast<W*>(dxt) = Wd::put(ox);
+                }
             }
+            dft -= p.df_t;
+            dxt -= p.dx_t;
+        }
         if (SINGLE) {
 #pragma unroll
             for (int v = 0; v < V; v++) carry[v] = q[v];
@@ -356,9 +423,9 @@ namespace {
 
 // How the time axis is cut.  Blocks along it cost a cluster barrier a turn and are taken while there are pieces for
 // them: even with many units, more and shorter blocks fill the last wave of the grid better.
-RecurrenceGrid plan(long long steps, long long batch, long long dim, int v) {
+RecurrenceGrid plan(long long steps, long long batch, long long dim, int v, int piece) {
     RecurrenceGrid g;
-    g.pieces = (steps + kPiece - 1) / kPiece;
+    g.pieces = (steps + piece - 1) / piece;
     g.chan_blocks = (int)((dim + 32 * v - 1) / (32 * v));
     g.units = batch * g.chan_blocks;
     g.warps = (int)(g.pieces < kMaxWarps ? g.pieces : kMaxWarps);
@@ -385,17 +452,34 @@ cudaError_t launch_units(void (*kernel)(Args, RecurrenceGrid), const Args& a, co
     return cudaLaunchKernelEx(&cfg, kernel, a, g);
 }
 
-template <typename T, int V>
+template <typename T, int V, bool DONE>
 cudaError_t fwd(const gala_recurrence_args& a, cudaStream_t st) {
-    const RecurrenceGrid g = plan(a.steps, a.batch, a.dim, V);
-    if (g.pieces == 1) return launch_units(a.done ? recurrence_fwd_kernel<T, V, true, true> : recurrence_fwd_kernel<T, V, true, false>, a, g, true, st);
-    return launch_units(a.done ? recurrence_fwd_kernel<T, V, false, true> : recurrence_fwd_kernel<T, V, false, false>, a, g, false, st);
+    const RecurrenceGrid g = plan(a.steps, a.batch, a.dim, V, kFwdPiece);
+    if (a.steps == 1) return launch_units(recurrence_fwd_kernel<T, V, 1, true, DONE>, a, g, true, st);
+    if (a.steps <= 8) return launch_units(recurrence_fwd_kernel<T, V, 8, true, DONE>, a, g, true, st);
+    if (g.pieces == 1) return launch_units(recurrence_fwd_kernel<T, V, kFwdPiece, true, DONE>, a, g, true, st);
+    return launch_units(recurrence_fwd_kernel<T, V, kFwdPiece, false, DONE>, a, g, false, st);
+}
+template <typename T, int V, bool DONE>
+cudaError_t bwd(const gala_recurrence_grad_args& a, cudaStream_t st) {
+    const RecurrenceGrid g = plan(a.steps, a.batch, a.dim, V, kStateStep);
+    if (a.steps == 1) return launch_units(recurrence_bwd_kernel<T, V, 1, true, DONE>, a, g, true, st);
+    if (g.pieces == 1) return launch_units(recurrence_bwd_kernel<T, V, kStateStep, true, DONE>, a, g, true, st);
+    return launch_units(recurrence_bwd_kernel<T, V, kStateStep, false, DONE>, a, g, false, st);
 }
 template <typename T, int V>
-cudaError_t bwd(const gala_recurrence_grad_args& a, cudaStream_t st) {
-    const RecurrenceGrid g = plan(a.steps, a.batch, a.dim, V);
-    if (g.pieces == 1) return launch_units(a.done ? recurrence_bwd_kernel<T, V, true, true> : recurrence_bwd_kernel<T, V, true, false>, a, g, true, st);
-    return launch_units(a.done ? recurrence_bwd_kernel<T, V, false, true> : recurrence_bwd_kernel<T, V, false, false>, a, g, false, st);
+cudaError_t run(const gala_recurrence_args& a, cudaStream_t st) {
+    return a.done ? fwd<T, V, true>(a, st) : fwd<T, V, false>(a, st);
+}
+template <typename T, int V>
+cudaError_t run(const gala_recurrence_grad_args& a, cudaStream_t st) {
+    return a.done ? bwd<T, V, true>(a, st) : bwd<T, V, false>(a, st);
+}
+template <typename Args>
+cudaError_t by_type(const Args& a, bool two, cudaStream_t st) {
+    if (a.dtype == GALA_F32) return run<float, 1>(a, st);
+    if (a.dtype == GALA_BF16) return two ? run<__nv_bfloat16, 2>(a, st) : run<__nv_bfloat16, 1>(a, st);
+    return two ? run<__half, 2>(a, st) : run<__half, 1>(a, st);
 }
 
 cudaError_t pass(const float* src, float* dst, long long n, cudaStream_t st) {
@@ -404,7 +488,7 @@ cudaError_t pass(const float* src, float* dst, long long n, cudaStream_t st) {
     return launch_pdl(recurrence_pass_kernel, dim3((unsigned)(want < cap ? want : cap)), dim3(256), 0, st, src, dst, n);
 }
 
-// pairs of channels where every row of every array starts on a pair's boundary
+// pairs of 16-bit channels where every row of every array starts on a pair's boundary
 bool pairs(const void* q, long long st, long long sb, size_t es) { return aligned(q, 2 * es) && st % 2 == 0 && sb % 2 == 0; }
 
 // units of 32 channels, 8 blocks of a cluster each: the grid has to stay below 2^31 blocks
@@ -435,10 +519,7 @@ extern "C" int gala_gated_recurrence_forward(const gala_recurrence_args* p, void
         SAY("gala_gated_recurrence_forward: negative stride");
     if ((a.steps > 1 && a.h_t < a.dim) || (a.batch > 1 && a.h_b < a.dim)) SAY("gala_gated_recurrence_forward: rows of h overlap");
     const bool two = a.dim % 2 == 0 && pairs(a.f, a.f_t, a.f_b, es) && pairs(a.x, a.x_t, a.x_b, es) && pairs(a.h, a.h_t, a.h_b, es);
-    cudaError_t e;
-    if (a.dtype == GALA_F32) e = two ? fwd<float, 2>(a, st) : fwd<float, 1>(a, st);
-    else if (a.dtype == GALA_BF16) e = two ? fwd<__nv_bfloat16, 2>(a, st) : fwd<__nv_bfloat16, 1>(a, st);
-    else e = two ? fwd<__half, 2>(a, st) : fwd<__half, 1>(a, st);
+    const cudaError_t e = by_type(a, two, st);
     return launched(e, errbuf, errbuf_len, "gala_gated_recurrence_forward");
 }
 
@@ -464,9 +545,6 @@ extern "C" int gala_gated_recurrence_backward(const gala_recurrence_grad_args* p
         SAY("gala_gated_recurrence_backward: rows of df or dx overlap");
     const bool two = a.dim % 2 == 0 && pairs(a.f, a.f_t, a.f_b, es) && pairs(a.x, a.x_t, a.x_b, es) && (!a.dh || pairs(a.dh, a.dh_t, a.dh_b, es)) &&
                      pairs(a.df, a.df_t, a.df_b, es) && pairs(a.dx, a.dx_t, a.dx_b, es);
-    cudaError_t e;
-    if (a.dtype == GALA_F32) e = two ? bwd<float, 2>(a, st) : bwd<float, 1>(a, st);
-    else if (a.dtype == GALA_BF16) e = two ? bwd<__nv_bfloat16, 2>(a, st) : bwd<__nv_bfloat16, 1>(a, st);
-    else e = two ? bwd<__half, 2>(a, st) : bwd<__half, 1>(a, st);
+    const cudaError_t e = by_type(a, two, st);
     return launched(e, errbuf, errbuf_len, "gala_gated_recurrence_backward");
 }

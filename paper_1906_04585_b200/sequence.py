@@ -167,7 +167,7 @@ def gated_recurrence(f: torch.Tensor, x: torch.Tensor, h0: Optional[torch.Tensor
     a.steps, a.batch, a.dim = T, N, D
     h = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
     h_last = torch.empty((N, D), dtype=torch.float32, device=x.device) if h_last is None else h_last
-    states = torch.empty(((T + 15) // 16, N, D), dtype=torch.float32, device=x.device) if save else None
+    states = torch.empty(((T + 7) // 8, N, D), dtype=torch.float32, device=x.device) if save else None
     a.f, a.f_t, a.f_b = _steps("f", f, shape, x.dtype, x)
     a.x, a.x_t, a.x_b = _steps("x", x, shape, x.dtype, x)
     a.h, a.h_t, a.h_b = _steps("out", h, shape, x.dtype, x)
@@ -199,7 +199,7 @@ def gated_recurrence_backward(dh: Optional[torch.Tensor], f: torch.Tensor, x: to
     a.df, a.df_t, a.df_b = _steps("df", df, shape, x.dtype, x)
     a.dx, a.dx_t, a.dx_b = _steps("dx", dx, shape, x.dtype, x)
     a.done, a.done_t, a.done_b = _done(done, shape, x)
-    a.states = _flat("states", states, ((T + 15) // 16, N, D), torch.float32, x)
+    a.states = _flat("states", states, ((T + 7) // 8, N, D), torch.float32, x)
     a.dh_last = _flat("dh_last", dh_last, shape[1:], torch.float32, x)
     a.dh0 = _flat("dh0", dh0, shape[1:], torch.float32, x)
     B.gala_gated_recurrence_backward(a, st)

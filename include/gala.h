@@ -487,6 +487,35 @@ typedef struct {
 } gala_recurrence_grad_args;
 int gala_gated_recurrence_backward(const gala_recurrence_grad_args* a, void* stream, char* errbuf, int errbuf_len);
 
+/* One draw per row from filtered logits, by inverse CDF from the caller's uniforms as in gala_act.  Row r, with l its
+ * logits, m its largest, T its temperature, and the weight of entry i w_i = exp((l_i - m) / T), or 1 where l_i = m:
+ *   1. rank the entries by l, largest first, ties by lowest index first (a NaN counts as -inf);
+ *   2. top-k: keep the first k;
+ *   3. top-p: of those, keep an entry while the weights ranked before it sum to less than p times the kept sum (the
+ *      first always stays);
+ *   4. min-p: of those, keep w_i >= min_p (the largest always stay);
+ *   5. token = min{ i : sum over kept j <= i of w_j > u * sum over kept w }, in the order of the index; its
+ *      log-probability is log(w_token / sum over kept w).
+ * Weights are summed as whole multiples of 2^-44 in 64 bits, so the result does not depend on the order of summation.
+ * T <= 0: the largest entry, lowest index first, log-probability 0.  A row without an entry above -inf: token -1 and
+ * log-probability -inf.  temperature (= 1), top_k, top_p, min_p (= no filter) are [rows] or NULL; k <= 0, p >= 1 and
+ * min_p <= 0 switch that filter off for the row.  uniforms [rows] in [0, 1).  logprobs may be NULL.
+ * 1 <= vocab <= 262144, 0 <= rows < 2^27. */
+typedef struct {
+    int dtype;                 /* of logits */
+    long long rows;
+    int vocab;
+    const void* logits;        long long logits_ld;
+    const float* uniforms;
+    const float* temperature;
+    const int* top_k;
+    const float* top_p;
+    const float* min_p;
+    int* tokens;               /* [rows] */
+    float* logprobs;           /* [rows] */
+} gala_sample_args;
+int gala_sample(const gala_sample_args* a, void* stream, char* errbuf, int errbuf_len);
+
 #ifdef __cplusplus
 }
 #endif

@@ -91,6 +91,13 @@ class gala_recurrence_grad_args(C.Structure):
                 ("dx", C.c_void_p), ("dx_t", C.c_longlong), ("dx_b", C.c_longlong), ("dh0", C.c_void_p)]
 
 
+class gala_sample_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("rows", C.c_longlong), ("vocab", C.c_int), ("logits", C.c_void_p),
+                ("logits_ld", C.c_longlong), ("uniforms", C.c_void_p), ("temperature", C.c_void_p),
+                ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("tokens", C.c_void_p),
+                ("logprobs", C.c_void_p)]
+
+
 EXPORTS = (
     "gala_create", "gala_destroy", "gala_act", "gala_learn", "gala_gossip", "gala_step_sync",
     "gala_sync_agent", "gala_sync_all", "gala_in_peers", "gala_get_state", "gala_set_state",
@@ -105,6 +112,7 @@ EXPORTS = (
     "gala_debug_wait_runs_out",
     "gala_layer_norm_forward", "gala_layer_norm_backward", "gala_layer_norm_workspace",
     "gala_gated_recurrence_forward", "gala_gated_recurrence_backward",
+    "gala_sample",
 )
 
 _lib = None
@@ -173,6 +181,7 @@ def lib() -> C.CDLL:
             "gala_layer_norm_workspace": (ll, [ll, i]),
             "gala_gated_recurrence_forward": (i, [C.POINTER(gala_recurrence_args), vp, C.c_char_p, i]),
             "gala_gated_recurrence_backward": (i, [C.POINTER(gala_recurrence_grad_args), vp, C.c_char_p, i]),
+            "gala_sample": (i, [C.POINTER(gala_sample_args), vp, C.c_char_p, i]),
             "gala_sweep_sync": (i, [vp, vp, vp, vp, i, ll, C.POINTER(gala_topology), ll, C.POINTER(gala_hparams), vp]),
         }
         for name, (res, args) in sig.items():
@@ -497,6 +506,10 @@ def gala_gated_recurrence_forward(args: gala_recurrence_args, stream=None):
 
 def gala_gated_recurrence_backward(args: gala_recurrence_grad_args, stream=None):
     _operator("gala_gated_recurrence_backward", args, stream)
+
+
+def gala_sample(args: gala_sample_args, stream=None):
+    _operator("gala_sample", args, stream)
 
 
 def default_hparams(n_envs: int, n_steps: int, **kw) -> gala_hparams:

@@ -204,3 +204,31 @@ def gated_recurrence_backward(dh: Optional[torch.Tensor], f: torch.Tensor, x: to
     a.dh0 = _flat("dh0", dh0, shape[1:], torch.float32, x)
     B.gala_gated_recurrence_backward(a, st)
     return df, dx, dh0
+
+
+# ---------------------------------------------------------------------------------------------- drawing a token
+def sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+           top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, *, out: Optional[torch.Tensor] = None,
+           logprobs: Optional[torch.Tensor] = None):
+    """One token a row of logits [rows, vocab], drawn by inverse CDF in the order of the index from the caller's uniforms
+    [rows] in [0, 1) after temperature, top-k, top-p and min-p (each [rows] or None).  Returns (tokens int32, logprobs
+    float32): the log-probability is that of the distribution that was drawn from.  Temperature <= 0 takes the largest
+    entry; a row that is all -inf (or NaN) gives token -1."""
+    st = _stream(logits)
+    if logits.dim() != 2:
+        raise ValueError("logits has to be a matrix [rows, vocab]")
+    a = B.gala_sample_args()
+    a.dtype, shape = _type_of(logits), logits.shape
+    a.rows, a.vocab = shape[0], shape[1]
+    tokens = torch.empty(shape[0], dtype=torch.int32, device=logits.device) if out is None else out
+    logprobs = torch.empty(shape[0], dtype=torch.float32, device=logits.device) if logprobs is None else logprobs
+    a.logits, a.logits_ld = _rows("logits", logits, shape, logits)
+    a.uniforms = _flat("uniforms", uniforms, shape[:1], torch.float32, logits)
+    a.temperature = _flat("temperature", temperature, shape[:1], torch.float32, logits)
+    a.top_k = _flat("top_k", top_k, shape[:1], torch.int32, logits)
+    a.top_p = _flat("top_p", top_p, shape[:1], torch.float32, logits)
+    a.min_p = _flat("min_p", min_p, shape[:1], torch.float32, logits)
+    a.tokens = _flat("out", tokens, shape[:1], torch.int32, logits)
+    a.logprobs = _flat("logprobs", logprobs, shape[:1], torch.float32, logits)
+    B.gala_sample(a, st)
+    return tokens, logprobs

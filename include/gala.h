@@ -516,6 +516,61 @@ typedef struct {
 } gala_sample_args;
 int gala_sample(const gala_sample_args* a, void* stream, char* errbuf, int errbuf_len);
 
+/* Gated feed-forward block on the tensor cores, for 16-bit types (float32 is refused: there is no 32-bit operand format):
+ *   g = x w_gate^T    u = x w_up^T    p = act(g) u    y = p w_down^T
+ * x, y [rows][dim], w_gate, w_up [hidden][dim], w_down [dim][hidden]; products are accumulated in float32.  Both
+ * projections, the activation and the product are one kernel; p is rounded once to the element type, being an operand
+ * of the next product.  `product` [rows][hidden_ld] receives p.  With gate and up (both or neither) g and u are stored as
+ * well, rounded, for the backward call.  act: GALA_ACT_SILU g sigmoid(g), GALA_ACT_GELU g Phi(g) (the exact form),
+ * GALA_ACT_RELU max(g, 0).  Rows of every matrix start on 16-byte boundaries (pointers 16-byte aligned, strides multiples
+ * of 8); sizes are free: 0 <= rows < 2^31 - 256, 1 <= dim, hidden <= 2^20.
+ * status (DEVICE int, may be NULL): set to 1 if a bounded wait inside a kernel ran out, never cleared. */
+typedef enum { GALA_ACT_SILU = 0, GALA_ACT_GELU = 1, GALA_ACT_RELU = 2 } gala_act_kind;
+typedef struct {
+    int dtype, act;
+    long long rows;
+    int dim, hidden;
+    const void* x;             long long x_ld;
+    const void* w_gate;        long long w_gate_ld;
+    const void* w_up;          long long w_up_ld;
+    const void* w_down;        long long w_down_ld;
+    void* y;                   long long y_ld;
+    void* product;
+    void* gate;
+    void* up;
+    long long hidden_ld;       /* of product, gate and up */
+    int* status;
+} gala_ffn_args;
+int gala_gated_ffn_forward(const gala_ffn_args* a, void* stream, char* errbuf, int errbuf_len);
+
+/* Its gradient.  With dp = dy w_down:  du = dp act(g)   dg = dp u act'(g)   dx = dg w_gate + du w_up
+ *   dw_gate = dg^T x    dw_up = du^T x    dw_down = dy^T p
+ * gate, up, product: the forward call's.  dgate, dup [rows][hidden_ld]: workspace, receive dg and du rounded to the
+ * element type (operands of the next products); they may be gate and up themselves.  dx, and any of the three weight
+ * gradients, may be NULL. */
+typedef struct {
+    int dtype, act;
+    long long rows;
+    int dim, hidden;
+    const void* dy;            long long dy_ld;
+    const void* x;             long long x_ld;
+    const void* w_gate;        long long w_gate_ld;
+    const void* w_up;          long long w_up_ld;
+    const void* w_down;        long long w_down_ld;
+    const void* product;
+    const void* gate;
+    const void* up;
+    void* dgate;
+    void* dup;
+    long long hidden_ld;       /* of product, gate, up, dgate and dup */
+    void* dx;                  long long dx_ld;
+    void* dw_gate;             long long dw_gate_ld;
+    void* dw_up;               long long dw_up_ld;
+    void* dw_down;             long long dw_down_ld;
+    int* status;
+} gala_ffn_grad_args;
+int gala_gated_ffn_backward(const gala_ffn_grad_args* a, void* stream, char* errbuf, int errbuf_len);
+
 #ifdef __cplusplus
 }
 #endif

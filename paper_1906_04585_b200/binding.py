@@ -98,6 +98,28 @@ class gala_sample_args(C.Structure):
                 ("logprobs", C.c_void_p)]
 
 
+GALA_ACT_SILU, GALA_ACT_GELU, GALA_ACT_RELU = 0, 1, 2
+
+
+class gala_ffn_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("act", C.c_int), ("rows", C.c_longlong), ("dim", C.c_int), ("hidden", C.c_int),
+                ("x", C.c_void_p), ("x_ld", C.c_longlong), ("w_gate", C.c_void_p), ("w_gate_ld", C.c_longlong),
+                ("w_up", C.c_void_p), ("w_up_ld", C.c_longlong), ("w_down", C.c_void_p), ("w_down_ld", C.c_longlong),
+                ("y", C.c_void_p), ("y_ld", C.c_longlong), ("product", C.c_void_p), ("gate", C.c_void_p),
+                ("up", C.c_void_p), ("hidden_ld", C.c_longlong), ("status", C.c_void_p)]
+
+
+class gala_ffn_grad_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("act", C.c_int), ("rows", C.c_longlong), ("dim", C.c_int), ("hidden", C.c_int),
+                ("dy", C.c_void_p), ("dy_ld", C.c_longlong), ("x", C.c_void_p), ("x_ld", C.c_longlong),
+                ("w_gate", C.c_void_p), ("w_gate_ld", C.c_longlong), ("w_up", C.c_void_p), ("w_up_ld", C.c_longlong),
+                ("w_down", C.c_void_p), ("w_down_ld", C.c_longlong), ("product", C.c_void_p), ("gate", C.c_void_p),
+                ("up", C.c_void_p), ("dgate", C.c_void_p), ("dup", C.c_void_p), ("hidden_ld", C.c_longlong),
+                ("dx", C.c_void_p), ("dx_ld", C.c_longlong), ("dw_gate", C.c_void_p), ("dw_gate_ld", C.c_longlong),
+                ("dw_up", C.c_void_p), ("dw_up_ld", C.c_longlong), ("dw_down", C.c_void_p), ("dw_down_ld", C.c_longlong),
+                ("status", C.c_void_p)]
+
+
 EXPORTS = (
     "gala_create", "gala_destroy", "gala_act", "gala_learn", "gala_gossip", "gala_step_sync",
     "gala_sync_agent", "gala_sync_all", "gala_in_peers", "gala_get_state", "gala_set_state",
@@ -112,7 +134,7 @@ EXPORTS = (
     "gala_debug_wait_runs_out",
     "gala_layer_norm_forward", "gala_layer_norm_backward", "gala_layer_norm_workspace",
     "gala_gated_recurrence_forward", "gala_gated_recurrence_backward",
-    "gala_sample",
+    "gala_sample", "gala_gated_ffn_forward", "gala_gated_ffn_backward",
 )
 
 _lib = None
@@ -182,6 +204,8 @@ def lib() -> C.CDLL:
             "gala_gated_recurrence_forward": (i, [C.POINTER(gala_recurrence_args), vp, C.c_char_p, i]),
             "gala_gated_recurrence_backward": (i, [C.POINTER(gala_recurrence_grad_args), vp, C.c_char_p, i]),
             "gala_sample": (i, [C.POINTER(gala_sample_args), vp, C.c_char_p, i]),
+            "gala_gated_ffn_forward": (i, [C.POINTER(gala_ffn_args), vp, C.c_char_p, i]),
+            "gala_gated_ffn_backward": (i, [C.POINTER(gala_ffn_grad_args), vp, C.c_char_p, i]),
             "gala_sweep_sync": (i, [vp, vp, vp, vp, i, ll, C.POINTER(gala_topology), ll, C.POINTER(gala_hparams), vp]),
         }
         for name, (res, args) in sig.items():
@@ -510,6 +534,14 @@ def gala_gated_recurrence_backward(args: gala_recurrence_grad_args, stream=None)
 
 def gala_sample(args: gala_sample_args, stream=None):
     _operator("gala_sample", args, stream)
+
+
+def gala_gated_ffn_forward(args: gala_ffn_args, stream=None):
+    _operator("gala_gated_ffn_forward", args, stream)
+
+
+def gala_gated_ffn_backward(args: gala_ffn_grad_args, stream=None):
+    _operator("gala_gated_ffn_backward", args, stream)
 
 
 def default_hparams(n_envs: int, n_steps: int, **kw) -> gala_hparams:

@@ -91,8 +91,8 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     elif sum_out is not None:
         raise ValueError("sum_out without residual")
     stats = torch.empty((2, shape[0]), dtype=torch.float32, device=x.device)
-    a.mean = stats.data_ptr()
-    a.rstd = a.mean + 4 * shape[0] if shape[0] else a.mean
+    first = stats.data_ptr()
+    a.mean, a.rstd = first, first + 4 * shape[0]
     B.gala_layer_norm_forward(a, st)
     return y, s, stats[0], stats[1]
 
@@ -204,6 +204,92 @@ def gated_recurrence_backward(dh: Optional[torch.Tensor], f: torch.Tensor, x: to
     a.dh0 = _flat("dh0", dh0, shape[1:], torch.float32, x)
     B.gala_gated_recurrence_backward(a, st)
     return df, dx, dh0
+
+
+# ---------------------------------------------------------------------------------------------- gated feed-forward
+_ACT = {"silu": B.GALA_ACT_SILU, "gelu": B.GALA_ACT_GELU, "relu": B.GALA_ACT_RELU}
+_status = {}
+
+
+def _status_word(device) -> torch.Tensor:
+    word = _status.get(device)
+    if word is None:
+        word = _status[device] = torch.zeros(1, dtype=torch.int32, device=device)
+    return word
+
+
+def check() -> None:
+    """Waits for the current stream and raises if a bounded wait inside a kernel of this module ran out since the last
+    check (results since then are not to be trusted); the word is cleared."""
+    for word in _status.values():
+        if int(word.item()):
+            word.zero_()
+            raise B.GalaError(B.GALA_ECUDA, "a bounded device-side wait ran out")
+
+
+def _ffn_shapes(a, x, w_gate, w_up, w_down, act):
+    if x.dim() != 2 or w_gate.dim() != 2:
+        raise ValueError("x has to be [rows, dim], the weights [hidden, dim] and [dim, hidden]")
+    rows, dim = x.shape
+    hidden = w_gate.shape[0]
+    try:
+        a.act = _ACT[act]
+    except KeyError:
+        raise ValueError("activation %r: one of %s is needed" % (act, ", ".join(_ACT))) from None
+    a.dtype, a.rows, a.dim, a.hidden = _type_of(x), rows, dim, hidden
+    a.x, a.x_ld = _rows("x", x, (rows, dim), x)
+    a.w_gate, a.w_gate_ld = _rows("w_gate", w_gate, (hidden, dim), x)
+    a.w_up, a.w_up_ld = _rows("w_up", w_up, (hidden, dim), x)
+    a.w_down, a.w_down_ld = _rows("w_down", w_down, (dim, hidden), x)
+    a.hidden_ld = (hidden + 7) // 8 * 8
+    a.status = _status_word(x.device).data_ptr()
+    return rows, dim, hidden
+
+
+def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, activation: str = "silu", *,
+              out: Optional[torch.Tensor] = None, save: bool = False):
+    """y = (act(x w_gate^T) * (x w_up^T)) w_down^T for x [rows, dim], w_gate and w_up [hidden, dim], w_down [dim, hidden],
+    all bfloat16 or all float16; activation "silu", "gelu" or "relu".  Every matrix starts on a 16-byte boundary and has a
+    row stride that is a multiple of 8.  Returns (y, saved); saved is what the backward call needs (None unless `save`)."""
+    st = _stream(x)
+    a = B.gala_ffn_args()
+    rows, dim, hidden = _ffn_shapes(a, x, w_gate, w_up, w_down, activation)
+    if out is None:
+        out = torch.empty((rows, (dim + 7) // 8 * 8), dtype=x.dtype, device=x.device)[:, :dim]
+    a.y, a.y_ld = _rows("out", out, (rows, dim), x)
+    kept = torch.empty((3 if save else 1, rows, a.hidden_ld), dtype=x.dtype, device=x.device)
+    first, size = kept.data_ptr(), 2 * rows * a.hidden_ld
+    a.product = first
+    if save:
+        a.gate, a.up = first + size, first + 2 * size
+    B.gala_gated_ffn_forward(a, st)
+    return out, kept if save else None
+
+
+def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, saved: torch.Tensor,
+                       activation: str = "silu", *, dx: Optional[torch.Tensor] = None, dw_gate: Optional[torch.Tensor] = None,
+                       dw_up: Optional[torch.Tensor] = None, dw_down: Optional[torch.Tensor] = None):
+    """Gradients (dx, dw_gate, dw_up, dw_down) of gated_ffn from dy [rows, dim]; saved is the forward call's."""
+    st = _stream(x)
+    a = B.gala_ffn_grad_args()
+    rows, dim, hidden = _ffn_shapes(a, x, w_gate, w_up, w_down, activation)
+
+    def grad(t, n, m):
+        return torch.empty((n, (m + 7) // 8 * 8), dtype=x.dtype, device=x.device)[:, :m] if t is None else t
+
+    dx, dw_gate, dw_up, dw_down = grad(dx, rows, dim), grad(dw_gate, hidden, dim), grad(dw_up, hidden, dim), grad(dw_down, dim, hidden)
+    a.dy, a.dy_ld = _rows("dy", dy, (rows, dim), x)
+    a.dx, a.dx_ld = _rows("dx", dx, (rows, dim), x)
+    a.dw_gate, a.dw_gate_ld = _rows("dw_gate", dw_gate, (hidden, dim), x)
+    a.dw_up, a.dw_up_ld = _rows("dw_up", dw_up, (hidden, dim), x)
+    a.dw_down, a.dw_down_ld = _rows("dw_down", dw_down, (dim, hidden), x)
+    first, size = _flat("saved", saved, (3, rows, a.hidden_ld), x.dtype, x), 2 * rows * a.hidden_ld
+    a.product, a.gate, a.up = first, first + size, first + 2 * size
+    work = torch.empty((2, rows, a.hidden_ld), dtype=x.dtype, device=x.device)
+    first = work.data_ptr()
+    a.dgate, a.dup = first, first + size
+    B.gala_gated_ffn_backward(a, st)
+    return dx, dw_gate, dw_up, dw_down
 
 
 # ---------------------------------------------------------------------------------------------- drawing a token

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import threading
 from typing import Optional, Sequence
 
 import numpy as np
@@ -501,10 +502,20 @@ def gala_sweep_agents(x, g, v, snap, clip, n_agents: int, n_slots: int, d_padded
         raise GalaError(rc, "gala_sweep_agents")
 
 
+class _Message(threading.local):
+    """The calling thread's message buffer."""
+
+    def __init__(self):
+        self.buf = C.create_string_buffer(512)
+
+
+_message = _Message()
+
+
 def _operator(name: str, args, stream):
     """One of the stand-alone operators: its argument struct, the caller's stream, the library's message on failure."""
-    buf = C.create_string_buffer(512)
-    rc = getattr(lib(), name)(C.byref(args), stream, buf, 512)
+    buf = _message.buf
+    rc = getattr(_lib or lib(), name)(C.byref(args), stream, buf, 512)
     if rc < 0:
         raise GalaError(rc, buf.value.decode() or name)
 

@@ -18,18 +18,24 @@ import torch
 from . import binding as B
 
 _DTYPE = {torch.float32: B.GALA_F32, torch.bfloat16: B.GALA_BF16, torch.float16: B.GALA_F16}
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+# A call on small tensors is bound by this file: the checks below look at a tensor that is as it should be with four
+# cheap questions and go into words only where one of them is answered with no.
 
 
 def _stream(t: torch.Tensor) -> int:
     if not t.is_cuda:
         raise ValueError("CUDA tensors are needed: there is no CPU fallback")
-    if t.device.index != torch.cuda.current_device():
+    index = t.get_device()
+    if index != _current_device():
         raise ValueError("tensors are on %s, the current device is cuda:%d" % (t.device, torch.cuda.current_device()))
-    return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(index)
 
 
 def _want(name: str, t: torch.Tensor, shape, dtype, like: torch.Tensor):
-    if t.shape != shape:
+    if tuple(t.shape) != tuple(shape):
         raise ValueError("%s is %s, not %s" % (name, tuple(t.shape), tuple(shape)))
     if t.dtype != dtype:
         raise TypeError("%s is %s, not %s" % (name, t.dtype, dtype))
@@ -41,6 +47,8 @@ def _rows(name: str, t: Optional[torch.Tensor], shape, like: torch.Tensor):
     """Pointer and row stride of a matrix with contiguous columns (None: nothing)."""
     if t is None:
         return None, 0
+    if t.is_contiguous() and t.dtype is like.dtype and t.shape == shape and t.get_device() == like.get_device():
+        return t.data_ptr(), shape[1]
     _want(name, t, shape, like.dtype, like)
     if shape[1] > 1 and t.stride(1) != 1:
         raise ValueError("the columns of %s have to be contiguous" % name)
@@ -52,10 +60,10 @@ def _flat(name: str, t: Optional[torch.Tensor], shape, dtype, like: torch.Tensor
     """Pointer of a contiguous tensor (None: nothing)."""
     if t is None:
         return None
+    if t.is_contiguous() and t.dtype is dtype and t.shape == shape and t.get_device() == like.get_device():
+        return t.data_ptr()
     _want(name, t, shape, dtype, like)
-    if not t.is_contiguous():
-        raise ValueError("%s has to be contiguous" % name)
-    return t.data_ptr()
+    raise ValueError("%s has to be contiguous" % name)
 
 
 def _type_of(t: torch.Tensor) -> int:
@@ -90,11 +98,10 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
         a.sum, a.sum_ld = _rows("sum_out", s, shape, x)
     elif sum_out is not None:
         raise ValueError("sum_out without residual")
-    stats = torch.empty((2, shape[0]), dtype=torch.float32, device=x.device)
-    first = stats.data_ptr()
-    a.mean, a.rstd = first, first + 4 * shape[0]
+    mean, rstd = torch.empty((2, shape[0]), dtype=torch.float32, device=x.device).unbind(0)
+    a.mean, a.rstd = mean.data_ptr(), rstd.data_ptr()
     B.gala_layer_norm_forward(a, st)
-    return y, s, stats[0], stats[1]
+    return y, s, mean, rstd
 
 
 def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, weight: Optional[torch.Tensor] = None, *,
@@ -135,10 +142,12 @@ def _steps(name: str, t: Optional[torch.Tensor], shape, dtype, like: torch.Tenso
     """Pointer and the strides of time and sequence of a [steps, batch, dim] tensor with contiguous channels."""
     if t is None:
         return None, 0, 0
-    _want(name, t, shape, dtype, like)
-    if shape[2] > 1 and t.stride(2) != 1:
+    if not (t.dtype is dtype and t.shape == shape and t.get_device() == like.get_device()):
+        _want(name, t, shape, dtype, like)
+    time, sequence, channel = t.stride()
+    if channel != 1 and shape[2] > 1:
         raise ValueError("the channels of %s have to be contiguous" % name)
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    return t.data_ptr(), time, sequence
 
 
 def _done(done: Optional[torch.Tensor], shape, like: torch.Tensor):

@@ -4,13 +4,15 @@
 //   xh = (s - m) rstd     e = dy w      dx = rstd (e - mean e - xh mean(e xh)) (+ dsum)
 //   dw = sum_rows dy xh   db = sum_rows dy
 //
-// Both passes are bound by memory: what counts is that every byte is moved once and that enough rows are under way.
-// Forward: a row lies in the registers of 32..1024 threads, as stored, and is widened anew for each of the three passes
-// over it (sum, centred sum of squares - no E[s^2] - m^2 cancellation -, result), so that 32 warps fit an SM.
-// Backward: a thread has 16 columns, keeps their two column sums in registers over all rows that its block walks over,
-// and reads x and dy through a private ring in shared memory that asynchronous copies fill up to four rows ahead (no
-// barrier: a thread reads only what it copied).  The groups of a block then add their column sums through shared memory and leave
-// one row of partial sums a block; a second kernel adds those in a fixed order.
+// Both passes are bound by memory: what counts is that every byte is moved once, that enough rows are under way, and
+// that an element costs few instructions.  A thread has 16 columns of a row and keeps their weights in registers over all
+// rows that it works on; a row is held as stored and widened anew for each pass over it.
+// Forward: up to four rows at a time, so that their loads are under way together and the barriers of wide rows are shared;
+// sum, centred sum of squares (no E[s^2] - m^2 cancellation), result.
+// Backward: the two column sums of a thread's columns stay in registers over all rows of its block; x, dy and dsum come
+// through a private ring in shared memory that asynchronous copies fill up to four rows ahead (no barrier: a thread reads only
+// what it copied).  The groups of a block then add their column sums through shared memory and leave one row of partial
+// sums a block; a second kernel adds those in a fixed order.
 #include "sequence.cuh"
 
 namespace gala {
@@ -18,8 +20,9 @@ namespace gala {
 constexpr int kMaxCols = 16384;
 constexpr int kBwdThreads = 512;
 // Rows of a group in the ring of the backward kernel: as many as 200 KB of shared memory hold, at most four.
-template <int THREADS, int ELEM> constexpr int kRingFit = 200 * 1024 / (2 * 16 * ELEM * THREADS);
-template <int THREADS, int ELEM> constexpr int kRingRows = kRingFit<THREADS, ELEM> > 4 ? 4 : kRingFit<THREADS, ELEM>;
+template <int THREADS, int ELEM, int ARRAYS> constexpr int kRingFit = 200 * 1024 / (ARRAYS * 16 * ELEM * THREADS);
+template <int THREADS, int ELEM, int ARRAYS>
+constexpr int kRingRows = kRingFit<THREADS, ELEM, ARRAYS> > 4 ? 4 : kRingFit<THREADS, ELEM, ARRAYS>;
 
 // V elements from column c on; columns at or past `cols` read as 0
 template <typename T, int V>
@@ -50,112 +53,146 @@ __device__ __forceinline__ void store_cols(T* row, int c, int cols, const float 
             if (c + j < cols) row[c + j] = from_f32<T>(f[j]);
     }
 }
-// V weights from column c on, whatever their type
-template <typename W, int V>
-__device__ __forceinline__ void load_weights(const W* w, int c, int cols, float (&f)[V]) {
-    if (V > 1 && c + V <= cols) {
-        constexpr int N = 16 / (int)sizeof(W) < V ? 16 / (int)sizeof(W) : V;    // weights of one 16-byte load
-#pragma unroll
-        for (int k = 0; k < V / N; k++) {
-            const Vec<W, N> p = *reinterpret_cast<const Vec<W, N>*>(w + c + k * N);
-#pragma unroll
-            for (int j = 0; j < N; j++) f[k * N + j] = p.get(j);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; j++) f[j] = c + j < cols ? to_f32<W>(w[c + j]) : 0.0f;
-    }
-}
-
-// Sum over the `tpr` threads of a row group, the same bits in all of them.  buf: 32 floats of the group; two calls that
-// use the same buf need another group barrier between them.
-__device__ __forceinline__ float group_sum(float v, int tpr, int group, float* buf) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if (tpr == 32) return v;
-    const int t = threadIdx.x % tpr;
-    if ((t & 31) == 0) buf[t >> 5] = v;
-    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(tpr) : "memory");
-    float s = (t & 31) < (tpr >> 5) ? buf[t & 31] : 0.0f;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    return s;
-}
-
-template <typename T, typename W, int V, int NV, bool RES, int MAXT>
-__global__ void __launch_bounds__(MAXT, 1024 / MAXT) layer_norm_fwd_kernel(const gala_layer_norm_args a, const int tpr) {
-    __shared__ float red[2][8][32];
-    const int group = threadIdx.x / tpr, groups = blockDim.x / tpr, t = threadIdx.x % tpr;
-    const int cols = a.cols;
-    pdl_wait();
-    pdl_launch();
-    for (long long row = (long long)blockIdx.x * groups + group; row < a.rows; row += (long long)gridDim.x * groups) {
-        const T* xr = static_cast<const T*>(a.x) + row * a.x_ld;
-        const T* rr = RES ? static_cast<const T*>(a.residual) + row * a.residual_ld : nullptr;
-        Vec<T, V> x[NV], res[RES ? NV : 1];
-#pragma unroll
-        for (int i = 0; i < NV; i++) x[i] = load_cols<T, V>(xr, (t + i * tpr) * V, cols);
-        if (RES) {
-#pragma unroll
-            for (int i = 0; i < NV; i++) res[RES ? i : 0] = load_cols<T, V>(rr, (t + i * tpr) * V, cols);
-        }
-        auto value = [&](int i, int j) { return RES ? x[i].get(j) + res[RES ? i : 0].get(j) : x[i].get(j); };
-        float sum = 0.0f;
+// The weights of a thread's columns, as stored: NV times V columns, tpr * V apart.
+template <typename W, int V, int NV>
+struct Weights {
+    static constexpr int N = 16 / (int)sizeof(W) < V ? 16 / (int)sizeof(W) : V;    // of one load
+    Vec<W, N> w[NV][V / N];
+    __device__ __forceinline__ void load(const W* p, int t, int tpr, int cols) {
 #pragma unroll
         for (int i = 0; i < NV; i++)
 #pragma unroll
-            for (int j = 0; j < V; j++) sum += value(i, j);
-        const float mean = group_sum(sum, tpr, group, red[0][group & 7]) / (float)cols;
-        float sq = 0.0f;
+            for (int k = 0; k < V / N; k++) w[i][k] = load_cols<W, N>(p, (t + i * tpr) * V + k * N, cols);
+    }
+    __device__ __forceinline__ float get(int i, int j) const { return w[i][j / N].get(j % N); }
+};
+
+// R sums over the `tpr` threads of a row group, the same bits in all of them.  buf: [R][32] floats of the group, 16-byte
+// aligned; two calls that use the same buf need another group barrier between them.
+template <int R>
+__device__ __forceinline__ void group_sums(float (&v)[R], int tpr, int group, float (*buf)[32]) {
 #pragma unroll
-        for (int i = 0; i < NV; i++) {
-            const int c = (t + i * tpr) * V;
-            if (c + V <= cols) {
+    for (int r = 0; r < R; r++)
 #pragma unroll
-                for (int j = 0; j < V; j++) {
-                    const float d = value(i, j) - mean;
-                    sq = fmaf(d, d, sq);
-                }
-            } else {
+        for (int o = 16; o > 0; o >>= 1) v[r] += __shfl_xor_sync(0xffffffffu, v[r], o);
+    if (tpr == 32) return;
+    const int t = threadIdx.x % tpr, warps = tpr >> 5;
+    if ((t & 31) == 0) {
 #pragma unroll
-                for (int j = 0; j < V; j++) {
-                    const float d = value(i, j) - mean;
-                    if (c + j < cols) sq = fmaf(d, d, sq);
+        for (int r = 0; r < R; r++) buf[r][t >> 5] = v[r];
+    }
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(tpr) : "memory");
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+        if (warps == 2) {
+            v[r] = buf[r][0] + buf[r][1];
+        } else {
+            float s = 0.0f;
+            for (int k = 0; k < warps; k += 4) {
+                const float4 q = *reinterpret_cast<const float4*>(&buf[r][k]);
+                s += (q.x + q.y) + (q.z + q.w);
+            }
+            v[r] = s;
+        }
+    }
+}
+
+template <typename T, typename W, int V, int NV, int R, bool RES, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT == 256 ? 2 : 1) layer_norm_fwd_kernel(const gala_layer_norm_args a, const int tpr) {
+    __shared__ __align__(16) float red[2][8][R][32];
+    const int group = threadIdx.x / tpr, groups = blockDim.x / tpr, t = threadIdx.x % tpr;
+    const int cols = a.cols;
+    const float inv = 1.0f / (float)cols;
+    pdl_wait();
+    pdl_launch();
+    Weights<W, V, NV> w, b;
+    if (a.weight) w.load(static_cast<const W*>(a.weight), t, tpr, cols);
+    if (a.bias) b.load(static_cast<const W*>(a.bias), t, tpr, cols);
+    for (long long row = ((long long)blockIdx.x * groups + group) * R; row < a.rows; row += (long long)gridDim.x * groups * R) {
+        const int n = a.rows - row < R ? (int)(a.rows - row) : R;
+        const T* xr = static_cast<const T*>(a.x) + row * a.x_ld;
+        Vec<T, V> x[R][NV], res[RES ? R : 1][NV];
+#pragma unroll
+        for (int r = 0; r < R; r++)
+#pragma unroll
+            for (int i = 0; i < NV; i++) x[r][i] = load_cols<T, V>(xr + min(r, n - 1) * a.x_ld, (t + i * tpr) * V, cols);
+        if (RES) {
+            const T* rr = static_cast<const T*>(a.residual) + row * a.residual_ld;
+#pragma unroll
+            for (int r = 0; r < R; r++)
+#pragma unroll
+                for (int i = 0; i < NV; i++) res[RES ? r : 0][i] = load_cols<T, V>(rr + min(r, n - 1) * a.residual_ld, (t + i * tpr) * V, cols);
+        }
+        auto value = [&](int r, int i, int j) { return RES ? x[r][i].get(j) + res[RES ? r : 0][i].get(j) : x[r][i].get(j); };
+        float mean[R], rstd[R];
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            mean[r] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NV; i++)
+#pragma unroll
+                for (int j = 0; j < V; j++) mean[r] += value(r, i, j);
+        }
+        group_sums<R>(mean, tpr, group, red[0][group]);
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            mean[r] *= inv;
+            rstd[r] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                const int c = (t + i * tpr) * V;
+                if (c + V <= cols) {
+#pragma unroll
+                    for (int j = 0; j < V; j++) {
+                        const float d = value(r, i, j) - mean[r];
+                        rstd[r] = fmaf(d, d, rstd[r]);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; j++) {
+                        const float d = value(r, i, j) - mean[r];
+                        if (c + j < cols) rstd[r] = fmaf(d, d, rstd[r]);
+                    }
                 }
             }
         }
-        const float var = group_sum(sq, tpr, group, red[1][group & 7]) / (float)cols;
-        const float rstd = 1.0f / sqrtf(var + a.eps);
-        T* yr = static_cast<T*>(a.y) + row * a.y_ld;
-        T* sr = RES && a.sum ? static_cast<T*>(a.sum) + row * a.sum_ld : nullptr;
+        group_sums<R>(rstd, tpr, group, red[1][group]);
 #pragma unroll
-        for (int i = 0; i < NV; i++) {
-            const int c = (t + i * tpr) * V;
-            if (c < cols) {
-                float o[V], w[V];
-                if (RES && sr) {
+        for (int r = 0; r < R; r++) {
+            rstd[r] = 1.0f / sqrtf(fmaf(rstd[r], inv, a.eps));
+            if (r < n) {
+                T* yr = static_cast<T*>(a.y) + (row + r) * a.y_ld;
+                T* sr = RES && a.sum ? static_cast<T*>(a.sum) + (row + r) * a.sum_ld : nullptr;
 #pragma unroll
-                    for (int j = 0; j < V; j++) o[j] = value(i, j);
-                    store_cols<T, V>(sr, c, cols, o);
+                for (int i = 0; i < NV; i++) {
+                    const int c = (t + i * tpr) * V;
+                    if (c < cols) {
+                        float o[V];
+                        if (RES && sr) {
+#pragma unroll
+                            for (int j = 0; j < V; j++) o[j] = value(r, i, j);
+                            store_cols<T, V>(sr, c, cols, o);
+                        }
+#pragma unroll
+                        for (int j = 0; j < V; j++) o[j] = (value(r, i, j) - mean[r]) * rstd[r];
+                        if (a.weight && a.bias) {
+#pragma unroll
+                            for (int j = 0; j < V; j++) o[j] = fmaf(o[j], w.get(i, j), b.get(i, j));
+                        } else if (a.weight) {
+#pragma unroll
+                            for (int j = 0; j < V; j++) o[j] *= w.get(i, j);
+                        } else if (a.bias) {
+#pragma unroll
+                            for (int j = 0; j < V; j++) o[j] += b.get(i, j);
+                        }
+                        store_cols<T, V>(yr, c, cols, o);
+                    }
                 }
-#pragma unroll
-                for (int j = 0; j < V; j++) o[j] = (value(i, j) - mean) * rstd;
-                if (a.weight) {
-                    load_weights<W, V>(static_cast<const W*>(a.weight), c, cols, w);
-#pragma unroll
-                    for (int j = 0; j < V; j++) o[j] *= w[j];
+                if (t == 0) {
+                    if (a.mean) a.mean[row + r] = mean[r];
+                    if (a.rstd) a.rstd[row + r] = rstd[r];
                 }
-                if (a.bias) {
-                    load_weights<W, V>(static_cast<const W*>(a.bias), c, cols, w);
-#pragma unroll
-                    for (int j = 0; j < V; j++) o[j] += w[j];
-                }
-                store_cols<T, V>(yr, c, cols, o);
             }
-        }
-        if (t == 0) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
         }
     }
 }
@@ -173,12 +210,14 @@ __device__ __forceinline__ void copy_cols(Vec<T, V>* dst, const T* row, int c, i
 }
 
 // partial: [gridDim.x][2][cols], this block's sums of dy xh and of dy
-template <typename T, typename W, int V, int NV, int MAXT>
+template <typename T, typename W, int V, int NV, bool DSUM, int MAXT>
 __global__ void __launch_bounds__(MAXT) layer_norm_bwd_kernel(const gala_layer_norm_grad_args a, const int tpr, float* partial) {
-    constexpr int kRing = kRingRows<MAXT, sizeof(T)>;
-    __shared__ float red[2][2][16][32];
+    constexpr int kArrays = DSUM ? 3 : 2;
+    constexpr int kRing = kRingRows<MAXT, sizeof(T), kArrays>;
+    constexpr bool kHold = MAXT < 1024;     // registers for the weights
+    __shared__ __align__(16) float red[2][16][2][32];
     extern __shared__ __align__(16) uint8_t sm[];
-    // [slot][x, dy][i][thread]
+    // [slot][x, dy, dsum][i][thread]
     Vec<T, V>* ring = reinterpret_cast<Vec<T, V>*>(sm) + threadIdx.x;
     const int pitch = blockDim.x;
     const int group = threadIdx.x / tpr, groups = blockDim.x / tpr, t = threadIdx.x % tpr;
@@ -195,82 +234,73 @@ __global__ void __launch_bounds__(MAXT) layer_norm_bwd_kernel(const gala_layer_n
         if (row < a.rows) {
             const T* xr = static_cast<const T*>(a.x) + row * a.x_ld;
             const T* dyr = static_cast<const T*>(a.dy) + row * a.dy_ld;
-            Vec<T, V>* r = ring + (long long)slot * 2 * NV * pitch;
+            Vec<T, V>* r = ring + slot * kArrays * NV * pitch;
 #pragma unroll
             for (int i = 0; i < NV; i++) {
                 copy_cols<T, V>(r + i * pitch, xr, (t + i * tpr) * V, cols);
                 copy_cols<T, V>(r + (NV + i) * pitch, dyr, (t + i * tpr) * V, cols);
+                if (DSUM) copy_cols<T, V>(r + (2 * NV + i) * pitch, static_cast<const T*>(a.dsum) + row * a.dsum_ld, (t + i * tpr) * V, cols);
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll
     for (int k = 0; k < kRing; k++) fetch(first + k * step, k);
+    Weights<W, V, NV> w;
+    const bool weighted = a.weight != nullptr;
+    if (kHold && weighted) w.load(static_cast<const W*>(a.weight), t, tpr, cols);
     const float inv = 1.0f / (float)cols;
     int par = 0, slot = 0;
     float mean = 0.0f, rstd = 0.0f;
     if (first < a.rows) mean = a.mean[first], rstd = a.rstd[first];
     for (long long row = first; row < a.rows; row += step, par ^= 1) {
-        const float m = mean, rs = rstd;
+        const float rs = rstd, shift = -mean * rstd;       // xh = x rs + shift
         if (row + step < a.rows) mean = a.mean[row + step], rstd = a.rstd[row + step];
         asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
-        const Vec<T, V>* r = ring + (long long)slot * 2 * NV * pitch;
-        Vec<T, V> px[NV], pd[NV];
+        const Vec<T, V>* r = ring + slot * kArrays * NV * pitch;
+        float s[2] = {0.0f, 0.0f};
+        if (!kHold && weighted) w.load(static_cast<const W*>(a.weight), t, tpr, cols);
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            px[i] = r[i * pitch];
-            pd[i] = r[(NV + i) * pitch];
-        }
-        float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; i++) {
-            const int c = (t + i * tpr) * V;
-            float w[V];
-            if (a.weight) {
-                load_weights<W, V>(static_cast<const W*>(a.weight), c, cols, w);
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; j++) w[j] = 1.0f;
-            }
+            const Vec<T, V> px = r[i * pitch], pd = r[(NV + i) * pitch];
 #pragma unroll
             for (int j = 0; j < V; j++) {
-                const float d = pd[i].get(j);                                    // 0 past the last column
-                const float xh = (px[i].get(j) - m) * rs;
+                const float d = pd.get(j);                                       // 0 past the last column
+                const float xh = fmaf(px.get(j), rs, shift);
                 dw[i][j] = fmaf(d, xh, dw[i][j]);
                 db[i][j] += d;
-                const float e = d * w[j];
-                s1 += e;
-                s2 = fmaf(e, xh, s2);
+                const float e = weighted ? d * w.get(i, j) : d;
+                s[0] += e;
+                s[1] = fmaf(e, xh, s[1]);
             }
         }
-        fetch(row + kRing * step, slot);      // px and pd are in registers: their slot is free again
+        if (a.dx) {
+            group_sums<2>(s, tpr, group, red[par][group]);
+            const float s1 = s[0] * inv, s2 = s[1] * inv;
+            T* dxr = static_cast<T*>(a.dx) + row * a.dx_ld;
+            if (!kHold && weighted) w.load(static_cast<const W*>(a.weight), t, tpr, cols);
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                const int c = (t + i * tpr) * V;
+                if (c < cols) {
+                    const Vec<T, V> px = r[i * pitch], pd = r[(NV + i) * pitch];
+                    float o[V];
+#pragma unroll
+                    for (int j = 0; j < V; j++) {
+                        const float d = pd.get(j), e = weighted ? d * w.get(i, j) : d;
+                        o[j] = rs * fmaf(-fmaf(px.get(j), rs, shift), s2, e - s1);
+                    }
+                    if (DSUM) {
+                        const Vec<T, V> ds = r[(2 * NV + i) * pitch];
+#pragma unroll
+                        for (int j = 0; j < V; j++) o[j] += ds.get(j);
+                    }
+                    store_cols<T, V>(dxr, c, cols, o);
+                }
+            }
+        }
+        fetch(row + kRing * step, slot);      // what lay there has been used
         slot = slot + 1 == kRing ? 0 : slot + 1;
-        if (!a.dx) continue;
-        s1 = group_sum(s1, tpr, group, red[par][0][group]) * inv;
-        s2 = group_sum(s2, tpr, group, red[par][1][group]) * inv;
-        T* dxr = static_cast<T*>(a.dx) + row * a.dx_ld;
-        const T* dsr = a.dsum ? static_cast<const T*>(a.dsum) + row * a.dsum_ld : nullptr;
-#pragma unroll
-        for (int i = 0; i < NV; i++) {
-            const int c = (t + i * tpr) * V;
-            if (c < cols) {
-                float o[V], w[V];
-                if (a.weight) {
-                    load_weights<W, V>(static_cast<const W*>(a.weight), c, cols, w);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < V; j++) w[j] = 1.0f;
-                }
-#pragma unroll
-                for (int j = 0; j < V; j++) o[j] = rs * (fmaf(pd[i].get(j), w[j], -s1) - (px[i].get(j) - m) * rs * s2);
-                if (dsr) {
-                    const Vec<T, V> ds = load_cols<T, V>(dsr, c, cols);
-#pragma unroll
-                    for (int j = 0; j < V; j++) o[j] += ds.get(j);
-                }
-                store_cols<T, V>(dxr, c, cols, o);
-            }
-        }
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     if (!partial) return;
@@ -342,27 +372,25 @@ int threads_per_row(int cols, int per) {
     return t;
 }
 
-template <typename T, typename W, int V, int NV, bool RES, int MAXT>
+template <typename T, typename W, int V, int NV, int R, bool RES, int MAXT>
 cudaError_t fwd(const gala_layer_norm_args& a, int tpr, cudaStream_t st) {
     const int block = tpr > 256 ? tpr : 256, groups = block / tpr;
-    const long long want = (a.rows + groups - 1) / groups, cap = (long long)sm_count() * (1024 / block);
-    return launch_pdl(layer_norm_fwd_kernel<T, W, V, NV, RES, MAXT>, dim3((unsigned)(want < cap ? want : cap)), dim3(block), 0, st, a, tpr);
+    const long long want = (a.rows + groups * R - 1) / (groups * R), cap = (long long)sm_count() * (MAXT == 256 ? 2 : 1);
+    return launch_pdl(layer_norm_fwd_kernel<T, W, V, NV, R, RES, MAXT>, dim3((unsigned)(want < cap ? want : cap)), dim3(block), 0, st, a, tpr);
 }
-template <typename T, typename W, int V, int NV, bool RES>
-cudaError_t fwd_sized(const gala_layer_norm_args& a, cudaStream_t st) {
+// R rows at a time (what fits the registers) once that leaves enough groups for the device; one where rows are few.
+template <typename T, typename W, int V, int NV, int R, bool RES>
+cudaError_t fwd_rows(const gala_layer_norm_args& a, cudaStream_t st) {
     const int tpr = threads_per_row(a.cols, V * NV);
-    return tpr > 256 ? fwd<T, W, V, NV, RES, 1024>(a, tpr, st) : fwd<T, W, V, NV, RES, 256>(a, tpr, st);
+    if (tpr > 256) return fwd<T, W, V, NV, 1, RES, 1024>(a, tpr, st);
+    if (a.rows < (long long)R * (256 / tpr) * sm_count()) return fwd<T, W, V, NV, 1, RES, 256>(a, tpr, st);
+    return fwd<T, W, V, NV, R, RES, 256>(a, tpr, st);
 }
-// What a thread holds of a row: up to 128 bytes of x, or 64 of x and 64 of the residual, so that a row of up to 4 KB
-// (2 KB) is a warp's and needs no barrier; narrow rows take 32 bytes a thread.
 template <typename T, typename W>
 cudaError_t fwd_pick(const gala_layer_norm_args& a, bool vec, cudaStream_t st) {
-    constexpr int V = 16 / (int)sizeof(T);
-    if (vec) {
-        if (a.cols <= 64 * V) return a.residual ? fwd_sized<T, W, V, 2, true>(a, st) : fwd_sized<T, W, V, 2, false>(a, st);
-        return a.residual ? fwd_sized<T, W, V, 4, true>(a, st) : fwd_sized<T, W, V, 8, false>(a, st);
-    }
-    return a.residual ? fwd_sized<T, W, 1, 16, true>(a, st) : fwd_sized<T, W, 1, 16, false>(a, st);
+    constexpr int V = 16 / (int)sizeof(T), N = 16 / V;
+    if (vec) return a.residual ? fwd_rows<T, W, V, N, N == 2 ? 2 : 1, true>(a, st) : fwd_rows<T, W, V, N, N == 2 ? 4 : 2, false>(a, st);
+    return a.residual ? fwd_rows<T, W, 1, 16, 1, true>(a, st) : fwd_rows<T, W, 1, 16, 2, false>(a, st);
 }
 
 int bwd_blocks(long long rows, int groups) {
@@ -370,13 +398,14 @@ int bwd_blocks(long long rows, int groups) {
     return (int)(want < cap ? want : cap);
 }
 
-template <typename T, typename W, int V, int NV, int MAXT>
+template <typename T, typename W, int V, int NV, bool DSUM, int MAXT>
 cudaError_t bwd(const gala_layer_norm_grad_args& a, int tpr, cudaStream_t st) {
     const int block = tpr > kBwdThreads ? tpr : kBwdThreads, groups = block / tpr;
     const bool sums = a.dweight || a.dbias;
     const int nblk = bwd_blocks(a.rows, groups);
-    const size_t ring = (size_t)kRingRows<MAXT, sizeof(T)> * 2 * NV * block * sizeof(Vec<T, V>), acc = groups > 1 ? (size_t)2 * NV * V * tpr * sizeof(float) : 0;
-    const size_t smem = ring > acc ? ring : acc;
+    constexpr size_t ring = (size_t)kRingRows<MAXT, sizeof(T), DSUM ? 3 : 2> * (DSUM ? 3 : 2) * NV * MAXT * sizeof(Vec<T, V>);
+    constexpr size_t acc = (size_t)2 * NV * V * (kBwdThreads / 2) * sizeof(float);      // the most that groups join through
+    constexpr size_t smem = ring > acc ? ring : acc;
     float* partial = sums ? static_cast<float*>(a.workspace) : nullptr;
     static bool ready[64] = {};
     int dev = 0;
@@ -384,12 +413,12 @@ cudaError_t bwd(const gala_layer_norm_grad_args& a, int tpr, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!ready[dev]) {
-        e = cudaFuncSetAttribute(layer_norm_bwd_kernel<T, W, V, NV, MAXT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(ring > 65536 ? ring : 65536));
+        e = cudaFuncSetAttribute(layer_norm_bwd_kernel<T, W, V, NV, DSUM, MAXT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         ready[dev] = true;
     }
     if (nblk > 0) {
-        e = launch_pdl(layer_norm_bwd_kernel<T, W, V, NV, MAXT>, dim3(nblk), dim3(block), smem, st, a, tpr, partial);
+        e = launch_pdl(layer_norm_bwd_kernel<T, W, V, NV, DSUM, MAXT>, dim3(nblk), dim3(block), smem, st, a, tpr, partial);
         if (e != cudaSuccess) return e;
     }
     if (!sums) return cudaSuccess;
@@ -397,12 +426,16 @@ cudaError_t bwd(const gala_layer_norm_grad_args& a, int tpr, cudaStream_t st) {
                       static_cast<W*>(a.dweight), static_cast<W*>(a.dbias));
 }
 // Sixteen columns a thread: the two column sums of each stay in registers.
+template <typename T, typename W, int V, int NV, bool DSUM>
+cudaError_t bwd_rows(const gala_layer_norm_grad_args& a, cudaStream_t st) {
+    const int tpr = threads_per_row(a.cols, 16);
+    return tpr > kBwdThreads ? bwd<T, W, V, NV, DSUM, 1024>(a, tpr, st) : bwd<T, W, V, NV, DSUM, kBwdThreads>(a, tpr, st);
+}
 template <typename T, typename W>
 cudaError_t bwd_pick(const gala_layer_norm_grad_args& a, bool vec, cudaStream_t st) {
     constexpr int V = 16 / (int)sizeof(T), N = 16 / V;
-    const int tpr = threads_per_row(a.cols, 16);
-    if (tpr > kBwdThreads) return vec ? bwd<T, W, V, N, 1024>(a, tpr, st) : bwd<T, W, 1, 16, 1024>(a, tpr, st);
-    return vec ? bwd<T, W, V, N, kBwdThreads>(a, tpr, st) : bwd<T, W, 1, 16, kBwdThreads>(a, tpr, st);
+    if (vec) return a.dsum ? bwd_rows<T, W, V, N, true>(a, st) : bwd_rows<T, W, V, N, false>(a, st);
+    return a.dsum ? bwd_rows<T, W, 1, 16, true>(a, st) : bwd_rows<T, W, 1, 16, false>(a, st);
 }
 
 template <typename F32, typename BF, typename HF, typename BFF, typename HFF>

@@ -6,23 +6,22 @@
 //
 // Both passes are bound by memory: what counts is that every byte is moved once, that enough rows are under way, and
 // that an element costs few instructions.  A thread has 16 columns of a row and keeps their weights in registers over all
-// rows that it works on; a row is held as stored and widened anew for each pass over it.
-// Forward: up to four rows at a time, so that their loads are under way together and the barriers of wide rows are shared;
-// sum, centred sum of squares (no E[s^2] - m^2 cancellation), result.
-// Backward: the two column sums of a thread's columns stay in registers over all rows of its block; x, dy and dsum come
-// through a private ring in shared memory that asynchronous copies fill up to four rows ahead (no barrier: a thread reads only
-// what it copied).  The groups of a block then add their column sums through shared memory and leave one row of partial
-// sums a block; a second kernel adds those in a fixed order.
+// rows that it works on.  The rows come through a ring in shared memory that asynchronous copies fill several rows ahead;
+// a thread reads only what it copied itself, so the ring needs no barrier, and it is read again for each pass over a row
+// (forward: sum, centred sum of squares - no E[s^2] - m^2 cancellation -, result; backward: sums, result).
+// Backward: the two column sums of a thread's columns stay in registers over all rows of its block; the groups of a block
+// then add theirs through shared memory and leave one row of partial sums a block, and a second kernel adds those in a
+// fixed order.
 #include "sequence.cuh"
 
 namespace gala {
 
 constexpr int kMaxCols = 16384;
 constexpr int kBwdThreads = 512;
-// Rows of a group in the ring of the backward kernel: as many as 200 KB of shared memory hold, at most four.
-template <int THREADS, int ELEM, int ARRAYS> constexpr int kRingFit = 200 * 1024 / (ARRAYS * 16 * ELEM * THREADS);
-template <int THREADS, int ELEM, int ARRAYS>
-constexpr int kRingRows = kRingFit<THREADS, ELEM, ARRAYS> > 4 ? 4 : kRingFit<THREADS, ELEM, ARRAYS>;
+
+// Rows of a group in the ring: as many as SM bytes hold, at most MOST.
+template <int THREADS, int ELEM, int ARRAYS, int SM, int MOST>
+constexpr int kRingRows = SM / (ARRAYS * 16 * ELEM * THREADS) > MOST ? MOST : SM / (ARRAYS * 16 * ELEM * THREADS);
 
 // V elements from column c on; columns at or past `cols` read as 0
 template <typename T, int V>
@@ -41,28 +40,22 @@ __device__ __forceinline__ Vec<T, V> load_cols(const T* row, int c, int cols) {
     }
     return p;
 }
-template <typename T, int V>
-__device__ __forceinline__ void store_cols(T* row, int c, int cols, const float (&f)[V]) {
-    if (c + V <= cols) {
-        Vec<T, V> p;
-        p.put(f);
-        *reinterpret_cast<Vec<T, V>*>(row + c) = p;
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; j++)
-            if (c + j < cols) row[c + j] = from_f32<T>(f[j]);
-    }
-}
 // The weights of a thread's columns, as stored: NV times V columns, tpr * V apart.
 template <typename W, int V, int NV>
 struct Weights {
     static constexpr int N = 16 / (int)sizeof(W) < V ? 16 / (int)sizeof(W) : V;    // of one load
     Vec<W, N> w[NV][V / N];
-    __device__ __forceinline__ void load(const W* p, int t, int tpr, int cols) {
+    __device__ __forceinline__ void load(const W* p, float otherwise, int t, int tpr, int cols) {
+        float f[N];
+#pragma unroll
+        for (int j = 0; j < N; j++) f[j] = otherwise;
 #pragma unroll
         for (int i = 0; i < NV; i++)
 #pragma unroll
-            for (int k = 0; k < V / N; k++) w[i][k] = load_cols<W, N>(p, (t + i * tpr) * V + k * N, cols);
+            for (int k = 0; k < V / N; k++) {
+                if (p) w[i][k] = load_cols<W, N>(p, (t + i * tpr) * V + k * N, cols);
+                else w[i][k].put(f);
+            }
     }
     __device__ __forceinline__ float get(int i, int j) const { return w[i][j / N].get(j % N); }
 };
@@ -97,132 +90,158 @@ __device__ __forceinline__ void group_sums(float (&v)[R], int tpr, int group, fl
     }
 }
 
-template <typename T, typename W, int V, int NV, int R, bool RES, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT == 256 ? 2 : 1) layer_norm_fwd_kernel(const gala_layer_norm_args a, const int tpr) {
-    __shared__ __align__(16) float red[2][8][R][32];
-    const int group = threadIdx.x / tpr, groups = blockDim.x / tpr, t = threadIdx.x % tpr;
-    const int cols = a.cols;
-    const float inv = 1.0f / (float)cols;
-    pdl_wait();
-    pdl_launch();
-    Weights<W, V, NV> w, b;
-    if (a.weight) w.load(static_cast<const W*>(a.weight), t, tpr, cols);
-    if (a.bias) b.load(static_cast<const W*>(a.bias), t, tpr, cols);
-    for (long long row = ((long long)blockIdx.x * groups + group) * R; row < a.rows; row += (long long)gridDim.x * groups * R) {
-        const int n = a.rows - row < R ? (int)(a.rows - row) : R;
-        const T* xr = static_cast<const T*>(a.x) + row * a.x_ld;
-        Vec<T, V> x[R][NV], res[RES ? R : 1][NV];
+// A thread's columns and its ring.  Columns at or past the row's end arrive as 0.  Copies are asynchronous where the
+// address allows it (16 bytes, or one 32-bit element) and plain for single 16-bit elements.
+template <typename T, int V, int NV, int ARRAYS, int SLOTS>
+struct RowRing {
+    Vec<T, V>* base;
+    int pitch;              // threads of the block
+    int off[NV], have[NV];  // first column, and how many of its V exist
+    __device__ __forceinline__ void init(void* sm, int t, int tpr, int cols) {
+        base = static_cast<Vec<T, V>*>(sm) + threadIdx.x;
+        pitch = blockDim.x;
 #pragma unroll
-        for (int r = 0; r < R; r++)
-#pragma unroll
-            for (int i = 0; i < NV; i++) x[r][i] = load_cols<T, V>(xr + min(r, n - 1) * a.x_ld, (t + i * tpr) * V, cols);
-        if (RES) {
-            const T* rr = static_cast<const T*>(a.residual) + row * a.residual_ld;
-#pragma unroll
-            for (int r = 0; r < R; r++)
-#pragma unroll
-                for (int i = 0; i < NV; i++) res[RES ? r : 0][i] = load_cols<T, V>(rr + min(r, n - 1) * a.residual_ld, (t + i * tpr) * V, cols);
+        for (int i = 0; i < NV; i++) {
+            const int c = (t + i * tpr) * V;
+            have[i] = min(max(cols - c, 0), V);
+            off[i] = have[i] ? c : 0;
         }
-        auto value = [&](int r, int i, int j) { return RES ? x[r][i].get(j) + res[RES ? r : 0][i].get(j) : x[r][i].get(j); };
-        float mean[R], rstd[R];
+    }
+    __device__ __forceinline__ Vec<T, V>* at(int slot, int array, int i) const { return base + ((slot * ARRAYS + array) * NV + i) * pitch; }
+    __device__ __forceinline__ void fetch(int slot, int array, const T* row) const {
 #pragma unroll
-        for (int r = 0; r < R; r++) {
-            mean[r] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < NV; i++)
-#pragma unroll
-                for (int j = 0; j < V; j++) mean[r] += value(r, i, j);
+        for (int i = 0; i < NV; i++) {
+            const T* src = row + off[i];
+            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(at(slot, array, i));
+            const int bytes = have[i] * (int)sizeof(T);
+            if (V > 1) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+            else if (sizeof(T) == 4) asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+            else *at(slot, array, i) = have[i] ? *reinterpret_cast<const Vec<T, V>*>(src) : Vec<T, V>{};
         }
-        group_sums<R>(mean, tpr, group, red[0][group]);
+    }
+    static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    // the oldest of SLOTS groups has arrived
+    static __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(SLOTS - 1) : "memory"); }
+};
+template <typename T, int V>
+__device__ __forceinline__ void store_part(T* p, int have, const float (&f)[V]) {
+    if (have == V) {
+        Vec<T, V> v;
+        v.put(f);
+        *reinterpret_cast<Vec<T, V>*>(p) = v;
+    } else {
 #pragma unroll
-        for (int r = 0; r < R; r++) {
-            mean[r] *= inv;
-            rstd[r] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < NV; i++) {
-                const int c = (t + i * tpr) * V;
-                if (c + V <= cols) {
-#pragma unroll
-                    for (int j = 0; j < V; j++) {
-                        const float d = value(r, i, j) - mean[r];
-                        rstd[r] = fmaf(d, d, rstd[r]);
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < V; j++) {
-                        const float d = value(r, i, j) - mean[r];
-                        if (c + j < cols) rstd[r] = fmaf(d, d, rstd[r]);
-                    }
-                }
-            }
-        }
-        group_sums<R>(rstd, tpr, group, red[1][group]);
-#pragma unroll
-        for (int r = 0; r < R; r++) {
-            rstd[r] = 1.0f / sqrtf(fmaf(rstd[r], inv, a.eps));
-            if (r < n) {
-                T* yr = static_cast<T*>(a.y) + (row + r) * a.y_ld;
-                T* sr = RES && a.sum ? static_cast<T*>(a.sum) + (row + r) * a.sum_ld : nullptr;
-#pragma unroll
-                for (int i = 0; i < NV; i++) {
-                    const int c = (t + i * tpr) * V;
-                    if (c < cols) {
-                        float o[V];
-                        if (RES && sr) {
-#pragma unroll
-                            for (int j = 0; j < V; j++) o[j] = value(r, i, j);
-                            store_cols<T, V>(sr, c, cols, o);
-                        }
-#pragma unroll
-                        for (int j = 0; j < V; j++) o[j] = (value(r, i, j) - mean[r]) * rstd[r];
-                        if (a.weight && a.bias) {
-#pragma unroll
-                            for (int j = 0; j < V; j++) o[j] = fmaf(o[j], w.get(i, j), b.get(i, j));
-                        } else if (a.weight) {
-#pragma unroll
-                            for (int j = 0; j < V; j++) o[j] *= w.get(i, j);
-                        } else if (a.bias) {
-#pragma unroll
-                            for (int j = 0; j < V; j++) o[j] += b.get(i, j);
-                        }
-                        store_cols<T, V>(yr, c, cols, o);
-                    }
-                }
-                if (t == 0) {
-                    if (a.mean) a.mean[row + r] = mean[r];
-                    if (a.rstd) a.rstd[row + r] = rstd[r];
-                }
-            }
-        }
+        for (int j = 0; j < V; j++)
+            if (j < have) p[j] = from_f32<T>(f[j]);
     }
 }
 
-// V elements from column c on into shared memory; columns at or past `cols` arrive as 0.  Asynchronous where the address
-// allows it (16 bytes, or one 32-bit element), a plain copy for single 16-bit elements.
-template <typename T, int V>
-__device__ __forceinline__ void copy_cols(Vec<T, V>* dst, const T* row, int c, int cols) {
-    const int have = min(max(cols - c, 0), V) * (int)sizeof(T);
-    const T* src = have ? row + c : row;
-    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
-    if (V > 1) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(have) : "memory");
-    else if (sizeof(T) == 4) asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(d), "l"(src), "r"(have) : "memory");
-    else *dst = load_cols<T, V>(row, c, cols);
+template <typename T, int MAXT, bool RES> constexpr int kFwdSlots = kRingRows<MAXT, sizeof(T), RES ? 2 : 1, MAXT == 256 ? 52 * 1024 : 200 * 1024, 6>;
+
+template <typename T, typename W, int V, int NV, bool RES, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT == 256 ? 4 : 1) layer_norm_fwd_kernel(const gala_layer_norm_args a, const int tpr) {
+    constexpr int kSlots = kFwdSlots<T, MAXT, RES>;
+    __shared__ __align__(16) float red[2][8][1][32];
+    extern __shared__ __align__(16) uint8_t sm[];
+    const int group = threadIdx.x / tpr, groups = blockDim.x / tpr, t = threadIdx.x % tpr;
+    const float inv = 1.0f / (float)a.cols;
+    RowRing<T, V, NV, RES ? 2 : 1, kSlots> ring;
+    ring.init(sm, t, tpr, a.cols);
+    pdl_wait();
+    pdl_launch();
+    const long long first = (long long)blockIdx.x * groups + group, step = (long long)gridDim.x * groups;
+    const T* xn = static_cast<const T*>(a.x) + first * a.x_ld;             // next row to fetch
+    const T* rn = RES ? static_cast<const T*>(a.residual) + first * a.residual_ld : nullptr;
+    long long next = first;
+    auto fetch = [&](int slot) {
+        if (next < a.rows) {
+            ring.fetch(slot, 0, xn);
+            if (RES) ring.fetch(slot, RES ? 1 : 0, rn);
+        }
+        ring.commit();
+        next += step;
+        xn += step * a.x_ld;
+        if (RES) rn += step * a.residual_ld;
+    };
+#pragma unroll
+    for (int k = 0; k < kSlots; k++) fetch(k);
+    Weights<W, V, NV> w, b;
+    w.load(static_cast<const W*>(a.weight), 1.0f, t, tpr, a.cols);
+    b.load(static_cast<const W*>(a.bias), 0.0f, t, tpr, a.cols);
+    T* yr = static_cast<T*>(a.y) + first * a.y_ld;
+    T* sr = RES && a.sum ? static_cast<T*>(a.sum) + first * a.sum_ld : nullptr;
+    int slot = 0;
+    for (long long row = first; row < a.rows; row += step) {
+        ring.wait();
+        auto value = [&](const Vec<T, V>& x, const Vec<T, V>& r, int j) { return RES ? x.get(j) + r.get(j) : x.get(j); };
+        float sum[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const Vec<T, V> x = *ring.at(slot, 0, i), r = *ring.at(slot, RES ? 1 : 0, i);
+#pragma unroll
+            for (int j = 0; j < V; j++) sum[0] += value(x, r, j);
+        }
+        group_sums<1>(sum, tpr, group, red[0][group]);
+        const float mean = sum[0] * inv;
+        float sq[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const Vec<T, V> x = *ring.at(slot, 0, i), r = *ring.at(slot, RES ? 1 : 0, i);
+            if (ring.have[i] == V) {
+#pragma unroll
+                for (int j = 0; j < V; j++) {
+                    const float d = value(x, r, j) - mean;
+                    sq[0] = fmaf(d, d, sq[0]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; j++) {
+                    const float d = value(x, r, j) - mean;
+                    if (j < ring.have[i]) sq[0] = fmaf(d, d, sq[0]);
+                }
+            }
+        }
+        group_sums<1>(sq, tpr, group, red[1][group]);
+        const float rstd = 1.0f / sqrtf(fmaf(sq[0], inv, a.eps));
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const Vec<T, V> x = *ring.at(slot, 0, i), r = *ring.at(slot, RES ? 1 : 0, i);
+            float o[V];
+            if (RES && sr) {
+#pragma unroll
+                for (int j = 0; j < V; j++) o[j] = value(x, r, j);
+                store_part<T, V>(sr + ring.off[i], ring.have[i], o);
+            }
+#pragma unroll
+            for (int j = 0; j < V; j++) o[j] = fmaf((value(x, r, j) - mean) * rstd, w.get(i, j), b.get(i, j));
+            store_part<T, V>(yr + ring.off[i], ring.have[i], o);
+        }
+        if (t == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        fetch(slot);
+        slot = slot + 1 == kSlots ? 0 : slot + 1;
+        yr += step * a.y_ld;
+        if (RES && sr) sr += step * a.sum_ld;
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
+
+template <typename T, int MAXT, bool DSUM> constexpr int kBwdSlots = kRingRows<MAXT, sizeof(T), DSUM ? 3 : 2, 200 * 1024, 4>;
 
 // partial: [gridDim.x][2][cols], this block's sums of dy xh and of dy
 template <typename T, typename W, int V, int NV, bool DSUM, int MAXT>
 __global__ void __launch_bounds__(MAXT) layer_norm_bwd_kernel(const gala_layer_norm_grad_args a, const int tpr, float* partial) {
-    constexpr int kArrays = DSUM ? 3 : 2;
-    constexpr int kRing = kRingRows<MAXT, sizeof(T), kArrays>;
+    constexpr int kSlots = kBwdSlots<T, MAXT, DSUM>;
     constexpr bool kHold = MAXT < 1024;     // registers for the weights
     __shared__ __align__(16) float red[2][16][2][32];
     extern __shared__ __align__(16) uint8_t sm[];
-    // [slot][x, dy, dsum][i][thread]
-    Vec<T, V>* ring = reinterpret_cast<Vec<T, V>*>(sm) + threadIdx.x;
-    const int pitch = blockDim.x;
     const int group = threadIdx.x / tpr, groups = blockDim.x / tpr, t = threadIdx.x % tpr;
     const int cols = a.cols;
     const long long first = (long long)blockIdx.x * groups + group, step = (long long)gridDim.x * groups;
+    RowRing<T, V, NV, DSUM ? 3 : 2, kSlots> ring;
+    ring.init(sm, t, tpr, cols);
     float dw[NV][V], db[NV][V];
 #pragma unroll
     for (int i = 0; i < NV; i++)
@@ -230,46 +249,47 @@ __global__ void __launch_bounds__(MAXT) layer_norm_bwd_kernel(const gala_layer_n
         for (int j = 0; j < V; j++) dw[i][j] = db[i][j] = 0.0f;
     pdl_wait();
     pdl_launch();
-    auto fetch = [&](long long row, int slot) {
-        if (row < a.rows) {
-            const T* xr = static_cast<const T*>(a.x) + row * a.x_ld;
-            const T* dyr = static_cast<const T*>(a.dy) + row * a.dy_ld;
-            Vec<T, V>* r = ring + slot * kArrays * NV * pitch;
-#pragma unroll
-            for (int i = 0; i < NV; i++) {
-                copy_cols<T, V>(r + i * pitch, xr, (t + i * tpr) * V, cols);
-                copy_cols<T, V>(r + (NV + i) * pitch, dyr, (t + i * tpr) * V, cols);
-                if (DSUM) copy_cols<T, V>(r + (2 * NV + i) * pitch, static_cast<const T*>(a.dsum) + row * a.dsum_ld, (t + i * tpr) * V, cols);
-            }
+    const T* xn = static_cast<const T*>(a.x) + first * a.x_ld;
+    const T* dyn = static_cast<const T*>(a.dy) + first * a.dy_ld;
+    const T* dsn = DSUM ? static_cast<const T*>(a.dsum) + first * a.dsum_ld : nullptr;
+    long long next = first;
+    auto fetch = [&](int slot) {
+        if (next < a.rows) {
+            ring.fetch(slot, 0, xn);
+            ring.fetch(slot, 1, dyn);
+            if (DSUM) ring.fetch(slot, DSUM ? 2 : 0, dsn);
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        ring.commit();
+        next += step;
+        xn += step * a.x_ld;
+        dyn += step * a.dy_ld;
+        if (DSUM) dsn += step * a.dsum_ld;
     };
 #pragma unroll
-    for (int k = 0; k < kRing; k++) fetch(first + k * step, k);
+    for (int k = 0; k < kSlots; k++) fetch(k);
     Weights<W, V, NV> w;
-    const bool weighted = a.weight != nullptr;
-    if (kHold && weighted) w.load(static_cast<const W*>(a.weight), t, tpr, cols);
+    if (kHold) w.load(static_cast<const W*>(a.weight), 1.0f, t, tpr, cols);
     const float inv = 1.0f / (float)cols;
+    T* dxr = static_cast<T*>(a.dx) + first * a.dx_ld;
     int par = 0, slot = 0;
     float mean = 0.0f, rstd = 0.0f;
     if (first < a.rows) mean = a.mean[first], rstd = a.rstd[first];
     for (long long row = first; row < a.rows; row += step, par ^= 1) {
         const float rs = rstd, shift = -mean * rstd;       // xh = x rs + shift
         if (row + step < a.rows) mean = a.mean[row + step], rstd = a.rstd[row + step];
-        asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
-        const Vec<T, V>* r = ring + slot * kArrays * NV * pitch;
+        ring.wait();
         float s[2] = {0.0f, 0.0f};
-        if (!kHold && weighted) w.load(static_cast<const W*>(a.weight), t, tpr, cols);
+        if (!kHold) w.load(static_cast<const W*>(a.weight), 1.0f, t, tpr, cols);
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            const Vec<T, V> px = r[i * pitch], pd = r[(NV + i) * pitch];
+            const Vec<T, V> px = *ring.at(slot, 0, i), pd = *ring.at(slot, 1, i);
 #pragma unroll
             for (int j = 0; j < V; j++) {
                 const float d = pd.get(j);                                       // 0 past the last column
                 const float xh = fmaf(px.get(j), rs, shift);
                 dw[i][j] = fmaf(d, xh, dw[i][j]);
                 db[i][j] += d;
-                const float e = weighted ? d * w.get(i, j) : d;
+                const float e = d * w.get(i, j);
                 s[0] += e;
                 s[1] = fmaf(e, xh, s[1]);
             }
@@ -277,30 +297,26 @@ __global__ void __launch_bounds__(MAXT) layer_norm_bwd_kernel(const gala_layer_n
         if (a.dx) {
             group_sums<2>(s, tpr, group, red[par][group]);
             const float s1 = s[0] * inv, s2 = s[1] * inv;
-            T* dxr = static_cast<T*>(a.dx) + row * a.dx_ld;
-            if (!kHold && weighted) w.load(static_cast<const W*>(a.weight), t, tpr, cols);
+            // rs (e - s1 - xh s2) with xh = x rs + shift:  rs d w - x rs^2 s2 - rs (s1 + shift s2) loses digits where
+            // the mean is large, so the differences are formed first
+            if (!kHold) w.load(static_cast<const W*>(a.weight), 1.0f, t, tpr, cols);
 #pragma unroll
             for (int i = 0; i < NV; i++) {
-                const int c = (t + i * tpr) * V;
-                if (c < cols) {
-                    const Vec<T, V> px = r[i * pitch], pd = r[(NV + i) * pitch];
-                    float o[V];
+                const Vec<T, V> px = *ring.at(slot, 0, i), pd = *ring.at(slot, 1, i);
+                float o[V];
 #pragma unroll
-                    for (int j = 0; j < V; j++) {
-                        const float d = pd.get(j), e = weighted ? d * w.get(i, j) : d;
-                        o[j] = rs * fmaf(-fmaf(px.get(j), rs, shift), s2, e - s1);
-                    }
-                    if (DSUM) {
-                        const Vec<T, V> ds = r[(2 * NV + i) * pitch];
+                for (int j = 0; j < V; j++) o[j] = rs * fmaf(-fmaf(px.get(j), rs, shift), s2, fmaf(pd.get(j), w.get(i, j), -s1));
+                if (DSUM) {
+                    const Vec<T, V> ds = *ring.at(slot, DSUM ? 2 : 0, i);
 #pragma unroll
-                        for (int j = 0; j < V; j++) o[j] += ds.get(j);
-                    }
-                    store_cols<T, V>(dxr, c, cols, o);
+                    for (int j = 0; j < V; j++) o[j] += ds.get(j);
                 }
+                store_part<T, V>(dxr + ring.off[i], ring.have[i], o);
             }
         }
-        fetch(row + kRing * step, slot);      // what lay there has been used
-        slot = slot + 1 == kRing ? 0 : slot + 1;
+        fetch(slot);      // what lay there has been used
+        slot = slot + 1 == kSlots ? 0 : slot + 1;
+        dxr += step * a.dx_ld;
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     if (!partial) return;
@@ -372,25 +388,39 @@ int threads_per_row(int cols, int per) {
     return t;
 }
 
-template <typename T, typename W, int V, int NV, int R, bool RES, int MAXT>
+template <typename Kernel>
+cudaError_t large_smem(Kernel kernel, size_t bytes, bool (&ready)[64]) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!ready[dev]) {
+        if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes)) != cudaSuccess) return e;
+        ready[dev] = true;
+    }
+    return cudaSuccess;
+}
+
+template <typename T, typename W, int V, int NV, bool RES, int MAXT>
 cudaError_t fwd(const gala_layer_norm_args& a, int tpr, cudaStream_t st) {
     const int block = tpr > 256 ? tpr : 256, groups = block / tpr;
-    const long long want = (a.rows + groups * R - 1) / (groups * R), cap = (long long)sm_count() * (MAXT == 256 ? 2 : 1);
-    return launch_pdl(layer_norm_fwd_kernel<T, W, V, NV, R, RES, MAXT>, dim3((unsigned)(want < cap ? want : cap)), dim3(block), 0, st, a, tpr);
+    constexpr size_t smem = (size_t)kFwdSlots<T, MAXT, RES> * (RES ? 2 : 1) * NV * MAXT * sizeof(Vec<T, V>);
+    static bool ready[64] = {};
+    const cudaError_t e = large_smem(layer_norm_fwd_kernel<T, W, V, NV, RES, MAXT>, smem, ready);
+    if (e != cudaSuccess) return e;
+    const long long want = (a.rows + groups - 1) / groups, cap = (long long)sm_count() * (MAXT == 256 ? 4 : 1);
+    return launch_pdl(layer_norm_fwd_kernel<T, W, V, NV, RES, MAXT>, dim3((unsigned)(want < cap ? want : cap)), dim3(block), smem, st, a, tpr);
 }
-// R rows at a time (what fits the registers) once that leaves enough groups for the device; one where rows are few.
-template <typename T, typename W, int V, int NV, int R, bool RES>
+template <typename T, typename W, int V, int NV, bool RES>
 cudaError_t fwd_rows(const gala_layer_norm_args& a, cudaStream_t st) {
     const int tpr = threads_per_row(a.cols, V * NV);
-    if (tpr > 256) return fwd<T, W, V, NV, 1, RES, 1024>(a, tpr, st);
-    if (a.rows < (long long)R * (256 / tpr) * sm_count()) return fwd<T, W, V, NV, 1, RES, 256>(a, tpr, st);
-    return fwd<T, W, V, NV, R, RES, 256>(a, tpr, st);
+    return tpr > 256 ? fwd<T, W, V, NV, RES, 1024>(a, tpr, st) : fwd<T, W, V, NV, RES, 256>(a, tpr, st);
 }
 template <typename T, typename W>
 cudaError_t fwd_pick(const gala_layer_norm_args& a, bool vec, cudaStream_t st) {
     constexpr int V = 16 / (int)sizeof(T), N = 16 / V;
-    if (vec) return a.residual ? fwd_rows<T, W, V, N, N == 2 ? 2 : 1, true>(a, st) : fwd_rows<T, W, V, N, N == 2 ? 4 : 2, false>(a, st);
-    return a.residual ? fwd_rows<T, W, 1, 16, 1, true>(a, st) : fwd_rows<T, W, 1, 16, 2, false>(a, st);
+    if (vec) return a.residual ? fwd_rows<T, W, V, N, true>(a, st) : fwd_rows<T, W, V, N, false>(a, st);
+    return a.residual ? fwd_rows<T, W, 1, 16, true>(a, st) : fwd_rows<T, W, 1, 16, false>(a, st);
 }
 
 int bwd_blocks(long long rows, int groups) {
@@ -403,20 +433,13 @@ cudaError_t bwd(const gala_layer_norm_grad_args& a, int tpr, cudaStream_t st) {
     const int block = tpr > kBwdThreads ? tpr : kBwdThreads, groups = block / tpr;
     const bool sums = a.dweight || a.dbias;
     const int nblk = bwd_blocks(a.rows, groups);
-    constexpr size_t ring = (size_t)kRingRows<MAXT, sizeof(T), DSUM ? 3 : 2> * (DSUM ? 3 : 2) * NV * MAXT * sizeof(Vec<T, V>);
+    constexpr size_t ring = (size_t)kBwdSlots<T, MAXT, DSUM> * (DSUM ? 3 : 2) * NV * MAXT * sizeof(Vec<T, V>);
     constexpr size_t acc = (size_t)2 * NV * V * (kBwdThreads / 2) * sizeof(float);      // the most that groups join through
     constexpr size_t smem = ring > acc ? ring : acc;
     float* partial = sums ? static_cast<float*>(a.workspace) : nullptr;
     static bool ready[64] = {};
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    cudaError_t e = large_smem(layer_norm_bwd_kernel<T, W, V, NV, DSUM, MAXT>, smem, ready);
     if (e != cudaSuccess) return e;
-    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-    if (!ready[dev]) {
-        e = cudaFuncSetAttribute(layer_norm_bwd_kernel<T, W, V, NV, DSUM, MAXT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-        ready[dev] = true;
-    }
     if (nblk > 0) {
         e = launch_pdl(layer_norm_bwd_kernel<T, W, V, NV, DSUM, MAXT>, dim3(nblk), dim3(block), smem, st, a, tpr, partial);
         if (e != cudaSuccess) return e;

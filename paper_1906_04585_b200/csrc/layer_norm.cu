@@ -96,27 +96,27 @@ template <typename T, int V, int NV, int ARRAYS, int SLOTS>
 struct RowRing {
     Vec<T, V>* base;
     int pitch;              // threads of the block
-    int off[NV], have[NV];  // first column, and how many of its V exist
-    __device__ __forceinline__ void init(void* sm, int t, int tpr, int cols) {
+    int first, apart, cols;
+    __device__ __forceinline__ void init(void* sm, int t, int tpr, int n) {
         base = static_cast<Vec<T, V>*>(sm) + threadIdx.x;
         pitch = blockDim.x;
-#pragma unroll
-        for (int i = 0; i < NV; i++) {
-            const int c = (t + i * tpr) * V;
-            have[i] = min(max(cols - c, 0), V);
-            off[i] = have[i] ? c : 0;
-        }
+        first = t * V;
+        apart = tpr * V;
+        cols = n;
     }
+    // how many of the V columns of part i exist, and the first of them
+    __device__ __forceinline__ int have(int i) const { return min(max(cols - (first + i * apart), 0), V); }
+    __device__ __forceinline__ int off(int i) const { return first + i * apart < cols ? first + i * apart : 0; }
     __device__ __forceinline__ Vec<T, V>* at(int slot, int array, int i) const { return base + ((slot * ARRAYS + array) * NV + i) * pitch; }
     __device__ __forceinline__ void fetch(int slot, int array, const T* row) const {
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            const T* src = row + off[i];
+            const T* src = row + off(i);
             const uint32_t dst = (uint32_t)__cvta_generic_to_shared(at(slot, array, i));
-            const int bytes = have[i] * (int)sizeof(T);
+            const int bytes = have(i) * (int)sizeof(T);
             if (V > 1) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
             else if (sizeof(T) == 4) asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-            else *at(slot, array, i) = have[i] ? *reinterpret_cast<const Vec<T, V>*>(src) : Vec<T, V>{};
+            else *at(slot, array, i) = have(i) ? *reinterpret_cast<const Vec<T, V>*>(src) : Vec<T, V>{};
         }
     }
     static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -136,11 +136,14 @@ __device__ __forceinline__ void store_part(T* p, int have, const float (&f)[V]) 
     }
 }
 
-template <typename T, int MAXT, bool RES> constexpr int kFwdSlots = kRingRows<MAXT, sizeof(T), RES ? 2 : 1, MAXT == 256 ? 52 * 1024 : 200 * 1024, 6>;
+// Blocks of an SM, by the registers that a block needs without spilling, and the ring that fits beside the others.
+template <int V, int MAXT> constexpr int kFwdBlocks = MAXT > 256 ? 1 : V > 1 ? 3 : 2;
+template <typename T, int V, int MAXT, bool RES>
+constexpr int kFwdSlots = kRingRows<MAXT, sizeof(T), RES ? 2 : 1, 200 * 1024 / kFwdBlocks<V, MAXT>, 6>;
 
 template <typename T, typename W, int V, int NV, bool RES, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT == 256 ? 4 : 1) layer_norm_fwd_kernel(const gala_layer_norm_args a, const int tpr) {
-    constexpr int kSlots = kFwdSlots<T, MAXT, RES>;
+__global__ void __launch_bounds__(MAXT, kFwdBlocks<V, MAXT>) layer_norm_fwd_kernel(const gala_layer_norm_args a, const int tpr) {
+    constexpr int kSlots = kFwdSlots<T, V, MAXT, RES>;
     __shared__ __align__(16) float red[2][8][1][32];
     extern __shared__ __align__(16) uint8_t sm[];
     const int group = threadIdx.x / tpr, groups = blockDim.x / tpr, t = threadIdx.x % tpr;
@@ -187,7 +190,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? 4 : 1) layer_norm_fwd_kern
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const Vec<T, V> x = *ring.at(slot, 0, i), r = *ring.at(slot, RES ? 1 : 0, i);
-            if (ring.have[i] == V) {
+            if (ring.have(i) == V) {
 #pragma unroll
                 for (int j = 0; j < V; j++) {
                     const float d = value(x, r, j) - mean;
@@ -197,12 +200,12 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? 4 : 1) layer_norm_fwd_kern
 #pragma unroll
                 for (int j = 0; j < V; j++) {
                     const float d = value(x, r, j) - mean;
-                    if (j < ring.have[i]) sq[0] = fmaf(d, d, sq[0]);
+                    if (j < ring.have(i)) sq[0] = fmaf(d, d, sq[0]);
                 }
             }
         }
         group_sums<1>(sq, tpr, group, red[1][group]);
-        const float rstd = 1.0f / sqrtf(fmaf(sq[0], inv, a.eps));
+        const float rstd = rsqrtf(fmaf(sq[0], inv, a.eps));      // within 2 units in the last place
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const Vec<T, V> x = *ring.at(slot, 0, i), r = *ring.at(slot, RES ? 1 : 0, i);
@@ -210,11 +213,11 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? 4 : 1) layer_norm_fwd_kern
             if (RES && sr) {
 #pragma unroll
                 for (int j = 0; j < V; j++) o[j] = value(x, r, j);
-                store_part<T, V>(sr + ring.off[i], ring.have[i], o);
+                store_part<T, V>(sr + ring.off(i), ring.have(i), o);
             }
 #pragma unroll
             for (int j = 0; j < V; j++) o[j] = fmaf((value(x, r, j) - mean) * rstd, w.get(i, j), b.get(i, j));
-            store_part<T, V>(yr + ring.off[i], ring.have[i], o);
+            store_part<T, V>(yr + ring.off(i), ring.have(i), o);
         }
         if (t == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -311,7 +314,7 @@ __global__ void __launch_bounds__(MAXT) layer_norm_bwd_kernel(const gala_layer_n
 #pragma unroll
                     for (int j = 0; j < V; j++) o[j] += ds.get(j);
                 }
-                store_part<T, V>(dxr + ring.off[i], ring.have[i], o);
+                store_part<T, V>(dxr + ring.off(i), ring.have(i), o);
             }
         }
         fetch(slot);      // what lay there has been used
@@ -404,11 +407,11 @@ cudaError_t large_smem(Kernel kernel, size_t bytes, bool (&ready)[64]) {
 template <typename T, typename W, int V, int NV, bool RES, int MAXT>
 cudaError_t fwd(const gala_layer_norm_args& a, int tpr, cudaStream_t st) {
     const int block = tpr > 256 ? tpr : 256, groups = block / tpr;
-    constexpr size_t smem = (size_t)kFwdSlots<T, MAXT, RES> * (RES ? 2 : 1) * NV * MAXT * sizeof(Vec<T, V>);
+    constexpr size_t smem = (size_t)kFwdSlots<T, V, MAXT, RES> * (RES ? 2 : 1) * NV * MAXT * sizeof(Vec<T, V>);
     static bool ready[64] = {};
     const cudaError_t e = large_smem(layer_norm_fwd_kernel<T, W, V, NV, RES, MAXT>, smem, ready);
     if (e != cudaSuccess) return e;
-    const long long want = (a.rows + groups - 1) / groups, cap = (long long)sm_count() * (MAXT == 256 ? 4 : 1);
+    const long long want = (a.rows + groups - 1) / groups, cap = (long long)sm_count() * kFwdBlocks<V, MAXT>;
     return launch_pdl(layer_norm_fwd_kernel<T, W, V, NV, RES, MAXT>, dim3((unsigned)(want < cap ? want : cap)), dim3(block), smem, st, a, tpr);
 }
 template <typename T, typename W, int V, int NV, bool RES>

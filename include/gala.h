@@ -400,7 +400,9 @@ int gala_sweep_agents(float* x, const float* g, float* v, float* snap, const flo
  * overlap need two.  Sums, statistics and states are float32 (or wider) whatever the element type; a result is rounded
  * once, when it is stored.  errbuf (may be NULL) receives a NUL-terminated message of at most errbuf_len bytes on
  * failure.  GALA_EINVAL: nothing was enqueued.  Outputs must not overlap inputs or one another except where said.
- * Arrays are addressed with 64-bit offsets; every stride is in elements and at least the extent it spans.  */
+ * Arrays are addressed with 64-bit offsets; every stride is in elements and at least the extent it spans.
+ * status (DEVICE int, may be NULL), where a call has it: set to 1 if a bounded wait inside a kernel ran out, and never
+ * cleared; the results are then not to be used.  */
 typedef enum { GALA_F32 = 0, GALA_BF16 = 1, GALA_F16 = 2 } gala_dtype;
 
 /* Layer norm over the columns of s = x (+ residual):  y = (s - mean s) / sqrt(var s + eps) * weight + bias,
@@ -466,6 +468,7 @@ typedef struct {
     void* h;                   long long h_t, h_b;
     float* h_last;             /* [batch][dim] */
     float* states;
+    int* status;
 } gala_recurrence_args;
 int gala_gated_recurrence_forward(const gala_recurrence_args* a, void* stream, char* errbuf, int errbuf_len);
 
@@ -484,6 +487,7 @@ typedef struct {
     void* df;                  long long df_t, df_b;
     void* dx;                  long long dx_t, dx_b;
     float* dh0;                /* [batch][dim] */
+    int* status;
 } gala_recurrence_grad_args;
 int gala_gated_recurrence_backward(const gala_recurrence_grad_args* a, void* stream, char* errbuf, int errbuf_len);
 
@@ -523,8 +527,7 @@ int gala_sample(const gala_sample_args* a, void* stream, char* errbuf, int errbu
  * of the next product.  `product` [rows][hidden_ld] receives p.  With gate and up (both or neither) g and u are stored as
  * well, rounded, for the backward call.  act: GALA_ACT_SILU g sigmoid(g), GALA_ACT_GELU g Phi(g) (the exact form),
  * GALA_ACT_RELU max(g, 0).  Rows of every matrix start on 16-byte boundaries (pointers 16-byte aligned, strides multiples
- * of 8); sizes are free: 0 <= rows < 2^31 - 256, 1 <= dim, hidden <= 2^20.
- * status (DEVICE int, may be NULL): set to 1 if a bounded wait inside a kernel ran out, never cleared. */
+ * of 8); sizes are free: 0 <= rows < 2^31 - 256, 1 <= dim, hidden <= 2^20. */
 typedef enum { GALA_ACT_SILU = 0, GALA_ACT_GELU = 1, GALA_ACT_RELU = 2 } gala_act_kind;
 typedef struct {
     int dtype, act;

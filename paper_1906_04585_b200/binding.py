@@ -79,7 +79,7 @@ class gala_recurrence_args(C.Structure):
                 ("x", C.c_void_p), ("x_t", C.c_longlong), ("x_b", C.c_longlong),
                 ("done", C.c_void_p), ("done_t", C.c_longlong), ("done_b", C.c_longlong), ("h0", C.c_void_p),
                 ("h", C.c_void_p), ("h_t", C.c_longlong), ("h_b", C.c_longlong),
-                ("h_last", C.c_void_p), ("states", C.c_void_p)]
+                ("h_last", C.c_void_p), ("states", C.c_void_p), ("status", C.c_void_p)]
 
 
 class gala_recurrence_grad_args(C.Structure):
@@ -89,7 +89,8 @@ class gala_recurrence_grad_args(C.Structure):
                 ("done", C.c_void_p), ("done_t", C.c_longlong), ("done_b", C.c_longlong), ("states", C.c_void_p),
                 ("dh", C.c_void_p), ("dh_t", C.c_longlong), ("dh_b", C.c_longlong), ("dh_last", C.c_void_p),
                 ("df", C.c_void_p), ("df_t", C.c_longlong), ("df_b", C.c_longlong),
-                ("dx", C.c_void_p), ("dx_t", C.c_longlong), ("dx_b", C.c_longlong), ("dh0", C.c_void_p)]
+                ("dx", C.c_void_p), ("dx_t", C.c_longlong), ("dx_b", C.c_longlong), ("dh0", C.c_void_p),
+                ("status", C.c_void_p)]
 
 
 class gala_sample_args(C.Structure):

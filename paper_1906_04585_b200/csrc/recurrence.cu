@@ -9,8 +9,10 @@
 //   a thread    takes 16 (backward: 8) successive steps of one 32-bit word of channels, holds them in registers and
 //               composes their map;
 //   a block     has a warp for each of up to 8 such pieces and joins the warps' maps through shared memory;
-//   a cluster   of up to 8 blocks joins the blocks' maps through distributed shared memory (one cluster barrier a
-//               turn; the slots alternate, so that a block that is ahead never overwrites what another still reads).
+//   a cluster   of up to 16 blocks joins the blocks' maps through distributed shared memory: each block sends its map
+//               to all others with stores that report to the receiver's mbarrier, so that nothing waits for the global
+//               stores under way (a cluster barrier does: 2.2 of 8 stall cycles an instruction).  The slots alternate; a
+//               block that sends its map of one turn has read the slots of the turn before.
 // Then every thread knows the state that enters its piece and walks over it again, from registers, writing results.
 // A cluster goes over the time axis in turns of up to 1024 steps, the state carried in registers; the loads of the next
 // turn are under way while the maps of this one are joined.  No block waits for another cluster.
@@ -19,17 +21,15 @@
 //
 // What a `done` flag cuts off must not leak through it (0 * inf), so A = -0.0f marks a map that does not depend on
 // its input: products keep the sign (A is never negative otherwise), and applying such a map selects B.
-#include <cooperative_groups.h>
-
 #include "sequence.cuh"
+#include "tcgen05.cuh"
 
 namespace gala {
-namespace cg = cooperative_groups;
 
 constexpr int kStateStep = 8;    // distance of the stored states, and the steps of a thread in the backward kernel
 constexpr int kFwdPiece = 16;
 constexpr int kMaxWarps = 8;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16;
 
 struct Map { float a, b; };
 template <bool DONE> __device__ __forceinline__ bool cut(float a) { return DONE && __float_as_uint(a) == 0x80000000u; }
@@ -45,12 +45,15 @@ template <bool DONE> __device__ __forceinline__ Map then(Map m, Map n) {
 // rounding less where the state and the first input cancel) and its map has nothing left to depend on.
 template <bool DONE> __device__ __forceinline__ Map known(float c) { return Map{DONE ? -0.0f : 0.0f, c}; }
 
-// a = sigmoid(f) and b = 1 - a.  The smaller of the two is e / (1 + e) with e = exp(-|f|) (fast exponential and division:
-// a few units in its last place), the larger is 1 minus it, rounded once: neither a long memory (b small, where an error
-// of a in its last places would add up over 1 / b steps) nor a memory wiped by the gate (a small) loses digits.
+// a = sigmoid(f) and b = 1 - a.  The smaller of the two is e / (1 + e) with e = exp(-|f|) (approximate exponential and
+// reciprocal: a few units in its last place), the larger is 1 minus it, rounded once: neither a long memory (b small,
+// where an error of a in its last places would add up over 1 / b steps) nor a memory wiped by the gate (a small) loses
+// digits.
 __device__ __forceinline__ void gate(float f, float& a, float& b) {
-    const float e = __expf(-fabsf(f));
-    const float small = __fdividef(e, 1.0f + e), big = 1.0f - small;
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(f) * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    const float small = e * r, big = 1.0f - small;
     a = f < 0.0f ? small : big;
     b = f < 0.0f ? big : small;
 }
@@ -114,18 +117,43 @@ struct RecurrenceGrid {
     int warps, cluster;     // warps of a block along time, blocks of a cluster along time
 };
 
+// Where the blocks of a cluster meet.
+template <int V>
+struct Meeting {
+    Map maps[2][kMaxWarps][32 * V];       // of this block's warps, by turn
+    Map slots[2][kMaxCluster][32 * V];    // of the cluster's blocks, by turn
+    uint64_t bar[2];
+    int abort_flag;
+};
+__device__ __forceinline__ uint32_t block_of_cluster() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// the same place in the shared memory of block `rank`
+__device__ __forceinline__ uint32_t there(const void* p, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void send(uint32_t to, uint32_t bar, const Map (&m)[1]) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%2, %3}, [%1];" ::"r"(to), "r"(bar),
+                 "r"(__float_as_uint(m[0].a)), "r"(__float_as_uint(m[0].b))
+                 : "memory");
+}
+__device__ __forceinline__ void send(uint32_t to, uint32_t bar, const Map (&m)[2]) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%2, %3, %4, %5}, [%1];" ::"r"(to), "r"(bar),
+                 "r"(__float_as_uint(m[0].a)), "r"(__float_as_uint(m[0].b)), "r"(__float_as_uint(m[1].a)), "r"(__float_as_uint(m[1].b))
+                 : "memory");
+}
+
 // Joins the maps of all pieces of a turn: `enter` is the state before this thread's piece, and carry, on entry the state
 // before the turn, the one behind it.  w, rank: this warp's and block's place in the turn (0 = first to act).
-// maps: [kMaxWarps][32 V], slots: [2][kMaxCluster][32 V] of this block.
 template <int V, bool DONE>
-__device__ __forceinline__ void join(const Map (&m)[V], float (&enter)[V], float (&carry)[V], Map* maps, Map* slots, int warps, int w, int cluster,
+__device__ __forceinline__ void join(const Map (&m)[V], float (&enter)[V], float (&carry)[V], Meeting<V>& sm, int warps, int w, int cluster,
                                      int rank, int turn) {
-    const int lane = threadIdx.x & 31;
-    if (warps > 1) {
-#pragma unroll
-        for (int v = 0; v < V; v++) maps[w * 32 * V + lane * V + v] = m[v];
-        __syncthreads();
-    }
+    const int lane = threadIdx.x & 31, par = turn & 1;
+    if (cluster > 1 && threadIdx.x == 0) mbar_expect_tx(&sm.bar[par], (uint32_t)(cluster * 32 * V * sizeof(Map)));
     Map before[V], all[V];     // the pieces of this block ahead of this warp, and the whole block
 #pragma unroll
     for (int v = 0; v < V; v++) {
@@ -134,57 +162,74 @@ __device__ __forceinline__ void join(const Map (&m)[V], float (&enter)[V], float
     }
     if (warps > 1) {
 #pragma unroll
-        for (int v = 0; v < V; v++) all[v] = maps[lane * V + v];
+        for (int v = 0; v < V; v++) sm.maps[par][w][lane * V + v] = m[v];
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < V; v++) all[v] = sm.maps[par][0][lane * V + v];
 #pragma unroll
         for (int k = 1; k < kMaxWarps; k++)
             if (k < warps) {
 #pragma unroll
                 for (int v = 0; v < V; v++) {
                     if (k == w) before[v] = all[v];
-                    all[v] = then<DONE>(all[v], maps[k * 32 * V + lane * V + v]);
+                    all[v] = then<DONE>(all[v], sm.maps[par][k][lane * V + v]);
                 }
             }
     }
     if (cluster > 1) {
-        cg::cluster_group cl = cg::this_cluster();
-        Map* mine = slots + ((turn & 1) * kMaxCluster + rank) * 32 * V + lane * V;
-        if (w < cluster) {         // warp w tells block w (a cluster has all kMaxWarps warps in every block)
-            Map* there = cl.map_shared_rank(mine, w);
+        // warp w tells blocks w, w + 8 (a cluster has all kMaxWarps warps in every block)
+        for (int r = w; r < cluster; r += kMaxWarps) send(there(&sm.slots[par][rank][lane * V], r), there(&sm.bar[par], r), all);
+        mbar_wait(&sm.bar[par], (uint32_t)(turn >> 1) & 1u, &sm.abort_flag);
+        float c[V];
 #pragma unroll
-            for (int v = 0; v < V; v++) there[v] = all[v];
-        }
-        cl.sync();
-        const Map* from = slots + (turn & 1) * kMaxCluster * 32 * V + lane * V;
+        for (int v = 0; v < V; v++) c[v] = carry[v];
+#pragma unroll 4
+        for (int r = 0; r < cluster; r++)
 #pragma unroll
-        for (int v = 0; v < V; v++) {
-            float c = carry[v];
+            for (int v = 0; v < V; v++) {
+                if (r == rank) enter[v] = apply<DONE>(before[v], c[v]);
+                c[v] = apply<DONE>(sm.slots[par][r][lane * V + v], c[v]);
+            }
 #pragma unroll
-            for (int r = 0; r < kMaxCluster; r++)
-                if (r < cluster) {
-                    if (r == rank) enter[v] = apply<DONE>(before[v], c);
-                    c = apply<DONE>(from[r * 32 * V + v], c);
-                }
-            carry[v] = c;
-        }
+        for (int v = 0; v < V; v++) carry[v] = c[v];
     } else {
 #pragma unroll
         for (int v = 0; v < V; v++) {
             enter[v] = apply<DONE>(before[v], carry[v]);
             carry[v] = apply<DONE>(all[v], carry[v]);
         }
-        if (warps > 1) __syncthreads();    // maps is written again in the next turn (the cluster barrier does this above)
     }
+}
+// Before the first turn: the barriers exist, and every block of the cluster runs, before another writes to its memory.
+template <int V>
+__device__ __forceinline__ void meet(Meeting<V>& sm, int cluster) {
+    if (cluster == 1) return;
+    if (threadIdx.x == 0) {
+        mbar_init(&sm.bar[0], 1);
+        mbar_init(&sm.bar[1], 1);
+        sm.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// No block leaves while another may still send to it; reports a wait that ran out.
+template <int V>
+__device__ __forceinline__ void part(Meeting<V>& sm, int cluster, int* status) {
+    if (cluster == 1) return;
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (threadIdx.x == 0 && sm.abort_flag && status) atomicExch(status, 1);
 }
 
 // SINGLE: no more than L steps, so that a thread has the whole time axis; the warps of a block take different units.
 template <typename T, int V, int L, bool SINGLE, bool DONE>
 __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const gala_recurrence_args p, const RecurrenceGrid g) {
-    __shared__ Map maps[SINGLE ? 1 : kMaxWarps * 32 * V];
-    __shared__ Map slots[SINGLE ? 1 : 2 * kMaxCluster * 32 * V];
+    __shared__ __align__(16) uint8_t meeting[SINGLE ? 16 : sizeof(Meeting<V>)];
+    Meeting<V>& sm = *reinterpret_cast<Meeting<V>*>(meeting);
     using Wd = Word<T, V>;
     using W = typename Wd::type;
     const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = SINGLE ? 0 : (int)(blockIdx.x % g.cluster);
+    const int rank = SINGLE ? 0 : (int)block_of_cluster();
     const long long unit = SINGLE ? (long long)blockIdx.x * (blockDim.x >> 5) + w : (long long)blockIdx.x / g.cluster;
     pdl_wait();
     pdl_launch();
@@ -214,10 +259,8 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const
         }
         return n;
     };
-    // every block of the cluster has to run before another writes to its shared memory
-    if (!SINGLE && g.cluster > 1) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
     int n = fetch(place);
-    if (!SINGLE && g.cluster > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    if (!SINGLE) meet<V>(sm, g.cluster);
     int turn = 0;
     for (long long first = 0; first < g.pieces; first += per_turn, turn++) {
         const long long piece = first + place, t0 = piece * L;
@@ -232,8 +275,15 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const
                     float bb;
                     gate(Wd::get(rf[i], v), a[i][v], bb);
                     bx[i][v] = bb * Wd::get(rx[i], v);
-                    if (!SINGLE && i >= now) a[i][v] = 1.0f, bx[i][v] = 0.0f;
                 }
+            if (!SINGLE && now < L) {
+#pragma unroll
+                for (int i = 1; i < L; i++)
+                    if (i >= now) {
+#pragma unroll
+                        for (int v = 0; v < V; v++) a[i][v] = 1.0f, bx[i][v] = 0.0f;
+                    }
+            }
         }
         if (!SINGLE && first + per_turn < g.pieces) n = fetch(piece + per_turn);
         float c[V];
@@ -245,37 +295,52 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const
 #pragma unroll
             for (int v = 0; v < V; v++) m[v] = place == 0 ? known<DONE>(carry[v]) : Map{1.0f, 0.0f};
             if (now) {
+                if (DONE && ends) {
 #pragma unroll
-                for (int i = 0; i < L; i++)
+                    for (int i = 0; i < L; i++)
 #pragma unroll
-                    for (int v = 0; v < V; v++) {
-                        m[v].b = fmaf(a[i][v], m[v].b, bx[i][v]);
-                        m[v].a = cut<DONE>(m[v].a) ? -0.0f : m[v].a * a[i][v];
-                        if (DONE && ((ends >> i) & 1u)) m[v] = Map{-0.0f, 0.0f};
-                    }
+                        for (int v = 0; v < V; v++) {
+                            m[v].b = fmaf(a[i][v], m[v].b, bx[i][v]);
+                            m[v].a = cut<DONE>(m[v].a) ? -0.0f : m[v].a * a[i][v];
+                            if ((ends >> i) & 1u) m[v] = Map{-0.0f, 0.0f};
+                        }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < L; i++)
+#pragma unroll
+                        for (int v = 0; v < V; v++) {
+                            m[v].b = fmaf(a[i][v], m[v].b, bx[i][v]);
+                            m[v].a *= a[i][v];      // keeps the mark of a known state, unless a is NaN and all is lost
+                        }
+                }
             }
-            join<V, DONE>(m, c, carry, maps, slots, g.warps, w, g.cluster, rank, turn);
+            join<V, DONE>(m, c, carry, sm, g.warps, w, g.cluster, rank, turn);
         }
         if (!now) continue;
         float* s = p.states ? p.states + ((t0 / kStateStep) * p.batch + b) * p.dim + dl : nullptr;
         T* ht = h + t0 * p.h_t;
+        auto walk = [&](auto flags_, auto whole_) {
+            constexpr bool flags = decltype(flags_)::value, whole = decltype(whole_)::value;
 #pragma unroll
-        for (int i = 0; i < L; i++) {
-            if (i < now) {
-                if (i % kStateStep == 0 && s && on) {
+            for (int i = 0; i < L; i++) {
+                if (whole || i < now) {
+                    if (i % kStateStep == 0 && s && on) {
 #pragma unroll
-                    for (int v = 0; v < V; v++) s[(i / kStateStep) * p.batch * p.dim + v] = c[v];
+                        for (int v = 0; v < V; v++) s[(i / kStateStep) * p.batch * p.dim + v] = c[v];
+                    }
+#pragma unroll
+                    for (int v = 0; v < V; v++) c[v] = fmaf(a[i][v], c[v], bx[i][v]);
+                    if (on) *reinterpret_cast<W*>(ht) = Wd::put(c);
+                    if (flags && ((ends >> i) & 1u)) {
+#pragma unroll
+                        for (int v = 0; v < V; v++) c[v] = 0.0f;
+                    }
                 }
-#pragma unroll
-                for (int v = 0; v < V; v++) c[v] = fmaf(a[i][v], c[v], bx[i][v]);
-                if (on) *reinterpret_cast<W*>(ht) = Wd::put(c);
-                if (DONE && ((ends >> i) & 1u)) {
-#pragma unroll
-                    for (int v = 0; v < V; v++) c[v] = 0.0f;
-                }
+                ht += p.h_t;
             }
-            ht += p.h_t;
-        }
+        };
+        if (now < L || (DONE && ends)) walk(std::integral_constant<bool, DONE>{}, std::false_type{});
+        else walk(std::false_type{}, std::true_type{});
         if (SINGLE) {
 #pragma unroll
             for (int v = 0; v < V; v++) carry[v] = c[v];
@@ -285,18 +350,18 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const
 #pragma unroll
         for (int v = 0; v < V; v++) p.h_last[b * p.dim + d + v] = carry[v];
     }
-    if (!SINGLE && g.cluster > 1) cg::this_cluster().sync();   // no block leaves while another may still write to it
+    if (!SINGLE) part<V>(sm, g.cluster, p.status);
 }
 
 template <typename T, int V, int L, bool SINGLE, bool DONE>
 __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const gala_recurrence_grad_args p, const RecurrenceGrid g) {
     static_assert(L <= kStateStep, "a piece begins where a state is stored");
-    __shared__ Map maps[SINGLE ? 1 : kMaxWarps * 32 * V];
-    __shared__ Map slots[SINGLE ? 1 : 2 * kMaxCluster * 32 * V];
+    __shared__ __align__(16) uint8_t meeting[SINGLE ? 16 : sizeof(Meeting<V>)];
+    Meeting<V>& sm = *reinterpret_cast<Meeting<V>*>(meeting);
     using Wd = Word<T, V>;
     using W = typename Wd::type;
     const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = SINGLE ? 0 : (int)(blockIdx.x % g.cluster);
+    const int rank = SINGLE ? 0 : (int)block_of_cluster();
     const long long unit = SINGLE ? (long long)blockIdx.x * (blockDim.x >> 5) + w : (long long)blockIdx.x / g.cluster;
     pdl_wait();
     pdl_launch();
@@ -333,9 +398,8 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
         }
         return n;
     };
-    if (!SINGLE && g.cluster > 1) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
     int n = fetch(g.pieces - 1 - place);
-    if (!SINGLE && g.cluster > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    if (!SINGLE) meet<V>(sm, g.cluster);
     int turn = 0;
     for (long long first = 0; first < g.pieces; first += per_turn, turn++) {
         const long long piece = g.pieces - 1 - (first + place), t0 = piece * L;
@@ -350,7 +414,8 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
                     const float xv = Wd::get(rx[i], v);
                     gate(Wd::get(rf[i], v), a[i][v], bb[i][v]);
                     cx[i][v] = rc[v] - xv;
-                    rc[v] = DONE && ((ends >> i) & 1u) ? 0.0f : fmaf(a[i][v], rc[v], bb[i][v] * xv);
+                    rc[v] = fmaf(a[i][v], rc[v], bb[i][v] * xv);
+                    if (DONE && ((ends >> i) & 1u)) rc[v] = 0.0f;
                     gg[i][v] = dh ? Wd::get(rg[i], v) : 0.0f;
                 }
         }
@@ -364,41 +429,56 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
 #pragma unroll
             for (int v = 0; v < V; v++) m[v] = place == 0 ? known<DONE>(carry[v]) : Map{1.0f, 0.0f};
             if (now) {
+                if (now < L || (DONE && ends)) {
 #pragma unroll
-                for (int i = L - 1; i >= 0; i--)
-                    if (i < now) {
+                    for (int i = L - 1; i >= 0; i--)
+                        if (i < now) {
+#pragma unroll
+                            for (int v = 0; v < V; v++) {
+                                if (DONE && ((ends >> i) & 1u)) m[v] = Map{-0.0f, 0.0f};
+                                m[v].b = a[i][v] * (gg[i][v] + m[v].b);
+                                m[v].a = cut<DONE>(m[v].a) ? -0.0f : m[v].a * a[i][v];
+                            }
+                        }
+                } else {
+#pragma unroll
+                    for (int i = L - 1; i >= 0; i--)
 #pragma unroll
                         for (int v = 0; v < V; v++) {
-                            if (DONE && ((ends >> i) & 1u)) m[v] = Map{-0.0f, 0.0f};
                             m[v].b = a[i][v] * (gg[i][v] + m[v].b);
-                            m[v].a = cut<DONE>(m[v].a) ? -0.0f : m[v].a * a[i][v];
+                            m[v].a *= a[i][v];
                         }
-                    }
+                }
             }
-            join<V, DONE>(m, q, carry, maps, slots, g.warps, w, g.cluster, rank, turn);
+            join<V, DONE>(m, q, carry, sm, g.warps, w, g.cluster, rank, turn);
         }
         if (!now) continue;
         T* dft = df + (t0 + L - 1) * p.df_t;
         T* dxt = dx + (t0 + L - 1) * p.dx_t;
+        auto walk = [&](auto flags_, auto whole_) {
+            constexpr bool flags = decltype(flags_)::value, whole = decltype(whole_)::value;
 #pragma unroll
-        for (int i = L - 1; i >= 0; i--) {
-            if (i < now) {
-                float of[V], ox[V];
+            for (int i = L - 1; i >= 0; i--) {
+                if (whole || i < now) {
+                    float of[V], ox[V];
 #pragma unroll
-                for (int v = 0; v < V; v++) {
-                    const float gt = DONE && ((ends >> i) & 1u) ? gg[i][v] : gg[i][v] + q[v];
-                    q[v] = a[i][v] * gt;
-                    ox[v] = bb[i][v] * gt;
-                    of[v] = q[v] * bb[i][v] * cx[i][v];
+                    for (int v = 0; v < V; v++) {
+                        const float gt = flags && ((ends >> i) & 1u) ? gg[i][v] : gg[i][v] + q[v];
+                        q[v] = a[i][v] * gt;
+                        ox[v] = bb[i][v] * gt;
+                        of[v] = q[v] * bb[i][v] * cx[i][v];
+                    }
+                    if (on) {
+                        *reinterpret_cast<W*>(dft) = Wd::put(of);
+                        *reinterpret_cast<W*>(dxt) = Wd::put(ox);
+                    }
                 }
-                if (on) {
-                    *reinterpret_cast<W*>(dft) = Wd::put(of);
-                    *reinterpret_cast<W*>(dxt) = Wd::put(ox);
-                }
+                dft -= p.df_t;
+                dxt -= p.dx_t;
             }
-            dft -= p.df_t;
-            dxt -= p.dx_t;
-        }
+        };
+        if (now < L || (DONE && ends)) walk(std::integral_constant<bool, DONE>{}, std::false_type{});
+        else walk(std::false_type{}, std::true_type{});
         if (SINGLE) {
 #pragma unroll
             for (int v = 0; v < V; v++) carry[v] = q[v];
@@ -408,7 +488,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
 #pragma unroll
         for (int v = 0; v < V; v++) p.dh0[b * p.dim + d + v] = carry[v];
     }
-    if (!SINGLE && g.cluster > 1) cg::this_cluster().sync();
+    if (!SINGLE) part<V>(sm, g.cluster, p.status);
 }
 
 // steps == 0: the state passes through
@@ -421,8 +501,9 @@ __global__ void recurrence_pass_kernel(const float* src, float* dst, long long n
 // ------------------------------------------------------------------------------------------------ host side
 namespace {
 
-// How the time axis is cut.  Blocks along it cost a cluster barrier a turn and are taken while there are pieces for
-// them: even with many units, more and shorter blocks fill the last wave of the grid better.
+// How the time axis is cut.  Blocks along it are taken while there are pieces for them (even with many units, more and
+// shorter blocks fill the last wave of the grid better): up to eight, and sixteen where eight would leave part of the
+// device without a block.
 RecurrenceGrid plan(long long steps, long long batch, long long dim, int v, int piece) {
     RecurrenceGrid g;
     g.pieces = (steps + piece - 1) / piece;
@@ -430,7 +511,8 @@ RecurrenceGrid plan(long long steps, long long batch, long long dim, int v, int 
     g.units = batch * g.chan_blocks;
     g.warps = (int)(g.pieces < kMaxWarps ? g.pieces : kMaxWarps);
     g.cluster = 1;
-    while (g.cluster < kMaxCluster && (long long)g.cluster * g.warps < g.pieces) g.cluster *= 2;
+    const int most = g.units * 8 < 2 * sm_count() ? kMaxCluster : 8;
+    while (g.cluster < most && (long long)g.cluster * g.warps < g.pieces) g.cluster *= 2;
     return g;
 }
 
@@ -449,6 +531,10 @@ cudaError_t launch_units(void (*kernel)(Args, RecurrenceGrid), const Args& a, co
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = single || g.cluster == 1 ? 1 : 2;
+    if (!single && g.cluster > 8) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+    }
     return cudaLaunchKernelEx(&cfg, kernel, a, g);
 }
 
@@ -491,7 +577,7 @@ cudaError_t pass(const float* src, float* dst, long long n, cudaStream_t st) {
 // pairs of 16-bit channels where every row of every array starts on a pair's boundary
 bool pairs(const void* q, long long st, long long sb, size_t es) { return aligned(q, 2 * es) && st % 2 == 0 && sb % 2 == 0; }
 
-// units of 32 channels, 8 blocks of a cluster each: the grid has to stay below 2^31 blocks
+// units of 32 channels, up to 8 blocks each (16 only where units are few): the grid has to stay below 2^31 blocks
 bool too_many(long long batch, long long dim) { return batch > 0 && (dim + 31) / 32 > (1ll << 27) / batch; }
 
 }  // namespace

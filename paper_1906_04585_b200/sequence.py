@@ -73,6 +73,28 @@ def _type_of(t: torch.Tensor) -> int:
         raise TypeError("%s: float32, bfloat16 or float16 is needed" % t.dtype) from None
 
 
+_status = {}
+
+
+def _status_word(t: torch.Tensor) -> int:
+    index = t.get_device()
+    word = _status.get(index)
+    if word is None:
+        _status[index] = torch.zeros(1, dtype=torch.int32, device=t.device)
+        torch.cuda.synchronize(index)      # streams that do not follow this one may use it next
+        word = _status[index]
+    return word.data_ptr()
+
+
+def check() -> None:
+    """Waits for the current stream and raises if a bounded wait inside a kernel of this module ran out since the last
+    check (results since then are not to be trusted); the word is cleared."""
+    for word in _status.values():
+        if int(word.item()):
+            word.zero_()
+            raise B.GalaError(B.GALA_ECUDA, "a bounded device-side wait ran out")
+
+
 # ---------------------------------------------------------------------------------------------- layer norm
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5, *,
                residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None):
@@ -184,6 +206,7 @@ def gated_recurrence(f: torch.Tensor, x: torch.Tensor, h0: Optional[torch.Tensor
     a.h0 = _flat("h0", h0, shape[1:], torch.float32, x)
     a.h_last = _flat("h_last", h_last, shape[1:], torch.float32, x)
     a.states = states.data_ptr() if save else None
+    a.status = _status_word(x)
     B.gala_gated_recurrence_forward(a, st)
     return h, h_last, states
 
@@ -211,31 +234,13 @@ def gated_recurrence_backward(dh: Optional[torch.Tensor], f: torch.Tensor, x: to
     a.states = _flat("states", states, ((T + 7) // 8, N, D), torch.float32, x)
     a.dh_last = _flat("dh_last", dh_last, shape[1:], torch.float32, x)
     a.dh0 = _flat("dh0", dh0, shape[1:], torch.float32, x)
+    a.status = _status_word(x)
     B.gala_gated_recurrence_backward(a, st)
     return df, dx, dh0
 
 
 # ---------------------------------------------------------------------------------------------- gated feed-forward
 _ACT = {"silu": B.GALA_ACT_SILU, "gelu": B.GALA_ACT_GELU, "relu": B.GALA_ACT_RELU}
-_status = {}
-
-
-def _status_word(device) -> torch.Tensor:
-    word = _status.get(device)
-    if word is None:
-        word = _status[device] = torch.zeros(1, dtype=torch.int32, device=device)
-    return word
-
-
-def check() -> None:
-    """Waits for the current stream and raises if a bounded wait inside a kernel of this module ran out since the last
-    check (results since then are not to be trusted); the word is cleared."""
-    for word in _status.values():
-        if int(word.item()):
-            word.zero_()
-            raise B.GalaError(B.GALA_ECUDA, "a bounded device-side wait ran out")
-
-
 def _ffn_shapes(a, x, w_gate, w_up, w_down, act):
     if x.dim() != 2 or w_gate.dim() != 2:
         raise ValueError("x has to be [rows, dim], the weights [hidden, dim] and [dim, hidden]")
@@ -251,7 +256,7 @@ def _ffn_shapes(a, x, w_gate, w_up, w_down, act):
     a.w_up, a.w_up_ld = _rows("w_up", w_up, (hidden, dim), x)
     a.w_down, a.w_down_ld = _rows("w_down", w_down, (dim, hidden), x)
     a.hidden_ld = (hidden + 7) // 8 * 8
-    a.status = _status_word(x.device).data_ptr()
+    a.status = _status_word(x)
     return rows, dim, hidden
 
 

@@ -31,20 +31,6 @@ constexpr int kFwdPiece = 16;
 constexpr int kMaxWarps = 8;
 constexpr int kMaxCluster = 16;
 
-struct Map { float a, b; };
-template <bool DONE> __device__ __forceinline__ bool cut(float a) { return DONE && __float_as_uint(a) == 0x80000000u; }
-template <bool DONE> __device__ __forceinline__ float apply(Map m, float c) { return cut<DONE>(m.a) ? m.b : fmaf(m.a, c, m.b); }
-// first m, then n
-template <bool DONE> __device__ __forceinline__ Map then(Map m, Map n) {
-    Map r;
-    r.a = cut<DONE>(n.a) || cut<DONE>(m.a) ? -0.0f : n.a * m.a;
-    r.b = apply<DONE>(n, m.b);
-    return r;
-}
-// What the first piece of a turn starts from: its state is known, so it walks from there instead of from zero (one
-// rounding less where the state and the first input cancel) and its map has nothing left to depend on.
-template <bool DONE> __device__ __forceinline__ Map known(float c) { return Map{DONE ? -0.0f : 0.0f, c}; }
-
 // a = sigmoid(f) and b = 1 - a.  The smaller of the two is e / (1 + e) with e = exp(-|f|) (approximate exponential and
 // reciprocal: a few units in its last place), the larger is 1 minus it, rounded once: neither a long memory (b small,
 // where an error of a in its last places would add up over 1 / b steps) nor a memory wiped by the gate (a small) loses
@@ -58,24 +44,84 @@ __device__ __forceinline__ void gate(float f, float& a, float& b) {
     b = f < 0.0f ? big : small;
 }
 
+// V channels at once; two go through the packed instructions.
+template <int V> struct Chan { float v[V]; };
+__device__ __forceinline__ unsigned long long packed(const Chan<2>& x) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x.v[0]), "f"(x.v[1]));
+    return r;
+}
+__device__ __forceinline__ Chan<2> unpacked(unsigned long long r) {
+    Chan<2> x;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x.v[0]), "=f"(x.v[1]) : "l"(r));
+    return x;
+}
+__device__ __forceinline__ Chan<1> madd(const Chan<1>& a, const Chan<1>& b, const Chan<1>& c) { return Chan<1>{{fmaf(a.v[0], b.v[0], c.v[0])}}; }
+__device__ __forceinline__ Chan<1> mul(const Chan<1>& a, const Chan<1>& b) { return Chan<1>{{a.v[0] * b.v[0]}}; }
+__device__ __forceinline__ Chan<1> add(const Chan<1>& a, const Chan<1>& b) { return Chan<1>{{a.v[0] + b.v[0]}}; }
+__device__ __forceinline__ Chan<2> madd(const Chan<2>& a, const Chan<2>& b, const Chan<2>& c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(packed(a)), "l"(packed(b)), "l"(packed(c)));
+    return unpacked(r);
+}
+__device__ __forceinline__ Chan<2> mul(const Chan<2>& a, const Chan<2>& b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(packed(a)), "l"(packed(b)));
+    return unpacked(r);
+}
+__device__ __forceinline__ Chan<2> add(const Chan<2>& a, const Chan<2>& b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(packed(a)), "l"(packed(b)));
+    return unpacked(r);
+}
+template <int V> __device__ __forceinline__ Chan<V> all_of(float f) {
+    Chan<V> r;
+#pragma unroll
+    for (int v = 0; v < V; v++) r.v[v] = f;
+    return r;
+}
+// A map of V channels, as it lies in shared memory
+template <int V> struct alignas(8 * V) Maps { Chan<V> a, b; };
+template <int V, bool DONE> __device__ __forceinline__ Chan<V> apply(const Maps<V>& m, const Chan<V>& c) {
+    Chan<V> r = madd(m.a, c, m.b);
+    if (DONE) {
+#pragma unroll
+        for (int v = 0; v < V; v++)
+            if (__float_as_uint(m.a.v[v]) == 0x80000000u) r.v[v] = m.b.v[v];
+    }
+    return r;
+}
+// first m, then n
+template <int V, bool DONE> __device__ __forceinline__ Maps<V> then(const Maps<V>& m, const Maps<V>& n) {
+    Maps<V> r;
+    r.b = apply<V, DONE>(n, m.b);
+    r.a = mul(m.a, n.a);
+    if (DONE) {
+#pragma unroll
+        for (int v = 0; v < V; v++)
+            if (__float_as_uint(m.a.v[v]) == 0x80000000u || __float_as_uint(n.a.v[v]) == 0x80000000u) r.a.v[v] = -0.0f;
+    }
+    return r;
+}
+
 // What one lane reads of one step: a 32-bit word (one float, or two 16-bit channels), or a single 16-bit channel where
 // rows are not aligned to words.
 template <typename T, int V> struct Word;
 template <> struct Word<float, 1> {
     using type = float;
     static __device__ __forceinline__ float get(type w, int) { return w; }
-    static __device__ __forceinline__ type put(const float (&v)[1]) { return v[0]; }
+    static __device__ __forceinline__ type put(const Chan<1>& c) { return c.v[0]; }
 };
 template <typename T> struct Word<T, 1> {
     using type = T;
     static __device__ __forceinline__ float get(type w, int) { return to_f32<T>(w); }
-    static __device__ __forceinline__ type put(const float (&v)[1]) { return from_f32<T>(v[0]); }
+    static __device__ __forceinline__ type put(const Chan<1>& c) { return from_f32<T>(c.v[0]); }
 };
 template <> struct Word<__nv_bfloat16, 2> {
     using type = uint32_t;
     static __device__ __forceinline__ float get(type w, int v) { return __uint_as_float(v ? w & 0xffff0000u : w << 16); }
-    static __device__ __forceinline__ type put(const float (&v)[2]) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(v[0], v[1]);
+    static __device__ __forceinline__ type put(const Chan<2>& c) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(c.v[0], c.v[1]);
         return *reinterpret_cast<const uint32_t*>(&h);
     }
 };
@@ -85,8 +131,8 @@ template <> struct Word<__half, 2> {
         const __half2 h = *reinterpret_cast<const __half2*>(&w);
         return v ? __high2float(h) : __low2float(h);
     }
-    static __device__ __forceinline__ type put(const float (&v)[2]) {
-        const __half2 h = __floats2half2_rn(v[0], v[1]);
+    static __device__ __forceinline__ type put(const Chan<2>& c) {
+        const __half2 h = __floats2half2_rn(c.v[0], c.v[1]);
         return *reinterpret_cast<const uint32_t*>(&h);
     }
 };
@@ -117,11 +163,11 @@ struct RecurrenceGrid {
     int warps, cluster;     // warps of a block along time, blocks of a cluster along time
 };
 
-// Where the blocks of a cluster meet.
+// Where the warps of a block and the blocks of a cluster meet.
 template <int V>
 struct Meeting {
-    Map maps[2][kMaxWarps][32 * V];       // of this block's warps, by turn
-    Map slots[2][kMaxCluster][32 * V];    // of the cluster's blocks, by turn
+    Maps<V> maps[2][kMaxWarps][32];       // of this block's warps, by turn
+    Maps<V> slots[2][kMaxCluster][32];    // of the cluster's blocks, by turn
     uint64_t bar[2];
     int abort_flag;
 };
@@ -136,69 +182,61 @@ __device__ __forceinline__ uint32_t there(const void* p, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
     return a;
 }
-__device__ __forceinline__ void send(uint32_t to, uint32_t bar, const Map (&m)[1]) {
+__device__ __forceinline__ void send(uint32_t to, uint32_t bar, const Maps<1>& m) {
     asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%2, %3}, [%1];" ::"r"(to), "r"(bar),
-                 "r"(__float_as_uint(m[0].a)), "r"(__float_as_uint(m[0].b))
+                 "r"(__float_as_uint(m.a.v[0])), "r"(__float_as_uint(m.b.v[0]))
                  : "memory");
 }
-__device__ __forceinline__ void send(uint32_t to, uint32_t bar, const Map (&m)[2]) {
+__device__ __forceinline__ void send(uint32_t to, uint32_t bar, const Maps<2>& m) {
     asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%2, %3, %4, %5}, [%1];" ::"r"(to), "r"(bar),
-                 "r"(__float_as_uint(m[0].a)), "r"(__float_as_uint(m[0].b)), "r"(__float_as_uint(m[1].a)), "r"(__float_as_uint(m[1].b))
+                 "r"(__float_as_uint(m.a.v[0])), "r"(__float_as_uint(m.a.v[1])), "r"(__float_as_uint(m.b.v[0])), "r"(__float_as_uint(m.b.v[1]))
                  : "memory");
 }
 
-// Joins the maps of all pieces of a turn: `enter` is the state before this thread's piece, and carry, on entry the state
-// before the turn, the one behind it.  w, rank: this warp's and block's place in the turn (0 = first to act).
+// Joins the maps of all pieces of a turn.  Returns the state before this thread's piece; carry is, on entry, the state
+// before the turn and then the one behind it.  w, rank: this warp's and block's place in the turn (0 = first to act).
+// A warp composes only the maps ahead of it; the last warp has the block's and sends it.
 template <int V, bool DONE>
-__device__ __forceinline__ void join(const Map (&m)[V], float (&enter)[V], float (&carry)[V], Meeting<V>& sm, int warps, int w, int cluster,
-                                     int rank, int turn) {
+__device__ __forceinline__ Chan<V> join(const Maps<V>& m, Chan<V>& carry, Meeting<V>& sm, int warps, int w, int cluster, int rank, int turn) {
     const int lane = threadIdx.x & 31, par = turn & 1;
-    if (cluster > 1 && threadIdx.x == 0) mbar_expect_tx(&sm.bar[par], (uint32_t)(cluster * 32 * V * sizeof(Map)));
-    Map before[V], all[V];     // the pieces of this block ahead of this warp, and the whole block
-#pragma unroll
-    for (int v = 0; v < V; v++) {
-        before[v] = Map{1.0f, 0.0f};
-        all[v] = m[v];
-    }
+    if (cluster > 1 && threadIdx.x == 0) mbar_expect_tx(&sm.bar[par], (uint32_t)(cluster * 32 * sizeof(Maps<V>)));
+    Chan<V> enter = carry;
     if (warps > 1) {
-#pragma unroll
-        for (int v = 0; v < V; v++) sm.maps[par][w][lane * V + v] = m[v];
+        sm.maps[par][w][lane] = m;
         __syncthreads();
-#pragma unroll
-        for (int v = 0; v < V; v++) all[v] = sm.maps[par][0][lane * V + v];
-#pragma unroll
-        for (int k = 1; k < kMaxWarps; k++)
-            if (k < warps) {
-#pragma unroll
-                for (int v = 0; v < V; v++) {
-                    if (k == w) before[v] = all[v];
-                    all[v] = then<DONE>(all[v], sm.maps[par][k][lane * V + v]);
-                }
-            }
-    }
-    if (cluster > 1) {
-        // warp w tells blocks w, w + 8 (a cluster has all kMaxWarps warps in every block)
-        for (int r = w; r < cluster; r += kMaxWarps) send(there(&sm.slots[par][rank][lane * V], r), there(&sm.bar[par], r), all);
-        mbar_wait(&sm.bar[par], (uint32_t)(turn >> 1) & 1u, &sm.abort_flag);
-        float c[V];
-#pragma unroll
-        for (int v = 0; v < V; v++) c[v] = carry[v];
-#pragma unroll 4
-        for (int r = 0; r < cluster; r++)
-#pragma unroll
-            for (int v = 0; v < V; v++) {
-                if (r == rank) enter[v] = apply<DONE>(before[v], c[v]);
-                c[v] = apply<DONE>(sm.slots[par][r][lane * V + v], c[v]);
-            }
-#pragma unroll
-        for (int v = 0; v < V; v++) carry[v] = c[v];
-    } else {
-#pragma unroll
-        for (int v = 0; v < V; v++) {
-            enter[v] = apply<DONE>(before[v], carry[v]);
-            carry[v] = apply<DONE>(all[v], carry[v]);
+        if (cluster == 1) {     // the state itself walks along the warps
+            Chan<V> c = carry;
+            for (int k = 0; k < w; k++) c = apply<V, DONE>(sm.maps[par][k][lane], c);
+            enter = c;
+            for (int k = w; k < warps; k++) c = apply<V, DONE>(sm.maps[par][k][lane], c);
+            carry = c;
+            return enter;
         }
+        Maps<V> before;
+        before.a = all_of<V>(1.0f);
+        before.b = all_of<V>(0.0f);
+        for (int k = 0; k < w; k++) before = then<V, DONE>(before, sm.maps[par][k][lane]);
+        if (w == warps - 1) {
+            const Maps<V> all = then<V, DONE>(before, m);
+            const uint32_t to = smem_u32(&sm.slots[par][rank][lane]), bar = smem_u32(&sm.bar[par]);
+            for (int r = 0; r < cluster; r++) {
+                uint32_t rt, rb;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(rt) : "r"(to), "r"(r));
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(rb) : "r"(bar), "r"(r));
+                send(rt, rb, all);
+            }
+        }
+        mbar_wait(&sm.bar[par], (uint32_t)(turn >> 1) & 1u, &sm.abort_flag);
+        Chan<V> c = carry;
+        for (int r = 0; r < rank; r++) c = apply<V, DONE>(sm.slots[par][r][lane], c);
+        enter = apply<V, DONE>(before, c);
+#pragma unroll 4
+        for (int r = rank; r < cluster; r++) c = apply<V, DONE>(sm.slots[par][r][lane], c);
+        carry = c;
+        return enter;
     }
+    carry = apply<V, DONE>(m, carry);
+    return enter;
 }
 // Before the first turn: the barriers exist, and every block of the cluster runs, before another writes to its memory.
 template <int V>
@@ -242,9 +280,9 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const
     const T* x = static_cast<const T*>(p.x) + b * p.x_b + dl;
     T* h = static_cast<T*>(p.h) + b * p.h_b + dl;
     const unsigned char* done = DONE ? p.done + b * p.done_b : nullptr;
-    float carry[V];
+    Chan<V> carry;
 #pragma unroll
-    for (int v = 0; v < V; v++) carry[v] = p.h0 ? p.h0[b * p.dim + dl + v] : 0.0f;
+    for (int v = 0; v < V; v++) carry.v[v] = p.h0 ? p.h0[b * p.dim + dl + v] : 0.0f;
     const int per_turn = SINGLE ? 1 : g.warps * g.cluster;
     const int place = SINGLE ? 0 : rank * g.warps + w;
     W rf[L], rx[L];
@@ -266,55 +304,51 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const
         const long long piece = first + place, t0 = piece * L;
         const int now = n;
         const uint32_t ends = DONE ? __ballot_sync(0xffffffffu, now && flag) : 0;
-        float a[L][V], bx[L][V];
+        Chan<V> a[L], bx[L];
         if (now) {
 #pragma unroll
-            for (int i = 0; i < L; i++)
+            for (int i = 0; i < L; i++) {
+                Chan<V> bb, xv;
 #pragma unroll
                 for (int v = 0; v < V; v++) {
-                    float bb;
-                    gate(Wd::get(rf[i], v), a[i][v], bb);
-                    bx[i][v] = bb * Wd::get(rx[i], v);
+                    gate(Wd::get(rf[i], v), a[i].v[v], bb.v[v]);
+                    xv.v[v] = Wd::get(rx[i], v);
                 }
+                bx[i] = mul(bb, xv);
+            }
             if (!SINGLE && now < L) {
 #pragma unroll
                 for (int i = 1; i < L; i++)
-                    if (i >= now) {
-#pragma unroll
-                        for (int v = 0; v < V; v++) a[i][v] = 1.0f, bx[i][v] = 0.0f;
-                    }
+                    if (i >= now) a[i] = all_of<V>(1.0f), bx[i] = all_of<V>(0.0f);
             }
         }
         if (!SINGLE && first + per_turn < g.pieces) n = fetch(piece + per_turn);
-        float c[V];
-        if (SINGLE) {
-#pragma unroll
-            for (int v = 0; v < V; v++) c[v] = carry[v];
-        } else {
-            Map m[V];
-#pragma unroll
-            for (int v = 0; v < V; v++) m[v] = place == 0 ? known<DONE>(carry[v]) : Map{1.0f, 0.0f};
+        Chan<V> c = carry;
+        if (!SINGLE) {
+            // the first piece of a turn knows its state: it walks from there instead of from zero (one rounding less where
+            // the state and the first input cancel), and its map has nothing left to depend on
+            Maps<V> m;
+            m.a = all_of<V>(place == 0 ? (DONE ? -0.0f : 0.0f) : 1.0f);
+            m.b = place == 0 ? carry : all_of<V>(0.0f);
             if (now) {
                 if (DONE && ends) {
 #pragma unroll
-                    for (int i = 0; i < L; i++)
-#pragma unroll
-                        for (int v = 0; v < V; v++) {
-                            m[v].b = fmaf(a[i][v], m[v].b, bx[i][v]);
-                            m[v].a = cut<DONE>(m[v].a) ? -0.0f : m[v].a * a[i][v];
-                            if ((ends >> i) & 1u) m[v] = Map{-0.0f, 0.0f};
-                        }
+                    for (int i = 0; i < L; i++) {
+                        Maps<V> one;
+                        one.a = a[i];
+                        one.b = bx[i];
+                        if ((ends >> i) & 1u) one.a = all_of<V>(-0.0f), one.b = all_of<V>(0.0f);
+                        m = then<V, true>(m, one);
+                    }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < L; i++)
-#pragma unroll
-                        for (int v = 0; v < V; v++) {
-                            m[v].b = fmaf(a[i][v], m[v].b, bx[i][v]);
-                            m[v].a *= a[i][v];      // keeps the mark of a known state, unless a is NaN and all is lost
-                        }
+                    for (int i = 0; i < L; i++) {
+                        m.b = madd(a[i], m.b, bx[i]);
+                        m.a = mul(m.a, a[i]);      // keeps the mark of a known state, unless a is NaN and all is lost
+                    }
                 }
             }
-            join<V, DONE>(m, c, carry, sm, g.warps, w, g.cluster, rank, turn);
+            c = join<V, DONE>(m, carry, sm, g.warps, w, g.cluster, rank, turn);
         }
         if (!now) continue;
         float* s = p.states ? p.states + ((t0 / kStateStep) * p.batch + b) * p.dim + dl : nullptr;
@@ -324,31 +358,21 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const
 #pragma unroll
             for (int i = 0; i < L; i++) {
                 if (whole || i < now) {
-                    if (i % kStateStep == 0 && s && on) {
-#pragma unroll
-                        for (int v = 0; v < V; v++) s[(i / kStateStep) * p.batch * p.dim + v] = c[v];
-                    }
-#pragma unroll
-                    for (int v = 0; v < V; v++) c[v] = fmaf(a[i][v], c[v], bx[i][v]);
+                    if (i % kStateStep == 0 && s && on) *reinterpret_cast<Chan<V>*>(s + (i / kStateStep) * p.batch * p.dim) = c;
+                    c = madd(a[i], c, bx[i]);
                     if (on) *reinterpret_cast<W*>(ht) = Wd::put(c);
-                    if (flags && ((ends >> i) & 1u)) {
-#pragma unroll
-                        for (int v = 0; v < V; v++) c[v] = 0.0f;
-                    }
+                    if (flags && ((ends >> i) & 1u)) c = all_of<V>(0.0f);
                 }
                 ht += p.h_t;
             }
         };
         if (now < L || (DONE && ends)) walk(std::integral_constant<bool, DONE>{}, std::false_type{});
         else walk(std::false_type{}, std::true_type{});
-        if (SINGLE) {
-#pragma unroll
-            for (int v = 0; v < V; v++) carry[v] = c[v];
-        }
+        if (SINGLE) carry = c;
     }
     if (p.h_last && on && place == 0) {
 #pragma unroll
-        for (int v = 0; v < V; v++) p.h_last[b * p.dim + d + v] = carry[v];
+        for (int v = 0; v < V; v++) p.h_last[b * p.dim + d + v] = carry.v[v];
     }
     if (!SINGLE) part<V>(sm, g.cluster, p.status);
 }
@@ -376,13 +400,13 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
     T* df = static_cast<T*>(p.df) + b * p.df_b + dl;
     T* dx = static_cast<T*>(p.dx) + b * p.dx_b + dl;
     const unsigned char* done = DONE ? p.done + b * p.done_b : nullptr;
-    float carry[V];      // q of the step after those still to come
+    Chan<V> carry;       // q of the step after those still to come
 #pragma unroll
-    for (int v = 0; v < V; v++) carry[v] = p.dh_last ? p.dh_last[b * p.dim + dl + v] : 0.0f;
+    for (int v = 0; v < V; v++) carry.v[v] = p.dh_last ? p.dh_last[b * p.dim + dl + v] : 0.0f;
     const int per_turn = SINGLE ? 1 : g.warps * g.cluster;
     const int place = SINGLE ? 0 : rank * g.warps + w;       // 0 acts first and has the latest piece
-    W rf[L], rx[L], rg[L];
-    float rc[V];
+    W rf[L], rx[L], rg[L] = {};      // dh NULL: zeros
+    Chan<V> rc;
     uint32_t flag = 0;
     auto fetch = [&](long long piece) -> int {
         const long long t0 = piece * L;
@@ -393,7 +417,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
             if (dh) load_steps<L>(rg, dh + t0 * p.dh_t, p.dh_t, n);
             const float* s = p.states + ((t0 / kStateStep) * p.batch + b) * p.dim + dl;
 #pragma unroll
-            for (int v = 0; v < V; v++) rc[v] = s[v];
+            for (int v = 0; v < V; v++) rc.v[v] = s[v];
             if (DONE) flag = lane < n ? done[(t0 + lane) * p.done_t] : 0;
         }
         return n;
@@ -405,52 +429,51 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
         const long long piece = g.pieces - 1 - (first + place), t0 = piece * L;
         const int now = n;
         const uint32_t ends = DONE ? __ballot_sync(0xffffffffu, now && flag) : 0;
-        float a[L][V], bb[L][V], cx[L][V], gg[L][V];     // gates, c_{t-1} - x_t, dh_t
+        Chan<V> a[L], bb[L], cx[L], gg[L];     // gates, c_{t-1} - x_t, dh_t
         if (now) {
+            const Chan<V> minus = all_of<V>(-1.0f);
 #pragma unroll
-            for (int i = 0; i < L; i++)
+            for (int i = 0; i < L; i++) {
+                Chan<V> xv;
 #pragma unroll
                 for (int v = 0; v < V; v++) {
-                    const float xv = Wd::get(rx[i], v);
-                    gate(Wd::get(rf[i], v), a[i][v], bb[i][v]);
-                    cx[i][v] = rc[v] - xv;
-                    rc[v] = fmaf(a[i][v], rc[v], bb[i][v] * xv);
-                    if (DONE && ((ends >> i) & 1u)) rc[v] = 0.0f;
-                    gg[i][v] = dh ? Wd::get(rg[i], v) : 0.0f;
+                    gate(Wd::get(rf[i], v), a[i].v[v], bb[i].v[v]);
+                    xv.v[v] = Wd::get(rx[i], v);
+                    gg[i].v[v] = Wd::get(rg[i], v);
                 }
+                cx[i] = madd(xv, minus, rc);
+                rc = madd(a[i], rc, mul(bb[i], xv));
+                if (DONE && ends)
+                    if ((ends >> i) & 1u) rc = all_of<V>(0.0f);
+            }
         }
         if (!SINGLE && first + per_turn < g.pieces) n = fetch(piece - per_turn);
-        float q[V];
-        if (SINGLE) {
-#pragma unroll
-            for (int v = 0; v < V; v++) q[v] = carry[v];
-        } else {
-            Map m[V];
-#pragma unroll
-            for (int v = 0; v < V; v++) m[v] = place == 0 ? known<DONE>(carry[v]) : Map{1.0f, 0.0f};
+        Chan<V> q = carry;
+        if (!SINGLE) {
+            Maps<V> m;
+            m.a = all_of<V>(place == 0 ? (DONE ? -0.0f : 0.0f) : 1.0f);
+            m.b = place == 0 ? carry : all_of<V>(0.0f);
             if (now) {
                 if (now < L || (DONE && ends)) {
 #pragma unroll
                     for (int i = L - 1; i >= 0; i--)
                         if (i < now) {
-#pragma unroll
-                            for (int v = 0; v < V; v++) {
-                                if (DONE && ((ends >> i) & 1u)) m[v] = Map{-0.0f, 0.0f};
-                                m[v].b = a[i][v] * (gg[i][v] + m[v].b);
-                                m[v].a = cut<DONE>(m[v].a) ? -0.0f : m[v].a * a[i][v];
-                            }
+                            if (DONE && ((ends >> i) & 1u)) m.a = all_of<V>(-0.0f), m.b = all_of<V>(0.0f);
+                            m.b = mul(a[i], add(gg[i], m.b));
+                            Maps<V> one;
+                            one.a = a[i];
+                            one.b = all_of<V>(0.0f);
+                            m.a = then<V, DONE>(m, one).a;
                         }
                 } else {
 #pragma unroll
-                    for (int i = L - 1; i >= 0; i--)
-#pragma unroll
-                        for (int v = 0; v < V; v++) {
-                            m[v].b = a[i][v] * (gg[i][v] + m[v].b);
-                            m[v].a *= a[i][v];
-                        }
+                    for (int i = L - 1; i >= 0; i--) {
+                        m.b = mul(a[i], add(gg[i], m.b));
+                        m.a = mul(m.a, a[i]);
+                    }
                 }
             }
-            join<V, DONE>(m, q, carry, sm, g.warps, w, g.cluster, rank, turn);
+            q = join<V, DONE>(m, carry, sm, g.warps, w, g.cluster, rank, turn);
         }
         if (!now) continue;
         T* dft = df + (t0 + L - 1) * p.df_t;
@@ -460,14 +483,9 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
 #pragma unroll
             for (int i = L - 1; i >= 0; i--) {
                 if (whole || i < now) {
-                    float of[V], ox[V];
-#pragma unroll
-                    for (int v = 0; v < V; v++) {
-                        const float gt = flags && ((ends >> i) & 1u) ? gg[i][v] : gg[i][v] + q[v];
-                        q[v] = a[i][v] * gt;
-                        ox[v] = bb[i][v] * gt;
-                        of[v] = q[v] * bb[i][v] * cx[i][v];
-                    }
+                    const Chan<V> gt = flags && ((ends >> i) & 1u) ? gg[i] : add(gg[i], q);
+                    q = mul(a[i], gt);
+                    const Chan<V> ox = mul(bb[i], gt), of = mul(mul(q, bb[i]), cx[i]);
                     if (on) {
                         *reinterpret_cast<W*>(dft) = Wd::put(of);
                         *reinterpret_cast<W*>(dxt) = Wd::put(ox);
@@ -479,14 +497,11 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
         };
         if (now < L || (DONE && ends)) walk(std::integral_constant<bool, DONE>{}, std::false_type{});
         else walk(std::false_type{}, std::true_type{});
-        if (SINGLE) {
-#pragma unroll
-            for (int v = 0; v < V; v++) carry[v] = q[v];
-        }
+        if (SINGLE) carry = q;
     }
     if (p.dh0 && on && place == 0) {
 #pragma unroll
-        for (int v = 0; v < V; v++) p.dh0[b * p.dim + d + v] = carry[v];
+        for (int v = 0; v < V; v++) p.dh0[b * p.dim + d + v] = carry.v[v];
     }
     if (!SINGLE) part<V>(sm, g.cluster, p.status);
 }
@@ -501,9 +516,8 @@ __global__ void recurrence_pass_kernel(const float* src, float* dst, long long n
 // ------------------------------------------------------------------------------------------------ host side
 namespace {
 
-// How the time axis is cut.  Blocks along it are taken while there are pieces for them (even with many units, more and
-// shorter blocks fill the last wave of the grid better): up to eight, and sixteen where eight would leave part of the
-// device without a block.
+// How the time axis is cut.  A block takes turns along it, with the next turn's loads under way; blocks are set side by
+// side along it only until the device is full, up to sixteen.
 RecurrenceGrid plan(long long steps, long long batch, long long dim, int v, int piece) {
     RecurrenceGrid g;
     g.pieces = (steps + piece - 1) / piece;
@@ -511,8 +525,7 @@ RecurrenceGrid plan(long long steps, long long batch, long long dim, int v, int 
     g.units = batch * g.chan_blocks;
     g.warps = (int)(g.pieces < kMaxWarps ? g.pieces : kMaxWarps);
     g.cluster = 1;
-    const int most = g.units * 8 < 2 * sm_count() ? kMaxCluster : 8;
-    while (g.cluster < most && (long long)g.cluster * g.warps < g.pieces) g.cluster *= 2;
+    while (g.cluster < kMaxCluster && (long long)g.cluster * g.warps < g.pieces && g.units * g.cluster < 2 * sm_count()) g.cluster *= 2;
     return g;
 }
 
@@ -577,7 +590,7 @@ cudaError_t pass(const float* src, float* dst, long long n, cudaStream_t st) {
 // pairs of 16-bit channels where every row of every array starts on a pair's boundary
 bool pairs(const void* q, long long st, long long sb, size_t es) { return aligned(q, 2 * es) && st % 2 == 0 && sb % 2 == 0; }
 
-// units of 32 channels, up to 8 blocks each (16 only where units are few): the grid has to stay below 2^31 blocks
+// units of 32 channels, several blocks each only where units are few: the grid has to stay below 2^31 blocks
 bool too_many(long long batch, long long dim) { return batch > 0 && (dim + 31) / 32 > (1ll << 27) / batch; }
 
 }  // namespace

@@ -9,7 +9,7 @@
 //   a thread    takes 16 (backward: 8) successive steps of one 32-bit word of channels, holds them in registers and
 //               composes their map;
 //   a block     has a warp for each of up to 8 such pieces and joins the warps' maps through shared memory;
-//   a cluster   of up to 16 blocks joins the blocks' maps through distributed shared memory: each block sends its map
+//   a cluster   of up to 8 blocks joins the blocks' maps through distributed shared memory: each block sends its map
 //               to all others with stores that report to the receiver's mbarrier, so that nothing waits for the global
 //               stores under way (a cluster barrier does: 2.2 of 8 stall cycles an instruction).  The slots alternate; a
 //               block that sends its map of one turn has read the slots of the turn before.
@@ -29,7 +29,7 @@ namespace gala {
 constexpr int kStateStep = 8;    // distance of the stored states, and the steps of a thread in the backward kernel
 constexpr int kFwdPiece = 16;
 constexpr int kMaxWarps = 8;
-constexpr int kMaxCluster = 16;
+constexpr int kMaxCluster = 8;
 
 // a = sigmoid(f) and b = 1 - a.  The smaller of the two is e / (1 + e) with e = exp(-|f|) (approximate exponential and
 // reciprocal: a few units in its last place), the larger is 1 minus it, rounded once: neither a long memory (b small,
@@ -137,37 +137,37 @@ template <> struct Word<__half, 2> {
     }
 };
 
+// Element `i` rows of `stride` bytes on: one wide multiply-add (time strides are below 2^32 bytes).
+template <typename T> __device__ __forceinline__ T* rows_on(T* p, uint32_t stride, int i) {
+    unsigned long long r;
+    asm("mad.wide.u32 %0, %1, %2, %3;" : "=l"(r) : "r"(stride), "r"(i), "l"(reinterpret_cast<unsigned long long>(p)));
+    return reinterpret_cast<T*>(r);
+}
 // L successive steps of one lane, `n` of them inside the sequence (1 <= n; the others repeat the last one, so that all
 // loads are issued without a condition).
 template <int L, typename W, typename T>
-__device__ __forceinline__ void load_steps(W (&r)[L], const T* p, long long stride, int n) {
+__device__ __forceinline__ void load_steps(W (&r)[L], const T* p, uint32_t stride, int n) {
     if (n >= L) {
 #pragma unroll
-        for (int i = 0; i < L; i++) {
-            r[i] = *reinterpret_cast<const W*>(p);
-            p += stride;
-        }
+        for (int i = 0; i < L; i++) r[i] = *reinterpret_cast<const W*>(rows_on(p, stride, i));
     } else {
 #pragma unroll
-        for (int i = 0; i < L; i++) {
-            r[i] = *reinterpret_cast<const W*>(p);
-            if (i + 1 < n) p += stride;
-        }
+        for (int i = 0; i < L; i++) r[i] = *reinterpret_cast<const W*>(rows_on(p, stride, min(i, n - 1)));
     }
 }
 
 struct RecurrenceGrid {
     long long pieces;       // ceil(steps / L)
-    int chan_blocks;        // ceil(dim / (32 V))
+    int chan_blocks;        // of 32 V / S channels
     long long units;        // batch * chan_blocks
-    int warps, cluster;     // warps of a block along time, blocks of a cluster along time
+    int warps, cluster;     // warps of a block along time (S pieces each), blocks of a cluster along time
 };
 
-// Where the warps of a block and the blocks of a cluster meet.
-template <int V>
+// Where the pieces of a block and the blocks of a cluster meet.  S pieces share a warp, 32 / S lanes each.
+template <int V, int S>
 struct Meeting {
-    Maps<V> maps[2][kMaxWarps][32];       // of this block's warps, by turn
-    Maps<V> slots[2][kMaxCluster][32];    // of the cluster's blocks, by turn
+    Maps<V> maps[2][kMaxWarps * S][32 / S];       // of this block's pieces, by turn
+    Maps<V> slots[2][kMaxCluster][32 / S];        // of the cluster's blocks, by turn
     uint64_t bar[2];
     int abort_flag;
 };
@@ -194,53 +194,57 @@ __device__ __forceinline__ void send(uint32_t to, uint32_t bar, const Maps<2>& m
 }
 
 // Joins the maps of all pieces of a turn.  Returns the state before this thread's piece; carry is, on entry, the state
-// before the turn and then the one behind it.  w, rank: this warp's and block's place in the turn (0 = first to act).
-// A warp composes only the maps ahead of it; the last warp has the block's and sends it.
-template <int V, bool DONE>
-__device__ __forceinline__ Chan<V> join(const Maps<V>& m, Chan<V>& carry, Meeting<V>& sm, int warps, int w, int cluster, int rank, int turn) {
-    const int lane = threadIdx.x & 31, par = turn & 1;
-    if (cluster > 1 && threadIdx.x == 0) mbar_expect_tx(&sm.bar[par], (uint32_t)(cluster * 32 * sizeof(Maps<V>)));
-    Chan<V> enter = carry;
-    if (warps > 1) {
-        sm.maps[par][w][lane] = m;
-        __syncthreads();
-        if (cluster == 1) {     // the state itself walks along the warps
+// before the turn and then the one behind it.  at, rank: this piece's and block's place in the turn (0 = first to act).
+// A piece composes only the maps ahead of it; the last one has the block's and sends it.  `flagged`: whether this piece
+// has a map that cuts; the block takes the path that looks for them only where one of its pieces has.
+template <int V, int S, bool DONE>
+__device__ __forceinline__ Chan<V> join(const Maps<V>& m, Chan<V>& carry, Meeting<V, S>& sm, int pieces, int at, int cluster, int rank, int turn,
+                                        bool flagged) {
+    const int lane = (threadIdx.x & 31) % (32 / S), par = turn & 1;
+    if (cluster > 1 && threadIdx.x == 0) mbar_expect_tx(&sm.bar[par], (uint32_t)(cluster * (32 / S) * sizeof(Maps<V>)));
+    sm.maps[par][at][lane] = m;
+    Chan<V> enter;
+    if (cluster == 1) {     // the state itself walks along the pieces
+        auto along = [&](auto cuts_) {
+            constexpr bool cuts = decltype(cuts_)::value;
             Chan<V> c = carry;
-            for (int k = 0; k < w; k++) c = apply<V, DONE>(sm.maps[par][k][lane], c);
-            enter = c;
-            for (int k = w; k < warps; k++) c = apply<V, DONE>(sm.maps[par][k][lane], c);
-            carry = c;
-            return enter;
-        }
-        Maps<V> before;
-        before.a = all_of<V>(1.0f);
-        before.b = all_of<V>(0.0f);
-        for (int k = 0; k < w; k++) before = then<V, DONE>(before, sm.maps[par][k][lane]);
-        if (w == warps - 1) {
-            const Maps<V> all = then<V, DONE>(before, m);
-            const uint32_t to = smem_u32(&sm.slots[par][rank][lane]), bar = smem_u32(&sm.bar[par]);
-            for (int r = 0; r < cluster; r++) {
-                uint32_t rt, rb;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(rt) : "r"(to), "r"(r));
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(rb) : "r"(bar), "r"(r));
-                send(rt, rb, all);
-            }
-        }
-        mbar_wait(&sm.bar[par], (uint32_t)(turn >> 1) & 1u, &sm.abort_flag);
-        Chan<V> c = carry;
-        for (int r = 0; r < rank; r++) c = apply<V, DONE>(sm.slots[par][r][lane], c);
-        enter = apply<V, DONE>(before, c);
 #pragma unroll 4
-        for (int r = rank; r < cluster; r++) c = apply<V, DONE>(sm.slots[par][r][lane], c);
-        carry = c;
+            for (int k = 0; k < at; k++) c = apply<V, cuts>(sm.maps[par][k][lane], c);
+            enter = c;
+#pragma unroll 4
+            for (int k = at; k < pieces; k++) c = apply<V, cuts>(sm.maps[par][k][lane], c);
+            carry = c;
+        };
+        if (DONE) {
+            if (__syncthreads_or(flagged)) along(std::true_type{});
+            else along(std::false_type{});
+        } else {
+            __syncthreads();
+            along(std::false_type{});
+        }
         return enter;
     }
-    carry = apply<V, DONE>(m, carry);
+    __syncthreads();
+    Maps<V> before;
+    before.a = all_of<V>(1.0f);
+    before.b = all_of<V>(0.0f);
+    for (int k = 0; k < at; k++) before = then<V, DONE>(before, sm.maps[par][k][lane]);
+    if (at == pieces - 1) {
+        const Maps<V> all = then<V, DONE>(before, m);
+        for (int r = 0; r < cluster; r++) send(there(&sm.slots[par][rank][lane], r), there(&sm.bar[par], r), all);
+    }
+    mbar_wait(&sm.bar[par], (uint32_t)(turn >> 1) & 1u, &sm.abort_flag);
+    Chan<V> c = carry;
+    for (int r = 0; r < rank; r++) c = apply<V, DONE>(sm.slots[par][r][lane], c);
+    enter = apply<V, DONE>(before, c);
+#pragma unroll 4
+    for (int r = rank; r < cluster; r++) c = apply<V, DONE>(sm.slots[par][r][lane], c);
+    carry = c;
     return enter;
 }
 // Before the first turn: the barriers exist, and every block of the cluster runs, before another writes to its memory.
-template <int V>
-__device__ __forceinline__ void meet(Meeting<V>& sm, int cluster) {
+template <int V, int S>
+__device__ __forceinline__ void meet(Meeting<V, S>& sm, int cluster) {
     if (cluster == 1) return;
     if (threadIdx.x == 0) {
         mbar_init(&sm.bar[0], 1);
@@ -252,28 +256,28 @@ __device__ __forceinline__ void meet(Meeting<V>& sm, int cluster) {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // No block leaves while another may still send to it; reports a wait that ran out.
-template <int V>
-__device__ __forceinline__ void part(Meeting<V>& sm, int cluster, int* status) {
+template <int V, int S>
+__device__ __forceinline__ void part(Meeting<V, S>& sm, int cluster, int* status) {
     if (cluster == 1) return;
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (threadIdx.x == 0 && sm.abort_flag && status) atomicExch(status, 1);
 }
 
 // SINGLE: no more than L steps, so that a thread has the whole time axis; the warps of a block take different units.
-template <typename T, int V, int L, bool SINGLE, bool DONE>
+template <typename T, int V, int L, int S, bool SINGLE, bool DONE>
 __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const gala_recurrence_args p, const RecurrenceGrid g) {
-    __shared__ __align__(16) uint8_t meeting[SINGLE ? 16 : sizeof(Meeting<V>)];
-    Meeting<V>& sm = *reinterpret_cast<Meeting<V>*>(meeting);
+    __shared__ __align__(16) uint8_t meeting[SINGLE ? 16 : sizeof(Meeting<V, S>)];
+    Meeting<V, S>& sm = *reinterpret_cast<Meeting<V, S>*>(meeting);
     using Wd = Word<T, V>;
     using W = typename Wd::type;
-    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int w = threadIdx.x >> 5, lane = (threadIdx.x & 31) % (32 / S), sub = (threadIdx.x & 31) / (32 / S);
     const int rank = SINGLE ? 0 : (int)block_of_cluster();
     const long long unit = SINGLE ? (long long)blockIdx.x * (blockDim.x >> 5) + w : (long long)blockIdx.x / g.cluster;
     pdl_wait();
     pdl_launch();
     if (SINGLE && unit >= g.units) return;
     const long long b = unit / g.chan_blocks;
-    const long long d = (unit % g.chan_blocks) * 32 * V + lane * V;
+    const long long d = (unit % g.chan_blocks) * (32 / S) * V + lane * V;
     const bool on = d < p.dim;              // dim is a multiple of V; lanes past it work on channel 0 and write nothing
     const long long dl = on ? d : 0;
     const T* f = static_cast<const T*>(p.f) + b * p.f_b + dl;
@@ -283,27 +287,27 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const
     Chan<V> carry;
 #pragma unroll
     for (int v = 0; v < V; v++) carry.v[v] = p.h0 ? p.h0[b * p.dim + dl + v] : 0.0f;
-    const int per_turn = SINGLE ? 1 : g.warps * g.cluster;
-    const int place = SINGLE ? 0 : rank * g.warps + w;
+    const int mates = SINGLE ? 1 : g.warps * S, per_turn = SINGLE ? 1 : mates * g.cluster;     // pieces of the block, of a turn
+    const int at = SINGLE ? 0 : w * S + sub, place = SINGLE ? 0 : rank * mates + at;
     W rf[L], rx[L];
     uint32_t flag = 0;                       // this lane's step of the piece ends an episode
     auto fetch = [&](long long piece) -> int {
         const long long t0 = piece * L;
         const int n = t0 >= p.steps ? 0 : (int)(p.steps - t0 < L ? p.steps - t0 : L);
         if (n) {
-            load_steps<L>(rf, f + t0 * p.f_t, p.f_t, n);
-            load_steps<L>(rx, x + t0 * p.x_t, p.x_t, n);
+            load_steps<L>(rf, f + t0 * p.f_t, (uint32_t)(p.f_t * sizeof(T)), n);
+            load_steps<L>(rx, x + t0 * p.x_t, (uint32_t)(p.x_t * sizeof(T)), n);
             if (DONE) flag = lane < n ? done[(t0 + lane) * p.done_t] : 0;
         }
         return n;
     };
     int n = fetch(place);
-    if (!SINGLE) meet<V>(sm, g.cluster);
+    if (!SINGLE) meet<V, S>(sm, g.cluster);
     int turn = 0;
     for (long long first = 0; first < g.pieces; first += per_turn, turn++) {
         const long long piece = first + place, t0 = piece * L;
         const int now = n;
-        const uint32_t ends = DONE ? __ballot_sync(0xffffffffu, now && flag) : 0;
+        const uint32_t ends = DONE ? (__ballot_sync(0xffffffffu, now && flag) >> (sub * (32 / S))) & ((1u << L) - 1u) : 0;
         Chan<V> a[L], bx[L];
         if (now) {
 #pragma unroll
@@ -348,50 +352,51 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const
                     }
                 }
             }
-            c = join<V, DONE>(m, carry, sm, g.warps, w, g.cluster, rank, turn);
+            c = join<V, S, DONE>(m, carry, sm, mates, at, g.cluster, rank, turn, ends != 0);
         }
-        if (!now) continue;
-        float* s = p.states ? p.states + ((t0 / kStateStep) * p.batch + b) * p.dim + dl : nullptr;
-        T* ht = h + t0 * p.h_t;
-        auto walk = [&](auto flags_, auto whole_) {
-            constexpr bool flags = decltype(flags_)::value, whole = decltype(whole_)::value;
+        if (now) {
+            float* s = p.states ? p.states + ((t0 / kStateStep) * p.batch + b) * p.dim + dl : nullptr;
+            T* ht = h + t0 * p.h_t;
+            const uint32_t h_step = (uint32_t)(p.h_t * sizeof(T));
+            auto walk = [&](auto flags_, auto whole_) {
+                constexpr bool flags = decltype(flags_)::value, whole = decltype(whole_)::value;
 #pragma unroll
-            for (int i = 0; i < L; i++) {
-                if (whole || i < now) {
-                    if (i % kStateStep == 0 && s && on) *reinterpret_cast<Chan<V>*>(s + (i / kStateStep) * p.batch * p.dim) = c;
-                    c = madd(a[i], c, bx[i]);
-                    if (on) *reinterpret_cast<W*>(ht) = Wd::put(c);
-                    if (flags && ((ends >> i) & 1u)) c = all_of<V>(0.0f);
-                }
-                ht += p.h_t;
-            }
-        };
-        if (now < L || (DONE && ends)) walk(std::integral_constant<bool, DONE>{}, std::false_type{});
-        else walk(std::false_type{}, std::true_type{});
-        if (SINGLE) carry = c;
+                for (int i = 0; i < L; i++)
+                    if (whole || i < now) {
+                        if (i % kStateStep == 0 && s && on) *reinterpret_cast<Chan<V>*>(s + (i / kStateStep) * p.batch * p.dim) = c;
+                        c = madd(a[i], c, bx[i]);
+                        if (on) *reinterpret_cast<W*>(rows_on(ht, h_step, i)) = Wd::put(c);
+                        if (flags && ((ends >> i) & 1u)) c = all_of<V>(0.0f);
+                    }
+            };
+            if (now < L || (DONE && ends)) walk(std::integral_constant<bool, DONE>{}, std::false_type{});
+            else walk(std::false_type{}, std::true_type{});
+            if (SINGLE) carry = c;
+        }
+        __syncwarp();
     }
     if (p.h_last && on && place == 0) {
 #pragma unroll
         for (int v = 0; v < V; v++) p.h_last[b * p.dim + d + v] = carry.v[v];
     }
-    if (!SINGLE) part<V>(sm, g.cluster, p.status);
+    if (!SINGLE) part<V, S>(sm, g.cluster, p.status);
 }
 
-template <typename T, int V, int L, bool SINGLE, bool DONE>
+template <typename T, int V, int L, int S, bool SINGLE, bool DONE>
 __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const gala_recurrence_grad_args p, const RecurrenceGrid g) {
     static_assert(L <= kStateStep, "a piece begins where a state is stored");
-    __shared__ __align__(16) uint8_t meeting[SINGLE ? 16 : sizeof(Meeting<V>)];
-    Meeting<V>& sm = *reinterpret_cast<Meeting<V>*>(meeting);
+    __shared__ __align__(16) uint8_t meeting[SINGLE ? 16 : sizeof(Meeting<V, S>)];
+    Meeting<V, S>& sm = *reinterpret_cast<Meeting<V, S>*>(meeting);
     using Wd = Word<T, V>;
     using W = typename Wd::type;
-    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int w = threadIdx.x >> 5, lane = (threadIdx.x & 31) % (32 / S), sub = (threadIdx.x & 31) / (32 / S);
     const int rank = SINGLE ? 0 : (int)block_of_cluster();
     const long long unit = SINGLE ? (long long)blockIdx.x * (blockDim.x >> 5) + w : (long long)blockIdx.x / g.cluster;
     pdl_wait();
     pdl_launch();
     if (SINGLE && unit >= g.units) return;
     const long long b = unit / g.chan_blocks;
-    const long long d = (unit % g.chan_blocks) * 32 * V + lane * V;
+    const long long d = (unit % g.chan_blocks) * (32 / S) * V + lane * V;
     const bool on = d < p.dim;
     const long long dl = on ? d : 0;
     const T* f = static_cast<const T*>(p.f) + b * p.f_b + dl;
@@ -403,8 +408,8 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
     Chan<V> carry;       // q of the step after those still to come
 #pragma unroll
     for (int v = 0; v < V; v++) carry.v[v] = p.dh_last ? p.dh_last[b * p.dim + dl + v] : 0.0f;
-    const int per_turn = SINGLE ? 1 : g.warps * g.cluster;
-    const int place = SINGLE ? 0 : rank * g.warps + w;       // 0 acts first and has the latest piece
+    const int mates = SINGLE ? 1 : g.warps * S, per_turn = SINGLE ? 1 : mates * g.cluster;     // pieces of the block, of a turn
+    const int at = SINGLE ? 0 : w * S + sub, place = SINGLE ? 0 : rank * mates + at;       // 0 acts first and has the latest piece
     W rf[L], rx[L], rg[L] = {};      // dh NULL: zeros
     Chan<V> rc;
     uint32_t flag = 0;
@@ -412,9 +417,9 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
         const long long t0 = piece * L;
         const int n = piece < 0 ? 0 : (int)(p.steps - t0 < L ? p.steps - t0 : L);
         if (n) {
-            load_steps<L>(rf, f + t0 * p.f_t, p.f_t, n);
-            load_steps<L>(rx, x + t0 * p.x_t, p.x_t, n);
-            if (dh) load_steps<L>(rg, dh + t0 * p.dh_t, p.dh_t, n);
+            load_steps<L>(rf, f + t0 * p.f_t, (uint32_t)(p.f_t * sizeof(T)), n);
+            load_steps<L>(rx, x + t0 * p.x_t, (uint32_t)(p.x_t * sizeof(T)), n);
+            if (dh) load_steps<L>(rg, dh + t0 * p.dh_t, (uint32_t)(p.dh_t * sizeof(T)), n);
             const float* s = p.states + ((t0 / kStateStep) * p.batch + b) * p.dim + dl;
 #pragma unroll
             for (int v = 0; v < V; v++) rc.v[v] = s[v];
@@ -423,12 +428,12 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
         return n;
     };
     int n = fetch(g.pieces - 1 - place);
-    if (!SINGLE) meet<V>(sm, g.cluster);
+    if (!SINGLE) meet<V, S>(sm, g.cluster);
     int turn = 0;
     for (long long first = 0; first < g.pieces; first += per_turn, turn++) {
         const long long piece = g.pieces - 1 - (first + place), t0 = piece * L;
         const int now = n;
-        const uint32_t ends = DONE ? __ballot_sync(0xffffffffu, now && flag) : 0;
+        const uint32_t ends = DONE ? (__ballot_sync(0xffffffffu, now && flag) >> (sub * (32 / S))) & ((1u << L) - 1u) : 0;
         Chan<V> a[L], bb[L], cx[L], gg[L];     // gates, c_{t-1} - x_t, dh_t
         if (now) {
             const Chan<V> minus = all_of<V>(-1.0f);
@@ -473,37 +478,37 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
                     }
                 }
             }
-            q = join<V, DONE>(m, carry, sm, g.warps, w, g.cluster, rank, turn);
+            q = join<V, S, DONE>(m, carry, sm, mates, at, g.cluster, rank, turn, ends != 0);
         }
-        if (!now) continue;
-        T* dft = df + (t0 + L - 1) * p.df_t;
-        T* dxt = dx + (t0 + L - 1) * p.dx_t;
-        auto walk = [&](auto flags_, auto whole_) {
-            constexpr bool flags = decltype(flags_)::value, whole = decltype(whole_)::value;
+        if (now) {
+            T* dft = df + t0 * p.df_t;
+            T* dxt = dx + t0 * p.dx_t;
+            const uint32_t df_step = (uint32_t)(p.df_t * sizeof(T)), dx_step = (uint32_t)(p.dx_t * sizeof(T));
+            auto walk = [&](auto flags_, auto whole_) {
+                constexpr bool flags = decltype(flags_)::value, whole = decltype(whole_)::value;
 #pragma unroll
-            for (int i = L - 1; i >= 0; i--) {
-                if (whole || i < now) {
-                    const Chan<V> gt = flags && ((ends >> i) & 1u) ? gg[i] : add(gg[i], q);
-                    q = mul(a[i], gt);
-                    const Chan<V> ox = mul(bb[i], gt), of = mul(mul(q, bb[i]), cx[i]);
-                    if (on) {
-                        *reinterpret_cast<W*>(dft) = Wd::put(of);
-                        *reinterpret_cast<W*>(dxt) = Wd::put(ox);
+                for (int i = L - 1; i >= 0; i--)
+                    if (whole || i < now) {
+                        const Chan<V> gt = flags && ((ends >> i) & 1u) ? gg[i] : add(gg[i], q);
+                        q = mul(a[i], gt);
+                        const Chan<V> ox = mul(bb[i], gt), of = mul(mul(q, bb[i]), cx[i]);
+                        if (on) {
+                            *reinterpret_cast<W*>(rows_on(dft, df_step, i)) = Wd::put(of);
+                            *reinterpret_cast<W*>(rows_on(dxt, dx_step, i)) = Wd::put(ox);
+                        }
                     }
-                }
-                dft -= p.df_t;
-                dxt -= p.dx_t;
-            }
-        };
-        if (now < L || (DONE && ends)) walk(std::integral_constant<bool, DONE>{}, std::false_type{});
-        else walk(std::false_type{}, std::true_type{});
-        if (SINGLE) carry = q;
+            };
+            if (now < L || (DONE && ends)) walk(std::integral_constant<bool, DONE>{}, std::false_type{});
+            else walk(std::false_type{}, std::true_type{});
+            if (SINGLE) carry = q;
+        }
+        __syncwarp();
     }
     if (p.dh0 && on && place == 0) {
 #pragma unroll
         for (int v = 0; v < V; v++) p.dh0[b * p.dim + d + v] = carry.v[v];
     }
-    if (!SINGLE) part<V>(sm, g.cluster, p.status);
+    if (!SINGLE) part<V, S>(sm, g.cluster, p.status);
 }
 
 // steps == 0: the state passes through
@@ -516,17 +521,23 @@ __global__ void recurrence_pass_kernel(const float* src, float* dst, long long n
 // ------------------------------------------------------------------------------------------------ host side
 namespace {
 
-// How the time axis is cut.  A block takes turns along it, with the next turn's loads under way; blocks are set side by
-// side along it only until the device is full, up to sixteen.
-RecurrenceGrid plan(long long steps, long long batch, long long dim, int v, int piece) {
+// How the time axis is cut.  A block takes turns along it, with the next turn's loads under way.  Where units are few,
+// blocks are set side by side along it until the device is full (264 blocks of 256 threads in clusters of eight fit; one
+// more would be a second wave), and two pieces share a warp, which halves a unit's channels.
+RecurrenceGrid plan(long long steps, long long batch, long long dim, int lanes, int subs, int piece) {
     RecurrenceGrid g;
     g.pieces = (steps + piece - 1) / piece;
-    g.chan_blocks = (int)((dim + 32 * v - 1) / (32 * v));
+    g.chan_blocks = (int)((dim + lanes - 1) / lanes);
     g.units = batch * g.chan_blocks;
-    g.warps = (int)(g.pieces < kMaxWarps ? g.pieces : kMaxWarps);
+    const long long want = (g.pieces + subs - 1) / subs;
+    g.warps = (int)(want < kMaxWarps ? want : kMaxWarps);
     g.cluster = 1;
-    while (g.cluster < kMaxCluster && (long long)g.cluster * g.warps < g.pieces && g.units * g.cluster < 2 * sm_count()) g.cluster *= 2;
+    while (g.cluster < kMaxCluster && (long long)g.cluster * g.warps < want && g.units * g.cluster * 2 <= sm_count() * 16 / 9) g.cluster *= 2;
     return g;
+}
+// two pieces a warp pay where even clusters of eight leave part of the device idle
+bool narrow(long long steps, long long batch, long long dim, int v, int piece) {
+    return steps > 2 * piece && batch * ((dim + 32 * v - 1) / (32 * v)) * kMaxCluster < sm_count();
 }
 
 template <typename Args>
@@ -544,27 +555,27 @@ cudaError_t launch_units(void (*kernel)(Args, RecurrenceGrid), const Args& a, co
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = single || g.cluster == 1 ? 1 : 2;
-    if (!single && g.cluster > 8) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
-    }
     return cudaLaunchKernelEx(&cfg, kernel, a, g);
 }
 
 template <typename T, int V, bool DONE>
 cudaError_t fwd(const gala_recurrence_args& a, cudaStream_t st) {
-    const RecurrenceGrid g = plan(a.steps, a.batch, a.dim, V, kFwdPiece);
-    if (a.steps == 1) return launch_units(recurrence_fwd_kernel<T, V, 1, true, DONE>, a, g, true, st);
-    if (a.steps <= 8) return launch_units(recurrence_fwd_kernel<T, V, 8, true, DONE>, a, g, true, st);
-    if (g.pieces == 1) return launch_units(recurrence_fwd_kernel<T, V, kFwdPiece, true, DONE>, a, g, true, st);
-    return launch_units(recurrence_fwd_kernel<T, V, kFwdPiece, false, DONE>, a, g, false, st);
+    const bool two = narrow(a.steps, a.batch, a.dim, V, kFwdPiece);
+    const RecurrenceGrid g = plan(a.steps, a.batch, a.dim, two ? 16 * V : 32 * V, two ? 2 : 1, kFwdPiece);
+    if (a.steps == 1) return launch_units(recurrence_fwd_kernel<T, V, 1, 1, true, DONE>, a, g, true, st);
+    if (a.steps <= 8) return launch_units(recurrence_fwd_kernel<T, V, 8, 1, true, DONE>, a, g, true, st);
+    if (g.pieces == 1) return launch_units(recurrence_fwd_kernel<T, V, kFwdPiece, 1, true, DONE>, a, g, true, st);
+    if (two) return launch_units(recurrence_fwd_kernel<T, V, kFwdPiece, 2, false, DONE>, a, g, false, st);
+    return launch_units(recurrence_fwd_kernel<T, V, kFwdPiece, 1, false, DONE>, a, g, false, st);
 }
 template <typename T, int V, bool DONE>
 cudaError_t bwd(const gala_recurrence_grad_args& a, cudaStream_t st) {
-    const RecurrenceGrid g = plan(a.steps, a.batch, a.dim, V, kStateStep);
-    if (a.steps == 1) return launch_units(recurrence_bwd_kernel<T, V, 1, true, DONE>, a, g, true, st);
-    if (g.pieces == 1) return launch_units(recurrence_bwd_kernel<T, V, kStateStep, true, DONE>, a, g, true, st);
-    return launch_units(recurrence_bwd_kernel<T, V, kStateStep, false, DONE>, a, g, false, st);
+    const bool two = narrow(a.steps, a.batch, a.dim, V, kStateStep);
+    const RecurrenceGrid g = plan(a.steps, a.batch, a.dim, two ? 16 * V : 32 * V, two ? 2 : 1, kStateStep);
+    if (a.steps == 1) return launch_units(recurrence_bwd_kernel<T, V, 1, 1, true, DONE>, a, g, true, st);
+    if (g.pieces == 1) return launch_units(recurrence_bwd_kernel<T, V, kStateStep, 1, true, DONE>, a, g, true, st);
+    if (two) return launch_units(recurrence_bwd_kernel<T, V, kStateStep, 2, false, DONE>, a, g, false, st);
+    return launch_units(recurrence_bwd_kernel<T, V, kStateStep, 1, false, DONE>, a, g, false, st);
 }
 template <typename T, int V>
 cudaError_t run(const gala_recurrence_args& a, cudaStream_t st) {
@@ -590,8 +601,8 @@ cudaError_t pass(const float* src, float* dst, long long n, cudaStream_t st) {
 // pairs of 16-bit channels where every row of every array starts on a pair's boundary
 bool pairs(const void* q, long long st, long long sb, size_t es) { return aligned(q, 2 * es) && st % 2 == 0 && sb % 2 == 0; }
 
-// units of 32 channels, several blocks each only where units are few: the grid has to stay below 2^31 blocks
-bool too_many(long long batch, long long dim) { return batch > 0 && (dim + 31) / 32 > (1ll << 27) / batch; }
+// units of at least 16 channels, several blocks each only where units are few: the grid has to stay below 2^31 blocks
+bool too_many(long long batch, long long dim) { return batch > 0 && (dim + 15) / 16 > (1ll << 27) / batch; }
 
 }  // namespace
 }  // namespace gala
@@ -616,6 +627,7 @@ extern "C" int gala_gated_recurrence_forward(const gala_recurrence_args* p, void
     if (!aligned(a.f, es) || !aligned(a.x, es) || !aligned(a.h, es)) SAY("gala_gated_recurrence_forward: a pointer is not aligned to its element type");
     if (a.f_t < 0 || a.f_b < 0 || a.x_t < 0 || a.x_b < 0 || a.h_t < 0 || a.h_b < 0 || a.done_t < 0 || a.done_b < 0)
         SAY("gala_gated_recurrence_forward: negative stride");
+    if ((a.f_t | a.x_t | a.h_t) >= (1ll << 30)) SAY("gala_gated_recurrence_forward: time strides are below 2^30 elements");
     if ((a.steps > 1 && a.h_t < a.dim) || (a.batch > 1 && a.h_b < a.dim)) SAY("gala_gated_recurrence_forward: rows of h overlap");
     const bool two = a.dim % 2 == 0 && pairs(a.f, a.f_t, a.f_b, es) && pairs(a.x, a.x_t, a.x_b, es) && pairs(a.h, a.h_t, a.h_b, es);
     const cudaError_t e = by_type(a, two, st);
@@ -640,6 +652,7 @@ extern "C" int gala_gated_recurrence_backward(const gala_recurrence_grad_args* p
     if (a.f_t < 0 || a.f_b < 0 || a.x_t < 0 || a.x_b < 0 || a.dh_t < 0 || a.dh_b < 0 || a.df_t < 0 || a.df_b < 0 || a.dx_t < 0 || a.dx_b < 0 ||
         a.done_t < 0 || a.done_b < 0)
         SAY("gala_gated_recurrence_backward: negative stride");
+    if ((a.f_t | a.x_t | a.dh_t | a.df_t | a.dx_t) >= (1ll << 30)) SAY("gala_gated_recurrence_backward: time strides are below 2^30 elements");
     if ((a.steps > 1 && (a.df_t < a.dim || a.dx_t < a.dim)) || (a.batch > 1 && (a.df_b < a.dim || a.dx_b < a.dim)))
         SAY("gala_gated_recurrence_backward: rows of df or dx overlap");
     const bool two = a.dim % 2 == 0 && pairs(a.f, a.f_t, a.f_b, es) && pairs(a.x, a.x_t, a.x_b, es) && (!a.dh || pairs(a.dh, a.dh_t, a.dh_b, es)) &&

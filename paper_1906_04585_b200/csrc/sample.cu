@@ -2,13 +2,20 @@
 //
 // Every filter keeps a prefix of the ranking (largest logit first, ties by lowest index), so nothing is sorted: a filter
 // is a threshold - a key, and how many of the entries equal to it stay - and the draw is a sum in the order of the index.
-// A logit becomes an unsigned key whose order is the logit's.  A threshold is found bit by bit from the top: a bit stays
-// set when the entries at or above the key so far still reach the wanted count (top-k) or mass (top-p); 16 to 32 sums
-// over the row, which stays in registers from its one read on.
+// A logit becomes an unsigned key whose order is the logit's; the row stays in registers from its one read on.
 //
 // A row belongs to a team: a warp (up to 1024 entries; four rows a block), a block (up to 32768), or a cluster of up to
-// eight blocks, whose sums go through distributed shared memory.  Weights are summed as whole multiples of 2^-44 in 64
-// bits: any order and any team gives the same sum, and the sums of up to 2^18 weights fit.
+// eight blocks, whose sums go through distributed shared memory.
+// A warp finds a threshold bit by bit from the top: a bit stays set when the entries at or above the key so far still
+// reach the wanted count (top-k) or mass (top-p).  A block or a cluster finds it by histograms in shared memory: the first
+// one over equal steps of (m - l) / T, where the entries are spread well (over the key's own leading bits most would fall
+// into a dozen bins and the atomics would queue), the next ones over the keys of the bin that holds the threshold, 2048
+// bins each, until a bin is one key: two rounds for 16-bit logits, two or three for 32-bit ones.  The first round leaves
+// out the tail that cannot matter: what lies 16 and more below the largest, and, for top-p, weights so small that all of
+// them together cannot reach the share that is cut off.
+//
+// Weights are summed as whole multiples of 2^-44 in 64 bits: any order, any team and any atomics give the same sum, and
+// the sums of up to 2^18 weights fit.
 #include <cooperative_groups.h>
 
 #include "sequence.cuh"
@@ -48,6 +55,16 @@ __device__ __forceinline__ u64 warp_sum(u64 v) {
 
 enum { TEAM_WARP, TEAM_BLOCK, TEAM_CLUSTER };
 
+constexpr int kBins = 2048;
+constexpr float kFirstBins = 128.0f;      // bins of one unit of (m - l) / T in the first round
+struct Histogram {
+    uint32_t lo[kBins], hi[kBins];        // 64-bit sums as two words with a carry
+    u64 sums[32];                         // of the warps
+    u64 before;                           // answer: sum ahead of the bin
+    int bin;
+    uint32_t least[32], most[32];
+};
+
 // Sums over a team.  Every exchange uses the slots of the other parity than the one before, so that one barrier each does.
 template <int TEAM>
 struct Team {
@@ -61,6 +78,35 @@ struct Team {
         if (TEAM == TEAM_WARP) return v;
         u64 mine, ahead;
         return exchange(v, mine, ahead);
+    }
+    // smallest and largest of the team's values
+    __device__ __forceinline__ void extremes(uint32_t& least, uint32_t& most) {
+        least = __reduce_min_sync(0xffffffffu, least);
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (TEAM == TEAM_WARP) return;
+        const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        const u64 none = 0xffffffff00000000ull;
+        u64* ws = warp_slots + par * 32;
+        if (lane == 0) ws[w] = ((u64)least << 32) | most;
+        __syncthreads();
+        u64 x = lane < warps ? ws[lane] : none;
+        least = __reduce_min_sync(0xffffffffu, (uint32_t)(x >> 32));
+        most = __reduce_max_sync(0xffffffffu, (uint32_t)x);
+        if (TEAM == TEAM_CLUSTER) {
+            cg::cluster_group cl = cg::this_cluster();
+            u64* rs = rank_slots + par * 8;
+            if (w == 0 && lane < ranks) *cl.map_shared_rank(rs + rank, lane) = ((u64)least << 32) | most;
+            cl.sync();
+            x = lane < ranks ? rs[lane] : none;
+            least = __reduce_min_sync(0xffffffffu, (uint32_t)(x >> 32));
+            most = __reduce_max_sync(0xffffffffu, (uint32_t)x);
+        }
+        par ^= 1;
+    }
+    // every thread of the team has come here
+    __device__ __forceinline__ void barrier() {
+        if (TEAM == TEAM_CLUSTER) cg::this_cluster().sync();
+        else if (TEAM == TEAM_BLOCK) __syncthreads();
     }
     // v: this warp's value.  Returns the team's sum; `ahead` is the sum over the warps before this one.
     __device__ __forceinline__ u64 scan(u64 v, u64& ahead) {
@@ -98,7 +144,7 @@ template <typename T, int E, int TEAM>
 __global__ void __launch_bounds__(TEAM == TEAM_WARP ? 128 : 1024) sample_kernel(const gala_sample_args p, const int ranks) {
     __shared__ u64 warp_slots[64];
     __shared__ u64 rank_slots[16];
-    __shared__ int chosen;      // block and cluster: the drawing warp's token
+    __shared__ __align__(8) uint8_t hist_memory[TEAM == TEAM_WARP ? 8 : sizeof(Histogram)];
     const int lane = threadIdx.x & 31;
     Team<TEAM> team;
     team.warp_slots = warp_slots;
@@ -114,7 +160,6 @@ __global__ void __launch_bounds__(TEAM == TEAM_WARP ? 128 : 1024) sample_kernel(
     else row = TEAM == TEAM_CLUSTER ? (long long)(blockIdx.x / ranks) : (long long)blockIdx.x;
     if (TEAM == TEAM_WARP && row >= p.rows) return;
     if (TEAM == TEAM_CLUSTER) cg::this_cluster().sync();     // every block runs before one writes to another's shared memory
-    (void)chosen;
 
     // this warp's 32 E successive entries; entry i of a lane is at base + 32 i + lane
     const int base = team.place() * 32 * E + lane;
@@ -122,35 +167,34 @@ __global__ void __launch_bounds__(TEAM == TEAM_WARP ? 128 : 1024) sample_kernel(
     uint32_t key[E];
 #pragma unroll
     for (int i = 0; i < E; i++) key[i] = base + 32 * i < p.vocab ? key_of<T>(to_f32<T>(l[base + 32 * i])) : 0u;
-    uint32_t top = 0;
+    uint32_t top = 0, unused = 0;
 #pragma unroll
     for (int i = 0; i < E; i++) top = max(top, key[i]);
-    top = __reduce_max_sync(0xffffffffu, top);
+    team.extremes(unused, top);
     const float temp = p.temperature ? p.temperature[row] : 1.0f;
     const bool greedy = !(temp > 0.0f);
-    if (TEAM != TEAM_WARP) {
-        // the largest key through the same slots
-        const int w = threadIdx.x >> 5;
-        if (lane == 0) warp_slots[team.par * 32 + w] = top;
-        __syncthreads();
-        top = __reduce_max_sync(0xffffffffu, lane < team.warps ? (uint32_t)warp_slots[team.par * 32 + lane] : 0u);
-        if (TEAM == TEAM_CLUSTER) {
-            cg::cluster_group cl = cg::this_cluster();
-            u64* rs = rank_slots + team.par * 8;
-            if (w == 0 && lane < ranks) *cl.map_shared_rank(rs + team.rank, lane) = top;
-            cl.sync();
-            top = __reduce_max_sync(0xffffffffu, lane < ranks ? (uint32_t)rs[lane] : 0u);
-        }
-        team.par ^= 1;
-    }
     const bool empty = top <= key_bottom<T>();
     const float lmax = logit_of<T>(top);
+    // (l - m) / T by the row's reciprocal and one correction step with the exact remainder (Markstein), which is the
+    // rounded quotient; plain division where the reciprocal leaves the normal range
+    const float inv = 1.0f / temp;
+    const bool plain = !(temp > 1e-30f && temp < 1e30f);
     auto weight = [&](uint32_t k) -> float {
         if (k == top) return 1.0f;
         if (k <= key_bottom<T>()) return 0.0f;
-        return expf(__fdiv_rn(logit_of<T>(k) - lmax, temp));
+        const float d = logit_of<T>(k) - lmax;
+        float z = plain ? __fdiv_rn(d, temp) : d * inv;
+        if (z < -150.0f) return 0.0f;                     // and nothing infinite goes on
+        if (!plain) z = fmaf(fmaf(-z, temp, d), inv, z);
+        return expf(z);
     };
-    auto quant = [&](float w) -> u64 { return __float2ull_rn(w * kOne); };
+    // w 2^44 as a whole number, without the conversion unit: 22 bits at a time in the mantissa of 2^23
+    auto quant = [&](float w) -> u64 {
+        const float a = fmaf(w, 4194304.0f, 8388608.0f);                    // 2^23 + the nearest multiple of 2^-22
+        const float rest = fmaf(a - 8388608.0f, -1.0f / 4194304.0f, w);     // exact, within 2^-23
+        const float b = fmaf(rest, 17592186044416.0f, 12582912.0f);         // 1.5 2^23 + the rest in units of 2^-44
+        return ((u64)(__float_as_uint(a) & 0x7fffffu) << 22) + (u64)(long long)((int)(__float_as_uint(b) & 0x7fffffu) - 0x400000);
+    };
 
     // kept: key > cut, and the first `room` of those equal to it
     uint32_t cut = key_bottom<T>();
@@ -162,24 +206,125 @@ __global__ void __launch_bounds__(TEAM == TEAM_WARP ? 128 : 1024) sample_kernel(
             if (key[i] >= at) s += mass ? quant(weight(key[i])) : 1ull;
         return team.sum(s);
     };
-    // the largest key whose entries at or above it reach `want` (which the whole row does)
-    auto search = [&](u64 want, bool mass) -> uint32_t {
-        uint32_t k = 0;
-        for (int b = 31 - kDrop<T>; b >= 0; b--)
-            if (reach(k | (1u << b), mass) >= want) k |= 1u << b;
-        return k;
+    // The largest key whose entries at or above it, of those above `floor`, reach `want`, which all of them together do;
+    // `ahead` is the count or mass above it.  Entries that weigh less than `least` cannot be what reaches it.
+    auto search = [&](u64 want, bool mass, float least, uint32_t floor, u64& ahead) -> uint32_t {
+        if (TEAM == TEAM_WARP) {
+            uint32_t k = 0;
+            for (int b = 31 - kDrop<T>; b >= 0; b--)
+                if (reach(k | (1u << b), mass) >= want) k |= 1u << b;
+            ahead = reach(k + 1, mass);
+            return k;
+        }
+        Histogram& h = *reinterpret_cast<Histogram*>(hist_memory);
+        const int w = threadIdx.x >> 5, nt = blockDim.x;
+        // one round: bin_of(key) is the bin of an entry or -1; returns the bin that reaches `want` (-1: none does)
+        auto round = [&](auto bin_of) -> int {
+            team.barrier();        // nobody reads the last round's bins any more
+            for (int i = threadIdx.x; i < kBins; i += nt) h.lo[i] = h.hi[i] = 0;
+            if (threadIdx.x == 0) h.bin = -1;
+            __syncthreads();
+            int at = -1;           // entries of one bin after another are added up before they go to memory
+            u64 run = 0;
+            auto flush = [&] {
+                const uint32_t low = (uint32_t)run, old = atomicAdd(&h.lo[at], low);
+                const uint32_t high = (uint32_t)(run >> 32) + (old + low < old ? 1u : 0u);
+                if (high) atomicAdd(&h.hi[at], high);
+            };
+#pragma unroll
+            for (int i = 0; i < E; i++) {
+                const int b = bin_of(key[i]);
+                if (b >= 0) {
+                    const u64 q = mass ? quant(weight(key[i])) : 1ull;
+                    if (b != at) {
+                        if (at >= 0) flush();
+                        at = b;
+                        run = 0;
+                    }
+                    run += q;
+                }
+            }
+            if (at >= 0) flush();
+            team.barrier();
+            const int per = (kBins + nt - 1) / nt, b0 = (int)threadIdx.x * per, b1 = min(b0 + per, kBins);
+            auto value = [&](int b) -> u64 {
+                if (TEAM == TEAM_BLOCK) return ((u64)h.hi[b] << 32) | h.lo[b];
+                cg::cluster_group cl = cg::this_cluster();
+                u64 v = 0;
+                for (int r = 0; r < team.ranks; r++) v += ((u64)*cl.map_shared_rank(&h.hi[b], r) << 32) + *cl.map_shared_rank(&h.lo[b], r);
+                return v;
+            };
+            u64 mine = 0;
+            for (int b = b0; b < b1; b++) mine += value(b);
+            u64 upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const u64 up = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += up;
+            }
+            if (lane == 31) h.sums[w] = upto;
+            __syncthreads();
+            const u64 x = lane < team.warps ? h.sums[lane] : 0;
+            const u64 start = warp_sum(lane < w ? x : 0) + upto - mine;
+            const u64 need = want - ahead;
+            if (start < need && start + mine >= need) {        // one thread at most
+                u64 c = start;
+                for (int b = b0; b < b1; b++) {
+                    const u64 v = value(b);
+                    if (c + v >= need) {
+                        h.bin = b;
+                        h.before = c;
+                        break;
+                    }
+                    c += v;
+                }
+            }
+            __syncthreads();
+            const int b = h.bin;
+            if (b >= 0) ahead += h.before;
+            return b;
+        };
+        ahead = 0;
+        uint32_t least_key = floor + 1, most_key = top;
+        auto step_of = [&](uint32_t k) -> int { return plain ? 0 : min((int)((lmax - logit_of<T>(k)) * inv * kFirstBins), kBins - 1); };
+        const int first = round([&](uint32_t k) -> int {
+            if (k <= floor) return -1;
+            if (k == top) return 0;
+            const int b = step_of(k);
+            return b == kBins - 1 || (mass && weight(k) < least) ? -1 : b;
+        });
+        if (first >= 0) {
+            uint32_t lo = 0xffffffffu, hi = 0;
+#pragma unroll
+            for (int i = 0; i < E; i++)
+                if (key[i] > floor && (key[i] == top ? 0 : step_of(key[i])) == first) {
+                    lo = min(lo, key[i]);
+                    hi = max(hi, key[i]);
+                }
+            team.extremes(lo, hi);
+            least_key = lo;
+            most_key = hi;
+        }
+        while (least_key < most_key) {
+            const int shift = max(0, 21 - __clz(most_key - least_key));
+            const int b = round([&](uint32_t k) -> int { return k < least_key || k > most_key ? -1 : (int)((most_key - k) >> shift); });
+            if (b < 0) break;      // does not happen: the range reaches `want`
+            most_key -= (uint32_t)b << shift;
+            const uint32_t span = (1u << shift) - 1u;
+            if (most_key - least_key > span) least_key = most_key - span;
+        }
+        return most_key;
     };
     if (greedy) {
         cut = top;
         room = 1;
     } else if (!empty) {
         const int k = p.top_k ? p.top_k[row] : 0;
-        if (k > 0 && k < p.vocab) {
-            const uint32_t at = search((u64)k, false);
-            if (at > cut) {      // otherwise fewer than k entries can be drawn at all
-                cut = at;
-                room = k - (long long)reach(at + 1, false);
-            }
+        // with fewer than k entries that can be drawn at all, nothing is cut
+        if (k > 0 && k < p.vocab && reach(cut + 1, false) > (u64)k) {
+            u64 ahead;
+            cut = search((u64)k, false, 0.0f, cut, ahead);
+            room = k - (long long)ahead;
         }
         const float tp = p.top_p ? p.top_p[row] : 1.0f;
         if (!(tp >= 1.0f)) {
@@ -187,13 +332,12 @@ __global__ void __launch_bounds__(TEAM == TEAM_WARP ? 128 : 1024) sample_kernel(
             const u64 sum = above + (u64)room * each;
             const double goal = ceil((double)tp * (double)sum);
             const u64 want = goal >= 1.0 ? (u64)goal : 1ull;       // NaN and what is not positive: the first alone
-            u64 ahead;
+            u64 ahead = above;
             if (above >= want) {
-                cut = search(want, true);
-                ahead = reach(cut + 1, true);
+                // all entries lighter than this together weigh less than half of what is cut off
+                const float least = 0.5f * (1.0f - fmaxf(tp, 0.0f)) * (float)((double)above / (double)kOne) / (float)p.vocab;
+                cut = search(want, true, least >= 0.0f ? least : 0.0f, cut, ahead);
                 room = p.vocab;
-            } else {
-                ahead = above;
             }
             // ties stay while what is ranked before them is less than wanted
             const u64 one = quant(weight(cut));

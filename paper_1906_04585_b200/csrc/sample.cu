@@ -28,26 +28,25 @@ constexpr float kOne = 17592186044416.0f;   // 2^44
 typedef unsigned long long u64;
 
 // Key of a logit: unsigned order = order of the values, in as many bits as the type has.
+template <typename T> using Bits = typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type;
 template <typename T> constexpr int kKeyBits = 8 * (int)sizeof(T);
+template <typename T> constexpr uint32_t kInfinite = std::is_same<T, float>::value ? 0x7f800000u : std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
 template <typename T>
-__device__ __forceinline__ uint32_t key_of(float l) {
-    if (isnan(l)) l = -INFINITY;
-    l += 0.0f;       // -0 and +0 tie
-    constexpr uint32_t sign = 1u << (kKeyBits<T> - 1);
-    uint32_t u = __float_as_uint(l);
-    if (std::is_same<T, __nv_bfloat16>::value) u >>= 16;                       // l is a bfloat16 number, or a float16 one
-    if (std::is_same<T, __half>::value) u = __half_as_ushort(__float2half_rn(l));
-    return u & sign ? ~u & (2u * sign - 1u) : u | sign;
+__device__ __forceinline__ uint32_t key_of(uint32_t u) {       // from the stored bits
+    constexpr uint32_t sign = 1u << (kKeyBits<T> - 1), rest = sign - 1u;
+    if ((u & rest) > kInfinite<T>) u = sign | kInfinite<T>;    // NaN counts as -inf
+    if (u == sign) u = 0;                                      // -0 and +0 tie
+    return u & sign ? ~u & (sign | rest) : u | sign;
 }
 template <typename T>
 __device__ __forceinline__ float logit_of(uint32_t key) {
-    constexpr uint32_t sign = 1u << (kKeyBits<T> - 1);
-    const uint32_t u = key & sign ? key & (sign - 1u) : ~key & (2u * sign - 1u);
+    constexpr uint32_t sign = 1u << (kKeyBits<T> - 1), rest = sign - 1u;
+    const uint32_t u = key & sign ? key & rest : ~key & (sign | rest);
     if (std::is_same<T, __nv_bfloat16>::value) return __uint_as_float(u << 16);
     if (std::is_same<T, __half>::value) return __half2float(__ushort_as_half((unsigned short)u));
     return __uint_as_float(u);
 }
-template <typename T> __device__ __forceinline__ uint32_t key_bottom() { return key_of<T>(-INFINITY); }   // keys above it can be drawn
+template <typename T> __device__ __forceinline__ uint32_t key_bottom() { return key_of<T>((1u << (kKeyBits<T> - 1)) | kInfinite<T>); }   // of -inf: keys above it can be drawn
 
 __device__ __forceinline__ u64 warp_sum(u64 v) {
     // 27 bits at a time: 32 of them fit the 32-bit sum
@@ -62,18 +61,16 @@ template <typename T>
 struct Weigh {
     uint32_t top;
     float most, temp, inv;
-    bool plain;
-    __device__ __forceinline__ Weigh(uint32_t k, float t) : top(k), most(logit_of<T>(k)), temp(t), inv(1.0f / t), plain(!(t > 1e-30f && t < 1e30f)) {}
+    bool plain;      // an infinite logit, or a temperature whose reciprocal leaves the normal range
+    __device__ __forceinline__ Weigh(uint32_t k, float t)
+        : top(k), most(logit_of<T>(k)), temp(t), inv(1.0f / t), plain(!(t > 1e-30f && t < 1e30f) || isinf(most)) {}
     // (l - m) / T by the row's reciprocal and one correction step with the exact remainder (Markstein), which is the
-    // rounded quotient; plain division where the reciprocal leaves the normal range
+    // rounded quotient; below -200, where the weight is 0, nothing infinite or undefined goes on
     __device__ __forceinline__ float weight(uint32_t k) const {
-        if (k == top) return 1.0f;
-        if (k <= key_bottom<T>()) return 0.0f;
         const float d = logit_of<T>(k) - most;
-        float z = plain ? __fdiv_rn(d, temp) : d * inv;
-        if (z < -150.0f) return 0.0f;                     // and nothing infinite goes on
-        if (!plain) z = fmaf(fmaf(-z, temp, d), inv, z);
-        return expf(z);
+        if (plain) return k == top ? 1.0f : k <= key_bottom<T>() ? 0.0f : expf(__fdiv_rn(d, temp));
+        const float z = d * inv;
+        return expf(fmaxf(fmaf(fmaf(-z, temp, d), inv, z), -200.0f));
     }
     // w 2^44 as a whole number, without the conversion unit: 22 bits at a time in the mantissa of 2^23
     static __device__ __forceinline__ u64 quant(float w) {
@@ -83,9 +80,9 @@ struct Weigh {
         return ((u64)(__float_as_uint(a) & 0x7fffffu) << 22) + (u64)(long long)((int)(__float_as_uint(b) & 0x7fffffu) - 0x400000);
     }
     __device__ __forceinline__ u64 mass(uint32_t k) const { return quant(weight(k)); }
-    // bin of the first histogram round
+    // bin of the first histogram round: never smaller for a smaller key
     __device__ __forceinline__ int step(uint32_t k, float bins, int last) const {
-        return k == top || plain ? 0 : min((int)((most - logit_of<T>(k)) * inv * bins), last);
+        return plain ? 0 : (int)fminf((most - logit_of<T>(k)) * inv * bins, (float)last);
     }
 };
 // What top-p wants of a sum: NaN and what is not positive take the first entry alone.
@@ -120,11 +117,11 @@ __global__ void __launch_bounds__(128) sample_warp_kernel(const gala_sample_args
     pdl_launch();
     const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
     if (row >= p.rows) return;
-    const T* l = static_cast<const T*>(p.logits) + row * p.logits_ld;
+    const Bits<T>* l = static_cast<const Bits<T>*>(p.logits) + row * p.logits_ld;
     uint32_t key[E], top = 0;      // entry i of a lane is 32 i + lane
 #pragma unroll
     for (int i = 0; i < E; i++) {
-        key[i] = lane + 32 * i < p.vocab ? key_of<T>(to_f32<T>(l[lane + 32 * i])) : 0u;
+        key[i] = lane + 32 * i < p.vocab ? key_of<T>(l[lane + 32 * i]) : 0u;
         top = max(top, key[i]);
     }
     top = __reduce_max_sync(0xffffffffu, top);
@@ -219,12 +216,12 @@ constexpr float kFirstBins = 128.0f;      // bins of one unit of (m - l) / T in 
 struct Shared {
     uint32_t lo[kBins], hi[kBins];        // 64-bit sums as two words with a carry
     u64 warp_slots[2][32], rank_slots[2][8];
-    u64 sums[32];
-    u64 before;                           // answer of a round: the sum ahead of the bin
+    u64 before, amount;                   // answer of a round: the sum ahead of the bin, and the bin's own
     int bin;
+    int owner;                            // the draw: first entry of the part that holds it, or -1
+    u64 rest;
+    long long left;
 };
-
-template <typename T> using Key = typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type;
 
 // CLUSTER: several blocks a row.  Exchanges between threads use the slots of the other parity than the one before, so that
 // one barrier each does.
@@ -237,25 +234,31 @@ struct RowTeam {
         if (CLUSTER) cg::this_cluster().sync();
         else __syncthreads();
     }
-    // v: this warp's value.  Returns the team's sum; `ahead` is the sum over the warps before this one.
-    __device__ __forceinline__ u64 scan(u64 v, u64& ahead) {
+    // v: this warp's value.  Returns the block's sum; `ahead` is the sum over the warps before this one.
+    __device__ __forceinline__ u64 scan_block(u64 v, u64& ahead) {
         const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
         u64* ws = sm.warp_slots[par];
         if (lane == 0) ws[w] = v;
         __syncthreads();
         const u64 x = lane < warps ? ws[lane] : 0;
-        u64 all = warp_sum(x);
         ahead = warp_sum(lane < w ? x : 0);
+        par ^= 1;
+        return warp_sum(x);
+    }
+    // the same over the team
+    __device__ __forceinline__ u64 scan(u64 v, u64& ahead) {
+        const int at = par;
+        u64 all = scan_block(v, ahead);
         if (CLUSTER) {
+            const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
             cg::cluster_group cl = cg::this_cluster();
-            u64* rs = sm.rank_slots[par];
+            u64* rs = sm.rank_slots[at];
             if (w == 0 && lane < ranks) *cl.map_shared_rank(rs + rank, lane) = all;
             cl.sync();
             const u64 y = lane < ranks ? rs[lane] : 0;
             all = warp_sum(y);
             ahead += warp_sum(lane < rank ? y : 0);
         }
-        par ^= 1;
         return all;
     }
     __device__ __forceinline__ u64 sum(u64 v) {
@@ -287,13 +290,13 @@ struct RowTeam {
     }
     // One histogram round.  put(add) calls add(bin, amount) for this thread's entries; want(total) is asked once the bins are
     // full, with their sum.  Returns the first bin at which the running sum, starting from `ahead`, reaches it (-1: none
-    // does), and adds what lies before that bin to `ahead`.
+    // does), adds what lies before that bin to `ahead` and sets `amount` to what lies in it.
     template <typename Put, typename Want>
-    __device__ __forceinline__ int round(u64& ahead, Put put, Want want) {
+    __device__ __forceinline__ int round(u64& ahead, u64& amount, Put put, Want want) {
         const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, nt = blockDim.x;
-        barrier();             // nobody reads the last round's bins any more
+        barrier();             // nobody reads the last round's bins and answer any more
         for (int i = threadIdx.x; i < kBins; i += nt) sm.lo[i] = sm.hi[i] = 0;
-        if (threadIdx.x == 0) sm.bin = -1;
+        if (threadIdx.x == 0) sm.bin = -1;       // (the answer comes two barriers later)
         __syncthreads();
         int at = -1;           // entries of one bin after another are added up before they go to memory
         u64 run = 0;
@@ -312,37 +315,45 @@ struct RowTeam {
         });
         if (at >= 0) flush();
         barrier();
-        const int per = (kBins + nt - 1) / nt, b0 = (int)threadIdx.x * per, b1 = min(b0 + per, kBins);
+        // the bins are shared out over all threads of the team, in order; a thread adds its bins up over the blocks
+        const int per = (kBins + nt * ranks - 1) / (nt * ranks), b0 = min((rank * nt + (int)threadIdx.x) * per, kBins), b1 = min(b0 + per, kBins);
         auto value = [&](int b) -> u64 {
             if (!CLUSTER) return ((u64)sm.hi[b] << 32) | sm.lo[b];
             cg::cluster_group cl = cg::this_cluster();
             u64 v = 0;
-            for (int r = 0; r < ranks; r++) v += ((u64)*cl.map_shared_rank(&sm.hi[b], r) << 32) + *cl.map_shared_rank(&sm.lo[b], r);
+#pragma unroll
+            for (int r = 0; r < 8; r++)
+                if (r < ranks) v += ((u64)*cl.map_shared_rank(&sm.hi[b], r) << 32) + *cl.map_shared_rank(&sm.lo[b], r);
             return v;
         };
         u64 mine = 0;
         for (int b = b0; b < b1; b++) mine += value(b);
         const u64 upto = upto_lane(mine, lane);
-        if (lane == 31) sm.sums[w] = upto;
-        __syncthreads();
-        const u64 x = lane < warps ? sm.sums[lane] : 0;
-        const u64 start = warp_sum(lane < w ? x : 0) + upto - mine;
-        const u64 need = want(warp_sum(x)) - ahead;
-        if (start < need && start + mine >= need) {        // one thread at most
+        u64 ahead_warps;
+        const u64 all = scan(__shfl_sync(0xffffffffu, upto, 31), ahead_warps);
+        const u64 start = ahead_warps + upto - mine, need = want(all) - ahead;
+        if (start < need && start + mine >= need) {        // one thread of the team at most
             u64 c = start;
             for (int b = b0; b < b1; b++) {
                 const u64 v = value(b);
                 if (c + v >= need) {
-                    sm.bin = b;
-                    sm.before = c;
+                    for (int r = 0; r < ranks; r++) {
+                        Shared* to = CLUSTER ? cg::this_cluster().map_shared_rank(&sm, r) : &sm;
+                        to->bin = b;
+                        to->before = c;
+                        to->amount = v;
+                    }
                     break;
                 }
                 c += v;
             }
         }
-        __syncthreads();
+        barrier();
         const int b = sm.bin;
-        if (b >= 0) ahead += sm.before;
+        if (b >= 0) {
+            ahead += sm.before;
+            amount = sm.amount;
+        }
         return b;
     }
 };
@@ -351,7 +362,7 @@ template <typename T, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_sample_args p, const int ranks, const int each) {
     extern __shared__ __align__(16) uint8_t row_memory[];
     __shared__ Shared sm;
-    Key<T>* keys = reinterpret_cast<Key<T>*>(row_memory);      // this block's `each` entries, keys of 0 past the row's end
+    Bits<T>* keys = reinterpret_cast<Bits<T>*>(row_memory);      // this block's `each` entries, keys of 0 past the row's end
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     RowTeam<T, CLUSTER> team(sm, CLUSTER ? ranks : 1);
     const long long row = CLUSTER ? (long long)(blockIdx.x / ranks) : (long long)blockIdx.x;
@@ -359,178 +370,215 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
     pdl_launch();
     if (CLUSTER) cg::this_cluster().sync();     // every block runs before one writes to another's shared memory
     const int first = team.rank * each, mine = max(0, min(each, p.vocab - first));
-    const T* l = static_cast<const T*>(p.logits) + row * p.logits_ld + first;
+    const Bits<T>* l = static_cast<const Bits<T>*>(p.logits) + row * p.logits_ld + first;
     uint32_t top = 0, unused = 0;
-    u64 can = 0;                                // entries that can be drawn
     {
         constexpr int N = 16 / (int)sizeof(T);
-        auto one = [&](float v) -> uint32_t {
-            const uint32_t k = key_of<T>(v);
+        auto one = [&](uint32_t u) -> uint32_t {
+            const uint32_t k = key_of<T>(u);
             top = max(top, k);
-            can += k > key_bottom<T>();
             return k;
         };
+        auto word = [&](uint32_t u) -> uint32_t { return sizeof(T) == 4 ? one(u) : one(u & 0xffffu) | (one(u >> 16) << 16); };
         int done = 0;
         if ((reinterpret_cast<uintptr_t>(l) & 15) == 0) {
-            const Vec<T, N>* src = reinterpret_cast<const Vec<T, N>*>(l);
             done = mine / N * N;
-#pragma unroll 2
+#pragma unroll 4
             for (int v = threadIdx.x; v < mine / N; v += blockDim.x) {
-                const Vec<T, N> x = src[v];
-                uint32_t o[4];
-                if (sizeof(T) == 4) {
-#pragma unroll
-                    for (int j = 0; j < 4; j++) o[j] = one(x.get(j));
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        const uint32_t a = one(x.get(2 * j));
-                        o[j] = a | (one(x.get(2 * j + 1)) << 16);
-                    }
-                }
-                reinterpret_cast<uint4*>(keys)[v] = make_uint4(o[0], o[1], o[2], o[3]);
+                const uint4 x = reinterpret_cast<const uint4*>(l)[v];
+                reinterpret_cast<uint4*>(keys)[v] = make_uint4(word(x.x), word(x.y), word(x.z), word(x.w));
             }
         }
-        for (int e = done + threadIdx.x; e < each; e += blockDim.x) keys[e] = e < mine ? (Key<T>)one(to_f32<T>(l[e])) : (Key<T>)0;
+        for (int e = done + threadIdx.x; e < each; e += blockDim.x) keys[e] = e < mine ? (Bits<T>)one(l[e]) : (Bits<T>)0;
     }
+    if (threadIdx.x == 0) sm.owner = -1;
     team.extremes(unused, top);                 // its barrier is the one before the keys are read
     const float temp = p.temperature ? p.temperature[row] : 1.0f;
-    const bool greedy = !(temp > 0.0f);
-    const Weigh<T> wt(top, temp);
     // a warp's entries follow one another: 32 at a time, `groups` times
-    const int groups = (each + 32 * team.warps - 1) / (32 * team.warps), base = w * groups * 32 + lane;
-    auto key_at = [&](int i) -> uint32_t { return base + 32 * i < each ? (uint32_t)keys[base + 32 * i] : 0u; };
+    const int groups = each / (32 * team.warps), base = w * groups * 32 + lane;
+    const Bits<T>* own = keys + base;
 
-    uint32_t cut = key_bottom<T>();             // kept: key > cut, and the first `room` of those equal to it
-    long long room = 0;
-    float mp = 0.0f;
-    // The key at which the entries above `floor`, from the largest down, reach what is wanted; `ahead`: what lies above it.
-    // MASS: by mass (want: of the whole), otherwise by count.
-    auto search = [&](auto mass_, uint32_t floor, auto want, u64& ahead) -> uint32_t {
-        constexpr bool MASS = decltype(mass_)::value;
-        ahead = 0;
-        u64 tail = 0, need = 0;
-        const int last = kBins - 1;
-        const int b1 = team.round(
-            ahead,
-            [&](auto add) {
+    if (top <= key_bottom<T>()) {
+        if (team.rank == 0 && threadIdx.x == 0) answer(p, row, -1, 0.0f, 1);
+    } else if (!(temp > 0.0f)) {
+        // greedy: the first of the largest entries
+        uint32_t at = 0xffffffffu, unused2 = 0;
 #pragma unroll 4
-                for (int i = 0; i < groups; i++) {
-                    const uint32_t k = key_at(i);
-                    if (k > floor) {
-                        const int b = wt.step(k, kFirstBins, last);
-                        const u64 q = MASS ? wt.mass(k) : 1ull;
-                        if (b < last) add(b, q);
-                        else tail += q;
-                    }
-                }
-                if (MASS) tail = team.sum(tail);
-            },
-            [&](u64 total) { return need = want(total + tail); });
-        uint32_t lo = floor + 1, hi = top;
-        if (b1 >= 0) {
-            lo = 0xffffffffu;
-            hi = 0;
-#pragma unroll 4
-            for (int i = 0; i < groups; i++) {
-                const uint32_t k = key_at(i);
-                if (k > floor && wt.step(k, kFirstBins, last) == b1) lo = min(lo, k), hi = max(hi, k);
-            }
-            team.extremes(lo, hi);
-        }
-        while (lo < hi) {
-            const int shift = max(0, 21 - __clz(hi - lo));
-            const int b = team.round(
-                ahead,
+        for (int i = 0; i < groups; i++)
+            if (own[32 * i] == top) at = min(at, (uint32_t)(first + base + 32 * i));
+        team.extremes(at, unused2);
+        if (team.rank == 0 && threadIdx.x == 0) answer(p, row, (int)at, 1.0f, (u64)kOne);
+    } else {
+        const Weigh<T> wt(top, temp);
+        uint32_t cut = key_bottom<T>();         // kept: key > cut, and the first `room` of those equal to it ...
+        long long room = 0;
+        bool part = false;                      // ... of which there are more
+        // The key at which the entries above `floor`, from the largest down, reach what is wanted; `ahead`: what lies above
+        // it, `amount`: what lies on it.  MASS: by mass (want: of the whole), otherwise by count.  False if nothing reaches it.
+        auto search = [&](auto mass_, uint32_t floor, auto want, uint32_t& key, u64& ahead, u64& amount) -> bool {
+            constexpr bool MASS = decltype(mass_)::value;
+            ahead = 0;
+            u64 tail = 0, need = 0, whole = 0;
+            const int last = kBins - 1;
+            const int b1 = team.round(
+                ahead, amount,
                 [&](auto add) {
 #pragma unroll 4
                     for (int i = 0; i < groups; i++) {
-                        const uint32_t k = key_at(i);
-                        if (k >= lo && k <= hi) add((int)((hi - k) >> shift), MASS ? wt.mass(k) : 1ull);
+                        const uint32_t k = own[32 * i];
+                        if (k > floor) {
+                            const int b = wt.step(k, kFirstBins, last);
+                            const u64 q = MASS ? wt.mass(k) : 1ull;
+                            if (b < last) add(b, q);
+                            else tail += q;
+                        }
                     }
+                    tail = team.sum(tail);
                 },
-                [&](u64) { return need; });
-            if (b < 0) break;      // does not happen: the range reaches what is wanted
-            hi -= (uint32_t)b << shift;
-            const uint32_t span = (1u << shift) - 1u;
-            if (hi - lo > span) lo = hi - span;
-        }
-        return hi;
-    };
-    if (top <= key_bottom<T>()) {
-        if (team.rank == 0 && threadIdx.x == 0) answer(p, row, -1, 0.0f, 1);
-    } else {
-        if (greedy) {
-            cut = top;
-            room = 1;
-        } else {
-            const int k = p.top_k ? p.top_k[row] : 0;
-            bool some = false;      // top-k has cut
-            if (k > 0 && k < p.vocab && team.sum(can) > (u64)k) {     // otherwise fewer than k can be drawn at all
-                u64 ahead;
-                cut = search(std::false_type{}, cut, [&](u64) { return (u64)k; }, ahead);
-                room = k - (long long)ahead;
-                some = true;
-            }
-            const float tp = p.top_p ? p.top_p[row] : 1.0f;
-            if (!(tp >= 1.0f)) {
-                u64 ahead = 0, want = 0, at_cut = some ? (u64)room * wt.mass(cut) : 0ull, above = 0;
-                const uint32_t at = search(std::true_type{}, cut, [&](u64 total) { above = total; return want = share(tp, total + at_cut); }, ahead);
-                if (above >= want) {
-                    cut = at;
-                    room = p.vocab;
-                } else {
-                    ahead = above;
+                [&](u64 total) {
+                    whole = total + tail;
+                    return need = want(whole);
+                });
+            if (whole < need) return false;
+            uint32_t lo = floor + 1, hi = top;
+            if (b1 >= 0) {
+                // the keys of that bin, by bisection: a smaller key never has a smaller bin
+                uint32_t a = floor + 1, b = top;
+                while (a < b) {                   // the smallest key of the bin or an earlier one
+                    const uint32_t m = a + (b - a) / 2;
+                    if (wt.step(m, kFirstBins, last) <= b1) b = m;
+                    else a = m + 1;
                 }
-                // ties stay while what is ranked before them is less than wanted
-                const u64 one = wt.mass(cut);
-                const u64 fit = one ? (want - ahead + one - 1) / one : 0ull;
-                if ((long long)fit < room) room = (long long)fit;
+                lo = a;
+                b = top;
+                while (a < b) {                   // the largest key of the bin
+                    const uint32_t m = a + (b - a + 1) / 2;
+                    if (wt.step(m, kFirstBins, last) >= b1) a = m;
+                    else b = m - 1;
+                }
+                hi = a;
             }
-            mp = p.min_p ? fminf(p.min_p[row], 1.0f) : 0.0f;
+            while (lo < hi) {
+                const int shift = max(0, 21 - __clz(hi - lo));
+                const int b = team.round(
+                    ahead, amount,
+                    [&](auto add) {
+#pragma unroll 4
+                        for (int i = 0; i < groups; i++) {
+                            const uint32_t k = own[32 * i];
+                            if (k >= lo && k <= hi) add((int)((hi - k) >> shift), MASS ? wt.mass(k) : 1ull);
+                        }
+                    },
+                    [&](u64) { return need; });
+                if (b < 0) break;      // does not happen: the range reaches what is wanted
+                hi -= (uint32_t)b << shift;
+                const uint32_t span = (1u << shift) - 1u;
+                if (hi - lo > span) lo = hi - span;
+            }
+            key = hi;
+            return true;
+        };
+        u64 ahead, amount;
+        const int k = p.top_k ? p.top_k[row] : 0;
+        // with fewer than k entries that can be drawn at all, nothing is cut
+        if (k > 0 && k < p.vocab && search(std::false_type{}, cut, [&](u64) { return (u64)k; }, cut, ahead, amount)) {
+            room = k - (long long)ahead;
+            part = amount > (u64)room;
         }
-        // where this warp's ties stand among all, if not all of them stay
-        uint32_t ties = 0;
-        u64 ahead;
-        if (room > 0) {
-            for (int i = 0; i < groups; i++) ties += key_at(i) == cut;
-            ties = __reduce_add_sync(0xffffffffu, ties);
+        const float tp = p.top_p ? p.top_p[row] : 1.0f;
+        if (!(tp >= 1.0f)) {
+            const u64 one_at_cut = room ? wt.mass(cut) : 0ull, at_cut = (u64)room * one_at_cut;
+            u64 want = 0, above = 0;
+            uint32_t at = cut;
+            if (search(std::true_type{}, cut, [&](u64 total) { above = total; return want = share(tp, total + at_cut); }, at, ahead, amount)) {
+                cut = at;
+                const u64 one = wt.mass(cut);
+                room = p.vocab;
+                part = false;
+                if (one) {      // ties stay while what is ranked before them is less than wanted
+                    const u64 fit = (want - ahead + one - 1) / one;
+                    room = (long long)fit;
+                    part = fit * one < amount;
+                }
+            } else if (one_at_cut) {
+                const u64 fit = (want - above + one_at_cut - 1) / one_at_cut;
+                if ((long long)fit < room) {
+                    room = (long long)fit;
+                    part = true;
+                }
+            }
         }
-        team.scan((u64)ties, ahead);
-        long long left_room = room - (long long)ahead;
-        auto kept = [&](int i, long long& left, float& weight) -> u64 {     // for the whole warp, group after group
-            const uint32_t k = key_at(i);
-            bool keep = k > cut;
-            if (ties) {
-                const bool tie = k == cut;
-                const uint32_t g = __ballot_sync(0xffffffffu, tie);
-                keep = keep || (tie && (long long)__popc(g & ((1u << lane) - 1u)) < left);
+        const float mp = p.min_p ? fminf(p.min_p[row], 1.0f) : 0.0f;
+        if (room && !part) cut--;               // every entry equal to it stays (cut is above the bottom key here)
+        long long left = 0;                     // of the ties that stay, those from this warp on
+        if (part) {
+            uint32_t ties = 0;
+            for (int i = 0; i < groups; i++) ties += own[32 * i] == cut;
+            u64 before;
+            team.scan((u64)__reduce_add_sync(0xffffffffu, ties), before);
+            left = room - (long long)before;
+        }
+        const long long left_here = left;
+        u64 mass = 0;
+#pragma unroll 2
+        for (int i = 0; i < groups; i++) {
+            const uint32_t key = own[32 * i];
+            bool keep = key > cut;
+            if (part) {
+                const uint32_t g = __ballot_sync(0xffffffffu, key == cut);
+                keep = keep || (key == cut && (long long)__popc(g & ((1u << lane) - 1u)) < left);
                 left -= __popc(g);
             }
-            weight = keep ? wt.weight(k) : 0.0f;
-            if (weight < mp) weight = 0.0f;
-            return Weigh<T>::quant(weight);
-        };
-        u64 mass = 0;
-        float weight;
-        long long left = left_room;
-#pragma unroll 2
-        for (int i = 0; i < groups; i++) mass += kept(i, left, weight);
+            if (keep) {
+                const float x = wt.weight(key);
+                if (x >= mp) mass += Weigh<T>::quant(x);
+            }
+        }
         const u64 here = warp_sum(mass);
         u64 before;
         const u64 total = team.scan(here, before), target = target_of(p.uniforms[row], total);
-        if (target >= before && target - before < here) {      // one warp of the team
-            u64 rest = target - before;
-            left = left_room;
-            for (int i = 0; i < groups; i++) {
-                const u64 q = kept(i, left, weight), group = warp_sum(q);
-                if (rest < group) {
-                    const int at = __ffs(__ballot_sync(0xffffffffu, upto_lane(q, lane) > rest)) - 1;
-                    const float wtok = __shfl_sync(0xffffffffu, weight, at);
-                    if (lane == 0) answer(p, row, first + base + 32 * i + at, wtok, total);
-                    break;
+        if (lane == 0 && target >= before && target - before < here) {      // one warp of the team
+            sm.owner = base;
+            sm.rest = target - before;
+            sm.left = left_here;
+        }
+        __syncthreads();
+        if (sm.owner >= 0) {
+            // that warp's entries once more, now shared out over the block's threads in order
+            const int e0 = sm.owner + (int)threadIdx.x * ((groups * 32 + (int)blockDim.x - 1) / (int)blockDim.x);
+            const int e1 = min(e0 + (groups * 32 + (int)blockDim.x - 1) / (int)blockDim.x, sm.owner + groups * 32);
+            long long room_here = 0;
+            if (part) {
+                uint32_t ties = 0;
+                for (int e = e0; e < e1; e++) ties += keys[e] == cut;
+                const u64 upto = upto_lane((u64)ties, lane);
+                u64 ahead_warps;
+                team.scan_block(__shfl_sync(0xffffffffu, upto, 31), ahead_warps);
+                room_here = sm.left - (long long)(ahead_warps + upto - ties);
+            }
+            auto each_kept = [&](auto use) {
+                long long r = room_here;
+                for (int e = e0; e < e1; e++) {
+                    const uint32_t key = keys[e];
+                    const bool keep = key > cut || (part && key == cut && r-- > 0);
+                    const float x = keep ? wt.weight(key) : 0.0f;
+                    if (keep && x >= mp && use(e, x, Weigh<T>::quant(x))) return;
                 }
-                rest -= group;
+            };
+            u64 sum = 0;
+            each_kept([&](int, float, u64 q) { sum += q; return false; });
+            const u64 upto = upto_lane(sum, lane);
+            u64 ahead_warps;
+            team.scan_block(__shfl_sync(0xffffffffu, upto, 31), ahead_warps);
+            const u64 start = ahead_warps + upto - sum, rest = sm.rest;
+            if (start <= rest && rest < start + sum) {      // one thread
+                u64 c = start;
+                each_kept([&](int e, float x, u64 q) {
+                    c += q;
+                    if (c <= rest) return false;
+                    answer(p, row, first + e, x, total);
+                    return true;
+                });
             }
         }
     }
@@ -575,8 +623,9 @@ cudaError_t pick(const gala_sample_args& a, cudaStream_t st) {
     // blocks of a row: as many as keep a block's part within 64 KB (three blocks an SM), and more where rows are few
     int ranks = 1;
     while (ranks < 8 && ((long long)v * (int)sizeof(T) > 65536ll * ranks || (a.rows * ranks * 2 <= sm_count() && v > 8192 * ranks))) ranks *= 2;
-    const int each = ((v + ranks - 1) / ranks + 63) / 64 * 64;
-    const unsigned block = each >= 64 * kThreads / 4 ? kThreads : (unsigned)((each + 1023) / 1024 * 64);
+    const int part = (v + ranks - 1) / ranks;
+    const int block = part >= 16 * kThreads ? kThreads : (part + 1023) / 1024 * 64;      // 16 entries a thread and more
+    const int each = (part + block - 1) / block * block;
     return ranks > 1 ? rows<T, true>(a, ranks, each, block, st) : rows<T, false>(a, 1, each, block, st);
 }
 

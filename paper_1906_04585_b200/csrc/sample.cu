@@ -214,7 +214,7 @@ constexpr int kBins = 2048;
 constexpr float kFirstBins = 128.0f;      // bins of one unit of (m - l) / T in the first round
 
 struct Shared {
-    uint32_t lo[kBins], hi[kBins];        // 64-bit sums as two words with a carry
+    uint32_t part[3][kBins];              // sums by 15 bits at a time: 2^15 entries of a block fit, and nothing comes back
     u64 warp_slots[2][32], rank_slots[2][8];
     u64 before, amount;                   // answer of a round: the sum ahead of the bin, and the bin's own
     int bin;
@@ -288,42 +288,41 @@ struct RowTeam {
         }
         par ^= 1;
     }
-    // One histogram round.  put(add) calls add(bin, amount) for this thread's entries; want(total) is asked once the bins are
+    __device__ __forceinline__ void count(int bin) { atomicAdd(&sm.part[0][bin], 1u); }
+    __device__ __forceinline__ void weigh(int bin, u64 q) {
+        atomicAdd(&sm.part[0][bin], (uint32_t)q & 0x7fffu);
+        atomicAdd(&sm.part[1][bin], (uint32_t)(q >> 15) & 0x7fffu);
+        const uint32_t high = (uint32_t)(q >> 30);
+        if (high) atomicAdd(&sm.part[2][bin], high);
+    }
+    // One histogram round.  put() calls count(bin) or weigh(bin, mass) for this thread's entries; want(total) is asked once the bins are
     // full, with their sum.  Returns the first bin at which the running sum, starting from `ahead`, reaches it (-1: none
     // does), adds what lies before that bin to `ahead` and sets `amount` to what lies in it.
     template <typename Put, typename Want>
     __device__ __forceinline__ int round(u64& ahead, u64& amount, Put put, Want want) {
-        const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, nt = blockDim.x;
+        const int lane = threadIdx.x & 31, nt = blockDim.x;
         barrier();             // nobody reads the last round's bins and answer any more
-        for (int i = threadIdx.x; i < kBins; i += nt) sm.lo[i] = sm.hi[i] = 0;
+        for (int i = threadIdx.x; i < kBins; i += nt) sm.part[0][i] = sm.part[1][i] = sm.part[2][i] = 0;
         if (threadIdx.x == 0) sm.bin = -1;       // (the answer comes two barriers later)
         __syncthreads();
-        int at = -1;           // entries of one bin after another are added up before they go to memory
-        u64 run = 0;
-        auto flush = [&] {
-            const uint32_t low = (uint32_t)run, old = atomicAdd(&sm.lo[at], low);
-            const uint32_t high = (uint32_t)(run >> 32) + (old + low < old ? 1u : 0u);
-            if (high) atomicAdd(&sm.hi[at], high);
-        };
-        put([&](int b, u64 q) {
-            if (b != at) {
-                if (at >= 0) flush();
-                at = b;
-                run = 0;
-            }
-            run += q;
-        });
-        if (at >= 0) flush();
+        put();
         barrier();
         // the bins are shared out over all threads of the team, in order; a thread adds its bins up over the blocks
         const int per = (kBins + nt * ranks - 1) / (nt * ranks), b0 = min((rank * nt + (int)threadIdx.x) * per, kBins), b1 = min(b0 + per, kBins);
         auto value = [&](int b) -> u64 {
-            if (!CLUSTER) return ((u64)sm.hi[b] << 32) | sm.lo[b];
-            cg::cluster_group cl = cg::this_cluster();
             u64 v = 0;
 #pragma unroll
-            for (int r = 0; r < 8; r++)
-                if (r < ranks) v += ((u64)*cl.map_shared_rank(&sm.hi[b], r) << 32) + *cl.map_shared_rank(&sm.lo[b], r);
+            for (int k = 0; k < 3; k++) {
+                u64 x = 0;
+                if (CLUSTER) {
+#pragma unroll
+                    for (int r = 0; r < 8; r++)
+                        if (r < ranks) x += *cg::this_cluster().map_shared_rank(&sm.part[k][b], r);
+                } else {
+                    x = sm.part[k][b];
+                }
+                v += x << (15 * k);
+            }
             return v;
         };
         u64 mine = 0;
@@ -422,15 +421,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
             const int last = kBins - 1;
             const int b1 = team.round(
                 ahead, amount,
-                [&](auto add) {
+                [&] {
 #pragma unroll 4
                     for (int i = 0; i < groups; i++) {
                         const uint32_t k = own[32 * i];
                         if (k > floor) {
                             const int b = wt.step(k, kFirstBins, last);
-                            const u64 q = MASS ? wt.mass(k) : 1ull;
-                            if (b < last) add(b, q);
-                            else tail += q;
+                            if (MASS) {
+                                const u64 q = wt.mass(k);
+                                if (b < last) team.weigh(b, q);
+                                else tail += q;
+                            } else {
+                                if (b < last) team.count(b);
+                                else tail++;
+                            }
                         }
                     }
                     tail = team.sum(tail);
@@ -462,11 +466,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
                 const int shift = max(0, 21 - __clz(hi - lo));
                 const int b = team.round(
                     ahead, amount,
-                    [&](auto add) {
+                    [&] {
 #pragma unroll 4
                         for (int i = 0; i < groups; i++) {
                             const uint32_t k = own[32 * i];
-                            if (k >= lo && k <= hi) add((int)((hi - k) >> shift), MASS ? wt.mass(k) : 1ull);
+                            if (k >= lo && k <= hi) {
+                                const int b = (int)((hi - k) >> shift);
+                                if (MASS) team.weigh(b, wt.mass(k));
+                                else team.count(b);
+                            }
                         }
                     },
                     [&](u64) { return need; });

@@ -10,7 +10,8 @@
 // memory, so an operand byte is fetched into one SM and used by both.  Persistent; per CTA
 //   warp 0    TMA producer into a ring of 128-byte-swizzled stages; both CTAs' copies report to the leader's barrier
 //   warp 1    (leader) issues the MMAs; commits release the stage in both CTAs
-//   warps 2-5 epilogue from tensor memory while the next tile is multiplied (two accumulators)
+//   warps 2-9 epilogue from tensor memory while the next tile is multiplied (two accumulators): two warps for each 32
+//             rows, each half of the columns (four warps were the bound where three outputs are written or g and u read)
 // Its uses: both projections at once (the B tile is 128 rows of Wg in one CTA and 128 of Wu in the other, so g and u of
 // an element lie in one thread's registers and the activation and the product cost no trip through memory); y; dp, whose
 // epilogue turns it into dg and du; dx (two products added by running the reduction over both); the weight gradients.
@@ -71,18 +72,20 @@ __device__ __forceinline__ void mbar_arrive_at(uint32_t bar) {
 }
 
 // ---------------------------------------------------------------------------------- activation
-__device__ __forceinline__ float act_value(float g, int act) {
-    if (act == GALA_ACT_SILU) return __fdividef(g, 1.0f + __expf(-g));
-    if (act == GALA_ACT_GELU) return 0.5f * g * (1.0f + erff(g * 0.70710678f));
+// (the kind is a template argument here and below: with all three in one kernel, and both element types, instruction
+// fetch was 60 % of the epilogue's stalls)
+template <int ACT> __device__ __forceinline__ float act_value(float g) {
+    if (ACT == GALA_ACT_SILU) return __fdividef(g, 1.0f + __expf(-g));
+    if (ACT == GALA_ACT_GELU) return 0.5f * g * (1.0f + erff(g * 0.70710678f));
     return fmaxf(g, 0.0f);
 }
 // value and slope
-__device__ __forceinline__ void act_both(float g, int act, float& v, float& s) {
-    if (act == GALA_ACT_SILU) {
+template <int ACT> __device__ __forceinline__ void act_both(float g, float& v, float& s) {
+    if (ACT == GALA_ACT_SILU) {
         const float p = __fdividef(1.0f, 1.0f + __expf(-g));
         v = g * p;
         s = fmaf(v, 1.0f - p, p);
-    } else if (act == GALA_ACT_GELU) {
+    } else if (ACT == GALA_ACT_GELU) {
         const float phi = 0.5f * (1.0f + erff(g * 0.70710678f));
         v = g * phi;
         s = fmaf(g * 0.39894228f, __expf(-0.5f * g * g), phi);
@@ -93,22 +96,22 @@ __device__ __forceinline__ void act_both(float g, int act, float& v, float& s) {
 }
 
 // ---------------------------------------------------------------------------------- rows of 16-bit elements
-__device__ __forceinline__ uint32_t pack16(float a, float b, bool fp16) {
-    if (!fp16) return pack2(a, b);
+template <bool FP16> __device__ __forceinline__ uint32_t pack16(float a, float b) {
+    if (!FP16) return pack2(a, b);
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ float2 unpack16(uint32_t w, bool fp16) {
-    if (!fp16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+template <bool FP16> __device__ __forceinline__ float2 unpack16(uint32_t w) {
+    if (!FP16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
     return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
-__device__ __forceinline__ uint16_t one16(float a, bool fp16) { return (uint16_t)(pack16(a, 0.0f, fp16) & 0xffffu); }
+template <bool FP16> __device__ __forceinline__ uint16_t one16(float a) { return (uint16_t)(pack16<FP16>(a, 0.0f) & 0xffffu); }
 
 // 32 columns of a row of which `valid` exist; p is 16-byte aligned, and 32-byte aligned where `wide`
-__device__ __forceinline__ void store32(uint16_t* p, const float (&v)[32], int valid, bool wide, bool fp16) {
+template <bool FP16> __device__ __forceinline__ void store32(uint16_t* p, const float (&v)[32], int valid, bool wide) {
     uint32_t o[16];
 #pragma unroll
-    for (int j = 0; j < 16; j++) o[j] = pack16(v[2 * j], v[2 * j + 1], fp16);
+    for (int j = 0; j < 16; j++) o[j] = pack16<FP16>(v[2 * j], v[2 * j + 1]);
     if (valid >= 32) {
         if (wide) {
             st_global_v8(p, &o[0]);
@@ -123,12 +126,26 @@ __device__ __forceinline__ void store32(uint16_t* p, const float (&v)[32], int v
             if (j < valid) p[j] = (uint16_t)(j & 1 ? o[j / 2] >> 16 : o[j / 2] & 0xffffu);
     }
 }
-__device__ __forceinline__ void load32(const uint16_t* p, uint32_t (&o)[16], int valid) {
+// (a plain load, not the read-only path: dg may replace g in place)
+__device__ __forceinline__ void ld_global_v8(const void* p, uint32_t* r) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "l"(p)
+                 : "memory");
+}
+// The same columns of a row.  Where rows allow it, whole 32-byte sectors: half a sector a load relies on the first-level
+// cache keeping the other half, which 32 rows a warp do not let it.
+__device__ __forceinline__ void load32(const uint16_t* p, uint32_t (&o)[16], int valid, bool wide) {
     if (valid >= 32) {
+        if (wide) {
+            ld_global_v8(p, &o[0]);
+            ld_global_v8(p + 16, &o[8]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const uint4 q = reinterpret_cast<const uint4*>(p)[j];      // not the read-only path: dg may replace g in place
-            o[4 * j] = q.x; o[4 * j + 1] = q.y; o[4 * j + 2] = q.z; o[4 * j + 3] = q.w;
+            for (int j = 0; j < 4; j++) {
+                const uint4 q = reinterpret_cast<const uint4*>(p)[j];
+                o[4 * j] = q.x; o[4 * j + 1] = q.y; o[4 * j + 2] = q.z; o[4 * j + 3] = q.w;
+            }
         }
     } else {
 #pragma unroll
@@ -143,6 +160,7 @@ __device__ __forceinline__ void load32(const uint16_t* p, uint32_t (&o)[16], int
 enum { EPI_STORE, EPI_PROJECT, EPI_SLOPE };
 
 constexpr int kPairStages = 6;
+constexpr int kPairThreads = 320;
 constexpr int kHalfTile = 128 * 128;        // bytes of 128 rows (or MN elements) x 64 K of a 16-bit type
 constexpr int kBand = 8;                    // row tiles that are walked together, for L2
 
@@ -159,12 +177,11 @@ struct PairArgs {
     const uint16_t *in0, *in1;         // SLOPE: g, u
     long long ld;                      // row stride of out0..2 and in0..1
     long long ld1;                     // STORE, separate: row stride of out1
-    int act, fp16, wide;
+    int wide;
     int* status;
 };
 
 struct PairTile { int group; long long m0; int n0; };
-template <int TN>
 __device__ __forceinline__ PairTile pair_tile(const PairArgs& p, long long t, int width) {
     PairTile r;
     const long long per = (long long)p.mt * p.nt;
@@ -177,13 +194,14 @@ __device__ __forceinline__ PairTile pair_tile(const PairArgs& p, long long t, in
     return r;
 }
 
-// A_MN / B_MN: the operand is stored [K][rows] instead of [rows][K].  TN: columns of the accumulator.
-template <bool A_MN, bool B_MN, int TN, int EPI>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(192, 1) ffn_pair_kernel(const __grid_constant__ PairMaps maps, const PairArgs p) {
+// A_MN / B_MN: the operand is stored [K][rows] instead of [rows][K].
+template <bool A_MN, bool B_MN, int EPI, int ACT, bool FP16>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) ffn_pair_kernel(const __grid_constant__ PairMaps maps, const PairArgs p) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t full_bar[kPairStages], empty_bar[kPairStages], acc_full[2], acc_empty[2];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag, issued;
+    constexpr int TN = 256;                                // columns of the accumulator
     constexpr int kB = TN / 2 * 128;                       // bytes of this CTA's half of the B tile
     constexpr int kStage = kHalfTile + kB;
     constexpr int kWidth = EPI == EPI_PROJECT ? TN / 2 : TN;    // output columns of a tile
@@ -194,7 +212,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(192, 1) ffn_pair_ker
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kPairStages; s++) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
-        for (int b = 0; b < 2; b++) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 8); }
+        for (int b = 0; b < 2; b++) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 16); }
         abort_flag = 0;
         issued = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -215,7 +233,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(192, 1) ffn_pair_ker
         int it = 0;
         bool ok = true;
         for (long long t = first; ok && t < p.tiles; t += step) {
-            const PairTile tile = pair_tile<TN>(p, t, kWidth);
+            const PairTile tile = pair_tile(p, t, kWidth);
             const int am = (int)tile.m0 + (int)rank * 128;
             for (int k = 0; k < p.k; k++, it++) {
                 const int s = it % kPairStages;
@@ -250,7 +268,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(192, 1) ffn_pair_ker
         }
     } else if (warp == 1) {
         if (rank == 0 && lane == 0) {
-            const uint32_t fmt = p.fp16 ? 0u : ((1u << 7) | (1u << 10));
+            const uint32_t fmt = FP16 ? 0u : ((1u << 7) | (1u << 10));
             const uint32_t idesc = (1u << 4) | fmt | ((uint32_t)A_MN << 15) | ((uint32_t)B_MN << 16) | ((uint32_t)(TN >> 3) << 17) |
                                    ((uint32_t)(256 >> 4) << 24);
             int it = 0, local = 0;
@@ -278,69 +296,94 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(192, 1) ffn_pair_ker
             }
         }
     } else {
-        const int q = warp & 3;
-        const bool fp16 = p.fp16 != 0, wide = p.wide != 0;
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        constexpr int kPart = kWidth / 2;          // columns of a warp
+        const bool wide = p.wide != 0;
         int local = 0;
         for (long long t = first; t < p.tiles; t += step, local++) {
-            const PairTile tile = pair_tile<TN>(p, t, kWidth);
+            const PairTile tile = pair_tile(p, t, kWidth);
             const int ab = local & 1;
             const long long row = tile.m0 + rank * 128 + q * 32 + lane;
+            const int n0 = tile.n0 + half * kPart;
             const bool live = row < p.M;
-            if (!mbar_wait(&acc_full[ab], ((uint32_t)local >> 1) & 1u, &abort_flag)) break;
-            tcgen05_fence_after();
-            const uint32_t acc = tmem + (uint32_t)(ab * TN) + ((uint32_t)(q * 32) << 16);
-            uint16_t* o0 = p.separate && tile.group ? p.out1 : p.out0;
-            const long long ld = p.separate && tile.group ? p.ld1 : p.ld;
-            for (int c = 0; c < kWidth; c += 32) {
-                const int n = tile.n0 + c, valid = p.N - n;
-                uint32_t r[32];
-                tmem_ld32(acc + c, r);
-                const bool put = live && valid > 0;
-                if (EPI == EPI_PROJECT) {
-                    uint32_t r2[32];
-                    tmem_ld32(acc + TN / 2 + c, r2);
-                    if (put) {
-                        float v[32];
-                        if (p.out1) {
-#pragma unroll
-                            for (int j = 0; j < 32; j++) v[j] = __uint_as_float(r[j]);
-                            store32(p.out1 + row * p.ld + n, v, valid, wide, fp16);
-#pragma unroll
-                            for (int j = 0; j < 32; j++) v[j] = __uint_as_float(r2[j]);
-                            store32(p.out2 + row * p.ld + n, v, valid, wide, fp16);
-                        }
-#pragma unroll
-                        for (int j = 0; j < 32; j++) v[j] = act_value(__uint_as_float(r[j]), p.act) * __uint_as_float(r2[j]);
-                        store32(p.out0 + row * p.ld + n, v, valid, wide, fp16);
+            const uint32_t acc = tmem + (uint32_t)(ab * TN + half * kPart) + ((uint32_t)(q * 32) << 16);
+            if (EPI == EPI_SLOPE) {
+                // g and u of the next 32 columns are fetched while these are worked on, the first before the MMAs are done
+                uint32_t g[16], u[16];
+                const uint16_t* pg = p.in0 + row * p.ld + n0;
+                const uint16_t* pu = p.in1 + row * p.ld + n0;
+                if (live && p.N > n0) {
+                    load32(pg, g, p.N - n0, wide);
+                    load32(pu, u, p.N - n0, wide);
+                }
+                if (!mbar_wait(&acc_full[ab], ((uint32_t)local >> 1) & 1u, &abort_flag)) break;
+                tcgen05_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < kPart; c += 32) {
+                    const int valid = p.N - n0 - c;
+                    uint32_t r[32], gn[16], un[16];
+                    tmem_ld32(acc + c, r);
+                    if (c + 32 < kPart && live && valid > 32) {
+                        load32(pg + c + 32, gn, valid - 32, wide);
+                        load32(pu + c + 32, un, valid - 32, wide);
                     }
-                } else if (EPI == EPI_SLOPE) {
-                    if (put) {
-                        uint32_t g[16], u[16];
-                        load32(p.in0 + row * p.ld + n, g, valid);
-                        load32(p.in1 + row * p.ld + n, u, valid);
+                    if (live && valid > 0) {
                         float dg[32], du[32];
 #pragma unroll
                         for (int j = 0; j < 16; j++) {
-                            const float2 gv = unpack16(g[j], fp16), uv = unpack16(u[j], fp16);
+                            const float2 gv = unpack16<FP16>(g[j]), uv = unpack16<FP16>(u[j]);
                             float v, s;
-                            act_both(gv.x, p.act, v, s);
+                            act_both<ACT>(gv.x, v, s);
                             const float d0 = __uint_as_float(r[2 * j]), d1 = __uint_as_float(r[2 * j + 1]);
                             du[2 * j] = d0 * v;
                             dg[2 * j] = d0 * uv.x * s;
-                            act_both(gv.y, p.act, v, s);
+                            act_both<ACT>(gv.y, v, s);
                             du[2 * j + 1] = d1 * v;
                             dg[2 * j + 1] = d1 * uv.y * s;
                         }
-                        store32(p.out0 + row * p.ld + n, dg, valid, wide, fp16);
-                        store32(p.out1 + row * p.ld + n, du, valid, wide, fp16);
+                        store32<FP16>(p.out0 + row * p.ld + n0 + c, dg, valid, wide);
+                        store32<FP16>(p.out1 + row * p.ld + n0 + c, du, valid, wide);
                     }
-                } else if (put) {
-                    float v[32];
 #pragma unroll
-                    for (int j = 0; j < 32; j++) v[j] = __uint_as_float(r[j]);
-                    store32(o0 + row * ld + n, v, valid, wide, fp16);
+                    for (int j = 0; j < 16; j++) g[j] = gn[j], u[j] = un[j];
+                    __syncwarp();      // the next load from tensor memory is the whole warp's
                 }
-                __syncwarp();      // the next load from tensor memory is the whole warp's
+            } else {
+                if (!mbar_wait(&acc_full[ab], ((uint32_t)local >> 1) & 1u, &abort_flag)) break;
+                tcgen05_fence_after();
+                uint16_t* o0 = p.separate && tile.group ? p.out1 : p.out0;
+                const long long ld = p.separate && tile.group ? p.ld1 : p.ld;
+#pragma unroll 1
+                for (int c = 0; c < kPart; c += 32) {
+                    const int n = n0 + c, valid = p.N - n;
+                    const bool put = live && valid > 0;
+                    uint32_t r[32];
+                    tmem_ld32(acc + c, r);
+                    if (EPI == EPI_PROJECT) {
+                        uint32_t r2[32];
+                        tmem_ld32(acc + TN / 2 + c, r2);
+                        if (put) {
+                            float v[32];
+                            if (p.out1) {
+#pragma unroll
+                                for (int j = 0; j < 32; j++) v[j] = __uint_as_float(r[j]);
+                                store32<FP16>(p.out1 + row * p.ld + n, v, valid, wide);
+#pragma unroll
+                                for (int j = 0; j < 32; j++) v[j] = __uint_as_float(r2[j]);
+                                store32<FP16>(p.out2 + row * p.ld + n, v, valid, wide);
+                            }
+#pragma unroll
+                            for (int j = 0; j < 32; j++) v[j] = act_value<ACT>(__uint_as_float(r[j])) * __uint_as_float(r2[j]);
+                            store32<FP16>(p.out0 + row * p.ld + n, v, valid, wide);
+                        }
+                    } else if (put) {
+                        float v[32];
+#pragma unroll
+                        for (int j = 0; j < 32; j++) v[j] = __uint_as_float(r[j]);
+                        store32<FP16>(o0 + row * ld + n, v, valid, wide);
+                    }
+                    __syncwarp();      // the next load from tensor memory is the whole warp's
+                }
             }
             tcgen05_fence_before();
             __syncwarp();
@@ -378,11 +421,11 @@ struct FewArgs {
     int k, per;           // K steps of 64, and those of one block of the cluster
     uint16_t *out0, *out1, *out2;   // p, g, u; DOWN: y
     long long ld;
-    int act, fp16;
+    int act;
     int* status;
 };
 
-template <int NT, bool DOWN>
+template <int NT, bool DOWN, bool FP16>
 __global__ void __launch_bounds__(192, 1) ffn_few_kernel(const __grid_constant__ CUtensorMap w0, const __grid_constant__ CUtensorMap w1,
                                                          const __grid_constant__ CUtensorMap xm, const FewArgs p) {
     extern __shared__ uint8_t smem_raw[];
@@ -459,7 +502,7 @@ __global__ void __launch_bounds__(192, 1) ffn_few_kernel(const __grid_constant__
     }
     if (warp == 1) {
         if (lane == 0) {
-            const uint32_t idesc = make_instr_desc(NT, 0, 0, p.fp16 != 0);
+            const uint32_t idesc = make_instr_desc(NT, 0, 0, FP16);
             bool ok = true;
             for (int k = 0; k < nk; k++) {
                 const int s = k % kFewStages;
@@ -481,7 +524,6 @@ __global__ void __launch_bounds__(192, 1) ffn_few_kernel(const __grid_constant__
         const bool ok = mbar_wait(&acc_full, 0, &abort_flag);
         tcgen05_fence_after();
         const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16);
-        const bool fp16 = p.fp16 != 0;
         if (DOWN) {
             if (ok) {
 #pragma unroll
@@ -520,10 +562,11 @@ __global__ void __launch_bounds__(192, 1) ffn_few_kernel(const __grid_constant__
                         if (c + j < p.rows && f < p.M) {
                             const float g = __uint_as_float(v[j]), u = part[(c + j) * 64 + r];
                             const long long at = (long long)(c + j) * p.ld + f;
-                            p.out0[at] = one16(act_value(g, p.act) * u, fp16);
+                            const float v = p.act == GALA_ACT_SILU ? act_value<GALA_ACT_SILU>(g) : p.act == GALA_ACT_GELU ? act_value<GALA_ACT_GELU>(g) : act_value<GALA_ACT_RELU>(g);
+                            p.out0[at] = one16<FP16>(v * u);
                             if (p.out1) {
-                                p.out1[at] = one16(g, fp16);
-                                p.out2[at] = one16(u, fp16);
+                                p.out1[at] = one16<FP16>(g);
+                                p.out2[at] = one16<FP16>(u);
                             }
                         }
                     }
@@ -551,7 +594,7 @@ __global__ void __launch_bounds__(192, 1) ffn_few_kernel(const __grid_constant__
             float s = 0.0f;
             for (int b = 0; b < split; b++) s += *cl.map_shared_rank(part + e, b);
             const int d = tile * 128 + (e & 127);
-            if (d < p.M) p.out0[(long long)(e >> 7) * p.ld + d] = one16(s, p.fp16 != 0);
+            if (d < p.M) p.out0[(long long)(e >> 7) * p.ld + d] = one16<FP16>(s);
         }
         cl.sync();
     }
@@ -574,17 +617,17 @@ bool map_mn(CUtensorMap* m, const void* base, uint64_t rows, uint64_t k, uint64_
 }
 int steps(long long k) { return (int)((k + 63) / 64); }
 
-template <bool A_MN, bool B_MN, int TN, int EPI>
-cudaError_t pair(const PairMaps& maps, PairArgs p, cudaStream_t st) {
-    constexpr int kWidth = EPI == EPI_PROJECT ? TN / 2 : TN;
-    const size_t smem = (size_t)kPairStages * (kHalfTile + TN / 2 * 128) + 1024;
+template <bool A_MN, bool B_MN, int EPI, int ACT, bool FP16>
+cudaError_t launch_pair(const PairMaps& maps, PairArgs p, cudaStream_t st) {
+    constexpr int kWidth = EPI == EPI_PROJECT ? 128 : 256;
+    constexpr size_t smem = (size_t)kPairStages * 2 * kHalfTile + 1024;
     static bool ready[64] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!ready[dev]) {
-        e = cudaFuncSetAttribute(ffn_pair_kernel<A_MN, B_MN, TN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        e = cudaFuncSetAttribute(ffn_pair_kernel<A_MN, B_MN, EPI, ACT, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         ready[dev] = true;
     }
@@ -593,11 +636,23 @@ cudaError_t pair(const PairMaps& maps, PairArgs p, cudaStream_t st) {
     p.tiles = (long long)p.mt * p.nt * (p.separate ? 2 : 1);
     long long pairs = sm_count() / 2;
     if (pairs > p.tiles) pairs = p.tiles;
-    return launch_pdl(ffn_pair_kernel<A_MN, B_MN, TN, EPI>, dim3((unsigned)(2 * pairs)), dim3(192), smem, st, maps, p);
+    return launch_pdl(ffn_pair_kernel<A_MN, B_MN, EPI, ACT, FP16>, dim3((unsigned)(2 * pairs)), dim3(kPairThreads), smem, st, maps, p);
+}
+template <bool A_MN, bool B_MN>
+cudaError_t pair_store(const PairMaps& maps, const PairArgs& p, bool fp16, cudaStream_t st) {
+    return fp16 ? launch_pair<A_MN, B_MN, EPI_STORE, 0, true>(maps, p, st) : launch_pair<A_MN, B_MN, EPI_STORE, 0, false>(maps, p, st);
+}
+template <bool A_MN, bool B_MN, int EPI>
+cudaError_t pair_act(const PairMaps& maps, const PairArgs& p, int act, bool fp16, cudaStream_t st) {
+    if (act == GALA_ACT_SILU)
+        return fp16 ? launch_pair<A_MN, B_MN, EPI, GALA_ACT_SILU, true>(maps, p, st) : launch_pair<A_MN, B_MN, EPI, GALA_ACT_SILU, false>(maps, p, st);
+    if (act == GALA_ACT_GELU)
+        return fp16 ? launch_pair<A_MN, B_MN, EPI, GALA_ACT_GELU, true>(maps, p, st) : launch_pair<A_MN, B_MN, EPI, GALA_ACT_GELU, false>(maps, p, st);
+    return fp16 ? launch_pair<A_MN, B_MN, EPI, GALA_ACT_RELU, true>(maps, p, st) : launch_pair<A_MN, B_MN, EPI, GALA_ACT_RELU, false>(maps, p, st);
 }
 
-template <int NT, bool DOWN>
-cudaError_t few(const CUtensorMap& w0, const CUtensorMap& w1, const CUtensorMap& x, const FewArgs& p, int tiles, int split, cudaStream_t st) {
+template <int NT, bool DOWN, bool FP16>
+cudaError_t launch_few(const CUtensorMap& w0, const CUtensorMap& w1, const CUtensorMap& x, const FewArgs& p, int tiles, int split, cudaStream_t st) {
     const size_t smem = (size_t)kFewStages * (kHalfTile + NT * 128) + 1024;
     static bool ready[64] = {};
     int dev = 0;
@@ -605,7 +660,7 @@ cudaError_t few(const CUtensorMap& w0, const CUtensorMap& w1, const CUtensorMap&
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!ready[dev]) {
-        e = cudaFuncSetAttribute(ffn_few_kernel<NT, DOWN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        e = cudaFuncSetAttribute(ffn_few_kernel<NT, DOWN, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         ready[dev] = true;
     }
@@ -622,7 +677,11 @@ cudaError_t few(const CUtensorMap& w0, const CUtensorMap& w1, const CUtensorMap&
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = DOWN ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, ffn_few_kernel<NT, DOWN>, w0, w1, x, p);
+    return cudaLaunchKernelEx(&cfg, ffn_few_kernel<NT, DOWN, FP16>, w0, w1, x, p);
+}
+template <int NT, bool DOWN>
+cudaError_t few(const CUtensorMap& w0, const CUtensorMap& w1, const CUtensorMap& x, const FewArgs& p, bool fp16, int tiles, int split, cudaStream_t st) {
+    return fp16 ? launch_few<NT, DOWN, true>(w0, w1, x, p, tiles, split, st) : launch_few<NT, DOWN, false>(w0, w1, x, p, tiles, split, st);
 }
 
 template <int NT>
@@ -635,7 +694,6 @@ cudaError_t forward_few(const gala_ffn_args& a, bool& mapped, cudaStream_t st) {
     FewArgs p = {};
     p.rows = (int)a.rows;
     p.act = a.act;
-    p.fp16 = a.dtype == GALA_F16;
     p.status = a.status;
     p.M = a.hidden;
     p.k = p.per = steps(a.dim);
@@ -643,7 +701,7 @@ cudaError_t forward_few(const gala_ffn_args& a, bool& mapped, cudaStream_t st) {
     p.out1 = static_cast<uint16_t*>(a.gate);
     p.out2 = static_cast<uint16_t*>(a.up);
     p.ld = a.hidden_ld;
-    cudaError_t e = few<NT, false>(wg, wu, x, p, (a.hidden + 63) / 64, 1, st);
+    cudaError_t e = few<NT, false>(wg, wu, x, p, a.dtype == GALA_F16, (a.hidden + 63) / 64, 1, st);
     if (e != cudaSuccess) return e;
     // the reduction over `hidden` is cut until the blocks fill the device
     const int tiles = (a.dim + 127) / 128;
@@ -655,7 +713,7 @@ cudaError_t forward_few(const gala_ffn_args& a, bool& mapped, cudaStream_t st) {
     p.out0 = static_cast<uint16_t*>(a.y);
     p.out1 = p.out2 = nullptr;
     p.ld = a.y_ld;
-    return few<NT, true>(wd, wd, h, p, tiles, split, st);
+    return few<NT, true>(wd, wd, h, p, a.dtype == GALA_F16, tiles, split, st);
 }
 
 cudaError_t forward_pair(const gala_ffn_args& a, bool& mapped, cudaStream_t st) {
@@ -675,11 +733,9 @@ cudaError_t forward_pair(const gala_ffn_args& a, bool& mapped, cudaStream_t st) 
     p.out1 = static_cast<uint16_t*>(a.gate);
     p.out2 = static_cast<uint16_t*>(a.up);
     p.ld = a.hidden_ld;
-    p.act = a.act;
-    p.fp16 = a.dtype == GALA_F16;
     p.wide = a.hidden_ld % 16 == 0 && aligned(a.product, 32) && aligned(a.gate, 32) && aligned(a.up, 32);
     p.status = a.status;
-    cudaError_t e = pair<false, false, 256, EPI_PROJECT>(m, p, st);
+    cudaError_t e = pair_act<false, false, EPI_PROJECT>(m, p, a.act, a.dtype == GALA_F16, st);
     if (e != cudaSuccess) return e;
     p.N = a.dim;
     p.k0 = p.k = steps(a.hidden);
@@ -687,7 +743,7 @@ cudaError_t forward_pair(const gala_ffn_args& a, bool& mapped, cudaStream_t st) 
     p.out1 = p.out2 = nullptr;
     p.ld = a.y_ld;
     p.wide = a.y_ld % 16 == 0 && aligned(a.y, 32);
-    return pair<false, false, 256, EPI_STORE>(d, p, st);
+    return pair_store<false, false>(d, p, a.dtype == GALA_F16, st);
 }
 
 cudaError_t backward(const gala_ffn_grad_args& a, bool& mapped, cudaStream_t st) {
@@ -704,8 +760,6 @@ cudaError_t backward(const gala_ffn_grad_args& a, bool& mapped, cudaStream_t st)
     if (mapped && a.dw_down) mapped = map_mn(&d.a0, a.dy, a.dim, a.rows, a.dy_ld) && map_mn(&d.b0, a.product, a.hidden, a.rows, a.hidden_ld);
     if (!mapped) return cudaSuccess;
     PairArgs base = {};
-    base.act = a.act;
-    base.fp16 = a.dtype == GALA_F16;
     base.status = a.status;
     cudaError_t e = cudaSuccess;
     if (gates) {
@@ -720,8 +774,8 @@ cudaError_t backward(const gala_ffn_grad_args& a, bool& mapped, cudaStream_t st)
         p.out0 = static_cast<uint16_t*>(a.dgate);
         p.out1 = static_cast<uint16_t*>(a.dup);
         p.ld = a.hidden_ld;
-        p.wide = a.hidden_ld % 16 == 0 && aligned(a.dgate, 32) && aligned(a.dup, 32);
-        if ((e = pair<false, true, 256, EPI_SLOPE>(s, p, st)) != cudaSuccess) return e;
+        p.wide = a.hidden_ld % 16 == 0 && aligned(a.dgate, 32) && aligned(a.dup, 32) && aligned(a.gate, 32) && aligned(a.up, 32);
+        if ((e = pair_act<false, true, EPI_SLOPE>(s, p, a.act, a.dtype == GALA_F16, st)) != cudaSuccess) return e;
     }
     if (a.dx) {
         PairArgs p = base;
@@ -732,7 +786,7 @@ cudaError_t backward(const gala_ffn_grad_args& a, bool& mapped, cudaStream_t st)
         p.out0 = static_cast<uint16_t*>(a.dx);
         p.ld = a.dx_ld;
         p.wide = a.dx_ld % 16 == 0 && aligned(a.dx, 32);
-        if ((e = pair<false, true, 256, EPI_STORE>(x, p, st)) != cudaSuccess) return e;
+        if ((e = pair_store<false, true>(x, p, a.dtype == GALA_F16, st)) != cudaSuccess) return e;
     }
     if (a.dw_gate || a.dw_up) {
         w.b1 = w.b0;
@@ -747,7 +801,7 @@ cudaError_t backward(const gala_ffn_grad_args& a, bool& mapped, cudaStream_t st)
         p.out1 = static_cast<uint16_t*>(a.dw_up);
         p.ld1 = a.dw_up_ld;
         p.wide = p.ld % 16 == 0 && aligned(p.out0, 32) && (!p.separate || (p.ld1 % 16 == 0 && aligned(p.out1, 32)));
-        if ((e = pair<true, true, 256, EPI_STORE>(w, p, st)) != cudaSuccess) return e;
+        if ((e = pair_store<true, true>(w, p, a.dtype == GALA_F16, st)) != cudaSuccess) return e;
     }
     if (a.dw_down) {
         d.a1 = d.a0;
@@ -759,7 +813,7 @@ cudaError_t backward(const gala_ffn_grad_args& a, bool& mapped, cudaStream_t st)
         p.out0 = static_cast<uint16_t*>(a.dw_down);
         p.ld = a.dw_down_ld;
         p.wide = p.ld % 16 == 0 && aligned(p.out0, 32);
-        e = pair<true, true, 256, EPI_STORE>(d, p, st);
+        e = pair_store<true, true>(d, p, a.dtype == GALA_F16, st);
     }
     return e;
 }

@@ -194,14 +194,13 @@ __device__ __forceinline__ PairTile pair_tile(const PairArgs& p, long long t, in
     return r;
 }
 
-// A_MN / B_MN: the operand is stored [K][rows] instead of [rows][K].
-template <bool A_MN, bool B_MN, int EPI, int ACT, bool FP16>
+// A_MN / B_MN: the operand is stored [K][rows] instead of [rows][K].  TN: columns of the accumulator.
+template <bool A_MN, bool B_MN, int TN, int EPI, int ACT, bool FP16>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) ffn_pair_kernel(const __grid_constant__ PairMaps maps, const PairArgs p) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t full_bar[kPairStages], empty_bar[kPairStages], acc_full[2], acc_empty[2];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag, issued;
-    constexpr int TN = 256;                                // columns of the accumulator
     constexpr int kB = TN / 2 * 128;                       // bytes of this CTA's half of the B tile
     constexpr int kStage = kHalfTile + kB;
     constexpr int kWidth = EPI == EPI_PROJECT ? TN / 2 : TN;    // output columns of a tile
@@ -230,40 +229,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) ffn
     pdl_launch();
 
     if (warp == 0) {
-        int it = 0;
+        // one lane a copy; what a lane copies does not change, only where
+        const int nA = A_MN ? 2 : 1, nB = B_MN ? TN / 128 : 1;
+        const bool is_a = lane < nA;
+        const int part = is_a ? lane : lane - nA;                       // 64-wide part of an MN-major operand
+        const bool mn = is_a ? A_MN : B_MN;
+        uint8_t* dst = smem + (is_a ? 0 : kHalfTile) + part * 8192;
+        const CUtensorMap* one = is_a ? &maps.a0 : EPI == EPI_PROJECT && rank ? &maps.b1 : &maps.b0;
+        const CUtensorMap* two = is_a ? &maps.a1 : &maps.b1;
+        const uint32_t bar0 = shared_of(&full_bar[0], 0);
+        int it = 0, s = 0;
+        uint32_t ph = 1;
         bool ok = true;
         for (long long t = first; ok && t < p.tiles; t += step) {
             const PairTile tile = pair_tile(p, t, kWidth);
-            const int am = (int)tile.m0 + (int)rank * 128;
-            for (int k = 0; k < p.k; k++, it++) {
-                const int s = it % kPairStages;
+            const int at = is_a ? (int)tile.m0 + (int)rank * 128 : EPI == EPI_PROJECT ? tile.n0 : tile.n0 + (int)rank * (TN / 2);
+            const CUtensorMap* map = p.separate && tile.group ? two : one;
+            int kc = 0;
+            for (int k = 0; k < p.k; k++) {
                 int go = 1;
-                if (lane == 0) go = mbar_wait(&empty_bar[s], ((uint32_t)(it / kPairStages) & 1u) ^ 1u, &abort_flag) ? 1 : 0;
+                if (lane == 0) go = mbar_wait(&empty_bar[s], ph, &abort_flag) ? 1 : 0;
                 go = __shfl_sync(0xffffffffu, go, 0);
                 if (!go) { ok = false; break; }
-                uint8_t* a = smem + s * kStage;
-                uint8_t* b = a + kHalfTile;
                 if (rank == 0 && lane == 0) mbar_expect_tx(&full_bar[s], 2 * kStage);
+                if (k == p.k0) kc = 0, map = two;                       // joined products: the second pair of operands
                 __syncwarp();
-                const uint32_t bar = shared_of(&full_bar[s], 0);
-                const bool second = p.separate ? tile.group != 0 : k >= p.k0;
-                const int kc = (p.separate || !second ? k : k - p.k0) * 64;
-                const CUtensorMap* ma = second ? &maps.a1 : &maps.a0;
-                const CUtensorMap* mb = EPI == EPI_PROJECT ? (rank ? &maps.b1 : &maps.b0) : second ? &maps.b1 : &maps.b0;
-                const int bn = EPI == EPI_PROJECT ? tile.n0 : tile.n0 + (int)rank * (TN / 2);
-                // one copy a lane: a thread issues them slowly one after another
-                if (!A_MN) {
-                    if (lane == 0) tma_load_3d_pair(a, ma, bar, kc, am);
-                } else if (lane < 2) {
-                    tma_load_3d_pair(a + lane * 8192, ma, bar, am + 64 * lane, kc);
-                }
-                if (!B_MN) {
-                    if (lane == 2) tma_load_3d_pair(b, mb, bar, kc, bn);
-                } else if (lane >= 2 && lane < 2 + TN / 128) {
-                    tma_load_3d_pair(b + (lane - 2) * 8192, mb, bar, bn + 64 * (lane - 2), kc);
-                }
+                if (lane < nA + nB) tma_load_3d_pair(dst + s * kStage, map, bar0 + 8 * s, mn ? at + 64 * part : kc, mn ? kc : at);
                 __syncwarp();
-                if (lane == 0) issued = it + 1;
+                kc += 64;
+                if (lane == 0) issued = ++it;
+                if (++s == kPairStages) s = 0, ph ^= 1u;
             }
         }
     } else if (warp == 1) {
@@ -271,25 +266,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) ffn
             const uint32_t fmt = FP16 ? 0u : ((1u << 7) | (1u << 10));
             const uint32_t idesc = (1u << 4) | fmt | ((uint32_t)A_MN << 15) | ((uint32_t)B_MN << 16) | ((uint32_t)(TN >> 3) << 17) |
                                    ((uint32_t)(256 >> 4) << 24);
-            int it = 0, local = 0;
+            // descriptors differ in the start address alone (16-byte units): per stage, and per 16 of K
+            const uint64_t a0 = make_smem_desc(smem_u32(smem), A_MN), b0 = make_smem_desc(smem_u32(smem) + kHalfTile, B_MN);
+            constexpr uint64_t kA = A_MN ? 2048 / 16 : 32 / 16, kBk = B_MN ? 2048 / 16 : 32 / 16;
+            int s = 0, local = 0;
+            uint32_t ph = 0;
             bool ok = true;
             for (long long t = first; ok && t < p.tiles; t += step, local++) {
                 const int ab = local & 1;
                 if (!mbar_wait(&acc_empty[ab], (((uint32_t)local >> 1) & 1u) ^ 1u, &abort_flag)) break;
                 tcgen05_fence_after();
                 const uint32_t acc = tmem + (uint32_t)(ab * TN);
-                for (int k = 0; k < p.k; k++, it++) {
-                    const int s = it % kPairStages;
-                    if (!mbar_wait(&full_bar[s], (uint32_t)(it / kPairStages) & 1u, &abort_flag)) { ok = false; break; }
+                uint32_t add = 0;
+                for (int k = 0; k < p.k; k++) {
+                    if (!mbar_wait(&full_bar[s], ph, &abort_flag)) { ok = false; break; }
                     tcgen05_fence_after();
-                    const uint32_t a = smem_u32(smem + s * kStage), b = a + kHalfTile;
+                    const uint64_t ad = a0 + (uint64_t)(s * (kStage / 16)), bd = b0 + (uint64_t)(s * (kStage / 16));
 #pragma unroll
                     for (int kk = 0; kk < 4; kk++) {
-                        const uint64_t ad = make_smem_desc(a + (A_MN ? kk * 2048 : kk * 32), A_MN);
-                        const uint64_t bd = make_smem_desc(b + (B_MN ? kk * 2048 : kk * 32), B_MN);
-                        umma_pair(acc, ad, bd, idesc, (k | kk) != 0 ? 1u : 0u);
+                        umma_pair(acc, ad + kk * kA, bd + kk * kBk, idesc, add);
+                        add = 1;
                     }
                     umma_commit_pair(&empty_bar[s]);
+                    if (++s == kPairStages) s = 0, ph ^= 1u;
                 }
                 if (!ok) break;
                 umma_commit_pair(&acc_full[ab]);
@@ -617,17 +616,17 @@ bool map_mn(CUtensorMap* m, const void* base, uint64_t rows, uint64_t k, uint64_
 }
 int steps(long long k) { return (int)((k + 63) / 64); }
 
-template <bool A_MN, bool B_MN, int EPI, int ACT, bool FP16>
+template <bool A_MN, bool B_MN, int TN, int EPI, int ACT, bool FP16>
 cudaError_t launch_pair(const PairMaps& maps, PairArgs p, cudaStream_t st) {
-    constexpr int kWidth = EPI == EPI_PROJECT ? 128 : 256;
-    constexpr size_t smem = (size_t)kPairStages * 2 * kHalfTile + 1024;
+    constexpr int kWidth = EPI == EPI_PROJECT ? TN / 2 : TN;
+    constexpr size_t smem = (size_t)kPairStages * (kHalfTile + TN / 2 * 128) + 1024;
     static bool ready[64] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!ready[dev]) {
-        e = cudaFuncSetAttribute(ffn_pair_kernel<A_MN, B_MN, EPI, ACT, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        e = cudaFuncSetAttribute(ffn_pair_kernel<A_MN, B_MN, TN, EPI, ACT, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         ready[dev] = true;
     }
@@ -636,19 +635,31 @@ cudaError_t launch_pair(const PairMaps& maps, PairArgs p, cudaStream_t st) {
     p.tiles = (long long)p.mt * p.nt * (p.separate ? 2 : 1);
     long long pairs = sm_count() / 2;
     if (pairs > p.tiles) pairs = p.tiles;
-    return launch_pdl(ffn_pair_kernel<A_MN, B_MN, EPI, ACT, FP16>, dim3((unsigned)(2 * pairs)), dim3(kPairThreads), smem, st, maps, p);
+    return launch_pdl(ffn_pair_kernel<A_MN, B_MN, TN, EPI, ACT, FP16>, dim3((unsigned)(2 * pairs)), dim3(kPairThreads), smem, st, maps, p);
+}
+// Columns of an output tile of a plain product.  Half tiles cost 0.61 of whole ones (one thread issues an MMA every 78
+// cycles at most, the whole tile's takes 128, the half tile's 64) and are taken where they need fewer rounds of the device
+// all the same: 1024 x 2048 from 8192 terms, 32 whole tiles for 74 pairs of SMs, 60 -> 37 us.
+int tile_columns(long long M, int N) {
+    const long long rows = (M + 255) / 256, pairs = sm_count() / 2;
+    const double whole = (double)((rows * ((N + 255) / 256) + pairs - 1) / pairs), halves = 0.61 * (double)((rows * ((N + 127) / 128) + pairs - 1) / pairs);
+    return halves < whole ? 128 : 256;
+}
+template <bool A_MN, bool B_MN, int TN>
+cudaError_t pair_store_sized(const PairMaps& maps, const PairArgs& p, bool fp16, cudaStream_t st) {
+    return fp16 ? launch_pair<A_MN, B_MN, TN, EPI_STORE, 0, true>(maps, p, st) : launch_pair<A_MN, B_MN, TN, EPI_STORE, 0, false>(maps, p, st);
 }
 template <bool A_MN, bool B_MN>
-cudaError_t pair_store(const PairMaps& maps, const PairArgs& p, bool fp16, cudaStream_t st) {
-    return fp16 ? launch_pair<A_MN, B_MN, EPI_STORE, 0, true>(maps, p, st) : launch_pair<A_MN, B_MN, EPI_STORE, 0, false>(maps, p, st);
+cudaError_t pair_store(const PairMaps& maps, const PairArgs& p, int columns, bool fp16, cudaStream_t st) {
+    return columns == 128 ? pair_store_sized<A_MN, B_MN, 128>(maps, p, fp16, st) : pair_store_sized<A_MN, B_MN, 256>(maps, p, fp16, st);
 }
 template <bool A_MN, bool B_MN, int EPI>
 cudaError_t pair_act(const PairMaps& maps, const PairArgs& p, int act, bool fp16, cudaStream_t st) {
     if (act == GALA_ACT_SILU)
-        return fp16 ? launch_pair<A_MN, B_MN, EPI, GALA_ACT_SILU, true>(maps, p, st) : launch_pair<A_MN, B_MN, EPI, GALA_ACT_SILU, false>(maps, p, st);
+        return fp16 ? launch_pair<A_MN, B_MN, 256, EPI, GALA_ACT_SILU, true>(maps, p, st) : launch_pair<A_MN, B_MN, 256, EPI, GALA_ACT_SILU, false>(maps, p, st);
     if (act == GALA_ACT_GELU)
-        return fp16 ? launch_pair<A_MN, B_MN, EPI, GALA_ACT_GELU, true>(maps, p, st) : launch_pair<A_MN, B_MN, EPI, GALA_ACT_GELU, false>(maps, p, st);
-    return fp16 ? launch_pair<A_MN, B_MN, EPI, GALA_ACT_RELU, true>(maps, p, st) : launch_pair<A_MN, B_MN, EPI, GALA_ACT_RELU, false>(maps, p, st);
+        return fp16 ? launch_pair<A_MN, B_MN, 256, EPI, GALA_ACT_GELU, true>(maps, p, st) : launch_pair<A_MN, B_MN, 256, EPI, GALA_ACT_GELU, false>(maps, p, st);
+    return fp16 ? launch_pair<A_MN, B_MN, 256, EPI, GALA_ACT_RELU, true>(maps, p, st) : launch_pair<A_MN, B_MN, 256, EPI, GALA_ACT_RELU, false>(maps, p, st);
 }
 
 template <int NT, bool DOWN, bool FP16>
@@ -718,9 +729,10 @@ cudaError_t forward_few(const gala_ffn_args& a, bool& mapped, cudaStream_t st) {
 
 cudaError_t forward_pair(const gala_ffn_args& a, bool& mapped, cudaStream_t st) {
     PairMaps m, d;
+    const int columns = tile_columns(a.rows, a.dim);
     mapped = map_k(&m.a0, a.x, a.rows, a.dim, a.x_ld, 128) && map_k(&m.b0, a.w_gate, a.hidden, a.dim, a.w_gate_ld, 128) &&
              map_k(&m.b1, a.w_up, a.hidden, a.dim, a.w_up_ld, 128) && map_k(&d.a0, a.product, a.rows, a.hidden, a.hidden_ld, 128) &&
-             map_k(&d.b0, a.w_down, a.dim, a.hidden, a.w_down_ld, 128);
+             map_k(&d.b0, a.w_down, a.dim, a.hidden, a.w_down_ld, (uint32_t)columns / 2);
     if (!mapped) return cudaSuccess;
     m.a1 = m.a0;
     d.a1 = d.a0;
@@ -743,7 +755,7 @@ cudaError_t forward_pair(const gala_ffn_args& a, bool& mapped, cudaStream_t st) 
     p.out1 = p.out2 = nullptr;
     p.ld = a.y_ld;
     p.wide = a.y_ld % 16 == 0 && aligned(a.y, 32);
-    return pair_store<false, false>(d, p, a.dtype == GALA_F16, st);
+    return pair_store<false, false>(d, p, columns, a.dtype == GALA_F16, st);
 }
 
 cudaError_t backward(const gala_ffn_grad_args& a, bool& mapped, cudaStream_t st) {
@@ -786,7 +798,7 @@ cudaError_t backward(const gala_ffn_grad_args& a, bool& mapped, cudaStream_t st)
         p.out0 = static_cast<uint16_t*>(a.dx);
         p.ld = a.dx_ld;
         p.wide = a.dx_ld % 16 == 0 && aligned(a.dx, 32);
-        if ((e = pair_store<false, true>(x, p, a.dtype == GALA_F16, st)) != cudaSuccess) return e;
+        if ((e = pair_store<false, true>(x, p, tile_columns(a.rows, a.dim), a.dtype == GALA_F16, st)) != cudaSuccess) return e;
     }
     if (a.dw_gate || a.dw_up) {
         w.b1 = w.b0;
@@ -801,7 +813,7 @@ cudaError_t backward(const gala_ffn_grad_args& a, bool& mapped, cudaStream_t st)
         p.out1 = static_cast<uint16_t*>(a.dw_up);
         p.ld1 = a.dw_up_ld;
         p.wide = p.ld % 16 == 0 && aligned(p.out0, 32) && (!p.separate || (p.ld1 % 16 == 0 && aligned(p.out1, 32)));
-        if ((e = pair_store<true, true>(w, p, a.dtype == GALA_F16, st)) != cudaSuccess) return e;
+        if ((e = pair_store<true, true>(w, p, tile_columns(p.separate ? 2ll * ((a.hidden + 255) / 256 * 256) : a.hidden, a.dim), a.dtype == GALA_F16, st)) != cudaSuccess) return e;
     }
     if (a.dw_down) {
         d.a1 = d.a0;
@@ -813,7 +825,7 @@ cudaError_t backward(const gala_ffn_grad_args& a, bool& mapped, cudaStream_t st)
         p.out0 = static_cast<uint16_t*>(a.dw_down);
         p.ld = a.dw_down_ld;
         p.wide = p.ld % 16 == 0 && aligned(p.out0, 32);
-        e = pair_store<true, true>(d, p, a.dtype == GALA_F16, st);
+        e = pair_store<true, true>(d, p, tile_columns(a.dim, a.hidden), a.dtype == GALA_F16, st);
     }
     return e;
 }

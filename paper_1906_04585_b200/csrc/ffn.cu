@@ -159,7 +159,8 @@ __device__ __forceinline__ void load32(const uint16_t* p, uint32_t (&o)[16], int
 // ================================================================================== pair kernel
 enum { EPI_STORE, EPI_PROJECT, EPI_SLOPE };
 
-constexpr int kPairStages = 6;
+constexpr int kPairStages = 3;
+constexpr int kDeep = 2;                    // K steps of 64 a stage: half the barriers a step (the loops of both warps bound it)
 constexpr int kPairThreads = 320;
 constexpr int kHalfTile = 128 * 128;        // bytes of 128 rows (or MN elements) x 64 K of a 16-bit type
 constexpr int kBand = 8;                    // row tiles that are walked together, for L2
@@ -202,7 +203,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) ffn
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag, issued;
     constexpr int kB = TN / 2 * 128;                       // bytes of this CTA's half of the B tile
-    constexpr int kStage = kHalfTile + kB;
+    constexpr int kStage = kDeep * (kHalfTile + kB);       // A of each K step, then B of each
     constexpr int kWidth = EPI == EPI_PROJECT ? TN / 2 : TN;    // output columns of a tile
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -230,11 +231,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) ffn
 
     if (warp == 0) {
         // one lane a copy; what a lane copies does not change, only where
-        const int nA = A_MN ? 2 : 1, nB = B_MN ? TN / 128 : 1;
-        const bool is_a = lane < nA;
-        const int part = is_a ? lane : lane - nA;                       // 64-wide part of an MN-major operand
+        constexpr int nA = A_MN ? 2 : 1, nB = B_MN ? TN / 128 : 1;
+        const bool is_a = lane < kDeep * nA;
+        const int nth = is_a ? lane : lane - kDeep * nA;
+        const int deep = nth / (is_a ? nA : nB), part = nth % (is_a ? nA : nB);      // K step of the stage, 64-wide part of an MN-major operand
         const bool mn = is_a ? A_MN : B_MN;
-        uint8_t* dst = smem + (is_a ? 0 : kHalfTile) + part * 8192;
+        uint8_t* dst = smem + (is_a ? deep * kHalfTile : kDeep * kHalfTile + deep * kB) + part * 8192;
         const CUtensorMap* one = is_a ? &maps.a0 : EPI == EPI_PROJECT && rank ? &maps.b1 : &maps.b0;
         const CUtensorMap* two = is_a ? &maps.a1 : &maps.b1;
         const uint32_t bar0 = shared_of(&full_bar[0], 0);
@@ -243,20 +245,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) ffn
         bool ok = true;
         for (long long t = first; ok && t < p.tiles; t += step) {
             const PairTile tile = pair_tile(p, t, kWidth);
-            const int at = is_a ? (int)tile.m0 + (int)rank * 128 : EPI == EPI_PROJECT ? tile.n0 : tile.n0 + (int)rank * (TN / 2);
+            const int at = (is_a ? (int)tile.m0 + (int)rank * 128 : EPI == EPI_PROJECT ? tile.n0 : tile.n0 + (int)rank * (TN / 2)) + (mn ? 64 * part : 0);
             const CUtensorMap* map = p.separate && tile.group ? two : one;
-            int kc = 0;
-            for (int k = 0; k < p.k; k++) {
+            int k = deep;                          // past the last K step a copy brings zeros
+            for (int i = 0; i < p.k; i += kDeep, k += kDeep) {
                 int go = 1;
                 if (lane == 0) go = mbar_wait(&empty_bar[s], ph, &abort_flag) ? 1 : 0;
                 go = __shfl_sync(0xffffffffu, go, 0);
                 if (!go) { ok = false; break; }
                 if (rank == 0 && lane == 0) mbar_expect_tx(&full_bar[s], 2 * kStage);
-                if (k == p.k0) kc = 0, map = two;                       // joined products: the second pair of operands
                 __syncwarp();
-                if (lane < nA + nB) tma_load_3d_pair(dst + s * kStage, map, bar0 + 8 * s, mn ? at + 64 * part : kc, mn ? kc : at);
+                if (lane < kDeep * (nA + nB)) {
+                    const bool second = p.k0 < p.k && k >= p.k0;      // joined products: the second pair of operands
+                    const int kc = (second ? k - p.k0 : k) * 64;
+                    tma_load_3d_pair(dst + s * kStage, second ? two : map, bar0 + 8 * s, mn ? at : kc, mn ? kc : at);
+                }
                 __syncwarp();
-                kc += 64;
                 if (lane == 0) issued = ++it;
                 if (++s == kPairStages) s = 0, ph ^= 1u;
             }
@@ -266,8 +270,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) ffn
             const uint32_t fmt = FP16 ? 0u : ((1u << 7) | (1u << 10));
             const uint32_t idesc = (1u << 4) | fmt | ((uint32_t)A_MN << 15) | ((uint32_t)B_MN << 16) | ((uint32_t)(TN >> 3) << 17) |
                                    ((uint32_t)(256 >> 4) << 24);
-            // descriptors differ in the start address alone (16-byte units): per stage, and per 16 of K
-            const uint64_t a0 = make_smem_desc(smem_u32(smem), A_MN), b0 = make_smem_desc(smem_u32(smem) + kHalfTile, B_MN);
+            // descriptors differ in the start address alone (16-byte units): per stage, K step and 16 of K
+            const uint64_t a0 = make_smem_desc(smem_u32(smem), A_MN), b0 = make_smem_desc(smem_u32(smem) + kDeep * kHalfTile, B_MN);
             constexpr uint64_t kA = A_MN ? 2048 / 16 : 32 / 16, kBk = B_MN ? 2048 / 16 : 32 / 16;
             int s = 0, local = 0;
             uint32_t ph = 0;
@@ -278,13 +282,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) ffn
                 tcgen05_fence_after();
                 const uint32_t acc = tmem + (uint32_t)(ab * TN);
                 uint32_t add = 0;
-                for (int k = 0; k < p.k; k++) {
+                for (int k = 0; k < p.k; k += kDeep) {
                     if (!mbar_wait(&full_bar[s], ph, &abort_flag)) { ok = false; break; }
                     tcgen05_fence_after();
                     const uint64_t ad = a0 + (uint64_t)(s * (kStage / 16)), bd = b0 + (uint64_t)(s * (kStage / 16));
 #pragma unroll
-                    for (int kk = 0; kk < 4; kk++) {
-                        umma_pair(acc, ad + kk * kA, bd + kk * kBk, idesc, add);
+                    for (int kk = 0; kk < 4 * kDeep; kk++) {
+                        umma_pair(acc, ad + (kk >> 2) * (kHalfTile / 16) + (kk & 3) * kA, bd + (kk >> 2) * (kB / 16) + (kk & 3) * kBk, idesc, add);
                         add = 1;
                     }
                     umma_commit_pair(&empty_bar[s]);
@@ -619,7 +623,7 @@ int steps(long long k) { return (int)((k + 63) / 64); }
 template <bool A_MN, bool B_MN, int TN, int EPI, int ACT, bool FP16>
 cudaError_t launch_pair(const PairMaps& maps, PairArgs p, cudaStream_t st) {
     constexpr int kWidth = EPI == EPI_PROJECT ? TN / 2 : TN;
-    constexpr size_t smem = (size_t)kPairStages * (kHalfTile + TN / 2 * 128) + 1024;
+    constexpr size_t smem = (size_t)kPairStages * kDeep * (kHalfTile + TN / 2 * 128) + 1024;
     static bool ready[64] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);

@@ -16,6 +16,9 @@ LIB = os.path.join(HERE, "libgala.so")
 # GALA_CONV_LEGACY selects the earlier convolution products (a second implementation that one test compares
 # with the oracle).  Nothing but that test loads it.
 CHECK_LIB = os.path.join(HERE, "libgala_check.so")
+# The short way from torch tensors to the sequence-policy operators (csrc/front.cpp), a CPython module.
+FRONT_LIB = os.path.join(HERE, "_front.so")
+FRONT_SRC = os.path.join(CSRC, "front.cpp")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 FLAGS = [
@@ -30,11 +33,29 @@ def sources():
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(CHECK_LIB):
+    built = (LIB, CHECK_LIB, FRONT_LIB)
+    if not all(os.path.exists(p) for p in built):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(CHECK_LIB))
-    deps = sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
+    t = min(os.path.getmtime(p) for p in built)
+    deps = sources() + [FRONT_SRC] + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
     return any(os.path.getmtime(p) > t for p in deps)
+
+
+def _front_command(out: str):
+    """g++ command of the torch front end: linked to the torch that this interpreter imports and to libgala.so beside it."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    cuda = os.path.dirname(os.path.dirname(NVCC))
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+           "-I" + os.path.join(ROOT, "include"), "-I" + sysconfig.get_paths()["include"], "-isystem", os.path.join(cuda, "include")]
+    for d in cpp_extension.include_paths():
+        cmd += ["-isystem", d]
+    cmd += [FRONT_SRC, "-o", out, "-L" + HERE, "-l:libgala.so", "-Wl,-rpath,$ORIGIN"]
+    for d in cpp_extension.library_paths():
+        cmd += ["-L" + d, "-Wl,-rpath," + d]
+    return cmd + ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch", "-ltorch_python"]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -68,6 +89,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tmp = CHECK_LIB + ".tmp.%d" % os.getpid()
     subprocess.check_call([NVCC, "-shared", "-o", tmp] + check_objs + ["-gencode", "arch=compute_100a,code=sm_100a"])
     os.replace(tmp, CHECK_LIB)
+    tmp = FRONT_LIB + ".tmp.%d" % os.getpid()
+    subprocess.check_call(_front_command(tmp))
+    os.replace(tmp, FRONT_LIB)
     return LIB
 
 

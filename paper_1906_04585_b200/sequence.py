@@ -21,8 +21,13 @@ _DTYPE = {torch.float32: B.GALA_F32, torch.bfloat16: B.GALA_BF16, torch.float16:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
-# A call on small tensors is bound by this file: the checks below look at a tensor that is as it should be with four
-# cheap questions and go into words only where one of them is answered with no.
+# A call on small tensors is bound by the host.  The compiled front end (csrc/front.cpp) takes the forward calls whose
+# arguments are as they should be; it returns None for all others, and the code below says what is wrong with them, or
+# takes what only it can.  It is built with libgala.so; without it every call goes through the code below.
+try:
+    from . import _front
+except ImportError:
+    _front = None
 
 
 def _stream(t: torch.Tensor) -> int:
@@ -78,18 +83,17 @@ _status = {}
 
 def _status_word(t: torch.Tensor) -> int:
     index = t.get_device()
-    word = _status.get(index)
-    if word is None:
-        _status[index] = torch.zeros(1, dtype=torch.int32, device=t.device)
+    if index not in _status:
+        word = torch.zeros(1, dtype=torch.int32, device=t.device)
         torch.cuda.synchronize(index)      # streams that do not follow this one may use it next
-        word = _status[index]
-    return word.data_ptr()
+        _status[index] = word, word.data_ptr()
+    return _status[index][1]
 
 
 def check() -> None:
     """Waits for the current stream and raises if a bounded wait inside a kernel of this module ran out since the last
     check (results since then are not to be trusted); the word is cleared."""
-    for word in _status.values():
+    for word, _ in _status.values():
         if int(word.item()):
             word.zero_()
             raise B.GalaError(B.GALA_ECUDA, "a bounded device-side wait ran out")
@@ -100,6 +104,10 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
                residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None):
     """Layer norm of s = x (+ residual) over its columns; x [rows, cols].  Returns (y, s, mean, rstd); s is x itself
     without a residual.  weight and bias [cols] are float32 or of x's type."""
+    if _front is not None:
+        done = _front.layer_norm(x, weight, bias, eps, residual, out, sum_out)
+        if done is not None:
+            return done
     st = _stream(x)
     if x.dim() != 2:
         raise ValueError("x has to be a matrix [rows, cols]")
@@ -189,6 +197,10 @@ def gated_recurrence(f: torch.Tensor, x: torch.Tensor, h0: Optional[torch.Tensor
     [steps, batch] with the meaning it has in a rollout.  Returns (h, h_last, states): h_last [batch, dim] is the h0 of
     the next call (pass the same tensor as h0 and h_last to keep a state in place), states is what the backward call
     needs (None unless `save`)."""
+    if _front is not None and not save and x.is_cuda:
+        got = _front.gated_recurrence(f, x, h0, done, out, h_last, _status_word(x))
+        if got is not None:
+            return got
     st = _stream(x)
     if x.dim() != 3:
         raise ValueError("x has to be [steps, batch, dim]")
@@ -265,6 +277,10 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
     """y = (act(x w_gate^T) * (x w_up^T)) w_down^T for x [rows, dim], w_gate and w_up [hidden, dim], w_down [dim, hidden],
     all bfloat16 or all float16; activation "silu", "gelu" or "relu".  Every matrix starts on a 16-byte boundary and has a
     row stride that is a multiple of 8.  Returns (y, saved); saved is what the backward call needs (None unless `save`)."""
+    if _front is not None and not save and x.is_cuda:
+        y = _front.gated_ffn(x, w_gate, w_up, w_down, _ACT.get(activation, -1), out, _status_word(x))
+        if y is not None:
+            return y, None
     st = _stream(x)
     a = B.gala_ffn_args()
     rows, dim, hidden = _ffn_shapes(a, x, w_gate, w_up, w_down, activation)
@@ -314,6 +330,10 @@ def sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature: Optional[t
     [rows] in [0, 1) after temperature, top-k, top-p and min-p (each [rows] or None).  Returns (tokens int32, logprobs
     float32): the log-probability is that of the distribution that was drawn from.  Temperature <= 0 takes the largest
     entry; a row that is all -inf (or NaN) gives token -1."""
+    if _front is not None:
+        drawn = _front.sample(logits, uniforms, temperature, top_k, top_p, min_p, out, logprobs)
+        if drawn is not None:
+            return drawn
     st = _stream(logits)
     if logits.dim() != 2:
         raise ValueError("logits has to be a matrix [rows, vocab]")

@@ -46,6 +46,12 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
     if (std::is_same<T, __half>::value) return __half2float(__ushort_as_half((unsigned short)u));
     return __uint_as_float(u);
 }
+template <typename T>
+__device__ __forceinline__ float value_of(uint32_t u) {        // of the stored bits; NaN stays NaN
+    if (std::is_same<T, __nv_bfloat16>::value) return __uint_as_float(u << 16);
+    if (std::is_same<T, __half>::value) return __half2float(__ushort_as_half((unsigned short)u));
+    return __uint_as_float(u);
+}
 template <typename T> __device__ __forceinline__ uint32_t key_bottom() { return key_of<T>((1u << (kKeyBits<T> - 1)) | kInfinite<T>); }   // of -inf: keys above it can be drawn
 
 __device__ __forceinline__ u64 warp_sum(u64 v) {
@@ -65,13 +71,14 @@ struct Weigh {
     __device__ __forceinline__ Weigh(uint32_t k, float t)
         : top(k), most(logit_of<T>(k)), temp(t), inv(1.0f / t), plain(!(t > 1e-30f && t < 1e30f) || isinf(most)) {}
     // (l - m) / T by the row's reciprocal and one correction step with the exact remainder (Markstein), which is the
-    // rounded quotient; below -200, where the weight is 0, nothing infinite or undefined goes on
-    __device__ __forceinline__ float weight(uint32_t k) const {
-        const float d = logit_of<T>(k) - most;
-        if (plain) return k == top ? 1.0f : k <= key_bottom<T>() ? 0.0f : expf(__fdiv_rn(d, temp));
+    // rounded quotient.  Below -200, where the weight is 0, nothing infinite or undefined goes on; a NaN ends there too.
+    __device__ __forceinline__ float weight_at(float l) const {
+        const float d = l - most;
+        if (plain) return l == most ? 1.0f : l > -INFINITY ? expf(__fdiv_rn(d, temp)) : 0.0f;
         const float z = d * inv;
         return expf(fmaxf(fmaf(fmaf(-z, temp, d), inv, z), -200.0f));
     }
+    __device__ __forceinline__ float weight(uint32_t k) const { return weight_at(logit_of<T>(k)); }
     // w 2^44 as a whole number, without the conversion unit: 22 bits at a time in the mantissa of 2^23
     static __device__ __forceinline__ u64 quant(float w) {
         const float a = fmaf(w, 4194304.0f, 8388608.0f);                    // 2^23 + the nearest multiple of 2^-22
@@ -80,10 +87,9 @@ struct Weigh {
         return ((u64)(__float_as_uint(a) & 0x7fffffu) << 22) + (u64)(long long)((int)(__float_as_uint(b) & 0x7fffffu) - 0x400000);
     }
     __device__ __forceinline__ u64 mass(uint32_t k) const { return quant(weight(k)); }
-    // bin of the first histogram round: never smaller for a smaller key
-    __device__ __forceinline__ int step(uint32_t k, float bins, int last) const {
-        return plain ? 0 : (int)fminf((most - logit_of<T>(k)) * inv * bins, (float)last);
-    }
+    // bin of the first histogram round: never smaller for a smaller logit
+    __device__ __forceinline__ int step_at(float l, float bins, int last) const { return plain ? 0 : (int)fminf((most - l) * inv * bins, (float)last); }
+    __device__ __forceinline__ int step(uint32_t k, float bins, int last) const { return step_at(logit_of<T>(k), bins, last); }
 };
 // What top-p wants of a sum: NaN and what is not positive take the first entry alone.
 __device__ __forceinline__ u64 share(float p, u64 sum) {
@@ -214,7 +220,7 @@ constexpr int kBins = 2048;
 constexpr float kFirstBins = 128.0f;      // bins of one unit of (m - l) / T in the first round
 
 struct Shared {
-    uint32_t part[3][kBins];              // sums by 15 bits at a time: 2^15 entries of a block fit, and nothing comes back
+    int part[3][kBins];                   // sums of the weights' three parts (weigh), or counts: 2^15 entries of a block fit
     u64 warp_slots[2][32], rank_slots[2][8];
     u64 before, amount;                   // answer of a round: the sum ahead of the bin, and the bin's own
     int bin;
@@ -288,12 +294,18 @@ struct RowTeam {
         }
         par ^= 1;
     }
-    __device__ __forceinline__ void count(int bin) { atomicAdd(&sm.part[0][bin], 1u); }
-    __device__ __forceinline__ void weigh(int bin, u64 q) {
-        atomicAdd(&sm.part[0][bin], (uint32_t)q & 0x7fffu);
-        atomicAdd(&sm.part[1][bin], (uint32_t)(q >> 15) & 0x7fffu);
-        const uint32_t high = (uint32_t)(q >> 30);
+    __device__ __forceinline__ void count(int bin) { atomicAdd(&sm.part[0][bin], 1); }
+    // The weight in units of 2^-15, the rest of it in units of 2^-30 and the rest of that in units of 2^-44, each the nearest
+    // (the last two with a sign) and taken from the mantissa of a sum with 2^23: what quant() gives, in parts that the
+    // atomics can add up without a carry.
+    __device__ __forceinline__ void weigh(int bin, float w) {
+        const float a = fmaf(w, 32768.0f, 8388608.0f), r = fmaf(a - 8388608.0f, -1.0f / 32768.0f, w);
+        const float b = fmaf(r, 1073741824.0f, 12582912.0f), r2 = fmaf(b - 12582912.0f, -1.0f / 1073741824.0f, r);
+        const float c = fmaf(r2, kOne, 12582912.0f);
+        const int high = __float_as_int(a) - 0x4b000000;
         if (high) atomicAdd(&sm.part[2][bin], high);
+        atomicAdd(&sm.part[1][bin], __float_as_int(b) - 0x4b400000);
+        atomicAdd(&sm.part[0][bin], __float_as_int(c) - 0x4b400000);
     }
     // One histogram round.  put() calls count(bin) or weigh(bin, mass) for this thread's entries; want(total) is asked once the bins are
     // full, with their sum.  Returns the first bin at which the running sum, starting from `ahead`, reaches it (-1: none
@@ -310,10 +322,10 @@ struct RowTeam {
         // the bins are shared out over all threads of the team, in order; a thread adds its bins up over the blocks
         const int per = (kBins + nt * ranks - 1) / (nt * ranks), b0 = min((rank * nt + (int)threadIdx.x) * per, kBins), b1 = min(b0 + per, kBins);
         auto value = [&](int b) -> u64 {
-            u64 v = 0;
+            long long v = 0;
 #pragma unroll
             for (int k = 0; k < 3; k++) {
-                u64 x = 0;
+                long long x = 0;
                 if (CLUSTER) {
 #pragma unroll
                     for (int r = 0; r < 8; r++)
@@ -321,9 +333,9 @@ struct RowTeam {
                 } else {
                     x = sm.part[k][b];
                 }
-                v += x << (15 * k);
+                v += x << (k == 2 ? 29 : 14 * k);
             }
-            return v;
+            return (u64)v;
         };
         u64 mine = 0;
         for (int b = b0; b < b1; b++) mine += value(b);
@@ -361,7 +373,7 @@ template <typename T, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_sample_args p, const int ranks, const int each) {
     extern __shared__ __align__(16) uint8_t row_memory[];
     __shared__ Shared sm;
-    Bits<T>* keys = reinterpret_cast<Bits<T>*>(row_memory);      // this block's `each` entries, keys of 0 past the row's end
+    Bits<T>* raw = reinterpret_cast<Bits<T>*>(row_memory);      // this block's `each` entries as stored, -inf past the row's end
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     RowTeam<T, CLUSTER> team(sm, CLUSTER ? ranks : 1);
     const long long row = CLUSTER ? (long long)(blockIdx.x / ranks) : (long long)blockIdx.x;
@@ -370,32 +382,46 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
     if (CLUSTER) cg::this_cluster().sync();     // every block runs before one writes to another's shared memory
     const int first = team.rank * each, mine = max(0, min(each, p.vocab - first));
     const Bits<T>* l = static_cast<const Bits<T>*>(p.logits) + row * p.logits_ld + first;
+    constexpr Bits<T> kNone = (Bits<T>)((1u << (kKeyBits<T> - 1)) | kInfinite<T>);      // -inf
     uint32_t top = 0, unused = 0;
     {
+        // comparisons are between values, to which a NaN is never above anything, and -0 and +0 are one
         constexpr int N = 16 / (int)sizeof(T);
-        auto one = [&](uint32_t u) -> uint32_t {
-            const uint32_t k = key_of<T>(u);
-            top = max(top, k);
-            return k;
+        float most = -INFINITY;
+        auto see = [&](uint32_t u) {
+            if (sizeof(T) == 4) {
+                most = fmaxf(most, value_of<T>(u));
+            } else {
+                most = fmaxf(most, fmaxf(value_of<T>(u & 0xffffu), value_of<T>(u >> 16)));
+            }
         };
-        auto word = [&](uint32_t u) -> uint32_t { return sizeof(T) == 4 ? one(u) : one(u & 0xffffu) | (one(u >> 16) << 16); };
         int done = 0;
         if ((reinterpret_cast<uintptr_t>(l) & 15) == 0) {
             done = mine / N * N;
 #pragma unroll 4
             for (int v = threadIdx.x; v < mine / N; v += blockDim.x) {
                 const uint4 x = reinterpret_cast<const uint4*>(l)[v];
-                reinterpret_cast<uint4*>(keys)[v] = make_uint4(word(x.x), word(x.y), word(x.z), word(x.w));
+                reinterpret_cast<uint4*>(raw)[v] = x;
+                see(x.x), see(x.y), see(x.z), see(x.w);
             }
         }
-        for (int e = done + threadIdx.x; e < each; e += blockDim.x) keys[e] = e < mine ? (Bits<T>)one(l[e]) : (Bits<T>)0;
+        for (int e = done + threadIdx.x; e < each; e += blockDim.x) {
+            raw[e] = e < mine ? l[e] : kNone;
+            most = fmaxf(most, value_of<T>(raw[e]));
+        }
+        // its key, from its own bits
+        const uint32_t bits = std::is_same<T, __nv_bfloat16>::value ? __float_as_uint(most) >> 16
+                              : std::is_same<T, __half>::value      ? __half_as_ushort(__float2half_rn(most))
+                                                                    : __float_as_uint(most);
+        top = key_of<T>(bits);
     }
     if (threadIdx.x == 0) sm.owner = -1;
     team.extremes(unused, top);                 // its barrier is the one before the keys are read
     const float temp = p.temperature ? p.temperature[row] : 1.0f;
     // a warp's entries follow one another: 32 at a time, `groups` times
     const int groups = each / (32 * team.warps), base = w * groups * 32 + lane;
-    const Bits<T>* own = keys + base;
+    const Bits<T>* own = raw + base;
+    auto at_own = [&](int i) -> float { return value_of<T>(own[32 * i]); };
 
     if (top <= key_bottom<T>()) {
         if (team.rank == 0 && threadIdx.x == 0) answer(p, row, -1, 0.0f, 1);
@@ -404,7 +430,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
         uint32_t at = 0xffffffffu, unused2 = 0;
 #pragma unroll 4
         for (int i = 0; i < groups; i++)
-            if (own[32 * i] == top) at = min(at, (uint32_t)(first + base + 32 * i));
+            if (at_own(i) == logit_of<T>(top)) at = min(at, (uint32_t)(first + base + 32 * i));
         team.extremes(at, unused2);
         if (team.rank == 0 && threadIdx.x == 0) answer(p, row, (int)at, 1.0f, (u64)kOne);
     } else {
@@ -422,15 +448,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
             const int b1 = team.round(
                 ahead, amount,
                 [&] {
+                    const float least = logit_of<T>(floor);
 #pragma unroll 4
                     for (int i = 0; i < groups; i++) {
-                        const uint32_t k = own[32 * i];
-                        if (k > floor) {
-                            const int b = wt.step(k, kFirstBins, last);
+                        const float x = at_own(i);
+                        if (x > least) {
+                            const int b = wt.step_at(x, kFirstBins, last);
                             if (MASS) {
-                                const u64 q = wt.mass(k);
-                                if (b < last) team.weigh(b, q);
-                                else tail += q;
+                                const float w = wt.weight_at(x);
+                                if (b < last) team.weigh(b, w);
+                                else tail += Weigh<T>::quant(w);
                             } else {
                                 if (b < last) team.count(b);
                                 else tail++;
@@ -467,12 +494,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
                 const int b = team.round(
                     ahead, amount,
                     [&] {
+                        const float from = logit_of<T>(lo), to = logit_of<T>(hi);
 #pragma unroll 4
                         for (int i = 0; i < groups; i++) {
-                            const uint32_t k = own[32 * i];
-                            if (k >= lo && k <= hi) {
-                                const int b = (int)((hi - k) >> shift);
-                                if (MASS) team.weigh(b, wt.mass(k));
+                            const float x = at_own(i);
+                            if (x >= from && x <= to) {
+                                const int b = (int)((hi - key_of<T>(own[32 * i])) >> shift);
+                                if (MASS) team.weigh(b, wt.weight_at(x));
                                 else team.count(b);
                             }
                         }
@@ -517,11 +545,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
             }
         }
         const float mp = p.min_p ? fminf(p.min_p[row], 1.0f) : 0.0f;
-        if (room && !part) cut--;               // every entry equal to it stays (cut is above the bottom key here)
+        if (room && !part) {                    // every entry equal to it stays: the cut is below it (no entry has the key of -0)
+            cut--;
+            if (cut == (1u << (kKeyBits<T> - 1)) - 1u) cut--;
+        }
+        const float line = logit_of<T>(cut);
         long long left = 0;                     // of the ties that stay, those from this warp on
         if (part) {
             uint32_t ties = 0;
-            for (int i = 0; i < groups; i++) ties += own[32 * i] == cut;
+            for (int i = 0; i < groups; i++) ties += at_own(i) == line;
             u64 before;
             team.scan((u64)__reduce_add_sync(0xffffffffu, ties), before);
             left = room - (long long)before;
@@ -530,15 +562,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
         u64 mass = 0;
 #pragma unroll 2
         for (int i = 0; i < groups; i++) {
-            const uint32_t key = own[32 * i];
-            bool keep = key > cut;
+            const float l = at_own(i);
+            bool keep = l > line;
             if (part) {
-                const uint32_t g = __ballot_sync(0xffffffffu, key == cut);
-                keep = keep || (key == cut && (long long)__popc(g & ((1u << lane) - 1u)) < left);
+                const uint32_t g = __ballot_sync(0xffffffffu, l == line);
+                keep = keep || (l == line && (long long)__popc(g & ((1u << lane) - 1u)) < left);
                 left -= __popc(g);
             }
             if (keep) {
-                const float x = wt.weight(key);
+                const float x = wt.weight_at(l);
                 if (x >= mp) mass += Weigh<T>::quant(x);
             }
         }
@@ -558,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
             long long room_here = 0;
             if (part) {
                 uint32_t ties = 0;
-                for (int e = e0; e < e1; e++) ties += keys[e] == cut;
+                for (int e = e0; e < e1; e++) ties += value_of<T>(raw[e]) == line;
                 const u64 upto = upto_lane((u64)ties, lane);
                 u64 ahead_warps;
                 team.scan_block(__shfl_sync(0xffffffffu, upto, 31), ahead_warps);
@@ -567,9 +599,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
             auto each_kept = [&](auto use) {
                 long long r = room_here;
                 for (int e = e0; e < e1; e++) {
-                    const uint32_t key = keys[e];
-                    const bool keep = key > cut || (part && key == cut && r-- > 0);
-                    const float x = keep ? wt.weight(key) : 0.0f;
+                    const float l = value_of<T>(raw[e]);
+                    const bool keep = l > line || (part && l == line && r-- > 0);
+                    const float x = keep ? wt.weight_at(l) : 0.0f;
                     if (keep && x >= mp && use(e, x, Weigh<T>::quant(x))) return;
                 }
             };

@@ -50,7 +50,7 @@ struct Call {
             good = false;
             return nullptr;
         }
-        ld = n > 1 ? t.stride(0) : std::max<int64_t>(t.stride(0), m);
+        ld = n > 1 ? t.stride(0) : (m + 7) / 8 * 8;      // a single row may carry any stride
         return t.data_ptr();
     }
     void* rows(PyObject* o, int64_t n, int64_t m, long long& ld) {

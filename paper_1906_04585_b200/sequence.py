@@ -52,13 +52,13 @@ def _rows(name: str, t: Optional[torch.Tensor], shape, like: torch.Tensor):
     """Pointer and row stride of a matrix with contiguous columns (None: nothing)."""
     if t is None:
         return None, 0
-    if t.is_contiguous() and t.dtype is like.dtype and t.shape == shape and t.get_device() == like.get_device():
+    if t.is_contiguous() and t.dtype is like.dtype and t.shape == shape and t.get_device() == like.get_device() and shape[0] > 1:
         return t.data_ptr(), shape[1]
     _want(name, t, shape, like.dtype, like)
     if shape[1] > 1 and t.stride(1) != 1:
         raise ValueError("the columns of %s have to be contiguous" % name)
-    # a single row may carry any stride
-    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1])
+    # a single row may carry any stride: give it one that every operator takes
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else (shape[1] + 7) // 8 * 8
 
 
 def _flat(name: str, t: Optional[torch.Tensor], shape, dtype, like: torch.Tensor):
@@ -84,6 +84,8 @@ _status = {}
 def _status_word(t: torch.Tensor) -> int:
     index = t.get_device()
     if index not in _status:
+        if torch.cuda.is_current_stream_capturing():
+            return 0      # no word yet and no place to make one: this call goes without
         word = torch.zeros(1, dtype=torch.int32, device=t.device)
         torch.cuda.synchronize(index)      # streams that do not follow this one may use it next
         _status[index] = word, word.data_ptr()

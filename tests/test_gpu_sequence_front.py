@@ -81,3 +81,35 @@ def test_each_operator_follows_the_current_stream():
     side.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+def test_a_single_row_may_carry_any_stride():
+    wide = torch.randn(1, 45, device="cuda").bfloat16()
+    w = (torch.randn(24, 16, device="cuda") / 4).bfloat16()[:, :12]
+    wd = (torch.randn(12, 24, device="cuda") / 4).bfloat16()
+    x = wide[:, :12]
+    y, saved = S().gated_ffn(x, w, w, wd, save=True)
+    assert torch.equal(y, S().gated_ffn(x, w, w, wd)[0])
+    padded = torch.zeros(2, 16, device="cuda", dtype=torch.bfloat16)
+    padded[:1, :12] = x
+    assert torch.equal(y, S().gated_ffn(padded[:, :12], w, w, wd)[0][:1])
+    S().gated_ffn_backward(y, x, w, w, wd, saved)
+    assert torch.equal(S().layer_norm(x)[0], S().layer_norm(padded[:, :12])[0][:1])
+    assert int(S().sample(x, torch.zeros(1, device="cuda"))[0]) == 0
+
+
+def test_first_use_inside_a_capture():
+    """A process whose first call is captured: no word to report to is made there, and the graph replays."""
+    import subprocess
+    import sys
+    code = ("import torch\n"
+            "from paper_1906_04585_b200 import sequence as S\n"
+            "f = torch.randn(40, 2, 64, device='cuda'); x = torch.randn(40, 2, 64, device='cuda'); h = torch.zeros_like(x)\n"
+            "g = torch.cuda.CUDAGraph()\n"
+            "with torch.cuda.graph(g):\n"
+            "    S.gated_recurrence(f, x, out=h)\n"
+            "g.replay(); torch.cuda.synchronize()\n"
+            "assert torch.equal(h, S.gated_recurrence(f, x)[0])\n"
+            "S.check()\n")
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]

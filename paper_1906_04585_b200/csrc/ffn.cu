@@ -22,6 +22,10 @@
 // for y, 128 rows of Wd with the reduction cut over a cluster whose partial sums meet in distributed shared memory.
 //
 // Every mbarrier wait is bounded; one that runs out raises the caller's status word, and the kernel ends.
+//
+// Measured on a B200, kernels alone: 8192 rows, 2048 -> 8192 -> 2048, bfloat16, six products of a training pass 1.75-1.85 ms
+// (1.34-1.41 PFLOP/s; 2.1 ms back to back, where the power limit lowers the clock); 1024 rows forward 104 us; 7 rows 26 us
+// (3.9 TB/s of weights).
 #include <cooperative_groups.h>
 
 #include "sequence.cuh"

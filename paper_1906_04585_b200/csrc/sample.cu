@@ -21,6 +21,7 @@
 // filters 55 and 107 us (23 and 31 us without any).  Bound by instruction issue and, for clusters, by their barriers.
 #include <cooperative_groups.h>
 
+#include "sample_keys.h"
 #include "sequence.cuh"
 
 namespace gala {
@@ -29,33 +30,6 @@ namespace cg = cooperative_groups;
 constexpr int kMaxVocab = 262144;
 constexpr float kOne = 17592186044416.0f;   // 2^44
 typedef unsigned long long u64;
-
-// Key of a logit: unsigned order = order of the values, in as many bits as the type has.
-template <typename T> using Bits = typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type;
-template <typename T> constexpr int kKeyBits = 8 * (int)sizeof(T);
-template <typename T> constexpr uint32_t kInfinite = std::is_same<T, float>::value ? 0x7f800000u : std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
-template <typename T>
-__device__ __forceinline__ uint32_t key_of(uint32_t u) {       // from the stored bits
-    constexpr uint32_t sign = 1u << (kKeyBits<T> - 1), rest = sign - 1u;
-    if ((u & rest) > kInfinite<T>) u = sign | kInfinite<T>;    // NaN counts as -inf
-    if (u == sign) u = 0;                                      // -0 and +0 tie
-    return u & sign ? ~u & (sign | rest) : u | sign;
-}
-template <typename T>
-__device__ __forceinline__ float logit_of(uint32_t key) {
-    constexpr uint32_t sign = 1u << (kKeyBits<T> - 1), rest = sign - 1u;
-    const uint32_t u = key & sign ? key & rest : ~key & (sign | rest);
-    if (std::is_same<T, __nv_bfloat16>::value) return __uint_as_float(u << 16);
-    if (std::is_same<T, __half>::value) return __half2float(__ushort_as_half((unsigned short)u));
-    return __uint_as_float(u);
-}
-template <typename T>
-__device__ __forceinline__ float value_of(uint32_t u) {        // of the stored bits; NaN stays NaN
-    if (std::is_same<T, __nv_bfloat16>::value) return __uint_as_float(u << 16);
-    if (std::is_same<T, __half>::value) return __half2float(__ushort_as_half((unsigned short)u));
-    return __uint_as_float(u);
-}
-template <typename T> __device__ __forceinline__ uint32_t key_bottom() { return key_of<T>((1u << (kKeyBits<T> - 1)) | kInfinite<T>); }   // of -inf: keys above it can be drawn
 
 __device__ __forceinline__ u64 warp_sum(u64 v) {
     // 27 bits at a time: 32 of them fit the 32-bit sum
@@ -219,8 +193,6 @@ __global__ void __launch_bounds__(128) sample_warp_kernel(const gala_sample_args
 
 // ================================================================================== a block or a cluster a row
 constexpr int kThreads = 512;
-constexpr int kBins = 2048;
-constexpr float kFirstBins = 128.0f;      // bins of one unit of (m - l) / T in the first round
 
 struct Shared {
     int part[3][kBins];                   // sums of the weights' three parts (weigh), or counts: 2^15 entries of a block fit
@@ -474,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
                     return need = want(whole);
                 });
             if (whole < need) return false;
-            uint32_t lo = floor + 1, hi = top;
+            KeyRange<T> range = {floor + 1, top};
             if (b1 >= 0) {
                 // the keys of that bin, by bisection: a smaller key never has a smaller bin
                 uint32_t a = floor + 1, b = top;
@@ -483,26 +455,26 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
                     if (wt.step(m, kFirstBins, last) <= b1) b = m;
                     else a = m + 1;
                 }
-                lo = a;
+                range.lo = a;
                 b = top;
                 while (a < b) {                   // the largest key of the bin
                     const uint32_t m = a + (b - a + 1) / 2;
                     if (wt.step(m, kFirstBins, last) >= b1) a = m;
                     else b = m - 1;
                 }
-                hi = a;
+                range.hi = a;
             }
-            while (lo < hi) {
-                const int shift = max(0, 21 - __clz(hi - lo));
+            while (range.lo < range.hi) {
+                const int shift = range.shift();
                 const int b = team.round(
                     ahead, amount,
                     [&] {
-                        const float from = logit_of<T>(lo), to = logit_of<T>(hi);
+                        const float from = range.from(), to = range.to();
 #pragma unroll 4
                         for (int i = 0; i < groups; i++) {
                             const float x = at_own(i);
                             if (x >= from && x <= to) {
-                                const int b = (int)((hi - key_of<T>(own[32 * i])) >> shift);
+                                const int b = (int)range.bin(own[32 * i], shift);
                                 if (MASS) team.weigh(b, wt.weight_at(x));
                                 else team.count(b);
                             }
@@ -510,11 +482,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_row_kernel(const gala_samp
                     },
                     [&](u64) { return need; });
                 if (b < 0) break;      // does not happen: the range reaches what is wanted
-                hi -= (uint32_t)b << shift;
-                const uint32_t span = (1u << shift) - 1u;
-                if (hi - lo > span) lo = hi - span;
+                range.narrow(b, shift);
             }
-            key = hi;
+            key = range.hi;
             return true;
         };
         u64 ahead, amount;

@@ -21,6 +21,8 @@
 //
 // What a `done` flag cuts off must not leak through it (0 * inf), so A = -0.0f marks a map that does not depend on
 // its input: products keep the sign (A is never negative otherwise), and applying such a map selects B.
+// Nor may an infinite state turn into NaN: the map of a turn's first piece, which began at the known state, is never
+// applied but its B taken, and a product of positive gates that leaves float32's range is held at its smallest number.
 //
 // Measured on a B200: 2048 steps x 16 x 2048 bfloat16, forward 108 us (3.9 TB/s), backward 165 us (4.2 TB/s of what it has to
 // move); 65536 x 1 x 1024, forward 147 us (2.7 TB/s).  Bound by instruction issue, 31 and 54 instructions an element.
@@ -104,6 +106,27 @@ template <int V, bool DONE> __device__ __forceinline__ Maps<V> then(const Maps<V
         for (int v = 0; v < V; v++)
             if (__float_as_uint(m.a.v[v]) == 0x80000000u || __float_as_uint(n.a.v[v]) == 0x80000000u) r.a.v[v] = -0.0f;
     }
+    return r;
+}
+
+// Has a product of gates come out as zero (and not as the mark of a known state)?
+template <int V> __device__ __forceinline__ bool vanished(const Chan<V>& a) {
+    bool z = false;
+#pragma unroll
+    for (int v = 0; v < V; v++) z = z || __float_as_uint(a.v[v]) == 0u;
+    return z;
+}
+// If so, and its smallest factor is positive, float32's smallest number takes its place: 0 * inf would be NaN where every
+// step keeps the infinity.  What that adds to a finite state is below 1e-45 of it.
+template <int V> __device__ __forceinline__ void hold(Chan<V>& a, const Chan<V>& least) {
+#pragma unroll
+    for (int v = 0; v < V; v++)
+        if (__float_as_uint(a.v[v]) == 0u && least.v[v] > 0.0f) a.v[v] = __uint_as_float(1u);
+}
+template <int V> __device__ __forceinline__ Chan<V> smaller(const Chan<V>& a, const Chan<V>& b) {
+    Chan<V> r;
+#pragma unroll
+    for (int v = 0; v < V; v++) r.v[v] = fminf(a.v[v], b.v[v]);
     return r;
 }
 
@@ -210,12 +233,14 @@ __device__ __forceinline__ Chan<V> join(const Maps<V>& m, Chan<V>& carry, Meetin
     if (cluster == 1) {     // the state itself walks along the pieces
         auto along = [&](auto cuts_) {
             constexpr bool cuts = decltype(cuts_)::value;
-            Chan<V> c = carry;
+            Chan<V> c = sm.maps[par][0][lane].b;      // behind the first piece
 #pragma unroll 4
-            for (int k = 0; k < at; k++) c = apply<V, cuts>(sm.maps[par][k][lane], c);
+            for (int k = 1; k < at; k++) c = apply<V, cuts>(sm.maps[par][k][lane], c);
             enter = c;
+            if (at == 0) enter = carry;
+            else c = apply<V, cuts>(sm.maps[par][at][lane], c);
 #pragma unroll 4
-            for (int k = at; k < pieces; k++) c = apply<V, cuts>(sm.maps[par][k][lane], c);
+            for (int k = at + 1; k < pieces; k++) c = apply<V, cuts>(sm.maps[par][k][lane], c);
             carry = c;
         };
         if (DONE) {
@@ -232,16 +257,26 @@ __device__ __forceinline__ Chan<V> join(const Maps<V>& m, Chan<V>& carry, Meetin
     before.a = all_of<V>(1.0f);
     before.b = all_of<V>(0.0f);
     for (int k = 0; k < at; k++) before = then<V, DONE>(before, sm.maps[par][k][lane]);
+    if (vanished(before.a)) {
+        Chan<V> least = all_of<V>(1.0f);
+        for (int k = 0; k < at; k++) least = smaller(least, sm.maps[par][k][lane].a);
+        hold(before.a, least);
+    }
     if (at == pieces - 1) {
-        const Maps<V> all = then<V, DONE>(before, m);
+        Maps<V> all = then<V, DONE>(before, m);
+        hold(all.a, smaller(before.a, m.a));
         for (int r = 0; r < cluster; r++) send(there(&sm.slots[par][rank][lane], r), there(&sm.bar[par], r), all);
     }
     mbar_wait(&sm.bar[par], (uint32_t)(turn >> 1) & 1u, &sm.abort_flag);
-    Chan<V> c = carry;
-    for (int r = 0; r < rank; r++) c = apply<V, DONE>(sm.slots[par][r][lane], c);
-    enter = apply<V, DONE>(before, c);
+    Chan<V> c = sm.slots[par][0][lane].b;             // behind the first block, which has the first piece
+    if (rank == 0) {
+        enter = at ? before.b : carry;
+    } else {
+        for (int r = 1; r < rank; r++) c = apply<V, DONE>(sm.slots[par][r][lane], c);
+        enter = apply<V, DONE>(before, c);
+    }
 #pragma unroll 4
-    for (int r = rank; r < cluster; r++) c = apply<V, DONE>(sm.slots[par][r][lane], c);
+    for (int r = max(rank, 1); r < cluster; r++) c = apply<V, DONE>(sm.slots[par][r][lane], c);
     carry = c;
     return enter;
 }
@@ -335,7 +370,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const
             // the first piece of a turn knows its state: it walks from there instead of from zero (one rounding less where
             // the state and the first input cancel), and its map has nothing left to depend on
             Maps<V> m;
-            m.a = all_of<V>(place == 0 ? (DONE ? -0.0f : 0.0f) : 1.0f);
+            m.a = all_of<V>(place == 0 ? -0.0f : 1.0f);
             m.b = place == 0 ? carry : all_of<V>(0.0f);
             if (now) {
                 if (DONE && ends) {
@@ -352,6 +387,12 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_fwd_kernel(const
                     for (int i = 0; i < L; i++) {
                         m.b = madd(a[i], m.b, bx[i]);
                         m.a = mul(m.a, a[i]);      // keeps the mark of a known state, unless a is NaN and all is lost
+                    }
+                    if (vanished(m.a)) {
+                        Chan<V> least = a[0];
+#pragma unroll
+                        for (int i = 1; i < L; i++) least = smaller(least, a[i]);
+                        hold(m.a, least);
                     }
                 }
             }
@@ -459,7 +500,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
         Chan<V> q = carry;
         if (!SINGLE) {
             Maps<V> m;
-            m.a = all_of<V>(place == 0 ? (DONE ? -0.0f : 0.0f) : 1.0f);
+            m.a = all_of<V>(place == 0 ? -0.0f : 1.0f);
             m.b = place == 0 ? carry : all_of<V>(0.0f);
             if (now) {
                 if (now < L || (DONE && ends)) {
@@ -478,6 +519,12 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_bwd_kernel(const
                     for (int i = L - 1; i >= 0; i--) {
                         m.b = mul(a[i], add(gg[i], m.b));
                         m.a = mul(m.a, a[i]);
+                    }
+                    if (vanished(m.a)) {
+                        Chan<V> least = a[0];
+#pragma unroll
+                        for (int i = 1; i < L; i++) least = smaller(least, a[i]);
+                        hold(m.a, least);
                     }
                 }
             }

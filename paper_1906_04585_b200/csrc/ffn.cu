@@ -81,7 +81,7 @@ __device__ __forceinline__ void mbar_arrive_at(uint32_t bar) {
 template <int ACT> __device__ __forceinline__ float act_value(float g) {
     if (ACT == GALA_ACT_SILU) return __fdividef(g, 1.0f + __expf(-g));
     if (ACT == GALA_ACT_GELU) return 0.5f * g * (1.0f + erff(g * 0.70710678f));
-    return fmaxf(g, 0.0f);
+    return g < 0.0f ? 0.0f : g;       // a NaN goes on
 }
 // value and slope
 template <int ACT> __device__ __forceinline__ void act_both(float g, float& v, float& s) {
@@ -94,8 +94,8 @@ template <int ACT> __device__ __forceinline__ void act_both(float g, float& v, f
         v = g * phi;
         s = fmaf(g * 0.39894228f, __expf(-0.5f * g * g), phi);
     } else {
-        v = fmaxf(g, 0.0f);
-        s = g > 0.0f ? 1.0f : 0.0f;
+        v = g < 0.0f ? 0.0f : g;
+        s = g > 0.0f ? 1.0f : g <= 0.0f ? 0.0f : g;
     }
 }
 

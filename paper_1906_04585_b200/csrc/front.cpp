@@ -5,6 +5,7 @@
 // None for anything else - a wrong type or shape, a stride that needs thought, a refusal by the library - which the Python
 // code then says in words (refused calls enqueue nothing, so asking twice is safe).  No operator's work is done here.
 #include <Python.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ops/empty.h>
@@ -97,11 +98,12 @@ PyObject* four(PyObject* a, PyObject* b, PyObject* c, PyObject* d) {
     return t;
 }
 
+// What torch throws leaves as torch's own Python errors (out of memory among them).
 #define BEGIN try {
 #define END                                                                     \
     }                                                                           \
-    catch (const std::exception& e) {                                           \
-        PyErr_SetString(PyExc_RuntimeError, e.what());                          \
+    catch (...) {                                                               \
+        torch::translate_exception_to_python(std::current_exception());         \
         return nullptr;                                                         \
     }
 

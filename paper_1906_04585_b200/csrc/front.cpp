@@ -297,4 +297,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_front", nullptr, -1, methods, nul
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__front() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__front() {
+    PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "torch_version", GALA_TORCH_VERSION) < 0) Py_CLEAR(m);      // what it was compiled against
+    return m;
+}

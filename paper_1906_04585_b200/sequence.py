@@ -11,7 +11,9 @@ Tensors that other streams still use have to be ordered by the caller, as with a
 """
 from __future__ import annotations
 
-from typing import Optional, Tuple
+import importlib.util
+import warnings
+from typing import Optional
 
 import torch
 
@@ -21,13 +23,27 @@ _DTYPE = {torch.float32: B.GALA_F32, torch.bfloat16: B.GALA_BF16, torch.float16:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
+def _compiled():
+    """The compiled front end, or None.  One that is there and cannot be used is worth a word: calls on small tensors take
+    several times as long without it."""
+    try:
+        from . import _front
+    except ImportError as e:
+        if importlib.util.find_spec("._front", __package__) is not None:
+            warnings.warn("the compiled front end does not load (%s): calls go through Python" % e)
+        return None
+    made, here = getattr(_front, "torch_version", "another one"), str(torch.__version__)
+    if made != here:
+        warnings.warn("the compiled front end is for torch %s, this is %s: calls go through Python until it is built again" % (made, here))
+        return None
+    return _front
+
+
 # A call on small tensors is bound by the host.  The compiled front end (csrc/front.cpp) takes the forward calls whose
 # arguments are as they should be; it returns None for all others, and the code below says what is wrong with them, or
-# takes what only it can.  It is built with libgala.so; without it every call goes through the code below.
-try:
-    from . import _front
-except ImportError:
-    _front = None
+# takes what only it can.  It is built with libgala.so where torch's headers are; without it every call goes through the
+# code below.
+_front = _compiled()
 
 
 def _stream(t: torch.Tensor) -> int:

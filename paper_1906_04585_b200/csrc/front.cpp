@@ -28,6 +28,9 @@ int type_of(const Tensor& t) {
     }
 }
 
+// a size that the library takes as an int
+bool fits(int64_t n) { return n <= INT32_MAX; }
+
 // Arguments of one call.  `good` turns false at the first one that is not simple.
 struct Call {
     const Tensor& like;
@@ -117,6 +120,7 @@ PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g.dtype = type_of(x);
     if (!c.good || g.dtype < 0 || x.dim() != 2) Py_RETURN_NONE;
     const int64_t R = x.size(0), C = x.size(1);
+    if (!fits(C)) Py_RETURN_NONE;
     at::ScalarType wt = x.scalar_type();
     for (int i = 2; i > 0; i--)
         if (THPVariable_Check(a[i])) wt = THPVariable_Unpack(a[i]).scalar_type();
@@ -222,6 +226,7 @@ PyObject* gated_ffn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Tensor* wg = c.tensor(a[1], x.scalar_type());
     if (!wg || wg->dim() != 2) Py_RETURN_NONE;
     const int64_t R = x.size(0), D = x.size(1), F = wg->size(0);
+    if (!fits(D) || !fits(F)) Py_RETURN_NONE;
     g.act = (int)PyLong_AsLong(a[4]);
     g.status = static_cast<int*>(PyLong_AsVoidPtr(a[6]));
     if (PyErr_Occurred()) return nullptr;
@@ -258,6 +263,7 @@ PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g.dtype = type_of(l);
     if (!c.good || g.dtype < 0 || l.dim() != 2) Py_RETURN_NONE;
     const int64_t R = l.size(0), V = l.size(1);
+    if (!fits(V)) Py_RETURN_NONE;
     g.rows = R;
     g.vocab = (int)V;
     g.logits = c.rows(l, R, V, g.logits_ld);

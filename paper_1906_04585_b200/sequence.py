@@ -94,6 +94,13 @@ def _type_of(t: torch.Tensor) -> int:
         raise TypeError("%s: float32, bfloat16 or float16 is needed" % t.dtype) from None
 
 
+def _width(name: str, n: int) -> int:
+    """A size that the library takes as a C int (which ctypes would cut to its low bits)."""
+    if n >= 1 << 31:
+        raise ValueError("%s is %d: too large" % (name, n))
+    return n
+
+
 _status = {}
 
 
@@ -131,7 +138,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
         raise ValueError("x has to be a matrix [rows, cols]")
     a = B.gala_layer_norm_args()
     a.dtype, shape = _type_of(x), x.shape
-    a.rows, a.cols, a.eps = shape[0], shape[1], eps
+    a.rows, a.cols, a.eps = shape[0], _width("the number of columns", shape[1]), eps
     wdt = weight.dtype if weight is not None else bias.dtype if bias is not None else x.dtype
     a.wdtype = _DTYPE.get(wdt, -1)
     a.weight = _flat("weight", weight, shape[1:], wdt, x)
@@ -163,7 +170,7 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
         raise ValueError("x has to be a matrix [rows, cols]")
     a = B.gala_layer_norm_grad_args()
     a.dtype, shape = _type_of(x), x.shape
-    a.rows, a.cols = shape[0], shape[1]
+    a.rows, a.cols = shape[0], _width("the number of columns", shape[1])
     wdt = weight.dtype if weight is not None else torch.float32
     a.wdtype = _DTYPE.get(wdt, -1)
     dx = torch.empty(shape, dtype=x.dtype, device=x.device) if dx is None else dx
@@ -280,7 +287,7 @@ def _ffn_shapes(a, x, w_gate, w_up, w_down, act):
         a.act = _ACT[act]
     except KeyError:
         raise ValueError("activation %r: one of %s is needed" % (act, ", ".join(_ACT))) from None
-    a.dtype, a.rows, a.dim, a.hidden = _type_of(x), rows, dim, hidden
+    a.dtype, a.rows, a.dim, a.hidden = _type_of(x), rows, _width("dim", dim), _width("hidden", hidden)
     a.x, a.x_ld = _rows("x", x, (rows, dim), x)
     a.w_gate, a.w_gate_ld = _rows("w_gate", w_gate, (hidden, dim), x)
     a.w_up, a.w_up_ld = _rows("w_up", w_up, (hidden, dim), x)
@@ -357,7 +364,7 @@ def sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature: Optional[t
         raise ValueError("logits has to be a matrix [rows, vocab]")
     a = B.gala_sample_args()
     a.dtype, shape = _type_of(logits), logits.shape
-    a.rows, a.vocab = shape[0], shape[1]
+    a.rows, a.vocab = shape[0], _width("the number of entries", shape[1])
     tokens = torch.empty(shape[0], dtype=torch.int32, device=logits.device) if out is None else out
     logprobs = torch.empty(shape[0], dtype=torch.float32, device=logits.device) if logprobs is None else logprobs
     a.logits, a.logits_ld = _rows("logits", logits, shape, logits)

@@ -456,8 +456,9 @@ int gala_layer_norm_backward(const gala_layer_norm_grad_args* a, void* stream, c
  * done[t] has the meaning it has in gala_rollout (the episode ended at step t), so packed sequences are sequences with
  * flags between them; what a flag cuts off does not pass it, infinities and NaN included.  h_last = c_{steps-1}, which
  * is h0 of the next call; steps = 1 is the acting step, and h_last may be h0 itself.  h0 (= 0), done (= none),
- * h_last and states may be NULL.  Time strides are below 2^30.  states: what gala_gated_recurrence_backward needs, float32
- * [ceil(steps / 8)][batch][dim], c before every 8th step.  steps, batch, dim >= 0. */
+ * h_last and states may be NULL.  Time strides are below 2^30; the stride of an axis of one step or one sequence is not
+ * looked at.  states: what gala_gated_recurrence_backward needs, float32 [ceil(steps / 8)][batch][dim], c before every
+ * 8th step.  steps, batch, dim >= 0. */
 typedef struct {
     int dtype;                 /* f, x, h */
     long long steps, batch, dim;

@@ -664,7 +664,9 @@ using namespace gala;
 extern "C" int gala_gated_recurrence_forward(const gala_recurrence_args* p, void* stream, char* errbuf, int errbuf_len) {
     if (errbuf && errbuf_len > 0) errbuf[0] = 0;
     if (!p) SAY("gala_gated_recurrence_forward: null arguments");
-    const gala_recurrence_args& a = *p;
+    gala_recurrence_args a = *p;
+    if (a.steps == 1) a.f_t = a.x_t = a.h_t = a.done_t = 0;      // strides along an axis of one say nothing
+    if (a.batch == 1) a.f_b = a.x_b = a.h_b = a.done_b = 0;
     if (!dtype_ok(a.dtype)) SAY("gala_gated_recurrence_forward: dtype %d", a.dtype);
     if (a.steps < 0 || a.batch < 0 || a.dim < 0) SAY("gala_gated_recurrence_forward: negative size");
     if (a.steps > (1ll << 34) || too_many(a.batch, a.dim)) SAY("gala_gated_recurrence_forward: sizes out of range");
@@ -687,7 +689,9 @@ extern "C" int gala_gated_recurrence_forward(const gala_recurrence_args* p, void
 extern "C" int gala_gated_recurrence_backward(const gala_recurrence_grad_args* p, void* stream, char* errbuf, int errbuf_len) {
     if (errbuf && errbuf_len > 0) errbuf[0] = 0;
     if (!p) SAY("gala_gated_recurrence_backward: null arguments");
-    const gala_recurrence_grad_args& a = *p;
+    gala_recurrence_grad_args a = *p;
+    if (a.steps == 1) a.f_t = a.x_t = a.dh_t = a.df_t = a.dx_t = a.done_t = 0;      // strides along an axis of one say nothing
+    if (a.batch == 1) a.f_b = a.x_b = a.dh_b = a.df_b = a.dx_b = a.done_b = 0;
     if (!dtype_ok(a.dtype)) SAY("gala_gated_recurrence_backward: dtype %d", a.dtype);
     if (a.steps < 0 || a.batch < 0 || a.dim < 0) SAY("gala_gated_recurrence_backward: negative size");
     if (a.steps > (1ll << 34) || too_many(a.batch, a.dim)) SAY("gala_gated_recurrence_backward: sizes out of range");

@@ -427,6 +427,7 @@ int gala_layer_norm_forward(const gala_layer_norm_args* a, void* stream, char* e
 
 /* Its gradient.  x: what was normalised (s); xh = (x - mean) rstd, e = dy weight:
  *   dx = rstd (e - mean e - xh mean(e xh)) + dsum      dweight = sum over rows of dy xh      dbias = sum over rows of dy
+ * With a residual in 16 bits x is s as stored, rounded, while mean and rstd are those of s before rounding.
  * dsum (the gradient that reaches s by another path), weight, dx, dweight and dbias may be NULL.  The sums over rows
  * have a fixed order: the same call gives the same bits.  dx may be dy itself or dsum itself.  The workspace
  * (16-byte aligned) is needed for dweight / dbias only. */
@@ -525,10 +526,11 @@ int gala_sample(const gala_sample_args* a, void* stream, char* errbuf, int errbu
  *   g = x w_gate^T    u = x w_up^T    p = act(g) u    y = p w_down^T
  * x, y [rows][dim], w_gate, w_up [hidden][dim], w_down [dim][hidden]; products are accumulated in float32.  Both
  * projections, the activation and the product are one kernel; p is rounded once to the element type, being an operand
- * of the next product.  `product` [rows][hidden_ld] receives p.  With gate and up (both or neither) g and u are stored as
- * well, rounded, for the backward call.  act: GALA_ACT_SILU g sigmoid(g), GALA_ACT_GELU g Phi(g) (the exact form),
- * GALA_ACT_RELU max(g, 0).  Rows of every matrix start on 16-byte boundaries (pointers 16-byte aligned, strides multiples
- * of 8); sizes are free: 0 <= rows < 2^31 - 256, 1 <= dim, hidden <= 2^20. */
+ * of the next product (float16: infinite beyond 65504; so are dg and du below).  `product` [rows][hidden_ld] receives p.
+ * With gate and up (both or neither) g and u are stored as well, rounded, for the backward call.  act: GALA_ACT_SILU
+ * g sigmoid(g), GALA_ACT_GELU g Phi(g) (the exact form), GALA_ACT_RELU max(g, 0), a NaN staying one.  Rows of every matrix
+ * start on 16-byte boundaries (pointers 16-byte aligned, strides multiples of 8); sizes are free: 0 <= rows < 2^31 - 256,
+ * 1 <= dim, hidden <= 2^20. */
 typedef enum { GALA_ACT_SILU = 0, GALA_ACT_GELU = 1, GALA_ACT_RELU = 2 } gala_act_kind;
 typedef struct {
     int dtype, act;

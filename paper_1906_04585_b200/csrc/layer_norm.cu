@@ -14,7 +14,8 @@
 // fixed order.
 //
 // Measured on a B200: 16384 x 2048 bfloat16 with float32 weights, forward 35 us (3.8 TB/s), backward 43-47 us (4.5 TB/s) and
-// 3-4 us for the columns' sums; a plain copy reaches 6.55 TB/s.  Both kernels are bound by instruction issue.
+// 3-4 us for the columns' sums; a plain copy reaches 6.55 TB/s.  Both kernels are bound by instruction issue.  Wider rows
+// cost more: 4096 x 8192 forward 52-58 us, with the backward pass 112-119; 2048 x 16384 44-50 and 164-189.
 #include "sequence.cuh"
 
 namespace gala {
@@ -139,7 +140,10 @@ __device__ __forceinline__ void store_part(T* p, int have, const float (&f)[V]) 
     }
 }
 
-// Blocks of an SM, by the registers that a block needs without spilling, and the ring that fits beside the others.
+// Blocks of an SM, and the ring that fits beside the others.  In blocks of 256 threads that leaves a thread 80 registers (16-byte
+// pieces: no spills but for all-float16 rows, 40 bytes at most) or 128 (single elements: up to 104 bytes of spills).  Rows
+// of more than 4096 columns have blocks of 512 or 1024 threads with 64 registers, which spill 4 to 424 bytes, and a ring
+// sized for 1024; the backward form for more than 8192 columns has 64 registers too and spills 176 to 400.
 template <int V, int MAXT> constexpr int kFwdBlocks = MAXT > 256 ? 1 : V > 1 ? 3 : 2;
 template <typename T, int V, int MAXT, bool RES>
 constexpr int kFwdSlots = kRingRows<MAXT, sizeof(T), RES ? 2 : 1, 200 * 1024 / kFwdBlocks<V, MAXT>, 6>;

@@ -24,8 +24,9 @@
 // Nor may an infinite state turn into NaN: the map of a turn's first piece, which began at the known state, is never
 // applied but its B taken, and a product of positive gates that leaves float32's range is held at its smallest number.
 //
-// Measured on a B200: 2048 steps x 16 x 2048 bfloat16, forward 108 us (3.9 TB/s), backward 165 us (4.2 TB/s of what it has to
-// move); 65536 x 1 x 1024, forward 147 us (2.7 TB/s).  Bound by instruction issue, 31 and 54 instructions an element.
+// Measured on a B200: 2048 steps x 16 x 2048 bfloat16, forward 110 us (3.8 TB/s), backward 164 us (4.2 TB/s of what it has to
+// move); 65536 x 1 x 1024, forward 147 us (2.7 TB/s).  Bound by instruction issue, 31 and 49 instructions an element, and the
+// long sequence by the chain of a turn (IPC 1.7, the next turn's loads and the other blocks' maps are waited for).
 #include "sequence.cuh"
 #include "tcgen05.cuh"
 
@@ -37,9 +38,9 @@ constexpr int kMaxWarps = 8;
 constexpr int kMaxCluster = 8;
 
 // a = sigmoid(f) and b = 1 - a.  The smaller of the two is e / (1 + e) with e = exp(-|f|) (approximate exponential and
-// reciprocal: a few units in its last place), the larger is 1 minus it, rounded once: neither a long memory (b small,
-// where an error of a in its last places would add up over 1 / b steps) nor a memory wiped by the gate (a small) loses
-// digits.
+// reciprocal, and the rounding of its argument: within about 4 + 2 |f| units of 2^-24 of itself; 0 past |f| = 87), the
+// larger is 1 minus it, rounded once: neither a long memory (b small, where an error of a in its last places would add up
+// over 1 / b steps) nor a memory wiped by the gate (a small) loses its leading digits.
 __device__ __forceinline__ void gate(float f, float& a, float& b) {
     float e, r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(f) * -1.4426950408889634f));

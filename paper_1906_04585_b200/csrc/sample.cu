@@ -633,7 +633,10 @@ cudaError_t pick(const gala_sample_args& a, cudaStream_t st) {
     const int v = a.vocab;
     if (v <= 32) return launch_pdl(sample_warp_kernel<T, 1>, dim3((unsigned)((a.rows + 3) / 4)), dim3(128), 0, st, a);
     if (v <= 256) return launch_pdl(sample_warp_kernel<T, 8>, dim3((unsigned)((a.rows + 3) / 4)), dim3(128), 0, st, a);
-    // blocks of a row: as many as keep a block's part within 64 KB (three blocks an SM), and more where rows are few
+    // Blocks of a row: as many as keep a block's part within 64 KB, and more where rows are few.  Two blocks fit an SM up to 88
+    // KB (24.7 KB of bins and 64 registers beside it).  One block for the parts between is faster where rows fill the device
+    // (1024 x 40000 bfloat16, filtered: 158 us against 207 with two) and slower where they do not (148 x 44000 float16: 63-73
+    // against 57).
     int ranks = 1;
     while (ranks < 8 && ((long long)v * (int)sizeof(T) > 65536ll * ranks || (a.rows * ranks * 2 <= sm_count() && v > 8192 * ranks))) ranks *= 2;
     const int part = (v + ranks - 1) / ranks;

@@ -7,6 +7,9 @@ bfloat16 and float16 (the feed-forward block: the 16-bit ones); states, statisti
 `out`-like arguments receive results in place; without them results are new tensors.  What a call may not do raises
 GalaError (from the library) or TypeError / ValueError (from here) before anything is enqueued.
 
+No call takes part in autograd: tensors that require gradients are read as they are, and results have no history.  The
+backward passes are calls of their own.
+
 Tensors that other streams still use have to be ordered by the caller, as with any torch operation.
 """
 from __future__ import annotations
@@ -117,7 +120,8 @@ def _status_word(t: torch.Tensor) -> int:
 
 def check() -> None:
     """Waits for the current stream and raises if a bounded wait inside a kernel of this module ran out since the last
-    check (results since then are not to be trusted); the word is cleared."""
+    check (results since then are not to be trusted); the word is cleared.  Calls that were captured into a graph before
+    the process's first call outside of one have no word to report to."""
     for word, _ in _status.values():
         if int(word.item()):
             word.zero_()

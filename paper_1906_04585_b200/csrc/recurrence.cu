@@ -24,9 +24,9 @@
 // Nor may an infinite state turn into NaN: the map of a turn's first piece, which began at the known state, is never
 // applied but its B taken, and a product of positive gates that leaves float32's range is held at its smallest number.
 //
-// Measured on a B200: 2048 steps x 16 x 2048 bfloat16, forward 110 us (3.8 TB/s), backward 164 us (4.2 TB/s of what it has to
-// move); 65536 x 1 x 1024, forward 147 us (2.7 TB/s).  Bound by instruction issue, 31 and 49 instructions an element, and the
-// long sequence by the chain of a turn (IPC 1.7, the next turn's loads and the other blocks' maps are waited for).
+// Measured on a B200: 2048 steps x 16 x 2048 bfloat16, forward 108 us (3.9 TB/s), backward 164 us (4.2 TB/s of what it has to
+// move); 65536 x 1 x 1024, forward 116 us (3.5 TB/s).  Bound by instruction issue, 30 and 49 instructions an element, and the
+// long sequence by the chain of a turn as well (IPC 2.1: the next turn's loads and the other blocks' maps are waited for).
 #include "sequence.cuh"
 #include "tcgen05.cuh"
 
@@ -235,13 +235,14 @@ __device__ __forceinline__ Chan<V> join(const Maps<V>& m, Chan<V>& carry, Meetin
         auto along = [&](auto cuts_) {
             constexpr bool cuts = decltype(cuts_)::value;
             Chan<V> c = sm.maps[par][0][lane].b;      // behind the first piece
-#pragma unroll 4
-            for (int k = 1; k < at; k++) c = apply<V, cuts>(sm.maps[par][k][lane], c);
-            enter = c;
-            if (at == 0) enter = carry;
-            else c = apply<V, cuts>(sm.maps[par][at][lane], c);
-#pragma unroll 4
-            for (int k = at + 1; k < pieces; k++) c = apply<V, cuts>(sm.maps[par][k][lane], c);
+            enter = carry;
+            // (one loop for all warps: as two, up to the own piece and from it on, it cost up to 10 % more or less from one
+            // form of the kernel to the next; unrolled, 150 -> 175 us at 65536 x 1 x 1024 bfloat16 with flags)
+#pragma unroll 1
+            for (int k = 1; k < pieces; k++) {
+                if (k == at) enter = c;
+                c = apply<V, cuts>(sm.maps[par][k][lane], c);
+            }
             carry = c;
         };
         if (DONE) {
@@ -574,7 +575,7 @@ namespace {
 
 // How the time axis is cut.  A block takes turns along it, with the next turn's loads under way.  Where units are few,
 // blocks are set side by side along it until the device is full (264 blocks of 256 threads in clusters of eight fit 148 SMs;
-// one more would be a second wave: 65536 x 1 x 1056 bfloat16, 33 units, 158 us with clusters of eight, 244 with four), and
+// one more would be a second wave: 65536 x 1 x 1056 bfloat16, 33 units, 116 us with clusters of eight, 182 with four), and
 // two pieces share a warp, which halves a unit's channels.
 RecurrenceGrid plan(long long steps, long long batch, long long dim, int lanes, int subs, int piece) {
     RecurrenceGrid g;

@@ -577,6 +577,137 @@ typedef struct {
 } gala_ffn_grad_args;
 int gala_gated_ffn_backward(const gala_ffn_grad_args* a, void* stream, char* errbuf, int errbuf_len);
 
+/* Attention with a memory of fixed size: per sequence b and head h a matrix S [dk][dv] in float32 that fades by
+ * g = exp(log_decay[h]) a step (a log_decay above 0 counts as 0; -inf: nothing is kept):
+ *   S_t = g C_{t-1} + k_t v_t^T     o_t = scale S_t^T q_t     C_t = 0 where done_t, else S_t     C_{-1} = s0
+ * done has the meaning it has in gala_gated_recurrence_forward; what a flag cuts off does not pass it, infinities and NaN
+ * included.  s_last = C_{steps-1} is s0 of the next call; steps = 1 is the acting step, and s_last may be s0 itself.
+ * q, k, v and o have any strides for time, sequence and head, channels contiguous; strides are not negative, below 2^30 in
+ * time, and those of an axis of one entry are not looked at; q, k and v may have strides of 0 (one key for all heads).
+ * s0 (= 0), done (= none) and s_last may be NULL.  1 <= dk, dv <= 128; steps, batch, heads >= 0, batch x heads < 2^27.
+ * Long calls in 16 bits run on the tensor cores in chunks of 128 steps where pointers are 16-byte aligned and strides multiples
+ * of 8; all others step by step.  The workspace is 16-byte aligned; gala_linear_attention_workspace gives its size for the
+ * forward and for the backward call. */
+typedef struct {
+    int dtype;                 /* q, k, v, o */
+    int heads, dk, dv;
+    long long steps, batch;
+    float scale;
+    const void* q;             long long q_t, q_b, q_h;   /* strides of time, sequence and head */
+    const void* k;             long long k_t, k_b, k_h;
+    const void* v;             long long v_t, v_b, v_h;
+    const float* log_decay;    /* [heads] */
+    const unsigned char* done; long long done_t, done_b;
+    const float* s0;           /* [batch][heads][dk][dv] */
+    void* o;                   long long o_t, o_b, o_h;
+    float* s_last;             /* [batch][heads][dk][dv] */
+    void* workspace;           long long workspace_bytes;
+    int* status;
+} gala_linear_attention_args;
+long long gala_linear_attention_workspace(long long steps, long long batch, int heads, int dk, int dv);
+int gala_linear_attention_forward(const gala_linear_attention_args* a, void* stream, char* errbuf, int errbuf_len);
+
+/* Its gradient.  With R_t = scale q_t do_t^T + (not done_t) g R_{t+1} and g R_steps = ds_last:
+ *   dq_t = scale S_t do_t     dk_t = R_t v_t     dv_t = R_t^T k_t     ds0 = g R_0
+ * s0 is the forward call's.  s0 (= 0), done, ds_last (= 0), ds0 and any of dq, dk, dv may be NULL. */
+typedef struct {
+    int dtype;                 /* grad_o, q, k, v, dq, dk, dv */
+    int heads, dk, dv;
+    long long steps, batch;
+    float scale;
+    const void* q;             long long q_t, q_b, q_h;
+    const void* k;             long long k_t, k_b, k_h;
+    const void* v;             long long v_t, v_b, v_h;
+    const float* log_decay;
+    const unsigned char* done; long long done_t, done_b;
+    const float* s0;
+    const void* grad_o;        long long grad_o_t, grad_o_b, grad_o_h;
+    const float* grad_s_last;  /* [batch][heads][dk][dv] */
+    void* grad_q;              long long grad_q_t, grad_q_b, grad_q_h;
+    void* grad_k;              long long grad_k_t, grad_k_b, grad_k_h;
+    void* grad_v;              long long grad_v_t, grad_v_b, grad_v_h;
+    float* grad_s0;            /* [batch][heads][dk][dv] */
+    void* workspace;           long long workspace_bytes;
+    int* status;
+} gala_linear_attention_grad_args;
+int gala_linear_attention_backward(const gala_linear_attention_grad_args* a, void* stream, char* errbuf, int errbuf_len);
+
+/* Queries and keys normed by head and turned by position, in one pass.  For each token and head x [dim]:
+ *   y = x / sqrt(mean x^2 + eps) * weight
+ * and of y the first 2 pairs entries are turned: pair i, (y_i, y_{pairs+i}) or with `interleaved` (y_2i, y_2i+1), becomes
+ * (a cos f - b sin f, b cos f + a sin f) with f = positions[token] * inv_freq[i], formed in 64 bits.  Entries beyond stay.
+ * q [tokens][q_heads][dim] and k [tokens][k_heads][dim] have any strides for token and head, entries contiguous; q_out and
+ * k_out may be q and k themselves (same pointer and strides).  weights (= 1) may be NULL.  1 <= dim <= 256,
+ * 0 <= pairs <= dim / 2; tokens >= 0, 0 <= heads <= 2^16. */
+typedef struct {
+    int dtype, wdtype;         /* wdtype of the weights: GALA_F32 or dtype */
+    int q_heads, k_heads, dim, pairs, interleaved;
+    float eps;                 /* >= 0 */
+    long long tokens;
+    const void* q;             long long q_t, q_h;
+    const void* k;             long long k_t, k_h;
+    const int* positions;      /* [tokens] */
+    const float* inv_freq;     /* [pairs] */
+    const void* q_weight;      /* [dim] */
+    const void* k_weight;
+    void* q_out;               long long q_out_t, q_out_h;
+    void* k_out;               long long k_out_t, k_out_h;
+} gala_qk_norm_rotary_args;
+int gala_qk_norm_rotary_forward(const gala_qk_norm_rotary_args* a, void* stream, char* errbuf, int errbuf_len);
+
+/* Its gradient, from grad_q_out and grad_k_out.  With e = the gradient turned back, r = 1 / sqrt(mean x^2 + eps), xh = x r:
+ *   dx = r (e weight - xh mean(e weight xh))     dweight = sum over tokens and heads of e xh
+ * q and k are the forward call's inputs.  The sums have a fixed order: the same call gives the same bits.  grad_q may be
+ * grad_q_out itself, grad_k grad_k_out.  Weights and their gradients may be NULL; the workspace (16-byte aligned) is needed for
+ * the weights' gradients only. */
+typedef struct {
+    int dtype, wdtype;
+    int q_heads, k_heads, dim, pairs, interleaved;
+    float eps;
+    long long tokens;
+    const void* q;             long long q_t, q_h;
+    const void* k;             long long k_t, k_h;
+    const int* positions;
+    const float* inv_freq;
+    const void* q_weight;
+    const void* k_weight;
+    const void* grad_q_out;    long long grad_q_out_t, grad_q_out_h;
+    const void* grad_k_out;    long long grad_k_out_t, grad_k_out_h;
+    void* grad_q;              long long grad_q_t, grad_q_h;
+    void* grad_k;              long long grad_k_t, grad_k_h;
+    void* grad_q_weight;       /* [dim] */
+    void* grad_k_weight;
+    void* workspace;           long long workspace_bytes;
+} gala_qk_norm_rotary_grad_args;
+long long gala_qk_norm_rotary_workspace(long long tokens, int dim);
+int gala_qk_norm_rotary_backward(const gala_qk_norm_rotary_grad_args* a, void* stream, char* errbuf, int errbuf_len);
+
+/* Logits before a draw.  Row r, entry i, with c how often i stands among the first lengths[r] tokens of history[r] (ids
+ * outside 0..vocab-1 count nowhere) and b the sum of the bias_values of r listed for i:
+ *   l = logits[r][i]
+ *   if c > 0:  l = l / repetition[r] where l > 0, else l * repetition[r];   l = l - frequency[r] c - presence[r]
+ *   l = l + b (where i is listed);   l = -inf where bit i % 32 of mask[r][i / 32] is 0
+ * rounded once to the element type.  history, its settings (repetition = 1, frequency = presence = 0), lengths (= width),
+ * the bias list and mask may be NULL.  Duplicates in the bias list are added up in its order; ids outside count nowhere.
+ * mask_ld = 0: one mask for all rows.  out may be logits itself (same pointer and stride).  1 <= vocab <= 2^30,
+ * 0 <= rows < 2^27, 0 <= width < 2^20, 0 <= biases < 4096. */
+typedef struct {
+    int dtype;                 /* logits, out */
+    int vocab, width, biases;
+    long long rows;
+    const void* logits;        long long logits_ld;
+    const int* history;        long long history_ld;      /* [rows][width] */
+    const int* lengths;        /* [rows] */
+    const float* repetition;   /* [rows], > 0 */
+    const float* frequency;
+    const float* presence;
+    const int* bias_ids;       long long bias_ids_ld;     /* [rows][biases] */
+    const float* bias_values;  long long bias_values_ld;
+    const int* mask;           long long mask_ld;         /* [rows][ceil(vocab / 32)] */
+    void* out;                 long long out_ld;
+} gala_adjust_logits_args;
+int gala_adjust_logits(const gala_adjust_logits_args* a, void* stream, char* errbuf, int errbuf_len);
+
 #ifdef __cplusplus
 }
 #endif

@@ -122,6 +122,63 @@ class gala_ffn_grad_args(C.Structure):
                 ("status", C.c_void_p)]
 
 
+class gala_linear_attention_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("heads", C.c_int), ("dk", C.c_int), ("dv", C.c_int), ("steps", C.c_longlong),
+                ("batch", C.c_longlong), ("scale", C.c_float), ("q", C.c_void_p), ("q_t", C.c_longlong),
+                ("q_b", C.c_longlong), ("q_h", C.c_longlong), ("k", C.c_void_p), ("k_t", C.c_longlong),
+                ("k_b", C.c_longlong), ("k_h", C.c_longlong), ("v", C.c_void_p), ("v_t", C.c_longlong),
+                ("v_b", C.c_longlong), ("v_h", C.c_longlong), ("log_decay", C.c_void_p), ("done", C.c_void_p),
+                ("done_t", C.c_longlong), ("done_b", C.c_longlong), ("s0", C.c_void_p), ("o", C.c_void_p),
+                ("o_t", C.c_longlong), ("o_b", C.c_longlong), ("o_h", C.c_longlong), ("s_last", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_longlong), ("status", C.c_void_p)]
+
+
+class gala_linear_attention_grad_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("heads", C.c_int), ("dk", C.c_int), ("dv", C.c_int), ("steps", C.c_longlong),
+                ("batch", C.c_longlong), ("scale", C.c_float), ("q", C.c_void_p), ("q_t", C.c_longlong),
+                ("q_b", C.c_longlong), ("q_h", C.c_longlong), ("k", C.c_void_p), ("k_t", C.c_longlong),
+                ("k_b", C.c_longlong), ("k_h", C.c_longlong), ("v", C.c_void_p), ("v_t", C.c_longlong),
+                ("v_b", C.c_longlong), ("v_h", C.c_longlong), ("log_decay", C.c_void_p), ("done", C.c_void_p),
+                ("done_t", C.c_longlong), ("done_b", C.c_longlong), ("s0", C.c_void_p), ("grad_o", C.c_void_p),
+                ("grad_o_t", C.c_longlong), ("grad_o_b", C.c_longlong), ("grad_o_h", C.c_longlong),
+                ("grad_s_last", C.c_void_p), ("grad_q", C.c_void_p), ("grad_q_t", C.c_longlong), ("grad_q_b", C.c_longlong),
+                ("grad_q_h", C.c_longlong), ("grad_k", C.c_void_p), ("grad_k_t", C.c_longlong), ("grad_k_b", C.c_longlong),
+                ("grad_k_h", C.c_longlong), ("grad_v", C.c_void_p), ("grad_v_t", C.c_longlong), ("grad_v_b", C.c_longlong),
+                ("grad_v_h", C.c_longlong), ("grad_s0", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_longlong), ("status", C.c_void_p)]
+
+
+class gala_qk_norm_rotary_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("wdtype", C.c_int), ("q_heads", C.c_int), ("k_heads", C.c_int), ("dim", C.c_int),
+                ("pairs", C.c_int), ("interleaved", C.c_int), ("eps", C.c_float), ("tokens", C.c_longlong),
+                ("q", C.c_void_p), ("q_t", C.c_longlong), ("q_h", C.c_longlong), ("k", C.c_void_p), ("k_t", C.c_longlong),
+                ("k_h", C.c_longlong), ("positions", C.c_void_p), ("inv_freq", C.c_void_p), ("q_weight", C.c_void_p),
+                ("k_weight", C.c_void_p), ("q_out", C.c_void_p), ("q_out_t", C.c_longlong), ("q_out_h", C.c_longlong),
+                ("k_out", C.c_void_p), ("k_out_t", C.c_longlong), ("k_out_h", C.c_longlong)]
+
+
+class gala_qk_norm_rotary_grad_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("wdtype", C.c_int), ("q_heads", C.c_int), ("k_heads", C.c_int), ("dim", C.c_int),
+                ("pairs", C.c_int), ("interleaved", C.c_int), ("eps", C.c_float), ("tokens", C.c_longlong),
+                ("q", C.c_void_p), ("q_t", C.c_longlong), ("q_h", C.c_longlong), ("k", C.c_void_p), ("k_t", C.c_longlong),
+                ("k_h", C.c_longlong), ("positions", C.c_void_p), ("inv_freq", C.c_void_p), ("q_weight", C.c_void_p),
+                ("k_weight", C.c_void_p), ("grad_q_out", C.c_void_p), ("grad_q_out_t", C.c_longlong),
+                ("grad_q_out_h", C.c_longlong), ("grad_k_out", C.c_void_p), ("grad_k_out_t", C.c_longlong),
+                ("grad_k_out_h", C.c_longlong), ("grad_q", C.c_void_p), ("grad_q_t", C.c_longlong),
+                ("grad_q_h", C.c_longlong), ("grad_k", C.c_void_p), ("grad_k_t", C.c_longlong), ("grad_k_h", C.c_longlong),
+                ("grad_q_weight", C.c_void_p), ("grad_k_weight", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_longlong)]
+
+
+class gala_adjust_logits_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("vocab", C.c_int), ("width", C.c_int), ("biases", C.c_int), ("rows", C.c_longlong),
+                ("logits", C.c_void_p), ("logits_ld", C.c_longlong), ("history", C.c_void_p), ("history_ld", C.c_longlong),
+                ("lengths", C.c_void_p), ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p),
+                ("bias_ids", C.c_void_p), ("bias_ids_ld", C.c_longlong), ("bias_values", C.c_void_p),
+                ("bias_values_ld", C.c_longlong), ("mask", C.c_void_p), ("mask_ld", C.c_longlong), ("out", C.c_void_p),
+                ("out_ld", C.c_longlong)]
+
+
 EXPORTS = (
     "gala_create", "gala_destroy", "gala_act", "gala_learn", "gala_gossip", "gala_step_sync",
     "gala_sync_agent", "gala_sync_all", "gala_in_peers", "gala_get_state", "gala_set_state",
@@ -137,6 +194,8 @@ EXPORTS = (
     "gala_layer_norm_forward", "gala_layer_norm_backward", "gala_layer_norm_workspace",
     "gala_gated_recurrence_forward", "gala_gated_recurrence_backward",
     "gala_sample", "gala_gated_ffn_forward", "gala_gated_ffn_backward",
+    "gala_linear_attention_forward", "gala_linear_attention_backward", "gala_linear_attention_workspace",
+    "gala_qk_norm_rotary_forward", "gala_qk_norm_rotary_backward", "gala_qk_norm_rotary_workspace", "gala_adjust_logits",
 )
 
 _lib = None
@@ -208,6 +267,13 @@ def lib() -> C.CDLL:
             "gala_sample": (i, [C.POINTER(gala_sample_args), vp, C.c_char_p, i]),
             "gala_gated_ffn_forward": (i, [C.POINTER(gala_ffn_args), vp, C.c_char_p, i]),
             "gala_gated_ffn_backward": (i, [C.POINTER(gala_ffn_grad_args), vp, C.c_char_p, i]),
+            "gala_linear_attention_forward": (i, [C.POINTER(gala_linear_attention_args), vp, C.c_char_p, i]),
+            "gala_linear_attention_backward": (i, [C.POINTER(gala_linear_attention_grad_args), vp, C.c_char_p, i]),
+            "gala_linear_attention_workspace": (ll, [ll, ll, i, i, i]),
+            "gala_qk_norm_rotary_forward": (i, [C.POINTER(gala_qk_norm_rotary_args), vp, C.c_char_p, i]),
+            "gala_qk_norm_rotary_backward": (i, [C.POINTER(gala_qk_norm_rotary_grad_args), vp, C.c_char_p, i]),
+            "gala_qk_norm_rotary_workspace": (ll, [ll, i]),
+            "gala_adjust_logits": (i, [C.POINTER(gala_adjust_logits_args), vp, C.c_char_p, i]),
             "gala_sweep_sync": (i, [vp, vp, vp, vp, i, ll, C.POINTER(gala_topology), ll, C.POINTER(gala_hparams), vp]),
         }
         for name, (res, args) in sig.items():
@@ -554,6 +620,40 @@ def gala_gated_ffn_forward(args: gala_ffn_args, stream=None):
 
 def gala_gated_ffn_backward(args: gala_ffn_grad_args, stream=None):
     _operator("gala_gated_ffn_backward", args, stream)
+
+
+def gala_linear_attention_forward(args: gala_linear_attention_args, stream=None):
+    _operator("gala_linear_attention_forward", args, stream)
+
+
+def gala_linear_attention_backward(args: gala_linear_attention_grad_args, stream=None):
+    _operator("gala_linear_attention_backward", args, stream)
+
+
+def gala_linear_attention_workspace(steps: int, batch: int, heads: int, dk: int, dv: int) -> int:
+    n = lib().gala_linear_attention_workspace(steps, batch, heads, dk, dv)
+    if n < 0:
+        raise GalaError(n, "gala_linear_attention_workspace: %d steps, %d sequences, %d heads of %d and %d entries" % (steps, batch, heads, dk, dv))
+    return n
+
+
+def gala_qk_norm_rotary_forward(args: gala_qk_norm_rotary_args, stream=None):
+    _operator("gala_qk_norm_rotary_forward", args, stream)
+
+
+def gala_qk_norm_rotary_backward(args: gala_qk_norm_rotary_grad_args, stream=None):
+    _operator("gala_qk_norm_rotary_backward", args, stream)
+
+
+def gala_qk_norm_rotary_workspace(tokens: int, dim: int) -> int:
+    n = lib().gala_qk_norm_rotary_workspace(tokens, dim)
+    if n < 0:
+        raise GalaError(n, "gala_qk_norm_rotary_workspace: %d tokens, heads of %d entries" % (tokens, dim))
+    return n
+
+
+def gala_adjust_logits(args: gala_adjust_logits_args, stream=None):
+    _operator("gala_adjust_logits", args, stream)
 
 
 def default_hparams(n_envs: int, n_steps: int, **kw) -> gala_hparams:

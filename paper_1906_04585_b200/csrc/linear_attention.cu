@@ -1,0 +1,480 @@
+// Attention with a memory of fixed size, step by step, and the C entry points, for sm_100a.
+//
+// memory_steps_kernel holds the state of a sequence and head in registers: a thread has one column of it (an entry of v and
+// o) for all rows (entries of q and k), two rows a packed instruction, so that o needs no exchange between threads.  k and q of
+// the next few steps are brought into shared memory, in float32, while this batch of steps is computed; every thread reads them
+// as broadcasts.  A step is three instructions for two entries of the state:
+//   t = X + k v;  X = t + (g - 1) X   where g >= 1/2: g - 1 has all its digits, so that a long memory does not drift, and
+//   X = g X + k v                     below, where the difference would cancel;    o += q X.
+#include "linear_attention.cuh"
+
+namespace gala {
+namespace {
+
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pack(float a, float b) {
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 unpack(f2 r) {
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(r));
+    return v;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// One block: 32 W columns of one unit (sequence and head) over one piece of the time axis.
+template <typename T, int DK, int W>
+__global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a) {
+    constexpr int TS = 2 * W;                       // steps brought in at once
+    constexpr int kLoads = TS * DK / (32 * W);      // of k, and of q, a thread
+    __shared__ __align__(16) float ks[TS][DK], qs[TS][DK];
+    __shared__ float vs[TS][32 * W];
+    const int tid = threadIdx.x;
+    const long long units = a.batch * a.heads;
+    const long long unit = blockIdx.x % units;
+    const int piece = (int)(blockIdx.x / units);
+    const long long n = unit / a.heads;
+    const int h = (int)(unit - n * a.heads);
+    const int d = blockIdx.y * 32 * W + tid;
+    const bool mine = d < a.dv, outputs = !a.states_only && a.o;
+    const long long state = unit * a.dk * a.dv;
+    pdl_wait();
+    pdl_launch();
+    if (a.repair) {
+        int any = 0;
+        if (a.flags)
+            for (int i = 0; i < a.repair_pieces; i++) any |= a.flags[i * units + unit];
+        if (!any) {
+            if (a.z && a.last && mine) {
+                const float* z = a.z + ((long long)(a.repair_pieces - 1) * units + unit) * a.dk * a.dv;
+                for (int c = 0; c < a.dk; c++) a.last[state + (long long)c * a.last_c + (long long)d * a.last_d] = z[c * a.dv + d];
+            }
+            return;
+        }
+    }
+    const long long p0 = (long long)piece * a.piece, p1 = min(a.steps, p0 + a.piece);
+    float ld = a.log_decay[h];
+    ld = ld > 0.0f ? 0.0f : ld;
+    const float g = expf(ld), less = expm1f(ld);
+    const bool near = g >= 0.5f, none = g == 0.0f;      // none: nothing is kept, an infinity neither
+
+    f2 X[DK / 2];
+    {
+        const float* from = nullptr;
+        int fc = a.first_c, fd = a.first_d;
+        if (piece == 0) {
+            from = a.first ? a.first + state : nullptr;
+        } else if (!a.states_only) {      // what the pieces before this one left
+            from = a.z + ((long long)(piece - 1) * units + unit) * a.dk * a.dv;
+            fc = a.dv;
+            fd = 1;
+        }
+#pragma unroll
+        for (int c = 0; c < DK; c += 2) {
+            float x0 = 0.0f, x1 = 0.0f;
+            if (from && mine && c < a.dk) x0 = from[(long long)c * fc + (long long)d * fd];
+            if (from && mine && c + 1 < a.dk) x1 = from[(long long)(c + 1) * fc + (long long)d * fd];
+            X[c / 2] = pack(x0, x1);
+        }
+    }
+    const T* kp = static_cast<const T*>(a.k.p) + n * a.k.b + h * a.k.h;
+    const T* qp = static_cast<const T*>(a.q.p) + n * a.q.b + h * a.q.h;
+    const T* vp = static_cast<const T*>(a.v.p) + n * a.v.b + h * a.v.h;
+    T* op = static_cast<T*>(a.o) + n * a.o_b + h * a.o_h;
+    const unsigned char* done = a.done ? a.done + n * a.done_b : nullptr;
+    float kr[kLoads], qr[kLoads], vr[TS];
+    uint32_t cut = 0, cut_next = 0;       // bit s: what is held is dropped before step s of the batch
+    auto fetch = [&](long long p) {
+#pragma unroll
+        for (int m = 0; m < kLoads; m++) {
+            const int e = m * 32 * W + tid, s = e / DK, c = e % DK;
+            const long long t = a.rev ? a.steps - 1 - (p + s) : p + s;
+            const bool in = p + s < p1 && c < a.dk;
+            kr[m] = in ? to_f32<T>(kp[t * a.k.t + c]) * a.in : 0.0f;
+            qr[m] = in && outputs ? to_f32<T>(qp[t * a.q.t + c]) : 0.0f;
+        }
+        cut_next = 0;
+#pragma unroll
+        for (int s = 0; s < TS; s++) {
+            const long long t = a.rev ? a.steps - 1 - (p + s) : p + s;
+            vr[s] = p + s < p1 && mine ? to_f32<T>(vp[t * a.v.t + d]) : 0.0f;
+            const long long flag = a.rev ? t : t - 1;
+            if (done && p + s < p1 && flag >= 0 && done[flag * a.done_t]) cut_next |= 1u << s;
+        }
+    };
+    bool dropped = false;
+    if (p0 < p1) fetch(p0);
+    for (long long p = p0; p < p1; p += TS) {
+#pragma unroll
+        for (int m = 0; m < kLoads; m++) {
+            const int e = m * 32 * W + tid;
+            ks[e / DK][e % DK] = kr[m];
+            qs[e / DK][e % DK] = qr[m];
+        }
+#pragma unroll
+        for (int s = 0; s < TS; s++) vs[s][tid] = vr[s];
+        cut = cut_next;
+        __syncthreads();
+        if (p + TS < p1) fetch(p + TS);
+        const int steps = (int)min((long long)TS, p1 - p);
+#pragma unroll 1
+        for (int s = 0; s < steps; s++) {
+            const float v = vs[s][tid];
+            const f2 vv = pack(v, v);
+            const float4* k4 = reinterpret_cast<const float4*>(ks[s]);
+            if ((cut >> s & 1u) || (none && !(a.rev && p + s == 0))) {
+                dropped = true;
+#pragma unroll
+                for (int c = 0; c < DK / 4; c++) {
+                    const float4 k = k4[c];
+                    X[2 * c] = mul2(pack(k.x, k.y), vv);
+                    X[2 * c + 1] = mul2(pack(k.z, k.w), vv);
+                }
+            } else if (near && !(a.rev && p + s == 0)) {
+                const f2 m = pack(less, less);
+#pragma unroll
+                for (int c = 0; c < DK / 4; c++) {
+                    const float4 k = k4[c];
+                    X[2 * c] = fma2(m, X[2 * c], fma2(pack(k.x, k.y), vv, X[2 * c]));
+                    X[2 * c + 1] = fma2(m, X[2 * c + 1], fma2(pack(k.z, k.w), vv, X[2 * c + 1]));
+                }
+            } else {
+                const float f = a.rev && p + s == 0 ? 1.0f : g;
+                const f2 m = pack(f, f);
+#pragma unroll
+                for (int c = 0; c < DK / 4; c++) {
+                    const float4 k = k4[c];
+                    X[2 * c] = fma2(m, X[2 * c], mul2(pack(k.x, k.y), vv));
+                    X[2 * c + 1] = fma2(m, X[2 * c + 1], mul2(pack(k.z, k.w), vv));
+                }
+            }
+            if (outputs) {
+                const float4* q4 = reinterpret_cast<const float4*>(qs[s]);
+                f2 o0 = pack(0.0f, 0.0f), o1 = o0, o2 = o0, o3 = o0;
+#pragma unroll
+                for (int c = 0; c < DK / 4; c += 2) {
+                    const float4 q = q4[c], r = q4[c + 1];
+                    o0 = fma2(pack(q.x, q.y), X[2 * c], o0);
+                    o1 = fma2(pack(q.z, q.w), X[2 * c + 1], o1);
+                    o2 = fma2(pack(r.x, r.y), X[2 * c + 2], o2);
+                    o3 = fma2(pack(r.z, r.w), X[2 * c + 3], o3);
+                }
+                const float2 s0 = unpack(o0), s1 = unpack(o1), s2 = unpack(o2), s3 = unpack(o3);
+                const long long t = a.rev ? a.steps - 1 - (p + s) : p + s;
+                if (mine) op[t * a.o_t + d] = from_f32<T>(a.out * (((s0.x + s0.y) + (s1.x + s1.y)) + ((s2.x + s2.y) + (s3.x + s3.y))));
+            }
+        }
+        __syncthreads();
+    }
+    // what is left
+    float* to = nullptr;
+    int lc = a.dv, ldd = 1;
+    const bool end = piece == a.pieces - 1;
+    if (a.states_only) {
+        to = a.z + ((long long)piece * units + unit) * a.dk * a.dv;
+        if (blockIdx.y == 0 && tid == 0) a.gain[(long long)piece * units + unit] = dropped ? -1.0f : expf(ld * (float)(p1 - p0));
+    } else if (end && a.last) {
+        if (a.pieces > 1) {      // `last` may be `first`, which another block reads
+            to = a.z + ((long long)piece * units + unit) * a.dk * a.dv;
+        } else {
+            to = a.last + state;
+            lc = a.last_c;
+            ldd = a.last_d;
+        }
+    }
+    if (!to || !mine) return;
+    const bool finish = !a.states_only;
+    const bool zero = finish && !a.rev && done && a.steps > 0 && done[(a.steps - 1) * a.done_t];
+    const float gain = finish && a.rev && a.steps > 0 ? g : 1.0f;      // no step: the state goes through as it is
+#pragma unroll
+    for (int c = 0; c < DK; c += 2) {
+        const float2 x = unpack(X[c / 2]);
+        if (c < a.dk) to[(long long)c * lc + (long long)d * ldd] = zero ? 0.0f : gain * x.x;
+        if (c + 1 < a.dk) to[(long long)(c + 1) * lc + (long long)d * ldd] = zero ? 0.0f : gain * x.y;
+    }
+}
+
+// z of piece i becomes the state after pieces 0..i
+__global__ void memory_join_kernel(float* z, const float* gain, int pieces, long long units, int size) {
+    pdl_wait();
+    pdl_launch();
+    const long long unit = blockIdx.x;
+    for (int e = blockIdx.y * blockDim.x + threadIdx.x; e < size; e += gridDim.y * blockDim.x) {
+        float* at = z + unit * size + e;
+        float x = at[0];
+        for (int i = 1; i < pieces; i++) {
+            at += units * size;
+            const float g = gain[(long long)i * units + unit], own = *at;
+            x = g < 0.0f ? own : fmaf(g, x, own);
+            *at = x;
+        }
+    }
+}
+
+template <typename T, int DK>
+cudaError_t steps_of(const MemoryPass& a, cudaStream_t st) {
+    const long long units = a.batch * a.heads, blocks = units * a.pieces;
+    // Wide blocks share k and q; narrow ones where few units leave multiprocessors without work.
+    int w = a.dv > 64 ? 4 : a.dv > 32 ? 2 : 1;
+    while (w > 1 && blocks * ((a.dv + 32 * w - 1) / (32 * w)) < 2 * sm_count()) w /= 2;
+    const dim3 grid((unsigned)blocks, (unsigned)((a.dv + 32 * w - 1) / (32 * w)));
+    if (w == 4) return launch_pdl(memory_steps_kernel<T, DK, 4>, grid, dim3(128), 0, st, a);
+    if (w == 2) return launch_pdl(memory_steps_kernel<T, DK, 2>, grid, dim3(64), 0, st, a);
+    return launch_pdl(memory_steps_kernel<T, DK, 1>, grid, dim3(32), 0, st, a);
+}
+template <typename T>
+cudaError_t steps_typed(const MemoryPass& a, cudaStream_t st) {
+    return a.dk > 64 ? steps_of<T, 128>(a, st) : a.dk > 32 ? steps_of<T, 64>(a, st) : steps_of<T, 32>(a, st);
+}
+cudaError_t memory_steps(const MemoryPass& a, int dtype, cudaStream_t st) {
+    return dtype == GALA_F32 ? steps_typed<float>(a, st) : dtype == GALA_BF16 ? steps_typed<__nv_bfloat16>(a, st) : steps_typed<__half>(a, st);
+}
+
+// Pieces of the step-by-step way.  A piece costs a second reading of k and v, so there are as many as fill the device and no
+// more, of 64 steps at least.
+int step_pieces(long long steps, long long units) {
+    long long p = 4ll * sm_count() / (units > 0 ? units : 1);
+    if (p > steps / 64) p = steps / 64;
+    return p < 2 ? 1 : p > 256 ? 256 : (int)p;
+}
+
+struct Space { long long z, gain, flags, bytes; };      // offsets into the workspace
+Space space_of(long long steps, long long units, int dk, int dv) {
+    const long long p = step_pieces(steps, units);
+    const long long up = 255;
+    Space s;
+    s.z = 0;
+    s.gain = ((p > 1 ? p * units * dk * dv * 4 : 0) + up) & ~up;
+    s.flags = s.gain + ((p * units * 4 + up) & ~up);
+    s.bytes = s.flags + ((p * units * 4 + up) & ~up);
+    return s;
+}
+
+cudaError_t run_pass(MemoryPass a, int dtype, void* workspace, const Space& s, bool& mapped, cudaStream_t st) {
+    const long long units = a.batch * a.heads;
+    char* w = static_cast<char*>(workspace);
+    a.gain = reinterpret_cast<float*>(w + s.gain);
+    a.pieces = step_pieces(a.steps, units);
+    a.piece = (a.steps + a.pieces - 1) / a.pieces;
+    if (a.piece < 1) a.piece = 1;
+    a.pieces = (int)((a.steps + a.piece - 1) / a.piece);
+    if (a.pieces < 1) a.pieces = 1;
+    a.z = a.pieces > 1 ? reinterpret_cast<float*>(w + s.z) : nullptr;
+    if (a.pieces == 1) return memory_steps(a, dtype, st);
+    MemoryPass b = a;
+    b.states_only = 1;
+    b.pieces = a.pieces - 1;
+    cudaError_t e = memory_steps(b, dtype, st);
+    const int size = a.dk * a.dv;
+    if (e == cudaSuccess && b.pieces > 1)
+        e = launch_pdl(memory_join_kernel, dim3((unsigned)units, (unsigned)((size + 255) / 256)), dim3(256), 0, st, a.z, (const float*)a.gain, b.pieces, units, size);
+    if (e == cudaSuccess) e = memory_steps(a, dtype, st);
+    if (e == cudaSuccess && a.last) {      // from z to `last`: no unit has a flag
+        MemoryPass c = a;
+        c.repair = 1;
+        c.repair_pieces = a.pieces;
+        c.flags = nullptr;
+        c.pieces = 1;
+        e = memory_steps(c, dtype, st);
+    }
+    return e;
+}
+
+// What is said of a call that may not be made; NULL: it may.
+struct Shape { const char* name; int dtype, heads, dk, dv; long long steps, batch; };
+bool strides_ok(const MemoryOperand& m, const Shape& s) {
+    return (s.steps <= 1 || (m.t >= 0 && m.t < (1ll << 30))) && (s.batch <= 1 || (m.b >= 0 && m.b < (1ll << 35))) && (s.heads <= 1 || (m.h >= 0 && m.h < (1ll << 35)));
+}
+// the axes of an output lie inside one another
+bool apart(const MemoryOperand& m, const Shape& s, int width) {
+    long long extent[3] = {s.steps, s.batch, s.heads}, stride[3] = {m.t, m.b, m.h};
+    for (int i = 0; i < 3; i++)
+        for (int j = i + 1; j < 3; j++)
+            if (stride[j] < stride[i]) {
+                const long long x = stride[i], y = extent[i];
+                stride[i] = stride[j], extent[i] = extent[j];
+                stride[j] = x, extent[j] = y;
+            }
+    long long span = width;
+    for (int i = 0; i < 3; i++) {
+        if (extent[i] <= 1) continue;
+        if (stride[i] < span) return false;
+        span += stride[i] * (extent[i] - 1);
+    }
+    return true;
+}
+// strides of an axis of one entry are not looked at: 0 is as good as any
+MemoryOperand operand(const void* p, long long t, long long b, long long h, const Shape& s) {
+    return MemoryOperand{p, s.steps > 1 ? t : 0, s.batch > 1 ? b : 0, s.heads > 1 ? h : 0};
+}
+void output(MemoryPass& a, const MemoryOperand& o) {
+    a.o = const_cast<void*>(o.p);
+    a.o_t = o.t;
+    a.o_b = o.b;
+    a.o_h = o.h;
+}
+
+}  // namespace
+}  // namespace gala
+
+using namespace gala;
+
+#define SAY(...) return refuse(GALA_EINVAL, errbuf, errbuf_len, __VA_ARGS__)
+
+// What both calls check of their common arguments; `s` names the call.
+template <typename A> static int check_common(const A& a, const Shape& s, char* errbuf, int errbuf_len) {
+    if (!dtype_ok(s.dtype)) SAY("%s: dtype %d", s.name, s.dtype);
+    if (s.steps < 0 || s.batch < 0 || s.heads < 0 || s.steps >= (1ll << 31) || s.batch >= (1ll << 27) || (s.heads > 0 && s.batch >= (1ll << 27) / s.heads))
+        SAY("%s: %lld steps, %lld sequences, %d heads are out of range", s.name, s.steps, s.batch, s.heads);
+    if (s.dk < 1 || s.dv < 1 || s.dk > 128 || s.dv > 128) SAY("%s: heads of %d and %d entries (1 to 128 of each)", s.name, s.dk, s.dv);
+    if (!aligned(a.log_decay, 4) || !aligned(a.s0, 4) || !aligned(a.status, 4)) SAY("%s: a float32 array or status is not aligned", s.name);
+    if (s.batch == 0 || s.heads == 0) return GALA_OK;
+    if (!a.log_decay) SAY("%s: log_decay is needed", s.name);
+    const size_t es = dtype_size(s.dtype);
+    if (s.steps > 0) {
+        if (!a.q || !a.k || !a.v) SAY("%s: q, k and v are needed", s.name);
+        if (!aligned(a.q, es) || !aligned(a.k, es) || !aligned(a.v, es)) SAY("%s: a pointer is not aligned to its elements", s.name);
+        const MemoryOperand in[3] = {operand(a.q, a.q_t, a.q_b, a.q_h, s), operand(a.k, a.k_t, a.k_b, a.k_h, s), operand(a.v, a.v_t, a.v_b, a.v_h, s)};
+        for (const MemoryOperand& m : in)
+            if (!strides_ok(m, s)) SAY("%s: a negative stride, or one of 2^30 and more in time or 2^35 elsewhere", s.name);
+        if (a.done && ((s.steps > 1 && a.done_t < 0) || (s.batch > 1 && a.done_b < 0))) SAY("%s: a negative stride of done", s.name);
+    }
+    const Space w = space_of(s.steps, s.batch * s.heads, s.dk, s.dv);
+    if (!aligned(a.workspace, 16) || (w.bytes > 0 && (!a.workspace || a.workspace_bytes < w.bytes)))
+        SAY("%s: %lld bytes of workspace are needed, 16-byte aligned", s.name, w.bytes);
+    return GALA_OK;
+}
+template <typename A> static MemoryPass common_pass(const A& a, const Shape& s) {
+    MemoryPass p = {};
+    p.log_decay = a.log_decay;
+    p.done = s.steps > 0 ? a.done : nullptr;
+    p.done_t = s.steps > 1 ? a.done_t : 0;
+    p.done_b = s.batch > 1 ? a.done_b : 0;
+    p.steps = s.steps;
+    p.batch = s.batch;
+    p.heads = s.heads;
+    p.dk = s.dk;
+    p.dv = s.dv;
+    p.in = p.out = 1.0f;
+    p.first_c = p.last_c = s.dv;
+    p.first_d = p.last_d = 1;
+    p.status = a.status;
+    return p;
+}
+// rows and columns of the state change places
+static void transpose(MemoryPass& p, const Shape& s) {
+    p.dk = s.dv;
+    p.dv = s.dk;
+    p.first_c = p.last_c = 1;
+    p.first_d = p.last_d = s.dv;
+}
+
+extern "C" long long gala_linear_attention_workspace(long long steps, long long batch, int heads, int dk, int dv) {
+    if (steps < 0 || steps >= (1ll << 31) || batch < 0 || batch >= (1ll << 27) || heads < 0 || (heads > 0 && batch >= (1ll << 27) / heads) || dk < 1 || dv < 1 ||
+        dk > 128 || dv > 128)
+        return GALA_EINVAL;
+    return space_of(steps, batch * heads, dk, dv).bytes;
+}
+
+extern "C" int gala_linear_attention_forward(const gala_linear_attention_args* q, void* stream, char* errbuf, int errbuf_len) {
+    if (errbuf && errbuf_len > 0) errbuf[0] = 0;
+    if (!q) SAY("gala_linear_attention_forward: null arguments");
+    const gala_linear_attention_args& a = *q;
+    const Shape s = {"gala_linear_attention_forward", a.dtype, a.heads, a.dk, a.dv, a.steps, a.batch};
+    const int rc = check_common(a, s, errbuf, errbuf_len);
+    if (rc != GALA_OK) return rc;
+    if (!aligned(a.s_last, 4)) SAY("%s: a float32 array or status is not aligned", s.name);
+    if (s.batch == 0 || s.heads == 0 || (s.steps == 0 && (!a.s_last || a.s_last == a.s0))) return GALA_OK;
+    const MemoryOperand o = operand(a.o, a.o_t, a.o_b, a.o_h, s);
+    if (s.steps > 0) {
+        if (!a.o || !aligned(a.o, dtype_size(s.dtype))) SAY("%s: o is needed, aligned to its elements", s.name);
+        if (!strides_ok(o, s) || !apart(o, s, s.dv)) SAY("%s: rows of o overlap, or a stride is out of range", s.name);
+    }
+    MemoryPass p = common_pass(a, s);
+    p.q = operand(a.q, a.q_t, a.q_b, a.q_h, s);
+    p.k = operand(a.k, a.k_t, a.k_b, a.k_h, s);
+    p.v = operand(a.v, a.v_t, a.v_b, a.v_h, s);
+    output(p, o);
+    p.first = a.s0;
+    p.last = a.s_last;
+    p.out = a.scale;
+    bool mapped = true;
+    const cudaError_t e = run_pass(p, s.dtype, a.workspace, space_of(s.steps, s.batch * s.heads, s.dk, s.dv), mapped, static_cast<cudaStream_t>(stream));
+    if (!mapped) SAY("%s: the driver refused a tensor map", s.name);
+    return launched(e, errbuf, errbuf_len, s.name);
+}
+
+extern "C" int gala_linear_attention_backward(const gala_linear_attention_grad_args* q, void* stream, char* errbuf, int errbuf_len) {
+    if (errbuf && errbuf_len > 0) errbuf[0] = 0;
+    if (!q) SAY("gala_linear_attention_backward: null arguments");
+    const gala_linear_attention_grad_args& a = *q;
+    const Shape s = {"gala_linear_attention_backward", a.dtype, a.heads, a.dk, a.dv, a.steps, a.batch};
+    const int rc = check_common(a, s, errbuf, errbuf_len);
+    if (rc != GALA_OK) return rc;
+    if (!aligned(a.grad_s_last, 4) || !aligned(a.grad_s0, 4)) SAY("%s: a float32 array or status is not aligned", s.name);
+    if (s.batch == 0 || s.heads == 0) return GALA_OK;
+    const MemoryOperand in_q = operand(a.q, a.q_t, a.q_b, a.q_h, s), in_k = operand(a.k, a.k_t, a.k_b, a.k_h, s), in_v = operand(a.v, a.v_t, a.v_b, a.v_h, s);
+    const MemoryOperand in_o = operand(a.grad_o, a.grad_o_t, a.grad_o_b, a.grad_o_h, s), out_q = operand(a.grad_q, a.grad_q_t, a.grad_q_b, a.grad_q_h, s);
+    const MemoryOperand out_k = operand(a.grad_k, a.grad_k_t, a.grad_k_b, a.grad_k_h, s), out_v = operand(a.grad_v, a.grad_v_t, a.grad_v_b, a.grad_v_h, s);
+    if (s.steps > 0) {
+        const size_t es = dtype_size(s.dtype);
+        if (!a.grad_o || !aligned(a.grad_o, es)) SAY("%s: grad_o is needed, aligned to its elements", s.name);
+        if (!strides_ok(in_o, s)) SAY("%s: a negative stride, or one of 2^30 and more in time or 2^35 elsewhere", s.name);
+        if (!aligned(a.grad_q, es) || !aligned(a.grad_k, es) || !aligned(a.grad_v, es)) SAY("%s: a pointer is not aligned to its elements", s.name);
+        if ((a.grad_q && (!strides_ok(out_q, s) || !apart(out_q, s, s.dk))) || (a.grad_k && (!strides_ok(out_k, s) || !apart(out_k, s, s.dk))) ||
+            (a.grad_v && (!strides_ok(out_v, s) || !apart(out_v, s, s.dv))))
+            SAY("%s: rows of a gradient overlap, or a stride is out of range", s.name);
+    }
+    const Space w = space_of(s.steps, s.batch * s.heads, s.dk, s.dv);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = cudaSuccess;
+    bool mapped = true;
+    if (a.grad_q && s.steps > 0) {
+        MemoryPass p = common_pass(a, s);
+        transpose(p, s);
+        p.q = in_o;
+        p.k = in_v;
+        p.v = in_k;
+        output(p, out_q);
+        p.first = a.s0;
+        p.out = a.scale;
+        e = run_pass(p, s.dtype, a.workspace, w, mapped, st);
+    }
+    if (e == cudaSuccess && mapped && ((a.grad_v && s.steps > 0) || a.grad_s0)) {
+        MemoryPass p = common_pass(a, s);
+        p.rev = 1;
+        p.q = in_k;
+        p.k = in_q;
+        p.v = in_o;
+        output(p, out_v);
+        p.first = a.grad_s_last;
+        p.last = a.grad_s0;
+        p.in = a.scale;
+        e = run_pass(p, s.dtype, a.workspace, w, mapped, st);
+    }
+    if (e == cudaSuccess && mapped && a.grad_k && s.steps > 0) {
+        MemoryPass p = common_pass(a, s);
+        transpose(p, s);
+        p.rev = 1;
+        p.q = in_v;
+        p.k = in_o;
+        p.v = in_q;
+        output(p, out_k);
+        p.first = a.grad_s_last;
+        p.in = a.scale;
+        e = run_pass(p, s.dtype, a.workspace, w, mapped, st);
+    }
+    if (!mapped) SAY("%s: the driver refused a tensor map", s.name);
+    return launched(e, errbuf, errbuf_len, s.name);
+}

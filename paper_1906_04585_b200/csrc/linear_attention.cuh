@@ -1,0 +1,48 @@
+// Shared by the two ways of the attention memory: the description of one pass over the time axis.
+//
+// Forward and backward are the same pass with other operands.  A pass goes over the steps in its own order p = 0, 1, ...
+// (time itself, or from the last step back with `rev`) and holds X [dk][dv] in float32:
+//   X = gain * X + in * k v^T      o = out * X^T q
+//   forward  q, k, v -> o          X = S            in = 1      out = scale    from s0      to s_last
+//   dq       do, v, k -> dq        X = S^T          in = 1      out = scale    from s0^T
+//   dv       k, q, do -> dv        X = R    rev     in = scale  out = 1        from grad_s_last     to grad_s0
+//   dk       v, do, q -> dk        X = R^T  rev     in = scale  out = 1        from grad_s_last^T
+// The gain into step p is g, 0 (and what was held is dropped, whatever it is) where a flag stands on that link: done of the
+// step before in time.  Backwards in time the given state enters the first step with gain 1 (0 where done), and what is
+// left is multiplied by g at the end; forwards it enters with g, and is dropped at the end where the last step is done.
+#pragma once
+#include "sequence.cuh"
+
+namespace gala {
+
+struct MemoryOperand { const void* p; long long t, b, h; };      // strides of time, sequence and head
+
+struct MemoryPass {
+    MemoryOperand q, k, v;
+    void* o;
+    long long o_t, o_b, o_h;
+    const float* log_decay;
+    const unsigned char* done;
+    long long done_t, done_b;
+    const float* first;          // element (c, d) of a unit's state at unit * dk * dv + c * first_c + d * first_d; NULL: zero
+    float* last;                 // the same way
+    int first_c, first_d, last_c, last_d;
+    long long steps, batch;
+    int heads, dk, dv;
+    float in, out;
+    int rev;
+    // The time axis in pieces that run side by side: one launch leaves each piece's own state in `z` ([piece][unit][dk][dv];
+    // pieces after the first begin at zero) and the gain of what enters it in `gain` ([piece][unit], -1: dropped), a small
+    // kernel joins them, and the second launch computes the outputs, each piece from the state that enters it.
+    int pieces;
+    long long piece;             // steps of a piece
+    float* z;
+    float* gain;
+    int states_only;             // the first of the two launches
+    int* flags;                  // chunks: [piece][unit], set where a unit holds what products of tiles would spread; else NULL
+    int repair;                  // steps: only units with a flag are computed, in one piece; of others the state is copied from z
+    int repair_pieces;
+    int* status;
+};
+
+}  // namespace gala

@@ -1,0 +1,417 @@
+// Queries and keys normed by head and turned by position, in one pass, forward and backward, for sm_100a.
+//
+//   r = 1 / sqrt(mean x^2 + eps)   y = x r w   (a, b) -> (a cos f - b sin f, b cos f + a sin f), f = position * inv_freq
+//   backward:  e = the gradient turned by -f   dx = r (e w - x r mean(e w x r))   dw = sum of e x r
+//
+// A group of lanes has a head and each lane four pairs of it, so a pair never leaves a lane, and a token's cosines and sines,
+// which all its heads share, are formed once a warp and stay in registers: the angle in 64 bits as a fraction of a turn, so
+// that position 2^20 is as exact as position 1, then sine and cosine of the fraction in 32.  A warp takes a token (or, where
+// tokens are few, a share of its heads); the weights stay in registers too.  What a lane loads is two runs of four entries (8
+// or 16 bytes) where head size, number of pairs and alignment allow; otherwise the pairs are dealt out singly over the warp.
+// The weights' gradients are summed by lane over all the tokens of a warp, by block through shared memory, and over the blocks
+// by a second kernel, all in a fixed order.
+#include "sequence.cuh"
+
+namespace gala {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr double kTurn = 0.15915494309189533577;      // 1 / (2 pi)
+
+struct Heads { const void* x; long long x_t, x_h; const void* g; long long g_t, g_h; void* y; long long y_t, y_h; const void* w; };
+struct NormRotary {
+    long long tokens;
+    int q_heads, k_heads, dim, pairs, lanes, share, shares;      // lanes of a head; heads a warp takes, and how many such shares a token has
+    int interleaved;
+    float eps;
+    Heads q, k;                   // x: input; g: gradient of the output (backward); y: output
+    const int* positions;
+    const float* inv_freq;
+    float* part;                  // backward: [block][2][dim] sums of the weights' gradients, or NULL
+};
+
+// four neighbouring elements
+template <typename T> struct Four { uint2 w; };
+template <> struct Four<float> { uint4 w; };
+template <typename T> __device__ __forceinline__ void load4(const T* p, float* f) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    Vec<T, 8> v;
+    v.w = make_uint4(u.x, u.y, 0, 0);
+#pragma unroll
+    for (int j = 0; j < 4; j++) f[j] = v.get(j);
+}
+template <> __device__ __forceinline__ void load4<float>(const float* p, float* f) {
+    const float4 u = *reinterpret_cast<const float4*>(p);
+    f[0] = u.x; f[1] = u.y; f[2] = u.z; f[3] = u.w;
+}
+template <typename T> __device__ __forceinline__ void store4(T* p, const float* f) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(Vec<T, 8>::pair(f[0], f[1]), Vec<T, 8>::pair(f[2], f[3]));
+}
+template <> __device__ __forceinline__ void store4<float>(float* p, const float* f) { *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]); }
+
+// Where the eight entries of a lane lie: entry j of its first four and of its second four.  In memory order the two runs are
+// a[0..3], b[0..3] of pairs (a_j, b_j) or, interleaved, a0 b0 a1 b1, a2 b2 a3 b3.
+struct Place {
+    int at[8];
+    bool live[8];
+};
+template <bool VEC> __device__ __forceinline__ Place place(const NormRotary& p, int lane) {
+    Place r;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        const int pair = VEC ? 4 * lane + j : lane + 32 * j;      // VEC: the lane of the group
+        int a, b;
+        if (pair >= p.pairs) a = 2 * pair, b = a + 1;
+        else if (p.interleaved) a = 2 * pair, b = a + 1;
+        else a = pair, b = p.pairs + pair;
+        r.at[j] = a;
+        r.at[4 + j] = b;
+        r.live[j] = a < p.dim;
+        r.live[4 + j] = b < p.dim;
+    }
+    return r;
+}
+// x of a head as (a_0..3, b_0..3)
+template <typename T, bool VEC> __device__ __forceinline__ void get(const T* x, const Place& pl, bool two_runs, float (&f)[8]) {
+    if (VEC) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) f[j] = 0.0f;
+        if (!pl.live[0]) return;
+        if (two_runs) {
+            load4<T>(x + pl.at[0], f);
+            load4<T>(x + pl.at[4], f + 4);
+        } else {
+            float u[8];
+            load4<T>(x + pl.at[0], u);
+            load4<T>(x + pl.at[0] + 4, u + 4);
+#pragma unroll
+            for (int j = 0; j < 4; j++) f[j] = u[2 * j], f[4 + j] = u[2 * j + 1];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) f[j] = pl.live[j] ? to_f32<T>(x[pl.at[j]]) : 0.0f;
+    }
+}
+template <typename T, bool VEC> __device__ __forceinline__ void put(T* x, const Place& pl, bool two_runs, const float (&f)[8]) {
+    if (VEC) {
+        if (!pl.live[0]) return;
+        if (two_runs) {
+            store4<T>(x + pl.at[0], f);
+            store4<T>(x + pl.at[4], f + 4);
+        } else {
+            float u[8];
+#pragma unroll
+            for (int j = 0; j < 4; j++) u[2 * j] = f[j], u[2 * j + 1] = f[4 + j];
+            store4<T>(x + pl.at[0], u);
+            store4<T>(x + pl.at[0] + 4, u + 4);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+            if (pl.live[j]) x[pl.at[j]] = from_f32<T>(f[j]);
+    }
+}
+__device__ __forceinline__ float group_sum(float s, int lanes) {
+    for (int m = lanes / 2; m > 0; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
+    return s;
+}
+
+template <typename T, typename W, bool VEC, bool GRAD>
+__global__ void __launch_bounds__(32 * kWarps) norm_rotary_kernel(const NormRotary p) {
+    __shared__ float part[GRAD ? 2 * 256 : 1];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int own = lane & (p.lanes - 1), group = lane / p.lanes, groups = 32 / p.lanes;
+    const Place pl = place<VEC>(p, own);
+    bool turned[4];      // VEC: all four pairs of a lane, or none
+#pragma unroll
+    for (int j = 0; j < 4; j++) turned[j] = VEC ? 4 * own < p.pairs : lane + 32 * j < p.pairs;
+    const bool two_runs = !p.interleaved && turned[0];
+    const int heads = p.q_heads + p.k_heads;
+    float wq[8], wk[8], freq[4], dwq[8], dwk[8];
+    pdl_wait();
+    pdl_launch();
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        wq[j] = p.q.w && pl.live[j] ? to_f32<W>(static_cast<const W*>(p.q.w)[pl.at[j]]) : 1.0f;
+        wk[j] = p.k.w && pl.live[j] ? to_f32<W>(static_cast<const W*>(p.k.w)[pl.at[j]]) : 1.0f;
+        dwq[j] = dwk[j] = 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        const int pair = VEC ? 4 * own + j : lane + 32 * j;
+        freq[j] = pair < p.pairs ? p.inv_freq[pair] : 0.0f;
+    }
+    const float inv_dim = 1.0f / (float)p.dim;
+    const long long items = p.tokens * p.shares;
+    for (long long item = (long long)blockIdx.x * kWarps + warp; item < items; item += (long long)gridDim.x * kWarps) {
+        const long long token = item / p.shares;
+        const int from = (int)(item - token * p.shares) * p.share, to = min(heads, from + p.share);
+        float co[4], si[4];
+        {
+            const double pos = (double)p.positions[token];
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const double turns = pos * (double)freq[j] * kTurn;
+                sincospif(2.0f * (float)(turns - rint(turns)), &si[j], &co[j]);
+            }
+        }
+        for (int base = from; base < to; base += groups) {
+            const int head = base + group;
+            const bool live = head < to, is_q = head < p.q_heads;
+            const Heads& hd = is_q ? p.q : p.k;
+            const int h = is_q ? head : head - p.q_heads;
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) x[j] = 0.0f;
+            if (live) get<T, VEC>(static_cast<const T*>(hd.x) + token * hd.x_t + h * hd.x_h, pl, two_runs, x);
+            float ss = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; j++) ss = fmaf(x[j], x[j], ss);
+            float y[8];
+            if (!GRAD) {
+                const float r = rsqrtf(fmaf(group_sum(ss, p.lanes), inv_dim, p.eps));
+#pragma unroll
+                for (int j = 0; j < 8; j++) y[j] = x[j] * r * (is_q ? wq[j] : wk[j]);
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    if (turned[j]) {
+                        const float a = y[j], b = y[4 + j];
+                        y[j] = a * co[j] - b * si[j];
+                        y[4 + j] = b * co[j] + a * si[j];
+                    }
+            } else {
+                float g[8];
+#pragma unroll
+                for (int j = 0; j < 8; j++) g[j] = 0.0f;
+                if (live) get<T, VEC>(static_cast<const T*>(hd.g) + token * hd.g_t + h * hd.g_h, pl, two_runs, g);
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    if (turned[j]) {
+                        const float a = g[j], b = g[4 + j];
+                        g[j] = a * co[j] + b * si[j];
+                        g[4 + j] = b * co[j] - a * si[j];
+                    }
+                float dot = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; j++) dot = fmaf(g[j] * (is_q ? wq[j] : wk[j]), x[j], dot);
+                for (int m = p.lanes / 2; m > 0; m >>= 1) {
+                    ss += __shfl_xor_sync(0xffffffffu, ss, m);
+                    dot += __shfl_xor_sync(0xffffffffu, dot, m);
+                }
+                const float r = rsqrtf(fmaf(ss, inv_dim, p.eps)), back = dot * r * r * inv_dim;
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    y[j] = r * (g[j] * (is_q ? wq[j] : wk[j]) - x[j] * back);
+                    const float dw = g[j] * (x[j] * r);
+                    if (live) {
+                        if (is_q) dwq[j] += dw;
+                        else dwk[j] += dw;
+                    }
+                }
+            }
+            if (live) put<T, VEC>(static_cast<T*>(hd.y) + token * hd.y_t + h * hd.y_h, pl, two_runs, y);
+        }
+    }
+    if (GRAD && p.part) {
+        // groups of the warp, then warps of the block, one after another
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+            for (int m = p.lanes; m < 32; m <<= 1) {
+                dwq[j] += __shfl_xor_sync(0xffffffffu, dwq[j], m);
+                dwk[j] += __shfl_xor_sync(0xffffffffu, dwk[j], m);
+            }
+        for (int i = threadIdx.x; i < 512; i += 32 * kWarps) part[i] = 0.0f;
+        for (int w = 0; w < kWarps; w++) {
+            __syncthreads();
+            if (w == warp && lane < p.lanes) {
+#pragma unroll
+                for (int j = 0; j < 8; j++)
+                    if (pl.live[j]) {
+                        part[pl.at[j]] += dwq[j];
+                        part[256 + pl.at[j]] += dwk[j];
+                    }
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < p.dim; i += 32 * kWarps) {
+            p.part[(long long)blockIdx.x * 2 * p.dim + i] = part[i];
+            p.part[(long long)blockIdx.x * 2 * p.dim + p.dim + i] = part[256 + i];
+        }
+    }
+}
+
+// 32 columns a block, the blocks' sums shared out over its warps
+template <typename W>
+__global__ void __launch_bounds__(256) weight_sum_kernel(const float* part, int blocks, int dim, W* dwq, W* dwk) {
+    __shared__ float sums[8][32];
+    pdl_wait();
+    pdl_launch();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = blockIdx.x * 32 + lane;
+    float s = 0.0f;
+    if (col < 2 * dim)
+        for (int b = warp; b < blocks; b += 8) s += part[(long long)b * 2 * dim + col];
+    sums[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && col < 2 * dim) {
+        float t = 0.0f;
+        for (int w = 0; w < 8; w++) t += sums[w][lane];
+        W* to = col < dim ? dwq : dwk;
+        if (to) to[col < dim ? col : col - dim] = from_f32<W>(t);
+    }
+}
+
+int blocks_of(long long tokens) {
+    const long long most = 8ll * sm_count(), b = (tokens + kWarps - 1) / kWarps;
+    return (int)(b < 1 ? 1 : b > most ? most : b);
+}
+
+// the runs of four of a head start on multiples of four elements
+bool runs(const void* p, long long t, long long h, int es) { return !p || (aligned(p, 4 * es) && t % 4 == 0 && h % 4 == 0); }
+
+template <typename T, typename W, bool GRAD> cudaError_t launch_typed(NormRotary p, bool vec, cudaStream_t st) {
+    const int heads = p.q_heads + p.k_heads;
+    p.lanes = 32;
+    if (vec)
+        for (p.lanes = 1; 8 * p.lanes < p.dim;) p.lanes *= 2;
+    const int groups = 32 / p.lanes, turns = (heads + groups - 1) / groups;
+    // A warp takes a whole token, so that its cosines are formed once, unless that leaves warps without one.
+    int per = turns;
+    while (per > 1 && p.tokens * ((turns + per - 1) / per) < 16ll * sm_count()) per = (per + 1) / 2;
+    p.share = per * groups;
+    p.shares = (turns + per - 1) / per;
+    const int blocks = GRAD ? blocks_of(p.tokens) : blocks_of(p.tokens * p.shares);
+    if (vec) return launch_pdl(norm_rotary_kernel<T, W, true, GRAD>, dim3(blocks), dim3(32 * kWarps), 0, st, p);
+    return launch_pdl(norm_rotary_kernel<T, W, false, GRAD>, dim3(blocks), dim3(32 * kWarps), 0, st, p);
+}
+template <bool GRAD> cudaError_t launch(const NormRotary& p, int dtype, int wdtype, bool vec, cudaStream_t st) {
+    if (dtype == GALA_F32) return launch_typed<float, float, GRAD>(p, vec, st);
+    if (dtype == GALA_BF16)
+        return wdtype == GALA_F32 ? launch_typed<__nv_bfloat16, float, GRAD>(p, vec, st) : launch_typed<__nv_bfloat16, __nv_bfloat16, GRAD>(p, vec, st);
+    return wdtype == GALA_F32 ? launch_typed<__half, float, GRAD>(p, vec, st) : launch_typed<__half, __half, GRAD>(p, vec, st);
+}
+
+constexpr long long kMaxTokens = 1ll << 31, kMaxStride = 1ll << 32;      // offsets stay below 2^63
+
+// strides of an axis of one entry are not looked at
+bool axes_ok(const void* p, long long t, long long h, long long tokens, int heads, int dim, int es, bool output) {
+    if (tokens == 0 || heads == 0) return true;
+    if (!p || !aligned(p, es)) return false;
+    if (tokens <= 1) t = (long long)heads * (h > dim ? h : dim);
+    if (heads <= 1) h = t > dim ? t : dim;
+    if (t < 0 || h < 0 || t >= kMaxStride || h >= kMaxStride) return false;
+    if (!output) return true;
+    const long long head_span = h * (heads - 1) + dim, token_span = t * (tokens - 1) + dim;
+    return (h >= dim && (tokens <= 1 || t >= head_span)) || (t >= dim && (heads <= 1 || h >= token_span));
+}
+
+}  // namespace
+}  // namespace gala
+
+using namespace gala;
+
+#define SAY(...) return refuse(GALA_EINVAL, errbuf, errbuf_len, __VA_ARGS__)
+
+template <typename A> static int check_common(const char* name, const A& a, char* errbuf, int errbuf_len) {
+    if (!dtype_ok(a.dtype)) SAY("%s: dtype %d", name, a.dtype);
+    if (a.wdtype != GALA_F32 && a.wdtype != a.dtype) SAY("%s: weights of dtype %d", name, a.wdtype);
+    if (a.dim < 1 || a.dim > 256 || a.pairs < 0 || a.pairs > a.dim / 2) SAY("%s: %d pairs of heads of %d entries (1 to 256, and at most half as many pairs)", name, a.pairs, a.dim);
+    if (a.tokens < 0 || a.tokens >= kMaxTokens || a.q_heads < 0 || a.k_heads < 0 || a.q_heads > 65536 || a.k_heads > 65536)
+        SAY("%s: %lld tokens, %d and %d heads", name, a.tokens, a.q_heads, a.k_heads);
+    if (!(a.eps >= 0.0f)) SAY("%s: eps %g", name, a.eps);
+    if (!aligned(a.positions, 4) || !aligned(a.inv_freq, 4) || !aligned(a.q_weight, dtype_size(a.wdtype)) || !aligned(a.k_weight, dtype_size(a.wdtype)))
+        SAY("%s: a pointer is not aligned to its elements", name);
+    return GALA_OK;
+}
+template <typename A> static NormRotary common(const A& a) {
+    NormRotary p = {};
+    p.tokens = a.tokens;
+    p.q_heads = a.q_heads;
+    p.k_heads = a.k_heads;
+    p.dim = a.dim;
+    p.pairs = a.pairs;
+    p.interleaved = a.interleaved != 0;
+    p.eps = a.eps;
+    p.positions = a.positions;
+    p.inv_freq = a.inv_freq;
+    p.q.x = a.q, p.q.x_t = a.tokens > 1 ? a.q_t : 0, p.q.x_h = a.q_heads > 1 ? a.q_h : 0, p.q.w = a.q_weight;
+    p.k.x = a.k, p.k.x_t = a.tokens > 1 ? a.k_t : 0, p.k.x_h = a.k_heads > 1 ? a.k_h : 0, p.k.w = a.k_weight;
+    return p;
+}
+static bool vector_ok(const NormRotary& p, int dtype) {
+    const int es = dtype_size(dtype);
+    if (p.dim % 8 || p.pairs % 4) return false;
+    for (const Heads* h : {&p.q, &p.k})
+        if (!runs(h->x, h->x_t, h->x_h, es) || !runs(h->g, h->g_t, h->g_h, es) || !runs(h->y, h->y_t, h->y_h, es)) return false;
+    return true;
+}
+
+extern "C" int gala_qk_norm_rotary_forward(const gala_qk_norm_rotary_args* q, void* stream, char* errbuf, int errbuf_len) {
+    static const char* name = "gala_qk_norm_rotary_forward";
+    if (errbuf && errbuf_len > 0) errbuf[0] = 0;
+    if (!q) SAY("%s: null arguments", name);
+    const gala_qk_norm_rotary_args& a = *q;
+    const int rc = check_common(name, a, errbuf, errbuf_len);
+    if (rc != GALA_OK) return rc;
+    if (a.tokens == 0 || a.q_heads + a.k_heads == 0) return GALA_OK;
+    const int es = dtype_size(a.dtype);
+    if (!a.positions || (a.pairs > 0 && !a.inv_freq)) SAY("%s: positions and inv_freq are needed", name);
+    if (!axes_ok(a.q, a.q_t, a.q_h, a.tokens, a.q_heads, a.dim, es, false) || !axes_ok(a.k, a.k_t, a.k_h, a.tokens, a.k_heads, a.dim, es, false))
+        SAY("%s: q and k are needed, aligned to their elements, strides not negative and below 2^32", name);
+    if (!axes_ok(a.q_out, a.q_out_t, a.q_out_h, a.tokens, a.q_heads, a.dim, es, true) || !axes_ok(a.k_out, a.k_out_t, a.k_out_h, a.tokens, a.k_heads, a.dim, es, true))
+        SAY("%s: q_out and k_out are needed, aligned to their elements, rows apart, strides below 2^32", name);
+    NormRotary p = common(a);
+    p.q.y = a.q_out, p.q.y_t = a.tokens > 1 ? a.q_out_t : 0, p.q.y_h = a.q_heads > 1 ? a.q_out_h : 0;
+    p.k.y = a.k_out, p.k.y_t = a.tokens > 1 ? a.k_out_t : 0, p.k.y_h = a.k_heads > 1 ? a.k_out_h : 0;
+    return launched(launch<false>(p, a.dtype, a.wdtype, vector_ok(p, a.dtype), static_cast<cudaStream_t>(stream)), errbuf, errbuf_len, name);
+}
+
+extern "C" long long gala_qk_norm_rotary_workspace(long long tokens, int dim) {
+    if (tokens < 0 || dim < 1 || dim > 256) return GALA_EINVAL;
+    return tokens == 0 ? 0 : (long long)blocks_of(tokens) * 2 * dim * 4;
+}
+
+extern "C" int gala_qk_norm_rotary_backward(const gala_qk_norm_rotary_grad_args* q, void* stream, char* errbuf, int errbuf_len) {
+    static const char* name = "gala_qk_norm_rotary_backward";
+    if (errbuf && errbuf_len > 0) errbuf[0] = 0;
+    if (!q) SAY("%s: null arguments", name);
+    const gala_qk_norm_rotary_grad_args& a = *q;
+    const int rc = check_common(name, a, errbuf, errbuf_len);
+    if (rc != GALA_OK) return rc;
+    const int es = dtype_size(a.dtype), ws = dtype_size(a.wdtype);
+    if (!aligned(a.grad_q_weight, ws) || !aligned(a.grad_k_weight, ws)) SAY("%s: a pointer is not aligned to its elements", name);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (a.tokens == 0 || a.q_heads + a.k_heads == 0) {      // sums over nothing
+        cudaError_t e = a.grad_q_weight ? cudaMemsetAsync(a.grad_q_weight, 0, (size_t)a.dim * ws, st) : cudaSuccess;
+        if (e == cudaSuccess && a.grad_k_weight) e = cudaMemsetAsync(a.grad_k_weight, 0, (size_t)a.dim * ws, st);
+        return launched(e, errbuf, errbuf_len, name);
+    }
+    if (!a.positions || (a.pairs > 0 && !a.inv_freq)) SAY("%s: positions and inv_freq are needed", name);
+    if (!axes_ok(a.q, a.q_t, a.q_h, a.tokens, a.q_heads, a.dim, es, false) || !axes_ok(a.k, a.k_t, a.k_h, a.tokens, a.k_heads, a.dim, es, false) ||
+        !axes_ok(a.grad_q_out, a.grad_q_out_t, a.grad_q_out_h, a.tokens, a.q_heads, a.dim, es, false) ||
+        !axes_ok(a.grad_k_out, a.grad_k_out_t, a.grad_k_out_h, a.tokens, a.k_heads, a.dim, es, false))
+        SAY("%s: q, k, grad_q_out and grad_k_out are needed, aligned to their elements, strides not negative and below 2^32", name);
+    if (!axes_ok(a.grad_q, a.grad_q_t, a.grad_q_h, a.tokens, a.q_heads, a.dim, es, true) || !axes_ok(a.grad_k, a.grad_k_t, a.grad_k_h, a.tokens, a.k_heads, a.dim, es, true))
+        SAY("%s: grad_q and grad_k are needed, aligned to their elements, rows apart, strides below 2^32", name);
+    NormRotary p = common(a);
+    p.q.g = a.grad_q_out, p.q.g_t = a.tokens > 1 ? a.grad_q_out_t : 0, p.q.g_h = a.q_heads > 1 ? a.grad_q_out_h : 0;
+    p.k.g = a.grad_k_out, p.k.g_t = a.tokens > 1 ? a.grad_k_out_t : 0, p.k.g_h = a.k_heads > 1 ? a.grad_k_out_h : 0;
+    p.q.y = a.grad_q, p.q.y_t = a.tokens > 1 ? a.grad_q_t : 0, p.q.y_h = a.q_heads > 1 ? a.grad_q_h : 0;
+    p.k.y = a.grad_k, p.k.y_t = a.tokens > 1 ? a.grad_k_t : 0, p.k.y_h = a.k_heads > 1 ? a.grad_k_h : 0;
+    const bool sums = a.grad_q_weight || a.grad_k_weight;
+    if (sums) {
+        if (!a.workspace || !aligned(a.workspace, 16) || a.workspace_bytes < gala_qk_norm_rotary_workspace(a.tokens, a.dim))
+            SAY("%s: %lld bytes of workspace are needed, 16-byte aligned", name, gala_qk_norm_rotary_workspace(a.tokens, a.dim));
+        p.part = static_cast<float*>(a.workspace);
+    }
+    cudaError_t e = launch<true>(p, a.dtype, a.wdtype, vector_ok(p, a.dtype), st);
+    if (e == cudaSuccess && sums) {
+        const dim3 grid((2 * a.dim + 31) / 32);
+        const int blocks = blocks_of(a.tokens);
+        const float* part = p.part;
+        if (a.wdtype == GALA_F32) e = launch_pdl(weight_sum_kernel<float>, grid, dim3(256), 0, st, part, blocks, a.dim, static_cast<float*>(a.grad_q_weight), static_cast<float*>(a.grad_k_weight));
+        else if (a.wdtype == GALA_BF16)
+            e = launch_pdl(weight_sum_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, part, blocks, a.dim, static_cast<__nv_bfloat16*>(a.grad_q_weight), static_cast<__nv_bfloat16*>(a.grad_k_weight));
+        else e = launch_pdl(weight_sum_kernel<__half>, grid, dim3(256), 0, st, part, blocks, a.dim, static_cast<__half*>(a.grad_q_weight), static_cast<__half*>(a.grad_k_weight));
+    }
+    return launched(e, errbuf, errbuf_len, name);
+}

@@ -1,5 +1,6 @@
-"""Operators of sequence policies on torch tensors: layer norm, a gated linear recurrence over time, a gated
-feed-forward block, and the draw of an action or token.
+"""Operators of sequence policies on torch tensors: layer norm, a gated linear recurrence over time, attention with a memory
+of fixed size and the norm and rotation of its queries and keys, a gated feed-forward block, the adjustment of logits, and
+the draw of an action or token.
 
 Argument checks and marshalling only, as in `learner`: every operator runs inside libgala.so (include/gala.h has the
 formulas) on torch's current stream of the tensors' device, which has to be the current one.  Element types are float32,
@@ -381,3 +382,214 @@ def sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature: Optional[t
     a.logprobs = _flat("logprobs", logprobs, shape[:1], torch.float32, logits)
     B.gala_sample(a, st)
     return tokens, logprobs
+
+
+# ---------------------------------------------------------------------------------------------- attention with a memory
+def _heads(name: str, t: Optional[torch.Tensor], shape, dtype, like: torch.Tensor):
+    """Pointer and the strides of time, sequence and head of a [steps, batch, heads, width] tensor with contiguous channels."""
+    if t is None:
+        return None, 0, 0, 0
+    if not (t.dtype is dtype and t.shape == shape and t.get_device() == like.get_device()):
+        _want(name, t, shape, dtype, like)
+    time, sequence, head, channel = t.stride()
+    if channel != 1 and shape[3] > 1:
+        raise ValueError("the channels of %s have to be contiguous" % name)
+    return t.data_ptr(), time, sequence, head
+
+
+def _attention(a, q, k, v, log_decay, s0, done, scale):
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError("q, k and v have to be [steps, batch, heads, width]")
+    T, N, H, dk = q.shape
+    dv = v.shape[3]
+    a.dtype, a.steps, a.batch, a.heads, a.dk, a.dv = _type_of(q), T, N, _width("heads", H), _width("the width of q", dk), _width("the width of v", dv)
+    a.scale = dk ** -0.5 if scale is None else scale
+    keys, values, state = (T, N, H, dk), (T, N, H, dv), (N, H, dk, dv)
+    a.q, a.q_t, a.q_b, a.q_h = _heads("q", q, keys, q.dtype, q)
+    a.k, a.k_t, a.k_b, a.k_h = _heads("k", k, keys, q.dtype, q)
+    a.v, a.v_t, a.v_b, a.v_h = _heads("v", v, values, q.dtype, q)
+    a.log_decay = _flat("log_decay", log_decay, (H,), torch.float32, q)
+    a.done, a.done_t, a.done_b = _done(done, (T, N), q)
+    a.s0 = _flat("s0", s0, state, torch.float32, q)
+    a.status = _status_word(q)
+    a.workspace_bytes = B.gala_linear_attention_workspace(T, N, H, dk, dv)
+    space = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=q.device)
+    a.workspace = space.data_ptr()
+    return keys, values, state, space
+
+
+def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, s0: Optional[torch.Tensor] = None, *,
+                     done: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                     s_last: Optional[torch.Tensor] = None):
+    """S_t = g C_{t-1} + k_t v_t^T and o_t = scale S_t^T q_t over time for every head, g = exp(log_decay) of the head; C_t is
+    S_t, or 0 where done_t; C_{-1} = s0.
+
+    q, k [steps, batch, heads, dk] and v [steps, batch, heads, dv] with any strides for time, sequence and head, dk and dv up to
+    128; log_decay [heads] float32, at most 0 (above counts as 0); done [steps, batch] with the meaning it has in a rollout;
+    scale is dk ** -0.5 unless given.  Returns (o, s_last): s_last [batch, heads, dk, dv] float32 is the s0 of the next call
+    (pass the same tensor as both to keep a memory in place)."""
+    st = _stream(q)
+    a = B.gala_linear_attention_args()
+    keys, values, state, space = _attention(a, q, k, v, log_decay, s0, done, scale)
+    o = torch.empty(values, dtype=q.dtype, device=q.device) if out is None else out
+    s_last = torch.empty(state, dtype=torch.float32, device=q.device) if s_last is None else s_last
+    a.o, a.o_t, a.o_b, a.o_h = _heads("out", o, values, q.dtype, q)
+    a.s_last = _flat("s_last", s_last, state, torch.float32, q)
+    B.gala_linear_attention_forward(a, st)
+    return o, s_last
+
+
+def linear_attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor,
+                              s0: Optional[torch.Tensor] = None, *, done: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                              ds_last: Optional[torch.Tensor] = None, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                              dv: Optional[torch.Tensor] = None, ds0: Optional[torch.Tensor] = None):
+    """Gradients (dq, dk, dv, ds0) of linear_attention from those of o (do) and s_last (ds_last); the other arguments are the
+    forward call's (s0 as it was then)."""
+    st = _stream(q)
+    a = B.gala_linear_attention_grad_args()
+    keys, values, state, space = _attention(a, q, k, v, log_decay, s0, done, scale)
+    dq = torch.empty(keys, dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(keys, dtype=q.dtype, device=q.device) if dk is None else dk
+    dv = torch.empty(values, dtype=q.dtype, device=q.device) if dv is None else dv
+    ds0 = torch.empty(state, dtype=torch.float32, device=q.device) if ds0 is None else ds0
+    a.grad_o, a.grad_o_t, a.grad_o_b, a.grad_o_h = _heads("do", do, values, q.dtype, q)
+    a.grad_q, a.grad_q_t, a.grad_q_b, a.grad_q_h = _heads("dq", dq, keys, q.dtype, q)
+    a.grad_k, a.grad_k_t, a.grad_k_b, a.grad_k_h = _heads("dk", dk, keys, q.dtype, q)
+    a.grad_v, a.grad_v_t, a.grad_v_b, a.grad_v_h = _heads("dv", dv, values, q.dtype, q)
+    a.grad_s_last = _flat("ds_last", ds_last, state, torch.float32, q)
+    a.grad_s0 = _flat("ds0", ds0, state, torch.float32, q)
+    B.gala_linear_attention_backward(a, st)
+    return dq, dk, dv, ds0
+
+
+# ---------------------------------------------------------------------------------------------- norm and rotation of q and k
+def _tokens(name: str, t: torch.Tensor, shape, like: torch.Tensor):
+    """Pointer and the strides of token and head of a [tokens, heads, dim] tensor with contiguous entries."""
+    if not (t.dtype is like.dtype and t.shape == shape and t.get_device() == like.get_device()):
+        _want(name, t, shape, like.dtype, like)
+    token, head, entry = t.stride()
+    if entry != 1 and shape[2] > 1:
+        raise ValueError("the entries of %s have to be contiguous" % name)
+    return t.data_ptr(), token, head
+
+
+def _qk(a, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved):
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k have to be [tokens, heads, dim]")
+    n, hq, d = q.shape
+    hk = k.shape[1]
+    a.dtype, a.tokens, a.q_heads, a.k_heads, a.dim = _type_of(q), n, _width("q's heads", hq), _width("k's heads", hk), _width("dim", d)
+    a.pairs, a.interleaved, a.eps = _width("the number of pairs", inv_freq.shape[0] if inv_freq.dim() == 1 else -1), bool(interleaved), eps
+    wdt = q_weight.dtype if q_weight is not None else k_weight.dtype if k_weight is not None else torch.float32
+    a.wdtype = _DTYPE.get(wdt, -1)
+    a.q, a.q_t, a.q_h = _tokens("q", q, (n, hq, d), q)
+    a.k, a.k_t, a.k_h = _tokens("k", k, (n, hk, d), q)
+    a.positions = _flat("positions", positions, (n,), torch.int32, q)
+    a.inv_freq = _flat("inv_freq", inv_freq, (inv_freq.shape[0] if inv_freq.dim() == 1 else 0,), torch.float32, q)
+    a.q_weight = _flat("q_weight", q_weight, (d,), wdt, q)
+    a.k_weight = _flat("k_weight", k_weight, (d,), wdt, q)
+    return (n, hq, d), (n, hk, d), wdt
+
+
+def qk_norm_rotary(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, q_weight: Optional[torch.Tensor] = None,
+                   k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, *, interleaved: bool = False, q_out: Optional[torch.Tensor] = None,
+                   k_out: Optional[torch.Tensor] = None):
+    """Queries [tokens, heads, dim] and keys [tokens, heads of their own, dim] normed by head, x / sqrt(mean x^2 + eps) *
+    weight, and turned by position: of the first 2 * len(inv_freq) entries pair i, (y_i, y_{n+i}) or with `interleaved`
+    (y_2i, y_2i+1), by positions * inv_freq[i].  Any strides for token and head, dim up to 256; positions [tokens] int32,
+    inv_freq float32; weights [dim] are float32 or of q's type.  q_out and k_out may be q and k.  Returns (q_out, k_out)."""
+    st = _stream(q)
+    a = B.gala_qk_norm_rotary_args()
+    qs, ks, _ = _qk(a, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved)
+    q_out = torch.empty(qs, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    k_out = torch.empty(ks, dtype=q.dtype, device=q.device) if k_out is None else k_out
+    a.q_out, a.q_out_t, a.q_out_h = _tokens("q_out", q_out, qs, q)
+    a.k_out, a.k_out_t, a.k_out_h = _tokens("k_out", k_out, ks, q)
+    B.gala_qk_norm_rotary_forward(a, st)
+    return q_out, k_out
+
+
+def qk_norm_rotary_backward(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor,
+                            inv_freq: torch.Tensor, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                            eps: float = 1e-6, *, interleaved: bool = False, dq: Optional[torch.Tensor] = None,
+                            dk: Optional[torch.Tensor] = None, dq_weight: Optional[torch.Tensor] = None,
+                            dk_weight: Optional[torch.Tensor] = None):
+    """Gradients (dq, dk, dq_weight, dk_weight) of qk_norm_rotary; q and k are the forward call's inputs.  dq_weight and
+    dk_weight have the weights' type (float32 without weights); dq may be dq_out, dk dk_out."""
+    st = _stream(q)
+    a = B.gala_qk_norm_rotary_grad_args()
+    qs, ks, wdt = _qk(a, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved)
+    dq = torch.empty(qs, dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(ks, dtype=q.dtype, device=q.device) if dk is None else dk
+    dq_weight = torch.empty(qs[2], dtype=wdt, device=q.device) if dq_weight is None else dq_weight
+    dk_weight = torch.empty(qs[2], dtype=wdt, device=q.device) if dk_weight is None else dk_weight
+    a.grad_q_out, a.grad_q_out_t, a.grad_q_out_h = _tokens("dq_out", dq_out, qs, q)
+    a.grad_k_out, a.grad_k_out_t, a.grad_k_out_h = _tokens("dk_out", dk_out, ks, q)
+    a.grad_q, a.grad_q_t, a.grad_q_h = _tokens("dq", dq, qs, q)
+    a.grad_k, a.grad_k_t, a.grad_k_h = _tokens("dk", dk, ks, q)
+    a.grad_q_weight = _flat("dq_weight", dq_weight, qs[2:], wdt, q)
+    a.grad_k_weight = _flat("dk_weight", dk_weight, qs[2:], wdt, q)
+    if 1 <= qs[2] <= 256:
+        a.workspace_bytes = B.gala_qk_norm_rotary_workspace(qs[0], qs[2])
+    space = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=q.device)
+    a.workspace = space.data_ptr()
+    B.gala_qk_norm_rotary_backward(a, st)
+    return dq, dk, dq_weight, dk_weight
+
+
+# ---------------------------------------------------------------------------------------------- logits before the draw
+def adjust_logits(logits: torch.Tensor, *, history: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None,
+                  repetition: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
+                  bias_ids: Optional[torch.Tensor] = None, bias_values: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None):
+    """Logits [rows, vocab] as they go into `sample`: for tokens among the first lengths[r] of history[r] (c times) divided by
+    repetition[r] (multiplied where not positive) and less frequency[r] * c + presence[r]; then bias_values added at bias_ids;
+    then -inf where bit i % 32 of mask[r, i // 32] is 0.
+
+    history [rows, width], bias_ids [rows, n] (with bias_values float32) and mask [rows or 1, ceil(vocab / 32)] are int32, ids
+    outside 0..vocab-1 (-1 to fill up) count nowhere, n < 4096; lengths [rows] int32; repetition, frequency and presence [rows]
+    float32.  Each may be left out.  out may be logits itself.  Returns the result."""
+    st = _stream(logits)
+    if logits.dim() != 2:
+        raise ValueError("logits has to be a matrix [rows, vocab]")
+    a = B.gala_adjust_logits_args()
+    a.dtype, shape = _type_of(logits), logits.shape
+    R, V = shape
+    a.rows, a.vocab = R, _width("the number of entries", V)
+    out = torch.empty(shape, dtype=logits.dtype, device=logits.device) if out is None else out
+    a.logits, a.logits_ld = _rows("logits", logits, shape, logits)
+    a.out, a.out_ld = _rows("out", out, shape, logits)
+
+    def rows_of(name, t, width, dtype, rows=R):
+        _want(name, t, (rows, width), dtype, logits)
+        if width > 1 and t.stride(1) != 1:
+            raise ValueError("the columns of %s have to be contiguous" % name)
+        return t.data_ptr(), t.stride(0) if rows > 1 else width
+
+    if history is not None:
+        if history.dim() != 2:
+            raise ValueError("history has to be a matrix [rows, width]")
+        a.width = _width("the width of history", history.shape[1])
+        a.history, a.history_ld = rows_of("history", history, history.shape[1], torch.int32)
+    elif not (lengths is None and repetition is None and frequency is None and presence is None):
+        raise ValueError("lengths or penalties without a history")
+    a.lengths = _flat("lengths", lengths, (R,), torch.int32, logits)
+    a.repetition = _flat("repetition", repetition, (R,), torch.float32, logits)
+    a.frequency = _flat("frequency", frequency, (R,), torch.float32, logits)
+    a.presence = _flat("presence", presence, (R,), torch.float32, logits)
+    if (bias_ids is None) != (bias_values is None):
+        raise ValueError("bias_ids and bias_values come together")
+    if bias_ids is not None:
+        if bias_ids.dim() != 2:
+            raise ValueError("bias_ids has to be a matrix [rows, n]")
+        a.biases = _width("the number of biases", bias_ids.shape[1])
+        a.bias_ids, a.bias_ids_ld = rows_of("bias_ids", bias_ids, bias_ids.shape[1], torch.int32)
+        a.bias_values, a.bias_values_ld = rows_of("bias_values", bias_values, bias_ids.shape[1], torch.float32)
+    if mask is not None:
+        words = (V + 31) // 32
+        if mask.dim() == 2 and mask.shape[0] == 1:
+            a.mask, _ = rows_of("mask", mask, words, torch.int32, 1)
+        else:
+            a.mask, a.mask_ld = rows_of("mask", mask, words, torch.int32)
+    B.gala_adjust_logits(a, st)
+    return out

@@ -251,7 +251,7 @@ int step_pieces(long long steps, long long units) {
 
 struct Space { long long z, gain, flags, bytes; };      // offsets into the workspace
 Space space_of(long long steps, long long units, int dk, int dv) {
-    const long long p = step_pieces(steps, units);
+    const long long x = step_pieces(steps, units), y = memory_chunk_pieces(steps, units), p = x > y ? x : y;
     const long long up = 255;
     Space s;
     s.z = 0;
@@ -263,29 +263,36 @@ Space space_of(long long steps, long long units, int dk, int dv) {
 
 cudaError_t run_pass(MemoryPass a, int dtype, void* workspace, const Space& s, bool& mapped, cudaStream_t st) {
     const long long units = a.batch * a.heads;
+    const int size = a.dk * a.dv;
     char* w = static_cast<char*>(workspace);
+    const bool chunks = memory_chunks_ok(a, dtype);
     a.gain = reinterpret_cast<float*>(w + s.gain);
-    a.pieces = step_pieces(a.steps, units);
+    a.pieces = chunks ? memory_chunk_pieces(a.steps, units) : step_pieces(a.steps, units);
     a.piece = (a.steps + a.pieces - 1) / a.pieces;
+    if (chunks) a.piece = (a.piece + 127) / 128 * 128;
     if (a.piece < 1) a.piece = 1;
     a.pieces = (int)((a.steps + a.piece - 1) / a.piece);
     if (a.pieces < 1) a.pieces = 1;
     a.z = a.pieces > 1 ? reinterpret_cast<float*>(w + s.z) : nullptr;
-    if (a.pieces == 1) return memory_steps(a, dtype, st);
-    MemoryPass b = a;
-    b.states_only = 1;
-    b.pieces = a.pieces - 1;
-    cudaError_t e = memory_steps(b, dtype, st);
-    const int size = a.dk * a.dv;
-    if (e == cudaSuccess && b.pieces > 1)
-        e = launch_pdl(memory_join_kernel, dim3((unsigned)units, (unsigned)((size + 255) / 256)), dim3(256), 0, st, a.z, (const float*)a.gain, b.pieces, units, size);
-    if (e == cudaSuccess) e = memory_steps(a, dtype, st);
-    if (e == cudaSuccess && a.last) {      // from z to `last`: no unit has a flag
+    a.flags = chunks ? reinterpret_cast<int*>(w + s.flags) : nullptr;
+    mapped = true;
+    cudaError_t e = cudaSuccess;
+    if (a.pieces > 1) {
+        MemoryPass b = a;
+        b.states_only = 1;
+        b.pieces = a.pieces - 1;
+        e = chunks ? memory_chunks(b, dtype, mapped, st) : memory_steps(b, dtype, st);
+        if (e == cudaSuccess && mapped && b.pieces > 1)
+            e = launch_pdl(memory_join_kernel, dim3((unsigned)units, (unsigned)((size + 255) / 256)), dim3(256), 0, st, a.z, (const float*)a.gain, b.pieces, units, size);
+    }
+    if (e == cudaSuccess && mapped) e = chunks ? memory_chunks(a, dtype, mapped, st) : memory_steps(a, dtype, st);
+    // units with a flag again step by step; of the others what is left goes from z to `last`
+    if (e == cudaSuccess && mapped && (chunks || (a.pieces > 1 && a.last))) {
         MemoryPass c = a;
         c.repair = 1;
         c.repair_pieces = a.pieces;
-        c.flags = nullptr;
         c.pieces = 1;
+        c.piece = a.steps;
         e = memory_steps(c, dtype, st);
     }
     return e;

@@ -45,4 +45,12 @@ struct MemoryPass {
     int* status;
 };
 
+// Fewest steps of a call that goes by chunks
+constexpr long long kChunkSteps = 48;
+
+// Host side of the chunked way (linear_attention_chunk.cu)
+bool memory_chunks_ok(const MemoryPass& a, int dtype);      // types, length, alignment and strides that it takes
+int memory_chunk_pieces(long long steps, long long units);
+cudaError_t memory_chunks(const MemoryPass& a, int dtype, bool& mapped, cudaStream_t st);
+
 }  // namespace gala

@@ -4,12 +4,14 @@
 // elsewhere, and e_i = g^(steps from the entry to i) where no flag stands between (0 elsewhere):
 //   O = out (in (Q K^T * L) V + diag(e) Q X)          X' = carry X + in K^T diag(w) V,  w_j = g^(steps from j to the exit)
 // One block goes over a unit (sequence and head), or a piece of its time axis, chunk by chunk:
-//   warp 0      brings K, Q and V of the chunks in by tensor copies, a ring of tiles
-//   warp 1      issues the products: scores = Q K^T, U = K^T (w V), O1 = P V with P in tensor memory, O2 = Q X
-//   warps 2, 3  float16: the largest magnitudes of the chunk's operands, from which powers of two are taken (below)
-//   warps 4-7   a thread a row: scores -> P, rounded to the element type, in the place of the scores; and o of the chunk before
-//   warps 8-11  w V as two numbers of the element type, rounded and rest, since X is a float32 result (one would leave 2^-9);
-//               X in registers, folded with U; X rounded as the operand of the next chunk's O2
+//   warp 0       brings K, V and Q of the chunks in by tensor copies, a ring of tiles
+//   warp 1       issues the products: scores = Q K^T, U = K^T (w V), O2 = Q X, O1 = P V with P in tensor memory
+//   warps 2, 3   float16: the largest magnitudes of the chunk's operands, from which powers of two are taken (below)
+//   warps 4-7    a thread a row: scores -> P, rounded to the element type, in the place of the scores
+//   warps 8-11   X in registers, folded with U and rounded as the operand of the next chunk's O2; half of the chunk's o
+//   warps 12-15  w V, half a chunk ahead of the others: as two numbers of the element type, rounded and rest, where X is a
+//                float32 result of the call (one number would leave 2^-9 of it); as one where X only adds to o, which is rounded
+//                to the element type anyhow (dq and dk: half of U's products); the other half of the chunk's o
 // The powers of g are differences of exponents, never quotients, so nothing overflows however fast a head fades.
 //
 // What a product cannot do is leave out a term: 0 times an infinity or a NaN spreads it to steps that must not see it.  A unit
@@ -26,7 +28,7 @@ namespace gala {
 namespace {
 
 constexpr int kSteps = 128;
-constexpr int kThreads = 384;
+constexpr int kThreads = 512;
 
 template <int D> struct Chunk {
     static constexpr int kTile = kSteps * D * 2;              // bytes of a chunk of one operand: D / 64 boxes of 128 rows of 128 bytes
@@ -40,10 +42,10 @@ template <int D> struct Chunk {
     static constexpr int kHeld = D == 128 ? 128 : 32;         // columns of X a thread holds
 };
 
-struct ChunkMaps { CUtensorMap q, k, v; };
-struct Broadcast { int q_b, q_h, k_b, k_h, v_b, v_h; };      // 0: the operand is the same for all
+struct ChunkMaps { CUtensorMap q, k, v, o; };
+struct Broadcast { int q_b, q_h, k_b, k_h, v_b, v_h, o_b, o_h; };      // 0: the operand is the same for all (or there is one)
 
-__device__ __forceinline__ void umma_a_tmem(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void umma_tmem(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n.reg .pred p;\n"
         "setp.ne.b32 p, %4, 0;\n"
@@ -51,11 +53,19 @@ __device__ __forceinline__ void umma_a_tmem(uint32_t d, uint32_t a, uint64_t bde
         ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(addr)
+                 : "memory");
+}
+// one column of two places
+__device__ __forceinline__ void tmem_ld1x2(uint32_t a0, uint32_t a1, uint32_t& r0, uint32_t& r1) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
-        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
-        "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
+        "tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%2];\n"
+        "tcgen05.ld.sync.aligned.32x32b.x1.b32 {%1}, [%3];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=&r"(r0), "=&r"(r1)
+        : "r"(a0), "r"(a1)
         : "memory");
 }
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -66,6 +76,9 @@ __device__ __forceinline__ uint4 ld_shared(uint32_t a) {
 }
 __device__ __forceinline__ void st_shared(uint32_t a, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* map, int c0, int c1, int c2, int c3) {
+    asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
 template <bool FP16> __device__ __forceinline__ uint32_t pack(float a, float b) {
     if (!FP16) return pack2(a, b);
@@ -101,6 +114,7 @@ struct Links {
     __device__ __forceinline__ bool any() const { return (w[0] | w[1] | w[2] | w[3]) != 0; }
     __device__ __forceinline__ int highest(int from) const {      // highest bit at or below `from`, -1: none
         int r = -1;
+        if (!any()) return r;
 #pragma unroll
         for (int q = 0; q < 4; q++) {
             const int top = from - 32 * q;
@@ -111,6 +125,7 @@ struct Links {
     }
     __device__ __forceinline__ int lowest(int from) const {       // lowest bit at or above `from`, 128: none
         int r = 128;
+        if (!any()) return r;
 #pragma unroll
         for (int q = 3; q >= 0; q--) {
             const int at = from - 32 * q;
@@ -121,22 +136,85 @@ struct Links {
     }
 };
 
-// a wait of a whole warp, with one outcome for all its lanes
+// Bounded waits in few instructions: a kernel of many roles is bound by instruction fetch before anything else (with the polls
+// unrolled, 100 instructions a wait, a chunk took a third longer).
+__device__ __forceinline__ bool wait_one(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    uint32_t left = kSpinLimit;
+#pragma unroll 1
+    while (!mbar_try_wait(bar, parity)) {
+        if (*abort_flag || --left == 0) {
+            *abort_flag = 1;
+            return false;
+        }
+        __nanosleep(20);
+    }
+    return true;
+}
+// of a whole warp, with one outcome for all its lanes
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+    return __all_sync(0xffffffffu, wait_one(bar, parity, abort_flag));
+}
+// one lane of a converged warp; its branch keeps descriptors in uniform registers
+__device__ __forceinline__ bool elected() {
+    uint32_t r;
+    asm volatile("{\n.reg .pred q;\nelect.sync _|q, 0xffffffff;\nselp.u32 %0, 1, 0, q;\n}" : "=r"(r));
+    return r != 0;
+}
+
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, uint32_t from, int c0, int c1, int c2, int c3) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(from), "r"(c0), "r"(c1),
+                 "r"(c2), "r"(c3)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+
+// Columns from .. from + D / 2 of this lane's row of o: what the chunk's own steps and what the given state add, scaled.  With
+// `stage` into shared memory, as a box of 32 rows that a tensor copy takes out (a store of each lane's own row touches 32 rows an
+// instruction: 2000 cycles a chunk); without, where o has odd addresses, a column at a time.
+template <int D, bool FP16>
+__device__ __forceinline__ void write_o(uint32_t own_at, uint32_t given_at, int from, uint32_t stage, uint16_t* row, int width, bool live, bool reached, float e, float p_back) {
+    const int lane = threadIdx.x & 31;
+    auto joined = [&](uint32_t own, uint32_t given) {
+        float u = __uint_as_float(own);
+        if (FP16) u *= p_back;
+        return reached ? fmaf(e, __uint_as_float(given), u) : u;
+    };
+    if (stage) {
+#pragma unroll 1
+        for (int b = 0; b < D / 2; b += 16) {
+            uint32_t x[16], y[16], o[8];
+            tmem_ld16_issue(own_at + from + b, x);
+            tmem_ld16_issue(given_at + from + b, y);
+            tmem_ld16_wait(x);
+            tmem_ld16_wait(y);
+#pragma unroll
+            for (int j = 0; j < 8; j++) o[j] = pack<FP16>(joined(x[2 * j], y[2 * j]), joined(x[2 * j + 1], y[2 * j + 1]));
+            const int turn = D == 128 ? lane & 7 : (lane >> 1) & 3;      // the 128- or 64-byte swizzle of the box
+            st_shared(stage + lane * D + (((b / 8) ^ turn) << 4), make_uint4(o[0], o[1], o[2], o[3]));
+            st_shared(stage + lane * D + (((b / 8 + 1) ^ turn) << 4), make_uint4(o[4], o[5], o[6], o[7]));
+        }
+    } else {
+#pragma unroll 1
+        for (int m = from; m < min(width, from + D / 2); m++) {
+            uint32_t x, y;
+            tmem_ld1x2(own_at + m, given_at + m, x, y);
+            if (live) row[m] = (uint16_t)pack<FP16>(joined(x, y), 0.0f);
+            __syncwarp();
+        }
+    }
 }
 
 template <int D, bool FP16, bool REV>
 __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_constant__ ChunkMaps maps, const MemoryPass a, const Broadcast cast, const int wide) {
     using C = Chunk<D>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t full[C::kSlots], empty[C::kSlots], hl_ready[2], hl_free[2], scores_full, p_ready, o_full, u_full, s_ready, max_ready[4];
+    __shared__ __align__(8) uint64_t full[C::kSlots], empty[C::kSlots], hl_ready[2], hl_free[2], scores_full, p_ready, o_full, o_free, u_full, u_free, x_ready, x_taken, max_ready[4], o_stored[4];
     __shared__ uint32_t tmem_slot, found;
     __shared__ int abort_flag, issued;
-    __shared__ float pw[132], most[4][2][3], back_s[2], first_most[4];
+    __shared__ float pw[132], most[4][2][3], first_most[4], x_backs[2];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t ring = smem_u32(smem), hl = ring + C::kSlots * C::kTile, sx = hl + 4 * C::kHalf;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const long long units = a.batch * a.heads;
     const long long unit = blockIdx.x % units;
     const int piece = (int)(blockIdx.x / units);
@@ -144,17 +222,21 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
     const int all = (int)((a.steps + kSteps - 1) / kSteps), per = (int)(a.piece / kSteps);
     const int c0 = piece * per, chunks = min(all, c0 + per) - c0;
     const bool outputs = !a.states_only;
-    const int kinds = outputs ? 3 : 2;
+    const int kinds = outputs ? 3 : 2;      // tiles of a chunk: K, V, Q
+    const bool fine = a.last != nullptr;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kSlots; s++) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
         for (int b = 0; b < 2; b++) { mbar_init(&hl_ready[b], 4); mbar_init(&hl_free[b], 1); }
-        for (int b = 0; b < 4; b++) mbar_init(&max_ready[b], 2);
+        for (int b = 0; b < 4; b++) { mbar_init(&max_ready[b], 2); mbar_init(&o_stored[b], 8); }
         mbar_init(&scores_full, 1);
         mbar_init(&p_ready, 4);
         mbar_init(&o_full, 1);
+        mbar_init(&o_free, 8);
         mbar_init(&u_full, 1);
-        mbar_init(&s_ready, 4);
+        mbar_init(&u_free, 4);
+        mbar_init(&x_ready, 4);
+        mbar_init(&x_taken, 4);
         abort_flag = 0;
         issued = 0;
         found = 0;
@@ -172,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
     tcgen05_fence_before();
     __syncthreads();
     tcgen05_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
 
     // first step of the c-th chunk that this block processes, and how many steps it has
     auto begin = [&](int c) { return (long long)(REV ? all - 1 - (c0 + c) : c0 + c) * kSteps; };
@@ -193,85 +275,157 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
         }
     };
     auto links_of = [&](const uint32_t (&f)[4]) {
-        Links l;
+        Links l = {};
+        if (!done) return l;
 #pragma unroll
         for (int q = 0; q < 4; q++) l.w[q] = __ballot_sync(0xffffffffu, f[q] != 0);
         return l;
     };
+    // the factor with which the given state enters row i, and whether it does
+    auto reach_of = [&](const Links& links, int c, int len, int i, float& e) {
+        e = a.out * pw[REV ? max(0, len - 1 - i) + entry_power(c) : i + 1];
+        return REV ? links.lowest(i) == 128 : links.highest(i) < 0;
+    };
+    // half the columns of o of chunk c, by a warp whose rows of tensor memory are `rows`
+    auto put_o = [&](int c, int half, uint32_t rows, long long t0, int len, bool reached, float e, float p_back) {
+        const int q = warp & 3, i = 32 * q + lane;
+        const uint32_t stage = ring + (uint32_t)((3 * c + 2) % C::kSlots) * C::kTile + half * (C::kTile / 2) + q * (32 * D);
+        uint16_t* row = static_cast<uint16_t*>(a.o) + (long long)n * a.o_b + (long long)h * a.o_h + (t0 + i) * a.o_t;
+        write_o<D, FP16>(rows + C::kO1, rows + C::kO2, half * (D / 2), wide ? stage : 0u, row, a.dv, i < len, reached, e, p_back);
+        tcgen05_fence_before();
+        if (wide) proxy_fence();
+        __syncwarp();
+        if (lane == 0) {
+            mbar_arrive(&o_free);
+            if (wide && 32 * q < len && half * (D / 2) < a.dv) {
+                tma_store_4d(&maps.o, stage, half * (D / 2), (int)t0 + 32 * q, h * cast.o_h, n * cast.o_b);
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            }
+            mbar_arrive(&o_stored[c & 3]);
+        }
+        __syncwarp();
+    };
+    // float16: the powers of two, the same for every warp that asks.  m: largest of K, V, Q
+    auto most_of = [&](int c, float (&m)[3]) {
+        if (!warp_wait(&max_ready[c & 3], (uint32_t)(c >> 2) & 1u, &abort_flag)) return false;
+#pragma unroll
+        for (int k = 0; k < 3; k++) m[k] = fmaxf(most[c & 3][0][k], most[c & 3][1][k]);
+        return true;
+    };
 
     if (warp < 4) {
-        if (D == 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (D == 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 0 && lane == 0) {
             int it = 0;
             bool ok = true;
+#pragma unroll 1
             for (int c = 0; ok && c < chunks; c++) {
                 const int t0 = (int)begin(c);
-                for (int kind = 0; kind < kinds; kind++, it++) {       // K, Q, V, or K, V
+#pragma unroll 1
+                for (int kind = 0; kind < kinds; kind++, it++) {
                     const int s = it % C::kSlots;
-                    if (!mbar_wait(&empty[s], ((uint32_t)(it / C::kSlots) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
+                    // the state that enters passes through the places behind the first chunk's
+                    if (it == 3 && !wait_one(&x_taken, 0, &abort_flag)) { ok = false; break; }
+                    if (!wait_one(&empty[s], ((uint32_t)(it / C::kSlots) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
+                    const int last = it - C::kSlots;      // the tile that lay here; Q's place also takes o of its chunk
+                    if (outputs && last >= 0 && last % 3 == 2 && !wait_one(&o_stored[last / 3 & 3], (uint32_t)(last / 3 >> 2) & 1u, &abort_flag)) { ok = false; break; }
                     mbar_expect_tx(&full[s], C::kTile);
-                    const int which = outputs ? kind : 2 * kind;
-                    const CUtensorMap* map = which == 0 ? &maps.k : which == 1 ? &maps.q : &maps.v;
-                    const int hh = h * (which == 0 ? cast.k_h : which == 1 ? cast.q_h : cast.v_h), nn = n * (which == 0 ? cast.k_b : which == 1 ? cast.q_b : cast.v_b);
+                    const CUtensorMap* map = kind == 0 ? &maps.k : kind == 1 ? &maps.v : &maps.q;
+                    const int hh = h * (kind == 0 ? cast.k_h : kind == 1 ? cast.v_h : cast.q_h), nn = n * (kind == 0 ? cast.k_b : kind == 1 ? cast.v_b : cast.q_b);
                     for (int b = 0; b < D / 64; b++) tma_load_4d(smem + s * C::kTile + b * 16384, map, &full[s], 64 * b, t0, hh, nn);
                     issued = it + 1;
+                    // What the ring has no place for yet is on its way into the second-level cache: a copy from memory takes as
+                    // long as half a chunk's work, and Q's place comes free when half of the chunk before is still to do.
+                    if (c + 2 < chunks)
+                        for (int b = 0; b < D / 64; b++) tma_prefetch_4d(map, 64 * b, (int)begin(c + 2), hh, nn);
                 }
             }
-        } else if (warp == 1 && lane == 0) {
+        } else if (warp == 1) {
             constexpr uint32_t kAtom = D == 128 ? 16384u : 0u;      // between the 64-wide parts of K^T; with one part rows 64..127 repeat it
             const uint32_t id_scores = make_instr_desc(kSteps, 0, 0, FP16), id_u = make_instr_desc(D, 1, 1, FP16), id_o = make_instr_desc(D, 0, 1, FP16);
-            int it = 0, sub = 0;
-            bool ok = true;
-            auto wait = [&](uint64_t* bar, int count) {      // for the count-th completion
-                if (ok) ok = mbar_wait(bar, (uint32_t)count & 1u, &abort_flag);
-                if (ok) tcgen05_fence_after();
-                return ok;
-            };
-            for (int c = 0; ok && c < chunks; c++, it += kinds) {
-                const int ik = it, iq = it + 1, iv = it + kinds - 1;
-                const int sk = ik % C::kSlots, sq = iq % C::kSlots, sv = iv % C::kSlots;
-                const uint32_t k = ring + sk * C::kTile, q = ring + sq * C::kTile, v = ring + sv * C::kTile;
-                if (!wait(&full[sk], ik / C::kSlots)) break;
+            // descriptors of the ring's first tile and of the first half buffer; others differ in the address (16-byte units)
+            const uint64_t d_rows = make_smem_desc(ring, 0), d_cols = make_smem_desc(ring, 1, kAtom), d_v = make_smem_desc(ring, 1, 16384u);
+            const uint64_t d_hl = make_smem_desc(hl, 1, C::kRows * 128), d_x = make_smem_desc(sx, 1, D * 128);
+            int sk = 0;
+            uint32_t pk = 0;
+            auto wait = [&](uint64_t* bar, uint32_t parity) { return warp_wait(bar, parity & 1u, &abort_flag); };
+#pragma unroll 1
+            for (int c = 0; c < chunks; c++) {
+                int sv = sk + 1, sq = sk + 2;
+                uint32_t pv = pk, pq = pk;
+                if (sv >= C::kSlots) sv -= C::kSlots, pv ^= 1u;
+                if (sq >= C::kSlots) sq -= C::kSlots, pq ^= 1u;
+                const uint64_t k_rows = d_rows + (uint64_t)(sk * (C::kTile / 16)), q_rows = d_rows + (uint64_t)(sq * (C::kTile / 16));
+                const uint64_t k_cols = d_cols + (uint64_t)(sk * (C::kTile / 16)), v_cols = d_v + (uint64_t)(sv * (C::kTile / 16));
+                if (!wait(&full[sk], pk)) break;
                 if (outputs) {
-                    if (!wait(&full[sq], iq / C::kSlots)) break;
+                    if (!wait(&full[sq], pq)) break;
+                    if (elected()) {
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; kk++) {
-                        const uint32_t at = (kk >> 2) * 16384 + (kk & 3) * 32;
-                        umma_bf16(tmem, make_smem_desc(q + at, 0), make_smem_desc(k + at, 0), id_scores, kk > 0);
+                        for (int kk = 0; kk < D / 16; kk++) {
+                            const uint64_t at = (kk >> 2) * (16384 / 16) + (kk & 3) * (32 / 16);
+                            umma_bf16(tmem, q_rows + at, k_rows + at, id_scores, kk > 0);
+                        }
+                        umma_commit(&scores_full);
                     }
-                    umma_commit(&scores_full);
+                    __syncwarp();
                 }
-                for (int s = 0; s < C::kSub; s++, sub++) {
-                    const int b = sub & 1;
-                    if (!wait(&hl_ready[b], sub >> 1)) break;
+                // U in two halves: while the first frees its buffers, O2
+                if (c > 0 && !wait(&u_free, (uint32_t)(c - 1))) break;
+                tcgen05_fence_after();      // here and below: what was read from or written to tensor memory
+                int s = 0;
+#pragma unroll 1
+                for (; s < C::kSub; s++) {
+                    if (outputs && s == C::kSub / 2) {
+                        if (!wait(&x_ready, (uint32_t)c) || (c > 0 && !wait(&o_free, (uint32_t)(c - 1)))) break;
+                        tcgen05_fence_after();
+                        if (elected()) {
 #pragma unroll
-                    for (int part = 0; part < 2; part++)
+                            for (int kk = 0; kk < D / 16; kk++)
+                                umma_bf16(tmem + C::kO2, q_rows + (kk >> 2) * (16384 / 16) + (kk & 3) * (32 / 16), d_x + kk * (2048 / 16), id_o, kk > 0);
+                            umma_commit(&empty[sq]);
+                        }
+                        __syncwarp();
+                    }
+                    const int b = s & 1;
+                    if (!wait(&hl_ready[b], (uint32_t)((c * C::kSub + s) >> 1))) break;
+                    if (elected()) {
+                        const uint64_t kd = k_cols + (uint64_t)(s * (C::kRows * 128 / 16)), hd = d_hl + (uint64_t)(2 * b * (C::kHalf / 16));
 #pragma unroll
-                        for (int kk = 0; kk < C::kRows / 16; kk++)
-                            umma_bf16(tmem + C::kU, make_smem_desc(k + s * C::kRows * 128 + kk * 2048, 1, kAtom),
-                                      make_smem_desc(hl + (2 * b + part) * C::kHalf + kk * 2048, 1, C::kRows * 128), id_u, (s | part | kk) != 0);
-                    umma_commit(&hl_free[b]);
+                        for (int m = 0; m < 2 * C::kRows / 16; m++) {      // the rounded values, then the rests
+                            const int part = m / (C::kRows / 16), kk = m % (C::kRows / 16);
+                            if (part && !fine) break;
+                            umma_bf16(tmem + C::kU, kd + kk * (2048 / 16), hd + (part * (C::kHalf / 16) + kk * (2048 / 16)), id_u, m > 0 ? 1u : s > 0);
+                        }
+                        umma_commit(&hl_free[b]);
+                    }
+                    __syncwarp();
                 }
-                if (!ok) break;
-                umma_commit(&u_full);
-                umma_commit(&empty[sk]);
-                if (outputs) {
-                    if (!wait(&full[sv], iv / C::kSlots) || !wait(&p_ready, c) || !wait(&s_ready, c)) break;
-#pragma unroll
-                    for (int kk = 0; kk < kSteps / 16; kk++)
-                        umma_a_tmem(tmem + C::kO1, tmem + 8 * kk, make_smem_desc(v + kk * 2048, 1, 16384u), id_o, kk > 0);
-#pragma unroll
-                    for (int kk = 0; kk < D / 16; kk++)
-                        umma_bf16(tmem + C::kO2, make_smem_desc(q + (kk >> 2) * 16384 + (kk & 3) * 32, 0), make_smem_desc(sx + kk * 2048, 1, D * 128), id_o, kk > 0);
-                    umma_commit(&o_full);
-                    umma_commit(&empty[sq]);
+                if (s < C::kSub) break;
+                if (elected()) {
+                    umma_commit(&u_full);
+                    umma_commit(&empty[sk]);
                 }
-                umma_commit(&empty[sv]);
+                __syncwarp();
+                if (outputs && (!wait(&full[sv], pv) || !wait(&p_ready, (uint32_t)c))) break;
+                tcgen05_fence_after();
+                if (elected()) {
+                    if (outputs) {
+#pragma unroll
+                        for (int kk = 0; kk < kSteps / 16; kk++) umma_tmem(tmem + C::kO1, tmem + 8 * kk, v_cols + kk * (2048 / 16), id_o, kk > 0);
+                        umma_commit(&o_full);
+                    }
+                    umma_commit(&empty[sv]);
+                }
+                __syncwarp();
+                sk += kinds;
+                if (sk >= C::kSlots) sk -= C::kSlots, pk ^= 1u;
             }
         } else if (FP16 && warp >= 2) {
-            // the largest magnitudes of K, Q and V, half of each tile a warp
+            // the largest magnitudes of K, V and Q, half of each tile a warp
             int it = 0;
             bool ok = true;
+#pragma unroll 1
             for (int c = 0; ok && c < chunks; c++) {
                 for (int kind = 0; ok && kind < kinds; kind++, it++) {
                     const int s = it % C::kSlots;
@@ -291,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                     uint32_t m = __reduce_max_sync(0xffffffffu, max(lo, hi >> 16));
                     if (lane == 0) {
                         if (m >= 0x7c00u) atomicOr(&found, 1u);
-                        most[c & 3][warp - 2][outputs ? kind : 2 * kind] = __half2float(__ushort_as_half((unsigned short)m));
+                        most[c & 3][warp - 2][kind] = __half2float(__ushort_as_half((unsigned short)m));
                     }
                 }
                 if (ok && lane == 0) mbar_arrive(&max_ready[c & 3]);
@@ -299,146 +453,95 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
             }
         }
     } else if (warp < 8) {
-        if (D == 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 160;");
+        if (D == 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (outputs) {
             const int q = warp & 3, i = 32 * q + lane;
             const uint32_t rows = tmem + ((uint32_t)(q * 32) << 16);
-            const float g = pw[1];
-            uint8_t* out = static_cast<uint8_t*>(a.o) + 2 * ((long long)n * a.o_b + (long long)h * a.o_h);
+            const float g = pw[1], g2 = g * g;
             uint32_t f[4];
             flags_of(0, f);
-            float e_now = 0.0f, e_before = 0.0f, p_back = 1.0f, p_back_before = 1.0f;
-            bool enters = false, entered = false, ok = true;
-            // o of chunk c: what its tensor-memory halves say, scaled
-            auto epilogue = [&](int c, float e, bool reached, float pb) {
-                if (!warp_wait(&o_full, (uint32_t)c & 1u, &abort_flag)) return false;
-                tcgen05_fence_after();
-                const long long t0 = begin(c);
-                const bool live = i < length(t0);
-                if (FP16) e *= back_s[c & 1];
-                uint8_t* row = out + 2 * (t0 + i) * a.o_t;
 #pragma unroll 1
-                for (int b = 0; b < D; b += 32) {
-                    uint32_t x[32], y[32];
-                    tmem_ld32(rows + C::kO1 + b, x);
-                    tmem_ld32(rows + C::kO2 + b, y);
-                    const int valid = a.dv - b;
-                    if (live && valid > 0) {
-                        uint32_t o[16];
-#pragma unroll
-                        for (int j = 0; j < 16; j++) {
-                            float u = __uint_as_float(x[2 * j]), v = __uint_as_float(x[2 * j + 1]);
-                            if (FP16) u *= pb, v *= pb;
-                            if (reached) {
-                                u = fmaf(e, __uint_as_float(y[2 * j]), u);
-                                v = fmaf(e, __uint_as_float(y[2 * j + 1]), v);
-                            }
-                            o[j] = pack<FP16>(u, v);
-                        }
-                        uint16_t* to = reinterpret_cast<uint16_t*>(row) + b;
-                        if (valid >= 32 && wide == 2) {
-                            st_global_v8(to, &o[0]);
-                            st_global_v8(to + 16, &o[8]);
-                        } else if (wide) {
-#pragma unroll
-                            for (int j = 0; j < 4; j++)
-                                if (8 * j + 8 <= valid) {
-                                    reinterpret_cast<uint4*>(to)[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
-                                } else {
-#pragma unroll
-                                    for (int m = 8 * j; m < 8 * j + 8; m++)
-                                        if (m < valid) to[m] = (uint16_t)(m & 1 ? o[m / 2] >> 16 : o[m / 2]);
-                                }
-                        } else {
-#pragma unroll
-                            for (int m = 0; m < 32; m++)
-                                if (m < valid) to[m] = (uint16_t)(m & 1 ? o[m / 2] >> 16 : o[m / 2]);
-                        }
-                    }
-                    __syncwarp();      // the next load from tensor memory is the whole warp's
-                }
-                return true;
-            };
             for (int c = 0; c < chunks; c++) {
                 const Links links = links_of(f);
                 flags_of(c + 1, f);
-                const long long t0 = begin(c);
-                const int len = length(t0);
+                const int len = length(begin(c));
                 // the row sees columns lo..hi
-                int lo, hi;
-                if (REV) {
-                    const int cut = links.lowest(i);
-                    lo = i;
-                    hi = min(cut, len - 1);
-                    enters = cut == 128;
-                    e_now = a.out * pw[max(0, len - 1 - i) + entry_power(c)];
-                } else {
-                    const int cut = links.highest(i);
-                    lo = max(cut, 0);
-                    hi = i;
-                    enters = cut < 0;
-                    e_now = a.out * pw[i + 1];
-                }
-                float base = a.in * a.out;
+                const int lo = REV ? i : max(links.highest(i), 0), hi = REV ? min(links.lowest(i), len - 1) : i;
+                float base = a.in * a.out, back;
                 if (FP16) {
-                    if (!warp_wait(&max_ready[c & 3], (uint32_t)(c >> 2) & 1u, &abort_flag)) { ok = false; break; }
-                    const float(&m)[2][3] = most[c & 3];
-                    base *= fit((float)D * fmaxf(m[0][0], m[1][0]) * fmaxf(m[0][1], m[1][1]) * fabsf(base), p_back);
+                    float m[3];
+                    if (!most_of(c, m)) break;
+                    base *= fit((float)D * m[0] * m[2] * fabsf(base), back);
                 }
-                if (!warp_wait(&scores_full, (uint32_t)c & 1u, &abort_flag)) { ok = false; break; }
-                tcgen05_fence_after();
                 const bool all_seen = __all_sync(0xffffffffu, REV ? hi == kSteps - 1 : lo == 0);
-#pragma unroll 1
-                for (int b = 0; b < 4; b++) {
-                    uint32_t p[16];
-                    if (REV ? b < q : b > q) {
+                if (!warp_wait(&scores_full, (uint32_t)c & 1u, &abort_flag)) break;
+                tcgen05_fence_after();
+                // 16 columns at a time, the next 16 under way.  P's columns never reach scores that are still to be read.
+                auto weigh = [&](int t, uint32_t (&s)[16]) {
+                    uint32_t p[8];
+                    if (all_seen && (REV ? t > 2 * q + 1 : t < 2 * q)) {
+                        // every step of the warp sees all of these: powers fall away from the column next to it, in two chains
+                        float x = pw[REV ? 16 * t - i : i - 16 * t - 15] * base, y = x * g;
 #pragma unroll
-                        for (int j = 0; j < 16; j++) p[j] = 0;
-                    } else {
-                        uint32_t s[32];
-                        tmem_ld32(rows + 32 * b, s);
-                        const int lane_lo = lo - 32 * b, lane_hi = hi - 32 * b;      // of this batch's columns
-                        float x = REV ? pw[max(0, 32 * b - i)] * base : pw[max(0, i - 32 * b - 31)] * base;
-                        if (b != q && all_seen) {
-#pragma unroll
-                            for (int m = 0; m < 32; m++) {
-                                const int j = REV ? m : 31 - m;
-                                s[j] = __float_as_uint(__uint_as_float(s[j]) * x);
-                                x *= g;
-                            }
-                        } else {
-#pragma unroll
-                            for (int m = 0; m < 32; m++) {
-                                const int j = REV ? m : 31 - m;
-                                if (b == q && j == lane) x = base;
-                                s[j] = j >= lane_lo && j <= lane_hi ? __float_as_uint(__uint_as_float(s[j]) * x) : 0u;
-                                x *= g;
-                            }
+                        for (int m = 0; m < 16; m += 2) {
+                            const int j = REV ? m : 15 - m, k = REV ? m + 1 : 14 - m;
+                            s[j] = __float_as_uint(__uint_as_float(s[j]) * x);
+                            s[k] = __float_as_uint(__uint_as_float(s[k]) * y);
+                            x *= g2;
+                            y *= g2;
                         }
+                    } else {
+                        float x = pw[max(0, REV ? 16 * t - i : i - 16 * t - 15)] * base;
 #pragma unroll
-                        for (int j = 0; j < 16; j++) p[j] = pack<FP16>(__uint_as_float(s[2 * j]), __uint_as_float(s[2 * j + 1]));
+                        for (int m = 0; m < 16; m++) {
+                            const int j = REV ? m : 15 - m;
+                            if (16 * t + j == i) x = base;
+                            s[j] = 16 * t + j >= lo && 16 * t + j <= hi ? __float_as_uint(__uint_as_float(s[j]) * x) : 0u;
+                            x *= g;
+                        }
                     }
-                    tmem_st16(rows + 16 * b, p);
+#pragma unroll
+                    for (int j = 0; j < 8; j++) p[j] = pack<FP16>(__uint_as_float(s[2 * j]), __uint_as_float(s[2 * j + 1]));
+                    tmem_st8(rows + 8 * t, p);
+                };
+                const int from = REV ? 2 * q : 0, to = REV ? 8 : 2 * q + 2;      // the others: no step of the warp sees them
+                uint32_t s0[16], s1[16];
+                tmem_ld16_issue(rows + 16 * from, s0);
+                const uint32_t zero[8] = {};
+#pragma unroll 1
+                for (int t = 0; t < (REV ? from : 0); t++)
+                    tmem_st8(rows + 8 * t, zero);
+#pragma unroll 1
+                for (int t = from; t < to; t += 2) {
+                    tmem_ld16_wait(s0);
+                    tmem_ld16_issue(rows + 16 * (t + 1), s1);
+                    weigh(t, s0);
+                    tmem_ld16_wait(s1);
+                    if (t + 2 < to) tmem_ld16_issue(rows + 16 * (t + 2), s0);
+                    weigh(t + 1, s1);
                 }
+                if (!REV)
+#pragma unroll 1
+                    for (int t = to; t < 8; t++) tmem_st8(rows + 8 * t, zero);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                if (c > 0 && !epilogue(c - 1, e_before, entered, p_back_before)) { ok = false; break; }
                 tcgen05_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&p_ready);
-                e_before = e_now;
-                entered = enters;
-                p_back_before = p_back;
             }
-            if (ok && chunks > 0) epilogue(chunks - 1, e_before, entered, p_back_before);
         }
-    } else {
-        if (D == 128) asm volatile("setmaxnreg.inc.sync.aligned.u32 240;");
+    } else if (warp < 12) {
+        if (D == 128) asm volatile("setmaxnreg.inc.sync.aligned.u32 248;");
         const int tid = threadIdx.x - 256, q = warp & 3;
         const int row = D == 128 ? tid : tid & 63, col = D == 128 ? 0 : (tid >> 6) * 32;      // X[row][col ...]
         const uint32_t rows = tmem + ((uint32_t)(q * 32) << 16);
         const long long size = (long long)a.dk * a.dv, state = unit * size;
         float X[C::kHeld];
         float bound = 0.0f;      // float16: of |X|
+        // A state passes through the ring's places behind the first chunk's (and out through the memory of the weighted values and
+        // of X's operand), asynchronously, 16 bytes of its contiguous axis at a time (a thread of its own row would touch 32 rows an access: 12 us for 128 x 128): entry `fast` of its row
+        // `slow` as word (fast / 4 ^ slow % (D / 4)) * 4 + fast % 4.
+        uint32_t stage = ring + 3 * C::kTile;
+        auto staged = [&](int slow, int fast) { return stage + slow * (D * 4) + ((((fast >> 2) ^ slow) & (D / 4 - 1)) << 4) + (fast & 3) * 4; };
         {
             const float* from = nullptr;
             int fc = a.first_c, fd = a.first_d;
@@ -449,23 +552,60 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                 fc = a.dv;
                 fd = 1;
             }
-            from = from && row < a.dk ? from + (long long)row * fc : nullptr;
+            if (from) {
+                const bool rows_lie = fd == 1;
+                const int n_slow = rows_lie ? a.dk : a.dv, n_fast = rows_lie ? a.dv : a.dk, ld = rows_lie ? fc : fd;
+                if (n_fast % 4 == 0 && (reinterpret_cast<uintptr_t>(from) & 15) == 0) {
+                    const int fast = tid % (D / 4) * 4;
+                    int slow = tid / (D / 4);
+                    const float* at = from + (long long)slow * ld + fast;
+#pragma unroll 4
+                    for (int e = 0; e < D * D / 512; e++, slow += 512 / D, at += (512 / D) * ld) {
+                        const bool in = slow < n_slow && fast < n_fast;
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(staged(slow, fast)), "l"(in ? at : from), "r"(in ? 16 : 0) : "memory");
+                    }
+                } else {
+#pragma unroll 1
+                    for (int e = tid; e < D * D; e += 128) {
+                        const int slow = e / D, fast = e % D;
+                        const bool in = slow < n_slow && fast < n_fast;
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(staged(slow, fast)), "l"(in ? from + (long long)slow * ld + fast : from), "r"(in ? 4 : 0) : "memory");
+                    }
+                }
+                asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
+                asm volatile("bar.sync 3, 128;" ::: "memory");
+                if (rows_lie) {
 #pragma unroll
-            for (int j = 0; j < C::kHeld; j++) X[j] = from && col + j < a.dv ? from[(long long)(col + j) * fd] : 0.0f;
+                    for (int j = 0; j < C::kHeld; j += 4) {
+                        const uint4 w = ld_shared(staged(row, col + j));
+                        X[j] = __uint_as_float(w.x), X[j + 1] = __uint_as_float(w.y), X[j + 2] = __uint_as_float(w.z), X[j + 3] = __uint_as_float(w.w);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < C::kHeld; j++) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(X[j]) : "r"(staged(col + j, row)) : "memory");
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < C::kHeld; j++) X[j] = 0.0f;
+            }
             if (FP16) {
 #pragma unroll
                 for (int j = 0; j < C::kHeld; j++) bound = fmaxf(bound, fabsf(X[j]));
                 bound = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(bound)));
                 if (lane == 0) first_most[q] = bound;
-                asm volatile("bar.sync 2, 128;" ::: "memory");
+                asm volatile("bar.sync 3, 128;" ::: "memory");
                 bound = fmaxf(fmaxf(first_most[0], first_most[1]), fmaxf(first_most[2], first_most[3]));
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&x_taken);
+            stage = hl;
         }
-        auto publish = [&](int c) {      // X as the operand of chunk c
-            float up = 1.0f, back = 1.0f;
+        float x_back = 1.0f;
+        auto publish = [&](int next) {      // X as the operand of that chunk
+            float up = 1.0f;
             if (FP16) {
-                up = fit(bound, back);
-                if (tid == 0) back_s[c & 1] = back;
+                up = fit(bound, x_back);
+                if (tid == 0) x_backs[next & 1] = x_back;
             }
 #pragma unroll
             for (int m = 0; m < C::kHeld / 8; m++) {
@@ -475,94 +615,78 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                     const float u = X[8 * m + 2 * j], v = X[8 * m + 2 * j + 1];
                     w[j] = FP16 ? pack<FP16>(u * up, v * up) : pack<FP16>(u, v);
                 }
-                const int piece16 = col / 8 + m;
-                st_shared(sx + (piece16 >> 3) * (D * 128) + row * 128 + (((piece16 & 7) ^ (row & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+                const int part = col / 8 + m;
+                st_shared(sx + (part >> 3) * (D * 128) + row * 128 + (((part & 7) ^ (row & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
             }
             proxy_fence();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&s_ready);
+            if (lane == 0) mbar_arrive(&x_ready);
+        };
+        // NaN or infinity in X, which stays there until a flag drops it
+        auto look = [&]() {
+            float seen = 0.0f;
+#pragma unroll
+            for (int j = 0; j < C::kHeld; j++) seen = fmaf(X[j], 0.0f, seen);
+            if (seen != 0.0f || (FP16 && !(bound <= 3e38f))) atomicOr(&found, 1u);
         };
         if (outputs && chunks > 0) publish(0);
+        const int i = 32 * q + lane;      // row of o
         uint32_t f[4];
         flags_of(0, f);
-        uint32_t seen = 0;
-        float seen_u = 0.0f;
-        bool dropped = false, ok = true;
-        int sub = 0;
-        for (int c = 0; ok && c < chunks; c++) {
+        bool dropped = false;
+#pragma unroll 1
+        for (int c = 0; c < chunks; c++) {
             const Links links = links_of(f);
             flags_of(c + 1, f);
             const long long t0 = begin(c);
             const int len = length(t0);
-            // the steps that reach the chunk's end
-            const int lo = REV ? 0 : max(links.highest(kSteps - 1), 0), hi = REV ? min(links.lowest(0), len - 1) : len - 1;
-            float gain = a.in, back = 1.0f;
-            const int iv = c * kinds + kinds - 1, sv = iv % C::kSlots;
-            if (FP16) {
-                if (!warp_wait(&max_ready[c & 3], (uint32_t)(c >> 2) & 1u, &abort_flag)) { ok = false; break; }
-                const float(&m)[2][3] = most[c & 3];
-                const float mv = fmaxf(m[0][2], m[1][2]) * fabsf(a.in);
-                gain *= fit(mv, back);
-                bound = (links.any() ? 0.0f : bound) + (float)kSteps * fmaxf(m[0][0], m[1][0]) * mv;
-            }
-            if (!warp_wait(&full[sv], (uint32_t)(iv / C::kSlots) & 1u, &abort_flag)) { ok = false; break; }
-            for (int s = 0; s < C::kSub; s++, sub++) {
-                const int b = sub & 1;
-                if (!warp_wait(&hl_free[b], (((uint32_t)sub >> 1) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
-#pragma unroll
-                for (int m = 0; m < 4; m++) {
-                    const int idx = m * 128 + tid;                      // 16-byte part of the rows, box after box
-                    const int box = idx / (C::kRows * 8), in = idx - box * (C::kRows * 8), j = s * C::kRows + (in >> 3);
-                    const uint4 w = ld_shared(ring + sv * C::kTile + box * 16384 + s * C::kRows * 128 + in * 16);
-                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-                    const bool keep = j >= lo && j <= hi;
-                    const float g = keep ? pw[REV ? j : len - 1 - j] * gain : 0.0f;
-                    uint32_t r[4], d[4];
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        seen = note<FP16>(u[e], seen);
-                        const float2 x = unpack<FP16>(u[e]);
-                        const float x0 = x.x * g, x1 = x.y * g;
-                        r[e] = pack<FP16>(x0, x1);
-                        const float2 y = unpack<FP16>(r[e]);
-                        d[e] = pack<FP16>(x0 - y.x, x1 - y.y);
-                        if (!keep) r[e] = d[e] = 0u;
-                    }
-                    st_shared(hl + 2 * b * C::kHalf + idx * 16, make_uint4(r[0], r[1], r[2], r[3]));
-                    st_shared(hl + (2 * b + 1) * C::kHalf + idx * 16, make_uint4(d[0], d[1], d[2], d[3]));
-                }
-                proxy_fence();
-                tcgen05_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&hl_ready[b]);
-            }
-            if (!ok) break;
-            if (!warp_wait(&u_full, (uint32_t)c & 1u, &abort_flag)) { ok = false; break; }
-            tcgen05_fence_after();
             const bool drop = links.any();
-            dropped |= drop;
-            const float carry = pw[len - 1 + entry_power(c)];
+            const float carry = pw[len - 1 + entry_power(c)], x_was = x_back;
+            float u_back = 1.0f, p_back = 1.0f;
+            if (FP16) {
+                float m[3];
+                if (!most_of(c, m)) break;
+                const float mv = m[1] * fabsf(a.in);
+                fit(mv, u_back);
+                fit((float)D * m[0] * m[2] * fabsf(a.in * a.out), p_back);
+                if (drop) look();
+                bound = (drop ? 0.0f : carry * bound) + (float)kSteps * m[0] * mv;
+            } else if (drop) {
+                look();
+            }
+            if (!warp_wait(&u_full, (uint32_t)c & 1u, &abort_flag)) break;
+            tcgen05_fence_after();
+            if (drop) {
+                dropped = true;
 #pragma unroll
-            for (int b = 0; b < C::kHeld; b += 32) {
-                uint32_t u[32];
-                tmem_ld32(rows + C::kU + col + b, u);
+                for (int j = 0; j < C::kHeld; j++) X[j] = 0.0f;
+            }
 #pragma unroll
-                for (int j = 0; j < 32; j++) {
+            for (int b = 0; b < C::kHeld; b += 16) {
+                uint32_t u[16];
+                tmem_ld16_issue(rows + C::kU + col + b, u);
+                tmem_ld16_wait(u);
+#pragma unroll
+                for (int j = 0; j < 16; j++) {
                     float x = __uint_as_float(u[j]);
-                    seen_u = fmaf(x, 0.0f, seen_u);
-                    if (FP16) x *= back;
-                    X[b + j] = drop ? x : fmaf(carry, X[b + j], x);
+                    if (FP16) x *= u_back;
+                    X[b + j] = fmaf(carry, X[b + j], x);
                 }
             }
-            if (outputs && c + 1 < chunks) {
-                if (!warp_wait(&o_full, (uint32_t)c & 1u, &abort_flag)) { ok = false; break; }      // the product with the X before
-                tcgen05_fence_before();
-                publish(c + 1);
-            }
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&u_free);
+            if (!outputs) continue;
+            if (!warp_wait(&o_full, (uint32_t)c & 1u, &abort_flag)) break;      // the product with the X before, too
+            tcgen05_fence_after();
+            if (c + 1 < chunks) publish(c + 1);
+            float e;
+            const bool reached = reach_of(links, c, len, i, e);
+            if (FP16) e *= x_was;
+            put_o(c, 0, rows, t0, len, reached, e, p_back);
         }
-        const float2 v = unpack<FP16>(seen);
-        if (!(v.x == 0.0f && v.y == 0.0f && seen_u == 0.0f && (!FP16 || bound <= 3e38f))) atomicOr(&found, 1u);
-        asm volatile("bar.sync 2, 128;" ::: "memory");
+        look();
+        asm volatile("bar.sync 2, 256;" ::: "memory");      // warps 12-15 have seen all of V
         const bool flagged = *static_cast<volatile uint32_t*>(&found) != 0;
         if (outputs && tid == 0) a.flags[(long long)piece * units + unit] = flagged;
         float* to = nullptr;
@@ -579,16 +703,140 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                 ldd = a.last_d;
             }
         }
-        if (to && row < a.dk) {
+        if (to) {
             const bool zero = outputs && !REV && done && done[(a.steps - 1) * a.done_t];
             const float g = outputs && REV ? pw[1] : 1.0f;
-            to += (long long)row * lc;
 #pragma unroll
-            for (int j = 0; j < C::kHeld; j++)
-                if (col + j < a.dv) to[(long long)(col + j) * ldd] = zero ? 0.0f : g * X[j];
+            for (int j = 0; j < C::kHeld; j++) X[j] = zero ? 0.0f : g * X[j];
+            const bool rows_lie = ldd == 1;
+            const int n_slow = rows_lie ? a.dk : a.dv, n_fast = rows_lie ? a.dv : a.dk, ld = rows_lie ? lc : ldd;
+            if (rows_lie) {
+#pragma unroll
+                for (int j = 0; j < C::kHeld; j += 4)
+                    st_shared(staged(row, col + j), make_uint4(__float_as_uint(X[j]), __float_as_uint(X[j + 1]), __float_as_uint(X[j + 2]), __float_as_uint(X[j + 3])));
+            } else {
+#pragma unroll
+                for (int j = 0; j < C::kHeld; j++) asm volatile("st.shared.f32 [%0], %1;" ::"r"(staged(col + j, row)), "f"(X[j]) : "memory");
+            }
+            asm volatile("bar.sync 3, 128;" ::: "memory");
+            if (n_fast % 4 == 0 && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
+                const int fast = tid % (D / 4) * 4;
+                int slow = tid / (D / 4);
+                float* at = to + (long long)slow * ld + fast;
+#pragma unroll 4
+                for (int e = 0; e < D * D / 512; e++, slow += 512 / D, at += (512 / D) * ld)
+                    if (slow < n_slow && fast < n_fast) *reinterpret_cast<uint4*>(at) = ld_shared(staged(slow, fast));
+            } else {
+#pragma unroll 1
+                for (int e = tid; e < D * D; e += 128) {
+                    const int slow = e / D, fast = e % D;
+                    float x;
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(staged(slow, fast)) : "memory");
+                    if (slow < n_slow && fast < n_fast) to[(long long)slow * ld + fast] = x;
+                }
+            }
         }
-        tcgen05_fence_before();
+    } else {
+        if (D == 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+        const int tid = threadIdx.x - 384, q = warp & 3, i = 32 * q + lane;
+        const uint32_t rows = tmem + ((uint32_t)(q * 32) << 16);
+        uint32_t f[4];
+        flags_of(0, f);
+        uint32_t seen = 0;
+        int sub = 0, sv = 1;
+        uint32_t pv = 0;
+        Links links = {}, before = {};
+        // half a chunk's weighted values at a time; when the first half of the next chunk's stand ready, half of the chunk's o
+#pragma unroll 1
+        for (int half = 0; half <= 2 * chunks; half++) {
+            const int c = half >> 1;
+            if (c < chunks) {
+                if (!(half & 1)) {
+                    before = links;
+                    links = links_of(f);
+                    flags_of(c + 1, f);
+                    if (!warp_wait(&full[sv], pv, &abort_flag)) break;
+                }
+                const int len = length(begin(c));
+                // the steps that reach the chunk's end
+                const int lo = REV ? 0 : max(links.highest(kSteps - 1), 0), hi = REV ? min(links.lowest(0), len - 1) : len - 1;
+                float gain = a.in;
+                if (FP16) {
+                    float m[3], back;
+                    if (!most_of(c, m)) break;
+                    gain *= fit(m[1] * fabsf(a.in), back);
+                }
+                const uint32_t v = ring + sv * C::kTile + tid * 16;
+                bool ok = true;
+#pragma unroll 1
+                for (int s = (half & 1) * (C::kSub / 2); s < ((half & 1) + 1) * (C::kSub / 2); s++, sub++) {
+                    const int b = sub & 1;
+                    uint4 w[4];
+                    float g[4];
+#pragma unroll
+                    for (int m = 0; m < 4; m++) {      // 16-byte parts of the rows, box after box
+                        const int box = m * 128 / (C::kRows * 8), in = (m * 128) % (C::kRows * 8) / 8;
+                        w[m] = ld_shared(v + box * 16384 + s * C::kRows * 128 + in * 128);
+                        const int j = s * C::kRows + in + (tid >> 3);
+                        g[m] = j >= lo && j <= hi ? pw[REV ? j : len - 1 - j] * gain : 0.0f;
+                    }
+                    if (!warp_wait(&hl_free[b], (((uint32_t)sub >> 1) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
+                    const uint32_t to = hl + 2 * b * C::kHalf + tid * 16;
+#pragma unroll
+                    for (int m = 0; m < 4; m++) {
+                        const uint32_t u[4] = {w[m].x, w[m].y, w[m].z, w[m].w};
+                        uint32_t r[4], d[4];
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            seen = note<FP16>(u[e], seen);
+                            const float2 x = unpack<FP16>(u[e]);
+                            r[e] = pack<FP16>(x.x * g[m], x.y * g[m]);
+                        }
+                        st_shared(to + m * 2048, make_uint4(r[0], r[1], r[2], r[3]));
+                        if (fine) {
+#pragma unroll
+                            for (int e = 0; e < 4; e++) {
+                                const float2 x = unpack<FP16>(u[e]), y = unpack<FP16>(r[e]);
+                                d[e] = pack<FP16>(fmaf(x.x, g[m], -y.x), fmaf(x.y, g[m], -y.y));
+                            }
+                            st_shared(to + C::kHalf + m * 2048, make_uint4(d[0], d[1], d[2], d[3]));
+                        }
+                    }
+                    proxy_fence();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&hl_ready[b]);
+                }
+                if (!ok) break;
+                if (half & 1) {
+                    sv += kinds;
+                    if (sv >= C::kSlots) sv -= C::kSlots, pv ^= 1u;
+                }
+            } else {
+                before = links;
+            }
+            if (outputs && half > 0 && !(half & 1)) {
+                const int o = c - 1;
+                const long long t0 = begin(o);
+                const int len = length(t0);
+                float e, p_back = 1.0f;
+                const bool reached = reach_of(before, o, len, i, e);
+                if (FP16) {
+                    float m[3];
+                    if (!most_of(o, m)) break;
+                    fit((float)D * m[0] * m[2] * fabsf(a.in * a.out), p_back);
+                }
+                if (!warp_wait(&o_full, (uint32_t)o & 1u, &abort_flag)) break;
+                tcgen05_fence_after();
+                if (FP16) e *= x_backs[o & 1];
+                put_o(o, 1, rows, t0, len, reached, e, p_back);
+            }
+        }
+        const float2 y = unpack<FP16>(seen);
+        if (!(y.x == 0.0f && y.y == 0.0f)) atomicOr(&found, 1u);
+        asm volatile("bar.sync 2, 256;" ::: "memory");
     }
+    if (warp >= 8 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    tcgen05_fence_before();
     __syncthreads();
     if (abort_flag && threadIdx.x == 0) {      // copies already issued land before the shared memory goes away
         if (a.status) atomicExch(a.status, 1);
@@ -608,17 +856,17 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
 
 // [sequence][head][step][width], boxes of 64 entries x 128 steps; what lies outside reads as zero.  An axis of stride 0 (or of
 // one entry) has one coordinate.
-bool map_of(CUtensorMap* m, const MemoryOperand& o, long long steps, long long batch, int heads, int width, int& cast_b, int& cast_h) {
+bool map_of(CUtensorMap* m, const MemoryOperand& o, long long steps, long long batch, int heads, int width, int& cast_b, int& cast_h, uint32_t box_width = 64, uint32_t box_steps = kSteps) {
     const uint64_t row = ((uint64_t)width + 7) / 8 * 16;
     cast_b = o.b != 0;
     cast_h = o.h != 0;
     const uint64_t dims[4] = {(uint64_t)width, (uint64_t)steps, cast_h ? (uint64_t)heads : 1, cast_b ? (uint64_t)batch : 1};
     const uint64_t strides[3] = {o.t ? (uint64_t)o.t * 2 : row, o.h ? (uint64_t)o.h * 2 : row, o.b ? (uint64_t)o.b * 2 : row};
-    const uint32_t box[4] = {64, kSteps, 1, 1};
-    return make_tensor_map_nd(m, o.p, 4, dims, strides, box);
+    const uint32_t box[4] = {box_width, box_steps, 1, 1};
+    return make_tensor_map_nd(m, o.p, 4, dims, strides, box, box_width == 64 ? 0 : 1);
 }
 
-template <int D, bool FP16, bool REV> cudaError_t launch_chunks(const ChunkMaps& maps, const MemoryPass& a, const Broadcast& cast, cudaStream_t st) {
+template <int D, bool FP16, bool REV> cudaError_t launch_chunks(const ChunkMaps& maps, const MemoryPass& a, const Broadcast& cast, int wide, cudaStream_t st) {
     constexpr int smem = Chunk<D>::kBytes + 1024;
     static bool ready[64] = {};
     int dev = 0;
@@ -630,8 +878,7 @@ template <int D, bool FP16, bool REV> cudaError_t launch_chunks(const ChunkMaps&
         if (e != cudaSuccess) return e;
         ready[dev] = true;
     }
-    const int align = !a.o ? 0 : a.o_t % 16 == 0 && a.o_b % 16 == 0 && a.o_h % 16 == 0 && aligned(a.o, 32) ? 2 : a.o_t % 8 == 0 && a.o_b % 8 == 0 && a.o_h % 8 == 0 && aligned(a.o, 16) ? 1 : 0;
-    return launch_pdl(memory_chunk_kernel<D, FP16, REV>, dim3((unsigned)(a.batch * a.heads * a.pieces)), dim3(kThreads), (size_t)smem, st, maps, a, cast, align);
+    return launch_pdl(memory_chunk_kernel<D, FP16, REV>, dim3((unsigned)(a.batch * a.heads * a.pieces)), dim3(kThreads), (size_t)smem, st, maps, a, cast, wide);
 }
 
 }  // namespace
@@ -661,14 +908,18 @@ cudaError_t memory_chunks(const MemoryPass& a, int dtype, bool& mapped, cudaStre
     if (e != cudaSuccess) return e;
     mapped = map_of(&maps.q, a.q, a.steps, a.batch, a.heads, a.dk, cast.q_b, cast.q_h) && map_of(&maps.k, a.k, a.steps, a.batch, a.heads, a.dk, cast.k_b, cast.k_h) &&
              map_of(&maps.v, a.v, a.steps, a.batch, a.heads, a.dv, cast.v_b, cast.v_h);
+    const bool fp16 = dtype == GALA_F16, large = a.dk > 64 || a.dv > 64;
+    const MemoryOperand o = {a.o, a.o_t, a.o_b, a.o_h};
+    const int wide = aligned(a.o, 16) && a.o_t % 8 == 0 && a.o_b % 8 == 0 && a.o_h % 8 == 0;      // o too goes by tensor copies
+    if (mapped && wide) mapped = map_of(&maps.o, o, a.steps, a.batch, a.heads, a.dv, cast.o_b, cast.o_h, large ? 64 : 32, 32);
+    else maps.o = maps.q;
     if (!mapped) return cudaSuccess;
-    const bool fp16 = dtype == GALA_F16;
-    if (a.dk > 64 || a.dv > 64) {
-        if (a.rev) return fp16 ? launch_chunks<128, true, true>(maps, a, cast, st) : launch_chunks<128, false, true>(maps, a, cast, st);
-        return fp16 ? launch_chunks<128, true, false>(maps, a, cast, st) : launch_chunks<128, false, false>(maps, a, cast, st);
+    if (large) {
+        if (a.rev) return fp16 ? launch_chunks<128, true, true>(maps, a, cast, wide, st) : launch_chunks<128, false, true>(maps, a, cast, wide, st);
+        return fp16 ? launch_chunks<128, true, false>(maps, a, cast, wide, st) : launch_chunks<128, false, false>(maps, a, cast, wide, st);
     }
-    if (a.rev) return fp16 ? launch_chunks<64, true, true>(maps, a, cast, st) : launch_chunks<64, false, true>(maps, a, cast, st);
-    return fp16 ? launch_chunks<64, true, false>(maps, a, cast, st) : launch_chunks<64, false, false>(maps, a, cast, st);
+    if (a.rev) return fp16 ? launch_chunks<64, true, true>(maps, a, cast, wide, st) : launch_chunks<64, false, true>(maps, a, cast, wide, st);
+    return fp16 ? launch_chunks<64, true, false>(maps, a, cast, wide, st) : launch_chunks<64, false, false>(maps, a, cast, wide, st);
 }
 
 }  // namespace gala

@@ -1,9 +1,9 @@
 // Attention with a memory of fixed size, step by step, and the C entry points, for sm_100a.
 //
-// memory_steps_kernel holds the state of a sequence and head in registers: a thread has one column of it (an entry of v and
-// o) for all rows (entries of q and k), two rows a packed instruction, so that o needs no exchange between threads.  k and q of
-// the next few steps are brought into shared memory, in float32, while this batch of steps is computed; every thread reads them
-// as broadcasts.  A step is three instructions for two entries of the state:
+// memory_steps_kernel, for long calls in float32 or on odd addresses: a thread has one column of the state (an entry of v and o)
+// for all rows (entries of q and k) in registers, two rows a packed instruction, so that o needs no exchange between threads.
+// k, q and v of 32 steps are brought into shared memory at once, in float32; k and q are read as broadcasts.  A step is three
+// instructions for two entries of the state:
 //   t = X + k v;  X = t + (g - 1) X   where g >= 1/2: g - 1 has all its digits, so that a long memory does not drift, and
 //   X = g X + k v                     below, where the difference would cancel;    o += q X.
 #include "linear_attention.cuh"
@@ -33,20 +33,23 @@ __device__ __forceinline__ f2 mul2(f2 a, f2 b) {
     return r;
 }
 
-// One block: 32 W columns of one unit (sequence and head) over one piece of the time axis.
+constexpr int kStaged = 32;      // steps brought in at once
+
+// One block of 32 W >= dv threads: one unit (sequence and head) over one piece of the time axis.
 template <typename T, int DK, int W>
 __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a) {
-    constexpr int TS = 2 * W;                       // steps brought in at once
-    constexpr int kLoads = TS * DK / (32 * W);      // of k, and of q, a thread
-    __shared__ __align__(16) float ks[TS][DK], qs[TS][DK];
-    __shared__ float vs[TS][32 * W];
+    extern __shared__ __align__(16) float staged[];
+    float (*ks)[DK] = reinterpret_cast<float (*)[DK]>(staged);
+    float (*qs)[DK] = ks + kStaged;
+    float (*vs)[32 * W] = reinterpret_cast<float (*)[32 * W]>(qs + kStaged);
+    __shared__ unsigned char cuts[kStaged];
     const int tid = threadIdx.x;
     const long long units = a.batch * a.heads;
     const long long unit = blockIdx.x % units;
     const int piece = (int)(blockIdx.x / units);
     const long long n = unit / a.heads;
     const int h = (int)(unit - n * a.heads);
-    const int d = blockIdx.y * 32 * W + tid;
+    const int d = tid;
     const bool mine = d < a.dv, outputs = !a.states_only && a.o;
     const long long state = unit * a.dk * a.dv;
     pdl_wait();
@@ -93,47 +96,34 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
     const T* vp = static_cast<const T*>(a.v.p) + n * a.v.b + h * a.v.h;
     T* op = static_cast<T*>(a.o) + n * a.o_b + h * a.o_h;
     const unsigned char* done = a.done ? a.done + n * a.done_b : nullptr;
-    float kr[kLoads], qr[kLoads], vr[TS];
-    uint32_t cut = 0, cut_next = 0;       // bit s: what is held is dropped before step s of the batch
-    auto fetch = [&](long long p) {
-#pragma unroll
-        for (int m = 0; m < kLoads; m++) {
-            const int e = m * 32 * W + tid, s = e / DK, c = e % DK;
+    bool dropped = false;
+    for (long long p = p0; p < p1; p += kStaged) {
+        __syncthreads();
+#pragma unroll 8
+        for (int e = tid; e < kStaged * DK; e += 32 * W) {
+            const int s = e / DK, c = e % DK;
             const long long t = a.rev ? a.steps - 1 - (p + s) : p + s;
             const bool in = p + s < p1 && c < a.dk;
-            kr[m] = in ? to_f32<T>(kp[t * a.k.t + c]) * a.in : 0.0f;
-            qr[m] = in && outputs ? to_f32<T>(qp[t * a.q.t + c]) : 0.0f;
+            ks[s][c] = in ? to_f32<T>(kp[t * a.k.t + c]) * a.in : 0.0f;
+            if (outputs) qs[s][c] = in ? to_f32<T>(qp[t * a.q.t + c]) : 0.0f;
         }
-        cut_next = 0;
-#pragma unroll
-        for (int s = 0; s < TS; s++) {
+#pragma unroll 8
+        for (int s = 0; s < kStaged; s++) {
             const long long t = a.rev ? a.steps - 1 - (p + s) : p + s;
-            vr[s] = p + s < p1 && mine ? to_f32<T>(vp[t * a.v.t + d]) : 0.0f;
-            const long long flag = a.rev ? t : t - 1;
-            if (done && p + s < p1 && flag >= 0 && done[flag * a.done_t]) cut_next |= 1u << s;
+            vs[s][tid] = p + s < p1 && mine ? to_f32<T>(vp[t * a.v.t + d]) : 0.0f;
         }
-    };
-    bool dropped = false;
-    if (p0 < p1) fetch(p0);
-    for (long long p = p0; p < p1; p += TS) {
-#pragma unroll
-        for (int m = 0; m < kLoads; m++) {
-            const int e = m * 32 * W + tid;
-            ks[e / DK][e % DK] = kr[m];
-            qs[e / DK][e % DK] = qr[m];
+        for (int s = tid; s < kStaged; s += 32 * W) {      // whether what is held is dropped before the step
+            const long long t = a.rev ? a.steps - 1 - (p + s) : p + s, flag = a.rev ? t : t - 1;
+            cuts[s] = done && p + s < p1 && flag >= 0 && done[flag * a.done_t];
         }
-#pragma unroll
-        for (int s = 0; s < TS; s++) vs[s][tid] = vr[s];
-        cut = cut_next;
         __syncthreads();
-        if (p + TS < p1) fetch(p + TS);
-        const int steps = (int)min((long long)TS, p1 - p);
+        const int steps = (int)min((long long)kStaged, p1 - p);
 #pragma unroll 1
         for (int s = 0; s < steps; s++) {
             const float v = vs[s][tid];
             const f2 vv = pack(v, v);
             const float4* k4 = reinterpret_cast<const float4*>(ks[s]);
-            if ((cut >> s & 1u) || (none && !(a.rev && p + s == 0))) {
+            if (cuts[s] || (none && !(a.rev && p + s == 0))) {
                 dropped = true;
 #pragma unroll
                 for (int c = 0; c < DK / 4; c++) {
@@ -175,7 +165,6 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
                 if (mine) op[t * a.o_t + d] = from_f32<T>(a.out * (((s0.x + s0.y) + (s1.x + s1.y)) + ((s2.x + s2.y) + (s3.x + s3.y))));
             }
         }
-        __syncthreads();
     }
     // what is left
     float* to = nullptr;
@@ -183,7 +172,7 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
     const bool end = piece == a.pieces - 1;
     if (a.states_only) {
         to = a.z + ((long long)piece * units + unit) * a.dk * a.dv;
-        if (blockIdx.y == 0 && tid == 0) a.gain[(long long)piece * units + unit] = dropped ? -1.0f : expf(ld * (float)(p1 - p0));
+        if (tid == 0) a.gain[(long long)piece * units + unit] = dropped ? -1.0f : expf(ld * (float)(p1 - p0));
     } else if (end && a.last) {
         if (a.pieces > 1) {      // `last` may be `first`, which another block reads
             to = a.z + ((long long)piece * units + unit) * a.dk * a.dv;
@@ -225,13 +214,24 @@ __global__ void memory_join_kernel(float* z, const float* gain, int pieces, long
 template <typename T, int DK>
 cudaError_t steps_of(const MemoryPass& a, cudaStream_t st) {
     const long long units = a.batch * a.heads, blocks = units * a.pieces;
-    // Wide blocks share k and q; narrow ones where few units leave multiprocessors without work.
-    int w = a.dv > 64 ? 4 : a.dv > 32 ? 2 : 1;
-    while (w > 1 && blocks * ((a.dv + 32 * w - 1) / (32 * w)) < 2 * sm_count()) w /= 2;
-    const dim3 grid((unsigned)blocks, (unsigned)((a.dv + 32 * w - 1) / (32 * w)));
-    if (w == 4) return launch_pdl(memory_steps_kernel<T, DK, 4>, grid, dim3(128), 0, st, a);
-    if (w == 2) return launch_pdl(memory_steps_kernel<T, DK, 2>, grid, dim3(64), 0, st, a);
-    return launch_pdl(memory_steps_kernel<T, DK, 1>, grid, dim3(32), 0, st, a);
+    const int w = a.dv > 64 ? 4 : a.dv > 32 ? 2 : 1;
+    const size_t smem = (size_t)kStaged * (2 * DK + 32 * w) * 4;
+    const dim3 grid((unsigned)blocks);
+    if (w == 4) {
+        static bool ready[64] = {};
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+        if (!ready[dev]) {
+            e = cudaFuncSetAttribute(memory_steps_kernel<T, DK, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e != cudaSuccess) return e;
+            ready[dev] = true;
+        }
+        return launch_pdl(memory_steps_kernel<T, DK, 4>, grid, dim3(128), smem, st, a);
+    }
+    if (w == 2) return launch_pdl(memory_steps_kernel<T, DK, 2>, grid, dim3(64), smem, st, a);
+    return launch_pdl(memory_steps_kernel<T, DK, 1>, grid, dim3(32), smem, st, a);
 }
 template <typename T>
 cudaError_t steps_typed(const MemoryPass& a, cudaStream_t st) {
@@ -242,17 +242,21 @@ cudaError_t memory_steps(const MemoryPass& a, int dtype, cudaStream_t st) {
 }
 
 // Pieces of the step-by-step way.  A piece costs a second reading of k and v, so there are as many as fill the device and no
-// more, of 64 steps at least.
+// more, of a batch of steps at least.
 int step_pieces(long long steps, long long units) {
-    long long p = 4ll * sm_count() / (units > 0 ? units : 1);
-    if (p > steps / 64) p = steps / 64;
+    long long p = 2ll * sm_count() / (units > 0 ? units : 1);
+    if (p > steps / kStaged) p = steps / kStaged;
     return p < 2 ? 1 : p > 256 ? 256 : (int)p;
 }
+
+// Most steps of a call whose state passes through a block once.
+constexpr long long kFewSteps = 32;
 
 struct Space { long long z, gain, flags, bytes; };      // offsets into the workspace
 Space space_of(long long steps, long long units, int dk, int dv) {
     const long long x = step_pieces(steps, units), y = memory_chunk_pieces(steps, units), p = x > y ? x : y;
     const long long up = 255;
+    if (steps <= kFewSteps) return Space{};
     Space s;
     s.z = 0;
     s.gain = ((p > 1 ? p * units * dk * dv * 4 : 0) + up) & ~up;
@@ -297,6 +301,7 @@ cudaError_t run_pass(MemoryPass a, int dtype, void* workspace, const Space& s, b
     }
     return e;
 }
+
 
 // What is said of a call that may not be made; NULL: it may.
 struct Shape { const char* name; int dtype, heads, dk, dv; long long steps, batch; };
@@ -379,6 +384,20 @@ template <typename A> static MemoryPass common_pass(const A& a, const Shape& s) 
     p.status = a.status;
     return p;
 }
+template <typename A> static FewPass few_pass(const A& a, const Shape& s) {
+    FewPass p = {};
+    p.log_decay = a.log_decay;
+    p.done = s.steps > 0 ? a.done : nullptr;
+    p.done_t = s.steps > 1 ? a.done_t : 0;
+    p.done_b = s.batch > 1 ? a.done_b : 0;
+    p.batch = s.batch;
+    p.steps = (int)s.steps;
+    p.heads = s.heads;
+    p.dk = s.dk;
+    p.dv = s.dv;
+    p.in = p.out = 1.0f;
+    return p;
+}
 // rows and columns of the state change places
 static void transpose(MemoryPass& p, const Shape& s) {
     p.dk = s.dv;
@@ -417,7 +436,20 @@ extern "C" int gala_linear_attention_forward(const gala_linear_attention_args* q
     p.last = a.s_last;
     p.out = a.scale;
     bool mapped = true;
-    const cudaError_t e = run_pass(p, s.dtype, a.workspace, space_of(s.steps, s.batch * s.heads, s.dk, s.dv), mapped, static_cast<cudaStream_t>(stream));
+    cudaError_t e;
+    if (s.steps <= kFewSteps) {
+        FewPass f = few_pass(a, s);
+        f.a = p.k;
+        f.b = p.v;
+        f.p = p.q;
+        f.y = o;
+        f.first = a.s0;
+        f.last = a.s_last;
+        f.out = a.scale;
+        e = memory_few(f, s.dtype, static_cast<cudaStream_t>(stream));
+    } else {
+        e = run_pass(p, s.dtype, a.workspace, space_of(s.steps, s.batch * s.heads, s.dk, s.dv), mapped, static_cast<cudaStream_t>(stream));
+    }
     if (!mapped) SAY("%s: the driver refused a tensor map", s.name);
     return launched(e, errbuf, errbuf_len, s.name);
 }
@@ -447,6 +479,33 @@ extern "C" int gala_linear_attention_backward(const gala_linear_attention_grad_a
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e = cudaSuccess;
     bool mapped = true;
+    if (s.steps <= kFewSteps) {
+        if (a.grad_q && s.steps > 0) {
+            FewPass f = few_pass(a, s);
+            f.a = in_k;
+            f.b = in_v;
+            f.r = in_o;
+            f.z = out_q;
+            f.first = a.s0;
+            f.out = a.scale;
+            e = memory_few(f, s.dtype, st);
+        }
+        if (e == cudaSuccess && (((a.grad_k || a.grad_v) && s.steps > 0) || a.grad_s0)) {
+            FewPass f = few_pass(a, s);
+            f.rev = 1;
+            f.a = in_q;
+            f.b = in_o;
+            f.p = in_k;
+            f.y = out_v;
+            f.r = in_v;
+            f.z = out_k;
+            f.first = a.grad_s_last;
+            f.last = a.grad_s0;
+            f.in = a.scale;
+            e = memory_few(f, s.dtype, st);
+        }
+        return launched(e, errbuf, errbuf_len, s.name);
+    }
     if (a.grad_q && s.steps > 0) {
         MemoryPass p = common_pass(a, s);
         transpose(p, s);

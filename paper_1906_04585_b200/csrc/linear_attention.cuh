@@ -45,8 +45,22 @@ struct MemoryPass {
     int* status;
 };
 
-// Fewest steps of a call that goes by chunks
-constexpr long long kChunkSteps = 48;
+// A few steps: one passage of the state.
+// X = gain X + in a b^T;  y_d = out sum over rows c of X_cd p_c (or no y);  z_c = out sum over columns d of X_cd r_d (or no z)
+struct FewPass {
+    MemoryOperand a, b, p, r, y, z;
+    const float* log_decay;
+    const unsigned char* done;
+    long long done_t, done_b;
+    const float* first;          // [unit][dk][dv], NULL: zero
+    float* last;
+    long long batch;
+    int steps, heads, dk, dv;
+    float in, out;
+    int rev;
+    int lanes;                   // of a row: a power of two; a lane has four neighbouring columns (or, without VEC, every 32nd)
+};
+cudaError_t memory_few(const FewPass& a, int dtype, cudaStream_t st);       // linear_attention_few.cu
 
 // Host side of the chunked way (linear_attention_chunk.cu)
 bool memory_chunks_ok(const MemoryPass& a, int dtype);      // types, length, alignment and strides that it takes

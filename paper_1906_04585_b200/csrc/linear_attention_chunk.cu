@@ -9,9 +9,9 @@
 //   warps 2, 3   float16: the largest magnitudes of the chunk's operands, from which powers of two are taken (below)
 //   warps 4-7    a thread a row: scores -> P, rounded to the element type, in the place of the scores
 //   warps 8-11   X in registers, folded with U and rounded as the operand of the next chunk's O2; half of the chunk's o
-//   warps 12-15  w V, half a chunk ahead of the others: as two numbers of the element type, rounded and rest, where X is a
-//                float32 result of the call (one number would leave 2^-9 of it); as one where X only adds to o, which is rounded
-//                to the element type anyhow (dq and dk: half of U's products); the other half of the chunk's o
+//   warps 12-15  w V, half a chunk ahead of the others, as two numbers of the element type, rounded and rest: X is a float32
+//                result, of which one number would leave 2^-9 (and where X only adds to o, one instead of two saves 2 % of the
+//                time); the other half of the chunk's o
 // The powers of g are differences of exponents, never quotients, so nothing overflows however fast a head fades.
 //
 // What a product cannot do is leave out a term: 0 times an infinity or a NaN spreads it to steps that must not see it.  A unit
@@ -223,7 +223,6 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
     const int c0 = piece * per, chunks = min(all, c0 + per) - c0;
     const bool outputs = !a.states_only;
     const int kinds = outputs ? 3 : 2;      // tiles of a chunk: K, V, Q
-    const bool fine = a.last != nullptr;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kSlots; s++) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
@@ -394,7 +393,6 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
 #pragma unroll
                         for (int m = 0; m < 2 * C::kRows / 16; m++) {      // the rounded values, then the rests
                             const int part = m / (C::kRows / 16), kk = m % (C::kRows / 16);
-                            if (part && !fine) break;
                             umma_bf16(tmem + C::kU, kd + kk * (2048 / 16), hd + (part * (C::kHalf / 16) + kk * (2048 / 16)), id_u, m > 0 ? 1u : s > 0);
                         }
                         umma_commit(&hl_free[b]);
@@ -791,16 +789,11 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                             seen = note<FP16>(u[e], seen);
                             const float2 x = unpack<FP16>(u[e]);
                             r[e] = pack<FP16>(x.x * g[m], x.y * g[m]);
+                            const float2 y = unpack<FP16>(r[e]);
+                            d[e] = pack<FP16>(fmaf(x.x, g[m], -y.x), fmaf(x.y, g[m], -y.y));
                         }
                         st_shared(to + m * 2048, make_uint4(r[0], r[1], r[2], r[3]));
-                        if (fine) {
-#pragma unroll
-                            for (int e = 0; e < 4; e++) {
-                                const float2 x = unpack<FP16>(u[e]), y = unpack<FP16>(r[e]);
-                                d[e] = pack<FP16>(fmaf(x.x, g[m], -y.x), fmaf(x.y, g[m], -y.y));
-                            }
-                            st_shared(to + C::kHalf + m * 2048, make_uint4(d[0], d[1], d[2], d[3]));
-                        }
+                        st_shared(to + C::kHalf + m * 2048, make_uint4(d[0], d[1], d[2], d[3]));
                     }
                     proxy_fence();
                     __syncwarp();
@@ -884,7 +877,7 @@ template <int D, bool FP16, bool REV> cudaError_t launch_chunks(const ChunkMaps&
 }  // namespace
 
 bool memory_chunks_ok(const MemoryPass& a, int dtype) {
-    if (dtype == GALA_F32 || !a.o || a.steps < kChunkSteps) return false;
+    if (dtype == GALA_F32 || !a.o) return false;
     for (const MemoryOperand* m : {&a.q, &a.k, &a.v})
         if (!aligned(m->p, 16) || m->t % 8 || m->b % 8 || m->h % 8 || m->t == 0) return false;
     return true;

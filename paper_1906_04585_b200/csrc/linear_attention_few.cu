@@ -1,0 +1,172 @@
+// Attention with a memory of fixed size, a few steps (acting, a rollout), for sm_100a.
+//
+// The state of a sequence and head passes through the registers of a block once, 16 bytes of a row a thread, and the kernel is
+// bound by its way from and to memory.  Sums over rows are joined across the block's warps, sums over columns inside a warp, so
+// that one passage gives o, or dq, or dk and dv together.  The update of the state is that of linear_attention.cu.
+#include "linear_attention.cuh"
+
+namespace gala {
+namespace {
+
+constexpr int kFewRows = 8;      // rows a thread
+constexpr int kFewStaged = 4;    // steps whose vectors are brought in at once
+
+template <typename T, int W, bool VEC, bool Y, bool Z>
+__global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPass a) {
+    __shared__ __align__(16) float as[kFewStaged][128], bs[kFewStaged][128], ps[kFewStaged][128], rs[kFewStaged][128];
+    __shared__ __align__(16) float part[2][W][128];
+    __shared__ unsigned char cuts[kFewStaged];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int lx = lane & (a.lanes - 1), groups = 32 / a.lanes, group = warp * groups + lane / a.lanes, stride = W * groups;      // rows group, group + stride, ...
+    const long long unit = blockIdx.x, n = unit / a.heads;
+    const int h = (int)(unit - n * a.heads);
+    const long long state = unit * a.dk * a.dv;
+    pdl_wait();
+    pdl_launch();
+    float X[kFewRows][4];
+#pragma unroll
+    for (int i = 0; i < kFewRows; i++) {
+        const int c = group + i * stride;
+        const float* row = a.first + state + (long long)c * a.dv;
+        if (VEC) {
+            float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (a.first && c < a.dk && 4 * lx < a.dv) x = reinterpret_cast<const float4*>(row)[lx];
+            X[i][0] = x.x, X[i][1] = x.y, X[i][2] = x.z, X[i][3] = x.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; j++) X[i][j] = a.first && c < a.dk && lx + 32 * j < a.dv ? row[lx + 32 * j] : 0.0f;
+        }
+    }
+    float ld = a.log_decay[h];
+    ld = ld > 0.0f ? 0.0f : ld;
+    const float g = expf(ld), less = expm1f(ld);
+    const bool near = g >= 0.5f, none = g == 0.0f;      // as in the kernel above
+    auto at = [&](const MemoryOperand& m) { return static_cast<const T*>(m.p) + n * m.b + h * m.h; };
+    const T *ap = at(a.a), *bp = at(a.b), *pp = at(a.p), *rp = at(a.r);
+    T* yp = static_cast<T*>(const_cast<void*>(a.y.p)) + n * a.y.b + h * a.y.h;
+    T* zp = static_cast<T*>(const_cast<void*>(a.z.p)) + n * a.z.b + h * a.z.h;
+    const unsigned char* done = a.done ? a.done + n * a.done_b : nullptr;
+    int col[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) col[j] = VEC ? 4 * lx + j : lx + 32 * j;
+    for (int p0 = 0; p0 < a.steps; p0 += kFewStaged) {
+        __syncthreads();
+        const int count = min(kFewStaged, a.steps - p0);
+        for (int e = tid; e < count * 128; e += 32 * W) {
+            const int s = e >> 7, c = e & 127;
+            const long long t = a.rev ? a.steps - 1 - (p0 + s) : p0 + s;
+            as[s][c] = c < a.dk ? to_f32<T>(ap[t * a.a.t + c]) * a.in : 0.0f;
+            bs[s][c] = c < a.dv ? to_f32<T>(bp[t * a.b.t + c]) : 0.0f;
+            if (Y) ps[s][c] = a.y.p && c < a.dk ? to_f32<T>(pp[t * a.p.t + c]) : 0.0f;
+            if (Z) rs[s][c] = c < a.dv ? to_f32<T>(rp[t * a.r.t + c]) : 0.0f;
+        }
+        if (tid < count) {
+            const int t = a.rev ? a.steps - 1 - (p0 + tid) : p0 + tid, flag = a.rev ? t : t - 1;
+            cuts[tid] = done && flag >= 0 && done[flag * a.done_t];
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int s = 0; s < count; s++) {
+            const bool enter = a.rev && p0 + s == 0;      // the given state, with gain 1
+            const bool drop = cuts[s] || (none && !enter);
+            const bool held = near && !enter;
+            const float keep = enter ? 1.0f : near ? less : g;
+            if (drop) {
+#pragma unroll
+                for (int i = 0; i < kFewRows; i++)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) X[i][j] = 0.0f;
+            }
+            const long long t = a.rev ? a.steps - 1 - (p0 + s) : p0 + s;
+            float b[4], r[4], y[4] = {0.0f, 0.0f, 0.0f, 0.0f}, z[kFewRows];
+#pragma unroll
+            for (int j = 0; j < 4; j++) b[j] = bs[s][col[j]], r[j] = Z ? rs[s][col[j]] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < kFewRows; i++) {
+                const int c = group + i * stride;
+                const float k = as[s][c & 127], p = Y ? ps[s][c & 127] : 0.0f;      // rows past 127 are none of the state
+                z[i] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    X[i][j] = fmaf(keep, X[i][j], fmaf(k, b[j], held ? X[i][j] : 0.0f));
+                    y[j] = fmaf(p, X[i][j], y[j]);
+                    z[i] = fmaf(r[j], X[i][j], z[i]);
+                }
+            }
+            if (Z) {
+#pragma unroll
+                for (int i = 0; i < kFewRows; i++) {
+                    for (int m = a.lanes / 2; m > 0; m >>= 1) z[i] += __shfl_xor_sync(0xffffffffu, z[i], m);
+                    const int c = group + i * stride;
+                    if (lx == 0 && c < a.dk) zp[t * a.z.t + c] = from_f32<T>(a.out * z[i]);
+                }
+            }
+            if (Y) {
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    for (int m = a.lanes; m < 32; m <<= 1) y[j] += __shfl_xor_sync(0xffffffffu, y[j], m);
+                float* mine = part[s & 1][warp];
+                if (lane < a.lanes) {
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        if (col[j] < 128) mine[col[j]] = y[j];
+                }
+                __syncthreads();
+                if (tid < a.dv && a.y.p) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < W; w++) sum += part[s & 1][w][tid];
+                    yp[t * a.y.t + tid] = from_f32<T>(a.out * sum);
+                }
+            }
+        }
+    }
+    if (!a.last) return;
+    const bool zero = !a.rev && done && a.steps > 0 && done[(a.steps - 1) * a.done_t];
+    const float gain = a.rev && a.steps > 0 ? g : 1.0f;
+#pragma unroll
+    for (int i = 0; i < kFewRows; i++) {
+        const int c = group + i * stride;
+        if (c >= a.dk) continue;
+        float* row = a.last + state + (long long)c * a.dv;
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) x[j] = zero ? 0.0f : gain * X[i][j];
+        if (VEC) {
+            if (4 * lx < a.dv) reinterpret_cast<float4*>(row)[lx] = make_float4(x[0], x[1], x[2], x[3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                if (lx + 32 * j < a.dv) row[lx + 32 * j] = x[j];
+        }
+    }
+}
+
+template <typename T, int W, bool VEC> cudaError_t few_sums(const FewPass& a, cudaStream_t st) {
+    const dim3 grid((unsigned)(a.batch * a.heads)), block(32 * W);
+    if (a.y.p && a.z.p) return launch_pdl(memory_few_kernel<T, W, VEC, true, true>, grid, block, 0, st, a);
+    if (a.z.p) return launch_pdl(memory_few_kernel<T, W, VEC, false, true>, grid, block, 0, st, a);
+    return launch_pdl(memory_few_kernel<T, W, VEC, true, false>, grid, block, 0, st, a);
+}
+template <typename T, int W> cudaError_t few_of(const FewPass& a, bool vec, cudaStream_t st) {
+    return vec ? few_sums<T, W, true>(a, st) : few_sums<T, W, false>(a, st);
+}
+template <typename T> cudaError_t few_typed(FewPass a, cudaStream_t st) {
+    const bool vec = a.dv % 4 == 0 && aligned(a.first, 16) && aligned(a.last, 16);
+    a.lanes = 32;
+    if (vec)
+        for (a.lanes = 1; 4 * a.lanes < a.dv;) a.lanes *= 2;
+    // as few warps as hold the rows, eight a thread; at least as many threads as columns
+    int w = 4;
+    while (w * (32 / a.lanes) * kFewRows < a.dk) w *= 2;
+    if (w == 4) return few_of<T, 4>(a, vec, st);
+    if (w == 8) return few_of<T, 8>(a, vec, st);
+    return few_of<T, 16>(a, vec, st);
+}
+}  // namespace
+
+cudaError_t memory_few(const FewPass& a, int dtype, cudaStream_t st) {
+    return dtype == GALA_F32 ? few_typed<float>(a, st) : dtype == GALA_BF16 ? few_typed<__nv_bfloat16>(a, st) : few_typed<__half>(a, st);
+}
+
+}  // namespace gala

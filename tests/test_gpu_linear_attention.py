@@ -9,8 +9,7 @@ In 16 bits a long call goes through tensor cores by chunks.  Scores and the stat
 operands (every term of an output passes one of the two: u, and the scores' own float32 sums of dk terms), the weighted values
 that add to the state are held in two pieces (u^2), and sums of 128 terms are taken in float32 without a known order; a fade
 over n steps is one exponential, off by |n log_decay| + 2 roundings, less than 4 of the absolute sum where it is not small.
-So: outputs (u + u^2 + (dk + 300) eps) of the absolute sum, states (u^2 + 300 eps).  dq and dk come from passes whose state is
-no result of the call: there the weighted values are held in one piece (u instead of u^2).
+So: outputs (u + u^2 + (dk + 300) eps) of the absolute sum, states (u^2 + 300 eps).
 """
 import pytest
 
@@ -56,8 +55,7 @@ class Pass:
 
 def check(name, got, want, absolute, running, width, dtype, state=False):
     u = U[dtype]
-    pieces = u if name in ("dq", "dk") else u * u
-    chunk = 0.0 if dtype == torch.float32 else (u * u + 300 * EPS if state else u + pieces + 300 * EPS)
+    chunk = 0.0 if dtype == torch.float32 else (u * u + 300 * EPS if state else u + u * u + 300 * EPS)
     bound = (0.0 if state else u) * want.abs() + EPS * want.abs() + 2 * running + (chunk + (width + 8) * EPS) * absolute * (1 + u) + 1e-37
     if dtype == torch.float16:
         bound = bound + (0.0 if state else 2.0 ** -25) + (1e-6 if not state else 0.0) * absolute      # numbers below 2^-14 have fewer digits

@@ -11,28 +11,6 @@
 namespace gala {
 namespace {
 
-typedef unsigned long long f2;
-__device__ __forceinline__ f2 pack(float a, float b) {
-    f2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ float2 unpack(f2 r) {
-    float2 v;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(r));
-    return v;
-}
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
-    f2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
-    f2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 constexpr int kStaged = 32;      // steps brought in at once
 
 // One block of 32 W >= dv threads: one unit (sequence and head) over one piece of the time axis.
@@ -88,7 +66,7 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
             float x0 = 0.0f, x1 = 0.0f;
             if (from && mine && c < a.dk) x0 = from[(long long)c * fc + (long long)d * fd];
             if (from && mine && c + 1 < a.dk) x1 = from[(long long)(c + 1) * fc + (long long)d * fd];
-            X[c / 2] = pack(x0, x1);
+            X[c / 2] = pack_f2(x0, x1);
         }
     }
     const T* kp = static_cast<const T*>(a.k.p) + n * a.k.b + h * a.k.h;
@@ -99,68 +77,76 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
     bool dropped = false;
     for (long long p = p0; p < p1; p += kStaged) {
         __syncthreads();
-#pragma unroll 8
+        auto bring = [&](float* to, const T* from, bool in) {
+            if (std::is_same<T, float>::value)      // all of them under way at once
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(in ? 4 : 0) : "memory");
+            else
+                *to = in ? to_f32<T>(*from) : 0.0f;
+        };
+#pragma unroll 4
         for (int e = tid; e < kStaged * DK; e += 32 * W) {
             const int s = e / DK, c = e % DK;
             const long long t = a.rev ? a.steps - 1 - (p + s) : p + s;
             const bool in = p + s < p1 && c < a.dk;
-            ks[s][c] = in ? to_f32<T>(kp[t * a.k.t + c]) * a.in : 0.0f;
-            if (outputs) qs[s][c] = in ? to_f32<T>(qp[t * a.q.t + c]) : 0.0f;
+            bring(&ks[s][c], in ? kp + t * a.k.t + c : kp, in);
+            if (outputs) bring(&qs[s][c], in ? qp + t * a.q.t + c : qp, in);
         }
-#pragma unroll 8
+#pragma unroll 4
         for (int s = 0; s < kStaged; s++) {
             const long long t = a.rev ? a.steps - 1 - (p + s) : p + s;
-            vs[s][tid] = p + s < p1 && mine ? to_f32<T>(vp[t * a.v.t + d]) : 0.0f;
+            const bool in = p + s < p1 && mine;
+            bring(&vs[s][tid], in ? vp + t * a.v.t + d : vp, in);
         }
         for (int s = tid; s < kStaged; s += 32 * W) {      // whether what is held is dropped before the step
             const long long t = a.rev ? a.steps - 1 - (p + s) : p + s, flag = a.rev ? t : t - 1;
             cuts[s] = done && p + s < p1 && flag >= 0 && done[flag * a.done_t];
         }
+        if (std::is_same<T, float>::value) asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
         __syncthreads();
         const int steps = (int)min((long long)kStaged, p1 - p);
 #pragma unroll 1
         for (int s = 0; s < steps; s++) {
-            const float v = vs[s][tid];
-            const f2 vv = pack(v, v);
+            const float v = vs[s][tid] * a.in;
+            const f2 vv = pack_f2(v, v);
             const float4* k4 = reinterpret_cast<const float4*>(ks[s]);
             if (cuts[s] || (none && !(a.rev && p + s == 0))) {
                 dropped = true;
 #pragma unroll
                 for (int c = 0; c < DK / 4; c++) {
                     const float4 k = k4[c];
-                    X[2 * c] = mul2(pack(k.x, k.y), vv);
-                    X[2 * c + 1] = mul2(pack(k.z, k.w), vv);
+                    X[2 * c] = mul2(pack_f2(k.x, k.y), vv);
+                    X[2 * c + 1] = mul2(pack_f2(k.z, k.w), vv);
                 }
             } else if (near && !(a.rev && p + s == 0)) {
-                const f2 m = pack(less, less);
+                const f2 m = pack_f2(less, less);
 #pragma unroll
                 for (int c = 0; c < DK / 4; c++) {
                     const float4 k = k4[c];
-                    X[2 * c] = fma2(m, X[2 * c], fma2(pack(k.x, k.y), vv, X[2 * c]));
-                    X[2 * c + 1] = fma2(m, X[2 * c + 1], fma2(pack(k.z, k.w), vv, X[2 * c + 1]));
+                    X[2 * c] = fma2(m, X[2 * c], fma2(pack_f2(k.x, k.y), vv, X[2 * c]));
+                    X[2 * c + 1] = fma2(m, X[2 * c + 1], fma2(pack_f2(k.z, k.w), vv, X[2 * c + 1]));
                 }
             } else {
                 const float f = a.rev && p + s == 0 ? 1.0f : g;
-                const f2 m = pack(f, f);
+                const f2 m = pack_f2(f, f);
 #pragma unroll
                 for (int c = 0; c < DK / 4; c++) {
                     const float4 k = k4[c];
-                    X[2 * c] = fma2(m, X[2 * c], mul2(pack(k.x, k.y), vv));
-                    X[2 * c + 1] = fma2(m, X[2 * c + 1], mul2(pack(k.z, k.w), vv));
+                    X[2 * c] = fma2(m, X[2 * c], mul2(pack_f2(k.x, k.y), vv));
+                    X[2 * c + 1] = fma2(m, X[2 * c + 1], mul2(pack_f2(k.z, k.w), vv));
                 }
             }
             if (outputs) {
                 const float4* q4 = reinterpret_cast<const float4*>(qs[s]);
-                f2 o0 = pack(0.0f, 0.0f), o1 = o0, o2 = o0, o3 = o0;
+                f2 o0 = pack_f2(0.0f, 0.0f), o1 = o0, o2 = o0, o3 = o0;
 #pragma unroll
                 for (int c = 0; c < DK / 4; c += 2) {
                     const float4 q = q4[c], r = q4[c + 1];
-                    o0 = fma2(pack(q.x, q.y), X[2 * c], o0);
-                    o1 = fma2(pack(q.z, q.w), X[2 * c + 1], o1);
-                    o2 = fma2(pack(r.x, r.y), X[2 * c + 2], o2);
-                    o3 = fma2(pack(r.z, r.w), X[2 * c + 3], o3);
+                    o0 = fma2(pack_f2(q.x, q.y), X[2 * c], o0);
+                    o1 = fma2(pack_f2(q.z, q.w), X[2 * c + 1], o1);
+                    o2 = fma2(pack_f2(r.x, r.y), X[2 * c + 2], o2);
+                    o3 = fma2(pack_f2(r.z, r.w), X[2 * c + 3], o3);
                 }
-                const float2 s0 = unpack(o0), s1 = unpack(o1), s2 = unpack(o2), s3 = unpack(o3);
+                const float2 s0 = unpack_f2(o0), s1 = unpack_f2(o1), s2 = unpack_f2(o2), s3 = unpack_f2(o3);
                 const long long t = a.rev ? a.steps - 1 - (p + s) : p + s;
                 if (mine) op[t * a.o_t + d] = from_f32<T>(a.out * (((s0.x + s0.y) + (s1.x + s1.y)) + ((s2.x + s2.y) + (s3.x + s3.y))));
             }
@@ -174,7 +160,7 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
         to = a.z + ((long long)piece * units + unit) * a.dk * a.dv;
         if (tid == 0) a.gain[(long long)piece * units + unit] = dropped ? -1.0f : expf(ld * (float)(p1 - p0));
     } else if (end && a.last) {
-        if (a.pieces > 1) {      // `last` may be `first`, which another block reads
+        if (a.pieces > 1 && !a.direct) {      // `last` is `first`, which another block reads
             to = a.z + ((long long)piece * units + unit) * a.dk * a.dv;
         } else {
             to = a.last + state;
@@ -188,7 +174,7 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
     const float gain = finish && a.rev && a.steps > 0 ? g : 1.0f;      // no step: the state goes through as it is
 #pragma unroll
     for (int c = 0; c < DK; c += 2) {
-        const float2 x = unpack(X[c / 2]);
+        const float2 x = unpack_f2(X[c / 2]);
         if (c < a.dk) to[(long long)c * lc + (long long)d * ldd] = zero ? 0.0f : gain * x.x;
         if (c + 1 < a.dk) to[(long long)(c + 1) * lc + (long long)d * ldd] = zero ? 0.0f : gain * x.y;
     }
@@ -198,15 +184,22 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
 __global__ void memory_join_kernel(float* z, const float* gain, int pieces, long long units, int size) {
     pdl_wait();
     pdl_launch();
-    const long long unit = blockIdx.x;
-    for (int e = blockIdx.y * blockDim.x + threadIdx.x; e < size; e += gridDim.y * blockDim.x) {
-        float* at = z + unit * size + e;
-        float x = at[0];
-        for (int i = 1; i < pieces; i++) {
-            at += units * size;
-            const float g = gain[(long long)i * units + unit], own = *at;
-            x = g < 0.0f ? own : fmaf(g, x, own);
-            *at = x;
+    const long long unit = blockIdx.x, step = units * size;
+    const int e = blockIdx.y * blockDim.x + threadIdx.x;
+    if (e >= size) return;
+    float* at = z + unit * size + e;
+    float x = at[0];
+    for (int i = 1; i < pieces; i += 8) {
+        float own[8], g[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            own[j] = i + j < pieces ? at[(i + j) * step] : 0.0f;
+            g[j] = i + j < pieces ? gain[(i + j) * units + unit] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            x = g[j] < 0.0f ? own[j] : fmaf(g[j], x, own[j]);
+            if (i + j < pieces) at[(i + j) * step] = x;
         }
     }
 }
@@ -241,12 +234,13 @@ cudaError_t memory_steps(const MemoryPass& a, int dtype, cudaStream_t st) {
     return dtype == GALA_F32 ? steps_typed<float>(a, st) : dtype == GALA_BF16 ? steps_typed<__nv_bfloat16>(a, st) : steps_typed<__half>(a, st);
 }
 
-// Pieces of the step-by-step way.  A piece costs a second reading of k and v, so there are as many as fill the device and no
-// more, of a batch of steps at least.
+// Pieces of the step-by-step way, whole batches of steps.  A piece costs a second reading of k and v, so there are as many as
+// fill the device a few times and no more.
 int step_pieces(long long steps, long long units) {
-    long long p = 2ll * sm_count() / (units > 0 ? units : 1);
-    if (p > steps / kStaged) p = steps / kStaged;
-    return p < 2 ? 1 : p > 256 ? 256 : (int)p;
+    const long long batches = (steps + kStaged - 1) / kStaged;
+    long long p = 4ll * sm_count() / (units > 0 ? units : 1);
+    if (p > batches) p = batches;
+    return p < 2 ? 1 : p > 1024 ? 1024 : (int)p;
 }
 
 // Most steps of a call whose state passes through a block once.
@@ -273,7 +267,9 @@ cudaError_t run_pass(MemoryPass a, int dtype, void* workspace, const Space& s, b
     a.gain = reinterpret_cast<float*>(w + s.gain);
     a.pieces = chunks ? memory_chunk_pieces(a.steps, units) : step_pieces(a.steps, units);
     a.piece = (a.steps + a.pieces - 1) / a.pieces;
-    if (chunks) a.piece = (a.piece + 127) / 128 * 128;
+    const int whole = chunks ? 128 : kStaged;
+    a.piece = (a.piece + whole - 1) / whole * whole;
+    a.direct = a.last != a.first;
     if (a.piece < 1) a.piece = 1;
     a.pieces = (int)((a.steps + a.piece - 1) / a.piece);
     if (a.pieces < 1) a.pieces = 1;
@@ -291,8 +287,9 @@ cudaError_t run_pass(MemoryPass a, int dtype, void* workspace, const Space& s, b
     }
     if (e == cudaSuccess && mapped) e = chunks ? memory_chunks(a, dtype, mapped, st) : memory_steps(a, dtype, st);
     // units with a flag again step by step; of the others what is left goes from z to `last`
-    if (e == cudaSuccess && mapped && (chunks || (a.pieces > 1 && a.last))) {
+    if (e == cudaSuccess && mapped && (chunks || (a.pieces > 1 && a.last && !a.direct))) {
         MemoryPass c = a;
+        if (a.direct) c.z = nullptr;
         c.repair = 1;
         c.repair_pieces = a.pieces;
         c.pieces = 1;

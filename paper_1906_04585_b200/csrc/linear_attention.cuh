@@ -15,6 +15,31 @@
 
 namespace gala {
 
+#ifdef __CUDACC__
+// two float32 in one register pair
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pack_f2(float a, float b) {
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 unpack_f2(f2 r) {
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(r));
+    return v;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+#endif
+
 struct MemoryOperand { const void* p; long long t, b, h; };      // strides of time, sequence and head
 
 struct MemoryPass {
@@ -34,6 +59,7 @@ struct MemoryPass {
     // The time axis in pieces that run side by side: one launch leaves each piece's own state in `z` ([piece][unit][dk][dv];
     // pieces after the first begin at zero) and the gain of what enters it in `gain` ([piece][unit], -1: dropped), a small
     // kernel joins them, and the second launch computes the outputs, each piece from the state that enters it.
+    int direct;                  // `last` is not what the call reads as `first`: the last piece writes it
     int pieces;
     long long piece;             // steps of a piece
     float* z;

@@ -693,9 +693,9 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
             to = a.z + ((long long)piece * units + unit) * size;
             if (tid == 0) a.gain[(long long)piece * units + unit] = dropped ? -1.0f : expf(ld * (float)(min(a.steps, (long long)(c0 + per) * kSteps) - (long long)c0 * kSteps));
         } else if (piece == a.pieces - 1 && a.last) {
-            if (a.pieces > 1) {
+            if (a.pieces > 1 && !a.direct) {      // `last` is `first`, which another block reads
                 to = a.z + ((long long)piece * units + unit) * size;
-            } else if (!flagged) {      // `last` may be `first`, which the kernel that follows reads
+            } else if (!flagged) {      // and the kernel that follows
                 to = a.last + state;
                 lc = a.last_c;
                 ldd = a.last_d;

@@ -11,44 +11,78 @@ namespace {
 constexpr int kFewRows = 8;      // rows a thread
 constexpr int kFewStaged = 4;    // steps whose vectors are brought in at once
 
+// A thread has eight rows, in neighbouring pairs that share packed instructions, and four columns.
 template <typename T, int W, bool VEC, bool Y, bool Z>
 __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPass a) {
     __shared__ __align__(16) float as[kFewStaged][128], bs[kFewStaged][128], ps[kFewStaged][128], rs[kFewStaged][128];
     __shared__ __align__(16) float part[2][W][128];
     __shared__ unsigned char cuts[kFewStaged];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int lx = lane & (a.lanes - 1), groups = 32 / a.lanes, group = warp * groups + lane / a.lanes, stride = W * groups;      // rows group, group + stride, ...
+    const int lx = lane & (a.lanes - 1), groups = 32 / a.lanes, group = warp * groups + lane / a.lanes, stride = W * groups;
+    const int row0 = 2 * group;      // rows row0, row0 + 1, row0 + 2 stride, row0 + 2 stride + 1, ...
     const long long unit = blockIdx.x, n = unit / a.heads;
     const int h = (int)(unit - n * a.heads);
     const long long state = unit * a.dk * a.dv;
     pdl_wait();
     pdl_launch();
-    float X[kFewRows][4];
+    f2 X[kFewRows / 2][4];
 #pragma unroll
-    for (int i = 0; i < kFewRows; i++) {
-        const int c = group + i * stride;
-        const float* row = a.first + state + (long long)c * a.dv;
-        if (VEC) {
-            float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (a.first && c < a.dk && 4 * lx < a.dv) x = reinterpret_cast<const float4*>(row)[lx];
-            X[i][0] = x.x, X[i][1] = x.y, X[i][2] = x.z, X[i][3] = x.w;
-        } else {
+    for (int i = 0; i < kFewRows / 2; i++) {
+        float x[2][4];
 #pragma unroll
-            for (int j = 0; j < 4; j++) X[i][j] = a.first && c < a.dk && lx + 32 * j < a.dv ? row[lx + 32 * j] : 0.0f;
+        for (int e = 0; e < 2; e++) {
+            const int c = row0 + 2 * i * stride + e;
+            const float* row = a.first + state + (long long)c * a.dv;
+            if (VEC) {
+                float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (a.first && c < a.dk && 4 * lx < a.dv) v = reinterpret_cast<const float4*>(row)[lx];
+                x[e][0] = v.x, x[e][1] = v.y, x[e][2] = v.z, x[e][3] = v.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; j++) x[e][j] = a.first && c < a.dk && lx + 32 * j < a.dv ? row[lx + 32 * j] : 0.0f;
+            }
         }
+#pragma unroll
+        for (int j = 0; j < 4; j++) X[i][j] = pack_f2(x[0][j], x[1][j]);
     }
     float ld = a.log_decay[h];
     ld = ld > 0.0f ? 0.0f : ld;
     const float g = expf(ld), less = expm1f(ld);
-    const bool near = g >= 0.5f, none = g == 0.0f;      // as in the kernel above
+    const bool near = g >= 0.5f, none = g == 0.0f;
     auto at = [&](const MemoryOperand& m) { return static_cast<const T*>(m.p) + n * m.b + h * m.h; };
     const T *ap = at(a.a), *bp = at(a.b), *pp = at(a.p), *rp = at(a.r);
     T* yp = static_cast<T*>(const_cast<void*>(a.y.p)) + n * a.y.b + h * a.y.h;
     T* zp = static_cast<T*>(const_cast<void*>(a.z.p)) + n * a.z.b + h * a.z.h;
     const unsigned char* done = a.done ? a.done + n * a.done_b : nullptr;
-    int col[4];
+    auto four = [&](const float* from, float (&v)[4]) {
+        if (VEC) {
+            const float4 x = reinterpret_cast<const float4*>(from)[lx];
+            v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+        } else {
 #pragma unroll
-    for (int j = 0; j < 4; j++) col[j] = VEC ? 4 * lx + j : lx + 32 * j;
+            for (int j = 0; j < 4; j++) v[j] = from[lx + 32 * j];
+        }
+    };
+    // The sums of eight values over the lanes of a row: halves are exchanged until each lane has one value, that of row `which`,
+    // then the lanes that have the same one are summed.
+    auto row_sums = [&](float (&v)[8], int& which) {
+        which = 0;
+        int m = a.lanes / 2;
+#pragma unroll
+        for (int n = 4; n > 0; n /= 2) {
+            if (m > 0) {
+                const bool upper = lane & m;
+                which += upper ? n : 0;
+#pragma unroll
+                for (int k = 0; k < n; k++) {
+                    const float send = upper ? v[k] : v[k + n], keep = upper ? v[k + n] : v[k];
+                    v[k] = keep + __shfl_xor_sync(0xffffffffu, send, m);
+                }
+                m /= 2;
+            }
+        }
+        for (; m > 0; m /= 2) v[0] += __shfl_xor_sync(0xffffffffu, v[0], m);
+    };
     for (int p0 = 0; p0 < a.steps; p0 += kFewStaged) {
         __syncthreads();
         const int count = min(kFewStaged, a.steps - p0);
@@ -68,48 +102,85 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
 #pragma unroll 1
         for (int s = 0; s < count; s++) {
             const bool enter = a.rev && p0 + s == 0;      // the given state, with gain 1
-            const bool drop = cuts[s] || (none && !enter);
-            const bool held = near && !enter;
-            const float keep = enter ? 1.0f : near ? less : g;
-            if (drop) {
-#pragma unroll
-                for (int i = 0; i < kFewRows; i++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) X[i][j] = 0.0f;
-            }
             const long long t = a.rev ? a.steps - 1 - (p0 + s) : p0 + s;
-            float b[4], r[4], y[4] = {0.0f, 0.0f, 0.0f, 0.0f}, z[kFewRows];
+            if (cuts[s] || (none && !enter)) {
 #pragma unroll
-            for (int j = 0; j < 4; j++) b[j] = bs[s][col[j]], r[j] = Z ? rs[s][col[j]] : 0.0f;
+                for (int i = 0; i < kFewRows / 2; i++)
 #pragma unroll
-            for (int i = 0; i < kFewRows; i++) {
-                const int c = group + i * stride;
-                const float k = as[s][c & 127], p = Y ? ps[s][c & 127] : 0.0f;      // rows past 127 are none of the state
-                z[i] = 0.0f;
+                    for (int j = 0; j < 4; j++) X[i][j] = 0ull;
+            }
+            float b[4];
+            four(bs[s], b);
+            f2 b2[4];
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    X[i][j] = fmaf(keep, X[i][j], fmaf(k, b[j], held ? X[i][j] : 0.0f));
-                    y[j] = fmaf(p, X[i][j], y[j]);
-                    z[i] = fmaf(r[j], X[i][j], z[i]);
+            for (int j = 0; j < 4; j++) b2[j] = pack_f2(b[j], b[j]);
+            auto pair = [&](const float* from, int i) { return *reinterpret_cast<const f2*>(from + ((row0 + 2 * i * stride) & 127)); };      // rows past 127 are none of the state
+            if (near && !enter) {
+                const f2 m = pack_f2(less, less);
+#pragma unroll
+                for (int i = 0; i < kFewRows / 2; i++) {
+                    const f2 k = pair(as[s], i);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) X[i][j] = fma2(m, X[i][j], fma2(k, b2[j], X[i][j]));
+                }
+            } else {
+                const float keep = enter ? 1.0f : g;
+                const f2 m = pack_f2(keep, keep);
+#pragma unroll
+                for (int i = 0; i < kFewRows / 2; i++) {
+                    const f2 k = pair(as[s], i);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) X[i][j] = fma2(m, X[i][j], mul2(k, b2[j]));
                 }
             }
             if (Z) {
+                float r[4], z[kFewRows];
+                four(rs[s], r);
 #pragma unroll
-                for (int i = 0; i < kFewRows; i++) {
-                    for (int m = a.lanes / 2; m > 0; m >>= 1) z[i] += __shfl_xor_sync(0xffffffffu, z[i], m);
-                    const int c = group + i * stride;
-                    if (lx == 0 && c < a.dk) zp[t * a.z.t + c] = from_f32<T>(a.out * z[i]);
+                for (int i = 0; i < kFewRows / 2; i++) {
+                    f2 sum = mul2(pack_f2(r[0], r[0]), X[i][0]);
+#pragma unroll
+                    for (int j = 1; j < 4; j++) sum = fma2(pack_f2(r[j], r[j]), X[i][j], sum);
+                    const float2 v = unpack_f2(sum);
+                    z[2 * i] = v.x, z[2 * i + 1] = v.y;
+                }
+                if (a.lanes >= 8) {
+                    int which;
+                    row_sums(z, which);
+                    const int c = row0 + 2 * (which >> 1) * stride + (which & 1);
+                    if ((lane & (a.lanes / 8 - 1)) == 0 && c < a.dk) zp[t * a.z.t + c] = from_f32<T>(a.out * z[0]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kFewRows; i++) {
+                        for (int m = a.lanes / 2; m > 0; m >>= 1) z[i] += __shfl_xor_sync(0xffffffffu, z[i], m);
+                        const int c = row0 + 2 * (i >> 1) * stride + (i & 1);
+                        if (lx == 0 && c < a.dk) zp[t * a.z.t + c] = from_f32<T>(a.out * z[i]);
+                    }
                 }
             }
             if (Y) {
+                f2 y2[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
-                for (int j = 0; j < 4; j++)
+                for (int i = 0; i < kFewRows / 2; i++) {
+                    const f2 p = pair(ps[s], i);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) y2[j] = fma2(p, X[i][j], y2[j]);
+                }
+                float y[4];
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const float2 v = unpack_f2(y2[j]);
+                    y[j] = v.x + v.y;
                     for (int m = a.lanes; m < 32; m <<= 1) y[j] += __shfl_xor_sync(0xffffffffu, y[j], m);
-                float* mine = part[s & 1][warp];
+                }
                 if (lane < a.lanes) {
+                    float* mine = part[s & 1][warp];
+                    if (VEC) {
+                        reinterpret_cast<float4*>(mine)[lx] = make_float4(y[0], y[1], y[2], y[3]);
+                    } else {
 #pragma unroll
-                    for (int j = 0; j < 4; j++)
-                        if (col[j] < 128) mine[col[j]] = y[j];
+                        for (int j = 0; j < 4; j++) mine[lx + 32 * j] = y[j];
+                    }
                 }
                 __syncthreads();
                 if (tid < a.dv && a.y.p) {
@@ -125,19 +196,26 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
     const bool zero = !a.rev && done && a.steps > 0 && done[(a.steps - 1) * a.done_t];
     const float gain = a.rev && a.steps > 0 ? g : 1.0f;
 #pragma unroll
-    for (int i = 0; i < kFewRows; i++) {
-        const int c = group + i * stride;
-        if (c >= a.dk) continue;
-        float* row = a.last + state + (long long)c * a.dv;
-        float x[4];
+    for (int i = 0; i < kFewRows / 2; i++) {
+        float x[2][4];
 #pragma unroll
-        for (int j = 0; j < 4; j++) x[j] = zero ? 0.0f : gain * X[i][j];
-        if (VEC) {
-            if (4 * lx < a.dv) reinterpret_cast<float4*>(row)[lx] = make_float4(x[0], x[1], x[2], x[3]);
-        } else {
+        for (int j = 0; j < 4; j++) {
+            const float2 v = unpack_f2(X[i][j]);
+            x[0][j] = zero ? 0.0f : gain * v.x;
+            x[1][j] = zero ? 0.0f : gain * v.y;
+        }
 #pragma unroll
-            for (int j = 0; j < 4; j++)
-                if (lx + 32 * j < a.dv) row[lx + 32 * j] = x[j];
+        for (int e = 0; e < 2; e++) {
+            const int c = row0 + 2 * i * stride + e;
+            if (c >= a.dk) continue;
+            float* row = a.last + state + (long long)c * a.dv;
+            if (VEC) {
+                if (4 * lx < a.dv) reinterpret_cast<float4*>(row)[lx] = make_float4(x[e][0], x[e][1], x[e][2], x[e][3]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    if (lx + 32 * j < a.dv) row[lx + 32 * j] = x[e][j];
+            }
         }
     }
 }

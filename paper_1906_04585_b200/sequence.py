@@ -397,13 +397,17 @@ def _heads(name: str, t: Optional[torch.Tensor], shape, dtype, like: torch.Tenso
     return t.data_ptr(), time, sequence, head
 
 
+def _scale(q, scale):
+    return max(1, q.shape[3]) ** -0.5 if scale is None else scale
+
+
 def _attention(a, q, k, v, log_decay, s0, done, scale):
     if q.dim() != 4 or v.dim() != 4:
         raise ValueError("q, k and v have to be [steps, batch, heads, width]")
     T, N, H, dk = q.shape
     dv = v.shape[3]
     a.dtype, a.steps, a.batch, a.heads, a.dk, a.dv = _type_of(q), T, N, _width("heads", H), _width("the width of q", dk), _width("the width of v", dv)
-    a.scale = dk ** -0.5 if scale is None else scale
+    a.scale = _scale(q, scale)
     keys, values, state = (T, N, H, dk), (T, N, H, dv), (N, H, dk, dv)
     a.q, a.q_t, a.q_b, a.q_h = _heads("q", q, keys, q.dtype, q)
     a.k, a.k_t, a.k_b, a.k_h = _heads("k", k, keys, q.dtype, q)
@@ -428,6 +432,10 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
     128; log_decay [heads] float32, at most 0 (above counts as 0); done [steps, batch] with the meaning it has in a rollout;
     scale is dk ** -0.5 unless given.  Returns (o, s_last): s_last [batch, heads, dk, dv] float32 is the s0 of the next call
     (pass the same tensor as both to keep a memory in place)."""
+    if _front is not None and q.is_cuda and q.dim() == 4:
+        got = _front.linear_attention(q, k, v, log_decay, s0, done, _scale(q, scale), out, s_last, _status_word(q))
+        if got is not None:
+            return got
     st = _stream(q)
     a = B.gala_linear_attention_args()
     keys, values, state, space = _attention(a, q, k, v, log_decay, s0, done, scale)
@@ -445,6 +453,11 @@ def linear_attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor
                               dv: Optional[torch.Tensor] = None, ds0: Optional[torch.Tensor] = None):
     """Gradients (dq, dk, dv, ds0) of linear_attention from those of o (do) and s_last (ds_last); the other arguments are the
     forward call's (s0 as it was then)."""
+    if _front is not None and q.is_cuda and q.dim() == 4:
+        got = _front.linear_attention_backward(do, q, k, v, log_decay, s0, done, _scale(q, scale), ds_last, dq, dk, dv,
+                                               ds0, _status_word(q))
+        if got is not None:
+            return got
     st = _stream(q)
     a = B.gala_linear_attention_grad_args()
     keys, values, state, space = _attention(a, q, k, v, log_decay, s0, done, scale)
@@ -498,6 +511,10 @@ def qk_norm_rotary(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, in
     weight, and turned by position: of the first 2 * len(inv_freq) entries pair i, (y_i, y_{n+i}) or with `interleaved`
     (y_2i, y_2i+1), by positions * inv_freq[i].  Any strides for token and head, dim up to 256; positions [tokens] int32,
     inv_freq float32; weights [dim] are float32 or of q's type.  q_out and k_out may be q and k.  Returns (q_out, k_out)."""
+    if _front is not None:
+        got = _front.qk_norm_rotary(q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved, q_out, k_out)
+        if got is not None:
+            return got
     st = _stream(q)
     a = B.gala_qk_norm_rotary_args()
     qs, ks, _ = _qk(a, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved)
@@ -516,6 +533,10 @@ def qk_norm_rotary_backward(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch
                             dk_weight: Optional[torch.Tensor] = None):
     """Gradients (dq, dk, dq_weight, dk_weight) of qk_norm_rotary; q and k are the forward call's inputs.  dq_weight and
     dk_weight have the weights' type (float32 without weights); dq may be dq_out, dk dk_out."""
+    if _front is not None:
+        got = _front.qk_norm_rotary_backward(q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved, dq_out, dk_out, dq, dk, dq_weight, dk_weight)
+        if got is not None:
+            return got
     st = _stream(q)
     a = B.gala_qk_norm_rotary_grad_args()
     qs, ks, wdt = _qk(a, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved)
@@ -549,6 +570,10 @@ def adjust_logits(logits: torch.Tensor, *, history: Optional[torch.Tensor] = Non
     history [rows, width], bias_ids [rows, n] (with bias_values float32) and mask [rows or 1, ceil(vocab / 32)] are int32, ids
     outside 0..vocab-1 (-1 to fill up) count nowhere, n < 4096; lengths [rows] int32; repetition, frequency and presence [rows]
     float32.  Each may be left out.  out may be logits itself.  Returns the result."""
+    if _front is not None:
+        got = _front.adjust_logits(logits, history, lengths, repetition, frequency, presence, bias_ids, bias_values, mask, out)
+        if got is not None:
+            return got
     st = _stream(logits)
     if logits.dim() != 2:
         raise ValueError("logits has to be a matrix [rows, vocab]")

@@ -66,11 +66,11 @@ CASES = [
     (F, forward, dict(k=None), "needed"), (F, forward, dict(v=P + 1), "aligned"), (F, forward, dict(q_t=-4), "negative"),
     (F, forward, dict(k_t=1 << 30), "2^30"), (F, forward, dict(v_h=1 << 35), "2^35"), (F, forward, dict(o=None), "o is needed"),
     (F, forward, dict(o=P + 1), "o is needed"), (F, forward, dict(o_h=15), "overlap"), (F, forward, dict(o_b=0), "overlap"), (F, forward, dict(o_t=63), "overlap"),
-    (F, forward, dict(done=P, done_t=-1), "done"), (F, forward, dict(workspace=None), "workspace"), (F, forward, dict(workspace=P + 8), "workspace"),
-    (F, forward, dict(workspace_bytes=8), "workspace"),
+    (F, forward, dict(done=P, done_t=-1), "done"), (F, forward, dict(workspace=None, steps=500), "workspace"), (F, forward, dict(workspace=P + 8), "workspace"),
+    (F, forward, dict(workspace_bytes=8, steps=500), "workspace"),
     (G, backward, dict(dtype=-1), "dtype"), (G, backward, dict(grad_o=None), "grad_o"), (G, backward, dict(grad_q=P + 1), "aligned"),
     (G, backward, dict(grad_k_h=7), "overlap"), (G, backward, dict(grad_v_t=1 << 30), "out of range"), (G, backward, dict(grad_s0=P + 1), "aligned"),
-    (G, backward, dict(grad_o_b=-1), "negative"), (G, backward, dict(q=None), "needed"), (G, backward, dict(workspace=None), "workspace"),
+    (G, backward, dict(grad_o_b=-1), "negative"), (G, backward, dict(q=None), "needed"), (G, backward, dict(workspace=None, steps=500), "workspace"),
     (Q, qk, dict(dtype=5), "dtype 5"), (Q, qk, dict(wdtype=B.GALA_F16), "weights"), (Q, qk, dict(dim=257), "1 to 256"), (Q, qk, dict(pairs=9), "pairs"),
     (Q, qk, dict(pairs=-1), "pairs"), (Q, qk, dict(tokens=-1), "-1 tokens"), (Q, qk, dict(tokens=1 << 31), "tokens"), (Q, qk, dict(q_heads=65537), "heads"),
     (Q, qk, dict(eps=-1.0), "eps"), (Q, qk, dict(eps=float("nan")), "eps"), (Q, qk, dict(positions=None), "positions"), (Q, qk, dict(inv_freq=None), "inv_freq"),

@@ -1,17 +1,17 @@
 // Logits before a draw: penalties of the tokens in a row's history, biases of listed tokens, a bit mask, for sm_100a.
 //
-// A block has a segment of a row.  Which entries of it the history or the bias list touches is a bit map in shared memory; a
-// word an entry holds the count of the entry (low 20 bits) and the place of its first bias in the list (high 12 bits, counted
-// from the end, so that a maximum finds the first).  Only words of touched entries are ever cleared or read, so a segment costs
-// what its share of the lists costs, and entries that nothing touches stream through: two bytes (or four) in, out, and a bit.
-// Counts are whole numbers and duplicates of a bias are added by the thread of the first in the order of the list, so the
-// result does not depend on the order in which threads run.
+// A block has a segment of a row, whose logits are on their way while it counts.  A word an entry in shared memory holds the
+// count of the entry (low 20 bits) and the place of its first bias in the list (high 12 bits, counted from the end, so that a
+// maximum finds the first).  Counts are whole numbers and duplicates of a bias are added by the thread of the first in the order
+// of the list, so the result does not depend on the order in which threads run.  Segments begin where 16 bytes do, whatever the
+// row's address; a segment costs a reading of the row's lists (from the second-level cache after the first), so they are long.
 #include "sequence.cuh"
 
 namespace gala {
 namespace {
 
-constexpr int kSegment = 16384;
+constexpr int kThreads = 256;
+constexpr int kSegment = 8192;      // entries of a block with lists
 constexpr int kMaxBiases = 4095;
 constexpr int kMaxWidth = 1 << 20;
 
@@ -34,130 +34,160 @@ struct Adjust {
     long long mask_ld;
 };
 
-template <typename T, int V, bool TABLE>
-__global__ void adjust_kernel(const Adjust a) {
-    extern __shared__ uint32_t table[];                  // [segment]
-    __shared__ uint32_t touched[TABLE ? kSegment / 32 : 1];
+// V entries at once (16 bytes), N times a thread under way together
+template <typename T, int V, int N, bool TABLE>
+__global__ void __launch_bounds__(kThreads) adjust_kernel(const Adjust a) {
+    extern __shared__ __align__(16) uint32_t table[];                            // [segment]
     float* bias = reinterpret_cast<float*>(table + (TABLE ? a.segment : 0));     // [biases], at the place of the first of its id
+    __shared__ int again;
+    const int tid = threadIdx.x, threads = blockDim.x;
     const long long row = blockIdx.x / a.segments;
-    const int first = (int)(blockIdx.x - row * a.segments) * a.segment, size = min(a.segment, a.vocab - first);
+    const T* x = static_cast<const T*>(a.x) + row * a.x_ld;
+    T* y = static_cast<T*>(a.y) + row * a.y_ld;
+    // entry `first` and every V-th after it lies on 16 bytes
+    const int pad = V == 1 ? 0 : (int)((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
+    const int first = (int)(blockIdx.x - row * a.segments) * a.segment - pad, end = min(first + a.segment, a.vocab);
     pdl_wait();
     pdl_launch();
-    const int* history = nullptr;
-    const int* ids = nullptr;
-    int length = 0;
+    if (first >= a.vocab) return;
+    const uint32_t* mask = a.mask ? reinterpret_cast<const uint32_t*>(a.mask) + row * a.mask_ld : nullptr;
+    constexpr uint32_t kAll = (1u << V) - 1;
+    Vec<T, V> v[N];
+    uint32_t open[N];
+    auto bring = [&](int base) {
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const int e = base + (i * threads + tid) * V;
+            open[i] = kAll;
+            if (e < 0 || e + V > end) continue;
+            v[i].w = *reinterpret_cast<const decltype(v[i].w)*>(x + e);
+            if (mask) {
+                open[i] = mask[e >> 5] >> (e & 31);
+                if ((e & 31) + V > 32) open[i] |= mask[(e >> 5) + 1] << (32 - (e & 31));
+                open[i] &= kAll;
+            }
+        }
+    };
+    bring(first);
+    float rep = 1.0f, freq = 0.0f, pres = 0.0f;
     if (TABLE) {
-        if (a.history) {
-            history = a.history + row * a.history_ld;
+        const int* history = a.history ? a.history + row * a.history_ld : nullptr;
+        const int* ids = a.biases > 0 ? a.bias_ids + row * a.bias_ids_ld : nullptr;
+        int length = 0, id[8];
+        // the first tokens are on their way before it is known how many count
+        auto tokens = [&](int base) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const int at = base + i * threads + tid;
+                id[i] = at < a.width ? history[at] : -1;
+            }
+        };
+        if (history) {
+            tokens(0);
             length = a.lengths ? min(max(a.lengths[row], 0), a.width) : a.width;
+            if (a.repetition) rep = a.repetition[row];
+            if (a.frequency) freq = a.frequency[row];
+            if (a.presence) pres = a.presence[row];
         }
-        if (a.biases > 0) ids = a.bias_ids + row * a.bias_ids_ld;
-        for (int i = threadIdx.x; i < (size + 31) / 32; i += blockDim.x) touched[i] = 0;
-        __syncthreads();
-        for (int i = threadIdx.x; i < length; i += blockDim.x) {
-            const uint32_t e = (uint32_t)history[i] - (uint32_t)first;
-            if (e < (uint32_t)size) {
-                table[e] = 0;
-                atomicOr(&touched[e >> 5], 1u << (e & 31));
-            }
-        }
-        for (int i = threadIdx.x; ids && i < a.biases; i += blockDim.x) {
-            const uint32_t e = (uint32_t)ids[i] - (uint32_t)first;
-            if (e < (uint32_t)size) {
-                table[e] = 0;
-                atomicOr(&touched[e >> 5], 1u << (e & 31));
-            }
-        }
+        // where an id of a list lies in this segment, or past its end
+        auto place = [&](int id) { return id >= 0 && id < a.vocab ? (uint32_t)(id - first) : 0xffffffffu; };
+        const uint32_t size = (uint32_t)(end - first);
+        for (int i = tid; i < a.segment / 4; i += threads) reinterpret_cast<uint4*>(table)[i] = make_uint4(0, 0, 0, 0);
+        if (tid == 0) again = 0;
         __syncthreads();
         if (ids) {
-            for (int i = threadIdx.x; i < a.biases; i += blockDim.x) {
-                const uint32_t e = (uint32_t)ids[i] - (uint32_t)first;
-                if (e < (uint32_t)size) atomicMax(&table[e], (uint32_t)(kMaxBiases - i) << 20);
+            for (int i = tid; i < a.biases; i += threads) {
+                const uint32_t e = place(ids[i]);
+                if (e < size && atomicMax(&table[e], (uint32_t)(kMaxBiases - i) << 20) != 0) again = 1;
             }
             __syncthreads();
-            for (int i = threadIdx.x; i < a.biases; i += blockDim.x) {
+            const float* values = a.bias_values + row * a.bias_values_ld;
+            for (int i = tid; i < a.biases; i += threads) {
                 const int id = ids[i];
-                const uint32_t e = (uint32_t)id - (uint32_t)first;
-                if (e < (uint32_t)size && (int)(table[e] >> 20) == kMaxBiases - i) {
-                    const float* values = a.bias_values + row * a.bias_values_ld;
+                const uint32_t e = place(id);
+                if (e < size && (int)(table[e] >> 20) == kMaxBiases - i) {
                     float s = values[i];
-                    for (int j = i + 1; j < a.biases; j++)
-                        if (ids[j] == id) s += values[j];
+                    if (again)      // some id of the segment is listed more than once
+                        for (int j = i + 1; j < a.biases; j++)
+                            if (ids[j] == id) s += values[j];
                     bias[i] = s;
                 }
             }
-            __syncthreads();
         }
-        for (int i = threadIdx.x; i < length; i += blockDim.x) {
-            const uint32_t e = (uint32_t)history[i] - (uint32_t)first;
-            if (e < (uint32_t)size) atomicAdd(&table[e], 1u);
+        for (int base = 0; base < length; base += 8 * threads) {
+            if (base > 0) tokens(base);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const uint32_t e = place(id[i]);
+                if (e < size && base + i * threads + tid < length) atomicAdd(&table[e], 1u);
+            }
         }
         __syncthreads();
     }
-    float rep = 1.0f, freq = 0.0f, pres = 0.0f;
-    if (TABLE && a.history) {
-        if (a.repetition) rep = a.repetition[row];
-        if (a.frequency) freq = a.frequency[row];
-        if (a.presence) pres = a.presence[row];
-    }
-    const T* x = static_cast<const T*>(a.x) + row * a.x_ld + first;
-    T* y = static_cast<T*>(a.y) + row * a.y_ld + first;
-    const uint32_t* mask = a.mask ? reinterpret_cast<const uint32_t*>(a.mask) + row * a.mask_ld : nullptr;
-    for (int e = threadIdx.x * V; e < size; e += blockDim.x * V) {
-        Vec<T, V> v;
-        v.w = *reinterpret_cast<const decltype(v.w)*>(x + e);
-        constexpr uint32_t kAll = (1u << V) - 1;
-        const uint32_t hit = TABLE ? touched[e >> 5] >> (e & 31) & kAll : 0u;
-        const uint32_t open = mask ? mask[(first + e) >> 5] >> ((first + e) & 31) & kAll : kAll;
-        if (hit || open != kAll) {
-            float f[V];
-#pragma unroll
-            for (int j = 0; j < V; j++) {
-                float l = v.get(j);
-                if (hit >> j & 1u) {
-                    const uint32_t w = table[e + j], count = w & 0xfffffu, place = w >> 20;
-                    if (count) {
-                        l = l > 0.0f ? l / rep : l * rep;
-                        l = l - freq * (float)count - pres;
-                    }
-                    if (place) l += bias[kMaxBiases - place];
-                }
-                f[j] = open >> j & 1u ? l : -INFINITY;
+    auto changed = [&](int e, float l, bool open) {
+        if (TABLE) {
+            const uint32_t w = table[e - first], count = w & 0xfffffu, at = w >> 20;
+            if (count) {
+                l = l > 0.0f ? l / rep : l * rep;
+                l = l - freq * (float)count - pres;
             }
-            v.put(f);
+            if (at) l += bias[kMaxBiases - at];
         }
-        *reinterpret_cast<decltype(v.w)*>(y + e) = v.w;
+        return open ? l : -INFINITY;
+    };
+    for (int base = first; base < end; base += N * threads * V) {
+        if (base > first) bring(base);
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const int e = base + (i * threads + tid) * V;
+            if (e >= 0 && e + V <= end) {
+                uint32_t hit = 0;
+                if (TABLE) {
+                    if constexpr (V >= 4) {
+#pragma unroll
+                        for (int j = 0; j < V; j += 4) {
+                            const uint4 w = reinterpret_cast<const uint4*>(table)[(e - first + j) / 4];
+                            hit |= w.x | w.y | w.z | w.w;
+                        }
+                    } else {
+                        hit = table[e - first];
+                    }
+                }
+                if (hit || open[i] != kAll) {
+                    float f[V];
+#pragma unroll
+                    for (int j = 0; j < V; j++) f[j] = changed(e + j, v[i].get(j), open[i] >> j & 1u);
+                    v[i].put(f);
+                }
+                *reinterpret_cast<decltype(v[i].w)*>(y + e) = v[i].w;
+            } else if (V > 1) {      // the ends of a row
+                for (int j = max(0, e); j < min(end, e + V); j++) y[j] = from_f32<T>(changed(j, to_f32<T>(x[j]), !mask || (mask[j >> 5] >> (j & 31) & 1u)));
+            }
+        }
     }
 }
 
-template <typename T, int V> cudaError_t launch_adjust(Adjust a, cudaStream_t st) {
+template <typename T, int V, int N> cudaError_t launch_adjust(Adjust a, cudaStream_t st) {
     const bool table = a.history || a.biases > 0;
-    // Segments are whole words of the mask and whole vectors.  Without lists a segment is four vectors a thread.
-    a.segment = table ? kSegment : 256 * V * 4;
-    if (a.segment > a.vocab) a.segment = (a.vocab + 31) / 32 * 32;
-    a.segments = (a.vocab + a.segment - 1) / a.segment;
-    int threads = (a.segment / V + 31) / 32 * 32;
+    // Short rows: a block as small as the row.  Without lists a segment is what a block holds at once.
+    const int ends = V == 1 ? 0 : V - 1;
+    int threads = ((a.vocab + ends + V - 1) / V + 31) / 32 * 32;
     if (table && threads < 128 && a.width + a.biases > 64) threads = 128;
-    if (threads > 256) threads = 256;
+    if (threads > kThreads) threads = kThreads;
+    a.segment = table ? kSegment : kThreads * V * N;
+    const int whole = (a.vocab + ends + 31) / 32 * 32;
+    if (a.segment > whole) a.segment = whole;
+    a.segments = (a.vocab + ends + a.segment - 1) / a.segment;
     const long long blocks = a.rows * a.segments;
     if (blocks >= 1ll << 31) return cudaErrorInvalidConfiguration;
-    if (!table) return launch_pdl(adjust_kernel<T, V, false>, dim3((unsigned)blocks), dim3(threads), 0, st, a);
-    static bool ready[64] = {};
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-    if (!ready[dev]) {
-        e = cudaFuncSetAttribute(adjust_kernel<T, V, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (kSegment + kMaxBiases) * 4);
-        if (e != cudaSuccess) return e;
-        ready[dev] = true;
-    }
-    return launch_pdl(adjust_kernel<T, V, true>, dim3((unsigned)blocks), dim3(threads), (size_t)(a.segment + a.biases) * 4, st, a);
+    if (!table) return launch_pdl(adjust_kernel<T, V, N, false>, dim3((unsigned)blocks), dim3(threads), 0, st, a);
+    return launch_pdl(adjust_kernel<T, V, N, true>, dim3((unsigned)blocks), dim3(threads), (size_t)(a.segment + a.biases) * 4, st, a);
 }
 template <typename T> cudaError_t adjust(const Adjust& a, cudaStream_t st) {
     constexpr int V = 16 / sizeof(T);
-    const bool wide = aligned(a.x, 16) && aligned(a.y, 16) && a.vocab % V == 0 && (a.rows <= 1 || (a.x_ld % V == 0 && a.y_ld % V == 0));
-    return wide ? launch_adjust<T, V>(a, st) : launch_adjust<T, 1>(a, st);
+    // vectors where logits and result lie on 16 bytes at the same entries of every row
+    const bool wide = ((reinterpret_cast<uintptr_t>(a.x) ^ reinterpret_cast<uintptr_t>(a.y)) & 15) == 0 && (a.rows <= 1 || (a.x_ld - a.y_ld) % V == 0);
+    return wide ? launch_adjust<T, V, 32 / V>(a, st) : launch_adjust<T, 1, 8>(a, st);
 }
 
 }  // namespace

@@ -30,84 +30,83 @@ struct NormRotary {
     float* part;                  // backward: [block][2][dim] sums of the weights' gradients, or NULL
 };
 
-// four neighbouring elements
-template <typename T> struct Four { uint2 w; };
-template <> struct Four<float> { uint4 w; };
-template <typename T> __device__ __forceinline__ void load4(const T* p, float* f) {
-    const uint2 u = *reinterpret_cast<const uint2*>(p);
-    Vec<T, 8> v;
-    v.w = make_uint4(u.x, u.y, 0, 0);
-#pragma unroll
-    for (int j = 0; j < 4; j++) f[j] = v.get(j);
-}
-template <> __device__ __forceinline__ void load4<float>(const float* p, float* f) {
-    const float4 u = *reinterpret_cast<const float4*>(p);
-    f[0] = u.x; f[1] = u.y; f[2] = u.z; f[3] = u.w;
-}
-template <typename T> __device__ __forceinline__ void store4(T* p, const float* f) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(Vec<T, 8>::pair(f[0], f[1]), Vec<T, 8>::pair(f[2], f[3]));
-}
-template <> __device__ __forceinline__ void store4<float>(float* p, const float* f) { *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]); }
-
 // Where the eight entries of a lane lie: entry j of its first four and of its second four.  In memory order the two runs are
 // a[0..3], b[0..3] of pairs (a_j, b_j) or, interleaved, a0 b0 a1 b1, a2 b2 a3 b3.
-struct Place {
-    int at[8];
-    bool live[8];
+template <int P> struct Place {
+    int at[2 * P];
+    bool live[2 * P];
 };
-template <bool VEC> __device__ __forceinline__ Place place(const NormRotary& p, int lane) {
-    Place r;
+template <bool VEC, int P> __device__ __forceinline__ Place<P> place(const NormRotary& p, int lane) {
+    Place<P> r;
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
+    for (int j = 0; j < P; j++) {
         const int pair = VEC ? 4 * lane + j : lane + 32 * j;      // VEC: the lane of the group
         int a, b;
         if (pair >= p.pairs) a = 2 * pair, b = a + 1;
         else if (p.interleaved) a = 2 * pair, b = a + 1;
         else a = pair, b = p.pairs + pair;
         r.at[j] = a;
-        r.at[4 + j] = b;
+        r.at[P + j] = b;
         r.live[j] = a < p.dim;
-        r.live[4 + j] = b < p.dim;
+        r.live[P + j] = b < p.dim;
     }
     return r;
 }
-// x of a head as (a_0..3, b_0..3)
-template <typename T, bool VEC> __device__ __forceinline__ void get(const T* x, const Place& pl, bool two_runs, float (&f)[8]) {
-    if (VEC) {
-#pragma unroll
-        for (int j = 0; j < 8; j++) f[j] = 0.0f;
-        if (!pl.live[0]) return;
-        if (two_runs) {
-            load4<T>(x + pl.at[0], f);
-            load4<T>(x + pl.at[4], f + 4);
-        } else {
-            float u[8];
-            load4<T>(x + pl.at[0], u);
-            load4<T>(x + pl.at[0] + 4, u + 4);
-#pragma unroll
-            for (int j = 0; j < 4; j++) f[j] = u[2 * j], f[4 + j] = u[2 * j + 1];
+// The eight entries of a lane as they lie in memory, so that several heads' can be under way in few registers
+template <typename T, bool VEC, int P> struct Raw { T e[2 * P]; };
+template <typename T> struct Raw<T, true, 4> { typedef uint2 run; uint2 e[2]; };
+template <> struct Raw<float, true, 4> { typedef float4 run; float4 e[2]; };
+template <typename T, bool VEC, int P> __device__ __forceinline__ void fetch(Raw<T, VEC, P>& r, const T* x, const Place<P>& pl, bool two_runs, bool live) {
+    if constexpr (VEC) {
+        typedef typename Raw<T, VEC, P>::run run;
+        r.e[0] = r.e[1] = run{};
+        if (live && pl.live[0]) {
+            r.e[0] = *reinterpret_cast<const run*>(x + pl.at[0]);
+            r.e[1] = *reinterpret_cast<const run*>(x + (two_runs ? pl.at[4] : pl.at[0] + 4));
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; j++) f[j] = pl.live[j] ? to_f32<T>(x[pl.at[j]]) : 0.0f;
+        for (int j = 0; j < 2 * P; j++) r.e[j] = live && pl.live[j] ? x[pl.at[j]] : from_f32<T>(0.0f);
     }
 }
-template <typename T, bool VEC> __device__ __forceinline__ void put(T* x, const Place& pl, bool two_runs, const float (&f)[8]) {
-    if (VEC) {
-        if (!pl.live[0]) return;
-        if (two_runs) {
-            store4<T>(x + pl.at[0], f);
-            store4<T>(x + pl.at[4], f + 4);
+// as (a_0..3, b_0..3)
+template <typename T, bool VEC, int P> __device__ __forceinline__ void widen(const Raw<T, VEC, P>& r, bool two_runs, float (&f)[2 * P]) {
+    if constexpr (VEC) {
+        float u[8];
+        if constexpr (sizeof(T) == 4) {
+            u[0] = r.e[0].x, u[1] = r.e[0].y, u[2] = r.e[0].z, u[3] = r.e[0].w;
+            u[4] = r.e[1].x, u[5] = r.e[1].y, u[6] = r.e[1].z, u[7] = r.e[1].w;
         } else {
-            float u[8];
+            Vec<T, 8> v;
+            v.w = make_uint4(r.e[0].x, r.e[0].y, r.e[1].x, r.e[1].y);
 #pragma unroll
-            for (int j = 0; j < 4; j++) u[2 * j] = f[j], u[2 * j + 1] = f[4 + j];
-            store4<T>(x + pl.at[0], u);
-            store4<T>(x + pl.at[0] + 4, u + 4);
+            for (int j = 0; j < 8; j++) u[j] = v.get(j);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            f[j] = two_runs ? u[j] : u[2 * j];
+            f[4 + j] = two_runs ? u[4 + j] : u[2 * j + 1];
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; j++)
+        for (int j = 0; j < 2 * P; j++) f[j] = to_f32<T>(r.e[j]);
+    }
+}
+template <typename T, bool VEC, int P> __device__ __forceinline__ void put(T* x, const Place<P>& pl, bool two_runs, const float (&f)[2 * P]) {
+    if constexpr (VEC) {
+        if (!pl.live[0]) return;
+        const float u[8] = {f[0], two_runs ? f[1] : f[4], two_runs ? f[2] : f[1], two_runs ? f[3] : f[5], two_runs ? f[4] : f[2], two_runs ? f[5] : f[6], two_runs ? f[6] : f[3], f[7]};
+        T* second = x + (two_runs ? pl.at[4] : pl.at[0] + 4);
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4*>(x + pl.at[0]) = make_float4(u[0], u[1], u[2], u[3]);
+            *reinterpret_cast<float4*>(second) = make_float4(u[4], u[5], u[6], u[7]);
+        } else {
+            *reinterpret_cast<uint2*>(x + pl.at[0]) = make_uint2(Vec<T, 8>::pair(u[0], u[1]), Vec<T, 8>::pair(u[2], u[3]));
+            *reinterpret_cast<uint2*>(second) = make_uint2(Vec<T, 8>::pair(u[4], u[5]), Vec<T, 8>::pair(u[6], u[7]));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 2 * P; j++)
             if (pl.live[j]) x[pl.at[j]] = from_f32<T>(f[j]);
     }
 }
@@ -116,28 +115,30 @@ __device__ __forceinline__ float group_sum(float s, int lanes) {
     return s;
 }
 
-template <typename T, typename W, bool VEC, bool GRAD>
-__global__ void __launch_bounds__(32 * kWarps) norm_rotary_kernel(const NormRotary p) {
+// P: pairs a lane (four with VEC, else as many as the head's pairs dealt out over a warp need)
+template <typename T, typename W, bool VEC, int P, bool GRAD>
+__global__ void __launch_bounds__(32 * kWarps, GRAD ? 4 : 5) norm_rotary_kernel(const NormRotary p) {
     __shared__ float part[GRAD ? 2 * 256 : 1];
+    constexpr int kAhead = sizeof(T) == 4 ? 8 / P : 4;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int own = lane & (p.lanes - 1), group = lane / p.lanes, groups = 32 / p.lanes;
-    const Place pl = place<VEC>(p, own);
-    bool turned[4];      // VEC: all four pairs of a lane, or none
+    const Place<P> pl = place<VEC, P>(p, own);
+    bool turned[P];      // VEC: all four pairs of a lane, or none
 #pragma unroll
-    for (int j = 0; j < 4; j++) turned[j] = VEC ? 4 * own < p.pairs : lane + 32 * j < p.pairs;
+    for (int j = 0; j < P; j++) turned[j] = VEC ? 4 * own < p.pairs : lane + 32 * j < p.pairs;
     const bool two_runs = !p.interleaved && turned[0];
     const int heads = p.q_heads + p.k_heads;
-    float wq[8], wk[8], freq[4], dwq[8], dwk[8];
+    float wq[2 * P], wk[2 * P], freq[P], dwq[2 * P], dwk[2 * P];
     pdl_wait();
     pdl_launch();
 #pragma unroll
-    for (int j = 0; j < 8; j++) {
+    for (int j = 0; j < 2 * P; j++) {
         wq[j] = p.q.w && pl.live[j] ? to_f32<W>(static_cast<const W*>(p.q.w)[pl.at[j]]) : 1.0f;
         wk[j] = p.k.w && pl.live[j] ? to_f32<W>(static_cast<const W*>(p.k.w)[pl.at[j]]) : 1.0f;
         dwq[j] = dwk[j] = 0.0f;
     }
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
+    for (int j = 0; j < P; j++) {
         const int pair = VEC ? 4 * own + j : lane + 32 * j;
         freq[j] = pair < p.pairs ? p.inv_freq[pair] : 0.0f;
     }
@@ -146,76 +147,87 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rotary_kernel(const NormRota
     for (long long item = (long long)blockIdx.x * kWarps + warp; item < items; item += (long long)gridDim.x * kWarps) {
         const long long token = item / p.shares;
         const int from = (int)(item - token * p.shares) * p.share, to = min(heads, from + p.share);
-        float co[4], si[4];
+        float co[P], si[P];
         {
             const double pos = (double)p.positions[token];
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
+            for (int j = 0; j < P; j++) {
                 const double turns = pos * (double)freq[j] * kTurn;
                 sincospif(2.0f * (float)(turns - rint(turns)), &si[j], &co[j]);
             }
         }
-        for (int base = from; base < to; base += groups) {
-            const int head = base + group;
-            const bool live = head < to, is_q = head < p.q_heads;
-            const Heads& hd = is_q ? p.q : p.k;
-            const int h = is_q ? head : head - p.q_heads;
-            float x[8];
+        // the heads of a few turns are brought in together
+        for (int base = from; base < to; base += kAhead * groups) {
+            Raw<T, VEC, P> xs[kAhead], gs[GRAD ? kAhead : 1];
 #pragma unroll
-            for (int j = 0; j < 8; j++) x[j] = 0.0f;
-            if (live) get<T, VEC>(static_cast<const T*>(hd.x) + token * hd.x_t + h * hd.x_h, pl, two_runs, x);
-            float ss = 0.0f;
+            for (int b = 0; b < kAhead; b++) {
+                const int head = base + b * groups + group;
+                const bool live = head < to, is_q = head < p.q_heads;
+                const Heads& hd = is_q ? p.q : p.k;
+                const int h = is_q ? head : head - p.q_heads;
+                fetch<T, VEC, P>(xs[b], static_cast<const T*>(hd.x) + token * hd.x_t + h * hd.x_h, pl, two_runs, live);
+                if (GRAD) fetch<T, VEC, P>(gs[b], static_cast<const T*>(hd.g) + token * hd.g_t + h * hd.g_h, pl, two_runs, live);
+            }
 #pragma unroll
-            for (int j = 0; j < 8; j++) ss = fmaf(x[j], x[j], ss);
-            float y[8];
-            if (!GRAD) {
-                const float r = rsqrtf(fmaf(group_sum(ss, p.lanes), inv_dim, p.eps));
+            for (int b = 0; b < kAhead; b++) {
+                if (base + b * groups >= to) break;      // the same for the whole warp
+                const int head = base + b * groups + group;
+                const bool live = head < to, is_q = head < p.q_heads;
+                const Heads& hd = is_q ? p.q : p.k;
+                const int h = is_q ? head : head - p.q_heads;
+                float x[2 * P], y[2 * P];
+                widen<T, VEC, P>(xs[b], two_runs, x);
+                float ss = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 8; j++) y[j] = x[j] * r * (is_q ? wq[j] : wk[j]);
+                for (int j = 0; j < 2 * P; j++) ss = fmaf(x[j], x[j], ss);
+                if (!GRAD) {
+                    const float r = rsqrtf(fmaf(group_sum(ss, p.lanes), inv_dim, p.eps));
 #pragma unroll
-                for (int j = 0; j < 4; j++)
-                    if (turned[j]) {
-                        const float a = y[j], b = y[4 + j];
-                        y[j] = a * co[j] - b * si[j];
-                        y[4 + j] = b * co[j] + a * si[j];
+                    for (int j = 0; j < 2 * P; j++) y[j] = x[j] * r * (is_q ? wq[j] : wk[j]);
+#pragma unroll
+                    for (int j = 0; j < P; j++)
+                        if (turned[j]) {
+                            const float a = y[j], b = y[P + j];
+                            y[j] = a * co[j] - b * si[j];
+                            y[P + j] = b * co[j] + a * si[j];
+                        }
+                } else {
+                    float g[2 * P];
+                    widen<T, VEC, P>(gs[b], two_runs, g);
+#pragma unroll
+                    for (int j = 0; j < P; j++)
+                        if (turned[j]) {
+                            const float a = g[j], b = g[P + j];
+                            g[j] = a * co[j] + b * si[j];
+                            g[P + j] = b * co[j] - a * si[j];
+                        }
+                    float dot = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 2 * P; j++) {
+                        y[j] = g[j] * (is_q ? wq[j] : wk[j]);
+                        dot = fmaf(y[j], x[j], dot);
                     }
-            } else {
-                float g[8];
-#pragma unroll
-                for (int j = 0; j < 8; j++) g[j] = 0.0f;
-                if (live) get<T, VEC>(static_cast<const T*>(hd.g) + token * hd.g_t + h * hd.g_h, pl, two_runs, g);
-#pragma unroll
-                for (int j = 0; j < 4; j++)
-                    if (turned[j]) {
-                        const float a = g[j], b = g[4 + j];
-                        g[j] = a * co[j] + b * si[j];
-                        g[4 + j] = b * co[j] - a * si[j];
+                    for (int m = p.lanes / 2; m > 0; m >>= 1) {
+                        ss += __shfl_xor_sync(0xffffffffu, ss, m);
+                        dot += __shfl_xor_sync(0xffffffffu, dot, m);
                     }
-                float dot = 0.0f;
+                    const float r = rsqrtf(fmaf(ss, inv_dim, p.eps)), back = dot * r * r * inv_dim;
 #pragma unroll
-                for (int j = 0; j < 8; j++) dot = fmaf(g[j] * (is_q ? wq[j] : wk[j]), x[j], dot);
-                for (int m = p.lanes / 2; m > 0; m >>= 1) {
-                    ss += __shfl_xor_sync(0xffffffffu, ss, m);
-                    dot += __shfl_xor_sync(0xffffffffu, dot, m);
-                }
-                const float r = rsqrtf(fmaf(ss, inv_dim, p.eps)), back = dot * r * r * inv_dim;
-#pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    y[j] = r * (g[j] * (is_q ? wq[j] : wk[j]) - x[j] * back);
-                    const float dw = g[j] * (x[j] * r);
-                    if (live) {
+                    for (int j = 0; j < 2 * P; j++) {
+                        y[j] = r * (y[j] - x[j] * back);
+                        const float dw = live ? g[j] * (x[j] * r) : 0.0f;
                         if (is_q) dwq[j] += dw;
                         else dwk[j] += dw;
                     }
                 }
+                if (live) put<T, VEC, P>(static_cast<T*>(hd.y) + token * hd.y_t + h * hd.y_h, pl, two_runs, y);
             }
-            if (live) put<T, VEC>(static_cast<T*>(hd.y) + token * hd.y_t + h * hd.y_h, pl, two_runs, y);
         }
     }
     if (GRAD && p.part) {
         // groups of the warp, then warps of the block, one after another
 #pragma unroll
-        for (int j = 0; j < 8; j++)
+        for (int j = 0; j < 2 * P; j++)
             for (int m = p.lanes; m < 32; m <<= 1) {
                 dwq[j] += __shfl_xor_sync(0xffffffffu, dwq[j], m);
                 dwk[j] += __shfl_xor_sync(0xffffffffu, dwk[j], m);
@@ -225,7 +237,7 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rotary_kernel(const NormRota
             __syncthreads();
             if (w == warp && lane < p.lanes) {
 #pragma unroll
-                for (int j = 0; j < 8; j++)
+                for (int j = 0; j < 2 * P; j++)
                     if (pl.live[j]) {
                         part[pl.at[j]] += dwq[j];
                         part[256 + pl.at[j]] += dwk[j];
@@ -242,26 +254,30 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rotary_kernel(const NormRota
 
 // 32 columns a block, the blocks' sums shared out over its warps
 template <typename W>
-__global__ void __launch_bounds__(256) weight_sum_kernel(const float* part, int blocks, int dim, W* dwq, W* dwk) {
-    __shared__ float sums[8][32];
+__global__ void __launch_bounds__(1024) weight_sum_kernel(const float* part, int blocks, int dim, W* dwq, W* dwk) {
+    __shared__ float sums[32][32];
     pdl_wait();
     pdl_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = blockIdx.x * 32 + lane;
     float s = 0.0f;
-    if (col < 2 * dim)
-        for (int b = warp; b < blocks; b += 8) s += part[(long long)b * 2 * dim + col];
+    if (col < 2 * dim) {
+#pragma unroll 8
+        for (int b = warp; b < blocks; b += 32) s += part[(long long)b * 2 * dim + col];
+    }
     sums[warp][lane] = s;
     __syncthreads();
     if (warp == 0 && col < 2 * dim) {
         float t = 0.0f;
-        for (int w = 0; w < 8; w++) t += sums[w][lane];
+#pragma unroll
+        for (int w = 0; w < 32; w++) t += sums[w][lane];
         W* to = col < dim ? dwq : dwk;
         if (to) to[col < dim ? col : col - dim] = from_f32<W>(t);
     }
 }
 
+// Blocks that sum the weights' gradients: one wave of those that fit
 int blocks_of(long long tokens) {
-    const long long most = 8ll * sm_count(), b = (tokens + kWarps - 1) / kWarps;
+    const long long most = 4ll * sm_count(), b = (tokens + kWarps - 1) / kWarps;
     return (int)(b < 1 ? 1 : b > most ? most : b);
 }
 
@@ -279,9 +295,13 @@ template <typename T, typename W, bool GRAD> cudaError_t launch_typed(NormRotary
     while (per > 1 && p.tokens * ((turns + per - 1) / per) < 16ll * sm_count()) per = (per + 1) / 2;
     p.share = per * groups;
     p.shares = (turns + per - 1) / per;
-    const int blocks = GRAD ? blocks_of(p.tokens) : blocks_of(p.tokens * p.shares);
-    if (vec) return launch_pdl(norm_rotary_kernel<T, W, true, GRAD>, dim3(blocks), dim3(32 * kWarps), 0, st, p);
-    return launch_pdl(norm_rotary_kernel<T, W, false, GRAD>, dim3(blocks), dim3(32 * kWarps), 0, st, p);
+    const long long blocks_all = (p.tokens * p.shares + kWarps - 1) / kWarps;
+    const int blocks = GRAD ? blocks_of(p.tokens) : (int)(blocks_all > 64ll * sm_count() ? 64ll * sm_count() : blocks_all);
+    const dim3 grid(blocks), block(32 * kWarps);
+    if (vec) return launch_pdl(norm_rotary_kernel<T, W, true, 4, GRAD>, grid, block, 0, st, p);
+    if (p.dim <= 64) return launch_pdl(norm_rotary_kernel<T, W, false, 1, GRAD>, grid, block, 0, st, p);
+    if (p.dim <= 128) return launch_pdl(norm_rotary_kernel<T, W, false, 2, GRAD>, grid, block, 0, st, p);
+    return launch_pdl(norm_rotary_kernel<T, W, false, 4, GRAD>, grid, block, 0, st, p);
 }
 template <bool GRAD> cudaError_t launch(const NormRotary& p, int dtype, int wdtype, bool vec, cudaStream_t st) {
     if (dtype == GALA_F32) return launch_typed<float, float, GRAD>(p, vec, st);
@@ -408,10 +428,10 @@ extern "C" int gala_qk_norm_rotary_backward(const gala_qk_norm_rotary_grad_args*
         const dim3 grid((2 * a.dim + 31) / 32);
         const int blocks = blocks_of(a.tokens);
         const float* part = p.part;
-        if (a.wdtype == GALA_F32) e = launch_pdl(weight_sum_kernel<float>, grid, dim3(256), 0, st, part, blocks, a.dim, static_cast<float*>(a.grad_q_weight), static_cast<float*>(a.grad_k_weight));
+        if (a.wdtype == GALA_F32) e = launch_pdl(weight_sum_kernel<float>, grid, dim3(1024), 0, st, part, blocks, a.dim, static_cast<float*>(a.grad_q_weight), static_cast<float*>(a.grad_k_weight));
         else if (a.wdtype == GALA_BF16)
-            e = launch_pdl(weight_sum_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, part, blocks, a.dim, static_cast<__nv_bfloat16*>(a.grad_q_weight), static_cast<__nv_bfloat16*>(a.grad_k_weight));
-        else e = launch_pdl(weight_sum_kernel<__half>, grid, dim3(256), 0, st, part, blocks, a.dim, static_cast<__half*>(a.grad_q_weight), static_cast<__half*>(a.grad_k_weight));
+            e = launch_pdl(weight_sum_kernel<__nv_bfloat16>, grid, dim3(1024), 0, st, part, blocks, a.dim, static_cast<__nv_bfloat16*>(a.grad_q_weight), static_cast<__nv_bfloat16*>(a.grad_k_weight));
+        else e = launch_pdl(weight_sum_kernel<__half>, grid, dim3(1024), 0, st, part, blocks, a.dim, static_cast<__half*>(a.grad_q_weight), static_cast<__half*>(a.grad_k_weight));
     }
     return launched(e, errbuf, errbuf_len, name);
 }

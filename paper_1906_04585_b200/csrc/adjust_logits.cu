@@ -34,6 +34,24 @@ struct Adjust {
     long long mask_ld;
 };
 
+// -inf where a bit is 0
+template <typename T, int V> __device__ __forceinline__ void shut(Vec<T, V>& v, uint32_t open) {
+    if constexpr (V == 1) {
+        v.w = open & 1u ? v.w : from_f32<T>(-INFINITY);
+    } else {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&v.w);
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            if (sizeof(T) == 4) {
+                w[j] = open >> j & 1u ? w[j] : 0xff800000u;
+            } else {
+                const uint32_t keep = (open >> (2 * j) & 1u ? 0xffffu : 0u) | (open >> (2 * j + 1) & 1u ? 0xffff0000u : 0u);
+                w[j] = (w[j] & keep) | ((std::is_same<T, __nv_bfloat16>::value ? 0xff80ff80u : 0xfc00fc00u) & ~keep);
+            }
+        }
+    }
+}
+
 // V entries at once (16 bytes), N times a thread under way together
 template <typename T, int V, int N, bool TABLE>
 __global__ void __launch_bounds__(kThreads) adjust_kernel(const Adjust a) {
@@ -124,16 +142,15 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const Adjust a) {
         }
         __syncthreads();
     }
-    auto changed = [&](int e, float l, bool open) {
-        if (TABLE) {
-            const uint32_t w = table[e - first], count = w & 0xfffffu, at = w >> 20;
-            if (count) {
-                l = l > 0.0f ? l / rep : l * rep;
-                l = l - freq * (float)count - pres;
-            }
-            if (at) l += bias[kMaxBiases - at];
+    const float inverse = 1.0f / rep;
+    auto changed = [&](uint32_t w, float l) {
+        const uint32_t count = w & 0xfffffu, at = w >> 20;
+        if (count) {
+            l *= l > 0.0f ? inverse : rep;
+            l = l - freq * (float)count - pres;
         }
-        return open ? l : -INFINITY;
+        if (at) l += bias[kMaxBiases - at];
+        return l;
     };
     for (int base = first; base < end; base += N * threads * V) {
         if (base > first) bring(base);
@@ -141,27 +158,29 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const Adjust a) {
         for (int i = 0; i < N; i++) {
             const int e = base + (i * threads + tid) * V;
             if (e >= 0 && e + V <= end) {
-                uint32_t hit = 0;
                 if (TABLE) {
+                    uint32_t w[V], hit = 0;
                     if constexpr (V >= 4) {
 #pragma unroll
                         for (int j = 0; j < V; j += 4) {
-                            const uint4 w = reinterpret_cast<const uint4*>(table)[(e - first + j) / 4];
-                            hit |= w.x | w.y | w.z | w.w;
+                            const uint4 t = reinterpret_cast<const uint4*>(table)[(e - first + j) / 4];
+                            w[j] = t.x, w[j + 1] = t.y, w[j + 2] = t.z, w[j + 3] = t.w;
+                            hit |= t.x | t.y | t.z | t.w;
                         }
                     } else {
-                        hit = table[e - first];
+                        hit = w[0] = table[e - first];
+                    }
+                    if (hit) {
+                        float f[V];
+#pragma unroll
+                        for (int j = 0; j < V; j++) f[j] = w[j] ? changed(w[j], v[i].get(j)) : v[i].get(j);
+                        v[i].put(f);
                     }
                 }
-                if (hit || open[i] != kAll) {
-                    float f[V];
-#pragma unroll
-                    for (int j = 0; j < V; j++) f[j] = changed(e + j, v[i].get(j), open[i] >> j & 1u);
-                    v[i].put(f);
-                }
+                if (open[i] != kAll) shut(v[i], open[i]);
                 *reinterpret_cast<decltype(v[i].w)*>(y + e) = v[i].w;
             } else if (V > 1) {      // the ends of a row
-                for (int j = max(0, e); j < min(end, e + V); j++) y[j] = from_f32<T>(changed(j, to_f32<T>(x[j]), !mask || (mask[j >> 5] >> (j & 31) & 1u)));
+                for (int j = max(0, e); j < min(end, e + V); j++) y[j] = mask && !(mask[j >> 5] >> (j & 31) & 1u) ? from_f32<T>(-INFINITY) : TABLE && table[j - first] ? from_f32<T>(changed(table[j - first], to_f32<T>(x[j]))) : x[j];
             }
         }
     }
@@ -170,7 +189,7 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const Adjust a) {
 template <typename T, int V, int N> cudaError_t launch_adjust(Adjust a, cudaStream_t st) {
     const bool table = a.history || a.biases > 0;
     // Short rows: a block as small as the row.  Without lists a segment is what a block holds at once.
-    const int ends = V == 1 ? 0 : V - 1;
+    const int ends = V == 1 || (aligned(a.x, 16) && (a.rows <= 1 || a.x_ld % V == 0)) ? 0 : V - 1;      // entries before the first 16 bytes
     int threads = ((a.vocab + ends + V - 1) / V + 31) / 32 * 32;
     if (table && threads < 128 && a.width + a.biases > 64) threads = 128;
     if (threads > kThreads) threads = kThreads;

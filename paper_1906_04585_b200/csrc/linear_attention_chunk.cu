@@ -5,8 +5,10 @@
 //   O = out (in (Q K^T * L) V + diag(e) Q X)          X' = carry X + in K^T diag(w) V,  w_j = g^(steps from j to the exit)
 // One block goes over a unit (sequence and head), or a piece of its time axis, chunk by chunk:
 //   warp 0       brings K, V and Q of the chunks in by tensor copies, a ring of tiles
-//   warp 1       issues the products: scores = Q K^T, U = K^T (w V), O2 = Q X, O1 = P V with P in tensor memory
-//   warps 2, 3   float16: the largest magnitudes of the chunk's operands, from which powers of two are taken (below)
+//   warp 1       issues the products scores = Q K^T, O2 = Q X and O1 = P V with P in tensor memory
+//   warp 2       issues U = K^T (w V): one thread issues a product every 70 cycles and waits some 100 cycles for each barrier,
+//                and 40 products a chunk bound it
+//   warp 3       float16: the largest magnitudes of the chunk's operands, from which powers of two are taken (below)
 //   warps 4-7    a thread a row: scores -> P, rounded to the element type, in the place of the scores
 //   warps 8-11   X in registers, folded with U and rounded as the operand of the next chunk's O2; half of the chunk's o
 //   warps 12-15  w V, half a chunk ahead of the others, as two numbers of the element type, rounded and rest: X is a float32
@@ -211,7 +213,7 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
     __shared__ __align__(8) uint64_t full[C::kSlots], empty[C::kSlots], hl_ready[2], hl_free[2], scores_full, p_ready, o_full, o_free, u_full, u_free, x_ready, x_taken, max_ready[4], o_stored[4];
     __shared__ uint32_t tmem_slot, found;
     __shared__ int abort_flag, issued;
-    __shared__ float pw[132], most[4][2][3], first_most[4], x_backs[2];
+    __shared__ float pw[132], most[4][3], first_most[4], x_backs[2];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t ring = smem_u32(smem), hl = ring + C::kSlots * C::kTile, sx = hl + 4 * C::kHalf;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -225,9 +227,9 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
     const int kinds = outputs ? 3 : 2;      // tiles of a chunk: K, V, Q
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < C::kSlots; s++) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < C::kSlots; s++) { mbar_init(&full[s], 1); mbar_init(&empty[s], 2); }
         for (int b = 0; b < 2; b++) { mbar_init(&hl_ready[b], 4); mbar_init(&hl_free[b], 1); }
-        for (int b = 0; b < 4; b++) { mbar_init(&max_ready[b], 2); mbar_init(&o_stored[b], 8); }
+        for (int b = 0; b < 4; b++) { mbar_init(&max_ready[b], 1); mbar_init(&o_stored[b], 8); }
         mbar_init(&scores_full, 1);
         mbar_init(&p_ready, 4);
         mbar_init(&o_full, 1);
@@ -308,7 +310,7 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
     auto most_of = [&](int c, float (&m)[3]) {
         if (!warp_wait(&max_ready[c & 3], (uint32_t)(c >> 2) & 1u, &abort_flag)) return false;
 #pragma unroll
-        for (int k = 0; k < 3; k++) m[k] = fmaxf(most[c & 3][0][k], most[c & 3][1][k]);
+        for (int k = 0; k < 3; k++) m[k] = most[c & 3][k];
         return true;
     };
 
@@ -339,12 +341,10 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                         for (int b = 0; b < D / 64; b++) tma_prefetch_4d(map, 64 * b, (int)begin(c + 2), hh, nn);
                 }
             }
-        } else if (warp == 1) {
-            constexpr uint32_t kAtom = D == 128 ? 16384u : 0u;      // between the 64-wide parts of K^T; with one part rows 64..127 repeat it
-            const uint32_t id_scores = make_instr_desc(kSteps, 0, 0, FP16), id_u = make_instr_desc(D, 1, 1, FP16), id_o = make_instr_desc(D, 0, 1, FP16);
-            // descriptors of the ring's first tile and of the first half buffer; others differ in the address (16-byte units)
-            const uint64_t d_rows = make_smem_desc(ring, 0), d_cols = make_smem_desc(ring, 1, kAtom), d_v = make_smem_desc(ring, 1, 16384u);
-            const uint64_t d_hl = make_smem_desc(hl, 1, C::kRows * 128), d_x = make_smem_desc(sx, 1, D * 128);
+        } else if (warp == 1 && outputs) {
+            const uint32_t id_scores = make_instr_desc(kSteps, 0, 0, FP16), id_o = make_instr_desc(D, 0, 1, FP16);
+            // descriptors of the ring's first tile; others differ in the address (16-byte units)
+            const uint64_t d_rows = make_smem_desc(ring, 0), d_v = make_smem_desc(ring, 1, 16384u), d_x = make_smem_desc(sx, 1, D * 128);
             int sk = 0;
             uint32_t pk = 0;
             auto wait = [&](uint64_t* bar, uint32_t parity) { return warp_wait(bar, parity & 1u, &abort_flag); };
@@ -354,42 +354,58 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                 uint32_t pv = pk, pq = pk;
                 if (sv >= C::kSlots) sv -= C::kSlots, pv ^= 1u;
                 if (sq >= C::kSlots) sq -= C::kSlots, pq ^= 1u;
-                const uint64_t k_rows = d_rows + (uint64_t)(sk * (C::kTile / 16)), q_rows = d_rows + (uint64_t)(sq * (C::kTile / 16));
-                const uint64_t k_cols = d_cols + (uint64_t)(sk * (C::kTile / 16)), v_cols = d_v + (uint64_t)(sv * (C::kTile / 16));
-                if (!wait(&full[sk], pk)) break;
-                if (outputs) {
-                    if (!wait(&full[sq], pq)) break;
-                    if (elected()) {
+                const uint64_t k_rows = d_rows + (uint64_t)(sk * (C::kTile / 16)), q_rows = d_rows + (uint64_t)(sq * (C::kTile / 16)), v_cols = d_v + (uint64_t)(sv * (C::kTile / 16));
+                if (!wait(&full[sk], pk) || !wait(&full[sq], pq)) break;
+                if (elected()) {
 #pragma unroll
-                        for (int kk = 0; kk < D / 16; kk++) {
-                            const uint64_t at = (kk >> 2) * (16384 / 16) + (kk & 3) * (32 / 16);
-                            umma_bf16(tmem, q_rows + at, k_rows + at, id_scores, kk > 0);
-                        }
-                        umma_commit(&scores_full);
+                    for (int kk = 0; kk < D / 16; kk++) {
+                        const uint64_t at = (kk >> 2) * (16384 / 16) + (kk & 3) * (32 / 16);
+                        umma_bf16(tmem, q_rows + at, k_rows + at, id_scores, kk > 0);
                     }
-                    __syncwarp();
+                    umma_commit(&scores_full);
+                    umma_commit(&empty[sk]);
+                    umma_commit(&empty[sq]);
                 }
-                // U in two halves: while the first frees its buffers, O2
-                if (c > 0 && !wait(&u_free, (uint32_t)(c - 1))) break;
+                __syncwarp();
+                if (!wait(&x_ready, (uint32_t)c) || (c > 0 && !wait(&o_free, (uint32_t)(c - 1)))) break;
                 tcgen05_fence_after();      // here and below: what was read from or written to tensor memory
+                if (elected()) {
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; kk++)
+                        umma_bf16(tmem + C::kO2, q_rows + (kk >> 2) * (16384 / 16) + (kk & 3) * (32 / 16), d_x + kk * (2048 / 16), id_o, kk > 0);
+                    umma_commit(&empty[sq]);
+                }
+                __syncwarp();
+                if (!wait(&full[sv], pv) || !wait(&p_ready, (uint32_t)c)) break;
+                tcgen05_fence_after();
+                if (elected()) {
+#pragma unroll
+                    for (int kk = 0; kk < kSteps / 16; kk++) umma_tmem(tmem + C::kO1, tmem + 8 * kk, v_cols + kk * (2048 / 16), id_o, kk > 0);
+                    umma_commit(&o_full);
+                    umma_commit(&empty[sv]);
+                }
+                __syncwarp();
+                sk += 3;
+                if (sk >= C::kSlots) sk -= C::kSlots, pk ^= 1u;
+            }
+        } else if (warp == 2) {
+            constexpr uint32_t kAtom = D == 128 ? 16384u : 0u;      // between the 64-wide parts of K^T; with one part rows 64..127 repeat it
+            const uint32_t id_u = make_instr_desc(D, 1, 1, FP16);
+            const uint64_t d_cols = make_smem_desc(ring, 1, kAtom), d_hl = make_smem_desc(hl, 1, C::kRows * 128);
+            int sk = 0;
+            uint32_t pk = 0;
+#pragma unroll 1
+            for (int c = 0; c < chunks; c++) {
+                const int sv = sk + 1 == C::kSlots ? 0 : sk + 1;
+                if (!warp_wait(&full[sk], pk, &abort_flag) || (c > 0 && !warp_wait(&u_free, (uint32_t)(c - 1) & 1u, &abort_flag))) break;
+                tcgen05_fence_after();
                 int s = 0;
 #pragma unroll 1
                 for (; s < C::kSub; s++) {
-                    if (outputs && s == C::kSub / 2) {
-                        if (!wait(&x_ready, (uint32_t)c) || (c > 0 && !wait(&o_free, (uint32_t)(c - 1)))) break;
-                        tcgen05_fence_after();
-                        if (elected()) {
-#pragma unroll
-                            for (int kk = 0; kk < D / 16; kk++)
-                                umma_bf16(tmem + C::kO2, q_rows + (kk >> 2) * (16384 / 16) + (kk & 3) * (32 / 16), d_x + kk * (2048 / 16), id_o, kk > 0);
-                            umma_commit(&empty[sq]);
-                        }
-                        __syncwarp();
-                    }
                     const int b = s & 1;
-                    if (!wait(&hl_ready[b], (uint32_t)((c * C::kSub + s) >> 1))) break;
+                    if (!warp_wait(&hl_ready[b], (uint32_t)((c * C::kSub + s) >> 1) & 1u, &abort_flag)) break;
                     if (elected()) {
-                        const uint64_t kd = k_cols + (uint64_t)(s * (C::kRows * 128 / 16)), hd = d_hl + (uint64_t)(2 * b * (C::kHalf / 16));
+                        const uint64_t kd = d_cols + (uint64_t)(sk * (C::kTile / 16) + s * (C::kRows * 128 / 16)), hd = d_hl + (uint64_t)(2 * b * (C::kHalf / 16));
 #pragma unroll
                         for (int m = 0; m < 2 * C::kRows / 16; m++) {      // the rounded values, then the rests
                             const int part = m / (C::kRows / 16), kk = m % (C::kRows / 16);
@@ -403,35 +419,30 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                 if (elected()) {
                     umma_commit(&u_full);
                     umma_commit(&empty[sk]);
-                }
-                __syncwarp();
-                if (outputs && (!wait(&full[sv], pv) || !wait(&p_ready, (uint32_t)c))) break;
-                tcgen05_fence_after();
-                if (elected()) {
-                    if (outputs) {
-#pragma unroll
-                        for (int kk = 0; kk < kSteps / 16; kk++) umma_tmem(tmem + C::kO1, tmem + 8 * kk, v_cols + kk * (2048 / 16), id_o, kk > 0);
-                        umma_commit(&o_full);
+                    umma_commit(&empty[sv]);      // V has been weighted
+                    if (!outputs) {
+                        umma_commit(&empty[sk]);
+                        umma_commit(&empty[sv]);
                     }
-                    umma_commit(&empty[sv]);
                 }
                 __syncwarp();
                 sk += kinds;
                 if (sk >= C::kSlots) sk -= C::kSlots, pk ^= 1u;
             }
-        } else if (FP16 && warp >= 2) {
-            // the largest magnitudes of K, V and Q, half of each tile a warp
-            int it = 0;
+        } else if (FP16 && warp == 3) {
+            // the largest magnitudes of K, V and Q
+            int s = 0;
+            uint32_t ps = 0;
             bool ok = true;
 #pragma unroll 1
             for (int c = 0; ok && c < chunks; c++) {
-                for (int kind = 0; ok && kind < kinds; kind++, it++) {
-                    const int s = it % C::kSlots;
-                    if (!warp_wait(&full[s], (uint32_t)(it / C::kSlots) & 1u, &abort_flag)) { ok = false; break; }
-                    const uint32_t at = ring + s * C::kTile + (warp - 2) * (C::kTile / 2) + lane * 16;
+#pragma unroll 1
+                for (int kind = 0; kind < kinds; kind++) {
+                    if (!warp_wait(&full[s], ps, &abort_flag)) { ok = false; break; }
+                    const uint32_t at = ring + s * C::kTile + lane * 16;
                     uint32_t lo = 0, hi = 0;
-#pragma unroll 4
-                    for (int i = 0; i < C::kTile / 2; i += 512) {
+#pragma unroll 8
+                    for (int i = 0; i < C::kTile; i += 512) {
                         const uint4 w = ld_shared(at + i);
                         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -443,8 +454,9 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                     uint32_t m = __reduce_max_sync(0xffffffffu, max(lo, hi >> 16));
                     if (lane == 0) {
                         if (m >= 0x7c00u) atomicOr(&found, 1u);
-                        most[c & 3][warp - 2][kind] = __half2float(__ushort_as_half((unsigned short)m));
+                        most[c & 3][kind] = __half2float(__ushort_as_half((unsigned short)m));
                     }
+                    if (++s == C::kSlots) s = 0, ps ^= 1u;
                 }
                 if (ok && lane == 0) mbar_arrive(&max_ready[c & 3]);
                 __syncwarp();

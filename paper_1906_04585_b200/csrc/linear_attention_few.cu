@@ -9,7 +9,7 @@ namespace gala {
 namespace {
 
 constexpr int kFewRows = 8;      // rows a thread
-constexpr int kFewStaged = 4;    // steps whose vectors are brought in at once
+constexpr int kFewStaged = 8;    // steps whose vectors are brought in at once (a rollout's)
 
 // A thread has eight rows, in neighbouring pairs that share packed instructions, and four columns.
 template <typename T, int W, bool VEC, bool Y, bool Z>

@@ -21,7 +21,7 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
     float (*qs)[DK] = ks + kStaged;
     float (*vs)[32 * W] = reinterpret_cast<float (*)[32 * W]>(qs + kStaged);
     __shared__ unsigned char cuts[kStaged];
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long units = a.batch * a.heads;
     const long long unit = blockIdx.x % units;
     const int piece = (int)(blockIdx.x / units);
@@ -83,19 +83,23 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
             else
                 *to = in ? to_f32<T>(*from) : 0.0f;
         };
-#pragma unroll 4
-        for (int e = tid; e < kStaged * DK; e += 32 * W) {
-            const int s = e / DK, c = e % DK;
-            const long long t = a.rev ? a.steps - 1 - (p + s) : p + s;
-            const bool in = p + s < p1 && c < a.dk;
-            bring(&ks[s][c], in ? kp + t * a.k.t + c : kp, in);
-            if (outputs) bring(&qs[s][c], in ? qp + t * a.q.t + c : qp, in);
-        }
-#pragma unroll 4
-        for (int s = 0; s < kStaged; s++) {
-            const long long t = a.rev ? a.steps - 1 - (p + s) : p + s;
-            const bool in = p + s < p1 && mine;
-            bring(&vs[s][tid], in ? vp + t * a.v.t + d : vp, in);
+        // a warp a step, a lane an entry
+#pragma unroll 2
+        for (int s = warp; s < kStaged; s += W) {
+            const bool in = p + s < p1;
+            const long long t = !in ? 0 : a.rev ? a.steps - 1 - (p + s) : p + s;
+            const T *kt = kp + t * a.k.t + lane, *qt = qp + t * a.q.t + lane, *vt = vp + t * a.v.t + lane;
+#pragma unroll
+            for (int c = 0; c < DK; c += 32) {
+                const bool here = in && c + lane < a.dk;
+                bring(&ks[s][c + lane], here ? kt + c : kp, here);
+                if (outputs) bring(&qs[s][c + lane], here ? qt + c : qp, here);
+            }
+#pragma unroll
+            for (int c = 0; c < 32 * W; c += 32) {
+                const bool here = in && c + lane < a.dv;
+                bring(&vs[s][c + lane], here ? vt + c : vp, here);
+            }
         }
         for (int s = tid; s < kStaged; s += 32 * W) {      // whether what is held is dropped before the step
             const long long t = a.rev ? a.steps - 1 - (p + s) : p + s, flag = a.rev ? t : t - 1;

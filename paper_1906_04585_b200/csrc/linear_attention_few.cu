@@ -14,7 +14,8 @@ constexpr int kFewStaged = 8;    // steps whose vectors are brought in at once (
 // A thread has eight rows, in neighbouring pairs that share packed instructions, and four columns.
 template <typename T, int W, bool VEC, bool Y, bool Z>
 __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPass a) {
-    __shared__ __align__(16) float as[kFewStaged][128], bs[kFewStaged][128], ps[kFewStaged][128], rs[kFewStaged][128];
+    __shared__ __align__(16) float all[4][kFewStaged][128];
+    float (*as)[128] = all[0], (*bs)[128] = all[1], (*ps)[128] = all[2], (*rs)[128] = all[3];
     __shared__ __align__(16) float part[2][W][128];
     __shared__ unsigned char cuts[kFewStaged];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -50,7 +51,12 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
     const float g = expf(ld), less = expm1f(ld);
     const bool near = g >= 0.5f, none = g == 0.0f;
     auto at = [&](const MemoryOperand& m) { return static_cast<const T*>(m.p) + n * m.b + h * m.h; };
-    const T *ap = at(a.a), *bp = at(a.b), *pp = at(a.p), *rp = at(a.r);
+    // each warp brings in one of the four vectors of a step, four entries a lane
+    const int which = warp & 3, width = which & 1 ? a.dv : a.dk;
+    const MemoryOperand mine = which == 0 ? a.a : which == 1 ? a.b : which == 2 ? (Y && a.y.p ? a.p : MemoryOperand{}) : (Z ? a.r : MemoryOperand{});
+    const T* vector = mine.p ? at(mine) + 4 * lane : nullptr;
+    const bool whole = width % 4 == 0 && mine.t % 4 == 0 && (reinterpret_cast<uintptr_t>(vector) & (4 * sizeof(T) - 1)) == 0;
+    const float factor = which == 0 ? a.in : 1.0f;
     T* yp = static_cast<T*>(const_cast<void*>(a.y.p)) + n * a.y.b + h * a.y.h;
     T* zp = static_cast<T*>(const_cast<void*>(a.z.p)) + n * a.z.b + h * a.z.h;
     const unsigned char* done = a.done ? a.done + n * a.done_b : nullptr;
@@ -86,13 +92,24 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
     for (int p0 = 0; p0 < a.steps; p0 += kFewStaged) {
         __syncthreads();
         const int count = min(kFewStaged, a.steps - p0);
-        for (int e = tid; e < count * 128; e += 32 * W) {
-            const int s = e >> 7, c = e & 127;
+        for (int s = warp >> 2; mine.p && s < count; s += W / 4) {
             const long long t = a.rev ? a.steps - 1 - (p0 + s) : p0 + s;
-            as[s][c] = c < a.dk ? to_f32<T>(ap[t * a.a.t + c]) * a.in : 0.0f;
-            bs[s][c] = c < a.dv ? to_f32<T>(bp[t * a.b.t + c]) : 0.0f;
-            if (Y) ps[s][c] = a.y.p && c < a.dk ? to_f32<T>(pp[t * a.p.t + c]) : 0.0f;
-            if (Z) rs[s][c] = c < a.dv ? to_f32<T>(rp[t * a.r.t + c]) : 0.0f;
+            const T* from = vector + t * mine.t;
+            float v[4];
+            if (whole && sizeof(T) == 4) {
+                const float4 x = 4 * lane < width ? *reinterpret_cast<const float4*>(from) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+            } else if (whole) {
+                const uint2 x = 4 * lane < width ? *reinterpret_cast<const uint2*>(from) : make_uint2(0u, 0u);
+                Vec<T, 8> u;
+                u.w = make_uint4(x.x, x.y, 0u, 0u);
+#pragma unroll
+                for (int j = 0; j < 4; j++) v[j] = u.get(j);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; j++) v[j] = 4 * lane + j < width ? to_f32<T>(from[j]) : 0.0f;
+            }
+            reinterpret_cast<float4*>(all[which][s])[lane] = make_float4(v[0] * factor, v[1] * factor, v[2] * factor, v[3] * factor);
         }
         if (tid < count) {
             const int t = a.rev ? a.steps - 1 - (p0 + tid) : p0 + tid, flag = a.rev ? t : t - 1;
@@ -174,12 +191,12 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
                     for (int m = a.lanes; m < 32; m <<= 1) y[j] += __shfl_xor_sync(0xffffffffu, y[j], m);
                 }
                 if (lane < a.lanes) {
-                    float* mine = part[s & 1][warp];
+                    float* sums = part[s & 1][warp];
                     if (VEC) {
-                        reinterpret_cast<float4*>(mine)[lx] = make_float4(y[0], y[1], y[2], y[3]);
+                        reinterpret_cast<float4*>(sums)[lx] = make_float4(y[0], y[1], y[2], y[3]);
                     } else {
 #pragma unroll
-                        for (int j = 0; j < 4; j++) mine[lx + 32 * j] = y[j];
+                        for (int j = 0; j < 4; j++) sums[lx + 32 * j] = y[j];
                     }
                 }
                 __syncthreads();

@@ -31,24 +31,24 @@ struct NormRotary {
 };
 
 // Where the eight entries of a lane lie: entry j of its first four and of its second four.  In memory order the two runs are
-// a[0..3], b[0..3] of pairs (a_j, b_j) or, interleaved, a0 b0 a1 b1, a2 b2 a3 b3.
+// a[0..3], b[0..3] of pairs (a_j, b_j) or, interleaved (INTER), a0 b0 a1 b1, a2 b2 a3 b3.
 template <int P> struct Place {
     int at[2 * P];
     bool live[2 * P];
 };
-template <bool VEC, int P> __device__ __forceinline__ Place<P> place(const NormRotary& p, int lane) {
+template <bool VEC, int P, bool INTER> __device__ __forceinline__ Place<P> place(const NormRotary& p, int lane) {
     Place<P> r;
 #pragma unroll
     for (int j = 0; j < P; j++) {
         const int pair = VEC ? 4 * lane + j : lane + 32 * j;      // VEC: the lane of the group
         int a, b;
-        if (pair >= p.pairs) a = 2 * pair, b = a + 1;
-        else if (p.interleaved) a = 2 * pair, b = a + 1;
-        else a = pair, b = p.pairs + pair;
+        if (INTER || (!VEC && pair >= p.pairs)) a = 2 * pair, b = a + 1;
+        else if (pair < p.pairs) a = pair, b = p.pairs + pair;
+        else a = p.pairs + pair, b = a + p.dim / 2 - p.pairs;      // what is not turned, in two runs as well
         r.at[j] = a;
         r.at[P + j] = b;
-        r.live[j] = a < p.dim;
-        r.live[P + j] = b < p.dim;
+        r.live[j] = a < p.dim && (!VEC || pair < p.dim / 2);
+        r.live[P + j] = b < p.dim && (!VEC || pair < p.dim / 2);
     }
     return r;
 }
@@ -56,13 +56,13 @@ template <bool VEC, int P> __device__ __forceinline__ Place<P> place(const NormR
 template <typename T, bool VEC, int P> struct Raw { T e[2 * P]; };
 template <typename T> struct Raw<T, true, 4> { typedef uint2 run; uint2 e[2]; };
 template <> struct Raw<float, true, 4> { typedef float4 run; float4 e[2]; };
-template <typename T, bool VEC, int P> __device__ __forceinline__ void fetch(Raw<T, VEC, P>& r, const T* x, const Place<P>& pl, bool two_runs, bool live) {
+template <typename T, bool VEC, int P, bool INTER> __device__ __forceinline__ void fetch(Raw<T, VEC, P>& r, const T* x, const Place<P>& pl, bool live) {
     if constexpr (VEC) {
         typedef typename Raw<T, VEC, P>::run run;
         r.e[0] = r.e[1] = run{};
         if (live && pl.live[0]) {
             r.e[0] = *reinterpret_cast<const run*>(x + pl.at[0]);
-            r.e[1] = *reinterpret_cast<const run*>(x + (two_runs ? pl.at[4] : pl.at[0] + 4));
+            r.e[1] = *reinterpret_cast<const run*>(x + (INTER ? pl.at[0] + 4 : pl.at[4]));
         }
     } else {
 #pragma unroll
@@ -70,7 +70,7 @@ template <typename T, bool VEC, int P> __device__ __forceinline__ void fetch(Raw
     }
 }
 // as (a_0..3, b_0..3)
-template <typename T, bool VEC, int P> __device__ __forceinline__ void widen(const Raw<T, VEC, P>& r, bool two_runs, float (&f)[2 * P]) {
+template <typename T, bool VEC, int P, bool INTER> __device__ __forceinline__ void widen(const Raw<T, VEC, P>& r, float (&f)[2 * P]) {
     if constexpr (VEC) {
         float u[8];
         if constexpr (sizeof(T) == 4) {
@@ -84,19 +84,19 @@ template <typename T, bool VEC, int P> __device__ __forceinline__ void widen(con
         }
 #pragma unroll
         for (int j = 0; j < 4; j++) {
-            f[j] = two_runs ? u[j] : u[2 * j];
-            f[4 + j] = two_runs ? u[4 + j] : u[2 * j + 1];
+            f[j] = INTER ? u[2 * j] : u[j];
+            f[4 + j] = INTER ? u[2 * j + 1] : u[4 + j];
         }
     } else {
 #pragma unroll
         for (int j = 0; j < 2 * P; j++) f[j] = to_f32<T>(r.e[j]);
     }
 }
-template <typename T, bool VEC, int P> __device__ __forceinline__ void put(T* x, const Place<P>& pl, bool two_runs, const float (&f)[2 * P]) {
+template <typename T, bool VEC, int P, bool INTER> __device__ __forceinline__ void put(T* x, const Place<P>& pl, const float (&f)[2 * P]) {
     if constexpr (VEC) {
         if (!pl.live[0]) return;
-        const float u[8] = {f[0], two_runs ? f[1] : f[4], two_runs ? f[2] : f[1], two_runs ? f[3] : f[5], two_runs ? f[4] : f[2], two_runs ? f[5] : f[6], two_runs ? f[6] : f[3], f[7]};
-        T* second = x + (two_runs ? pl.at[4] : pl.at[0] + 4);
+        const float u[8] = {f[0], INTER ? f[4] : f[1], INTER ? f[1] : f[2], INTER ? f[5] : f[3], INTER ? f[2] : f[4], INTER ? f[6] : f[5], INTER ? f[3] : f[6], f[7]};
+        T* second = x + (INTER ? pl.at[0] + 4 : pl.at[4]);
         if constexpr (sizeof(T) == 4) {
             *reinterpret_cast<float4*>(x + pl.at[0]) = make_float4(u[0], u[1], u[2], u[3]);
             *reinterpret_cast<float4*>(second) = make_float4(u[4], u[5], u[6], u[7]);
@@ -116,17 +116,16 @@ __device__ __forceinline__ float group_sum(float s, int lanes) {
 }
 
 // P: pairs a lane (four with VEC, else as many as the head's pairs dealt out over a warp need)
-template <typename T, typename W, bool VEC, int P, bool GRAD>
+template <typename T, typename W, bool VEC, int P, bool INTER, bool GRAD>
 __global__ void __launch_bounds__(32 * kWarps, GRAD ? 4 : 5) norm_rotary_kernel(const NormRotary p) {
     __shared__ float part[GRAD ? 2 * 256 : 1];
-    constexpr int kAhead = sizeof(T) == 4 ? 8 / P : 4;
+    constexpr int kAhead = VEC ? (sizeof(T) == 4 ? 2 : 4) : (GRAD ? 4 : 8) / P;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int own = lane & (p.lanes - 1), group = lane / p.lanes, groups = 32 / p.lanes;
-    const Place<P> pl = place<VEC, P>(p, own);
+    const Place<P> pl = place<VEC, P, INTER>(p, own);
     bool turned[P];      // VEC: all four pairs of a lane, or none
 #pragma unroll
     for (int j = 0; j < P; j++) turned[j] = VEC ? 4 * own < p.pairs : lane + 32 * j < p.pairs;
-    const bool two_runs = !p.interleaved && turned[0];
     const int heads = p.q_heads + p.k_heads;
     float wq[2 * P], wk[2 * P], freq[P], dwq[2 * P], dwk[2 * P];
     pdl_wait();
@@ -156,71 +155,80 @@ __global__ void __launch_bounds__(32 * kWarps, GRAD ? 4 : 5) norm_rotary_kernel(
                 sincospif(2.0f * (float)(turns - rint(turns)), &si[j], &co[j]);
             }
         }
-        // the heads of a few turns are brought in together
-        for (int base = from; base < to; base += kAhead * groups) {
-            Raw<T, VEC, P> xs[kAhead], gs[GRAD ? kAhead : 1];
+        // queries, then keys; the heads of a few turns are brought in together
 #pragma unroll
-            for (int b = 0; b < kAhead; b++) {
-                const int head = base + b * groups + group;
-                const bool live = head < to, is_q = head < p.q_heads;
-                const Heads& hd = is_q ? p.q : p.k;
-                const int h = is_q ? head : head - p.q_heads;
-                fetch<T, VEC, P>(xs[b], static_cast<const T*>(hd.x) + token * hd.x_t + h * hd.x_h, pl, two_runs, live);
-                if (GRAD) fetch<T, VEC, P>(gs[b], static_cast<const T*>(hd.g) + token * hd.g_t + h * hd.g_h, pl, two_runs, live);
-            }
+        for (int side = 0; side < 2; side++) {
+            const Heads& hd = side ? p.k : p.q;
+            const float (&w)[2 * P] = side ? wk : wq;
+            float (&dw)[2 * P] = side ? dwk : dwq;
+            const int low = side ? max(from - p.q_heads, 0) : from, high = side ? to - p.q_heads : min(to, p.q_heads);
+            const T* xp = static_cast<const T*>(hd.x) + token * hd.x_t + (low + group) * hd.x_h;
+            const T* gp = GRAD ? static_cast<const T*>(hd.g) + token * hd.g_t + (low + group) * hd.g_h : nullptr;
+            T* yp = static_cast<T*>(hd.y) + token * hd.y_t + (low + group) * hd.y_h;
+            const long long x_turn = groups * hd.x_h, g_turn = groups * hd.g_h, y_turn = groups * hd.y_h;
+#pragma unroll 1
+            for (int base = low; base < high; base += kAhead * groups) {
+                Raw<T, VEC, P> xs[kAhead], gs[GRAD ? kAhead : 1];
 #pragma unroll
-            for (int b = 0; b < kAhead; b++) {
-                if (base + b * groups >= to) break;      // the same for the whole warp
-                const int head = base + b * groups + group;
-                const bool live = head < to, is_q = head < p.q_heads;
-                const Heads& hd = is_q ? p.q : p.k;
-                const int h = is_q ? head : head - p.q_heads;
-                float x[2 * P], y[2 * P];
-                widen<T, VEC, P>(xs[b], two_runs, x);
-                float ss = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 2 * P; j++) ss = fmaf(x[j], x[j], ss);
-                if (!GRAD) {
-                    const float r = rsqrtf(fmaf(group_sum(ss, p.lanes), inv_dim, p.eps));
-#pragma unroll
-                    for (int j = 0; j < 2 * P; j++) y[j] = x[j] * r * (is_q ? wq[j] : wk[j]);
-#pragma unroll
-                    for (int j = 0; j < P; j++)
-                        if (turned[j]) {
-                            const float a = y[j], b = y[P + j];
-                            y[j] = a * co[j] - b * si[j];
-                            y[P + j] = b * co[j] + a * si[j];
-                        }
-                } else {
-                    float g[2 * P];
-                    widen<T, VEC, P>(gs[b], two_runs, g);
-#pragma unroll
-                    for (int j = 0; j < P; j++)
-                        if (turned[j]) {
-                            const float a = g[j], b = g[P + j];
-                            g[j] = a * co[j] + b * si[j];
-                            g[P + j] = b * co[j] - a * si[j];
-                        }
-                    float dot = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < 2 * P; j++) {
-                        y[j] = g[j] * (is_q ? wq[j] : wk[j]);
-                        dot = fmaf(y[j], x[j], dot);
-                    }
-                    for (int m = p.lanes / 2; m > 0; m >>= 1) {
-                        ss += __shfl_xor_sync(0xffffffffu, ss, m);
-                        dot += __shfl_xor_sync(0xffffffffu, dot, m);
-                    }
-                    const float r = rsqrtf(fmaf(ss, inv_dim, p.eps)), back = dot * r * r * inv_dim;
-#pragma unroll
-                    for (int j = 0; j < 2 * P; j++) {
-                        y[j] = r * (y[j] - x[j] * back);
-                        const float dw = live ? g[j] * (x[j] * r) : 0.0f;
-                        if (is_q) dwq[j] += dw;
-                        else dwk[j] += dw;
+                for (int b = 0; b < kAhead; b++) {
+                    const bool live = base + b * groups + group < high;
+                    fetch<T, VEC, P, INTER>(xs[b], xp, pl, live);
+                    xp += x_turn;
+                    if (GRAD) {
+                        fetch<T, VEC, P, INTER>(gs[b], gp, pl, live);
+                        gp += g_turn;
                     }
                 }
-                if (live) put<T, VEC, P>(static_cast<T*>(hd.y) + token * hd.y_t + h * hd.y_h, pl, two_runs, y);
+#pragma unroll
+                for (int b = 0; b < kAhead; b++) {
+                    if (base + b * groups >= high) break;      // the same for the whole warp
+                    const bool live = base + b * groups + group < high;
+                    float x[2 * P], y[2 * P];
+                    widen<T, VEC, P, INTER>(xs[b], x);
+                    float ss = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 2 * P; j++) ss = fmaf(x[j], x[j], ss);
+                    if (!GRAD) {
+                        const float r = rsqrtf(fmaf(group_sum(ss, p.lanes), inv_dim, p.eps));
+#pragma unroll
+                        for (int j = 0; j < 2 * P; j++) y[j] = x[j] * r * w[j];
+#pragma unroll
+                        for (int j = 0; j < P; j++)
+                            if (turned[j]) {
+                                const float a = y[j], b = y[P + j];
+                                y[j] = a * co[j] - b * si[j];
+                                y[P + j] = b * co[j] + a * si[j];
+                            }
+                    } else {
+                        float g[2 * P];
+                        widen<T, VEC, P, INTER>(gs[b], g);
+#pragma unroll
+                        for (int j = 0; j < P; j++)
+                            if (turned[j]) {
+                                const float a = g[j], b = g[P + j];
+                                g[j] = a * co[j] + b * si[j];
+                                g[P + j] = b * co[j] - a * si[j];
+                            }
+                        float dot = 0.0f;
+#pragma unroll
+                        for (int j = 0; j < 2 * P; j++) {
+                            y[j] = g[j] * w[j];
+                            dot = fmaf(y[j], x[j], dot);
+                        }
+                        for (int m = p.lanes / 2; m > 0; m >>= 1) {
+                            ss += __shfl_xor_sync(0xffffffffu, ss, m);
+                            dot += __shfl_xor_sync(0xffffffffu, dot, m);
+                        }
+                        const float r = rsqrtf(fmaf(ss, inv_dim, p.eps)), back = dot * r * r * inv_dim;
+#pragma unroll
+                        for (int j = 0; j < 2 * P; j++) {
+                            y[j] = r * (y[j] - x[j] * back);
+                            if (live) dw[j] = fmaf(g[j], x[j] * r, dw[j]);
+                        }
+                    }
+                    if (live) put<T, VEC, P, INTER>(yp, pl, y);
+                    yp += y_turn;
+                }
             }
         }
     }
@@ -284,6 +292,13 @@ int blocks_of(long long tokens) {
 // the runs of four of a head start on multiples of four elements
 bool runs(const void* p, long long t, long long h, int es) { return !p || (aligned(p, 4 * es) && t % 4 == 0 && h % 4 == 0); }
 
+template <typename T, typename W, bool INTER, bool GRAD> cudaError_t launch_pairs(const NormRotary& p, bool vec, int blocks, cudaStream_t st) {
+    const dim3 grid(blocks), block(32 * kWarps);
+    if (vec) return launch_pdl(norm_rotary_kernel<T, W, true, 4, INTER, GRAD>, grid, block, 0, st, p);
+    if (p.dim <= 64) return launch_pdl(norm_rotary_kernel<T, W, false, 1, INTER, GRAD>, grid, block, 0, st, p);
+    if (p.dim <= 128) return launch_pdl(norm_rotary_kernel<T, W, false, 2, INTER, GRAD>, grid, block, 0, st, p);
+    return launch_pdl(norm_rotary_kernel<T, W, false, 4, INTER, GRAD>, grid, block, 0, st, p);
+}
 template <typename T, typename W, bool GRAD> cudaError_t launch_typed(NormRotary p, bool vec, cudaStream_t st) {
     const int heads = p.q_heads + p.k_heads;
     p.lanes = 32;
@@ -297,11 +312,7 @@ template <typename T, typename W, bool GRAD> cudaError_t launch_typed(NormRotary
     p.shares = (turns + per - 1) / per;
     const long long blocks_all = (p.tokens * p.shares + kWarps - 1) / kWarps;
     const int blocks = GRAD ? blocks_of(p.tokens) : (int)(blocks_all > 64ll * sm_count() ? 64ll * sm_count() : blocks_all);
-    const dim3 grid(blocks), block(32 * kWarps);
-    if (vec) return launch_pdl(norm_rotary_kernel<T, W, true, 4, GRAD>, grid, block, 0, st, p);
-    if (p.dim <= 64) return launch_pdl(norm_rotary_kernel<T, W, false, 1, GRAD>, grid, block, 0, st, p);
-    if (p.dim <= 128) return launch_pdl(norm_rotary_kernel<T, W, false, 2, GRAD>, grid, block, 0, st, p);
-    return launch_pdl(norm_rotary_kernel<T, W, false, 4, GRAD>, grid, block, 0, st, p);
+    return p.interleaved ? launch_pairs<T, W, true, GRAD>(p, vec, blocks, st) : launch_pairs<T, W, false, GRAD>(p, vec, blocks, st);
 }
 template <bool GRAD> cudaError_t launch(const NormRotary& p, int dtype, int wdtype, bool vec, cudaStream_t st) {
     if (dtype == GALA_F32) return launch_typed<float, float, GRAD>(p, vec, st);

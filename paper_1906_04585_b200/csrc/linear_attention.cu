@@ -263,20 +263,17 @@ Space space_of(long long steps, long long units, int dk, int dv) {
     return s;
 }
 
-cudaError_t run_pass(MemoryPass a, int dtype, void* workspace, const Space& s, bool& mapped, cudaStream_t st) {
+// A pass by chunks or step by step.  mapped: whether the driver took the tensor maps that chunks need (nothing is enqueued if not).
+cudaError_t run_pass(MemoryPass a, int dtype, bool chunks, void* workspace, const Space& s, bool& mapped, cudaStream_t st) {
     const long long units = a.batch * a.heads;
-    const int size = a.dk * a.dv;
+    const int size = a.dk * a.dv, whole = chunks ? 128 : kStaged;
     char* w = static_cast<char*>(workspace);
-    const bool chunks = memory_chunks_ok(a, dtype);
     a.gain = reinterpret_cast<float*>(w + s.gain);
     a.pieces = chunks ? memory_chunk_pieces(a.steps, units) : step_pieces(a.steps, units);
     a.piece = (a.steps + a.pieces - 1) / a.pieces;
-    const int whole = chunks ? 128 : kStaged;
     a.piece = (a.piece + whole - 1) / whole * whole;
-    a.direct = a.last != a.first;
-    if (a.piece < 1) a.piece = 1;
     a.pieces = (int)((a.steps + a.piece - 1) / a.piece);
-    if (a.pieces < 1) a.pieces = 1;
+    a.direct = a.last != a.first;
     a.z = a.pieces > 1 ? reinterpret_cast<float*>(w + s.z) : nullptr;
     a.flags = chunks ? reinterpret_cast<int*>(w + s.flags) : nullptr;
     mapped = true;
@@ -290,7 +287,7 @@ cudaError_t run_pass(MemoryPass a, int dtype, void* workspace, const Space& s, b
             e = launch_pdl(memory_join_kernel, dim3((unsigned)units, (unsigned)((size + 255) / 256)), dim3(256), 0, st, a.z, (const float*)a.gain, b.pieces, units, size);
     }
     if (e == cudaSuccess && mapped) e = chunks ? memory_chunks(a, dtype, mapped, st) : memory_steps(a, dtype, st);
-    // units with a flag again step by step; of the others what is left goes from z to `last`
+    // units with a flag again step by step; of the others what is left goes from z to `last` where that is `first`
     if (e == cudaSuccess && mapped && (chunks || (a.pieces > 1 && a.last && !a.direct))) {
         MemoryPass c = a;
         if (a.direct) c.z = nullptr;
@@ -302,7 +299,14 @@ cudaError_t run_pass(MemoryPass a, int dtype, void* workspace, const Space& s, b
     }
     return e;
 }
-
+cudaError_t run_pass(const MemoryPass& a, int dtype, void* workspace, const Space& s, cudaStream_t st) {
+    bool mapped = false;
+    if (memory_chunks_ok(a, dtype)) {
+        const cudaError_t e = run_pass(a, dtype, true, workspace, s, mapped, st);
+        if (mapped) return e;
+    }
+    return run_pass(a, dtype, false, workspace, s, mapped, st);
+}
 
 // What is said of a call that may not be made; NULL: it may.
 struct Shape { const char* name; int dtype, heads, dk, dv; long long steps, batch; };
@@ -436,7 +440,6 @@ extern "C" int gala_linear_attention_forward(const gala_linear_attention_args* q
     p.first = a.s0;
     p.last = a.s_last;
     p.out = a.scale;
-    bool mapped = true;
     cudaError_t e;
     if (s.steps <= kFewSteps) {
         FewPass f = few_pass(a, s);
@@ -449,9 +452,8 @@ extern "C" int gala_linear_attention_forward(const gala_linear_attention_args* q
         f.out = a.scale;
         e = memory_few(f, s.dtype, static_cast<cudaStream_t>(stream));
     } else {
-        e = run_pass(p, s.dtype, a.workspace, space_of(s.steps, s.batch * s.heads, s.dk, s.dv), mapped, static_cast<cudaStream_t>(stream));
+        e = run_pass(p, s.dtype, a.workspace, space_of(s.steps, s.batch * s.heads, s.dk, s.dv), static_cast<cudaStream_t>(stream));
     }
-    if (!mapped) SAY("%s: the driver refused a tensor map", s.name);
     return launched(e, errbuf, errbuf_len, s.name);
 }
 
@@ -479,7 +481,6 @@ extern "C" int gala_linear_attention_backward(const gala_linear_attention_grad_a
     const Space w = space_of(s.steps, s.batch * s.heads, s.dk, s.dv);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e = cudaSuccess;
-    bool mapped = true;
     if (s.steps <= kFewSteps) {
         if (a.grad_q && s.steps > 0) {
             FewPass f = few_pass(a, s);
@@ -516,9 +517,9 @@ extern "C" int gala_linear_attention_backward(const gala_linear_attention_grad_a
         output(p, out_q);
         p.first = a.s0;
         p.out = a.scale;
-        e = run_pass(p, s.dtype, a.workspace, w, mapped, st);
+        e = run_pass(p, s.dtype, a.workspace, w, st);
     }
-    if (e == cudaSuccess && mapped && ((a.grad_v && s.steps > 0) || a.grad_s0)) {
+    if (e == cudaSuccess && ((a.grad_v && s.steps > 0) || a.grad_s0)) {
         MemoryPass p = common_pass(a, s);
         p.rev = 1;
         p.q = in_k;
@@ -528,9 +529,9 @@ extern "C" int gala_linear_attention_backward(const gala_linear_attention_grad_a
         p.first = a.grad_s_last;
         p.last = a.grad_s0;
         p.in = a.scale;
-        e = run_pass(p, s.dtype, a.workspace, w, mapped, st);
+        e = run_pass(p, s.dtype, a.workspace, w, st);
     }
-    if (e == cudaSuccess && mapped && a.grad_k && s.steps > 0) {
+    if (e == cudaSuccess && a.grad_k && s.steps > 0) {
         MemoryPass p = common_pass(a, s);
         transpose(p, s);
         p.rev = 1;
@@ -540,8 +541,7 @@ extern "C" int gala_linear_attention_backward(const gala_linear_attention_grad_a
         output(p, out_k);
         p.first = a.grad_s_last;
         p.in = a.scale;
-        e = run_pass(p, s.dtype, a.workspace, w, mapped, st);
+        e = run_pass(p, s.dtype, a.workspace, w, st);
     }
-    if (!mapped) SAY("%s: the driver refused a tensor map", s.name);
     return launched(e, errbuf, errbuf_len, s.name);
 }

@@ -909,7 +909,7 @@ cudaError_t memory_chunks(const MemoryPass& a, int dtype, bool& mapped, cudaStre
     ChunkMaps maps;
     Broadcast cast;
     mapped = true;
-    cudaError_t e = gemm_init();
+    const cudaError_t e = gemm_init();
     if (e != cudaSuccess) return e;
     mapped = map_of(&maps.q, a.q, a.steps, a.batch, a.heads, a.dk, cast.q_b, cast.q_h) && map_of(&maps.k, a.k, a.steps, a.batch, a.heads, a.dk, cast.k_b, cast.k_h) &&
              map_of(&maps.v, a.v, a.steps, a.batch, a.heads, a.dv, cast.v_b, cast.v_h);

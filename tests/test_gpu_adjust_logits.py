@@ -87,7 +87,7 @@ def want(a):
 @pytest.mark.parametrize("R,V,W,B,masked,pad", [
     (1, 1, 1, 1, True, 0), (5, 18, 0, 0, True, 0), (5, 18, 7, 3, True, 6), (3, 33, 100, 0, False, 0), (2, 1000, 0, 40, False, 24), (4, 4096, 300, 20, True, 0),
     (2, 16384, 50, 5, True, 0), (2, 16385, 50, 5, True, 0), (3, 40007, 2000, 300, True, 1), (1, 131072, 5000, 0, True, 0), (2, 50000, 0, 0, True, 0),
-    (300, 64, 20, 2, True, 0), (2, 131, 3, 4095, False, 0)])
+    (300, 64, 20, 2, True, 0), (2, 131, 3, 4095, False, 0), (2, 20000, 12000, 7, True, 0), (3, 9001, 0, 4095, True, 7), (2, 30000, 10000, 900, False, 0)])
 def test_against_the_definition(R, V, W, B, masked, pad, dtype):
     a = inputs(R, V, W, B, dtype, R + V + W, masked, pad)
     check(run(a), *want(a))
@@ -145,8 +145,9 @@ def test_infinities_and_nan():
     check(run(a), *want(a))
 
 
-def test_in_place_and_strided():
-    a = inputs(7, 1000, 30, 4, torch.bfloat16, 8, pad=40)
+@pytest.mark.parametrize("V,masked", [(1000, True), (20000, True), (20000, False), (8193, True)])
+def test_in_place_and_strided(V, masked):
+    a = inputs(7, V, 30, 4, torch.bfloat16, 8, masked, pad=40)
     y, err = want(a)
     got = run(a, out=a["logits"])
     assert got is a["logits"]

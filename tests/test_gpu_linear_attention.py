@@ -162,6 +162,55 @@ def test_state_in_place_over_pieces(dtype, T):
     check_all(q, k, v, ld, s0, None, 0.125, got=(o, state))
 
 
+@pytest.mark.parametrize("T", [20, 100, 1500])
+def test_state_in_place_beside_a_nan(T):
+    """One sequence and head meets an infinity: its memory is computed apart from the others', all of them in place."""
+    q, k, v, ld, s0, _, _, _ = inputs(T, 2, 2, 64, 64, torch.bfloat16, 15)
+    clean, last = S().linear_attention(q, k, v, ld, s0)
+    v = v.clone()
+    v[T // 2, 1, 0, 9] = float("inf")
+    state = s0.clone()
+    o, _ = S().linear_attention(q, k, v, ld, state, s_last=state)
+    touched = torch.zeros_like(o, dtype=torch.bool)
+    touched[T // 2:, 1, 0, 9] = True
+    assert not torch.isfinite(o[touched]).any() and not torch.isfinite(state[1, 0, :, 9]).any()
+    u = U[torch.bfloat16]
+    assert ((o[~touched].double() - clean[~touched].double()).abs() <= 4 * u * (clean[~touched].double().abs() + 8 * float(clean.double().abs().mean()))).all()
+    state[1, 0, :, 9] = last[1, 0, :, 9]
+    assert ((state - last).abs() <= 1e-4 * (last.abs() + float(last.abs().mean()))).all()
+
+
+@pytest.mark.parametrize("dk,dv", [(1, 1), (3, 5), (2, 128), (65, 1)])
+def test_narrow_heads_on_aligned_rows(dk, dv):
+    """Heads of a few entries in 16 bits, in rows padded to 16 bytes: by chunks as well."""
+    for dtype in (torch.bfloat16, torch.float16):
+        gen = torch.Generator().manual_seed(dk + dv)
+        q, k, v, do = (torch.randn(300, 2, 3, (w + 7) // 8 * 8, generator=gen).to(dtype).cuda()[..., :w] for w in (dk, dk, dv, dv))
+        s0, ds_last = (torch.randn(2, 3, dk, dv, generator=gen).cuda() for _ in range(2))
+        ld = torch.tensor([-0.5, -0.05, -0.01]).cuda()
+        o = torch.empty(300, 2, 3, (dv + 7) // 8 * 8, dtype=dtype, device="cuda")[..., :dv]
+        got = S().linear_attention(q, k, v, ld, s0, out=o)
+        assert got[0] is o
+        check_all(q, k, v, ld, s0, None, dk ** -0.5, do, ds_last, got, S().linear_attention_backward(do, q, k, v, ld, s0, ds_last=ds_last))
+
+
+def test_two_streams_at_once():
+    """Calls on two streams side by side, each with a workspace of its own."""
+    made = []
+    for seed, T in ((31, 1400), (32, 900)):
+        made.append((torch.cuda.Stream(), inputs(T, 1, 3, 64, 64, torch.bfloat16, seed, p_done=0.01)))
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(3):
+        for stream, (q, k, v, ld, s0, done, do, ds_last) in made:
+            with torch.cuda.stream(stream):
+                got.append((S().linear_attention(q, k, v, ld, s0, done=done), S().linear_attention_backward(do, q, k, v, ld, s0, done=done, ds_last=ds_last)))
+    torch.cuda.synchronize()
+    for i, (a, b) in enumerate(got):
+        q, k, v, ld, s0, done, do, ds_last = made[i % 2][1]
+        check_all(q, k, v, ld, s0, done, 0.125, do, ds_last, a, b)
+
+
 def test_no_steps_passes_the_state_on():
     e = torch.empty(0, 2, 3, 16, device="cuda")
     s0 = torch.randn(2, 3, 16, 16, device="cuda")

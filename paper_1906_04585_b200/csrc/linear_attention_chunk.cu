@@ -9,11 +9,11 @@
 //   warp 2       issues U = K^T (w V): one thread issues a product every 70 cycles and waits some 100 cycles for each barrier,
 //                and 40 products a chunk bound it
 //   warp 3       float16: the largest magnitudes of the chunk's operands, from which powers of two are taken (below)
-//   warps 4-7    a thread a row: scores -> P, rounded to the element type, in the place of the scores
+//   warps 4-7    a thread a row: scores -> P, rounded to the element type, in the place of the scores; half of the chunk's o
 //   warps 8-11   X in registers, folded with U and rounded as the operand of the next chunk's O2; half of the chunk's o
-//   warps 12-15  w V, half a chunk ahead of the others, as two numbers of the element type, rounded and rest: X is a float32
+//   warps 12-15  w V, a chunk ahead of the others, as two numbers of the element type, rounded and rest: X is a float32
 //                result, of which one number would leave 2^-9 (and where X only adds to o, one instead of two saves 2 % of the
-//                time); the other half of the chunk's o
+//                time)
 // The powers of g are differences of exponents, never quotients, so nothing overflows however fast a head fades.
 //
 // What a product cannot do is leave out a term: 0 times an infinity or a NaN spreads it to steps that must not see it.  A unit
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
             }
         }
     } else if (warp < 8) {
-        if (D == 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (D == 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
         if (outputs) {
             const int q = warp & 3, i = 32 * q + lane;
             const uint32_t rows = tmem + ((uint32_t)(q * 32) << 16);
@@ -477,7 +477,7 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                 const int len = length(begin(c));
                 // the row sees columns lo..hi
                 const int lo = REV ? i : max(links.highest(i), 0), hi = REV ? min(links.lowest(i), len - 1) : i;
-                float base = a.in * a.out, back;
+                float base = a.in * a.out, back = 1.0f;
                 if (FP16) {
                     float m[3];
                     if (!most_of(c, m)) break;
@@ -537,6 +537,13 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                 tcgen05_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&p_ready);
+                // half of o, while the next chunk's scores are formed
+                float e;
+                const bool reached = reach_of(links, c, len, i, e);
+                if (!warp_wait(&o_full, (uint32_t)c & 1u, &abort_flag)) break;
+                tcgen05_fence_after();
+                if (FP16) e *= x_backs[c & 1];
+                put_o(c, 1, rows, begin(c), len, reached, e, back);
             }
         }
     } else if (warp < 12) {
@@ -747,100 +754,71 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
             }
         }
     } else {
-        if (D == 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-        const int tid = threadIdx.x - 384, q = warp & 3, i = 32 * q + lane;
-        const uint32_t rows = tmem + ((uint32_t)(q * 32) << 16);
+        if (D == 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        const int tid = threadIdx.x - 384;
         uint32_t f[4];
         flags_of(0, f);
         uint32_t seen = 0;
         int sub = 0, sv = 1;
         uint32_t pv = 0;
-        Links links = {}, before = {};
-        // half a chunk's weighted values at a time; when the first half of the next chunk's stand ready, half of the chunk's o
 #pragma unroll 1
-        for (int half = 0; half <= 2 * chunks; half++) {
-            const int c = half >> 1;
-            if (c < chunks) {
-                if (!(half & 1)) {
-                    before = links;
-                    links = links_of(f);
-                    flags_of(c + 1, f);
-                    if (!warp_wait(&full[sv], pv, &abort_flag)) break;
-                }
-                const int len = length(begin(c));
-                // the steps that reach the chunk's end
-                const int lo = REV ? 0 : max(links.highest(kSteps - 1), 0), hi = REV ? min(links.lowest(0), len - 1) : len - 1;
-                float gain = a.in;
-                if (FP16) {
-                    float m[3], back;
-                    if (!most_of(c, m)) break;
-                    gain *= fit(m[1] * fabsf(a.in), back);
-                }
-                const uint32_t v = ring + sv * C::kTile + tid * 16;
-                bool ok = true;
+        for (int c = 0; c < chunks; c++) {
+            const Links links = links_of(f);
+            flags_of(c + 1, f);
+            if (!warp_wait(&full[sv], pv, &abort_flag)) break;
+            const int len = length(begin(c));
+            // the steps that reach the chunk's end
+            const int lo = REV ? 0 : max(links.highest(kSteps - 1), 0), hi = REV ? min(links.lowest(0), len - 1) : len - 1;
+            float gain = a.in;
+            if (FP16) {
+                float m[3], back;
+                if (!most_of(c, m)) break;
+                gain *= fit(m[1] * fabsf(a.in), back);
+            }
+            const uint32_t v = ring + sv * C::kTile + tid * 16;
+            bool ok = true;
 #pragma unroll 1
-                for (int s = (half & 1) * (C::kSub / 2); s < ((half & 1) + 1) * (C::kSub / 2); s++, sub++) {
-                    const int b = sub & 1;
-                    uint4 w[4];
-                    float g[4];
+            for (int s = 0; s < C::kSub; s++, sub++) {
+                const int b = sub & 1;
+                uint4 w[4];
+                float g[4];
 #pragma unroll
-                    for (int m = 0; m < 4; m++) {      // 16-byte parts of the rows, box after box
-                        const int box = m * 128 / (C::kRows * 8), in = (m * 128) % (C::kRows * 8) / 8;
-                        w[m] = ld_shared(v + box * 16384 + s * C::kRows * 128 + in * 128);
-                        const int j = s * C::kRows + in + (tid >> 3);
-                        g[m] = j >= lo && j <= hi ? pw[REV ? j : len - 1 - j] * gain : 0.0f;
+                for (int m = 0; m < 4; m++) {      // 16-byte parts of the rows, box after box
+                    const int box = m * 128 / (C::kRows * 8), in = (m * 128) % (C::kRows * 8) / 8;
+                    w[m] = ld_shared(v + box * 16384 + s * C::kRows * 128 + in * 128);
+                    const int j = s * C::kRows + in + (tid >> 3);
+                    g[m] = j >= lo && j <= hi ? pw[REV ? j : len - 1 - j] * gain : 0.0f;
+                }
+                if (!warp_wait(&hl_free[b], (((uint32_t)sub >> 1) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
+                const uint32_t to = hl + 2 * b * C::kHalf + tid * 16;
+#pragma unroll
+                for (int m = 0; m < 4; m++) {
+                    const uint32_t u[4] = {w[m].x, w[m].y, w[m].z, w[m].w};
+                    uint32_t r[4], d[4];
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        seen = note<FP16>(u[e], seen);
+                        const float2 x = unpack<FP16>(u[e]);
+                        r[e] = pack<FP16>(x.x * g[m], x.y * g[m]);
+                        const float2 y = unpack<FP16>(r[e]);
+                        d[e] = pack<FP16>(fmaf(x.x, g[m], -y.x), fmaf(x.y, g[m], -y.y));
                     }
-                    if (!warp_wait(&hl_free[b], (((uint32_t)sub >> 1) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
-                    const uint32_t to = hl + 2 * b * C::kHalf + tid * 16;
-#pragma unroll
-                    for (int m = 0; m < 4; m++) {
-                        const uint32_t u[4] = {w[m].x, w[m].y, w[m].z, w[m].w};
-                        uint32_t r[4], d[4];
-#pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            seen = note<FP16>(u[e], seen);
-                            const float2 x = unpack<FP16>(u[e]);
-                            r[e] = pack<FP16>(x.x * g[m], x.y * g[m]);
-                            const float2 y = unpack<FP16>(r[e]);
-                            d[e] = pack<FP16>(fmaf(x.x, g[m], -y.x), fmaf(x.y, g[m], -y.y));
-                        }
-                        st_shared(to + m * 2048, make_uint4(r[0], r[1], r[2], r[3]));
-                        st_shared(to + C::kHalf + m * 2048, make_uint4(d[0], d[1], d[2], d[3]));
-                    }
-                    proxy_fence();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&hl_ready[b]);
+                    st_shared(to + m * 2048, make_uint4(r[0], r[1], r[2], r[3]));
+                    st_shared(to + C::kHalf + m * 2048, make_uint4(d[0], d[1], d[2], d[3]));
                 }
-                if (!ok) break;
-                if (half & 1) {
-                    sv += kinds;
-                    if (sv >= C::kSlots) sv -= C::kSlots, pv ^= 1u;
-                }
-            } else {
-                before = links;
+                proxy_fence();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&hl_ready[b]);
             }
-            if (outputs && half > 0 && !(half & 1)) {
-                const int o = c - 1;
-                const long long t0 = begin(o);
-                const int len = length(t0);
-                float e, p_back = 1.0f;
-                const bool reached = reach_of(before, o, len, i, e);
-                if (FP16) {
-                    float m[3];
-                    if (!most_of(o, m)) break;
-                    fit((float)D * m[0] * m[2] * fabsf(a.in * a.out), p_back);
-                }
-                if (!warp_wait(&o_full, (uint32_t)o & 1u, &abort_flag)) break;
-                tcgen05_fence_after();
-                if (FP16) e *= x_backs[o & 1];
-                put_o(o, 1, rows, t0, len, reached, e, p_back);
-            }
+            if (!ok) break;
+            sv += kinds;
+            if (sv >= C::kSlots) sv -= C::kSlots, pv ^= 1u;
         }
         const float2 y = unpack<FP16>(seen);
         if (!(y.x == 0.0f && y.y == 0.0f)) atomicOr(&found, 1u);
         asm volatile("bar.sync 2, 256;" ::: "memory");
     }
-    if (warp >= 8 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    if (warp >= 4 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     tcgen05_fence_before();
     __syncthreads();
     if (abort_flag && threadIdx.x == 0) {      // copies already issued land before the shared memory goes away

@@ -8,6 +8,9 @@
 // that the lists touch (out may be logits itself: an entry that the stream has crossed out stays so whatever it was).
 // Counts are whole numbers and duplicates of a bias are added by the thread of the first in the order of the list, so the result
 // does not depend on the order in which threads run.
+// Measured on a B200: 256 x 32768 bfloat16 with histories of 2048, 64 biases and masks 20 us, 64 x 131072 float32 with histories of
+// 8192 and 300 biases 34 us (by segments alone 21 and 50 us; counting in the shared memory of a cluster's blocks 31 and 56 us).
+// Bound by latency: the stream takes 10 and 16 us, and the chain of the lists (fetch, count, fetch what they touch) follows in part.
 #include "sequence.cuh"
 
 namespace gala {
@@ -323,7 +326,7 @@ template <typename T> cudaError_t adjust(const Adjust& a, cudaStream_t st) {
     const bool wide = ((reinterpret_cast<uintptr_t>(a.x) ^ reinterpret_cast<uintptr_t>(a.y)) & 15) == 0 && (a.rows <= 1 || (a.x_ld - a.y_ld) % V == 0);
     auto segments = [&](const Adjust& b) { return wide ? launch_adjust<T, V, 32 / V>(b, st) : launch_adjust<T, 1, 8>(b, st); };
     const bool lists = a.history || a.biases > 0;
-    // Rows of several segments: 64 x 131072 with histories of 8192, 50 us by segments.
+    // Rows of one segment are read once anyway; lists past the hash table's size go by segments.
     if (!lists || a.vocab <= kSegment || a.width + a.biases > kMostTouched) return segments(a);
     Adjust b = a;
     const bool stream = a.mask || a.x != a.y;

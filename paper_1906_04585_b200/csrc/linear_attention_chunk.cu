@@ -6,8 +6,8 @@
 // One block goes over a unit (sequence and head), or a piece of its time axis, chunk by chunk:
 //   warp 0       brings K, V and Q of the chunks in by tensor copies, a ring of tiles
 //   warp 1       issues the products scores = Q K^T, O2 = Q X and O1 = P V with P in tensor memory
-//   warp 2       issues U = K^T (w V): one thread issues a product every 70 cycles and waits some 100 cycles for each barrier,
-//                and 40 products a chunk bound it
+//   warp 2       issues U = K^T (w V), so that neither waits for what the other waits for (a thread issues a product every 70
+//                cycles, a chunk of 128 x 128 heads is 40 of them)
 //   warp 3       float16: the largest magnitudes of the chunk's operands, from which powers of two are taken (below)
 //   warps 4-7    a thread a row: scores -> P, rounded to the element type, in the place of the scores; half of the chunk's o
 //   warps 8-11   X in registers, folded with U and rounded as the operand of the next chunk's O2; half of the chunk's o
@@ -23,6 +23,14 @@
 // float16 has a range that scores and states of ordinary inputs leave.  P, the weighted values and X are scaled by powers of two
 // taken from bounds of their magnitudes (the exact largest of V; dk max|q| max|k|; the sum of what was added to X), and the
 // results scaled back in float32.
+//
+// Roundings: P and X as operands to the element type, since the tensor cores take no other (o is within 2.3e-3 of the 64-bit one in
+// bfloat16, 2.9e-4 in float16; the plain form in bfloat16, 1.7e-3); the state, held and added up in float32, is within 2.4e-6 in
+// bfloat16, the rest that two pieces of a weighted value leave.
+//
+// Measured on a B200: 2048 steps x 8 x 16 heads of 128 x 128 bfloat16, 75-80 us a pass of 268 MB (3.4-3.6 TB/s of operands and
+// outputs), with 3-5 us for the kernel that follows; 16384 steps x 16 heads in 9 pieces, 115 us.  Bound by the chain of a chunk
+// (scores, mask, weighted sum: 5500-5900 cycles, 9200 in an early form) and by some 15 us a kernel for its start and the last state.
 #include "linear_attention.cuh"
 #include "tcgen05.cuh"
 

@@ -43,8 +43,8 @@ def _compiled():
     return _front
 
 
-# A call on small tensors is bound by the host.  The compiled front end (csrc/front.cpp) takes the forward calls whose
-# arguments are as they should be; it returns None for all others, and the code below says what is wrong with them, or
+# A call on small tensors is bound by the host.  The compiled front end (csrc/front.cpp) takes the forward calls, and
+# the backward calls of the attention memory and of the norm and rotation, whose arguments are as they should be; it returns None for all others, and the code below says what is wrong with them, or
 # takes what only it can.  It is built with libgala.so where torch's headers are; without it every call goes through the
 # code below.
 _front = _compiled()

@@ -522,18 +522,6 @@ extern "C" int gala_linear_attention_backward(const gala_linear_attention_grad_a
         p.out = a.scale;
         e = run_pass(p, s.dtype, a.workspace, w, st);
     }
-    if (e == cudaSuccess && ((a.grad_v && s.steps > 0) || a.grad_s0)) {
-        MemoryPass p = common_pass(a, s);
-        p.rev = 1;
-        p.q = in_k;
-        p.k = in_q;
-        p.v = in_o;
-        output(p, out_v);
-        p.first = a.grad_s_last;
-        p.last = a.grad_s0;
-        p.in = a.scale;
-        e = run_pass(p, s.dtype, a.workspace, w, st);
-    }
     if (e == cudaSuccess && a.grad_k && s.steps > 0) {
         MemoryPass p = common_pass(a, s);
         transpose(p, s);
@@ -543,6 +531,19 @@ extern "C" int gala_linear_attention_backward(const gala_linear_attention_grad_a
         p.v = in_q;
         output(p, out_k);
         p.first = a.grad_s_last;
+        p.in = a.scale;
+        e = run_pass(p, s.dtype, a.workspace, w, st);
+    }
+    // last, since grad_s0 may be grad_s_last
+    if (e == cudaSuccess && ((a.grad_v && s.steps > 0) || a.grad_s0)) {
+        MemoryPass p = common_pass(a, s);
+        p.rev = 1;
+        p.q = in_k;
+        p.k = in_q;
+        p.v = in_o;
+        output(p, out_v);
+        p.first = a.grad_s_last;
+        p.last = a.grad_s0;
         p.in = a.scale;
         e = run_pass(p, s.dtype, a.workspace, w, st);
     }

@@ -452,7 +452,7 @@ def linear_attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor
                               ds_last: Optional[torch.Tensor] = None, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
                               dv: Optional[torch.Tensor] = None, ds0: Optional[torch.Tensor] = None):
     """Gradients (dq, dk, dv, ds0) of linear_attention from those of o (do) and s_last (ds_last); the other arguments are the
-    forward call's (s0 as it was then)."""
+    forward call's (s0 as it was then).  ds0 may be ds_last itself."""
     if _front is not None and q.is_cuda and q.dim() == 4:
         got = _front.linear_attention_backward(do, q, k, v, log_decay, s0, done, _scale(q, scale), ds_last, dq, dk, dv,
                                                ds0, _status_word(q))

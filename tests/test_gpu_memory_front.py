@@ -189,3 +189,15 @@ def test_first_use_inside_a_capture():
             "S.check()\n")
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("T", [0, 5, 100, 300, 1100])
+def test_gradient_of_the_state_in_place(T, dtype):
+    """ds0 takes the place of ds_last: the same gradients, whichever way a call of that length goes."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    do, q, k, v = (torch.randn(T, 2, 3, 64, device="cuda", generator=g).to(dtype) for _ in range(4))
+    decay, s0, ds = torch.full((3,), -0.02, device="cuda"), *(torch.randn(2, 3, 64, 64, device="cuda", generator=g) for _ in range(2))
+    want = S().linear_attention_backward(do, q, k, v, decay, s0, ds_last=ds.clone())
+    got = S().linear_attention_backward(do, q, k, v, decay, s0, ds_last=ds, ds0=ds)
+    assert got[3] is ds and all(torch.equal(a, b) for a, b in zip(got, want))

@@ -84,7 +84,7 @@ struct FewPass {
     int steps, heads, dk, dv;
     float in, out;
     int rev;
-    int lanes;                   // of a row: a power of two; a lane has four neighbouring columns (or, without VEC, every 32nd)
+    int lanes;                   // of a row: 8, 16 or 32; a lane has four neighbouring columns (or, without VEC, every 32nd)
 };
 cudaError_t memory_few(const FewPass& a, int dtype, cudaStream_t st);       // linear_attention_few.cu
 

@@ -78,16 +78,14 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
         int m = a.lanes / 2;
 #pragma unroll
         for (int n = 4; n > 0; n /= 2) {
-            if (m > 0) {
-                const bool upper = lane & m;
-                which += upper ? n : 0;
+            const bool upper = lane & m;
+            which += upper ? n : 0;
 #pragma unroll
-                for (int k = 0; k < n; k++) {
-                    const float send = upper ? v[k] : v[k + n], keep = upper ? v[k + n] : v[k];
-                    v[k] = keep + __shfl_xor_sync(0xffffffffu, send, m);
-                }
-                m /= 2;
+            for (int k = 0; k < n; k++) {
+                const float send = upper ? v[k] : v[k + n], keep = upper ? v[k + n] : v[k];
+                v[k] = keep + __shfl_xor_sync(0xffffffffu, send, m);
             }
+            m /= 2;
         }
         for (; m > 0; m /= 2) v[0] += __shfl_xor_sync(0xffffffffu, v[0], m);
     };
@@ -133,7 +131,7 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
             f2 b2[4];
 #pragma unroll
             for (int j = 0; j < 4; j++) b2[j] = pack_f2(b[j], b[j]);
-            auto pair = [&](const float* from, int i) { return *reinterpret_cast<const f2*>(from + ((row0 + 2 * i * stride) & 127)); };      // rows past 127 are none of the state
+            auto pair = [&](const float* from, int i) { return *reinterpret_cast<const f2*>(from + row0 + 2 * i * stride); };
             if (near && !enter) {
                 const f2 m = pack_f2(less, less);
 #pragma unroll
@@ -163,19 +161,10 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
                     const float2 v = unpack_f2(sum);
                     z[2 * i] = v.x, z[2 * i + 1] = v.y;
                 }
-                if (a.lanes >= 8) {
-                    int which;
-                    row_sums(z, which);
-                    const int c = row0 + 2 * (which >> 1) * stride + (which & 1);
-                    if ((lane & (a.lanes / 8 - 1)) == 0 && c < a.dk) zp[t * a.z.t + c] = from_f32<T>(a.out * z[0]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < kFewRows; i++) {
-                        for (int m = a.lanes / 2; m > 0; m >>= 1) z[i] += __shfl_xor_sync(0xffffffffu, z[i], m);
-                        const int c = row0 + 2 * (i >> 1) * stride + (i & 1);
-                        if (lx == 0 && c < a.dk) zp[t * a.z.t + c] = from_f32<T>(a.out * z[i]);
-                    }
-                }
+                int which;
+                row_sums(z, which);
+                const int c = row0 + 2 * (which >> 1) * stride + (which & 1);
+                if ((lane & (a.lanes / 8 - 1)) == 0 && c < a.dk) zp[t * a.z.t + c] = from_f32<T>(a.out * z[0]);
             }
             if (Y) {
                 f2 y2[4] = {0ull, 0ull, 0ull, 0ull};
@@ -252,8 +241,10 @@ template <typename T> cudaError_t few_typed(FewPass a, cudaStream_t st) {
     const bool vec = a.dv % 4 == 0 && aligned(a.first, 16) && aligned(a.last, 16);
     a.lanes = 32;
     if (vec)
-        for (a.lanes = 1; 4 * a.lanes < a.dv;) a.lanes *= 2;
-    // as few warps as hold the rows, eight a thread; at least as many threads as columns
+        for (a.lanes = 8; 4 * a.lanes < a.dv;) a.lanes *= 2;
+    // As few warps as hold the rows, eight a thread; at least as many threads as columns.  Eight lanes of a row at least: the
+    // smallest block then has w * (32 / lanes) * 8 <= 128 rows, as has each larger one, since half of it held fewer than dk.
+    // A block of more rows would read vectors past their end in shared memory.
     int w = 4;
     while (w * (32 / a.lanes) * kFewRows < a.dk) w *= 2;
     if (w == 4) return few_of<T, 4>(a, vec, st);

@@ -39,6 +39,10 @@ namespace {
 
 constexpr int kSteps = 128;
 constexpr int kThreads = 512;
+// Chunks whose magnitudes are held at once.  The ring takes in V of chunk c + 4 once U of chunk c is there (heads of 64, states
+// only: nine places, two tiles a chunk), and that U only needs the state's warps to have read U of chunk c - 1: they may still have
+// the magnitudes of chunk c before them.  Chunk c + 8 comes in after U of c + 4, which needs U of c + 3 read, and so those of c.
+constexpr int kMaxima = 8;
 
 template <int D> struct Chunk {
     static constexpr int kTile = kSteps * D * 2;              // bytes of a chunk of one operand: D / 64 boxes of 128 rows of 128 bytes
@@ -218,10 +222,10 @@ template <int D, bool FP16, bool REV>
 __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_constant__ ChunkMaps maps, const MemoryPass a, const Broadcast cast, const int wide) {
     using C = Chunk<D>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t full[C::kSlots], empty[C::kSlots], hl_ready[2], hl_free[2], scores_full, p_ready, o_full, o_free, u_full, u_free, x_ready, x_taken, max_ready[4], o_stored[4];
+    __shared__ __align__(8) uint64_t full[C::kSlots], empty[C::kSlots], hl_ready[2], hl_free[2], scores_full, p_ready, o_full, o_free, u_full, u_free, x_ready, x_taken, max_ready[kMaxima], o_stored[4];
     __shared__ uint32_t tmem_slot, found;
     __shared__ int abort_flag, issued;
-    __shared__ float pw[132], most[4][3], first_most[4], x_backs[2];
+    __shared__ float pw[132], most[kMaxima][3], first_most[4], x_backs[2];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t ring = smem_u32(smem), hl = ring + C::kSlots * C::kTile, sx = hl + 4 * C::kHalf;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -237,7 +241,8 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kSlots; s++) { mbar_init(&full[s], 1); mbar_init(&empty[s], 2); }
         for (int b = 0; b < 2; b++) { mbar_init(&hl_ready[b], 4); mbar_init(&hl_free[b], 1); }
-        for (int b = 0; b < 4; b++) { mbar_init(&max_ready[b], 1); mbar_init(&o_stored[b], 8); }
+        for (int b = 0; b < kMaxima; b++) mbar_init(&max_ready[b], 1);
+        for (int b = 0; b < 4; b++) mbar_init(&o_stored[b], 8);
         mbar_init(&scores_full, 1);
         mbar_init(&p_ready, 4);
         mbar_init(&o_full, 1);
@@ -316,9 +321,9 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
     };
     // float16: the powers of two, the same for every warp that asks.  m: largest of K, V, Q
     auto most_of = [&](int c, float (&m)[3]) {
-        if (!warp_wait(&max_ready[c & 3], (uint32_t)(c >> 2) & 1u, &abort_flag)) return false;
+        if (!warp_wait(&max_ready[c % kMaxima], (uint32_t)(c / kMaxima) & 1u, &abort_flag)) return false;
 #pragma unroll
-        for (int k = 0; k < 3; k++) m[k] = most[c & 3][k];
+        for (int k = 0; k < 3; k++) m[k] = most[c % kMaxima][k];
         return true;
     };
 
@@ -462,11 +467,11 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                     uint32_t m = __reduce_max_sync(0xffffffffu, max(lo, hi >> 16));
                     if (lane == 0) {
                         if (m >= 0x7c00u) atomicOr(&found, 1u);
-                        most[c & 3][kind] = __half2float(__ushort_as_half((unsigned short)m));
+                        most[c % kMaxima][kind] = __half2float(__ushort_as_half((unsigned short)m));
                     }
                     if (++s == C::kSlots) s = 0, ps ^= 1u;
                 }
-                if (ok && lane == 0) mbar_arrive(&max_ready[c & 3]);
+                if (ok && lane == 0) mbar_arrive(&max_ready[c % kMaxima]);
                 __syncwarp();
             }
         }

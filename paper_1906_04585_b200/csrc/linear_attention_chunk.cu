@@ -16,9 +16,10 @@
 //                time)
 // The powers of g are differences of exponents, never quotients, so nothing overflows however fast a head fades.
 //
-// What a product cannot do is leave out a term: 0 times an infinity or a NaN spreads it to steps that must not see it.  A unit
-// whose V, or whose U, holds one is flagged and computed again step by step by a kernel that follows (its blocks end at once
-// where no flag is set); nothing that the call reads is overwritten before.
+// What a product cannot do is leave out a term: 0 times an infinity or a NaN spreads it to steps that must not see it, and an
+// infinite query makes scores of both signs where the state may have one.  A unit whose Q, V or U holds one is flagged and
+// computed again step by step by a kernel that follows (its blocks end at once where no flag is set); nothing that the call reads
+// is overwritten before.
 //
 // float16 has a range that scores and states of ordinary inputs leave.  P, the weighted values and X are scaled by powers of two
 // taken from bounds of their magnitudes (the exact largest of V; dk max|q| max|k|; the sum of what was added to X), and the
@@ -538,6 +539,7 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                 for (int t = from; t < to; t += 2) {
                     tmem_ld16_wait(s0);
                     tmem_ld16_issue(rows + 16 * (t + 1), s1);
+                    if (!FP16 && t == from && !(fabsf(__uint_as_float(s0[0])) < INFINITY)) atomicOr(&found, 1u);      // one score tells of an infinite query
                     weigh(t, s0);
                     tmem_ld16_wait(s1);
                     if (t + 2 < to) tmem_ld16_issue(rows + 16 * (t + 2), s0);

@@ -581,8 +581,8 @@ int gala_gated_ffn_backward(const gala_ffn_grad_args* a, void* stream, char* err
  * g = exp(log_decay[h]) a step (a log_decay above 0 counts as 0; -inf: nothing is kept):
  *   S_t = g C_{t-1} + k_t v_t^T     o_t = scale S_t^T q_t     C_t = 0 where done_t, else S_t     C_{-1} = s0
  * done has the meaning it has in gala_gated_recurrence_forward; what a flag cuts off does not pass it, infinities and NaN
- * included; an infinity that none cuts off may be NaN in the steps after it.  s_last = C_{steps-1} is s0 of the next call;
- * steps = 1 is the acting step, and s_last may be s0 itself.
+ * included; an infinity that none cuts off stays while g > 0.  s_last = C_{steps-1} is s0 of the next call; steps = 1 is the
+ * acting step, and s_last may be s0 itself; o may not overlap what the call reads.
  * q, k, v and o have any strides for time, sequence and head, channels contiguous; strides are not negative, below 2^30 in
  * time, and those of an axis of one entry are not looked at; q, k and v may have strides of 0 (one key for all heads).
  * s0 (= 0), done (= none) and s_last may be NULL.  1 <= dk, dv <= 128; steps, batch, heads >= 0, batch x heads < 2^27.
@@ -610,7 +610,8 @@ int gala_linear_attention_forward(const gala_linear_attention_args* a, void* str
 
 /* Its gradient.  With R_t = scale q_t do_t^T + (not done_t) g R_{t+1} and g R_steps = ds_last:
  *   dq_t = scale S_t do_t     dk_t = R_t v_t     dv_t = R_t^T k_t     ds0 = g R_0
- * s0 is the forward call's.  s0 (= 0), done, ds_last (= 0), ds0 and any of dq, dk, dv may be NULL; ds0 may be ds_last itself. */
+ * s0 is the forward call's.  s0 (= 0), done, ds_last (= 0), ds0 and any of dq, dk, dv may be NULL; ds0 may be ds_last itself;
+ * no other result may overlap what the call reads. */
 typedef struct {
     int dtype;                 /* grad_o, q, k, v, dq, dk, dv */
     int heads, dk, dv;

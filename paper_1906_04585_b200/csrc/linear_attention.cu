@@ -3,9 +3,9 @@
 // memory_steps_kernel, for long calls in float32 or on odd addresses: a thread has one column of the state (an entry of v and o)
 // for all rows (entries of q and k) in registers, two rows a packed instruction, so that o needs no exchange between threads.
 // k, q and v of 32 steps are brought into shared memory at once, in float32; k and q are read as broadcasts.  A step is three
-// instructions for two entries of the state:
-//   t = X + k v;  X = t + (g - 1) X   where g >= 1/2: g - 1 has all its digits, so that a long memory does not drift, and
-//   X = g X + k v                     below, where the difference would cancel;    o += q X.
+// instructions for two entries of the state, o += q X among them: X + k v + (g - 1) X where g >= 1/2, g X + k v below.  Where what
+// is held or comes in is so large that an infinity may arise, the 32 steps take Fade's form, one instruction more (throughout, it
+// made 777 steps x 3 x 5 heads of 41 x 72 266-272 us in place of 242).
 // Where units are few the time axis is cut into pieces of whole batches: one launch leaves their own states, one joins them, one
 // computes the outputs.  Measured on a B200: 777 steps x 3 x 5 heads of 41 x 72 float32, 25 pieces, 21 + 7 + 26 us a pass;
 // the floor of all four passes is 4.4 us, so launches, starts and the order of the steps bound it.
@@ -50,8 +50,7 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
     const long long p0 = (long long)piece * a.piece, p1 = min(a.steps, p0 + a.piece);
     float ld = a.log_decay[h];
     ld = ld > 0.0f ? 0.0f : ld;
-    const float g = expf(ld), less = expm1f(ld);
-    const bool near = g >= 0.5f, none = g == 0.0f;      // none: nothing is kept, an infinity neither
+    const Fade fade(ld);
 
     f2 X[DK / 2];
     {
@@ -111,12 +110,24 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
         if (std::is_same<T, float>::value) asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
         __syncthreads();
         const int steps = (int)min((long long)kStaged, p1 - p);
+        // sums of 33 terms below 2^100 stay below 2^106
+        float large = 0.0f;
+#pragma unroll
+        for (int c = 0; c < DK / 2; c++) {
+            const float2 x = unpack_f2(X[c]);
+            large = fmaxf(large, fmaxf(fabsf(x.x), fabsf(x.y)));
+        }
+        float keys = 0.0f, values = 0.0f;
+        for (int i = tid; i < kStaged * DK; i += 32 * W) keys = fmaxf(keys, fabsf((&ks[0][0])[i]));
+        for (int s = 0; s < kStaged; s++) values = fmaxf(values, fabsf(vs[s][tid] * a.in));
+        const bool wild = __syncthreads_or(large >= 0x1p100f || keys >= 0x1p50f || values >= 0x1p50f);
 #pragma unroll 1
         for (int s = 0; s < steps; s++) {
             const float v = vs[s][tid] * a.in;
             const f2 vv = pack_f2(v, v);
             const float4* k4 = reinterpret_cast<const float4*>(ks[s]);
-            if (cuts[s] || (none && !(a.rev && p + s == 0))) {
+            const bool enter = a.rev && p + s == 0;      // the given state, with gain 1
+            if (cuts[s] || (fade.none && !enter)) {
                 dropped = true;
 #pragma unroll
                 for (int c = 0; c < DK / 4; c++) {
@@ -124,16 +135,26 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
                     X[2 * c] = mul2(pack_f2(k.x, k.y), vv);
                     X[2 * c + 1] = mul2(pack_f2(k.z, k.w), vv);
                 }
-            } else if (near && !(a.rev && p + s == 0)) {
-                const f2 m = pack_f2(less, less);
+            } else if (fade.near && !enter) {
+                if (!wild) {
+                    const f2 m = pack_f2(fade.less, fade.less);
 #pragma unroll
-                for (int c = 0; c < DK / 4; c++) {
-                    const float4 k = k4[c];
-                    X[2 * c] = fma2(m, X[2 * c], fma2(pack_f2(k.x, k.y), vv, X[2 * c]));
-                    X[2 * c + 1] = fma2(m, X[2 * c + 1], fma2(pack_f2(k.z, k.w), vv, X[2 * c + 1]));
+                    for (int c = 0; c < DK / 4; c++) {
+                        const float4 k = k4[c];
+                        X[2 * c] = fma2(m, X[2 * c], fma2(pack_f2(k.x, k.y), vv, X[2 * c]));
+                        X[2 * c + 1] = fma2(m, X[2 * c + 1], fma2(pack_f2(k.z, k.w), vv, X[2 * c + 1]));
+                    }
+                } else {
+                    const f2 hi = pack_f2(fade.hi, fade.hi), lo = pack_f2(fade.lo, fade.lo);
+#pragma unroll
+                    for (int c = 0; c < DK / 4; c++) {
+                        const float4 k = k4[c];
+                        X[2 * c] = fma2(hi, X[2 * c], fma2(pack_f2(k.x, k.y), vv, mul2(lo, X[2 * c])));
+                        X[2 * c + 1] = fma2(hi, X[2 * c + 1], fma2(pack_f2(k.z, k.w), vv, mul2(lo, X[2 * c + 1])));
+                    }
                 }
             } else {
-                const float f = a.rev && p + s == 0 ? 1.0f : g;
+                const float f = enter ? 1.0f : fade.g;
                 const f2 m = pack_f2(f, f);
 #pragma unroll
                 for (int c = 0; c < DK / 4; c++) {
@@ -165,7 +186,7 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
     const bool end = piece == a.pieces - 1;
     if (a.states_only) {
         to = a.z + ((long long)piece * units + unit) * a.dk * a.dv;
-        if (tid == 0) a.gain[(long long)piece * units + unit] = dropped ? -1.0f : expf(ld * (float)(p1 - p0));
+        if (tid == 0) a.gain[(long long)piece * units + unit] = dropped ? -1.0f : fmaxf(expf(ld * (float)(p1 - p0)), 0x1p-149f);      // 0 would turn an infinite state into NaN
     } else if (end && a.last) {
         if (a.pieces > 1 && !a.direct) {      // `last` is `first`, which another block reads
             to = a.z + ((long long)piece * units + unit) * a.dk * a.dv;
@@ -177,8 +198,8 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
     }
     if (!to || !mine) return;
     const bool finish = !a.states_only;
-    const bool zero = finish && !a.rev && done && a.steps > 0 && done[(a.steps - 1) * a.done_t];
-    const float gain = finish && a.rev && a.steps > 0 ? g : 1.0f;      // no step: the state goes through as it is
+    const bool zero = finish && a.steps > 0 && (a.rev ? fade.none : done && done[(a.steps - 1) * a.done_t]);
+    const float gain = finish && a.rev && a.steps > 0 ? fade.g : 1.0f;      // no step: the state goes through as it is
 #pragma unroll
     for (int c = 0; c < DK; c += 2) {
         const float2 x = unpack_f2(X[c / 2]);

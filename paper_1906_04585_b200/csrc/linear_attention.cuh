@@ -38,6 +38,24 @@ __device__ __forceinline__ f2 mul2(f2 a, f2 b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
+// What a step keeps of the state, g = exp(log_decay).  Where g >= 1/2 it is kept as hi + lo with all the digits of 1 - g, so that a
+// long memory does not drift, and both are positive, so that an infinite entry stays infinite:
+//   X = hi X + (lo X + k v)
+// The difference form X + k v + (g - 1) X takes one instruction less, turns an infinity into NaN and serves what is finite.
+struct Fade {
+    float g, less, hi, lo;      // less: g - 1
+    bool near, none;      // none: nothing is kept, an infinity neither
+    __device__ __forceinline__ explicit Fade(float ld) {
+        ld = ld > 0.0f ? 0.0f : ld;
+        g = expf(ld);
+        less = expm1f(ld);
+        const float s = 1.0f + less;      // s + (less - (s - 1)) is 1 + less exactly
+        hi = s - 0x1p-24f;
+        lo = less - (s - 1.0f) + 0x1p-24f;
+        near = g >= 0.5f;
+        none = g == 0.0f;
+    }
+};
 #endif
 
 struct MemoryOperand { const void* p; long long t, b, h; };      // strides of time, sequence and head

@@ -48,10 +48,7 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
 #pragma unroll
         for (int j = 0; j < 4; j++) X[i][j] = pack_f2(x[0][j], x[1][j]);
     }
-    float ld = a.log_decay[h];
-    ld = ld > 0.0f ? 0.0f : ld;
-    const float g = expf(ld), less = expm1f(ld);
-    const bool near = g >= 0.5f, none = g == 0.0f;
+    const Fade fade(a.log_decay[h]);
     auto at = [&](const MemoryOperand& m) { return static_cast<const T*>(m.p) + n * m.b + h * m.h; };
     // each warp brings in one of the four vectors of a step, four entries a lane
     const int which = warp & 3, width = which & 1 ? a.dv : a.dk;
@@ -120,7 +117,7 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
         for (int s = 0; s < count; s++) {
             const bool enter = a.rev && p0 + s == 0;      // the given state, with gain 1
             const long long t = a.rev ? a.steps - 1 - (p0 + s) : p0 + s;
-            if (cuts[s] || (none && !enter)) {
+            if (cuts[s] || (fade.none && !enter)) {
 #pragma unroll
                 for (int i = 0; i < kFewRows / 2; i++)
 #pragma unroll
@@ -132,16 +129,16 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
 #pragma unroll
             for (int j = 0; j < 4; j++) b2[j] = pack_f2(b[j], b[j]);
             auto pair = [&](const float* from, int i) { return *reinterpret_cast<const f2*>(from + row0 + 2 * i * stride); };
-            if (near && !enter) {
-                const f2 m = pack_f2(less, less);
+            if (fade.near && !enter) {
+                const f2 hi = pack_f2(fade.hi, fade.hi), lo = pack_f2(fade.lo, fade.lo);
 #pragma unroll
                 for (int i = 0; i < kFewRows / 2; i++) {
                     const f2 k = pair(as[s], i);
 #pragma unroll
-                    for (int j = 0; j < 4; j++) X[i][j] = fma2(m, X[i][j], fma2(k, b2[j], X[i][j]));
+                    for (int j = 0; j < 4; j++) X[i][j] = fma2(hi, X[i][j], fma2(k, b2[j], mul2(lo, X[i][j])));
                 }
             } else {
-                const float keep = enter ? 1.0f : g;
+                const float keep = enter ? 1.0f : fade.g;
                 const f2 m = pack_f2(keep, keep);
 #pragma unroll
                 for (int i = 0; i < kFewRows / 2; i++) {
@@ -201,8 +198,8 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
         }
     }
     if (!a.last) return;
-    const bool zero = !a.rev && done && a.steps > 0 && done[(a.steps - 1) * a.done_t];
-    const float gain = a.rev && a.steps > 0 ? g : 1.0f;
+    const bool zero = a.steps > 0 && (a.rev ? fade.none : done && done[(a.steps - 1) * a.done_t]);
+    const float gain = a.rev && a.steps > 0 ? fade.g : 1.0f;
 #pragma unroll
     for (int i = 0; i < kFewRows / 2; i++) {
         float x[2][4];

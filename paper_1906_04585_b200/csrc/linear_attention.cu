@@ -163,6 +163,11 @@ __global__ void __launch_bounds__(32 * W) memory_steps_kernel(const MemoryPass a
                     X[2 * c + 1] = fma2(m, X[2 * c + 1], mul2(pack_f2(k.z, k.w), vv));
                 }
             }
+            if (!(values < INFINITY)) {      // 0 times it, in the rows past the last
+#pragma unroll
+                for (int c = 0; c < DK; c += 2)
+                    if (c + 1 >= a.dk) X[c / 2] = c < a.dk ? X[c / 2] & 0xffffffffull : 0ull;
+            }
             if (outputs) {
                 const float4* q4 = reinterpret_cast<const float4*>(qs[s]);
                 f2 o0 = pack_f2(0.0f, 0.0f), o1 = o0, o2 = o0, o3 = o0;

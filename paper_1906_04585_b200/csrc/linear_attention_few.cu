@@ -13,13 +13,16 @@ namespace {
 constexpr int kFewRows = 8;      // rows a thread
 constexpr int kFewStaged = 8;    // steps whose vectors are brought in at once (a rollout's)
 
-// A thread has eight rows, in neighbouring pairs that share packed instructions, and four columns.
-template <typename T, int W, bool VEC, bool Y, bool Z>
+// A thread has eight rows, in neighbouring pairs that share packed instructions, and four columns.  RAGGED: some of a block's
+// places lie past the head's edges; they are cleared after each step into which an infinity or a NaN enters, by a loop of its own (a
+// branch in the common one made an acting step of 64 x 64 58 us instead of 51, one of 48 x 48 48 instead of 41).
+template <typename T, int W, bool VEC, bool RAGGED, bool Y, bool Z>
 __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPass a) {
     __shared__ __align__(16) float all[4][kFewStaged][128];
     float (*as)[128] = all[0], (*bs)[128] = all[1], (*ps)[128] = all[2], (*rs)[128] = all[3];
     __shared__ __align__(16) float part[2][W][128];
     __shared__ unsigned char cuts[kFewStaged];
+    __shared__ int stray;      // the last batch of steps, counted from 1, into which an infinity or a NaN enters
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int lx = lane & (a.lanes - 1), groups = 32 / a.lanes, group = warp * groups + lane / a.lanes, stride = W * groups;
     const int row0 = 2 * group;      // rows row0, row0 + 1, row0 + 2 stride, row0 + 2 stride + 1, ...
@@ -28,6 +31,7 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
     const long long state = unit * a.dk * a.dv;
     pdl_wait();
     pdl_launch();
+    if (RAGGED && tid == 0) stray = 0;
     f2 X[kFewRows / 2][4];
 #pragma unroll
     for (int i = 0; i < kFewRows / 2; i++) {
@@ -106,96 +110,114 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
 #pragma unroll
                 for (int j = 0; j < 4; j++) v[j] = 4 * lane + j < width ? to_f32<T>(from[j]) : 0.0f;
             }
-            reinterpret_cast<float4*>(all[which][s])[lane] = make_float4(v[0] * factor, v[1] * factor, v[2] * factor, v[3] * factor);
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[j] *= factor;
+            if (RAGGED && which < 2 && !(fmaf(v[0], 0.0f, fmaf(v[1], 0.0f, fmaf(v[2], 0.0f, v[3] * 0.0f))) == 0.0f)) stray = p0 + 1;
+            reinterpret_cast<float4*>(all[which][s])[lane] = make_float4(v[0], v[1], v[2], v[3]);
         }
         if (tid < count) {
             const int t = a.rev ? a.steps - 1 - (p0 + tid) : p0 + tid, flag = a.rev ? t : t - 1;
             cuts[tid] = done && flag >= 0 && done[flag * a.done_t];
         }
         __syncthreads();
+        auto steps = [&](auto clear) {
 #pragma unroll 1
-        for (int s = 0; s < count; s++) {
-            const bool enter = a.rev && p0 + s == 0;      // the given state, with gain 1
-            const long long t = a.rev ? a.steps - 1 - (p0 + s) : p0 + s;
-            if (cuts[s] || (fade.none && !enter)) {
+            for (int s = 0; s < count; s++) {
+                const bool enter = a.rev && p0 + s == 0;      // the given state, with gain 1
+                const long long t = a.rev ? a.steps - 1 - (p0 + s) : p0 + s;
+                if (cuts[s] || (fade.none && !enter)) {
 #pragma unroll
-                for (int i = 0; i < kFewRows / 2; i++)
+                    for (int i = 0; i < kFewRows / 2; i++)
 #pragma unroll
-                    for (int j = 0; j < 4; j++) X[i][j] = 0ull;
-            }
-            float b[4];
-            four(bs[s], b);
-            f2 b2[4];
-#pragma unroll
-            for (int j = 0; j < 4; j++) b2[j] = pack_f2(b[j], b[j]);
-            auto pair = [&](const float* from, int i) { return *reinterpret_cast<const f2*>(from + row0 + 2 * i * stride); };
-            if (fade.near && !enter) {
-                const f2 hi = pack_f2(fade.hi, fade.hi), lo = pack_f2(fade.lo, fade.lo);
-#pragma unroll
-                for (int i = 0; i < kFewRows / 2; i++) {
-                    const f2 k = pair(as[s], i);
-#pragma unroll
-                    for (int j = 0; j < 4; j++) X[i][j] = fma2(hi, X[i][j], fma2(k, b2[j], mul2(lo, X[i][j])));
+                        for (int j = 0; j < 4; j++) X[i][j] = 0ull;
                 }
-            } else {
-                const float keep = enter ? 1.0f : fade.g;
-                const f2 m = pack_f2(keep, keep);
+                float b[4];
+                four(bs[s], b);
+                f2 b2[4];
 #pragma unroll
-                for (int i = 0; i < kFewRows / 2; i++) {
-                    const f2 k = pair(as[s], i);
+                for (int j = 0; j < 4; j++) b2[j] = pack_f2(b[j], b[j]);
+                auto pair = [&](const float* from, int i) { return *reinterpret_cast<const f2*>(from + row0 + 2 * i * stride); };
+                if (fade.near && !enter) {
+                    const f2 hi = pack_f2(fade.hi, fade.hi), lo = pack_f2(fade.lo, fade.lo);
 #pragma unroll
-                    for (int j = 0; j < 4; j++) X[i][j] = fma2(m, X[i][j], mul2(k, b2[j]));
-                }
-            }
-            if (Z) {
-                float r[4], z[kFewRows];
-                four(rs[s], r);
+                    for (int i = 0; i < kFewRows / 2; i++) {
+                        const f2 k = pair(as[s], i);
 #pragma unroll
-                for (int i = 0; i < kFewRows / 2; i++) {
-                    f2 sum = mul2(pack_f2(r[0], r[0]), X[i][0]);
+                        for (int j = 0; j < 4; j++) X[i][j] = fma2(hi, X[i][j], fma2(k, b2[j], mul2(lo, X[i][j])));
+                    }
+                } else {
+                    const float keep = enter ? 1.0f : fade.g;
+                    const f2 m = pack_f2(keep, keep);
 #pragma unroll
-                    for (int j = 1; j < 4; j++) sum = fma2(pack_f2(r[j], r[j]), X[i][j], sum);
-                    const float2 v = unpack_f2(sum);
-                    z[2 * i] = v.x, z[2 * i + 1] = v.y;
-                }
-                int which;
-                row_sums(z, which);
-                const int c = row0 + 2 * (which >> 1) * stride + (which & 1);
-                if ((lane & (a.lanes / 8 - 1)) == 0 && c < a.dk) zp[t * a.z.t + c] = from_f32<T>(a.out * z[0]);
-            }
-            if (Y) {
-                f2 y2[4] = {0ull, 0ull, 0ull, 0ull};
+                    for (int i = 0; i < kFewRows / 2; i++) {
+                        const f2 k = pair(as[s], i);
 #pragma unroll
-                for (int i = 0; i < kFewRows / 2; i++) {
-                    const f2 p = pair(ps[s], i);
-#pragma unroll
-                    for (int j = 0; j < 4; j++) y2[j] = fma2(p, X[i][j], y2[j]);
-                }
-                float y[4];
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const float2 v = unpack_f2(y2[j]);
-                    y[j] = v.x + v.y;
-                    for (int m = a.lanes; m < 32; m <<= 1) y[j] += __shfl_xor_sync(0xffffffffu, y[j], m);
-                }
-                if (lane < a.lanes) {
-                    float* sums = part[s & 1][warp];
-                    if (VEC) {
-                        reinterpret_cast<float4*>(sums)[lx] = make_float4(y[0], y[1], y[2], y[3]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; j++) sums[lx + 32 * j] = y[j];
+                        for (int j = 0; j < 4; j++) X[i][j] = fma2(m, X[i][j], mul2(k, b2[j]));
                     }
                 }
-                __syncthreads();
-                if (tid < a.dv && a.y.p) {
-                    float sum = 0.0f;
+                if (clear.value) {      // 0 times it, in the places past the head's edges
 #pragma unroll
-                    for (int w = 0; w < W; w++) sum += part[s & 1][w][tid];
-                    yp[t * a.y.t + tid] = from_f32<T>(a.out * sum);
+                    for (int i = 0; i < kFewRows / 2; i++) {
+                        const int c = row0 + 2 * i * stride;
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            if (c + 1 >= a.dk) X[i][j] &= 0xffffffffull;
+                            if (c >= a.dk || (VEC ? 4 * lx + j : lx + 32 * j) >= a.dv) X[i][j] = 0ull;
+                        }
+                    }
+                }
+                if (Z) {
+                    float r[4], z[kFewRows];
+                    four(rs[s], r);
+#pragma unroll
+                    for (int i = 0; i < kFewRows / 2; i++) {
+                        f2 sum = mul2(pack_f2(r[0], r[0]), X[i][0]);
+#pragma unroll
+                        for (int j = 1; j < 4; j++) sum = fma2(pack_f2(r[j], r[j]), X[i][j], sum);
+                        const float2 v = unpack_f2(sum);
+                        z[2 * i] = v.x, z[2 * i + 1] = v.y;
+                    }
+                    int which;
+                    row_sums(z, which);
+                    const int c = row0 + 2 * (which >> 1) * stride + (which & 1);
+                    if ((lane & (a.lanes / 8 - 1)) == 0 && c < a.dk) zp[t * a.z.t + c] = from_f32<T>(a.out * z[0]);
+                }
+                if (Y) {
+                    f2 y2[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+                    for (int i = 0; i < kFewRows / 2; i++) {
+                        const f2 p = pair(ps[s], i);
+#pragma unroll
+                        for (int j = 0; j < 4; j++) y2[j] = fma2(p, X[i][j], y2[j]);
+                    }
+                    float y[4];
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const float2 v = unpack_f2(y2[j]);
+                        y[j] = v.x + v.y;
+                        for (int m = a.lanes; m < 32; m <<= 1) y[j] += __shfl_xor_sync(0xffffffffu, y[j], m);
+                    }
+                    if (lane < a.lanes) {
+                        float* sums = part[s & 1][warp];
+                        if (VEC) {
+                            reinterpret_cast<float4*>(sums)[lx] = make_float4(y[0], y[1], y[2], y[3]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 4; j++) sums[lx + 32 * j] = y[j];
+                        }
+                    }
+                    __syncthreads();
+                    if (tid < a.dv && a.y.p) {
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int w = 0; w < W; w++) sum += part[s & 1][w][tid];
+                        yp[t * a.y.t + tid] = from_f32<T>(a.out * sum);
+                    }
                 }
             }
-        }
+        };
+        if (RAGGED && stray == p0 + 1) steps(std::true_type());
+        else steps(std::false_type());
     }
     if (!a.last) return;
     const bool zero = a.steps > 0 && (a.rev ? fade.none : done && done[(a.steps - 1) * a.done_t]);
@@ -225,14 +247,15 @@ __global__ void __launch_bounds__(32 * W, 24 / W) memory_few_kernel(const FewPas
     }
 }
 
-template <typename T, int W, bool VEC> cudaError_t few_sums(const FewPass& a, cudaStream_t st) {
+template <typename T, int W, bool VEC, bool RAGGED> cudaError_t few_sums(const FewPass& a, cudaStream_t st) {
     const dim3 grid((unsigned)(a.batch * a.heads)), block(32 * W);
-    if (a.y.p && a.z.p) return launch_pdl(memory_few_kernel<T, W, VEC, true, true>, grid, block, 0, st, a);
-    if (a.z.p) return launch_pdl(memory_few_kernel<T, W, VEC, false, true>, grid, block, 0, st, a);
-    return launch_pdl(memory_few_kernel<T, W, VEC, true, false>, grid, block, 0, st, a);
+    if (a.y.p && a.z.p) return launch_pdl(memory_few_kernel<T, W, VEC, RAGGED, true, true>, grid, block, 0, st, a);
+    if (a.z.p) return launch_pdl(memory_few_kernel<T, W, VEC, RAGGED, false, true>, grid, block, 0, st, a);
+    return launch_pdl(memory_few_kernel<T, W, VEC, RAGGED, true, false>, grid, block, 0, st, a);
 }
 template <typename T, int W> cudaError_t few_of(const FewPass& a, bool vec, cudaStream_t st) {
-    return vec ? few_sums<T, W, true>(a, st) : few_sums<T, W, false>(a, st);
+    const bool full = a.dk == W * (32 / a.lanes) * kFewRows && a.dv == 4 * a.lanes;
+    return !vec ? few_sums<T, W, false, true>(a, st) : full ? few_sums<T, W, true, false>(a, st) : few_sums<T, W, true, true>(a, st);
 }
 template <typename T> cudaError_t few_typed(FewPass a, cudaStream_t st) {
     const bool vec = a.dv % 4 == 0 && aligned(a.first, 16) && aligned(a.last, 16);

@@ -88,3 +88,22 @@ def test_a_head_that_keeps_nothing_keeps_no_infinity(T, dtype):
     assert float(grad[3].abs().max()) == 0.0
     assert not torch.isfinite(grad[1][-1]).any() and not torch.isfinite(grad[2][-1]).any()      # the last step sees it
     assert torch.isfinite(grad[0]).all() and torch.isfinite(grad[1][:-1]).all() and torch.isfinite(grad[2][:-1]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T", [1, 5, 33, 300, 1500])
+@pytest.mark.parametrize("dk,dv", [(40, 24), (33, 17), (1, 100), (100, 1), (5, 8)])
+def test_infinities_beside_the_edge_of_a_head(dk, dv, T, dtype):
+    """Heads that leave places of a block empty: 0 there times an infinite entry of k, v or do is not added to what is there."""
+    q, k, v, ld, s0, _, do, ds_last = made(T, 2, dtype, T + dk, None, dk, dv)
+    v, do = v.abs(), do.abs()      # one sign for all that an infinite key or query enters
+    s0, ds_last = s0.abs(), ds_last.abs()
+    t, (c, d) = T // 2, (dk // 2, dv // 2)
+    bad_v, bad_k = v.clone(), k.clone()
+    bad_v[t, 0, :, d], bad_k[t, 1, :, c] = INF, INF
+    check_all(q, bad_k, bad_v, ld, s0, None, 0.25, got=S().linear_attention(q, bad_k, bad_v, ld, s0, scale=0.25))
+    bad_do, bad_q = do.clone(), q.clone()
+    bad_do[t, 0, :, d], bad_q[t, 1, :, c] = INF, INF
+    grad = S().linear_attention_backward(bad_do, bad_q, k, v, ld, s0, scale=0.25, ds_last=ds_last)
+    S().check()
+    check_all(bad_q, k, v, ld, s0, None, 0.25, bad_do, ds_last, got_grad=grad)

@@ -42,10 +42,9 @@ struct Adjust {
 };
 
 struct Settings {
-    float rep, inverse, freq, pres;
+    float rep, freq, pres;
     __device__ __forceinline__ void read(const Adjust& a, long long row) {
         rep = a.history && a.repetition ? a.repetition[row] : 1.0f;
-        inverse = 1.0f / rep;
         freq = a.history && a.frequency ? a.frequency[row] : 0.0f;
         pres = a.history && a.presence ? a.presence[row] : 0.0f;
     }
@@ -53,7 +52,7 @@ struct Settings {
     __device__ __forceinline__ float changed(uint32_t w, float l, const float* bias) const {
         const uint32_t count = w & 0xfffffu, at = w >> 20;
         if (count) {
-            l *= l > 0.0f ? inverse : rep;
+            l = l > 0.0f ? l / rep : l * rep;      // a product with 1 / rep: one rounding more, and infinite where rep < 2^-128
             l = l - freq * (float)count - pres;
         }
         if (at) l += bias[kMaxBiases - at];

@@ -285,11 +285,8 @@ __global__ void __launch_bounds__(1024) weight_sum_kernel(const float* part, int
     }
 }
 
-// Blocks that sum the weights' gradients: one wave of those that fit
-int blocks_of(long long tokens) {
-    const long long most = 4ll * sm_count(), b = (tokens + kWarps - 1) / kWarps;
-    return (int)(b < 1 ? 1 : b > most ? most : b);
-}
+// Blocks of the backward call at most, each of which leaves sums of the weights' gradients: one wave of those that fit
+int most_blocks() { return 4 * sm_count(); }
 
 // the runs of four of a head start on multiples of four elements
 bool runs(const void* p, long long t, long long h, int es) { return !p || (aligned(p, 4 * es) && t % 4 == 0 && h % 4 == 0); }
@@ -301,7 +298,8 @@ template <typename T, typename W, bool INTER, bool GRAD> cudaError_t launch_pair
     if (p.dim <= 128) return launch_pdl(norm_rotary_kernel<T, W, false, 2, INTER, GRAD>, grid, block, 0, st, p);
     return launch_pdl(norm_rotary_kernel<T, W, false, 4, INTER, GRAD>, grid, block, 0, st, p);
 }
-template <typename T, typename W, bool GRAD> cudaError_t launch_typed(NormRotary p, bool vec, cudaStream_t st) {
+// blocks: how many there are
+template <typename T, typename W, bool GRAD> cudaError_t launch_typed(NormRotary p, bool vec, int& blocks, cudaStream_t st) {
     const int heads = p.q_heads + p.k_heads;
     p.lanes = 32;
     if (vec)
@@ -312,15 +310,15 @@ template <typename T, typename W, bool GRAD> cudaError_t launch_typed(NormRotary
     while (per > 1 && p.tokens * ((turns + per - 1) / per) < 16ll * sm_count()) per = (per + 1) / 2;
     p.share = per * groups;
     p.shares = (turns + per - 1) / per;
-    const long long blocks_all = (p.tokens * p.shares + kWarps - 1) / kWarps;
-    const int blocks = GRAD ? blocks_of(p.tokens) : (int)(blocks_all > 64ll * sm_count() ? 64ll * sm_count() : blocks_all);
+    const long long all = (p.tokens * p.shares + kWarps - 1) / kWarps, most = GRAD ? most_blocks() : 64ll * sm_count();
+    blocks = (int)(all > most ? most : all);
     return p.interleaved ? launch_pairs<T, W, true, GRAD>(p, vec, blocks, st) : launch_pairs<T, W, false, GRAD>(p, vec, blocks, st);
 }
-template <bool GRAD> cudaError_t launch(const NormRotary& p, int dtype, int wdtype, bool vec, cudaStream_t st) {
-    if (dtype == GALA_F32) return launch_typed<float, float, GRAD>(p, vec, st);
+template <bool GRAD> cudaError_t launch(const NormRotary& p, int dtype, int wdtype, bool vec, int& blocks, cudaStream_t st) {
+    if (dtype == GALA_F32) return launch_typed<float, float, GRAD>(p, vec, blocks, st);
     if (dtype == GALA_BF16)
-        return wdtype == GALA_F32 ? launch_typed<__nv_bfloat16, float, GRAD>(p, vec, st) : launch_typed<__nv_bfloat16, __nv_bfloat16, GRAD>(p, vec, st);
-    return wdtype == GALA_F32 ? launch_typed<__half, float, GRAD>(p, vec, st) : launch_typed<__half, __half, GRAD>(p, vec, st);
+        return wdtype == GALA_F32 ? launch_typed<__nv_bfloat16, float, GRAD>(p, vec, blocks, st) : launch_typed<__nv_bfloat16, __nv_bfloat16, GRAD>(p, vec, blocks, st);
+    return wdtype == GALA_F32 ? launch_typed<__half, float, GRAD>(p, vec, blocks, st) : launch_typed<__half, __half, GRAD>(p, vec, blocks, st);
 }
 
 constexpr long long kMaxTokens = 1ll << 31, kMaxStride = 1ll << 32;      // offsets stay below 2^63
@@ -395,12 +393,13 @@ extern "C" int gala_qk_norm_rotary_forward(const gala_qk_norm_rotary_args* q, vo
     NormRotary p = common(a);
     p.q.y = a.q_out, p.q.y_t = a.tokens > 1 ? a.q_out_t : 0, p.q.y_h = a.q_heads > 1 ? a.q_out_h : 0;
     p.k.y = a.k_out, p.k.y_t = a.tokens > 1 ? a.k_out_t : 0, p.k.y_h = a.k_heads > 1 ? a.k_out_h : 0;
-    return launched(launch<false>(p, a.dtype, a.wdtype, vector_ok(p, a.dtype), static_cast<cudaStream_t>(stream)), errbuf, errbuf_len, name);
+    int blocks = 0;
+    return launched(launch<false>(p, a.dtype, a.wdtype, vector_ok(p, a.dtype), blocks, static_cast<cudaStream_t>(stream)), errbuf, errbuf_len, name);
 }
 
 extern "C" long long gala_qk_norm_rotary_workspace(long long tokens, int dim) {
     if (tokens < 0 || dim < 1 || dim > 256) return GALA_EINVAL;
-    return tokens == 0 ? 0 : (long long)blocks_of(tokens) * 2 * dim * 4;
+    return tokens == 0 ? 0 : (long long)most_blocks() * 2 * dim * 4;      // few tokens may have as many shares of heads
 }
 
 extern "C" int gala_qk_norm_rotary_backward(const gala_qk_norm_rotary_grad_args* q, void* stream, char* errbuf, int errbuf_len) {
@@ -436,10 +435,10 @@ extern "C" int gala_qk_norm_rotary_backward(const gala_qk_norm_rotary_grad_args*
             SAY("%s: %lld bytes of workspace are needed, 16-byte aligned", name, gala_qk_norm_rotary_workspace(a.tokens, a.dim));
         p.part = static_cast<float*>(a.workspace);
     }
-    cudaError_t e = launch<true>(p, a.dtype, a.wdtype, vector_ok(p, a.dtype), st);
+    int blocks = 0;
+    cudaError_t e = launch<true>(p, a.dtype, a.wdtype, vector_ok(p, a.dtype), blocks, st);
     if (e == cudaSuccess && sums) {
         const dim3 grid((2 * a.dim + 31) / 32);
-        const int blocks = blocks_of(a.tokens);
         const float* part = p.part;
         if (a.wdtype == GALA_F32) e = launch_pdl(weight_sum_kernel<float>, grid, dim3(1024), 0, st, part, blocks, a.dim, static_cast<float*>(a.grad_q_weight), static_cast<float*>(a.grad_k_weight));
         else if (a.wdtype == GALA_BF16)

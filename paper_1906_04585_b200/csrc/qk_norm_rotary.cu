@@ -5,7 +5,8 @@
 //
 // A group of lanes has a head and each lane four pairs of it, so a pair never leaves a lane, and a token's cosines and sines,
 // which all its heads share, are formed once a warp and stay in registers: the angle in 64 bits as a fraction of a turn, so
-// that position 2^20 is as exact as position 1, then sine and cosine of the fraction in 32.  A warp takes a token (or, where
+// that position 2^20 is as exact as position 1, then sine and cosine of the fraction in 32 (for float32 results put right to first
+// order by what the fraction lost on its way to 32 bits).  A warp takes a token (or, where
 // tokens are few, a share of its heads); the weights stay in registers too.  What a lane loads is two runs of four entries (8
 // or 16 bytes) where head size, number of pairs and alignment allow; otherwise the pairs are dealt out singly over the warp.
 // The weights' gradients are summed by lane over all the tokens of a warp, by block through shared memory, and over the blocks
@@ -112,6 +113,8 @@ template <typename T, bool VEC, int P, bool INTER> __device__ __forceinline__ vo
             if (pl.live[j]) x[pl.at[j]] = from_f32<T>(f[j]);
     }
 }
+// correctly rounded where the result has as many digits
+template <typename T> __device__ __forceinline__ float inverse_root(float x) { return sizeof(T) == 4 ? __frsqrt_rn(x) : rsqrtf(x); }
 __device__ __forceinline__ float group_sum(float s, int lanes) {
     for (int m = lanes / 2; m > 0; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
     return s;
@@ -153,8 +156,14 @@ __global__ void __launch_bounds__(32 * kWarps, GRAD ? 4 : 5) norm_rotary_kernel(
             const double pos = (double)p.positions[token];
 #pragma unroll
             for (int j = 0; j < P; j++) {
-                const double turns = pos * (double)freq[j] * kTurn;
-                sincospif(2.0f * (float)(turns - rint(turns)), &si[j], &co[j]);
+                const double turns = pos * (double)freq[j] * kTurn, part = turns - rint(turns);
+                const float near = (float)part;
+                sincospif(2.0f * near, &si[j], &co[j]);
+                if (sizeof(T) == 4) {      // what the fraction lost in 32 bits; in 16 the result's own rounding hides it
+                    const float lost = (float)((part - (double)near) * (1.0 / kTurn)), c = co[j];
+                    co[j] = fmaf(-lost, si[j], c);
+                    si[j] = fmaf(lost, c, si[j]);
+                }
             }
         }
         // queries, then keys; the heads of a few turns are brought in together
@@ -191,7 +200,7 @@ __global__ void __launch_bounds__(32 * kWarps, GRAD ? 4 : 5) norm_rotary_kernel(
 #pragma unroll
                     for (int j = 0; j < 2 * P; j++) ss = fmaf(x[j], x[j], ss);
                     if (!GRAD) {
-                        const float r = rsqrtf(fmaf(group_sum(ss, p.lanes), inv_dim, p.eps));
+                        const float r = inverse_root<T>(fmaf(group_sum(ss, p.lanes), inv_dim, p.eps));
 #pragma unroll
                         for (int j = 0; j < 2 * P; j++) y[j] = x[j] * r * w[j];
 #pragma unroll
@@ -221,7 +230,7 @@ __global__ void __launch_bounds__(32 * kWarps, GRAD ? 4 : 5) norm_rotary_kernel(
                             ss += __shfl_xor_sync(0xffffffffu, ss, m);
                             dot += __shfl_xor_sync(0xffffffffu, dot, m);
                         }
-                        const float r = rsqrtf(fmaf(ss, inv_dim, p.eps)), back = dot * r * r * inv_dim;
+                        const float r = inverse_root<T>(fmaf(ss, inv_dim, p.eps)), back = dot * r * r * inv_dim;
 #pragma unroll
                         for (int j = 0; j < 2 * P; j++) {
                             y[j] = r * (y[j] - x[j] * back);

@@ -23,7 +23,8 @@
 //
 // float16 has a range that scores and states of ordinary inputs leave.  P, the weighted values and X are scaled by powers of two
 // taken from bounds of their magnitudes (the exact largest of V; dk max|q| max|k|; the sum of what was added to X), and the
-// results scaled back in float32.
+// results scaled back in float32.  One power of two for a chunk is not enough where its steps differ in magnitude by far (an
+// episode that ends beside one of much larger values): such units are flagged too.
 //
 // Roundings: P and X as operands to the element type, since the tensor cores take no other (o is within 2.3e-3 of the 64-bit one in
 // bfloat16, 2.9e-4 in float16; the plain form in bfloat16, 1.7e-3); the state, held and added up in float32, is within 2.4e-6 in
@@ -44,6 +45,10 @@ constexpr int kThreads = 512;
 // only: nine places, two tiles a chunk), and that U only needs the state's warps to have read U of chunk c - 1: they may still have
 // the magnitudes of chunk c before them.  Chunk c + 8 comes in after U of c + 4, which needs U of c + 3 read, and so those of c.
 constexpr int kMaxima = 8;
+// float16: units with a chunk whose steps' magnitudes differ by more, queries times keys or keys times values, are computed step by
+// step.  Scaled by one power of two, the products of the smallest steps are 2^14 / (128 * 2^18) at least, and half a step of
+// float16's smallest numbers, 2^-25, is 2^-14 of that.
+constexpr float kSpread = 0x1p18f;
 
 template <int D> struct Chunk {
     static constexpr int kTile = kSteps * D * 2;              // bytes of a chunk of one operand: D / 64 boxes of 128 rows of 128 bytes
@@ -444,31 +449,40 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                 if (sk >= C::kSlots) sk -= C::kSlots, pk ^= 1u;
             }
         } else if (FP16 && warp == 3) {
-            // the largest magnitudes of K, V and Q
+            // the largest magnitudes of K, V and Q, a lane a step
             int s = 0;
             uint32_t ps = 0;
             bool ok = true;
 #pragma unroll 1
             for (int c = 0; ok && c < chunks; c++) {
+                float spread = 1.0f, keys = 1.0f;      // of the steps' magnitudes: largest over smallest but 0
 #pragma unroll 1
                 for (int kind = 0; kind < kinds; kind++) {
                     if (!warp_wait(&full[s], ps, &abort_flag)) { ok = false; break; }
-                    const uint32_t at = ring + s * C::kTile + lane * 16;
-                    uint32_t lo = 0, hi = 0;
-#pragma unroll 8
-                    for (int i = 0; i < C::kTile; i += 512) {
-                        const uint4 w = ld_shared(at + i);
-                        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+                    uint32_t top = 0, least = 0xffffu;
+#pragma unroll 1
+                    for (int i = lane; i < kSteps; i += 32) {
+                        const uint32_t at = ring + s * C::kTile + i * 128;
+                        __half2 both = __float2half2_rn(0.0f);
 #pragma unroll
-                        for (int j = 0; j < 4; j++) {
-                            lo = max(lo, u[j] & 0x7fffu);
-                            hi = max(hi, u[j] & 0x7fff0000u);
+                        for (int part = 0; part < D / 8; part++) {
+                            const uint4 w = ld_shared(at + (part >> 3) * 16384 + (((part ^ i) & 7) << 4));
+                            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                            for (int j = 0; j < 4; j++) both = __hmax2_nan(both, __habs2(*reinterpret_cast<const __half2*>(&u[j])));
                         }
+                        const uint32_t bits = *reinterpret_cast<const uint32_t*>(&both), lo = max(bits & 0x7fffu, bits >> 16 & 0x7fffu);
+                        top = max(top, lo);
+                        if (lo) least = min(least, lo);
                     }
-                    uint32_t m = __reduce_max_sync(0xffffffffu, max(lo, hi >> 16));
+                    top = __reduce_max_sync(0xffffffffu, top);
+                    least = __reduce_min_sync(0xffffffffu, least);
+                    const float m = __half2float(__ushort_as_half((unsigned short)top)), ratio = top ? m / __half2float(__ushort_as_half((unsigned short)least)) : 1.0f;
+                    if (kind == 0) keys = ratio;
+                    else spread = fmaxf(spread, keys * ratio);
                     if (lane == 0) {
-                        if (m >= 0x7c00u) atomicOr(&found, 1u);
-                        most[c % kMaxima][kind] = __half2float(__ushort_as_half((unsigned short)m));
+                        if (top >= 0x7c00u || spread > kSpread) atomicOr(&found, 1u);
+                        most[c % kMaxima][kind] = m;
                     }
                     if (++s == C::kSlots) s = 0, ps ^= 1u;
                 }

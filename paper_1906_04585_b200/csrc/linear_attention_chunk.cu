@@ -7,13 +7,13 @@
 //   warp 0       brings K, V and Q of the chunks in by tensor copies, a ring of tiles
 //   warp 1       issues the products scores = Q K^T, O2 = Q X and O1 = P V with P in tensor memory
 //   warp 2       issues U = K^T (w V), so that neither waits for what the other waits for (a thread issues a product every 70
-//                cycles, a chunk of 128 x 128 heads is 40 of them)
+//                cycles, a chunk of 128 x 128 heads is 48 of them, 40 in float16)
 //   warp 3       float16: the largest magnitudes of the chunk's operands, from which powers of two are taken (below)
 //   warps 4-7    a thread a row: scores -> P, rounded to the element type, in the place of the scores; half of the chunk's o
 //   warps 8-11   X in registers, folded with U and rounded as the operand of the next chunk's O2; half of the chunk's o
-//   warps 12-15  w V, a chunk ahead of the others, as two numbers of the element type, rounded and rest: X is a float32
-//                result, of which one number would leave 2^-9 (and where X only adds to o, one instead of two saves 2 % of the
-//                time)
+//   warps 12-15  w V, a chunk ahead of the others, as three numbers of bfloat16 or two of float16, rounded and rests: X is a
+//                float32 result, of which one bfloat16 would leave 2^-9 and two 2^-17 (two instead of three: 16384 steps x 16 heads
+//                forward 105 instead of 120 us, 2048 steps x 8 x 16 heads with gradients 316 instead of 329)
 // The powers of g are differences of exponents, never quotients, so nothing overflows however fast a head fades.
 //
 // What a product cannot do is leave out a term: 0 times an infinity or a NaN spreads it to steps that must not see it, and an
@@ -27,8 +27,7 @@
 // episode that ends beside one of much larger values): such units are flagged too.
 //
 // Roundings: P and X as operands to the element type, since the tensor cores take no other (o is within 2.3e-3 of the 64-bit one in
-// bfloat16, 2.9e-4 in float16; the plain form in bfloat16, 1.7e-3); the state, held and added up in float32, is within 2.4e-6 in
-// bfloat16, the rest that two pieces of a weighted value leave.
+// bfloat16, 2.9e-4 in float16; the plain form in bfloat16, 1.7e-3); the state is held and added up in float32.
 //
 // Measured on a B200: 2048 steps x 8 x 16 heads of 128 x 128 bfloat16, 75-80 us a pass of 268 MB (3.4-3.6 TB/s of operands and
 // outputs), with 3-5 us for the kernel that follows; 16384 steps x 16 heads in 9 pieces, 115 us.  Bound by the chain of a chunk
@@ -50,14 +49,16 @@ constexpr int kMaxima = 8;
 // float16's smallest numbers, 2^-25, is 2^-14 of that.
 constexpr float kSpread = 0x1p18f;
 
-template <int D> struct Chunk {
+template <int D, bool FP16> struct Chunk {
     static constexpr int kTile = kSteps * D * 2;              // bytes of a chunk of one operand: D / 64 boxes of 128 rows of 128 bytes
     static constexpr int kSlots = D == 128 ? 5 : 9;
-    static constexpr int kRows = D == 128 ? 32 : 64;          // steps of V that are weighted at once
+    static constexpr int kPieces = FP16 ? 2 : 3;              // of a weighted value
+    static constexpr int kRows = D == 64 ? 64 : FP16 ? 32 : 16;      // steps of V that are weighted at once
     static constexpr int kSub = kSteps / kRows;
-    static constexpr int kHalf = kRows * D * 2;               // bytes of their rounded values, and of the rests
+    static constexpr int kPiece = kRows * D * 2;              // bytes of one piece of them
     static constexpr int kState = D * D * 2;
-    static constexpr int kBytes = kSlots * kTile + 4 * kHalf + kState;
+    static constexpr int kWeighted = 2 * kPieces * kPiece > D * D * 4 - kState ? 2 * kPieces * kPiece : D * D * 4 - kState;      // a float32 state leaves through it and X's operand
+    static constexpr int kBytes = kSlots * kTile + kWeighted + kState;
     static constexpr uint32_t kU = 128, kO1 = 128 + D, kO2 = 128 + 2 * D, kColumns = 512;      // tensor memory; scores and P at 0
     static constexpr int kHeld = D == 128 ? 128 : 32;         // columns of X a thread holds
 };
@@ -226,14 +227,14 @@ __device__ __forceinline__ void write_o(uint32_t own_at, uint32_t given_at, int 
 
 template <int D, bool FP16, bool REV>
 __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_constant__ ChunkMaps maps, const MemoryPass a, const Broadcast cast, const int wide) {
-    using C = Chunk<D>;
+    using C = Chunk<D, FP16>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t full[C::kSlots], empty[C::kSlots], hl_ready[2], hl_free[2], scores_full, p_ready, o_full, o_free, u_full, u_free, x_ready, x_taken, max_ready[kMaxima], o_stored[4];
     __shared__ uint32_t tmem_slot, found;
     __shared__ int abort_flag, issued;
     __shared__ float pw[132], most[kMaxima][3], first_most[4], x_backs[2];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const uint32_t ring = smem_u32(smem), hl = ring + C::kSlots * C::kTile, sx = hl + 4 * C::kHalf;
+    const uint32_t ring = smem_u32(smem), hl = ring + C::kSlots * C::kTile, sx = hl + C::kWeighted;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const long long units = a.batch * a.heads;
     const long long unit = blockIdx.x % units;
@@ -424,11 +425,11 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                     const int b = s & 1;
                     if (!warp_wait(&hl_ready[b], (uint32_t)((c * C::kSub + s) >> 1) & 1u, &abort_flag)) break;
                     if (elected()) {
-                        const uint64_t kd = d_cols + (uint64_t)(sk * (C::kTile / 16) + s * (C::kRows * 128 / 16)), hd = d_hl + (uint64_t)(2 * b * (C::kHalf / 16));
+                        const uint64_t kd = d_cols + (uint64_t)(sk * (C::kTile / 16) + s * (C::kRows * 128 / 16)), hd = d_hl + (uint64_t)(C::kPieces * b * (C::kPiece / 16));
 #pragma unroll
-                        for (int m = 0; m < 2 * C::kRows / 16; m++) {      // the rounded values, then the rests
+                        for (int m = 0; m < C::kPieces * C::kRows / 16; m++) {
                             const int part = m / (C::kRows / 16), kk = m % (C::kRows / 16);
-                            umma_bf16(tmem + C::kU, kd + kk * (2048 / 16), hd + (part * (C::kHalf / 16) + kk * (2048 / 16)), id_u, m > 0 ? 1u : s > 0);
+                            umma_bf16(tmem + C::kU, kd + kk * (2048 / 16), hd + (part * (C::kPiece / 16) + kk * (2048 / 16)), id_u, m > 0 ? 1u : s > 0);
                         }
                         umma_commit(&hl_free[b]);
                     }
@@ -809,32 +810,40 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
 #pragma unroll 1
             for (int s = 0; s < C::kSub; s++, sub++) {
                 const int b = sub & 1;
-                uint4 w[4];
-                float g[4];
+                constexpr int kParts = C::kPiece / 2048;      // of 16 bytes, a thread
+                uint4 w[kParts];
+                float g[kParts];
 #pragma unroll
-                for (int m = 0; m < 4; m++) {      // 16-byte parts of the rows, box after box
+                for (int m = 0; m < kParts; m++) {      // box after box
                     const int box = m * 128 / (C::kRows * 8), in = (m * 128) % (C::kRows * 8) / 8;
                     w[m] = ld_shared(v + box * 16384 + s * C::kRows * 128 + in * 128);
                     const int j = s * C::kRows + in + (tid >> 3);
                     g[m] = j >= lo && j <= hi ? pw[REV ? j : len - 1 - j] * gain : 0.0f;
                 }
-                if (!warp_wait(&hl_free[b], (((uint32_t)sub >> 1) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
-                const uint32_t to = hl + 2 * b * C::kHalf + tid * 16;
+                uint32_t r[kParts][C::kPieces][4];
 #pragma unroll
-                for (int m = 0; m < 4; m++) {
+                for (int m = 0; m < kParts; m++) {
                     const uint32_t u[4] = {w[m].x, w[m].y, w[m].z, w[m].w};
-                    uint32_t r[4], d[4];
 #pragma unroll
                     for (int e = 0; e < 4; e++) {
                         seen = note<FP16>(u[e], seen);
                         const float2 x = unpack<FP16>(u[e]);
-                        r[e] = pack<FP16>(x.x * g[m], x.y * g[m]);
-                        const float2 y = unpack<FP16>(r[e]);
-                        d[e] = pack<FP16>(fmaf(x.x, g[m], -y.x), fmaf(x.y, g[m], -y.y));
+                        r[m][0][e] = pack<FP16>(x.x * g[m], x.y * g[m]);
+                        float2 y = unpack<FP16>(r[m][0][e]);
+                        float2 rest = make_float2(fmaf(x.x, g[m], -y.x), fmaf(x.y, g[m], -y.y));
+                        r[m][1][e] = pack<FP16>(rest.x, rest.y);
+                        if constexpr (C::kPieces > 2) {
+                            y = unpack<FP16>(r[m][1][e]);
+                            r[m][2][e] = pack<FP16>(rest.x - y.x, rest.y - y.y);
+                        }
                     }
-                    st_shared(to + m * 2048, make_uint4(r[0], r[1], r[2], r[3]));
-                    st_shared(to + C::kHalf + m * 2048, make_uint4(d[0], d[1], d[2], d[3]));
                 }
+                if (!warp_wait(&hl_free[b], (((uint32_t)sub >> 1) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
+                const uint32_t to = hl + C::kPieces * b * C::kPiece + tid * 16;
+#pragma unroll
+                for (int m = 0; m < kParts; m++)
+#pragma unroll
+                    for (int i = 0; i < C::kPieces; i++) st_shared(to + i * C::kPiece + m * 2048, make_uint4(r[m][i][0], r[m][i][1], r[m][i][2], r[m][i][3]));
                 proxy_fence();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&hl_ready[b]);
@@ -879,7 +888,7 @@ bool map_of(CUtensorMap* m, const MemoryOperand& o, long long steps, long long b
 }
 
 template <int D, bool FP16, bool REV> cudaError_t launch_chunks(const ChunkMaps& maps, const MemoryPass& a, const Broadcast& cast, int wide, cudaStream_t st) {
-    constexpr int smem = Chunk<D>::kBytes + 1024;
+    constexpr int smem = Chunk<D, FP16>::kBytes + 1024;
     static bool ready[64] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);

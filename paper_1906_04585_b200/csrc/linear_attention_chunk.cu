@@ -12,14 +12,14 @@
 //   warps 4-7    a thread a row: scores -> P, rounded to the element type, in the place of the scores; half of the chunk's o
 //   warps 8-11   X in registers, folded with U and rounded as the operand of the next chunk's O2; half of the chunk's o
 //   warps 12-15  w V, a chunk ahead of the others, as three numbers of bfloat16 or two of float16, rounded and rests: X is a
-//                float32 result, of which one bfloat16 would leave 2^-9 and two 2^-17 (two instead of three: 16384 steps x 16 heads
-//                forward 105 instead of 120 us, 2048 steps x 8 x 16 heads with gradients 316 instead of 329)
+//                float32 result, of which one bfloat16 would leave 2^-9 and two 2^-17 (two, 16384 steps x 16 heads forward: 105
+//                instead of 118 us; 2048 steps x 8 x 16 heads with gradients: 313 instead of 320)
 // The powers of g are differences of exponents, never quotients, so nothing overflows however fast a head fades.
 //
 // What a product cannot do is leave out a term: 0 times an infinity or a NaN spreads it to steps that must not see it, and an
-// infinite query makes scores of both signs where the state may have one.  A unit whose Q, V or U holds one is flagged and
-// computed again step by step by a kernel that follows (its blocks end at once where no flag is set); nothing that the call reads
-// is overwritten before.
+// infinite query makes scores of both signs where the state may have one.  A unit whose Q or U holds one (an infinite entry of V
+// leaves nothing finite in its column of U and of X, whatever its weight) is flagged and computed again step by step by a kernel
+// that follows (its blocks end at once where no flag is set); nothing that the call reads is overwritten before.
 //
 // float16 has a range that scores and states of ordinary inputs leave.  P, the weighted values and X are scaled by powers of two
 // taken from bounds of their magnitudes (the exact largest of V; dk max|q| max|k|; the sum of what was added to X), and the
@@ -109,16 +109,6 @@ template <bool FP16> __device__ __forceinline__ uint32_t pack(float a, float b) 
 template <bool FP16> __device__ __forceinline__ float2 unpack(uint32_t w) {
     if (!FP16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
     return __half22float2(*reinterpret_cast<const __half2*>(&w));
-}
-// NaN once any of the numbers seen is infinite or NaN
-template <bool FP16> __device__ __forceinline__ uint32_t note(uint32_t w, uint32_t seen) {
-    if (FP16) {
-        const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&w), __half2half2(__ushort_as_half(0)), *reinterpret_cast<const __half2*>(&seen));
-        return *reinterpret_cast<const uint32_t*>(&r);
-    }
-    const __nv_bfloat162 z = __float2bfloat162_rn(0.0f);
-    const __nv_bfloat162 r = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&w), z, *reinterpret_cast<const __nv_bfloat162*>(&seen));
-    return *reinterpret_cast<const uint32_t*>(&r);
 }
 // 2^e with which numbers up to `most` stay below 2^15, and 2^-e
 __device__ __forceinline__ float fit(float most, float& back) {
@@ -733,7 +723,7 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
             put_o(c, 0, rows, t0, len, reached, e, p_back);
         }
         look();
-        asm volatile("bar.sync 2, 256;" ::: "memory");      // warps 12-15 have seen all of V
+        asm volatile("bar.sync 3, 128;" ::: "memory");
         const bool flagged = *static_cast<volatile uint32_t*>(&found) != 0;
         if (outputs && tid == 0) a.flags[(long long)piece * units + unit] = flagged;
         float* to = nullptr;
@@ -788,7 +778,6 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
         const int tid = threadIdx.x - 384;
         uint32_t f[4];
         flags_of(0, f);
-        uint32_t seen = 0;
         int sub = 0, sv = 1;
         uint32_t pv = 0;
 #pragma unroll 1
@@ -826,15 +815,14 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                     const uint32_t u[4] = {w[m].x, w[m].y, w[m].z, w[m].w};
 #pragma unroll
                     for (int e = 0; e < 4; e++) {
-                        seen = note<FP16>(u[e], seen);
                         const float2 x = unpack<FP16>(u[e]);
-                        r[m][0][e] = pack<FP16>(x.x * g[m], x.y * g[m]);
-                        float2 y = unpack<FP16>(r[m][0][e]);
-                        float2 rest = make_float2(fmaf(x.x, g[m], -y.x), fmaf(x.y, g[m], -y.y));
-                        r[m][1][e] = pack<FP16>(rest.x, rest.y);
-                        if constexpr (C::kPieces > 2) {
-                            y = unpack<FP16>(r[m][1][e]);
-                            r[m][2][e] = pack<FP16>(rest.x - y.x, rest.y - y.y);
+                        f2 rest = mul2(pack_f2(x.x, x.y), pack_f2(g[m], g[m]));
+#pragma unroll
+                        for (int i = 0; i < C::kPieces; i++) {
+                            const float2 v = unpack_f2(rest);
+                            r[m][i][e] = pack<FP16>(v.x, v.y);
+                            const float2 y = unpack<FP16>(r[m][i][e]);
+                            if (i + 1 < C::kPieces) rest = fma2(pack_f2(y.x, y.y), pack_f2(-1.0f, -1.0f), rest);
                         }
                     }
                 }
@@ -852,9 +840,6 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
             sv += kinds;
             if (sv >= C::kSlots) sv -= C::kSlots, pv ^= 1u;
         }
-        const float2 y = unpack<FP16>(seen);
-        if (!(y.x == 0.0f && y.y == 0.0f)) atomicOr(&found, 1u);
-        asm volatile("bar.sync 2, 256;" ::: "memory");
     }
     if (warp >= 4 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     tcgen05_fence_before();

@@ -276,7 +276,14 @@ int step_pieces(long long steps, long long units) {
     return p < 2 ? 1 : p > 1024 ? 1024 : (int)p;
 }
 
-// Most steps of a call whose state passes through a block once.
+// Most steps of a call whose state passes through a block once.  Measured on a B200, forward / with gradients, us, one passage
+// against the other ways (chunks; float32: step by step) at 16, 32, 48 and 64 steps:
+//   1024 x 8 heads of 64 bfloat16     201 369 540 710 against 385 390 392 394     647 1218 1807 2359 against 1548 1566 1575 1585
+//   32 x 16 heads of 128 bfloat16     56 101 147 197 against 44 45 46 47          200 362 526 691 against 183 188 191 196
+//   64 x 16 heads of 128 float16      110 191 272 352 against 92 93 95 95         363 649 933 1218 against 362 367 372 376
+//   256 x 8 heads of 64 float32       59 111 160 208 against 47 73 105 129        192 352 516 672 against 219 317 447 542
+// So 32 is where heads of 64 meet; heads of 128 would be done sooner by chunks from some 14 steps on, at the price of scores and a
+// state rounded to 16 bits, which a rollout's outputs are spared this way.
 constexpr long long kFewSteps = 32;
 
 struct Space { long long z, gain, flags, bytes; };      // offsets into the workspace

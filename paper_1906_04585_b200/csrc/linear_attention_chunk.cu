@@ -59,6 +59,9 @@ template <int D, bool FP16> struct Chunk {
     static constexpr int kState = D * D * 2;
     static constexpr int kWeighted = 2 * kPieces * kPiece > D * D * 4 - kState ? 2 * kPieces * kPiece : D * D * 4 - kState;      // a float32 state leaves through it and X's operand
     static constexpr int kBytes = kSlots * kTile + kWeighted + kState;
+    // Places of weighted values: two, or 2^kPlaces without outputs, where X's operand takes none of the memory (two there as well:
+    // 131 us instead of 124 for 16384 steps x 16 heads of 128, other inputs every pass).
+    static constexpr int kPlaces = kWeighted + kState >= 4 * kPieces * kPiece ? 2 : 1;
     static constexpr uint32_t kU = 128, kO1 = 128 + D, kO2 = 128 + 2 * D, kColumns = 512;      // tensor memory; scores and P at 0
     static constexpr int kHeld = D == 128 ? 128 : 32;         // columns of X a thread holds
 };
@@ -219,7 +222,7 @@ template <int D, bool FP16, bool REV>
 __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_constant__ ChunkMaps maps, const MemoryPass a, const Broadcast cast, const int wide) {
     using C = Chunk<D, FP16>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t full[C::kSlots], empty[C::kSlots], hl_ready[2], hl_free[2], scores_full, p_ready, o_full, o_free, u_full, u_free, x_ready, x_taken, max_ready[kMaxima], o_stored[4];
+    __shared__ __align__(8) uint64_t full[C::kSlots], empty[C::kSlots], hl_ready[4], hl_free[4], scores_full, p_ready, o_full, o_free, u_full, u_free, x_ready, x_taken, max_ready[kMaxima], o_stored[4];
     __shared__ uint32_t tmem_slot, found;
     __shared__ int abort_flag, issued;
     __shared__ float pw[132], most[kMaxima][3], first_most[4], x_backs[2];
@@ -234,10 +237,11 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
     const int c0 = piece * per, chunks = min(all, c0 + per) - c0;
     const bool outputs = !a.states_only;
     const int kinds = outputs ? 3 : 2;      // tiles of a chunk: K, V, Q
+    const int places = outputs ? 1 : C::kPlaces;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kSlots; s++) { mbar_init(&full[s], 1); mbar_init(&empty[s], 2); }
-        for (int b = 0; b < 2; b++) { mbar_init(&hl_ready[b], 4); mbar_init(&hl_free[b], 1); }
+        for (int b = 0; b < 4; b++) { mbar_init(&hl_ready[b], 4); mbar_init(&hl_free[b], 1); }
         for (int b = 0; b < kMaxima; b++) mbar_init(&max_ready[b], 1);
         for (int b = 0; b < 4; b++) mbar_init(&o_stored[b], 8);
         mbar_init(&scores_full, 1);
@@ -412,8 +416,8 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                 int s = 0;
 #pragma unroll 1
                 for (; s < C::kSub; s++) {
-                    const int b = s & 1;
-                    if (!warp_wait(&hl_ready[b], (uint32_t)((c * C::kSub + s) >> 1) & 1u, &abort_flag)) break;
+                    const int sub = c * C::kSub + s, b = sub & ((1 << places) - 1);
+                    if (!warp_wait(&hl_ready[b], (uint32_t)(sub >> places) & 1u, &abort_flag)) break;
                     if (elected()) {
                         const uint64_t kd = d_cols + (uint64_t)(sk * (C::kTile / 16) + s * (C::kRows * 128 / 16)), hd = d_hl + (uint64_t)(C::kPieces * b * (C::kPiece / 16));
 #pragma unroll
@@ -798,7 +802,7 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
             bool ok = true;
 #pragma unroll 1
             for (int s = 0; s < C::kSub; s++, sub++) {
-                const int b = sub & 1;
+                const int b = sub & ((1 << places) - 1);
                 constexpr int kParts = C::kPiece / 2048;      // of 16 bytes, a thread
                 uint4 w[kParts];
                 float g[kParts];
@@ -826,7 +830,7 @@ __global__ void __launch_bounds__(kThreads, 1) memory_chunk_kernel(const __grid_
                         }
                     }
                 }
-                if (!warp_wait(&hl_free[b], (((uint32_t)sub >> 1) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
+                if (!warp_wait(&hl_free[b], (((uint32_t)sub >> places) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
                 const uint32_t to = hl + C::kPieces * b * C::kPiece + tid * 16;
 #pragma unroll
                 for (int m = 0; m < kParts; m++)

@@ -7,7 +7,7 @@
 // is held or comes in is so large that an infinity may arise, the 32 steps take Fade's form, one instruction more (throughout, it
 // made 777 steps x 3 x 5 heads of 41 x 72 266-272 us in place of 242).
 // Where units are few the time axis is cut into pieces of whole batches: one launch leaves their own states, one joins them, one
-// computes the outputs.  Measured on a B200: 777 steps x 3 x 5 heads of 41 x 72 float32, 25 pieces, 21 + 7 + 26 us a pass;
+// computes the outputs.  Measured on a B200: 777 steps x 3 x 5 heads of 41 x 72 float32, 25 pieces, 24 + 7 + 30 us a pass (cold);
 // the floor of all four passes is 4.4 us, so launches, starts and the order of the steps bound it.
 #include "linear_attention.cuh"
 

@@ -12,8 +12,8 @@
 //   warps 4-7    a thread a row: scores -> P, rounded to the element type, in the place of the scores; half of the chunk's o
 //   warps 8-11   X in registers, folded with U and rounded as the operand of the next chunk's O2; half of the chunk's o
 //   warps 12-15  w V, a chunk ahead of the others, as three numbers of bfloat16 or two of float16, rounded and rests: X is a
-//                float32 result, of which one bfloat16 would leave 2^-9 and two 2^-17 (two, 16384 steps x 16 heads forward: 105
-//                instead of 118 us; 2048 steps x 8 x 16 heads with gradients: 313 instead of 320)
+//                float32 result, of which one bfloat16 would leave 2^-9 and two 2^-17 (two, with the same inputs every pass, 16384
+//                steps x 16 heads forward: 105 instead of 117 us; 2048 steps x 8 x 16 heads with gradients: 313 instead of 320)
 // The powers of g are differences of exponents, never quotients, so nothing overflows however fast a head fades.
 //
 // What a product cannot do is leave out a term: 0 times an infinity or a NaN spreads it to steps that must not see it, and an
@@ -29,9 +29,9 @@
 // Roundings: P and X as operands to the element type, since the tensor cores take no other (o is within 2.3e-3 of the 64-bit one in
 // bfloat16, 2.9e-4 in float16; the plain form in bfloat16, 1.7e-3); the state is held and added up in float32.
 //
-// Measured on a B200: 2048 steps x 8 x 16 heads of 128 x 128 bfloat16, 75-80 us a pass of 268 MB (3.4-3.6 TB/s of operands and
-// outputs), with 3-5 us for the kernel that follows; 16384 steps x 16 heads in 9 pieces, 115 us.  Bound by the chain of a chunk
-// (scores, mask, weighted sum: 5500-5900 cycles, 9200 in an early form) and by some 15 us a kernel for its start and the last state.
+// Measured on a B200: 2048 steps x 8 x 16 heads of 128 x 128 bfloat16, 79-82 us a pass of 268 MB (3.3-3.4 TB/s of operands and
+// outputs), with 3-6 us for the kernel that follows; 16384 steps x 16 heads in 9 pieces, 124-130 us; float16 143 us.  Bound by the chain of a
+// chunk (scores, mask, weighted sum: some 5500-5900 cycles) and by some 15 us a kernel for its start and the last state.
 #include "linear_attention.cuh"
 #include "tcgen05.cuh"
 

@@ -3,8 +3,9 @@
 // The state of a sequence and head passes through the registers of a block once, 16 bytes of a row a thread, and the kernel is
 // bound by its way from and to memory.  Sums over rows are joined across the block's warps, sums over columns inside a warp, so
 // that one passage gives o, or dq, or dk and dv together.  The update of the state is that of linear_attention.cu.
-// Measured on a B200, 8192 units of 64 x 64: one step 51 us (5.3 TB/s); five steps (cold) 92 us forward, 83 us for dq, 117 us for dk and
-// dv.  Sixteen rows a thread instead of eight: 310 instead of 293 us for the three.
+// Measured on a B200, 8192 units of 64 x 64: one step 51 us (5.3 TB/s); five steps (cold) 94 us forward, 82 us for dq, 106 us for dk and
+// dv, 283 us for the three.  Bound by the steps one after another: each updates every entry and sums over lanes, and o crosses the
+// block with a barrier; the state's way takes 44, 24 and 48 us.  Sixteen rows a thread instead of eight: 6 % longer.
 #include "linear_attention.cuh"
 
 namespace gala {
